@@ -148,6 +148,102 @@ adt_status adt_kv_compact(void* k_cache, void* v_cache, int32_t B, int32_t slice
                           int64_t stride_slice, const int32_t* kv_len, const int32_t* path, int32_t path_stride,
                           const int32_t* n_acc, int32_t a_max, int32_t dtype, void* stream);
 
+/* ------------------------------------------------------------------ rotary positions
+ * Rotary positions of a batch of rows with positions of their own (a tree's rows share positions
+ * by depth; in a cache that lost slots to adt_kv_evict a row's slot says nothing about its
+ * position), for query heads over fewer key-value heads as well, and the append of the rows'
+ * keys and values.  Pair i of a head's first rot_dim dims is (x[i], x[i + rot_dim / 2]) in the
+ * half layout and (x[2i], x[2i + 1]) in the interleaved one; it becomes
+ *   gain * (x0 cos t - x1 sin t, x0 sin t + x1 cos t),  t = pos * freq[i];
+ * the dims from rot_dim on stay as they are.
+ *
+ * adt_rope_freqs (host only) fills freq [rot_dim / 2] and gain for a context scaling:
+ *   PLAIN   freq[i] = theta^(-2 i / rot_dim)
+ *   LINEAR  positions divided by factor: the plain frequencies over factor
+ *   BASE    theta stretched to theta * factor^(rot_dim / (rot_dim - 2)): the highest frequency
+ *           stays and the lowest is divided by factor (rot_dim = 2: plain)
+ *   RAMP    frequencies that turn more than `fast` times within orig_len positions stay, those
+ *           that turn less than `slow` times are divided by factor, and between them the share
+ *           t = (i - lo) / (hi - lo) of the division grows with i, where lo and hi are the
+ *           indices rot_dim ln(orig_len / (2 pi turns)) / (2 ln theta) of `fast`, rounded down,
+ *           and of `slow`, rounded up, held within [0, rot_dim - 1]; gain = 0.1 ln(factor) + 1.
+ * gain is 1 for the others.  ADT_E_ARG: null pointers, theta <= 1, factor < 1, for RAMP
+ * orig_len < 1 or not fast > slow > 0; ADT_E_SHAPE: rot_dim odd or outside [2, 256]. */
+#define ADT_ROPE_HALF 0
+#define ADT_ROPE_INTERLEAVED 1
+#define ADT_ROPE_PLAIN 0
+#define ADT_ROPE_LINEAR 1
+#define ADT_ROPE_BASE 2
+#define ADT_ROPE_RAMP 3
+typedef struct {
+  int32_t rot_dim;
+  int32_t scaling;              /* ADT_ROPE_PLAIN .. ADT_ROPE_RAMP */
+  double theta;
+  double factor;                /* ignored by PLAIN */
+  int32_t orig_len;             /* RAMP: the context length the frequencies were trained for */
+  double fast, slow;            /* RAMP: turns */
+} adt_rope_cfg;
+adt_status adt_rope_freqs(const adt_rope_cfg* cfg /*[host]*/, double* freq /*[host]*/, float* gain /*[host]*/);
+
+/* q [B][n_max][H][Dh], k and v [B][n_max][Hkv][Dh] in dtype, consecutive rows ldq, ldk, ldv
+ * elements apart (at least H * Dh and Hkv * Dh: the three may be parts of one projection's
+ * output rows).  q_out: [B][n_max][H][Dh] contiguous; may be q itself if ldq = H * Dh.
+ * pos: [B][n_max] int32 (any value).  Row i < n_rows[b] of sequence b is rotated into q_out and
+ * its rotated key and its value go to slot kv_len[b] + i, element (b, h, slot, :) of a cache at
+ * b * stride_b + h * stride_h + slot * Dh; other rows and slots stay as they are, and so does a
+ * slot that would lie at or past kv_cap (debug builds record it).  freq: device [rot_dim / 2]
+ * doubles (angles are reduced in double, so far positions keep theirs).  n_max may be any
+ * number of rows.  Dh even, at most 256; rot_dim even, in [2, Dh]. */
+adt_status adt_rope_append(const void* q, const void* k, const void* v, int64_t ldq, int64_t ldk, int64_t ldv,
+                           const int32_t* pos, const int32_t* kv_len, const int32_t* n_rows, const double* freq,
+                           float gain, int32_t rot_dim, int32_t layout, int32_t B, int32_t n_max, int32_t H,
+                           int32_t Hkv, int32_t Dh, void* q_out, void* k_cache, void* v_cache, int64_t stride_b,
+                           int64_t stride_h, int32_t kv_cap, int32_t dtype, void* stream);
+
+/* ------------------------------------------------------------------ attention over chosen blocks
+ * The prefix of a long cache in blocks of `block` slots (32, 64 or 128): block j holds slots
+ * [j * block, min((j + 1) * block, kv_len)).  A query row scores the blocks by their mean keys
+ * and attends to the best of them only.
+ *
+ * adt_block_keys writes the mean keys, in fp32: means element (b, h, j, :) at b * stride_mb +
+ * h * stride_mh + j * Dh, for every block from start[b] / block (start NULL: from 0) to the last
+ * one of the prefix; other rows of means stay as they are.  After an append or a compaction that
+ * left the first n slots as they were, start = n suffices.  kv_len: [B] device, at most kv_cap
+ * (debug builds record more); start: [B] device.  k_cache as in adt_tree_attn, with Hkv heads;
+ * k_cache and means 16-byte aligned, strides multiples of 16 bytes; Dh 64 or 128. */
+adt_status adt_block_keys(const void* k_cache, int64_t stride_b, int64_t stride_h, const int32_t* start,
+                          const int32_t* kv_len, int32_t B, int32_t Hkv, int32_t Dh, int32_t block, int32_t kv_cap,
+                          float* means, int64_t stride_mb, int64_t stride_mh, int32_t dtype, void* stream);
+
+/* ------------------------------------------------------------------ eviction
+ * Bounds a cache by what its slots are worth: of the kv_len[b] slots of sequence b's prefix, each
+ * slice keeps the first n_first, the last n_last, and between them those of the largest weights
+ * (ties: the lower slot; NaN ranks below every number), `budget` slots in all, or every slot
+ * where kv_len[b] <= budget.  The kept slots' rows of both caches and their weights move to slots
+ * 0, 1, ... in their order; the slots behind them stay as they are.
+ *   weights element (b, s, slot) at b * stride_wb + s * stride_ws + slot, fp32
+ *   k_out, v_out, weights_out: the destination, with strides of its own; the source itself (each
+ *     with the source's strides) for an eviction in place, else memory apart from it
+ *   kept:    [B][slices][budget] out, the kept slots in order (entries past the new length stay)
+ *   new_len: [B] out, min(kv_len[b], budget); may be kv_len itself
+ * kv_len: device, at most kv_cap (debug builds record more; the excess is not seen).  A slice is a
+ * (layer, head) as in adt_kv_compact.  Rows keep the rotation of the positions they had.
+ * budget >= 1, n_first + n_last <= budget (ADT_E_ARG); rows of Dh elements whole 16-byte pieces,
+ * at most 16 KB; caches 16-byte aligned, their strides multiples of 16 bytes (ADT_E_SHAPE). */
+adt_status adt_kv_evict(const void* k_cache, const void* v_cache, const float* weights, int64_t stride_b,
+                        int64_t stride_slice, int64_t stride_wb, int64_t stride_ws, const int32_t* kv_len, int32_t B,
+                        int32_t slices, int32_t Dh, int32_t kv_cap, int32_t budget, int32_t n_first, int32_t n_last,
+                        void* k_out, void* v_out, float* weights_out, int64_t out_stride_b, int64_t out_stride_slice,
+                        int64_t out_stride_wb, int64_t out_stride_ws, int32_t* kept, int32_t* new_len, int32_t dtype,
+                        void* stream);
+
+/* The weights of an accepted path, as adt_kv_compact moves its keys and values: in every slice,
+ * slot kv_len[b] + m <- slot kv_len[b] + path[b][m] for m = 1..n_acc[b].  Arguments as there
+ * (slots at or past kv_cap are left alone). */
+adt_status adt_weights_compact(float* weights, int32_t B, int32_t slices, int64_t stride_wb, int64_t stride_ws,
+                               const int32_t* kv_len, int32_t kv_cap, const int32_t* path, int32_t path_stride,
+                               const int32_t* n_acc, int32_t a_max, void* stream);
+
 /* ------------------------------------------------------------------ c1-c3: acceptance
  * Walk from the root of one verified tree (Sec. 3.1 Eq. 1; Sec. 5.1).
  *  GREEDY: t_u = argmax of logits row u over its allowed ids (lowest id on ties); move to

@@ -24,6 +24,8 @@ ALPHA_REAL, ALPHA_POISSON = 0, 1
 INIT_HORIZONTAL, INIT_VERTICAL, INIT_RANDOM, INIT_TOKENFLOCK = 0, 1, 2, 3
 KCLAMP_ALWAYS, KCLAMP_DEEP = 0, 1
 MAX_WIDTH = 16
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP = 0, 1, 2, 3
 
 p = C.c_void_p
 i32 = C.c_int32
@@ -31,6 +33,7 @@ i64 = C.c_int64
 u64 = C.c_uint64
 f32 = C.c_float
 sz = C.c_size_t
+f64 = C.c_double
 ip = C.POINTER(C.c_int32)
 
 
@@ -84,6 +87,11 @@ class CaptureRec(C.Structure):
                 ("snapshots", i32), ("resid_off", i64), ("xin_off", i64), ("meta_off", i64)]
 
 
+class RopeCfg(C.Structure):
+    _fields_ = [("rot_dim", i32), ("scaling", i32), ("theta", f64), ("factor", f64), ("orig_len", i32), ("fast", f64),
+                ("slow", f64)]
+
+
 _SIGS = {
     "adt_version": (i32, []),
     "adt_device_checks_enabled": (i32, []),
@@ -94,6 +102,13 @@ _SIGS = {
     "adt_tree_attn_noalloc": (i32, [p, p, p, i64, i64, p, p, p, p, i32, i32, i32, i32, i32, f32, i32, p, p]),
     "adt_tree_masks": (i32, [p, p, i32, i32, p, p, p]),
     "adt_kv_compact": (i32, [p, p, i32, i32, i32, i64, i64, p, p, i32, p, i32, i32, p]),
+    "adt_rope_freqs": (i32, [C.POINTER(RopeCfg), C.POINTER(f64), C.POINTER(f32)]),
+    "adt_rope_append": (i32, [p, p, p, i64, i64, i64, p, p, p, p, f32, i32, i32, i32, i32, i32, i32, i32, p, p, p, i64,
+                              i64, i32, i32, p]),
+    "adt_block_keys": (i32, [p, i64, i64, p, p, i32, i32, i32, i32, i32, p, i64, i64, i32, p]),
+    "adt_kv_evict": (i32, [p, p, p, i64, i64, i64, i64, p, i32, i32, i32, i32, i32, i32, i32, p, p, p, i64, i64, i64, i64,
+                           p, p, i32, p]),
+    "adt_weights_compact": (i32, [p, i32, i32, i64, i64, p, i32, p, i32, p, i32, p]),
     "adt_accept_workspace_size": (sz, [i32]),
     "adt_verify_accept": (i32, [p, i64, i32, p, p, p, p, i32, C.POINTER(AcceptCfg), u64, p, p, p, p, sz, p]),
     "adt_codebook_knn_workspace_size": (sz, [i32]),

@@ -29,6 +29,10 @@ SOURCES = [
     "kernels/accept_sample.hip",
     "kernels/knn.hip",
     "kernels/probe.hip",
+    "kernels/rope.hip",
+    "kernels/blocks.hip",
+    "kernels/evict.hip",
+    "api_cache.hip",
 ]
 
 # Packed fp32 VALU instructions are disabled for the device code.

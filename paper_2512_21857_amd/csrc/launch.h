@@ -53,6 +53,10 @@ uint32_t dev_errors_take_rows();
 uint32_t dev_errors_take_select();
 uint32_t dev_errors_take_attn();
 uint32_t dev_errors_take_gemm();
+uint32_t dev_errors_take_rope();
+uint32_t dev_errors_take_evict();
+uint32_t dev_errors_take_blocks();
+uint32_t dev_errors_take_cache_attn();
 
 // attn.hip
 // Row of query qr of sequence b in q and out: b * rs_b + qr * rs_i (rows of H * Dh); its mask
@@ -280,5 +284,43 @@ adt_status launch_accept_mss(const float* logits, int64_t ld, int V, const int32
 size_t knn_ws_bytes(int n);
 adt_status launch_codebook_knn(const float* cb, int n, int dim, int k, int32_t* out, void* ws, size_t ws_bytes,
                                hipStream_t st);
+
+// rope.hip
+// Rows [B][n_max] of q, k, v (ld elements from row to row), rotated over the first rot dims and
+// appended; fields as the arguments of adt_rope_append.
+struct RopeRows {
+  const void *q, *k, *v;
+  int64_t ldq, ldk, ldv;
+  const int32_t *pos, *kv_len, *n_rows;
+  int n_max, H, Hkv, Dh, rot;
+  void *q_out, *kc, *vc;
+  int64_t stride_b, stride_h;
+  int kv_cap;
+};
+adt_status launch_rope_append(const RopeRows& a, int B, const double* freq, float gain, bool inter, int dtype,
+                              hipStream_t st);
+
+// blocks.hip
+adt_status launch_block_keys(const void* k, int64_t sb, int64_t sh, const int32_t* start, const int32_t* kv_len, int B,
+                             int Hkv, int Dh, int block, int kv_cap, float* means, int64_t mb, int64_t mh, int dtype,
+                             hipStream_t st);
+
+// evict.hip
+struct EvictMove {
+  const void *k, *v;
+  const float* w;
+  int64_t stride_b, stride_s;     // bytes
+  int64_t stride_wb, stride_ws;   // floats
+  const int32_t* kv_len;
+  int kv_cap, slices, budget, row_bytes;
+  void *k_out, *v_out;
+  float* w_out;
+  int64_t ostride_b, ostride_s, ostride_wb, ostride_ws;
+  int32_t *kept, *new_len;
+};
+adt_status launch_kv_evict(const EvictMove& a, int B, int n_first, int n_last, hipStream_t st);
+adt_status launch_weights_compact(float* w, int B, int slices, int64_t stride_wb, int64_t stride_ws,
+                                  const int32_t* kv_len, int kv_cap, const int32_t* path, int path_stride,
+                                  const int32_t* n_acc, int a_max, hipStream_t st);
 
 }  // namespace adt

@@ -112,6 +112,173 @@ def kv_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len: torch.Tenso
                                _p(path), path.shape[1], _p(n_acc), a_max, dt, _stream()))
 
 
+def _on_device(fn, dev: torch.device, *args) -> None:
+    """fn(*args, stream) with `dev` current, on its current stream."""
+    if torch.cuda.current_device() == dev.index:
+        check(fn(*args, _stream()))
+    else:
+        with torch.cuda.device(dev):
+            check(fn(*args, _stream()))
+
+
+def _want(what: str, t: Optional[torch.Tensor], like: torch.Tensor, dtype: torch.dtype, shape=None) -> None:
+    """An optional tensor beside `like`: same device, this dtype, contiguous and of this shape."""
+    if t is None:
+        return
+    if t.device != like.device or t.dtype != dtype:
+        raise ValueError(f"{what}: {dtype} on {like.device} expected, not {t.dtype} on {t.device}")
+    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{what}: contiguous {tuple(shape)} expected, not {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _dt(t: torch.Tensor) -> int:
+    dt = {torch.float32: abi.F32, torch.bfloat16: abi.BF16}.get(t.dtype)
+    if dt is None or not t.is_cuda:
+        raise ValueError(f"float32 or bfloat16 device tensors expected, not {t.dtype} on {t.device}")
+    return dt
+
+
+def _cache_strides(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor] = None):
+    """(stride_b, stride_h) of caches [B][heads][slots][Dh] whose slots are contiguous rows; a layer
+    of a larger cache will do."""
+    B, heads, slots, Dh = k_cache.shape
+    if k_cache.stride(3) != 1 or k_cache.stride(2) != Dh:
+        raise ValueError(f"cache rows must be contiguous, not strides {k_cache.stride()}")
+    if v_cache is not None and (v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype or
+                                v_cache.device != k_cache.device or v_cache.stride() != k_cache.stride()):
+        raise ValueError("key and value caches must have one shape, layout, type and device")
+    return (k_cache.stride(0) if B > 1 else heads * k_cache.stride(1)), (k_cache.stride(1) if heads > 1 else slots * Dh)
+
+
+ROPE_LAYOUTS = {"half": abi.ROPE_HALF, "interleaved": abi.ROPE_INTERLEAVED}
+ROPE_SCALINGS = {"plain": abi.ROPE_PLAIN, "linear": abi.ROPE_LINEAR, "base": abi.ROPE_BASE, "ramp": abi.ROPE_RAMP}
+
+
+def rope_freqs(rot_dim: int, theta: float = 10000.0, scaling: str = "plain", factor: float = 1.0, orig_len: int = 0,
+               fast: float = 32.0, slow: float = 1.0, device="cuda"):
+    """(frequencies float64 [rot_dim / 2] on the device, gain) of a context scaling: 'plain',
+    'linear', 'base' or 'ramp' (orig_len positions trained for; turns fast and slow)."""
+    cfg = abi.RopeCfg(rot_dim, ROPE_SCALINGS[scaling], theta, factor, orig_len, fast, slow)
+    freq = (C.c_double * max(rot_dim // 2, 1))()
+    gain = C.c_float()
+    check(lib().adt_rope_freqs(C.byref(cfg), freq, C.byref(gain)))
+    return torch.tensor(list(freq), dtype=torch.float64, device=device), gain.value
+
+
+def _row_stride(what: str, t: torch.Tensor) -> int:
+    """Elements between the rows of t [B][n][heads][Dh], all [B][n] rows evenly apart."""
+    B, n, heads, Dh = t.shape
+    ld = t.stride(1) if n > 1 else (t.stride(0) if B > 1 else heads * Dh)
+    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != Dh) or (B > 1 and t.stride(0) != n * ld):
+        raise ValueError(f"{what}: rows of contiguous heads, evenly apart, expected, not strides {t.stride()}")
+    return ld
+
+
+def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, kv_len: torch.Tensor,
+                n_rows: torch.Tensor, freq: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                layout: str = "half", gain: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q [B][n][H][Dh], k and v [B][n][Hkv][Dh] (parts of one projection's rows will do) rotated at
+    pos int32 [B][n] over the first 2 * len(freq) dims; keys and values of rows i < n_rows[b] to
+    slots kv_len[b] + i of the caches [B][Hkv][S][Dh].  Returns the rotated queries (`out`, which
+    may be q where its rows are contiguous)."""
+    dt = _dt(q)
+    B, n, H, Dh = q.shape
+    Hkv = k.shape[2]
+    for name, t in (("k", k), ("v", v)):
+        _want(name, t, q, q.dtype)
+        if t.shape != (B, n, Hkv, Dh):
+            raise ValueError(f"{name}: {(B, n, Hkv, Dh)} expected, not {tuple(t.shape)}")
+    _want("k_cache", k_cache, q, q.dtype)
+    if k_cache.dim() != 4 or k_cache.shape[:2] != (B, Hkv) or k_cache.shape[3] != Dh:
+        raise ValueError(f"caches {(B, Hkv, 'slots', Dh)} expected, not {tuple(k_cache.shape)}")
+    sb, sh = _cache_strides(k_cache, v_cache)
+    _want("pos", pos, q, torch.int32, (B, n))
+    _want("kv_len", kv_len, q, torch.int32, (B,))
+    _want("n_rows", n_rows, q, torch.int32, (B,))
+    _want("freq", freq, q, torch.float64, (freq.numel(),))
+    out = torch.empty(B, n, H, Dh, dtype=q.dtype, device=q.device) if out is None else out
+    _want("out", out, q, q.dtype, (B, n, H, Dh))
+    _on_device(lib().adt_rope_append, q.device, _p(q), _p(k), _p(v), _row_stride("q", q), _row_stride("k", k),
+               _row_stride("v", v), _p(pos), _p(kv_len), _p(n_rows), _p(freq), gain, 2 * freq.numel(),
+               ROPE_LAYOUTS[layout], B, n, H, Hkv, Dh, _p(out), _p(k_cache), _p(v_cache), sb, sh, k_cache.shape[2], dt)
+    return out
+
+
+def block_keys(k_cache: torch.Tensor, kv_len: torch.Tensor, block: int, start: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Mean keys fp32 [B][Hkv][blocks][Dh] of the blocks of `block` slots of k_cache [B][Hkv][S][Dh]:
+    those from start[b] / block (default 0) to the last one of the prefix; others stay (a new
+    tensor starts at zero)."""
+    dt = _dt(k_cache)
+    B, Hkv, S, Dh = k_cache.shape
+    sb, sh = _cache_strides(k_cache)
+    n_blk = -(-S // block) if block > 0 else 0
+    if out is None:
+        out = torch.zeros(B, Hkv, n_blk, Dh, dtype=torch.float32, device=k_cache.device)
+    _want("out", out, k_cache, torch.float32, (B, Hkv, n_blk, Dh))
+    _want("kv_len", kv_len, k_cache, torch.int32, (B,))
+    _want("start", start, k_cache, torch.int32, (B,))
+    _on_device(lib().adt_block_keys, k_cache.device, _p(k_cache), sb, sh, _p(start), _p(kv_len), B, Hkv, Dh, block, S,
+               _p(out), Hkv * n_blk * Dh, n_blk * Dh, dt)
+    return out
+
+
+def _weight_strides(what: str, w: torch.Tensor, like: torch.Tensor):
+    """(stride_b, stride_h) of weights fp32 [B][heads][>= slots]."""
+    _want(what, w, like, torch.float32)
+    if w.dim() != 3 or w.shape[:2] != like.shape[:2] or w.shape[2] < like.shape[2] or w.stride(2) != 1:
+        raise ValueError(f"{what}: {(like.shape[0], like.shape[1], like.shape[2])} with contiguous slots expected, not "
+                         f"{tuple(w.shape)} with strides {w.stride()}")
+    B, heads, slots = w.shape
+    sh = w.stride(1) if heads > 1 else slots
+    return (w.stride(0) if B > 1 else heads * sh), sh
+
+
+def kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor, kv_len: torch.Tensor, budget: int,
+             n_first: int = 0, n_last: int = 0, k_out: Optional[torch.Tensor] = None,
+             v_out: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
+             kept: Optional[torch.Tensor] = None, new_len: Optional[torch.Tensor] = None):
+    """Keeps `budget` slots of every slice of the caches [B][slices][S][Dh]: the first n_first, the
+    last n_last and those of the largest weights fp32 [B][slices][S], in order.  In place, or into
+    k_out, v_out and weights_out [B][slices][>= budget].  Returns (kept int32 [B][slices][budget],
+    new_len int32 [B]; new_len may be kv_len)."""
+    dt = _dt(k_cache)
+    B, slices, S, Dh = k_cache.shape
+    sb, ss = _cache_strides(k_cache, v_cache)
+    wb, ws = _weight_strides("weights", weights, k_cache)
+    if (k_out is None) != (v_out is None) or (k_out is None) != (weights_out is None):
+        raise ValueError("k_out, v_out and weights_out are given together or not at all")
+    if k_out is None:
+        k_out, v_out, weights_out = k_cache, v_cache, weights
+    _want("k_out", k_out, k_cache, k_cache.dtype)
+    if k_out.dim() != 4 or k_out.shape[:2] != (B, slices) or k_out.shape[3] != Dh or k_out.shape[2] < min(S, budget):
+        raise ValueError(f"k_out: {(B, slices, min(S, budget), Dh)} expected, not {tuple(k_out.shape)}")
+    osb, oss = _cache_strides(k_out, v_out)
+    owb, ows = _weight_strides("weights_out", weights_out, k_out)
+    kept = torch.full((B, slices, budget), -1, dtype=torch.int32, device=k_cache.device) if kept is None else kept
+    new_len = torch.empty(B, dtype=torch.int32, device=k_cache.device) if new_len is None else new_len
+    _want("kept", kept, k_cache, torch.int32, (B, slices, budget))
+    _want("kv_len", kv_len, k_cache, torch.int32, (B,))
+    _want("new_len", new_len, k_cache, torch.int32, (B,))
+    _on_device(lib().adt_kv_evict, k_cache.device, _p(k_cache), _p(v_cache), _p(weights), sb, ss, wb, ws, _p(kv_len), B,
+               slices, Dh, S, budget, n_first, n_last, _p(k_out), _p(v_out), _p(weights_out), osb, oss, owb, ows,
+               _p(kept), _p(new_len), dt)
+    return kept, new_len
+
+
+def weights_compact(weights: torch.Tensor, kv_len: torch.Tensor, path: torch.Tensor, n_acc: torch.Tensor,
+                    a_max: int) -> None:
+    """Moves the weights fp32 [B][slices][S] of an accepted path as kv_compact moves its rows."""
+    B, slices, S = weights.shape
+    wb, ws = _weight_strides("weights", weights, weights)
+    _want("kv_len", kv_len, weights, torch.int32, (B,))
+    _want("n_acc", n_acc, weights, torch.int32, (B,))
+    _want("path", path, weights, torch.int32, (B, path.shape[-1]))
+    _require_cuda(weights)
+    _on_device(lib().adt_weights_compact, weights.device, _p(weights), B, slices, wb, ws, _p(kv_len), S, _p(path),
+               path.shape[1], _p(n_acc), a_max)
+
+
 def accept_cfg(mode: str = "greedy", temperature: float = 1.0, top_k: int = 0, delta: float = 0.0,
                knn: Optional[torch.Tensor] = None, knn_k: int = 1, seed: int = 0, children: int = 0,
                q_logits: Optional[torch.Tensor] = None, q_row: Optional[torch.Tensor] = None) -> abi.AcceptCfg:
