@@ -215,6 +215,63 @@ adt_status adt_block_keys(const void* k_cache, int64_t stride_b, int64_t stride_
                           const int32_t* kv_len, int32_t B, int32_t Hkv, int32_t Dh, int32_t block, int32_t kv_cap,
                           float* means, int64_t stride_mb, int64_t stride_mh, int32_t dtype, void* stream);
 
+/* Tree attention of H query heads over Hkv key-value heads (head h reads key-value head
+ * h / (H / Hkv)) in which every row sees n_sel blocks of the prefix, and of the tree its own path:
+ *   score(i, h, j) = sum over the query heads of key-value head h of q[b][i][head] . means(b, h, j),
+ *     in double: rows that score two blocks nearly alike still take the better one;
+ *   the first n_first and the last n_last blocks of the prefix always count, then the best scores
+ *     (ties: the lower block; NaN below every number), n_sel in all, or all blocks where the prefix
+ *     has no more; the query heads of a key-value head share the choice;
+ *   out = softmax(scale * q . K) V over the slots of the chosen blocks and the tail slots
+ *     kv_len[b] + j, j < n_tail[b], whose bit j is set in anc_mask[b][i].
+ * means (adt_block_keys, with the strides given) has to be up to date for the whole prefix.
+ * sel: NULL, or [B][nq_max][Hkv][n_sel] int32 out: the chosen blocks of rows i < n_q[b] in rising
+ *   order, -1 after the last.  A row that sees no slot gives zeros.
+ * Other arguments as in adt_tree_attn.  workspace: adt_sparse_tree_attn_workspace_size() bytes,
+ * 16-byte aligned.  ADT_E_SHAPE: Dh, block, H not a multiple of Hkv, misaligned addresses or
+ * strides (16 bytes); ADT_E_CAPACITY: nq_max, workspace, more than 16384 blocks in kv_cap;
+ * ADT_E_ARG: n_first + n_last > n_sel, n_sel < 1. */
+size_t adt_sparse_tree_attn_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max,
+                                           int32_t kv_cap, int32_t block, int32_t n_sel, int32_t dtype);
+adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, const void* v_cache, int64_t stride_b,
+                                int64_t stride_h, const float* means, int64_t stride_mb, int64_t stride_mh,
+                                const int32_t* kv_len, const int32_t* n_q, const int32_t* n_tail,
+                                const uint64_t* anc_mask, int32_t B, int32_t H, int32_t Hkv, int32_t Dh,
+                                int32_t nq_max, int32_t kv_cap, int32_t block, int32_t n_sel, int32_t n_first,
+                                int32_t n_last, float scale, int32_t dtype, void* out, int32_t* sel, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------ attention that rates its slots
+ * adt_tree_attn (same rows, caches, masks and outputs, for H query heads over Hkv key-value heads:
+ * head h reads key-value head h / (H / Hkv)) that also adds up the softmax weight every cache slot
+ * received, what an eviction decides by:
+ *   weights_out[b][h][s] = decay * weights_in[b][h][s] + sum over i < n_q[b] of
+ *       row_weight[b][i] * sum over the query heads of h of p(row i, head, slot s)
+ * for every slot s < kv_len[b] + n_tail[b]; the tail's slots are new and take no earlier weight,
+ * and slots behind stay as they are.  All in fp32, in a fixed order.
+ * weights_in:  element (b, h, s) at b * stride_wb + h * stride_wh + s; NULL: none
+ * weights_out: the same strides; may be weights_in
+ * row_weight:  [B][nq_max] fp32 (a draft's path confidences, 0 for rows not to count); NULL: ones
+ * A row that sees no slot gives zeros and adds nothing.
+ * workspace: adt_tree_attn_weights_workspace_size() bytes, 16-byte aligned.  H a multiple of Hkv,
+ * nq_max * H / Hkv <= 8192 (ADT_E_SHAPE, ADT_E_CAPACITY); q, caches and out 16-byte aligned,
+ * strides multiples of 16 bytes. */
+size_t adt_tree_attn_weights_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max,
+                                            int32_t kv_cap, int32_t dtype);
+adt_status adt_tree_attn_weights(const void* q, const void* k_cache, const void* v_cache, int64_t stride_b,
+                                 int64_t stride_h, const int32_t* kv_len, const int32_t* n_q, const int32_t* n_tail,
+                                 const uint64_t* anc_mask, int32_t B, int32_t H, int32_t Hkv, int32_t Dh,
+                                 int32_t nq_max, int32_t kv_cap, float scale, int32_t dtype, void* out,
+                                 const float* weights_in, float* weights_out, int64_t stride_wb, int64_t stride_wh,
+                                 float decay, const float* row_weight, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+/* The weights of an accepted path, as adt_kv_compact moves its keys and values: in every slice,
+ * slot kv_len[b] + m <- slot kv_len[b] + path[b][m] for m = 1..n_acc[b].  Arguments as there
+ * (slots at or past kv_cap are left alone). */
+adt_status adt_weights_compact(float* weights, int32_t B, int32_t slices, int64_t stride_wb, int64_t stride_ws,
+                               const int32_t* kv_len, int32_t kv_cap, const int32_t* path, int32_t path_stride,
+                               const int32_t* n_acc, int32_t a_max, void* stream);
+
 /* ------------------------------------------------------------------ eviction
  * Bounds a cache by what its slots are worth: of the kv_len[b] slots of sequence b's prefix, each
  * slice keeps the first n_first, the last n_last, and between them those of the largest weights
@@ -236,13 +293,6 @@ adt_status adt_kv_evict(const void* k_cache, const void* v_cache, const float* w
                         void* k_out, void* v_out, float* weights_out, int64_t out_stride_b, int64_t out_stride_slice,
                         int64_t out_stride_wb, int64_t out_stride_ws, int32_t* kept, int32_t* new_len, int32_t dtype,
                         void* stream);
-
-/* The weights of an accepted path, as adt_kv_compact moves its keys and values: in every slice,
- * slot kv_len[b] + m <- slot kv_len[b] + path[b][m] for m = 1..n_acc[b].  Arguments as there
- * (slots at or past kv_cap are left alone). */
-adt_status adt_weights_compact(float* weights, int32_t B, int32_t slices, int64_t stride_wb, int64_t stride_ws,
-                               const int32_t* kv_len, int32_t kv_cap, const int32_t* path, int32_t path_stride,
-                               const int32_t* n_acc, int32_t a_max, void* stream);
 
 /* ------------------------------------------------------------------ c1-c3: acceptance
  * Walk from the root of one verified tree (Sec. 3.1 Eq. 1; Sec. 5.1).

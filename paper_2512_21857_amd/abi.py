@@ -106,6 +106,12 @@ _SIGS = {
     "adt_rope_append": (i32, [p, p, p, i64, i64, i64, p, p, p, p, f32, i32, i32, i32, i32, i32, i32, i32, p, p, p, i64,
                               i64, i32, i32, p]),
     "adt_block_keys": (i32, [p, i64, i64, p, p, i32, i32, i32, i32, i32, p, i64, i64, i32, p]),
+    "adt_sparse_tree_attn_workspace_size": (sz, [i32] * 9),
+    "adt_sparse_tree_attn": (i32, [p, p, p, i64, i64, p, i64, i64, p, p, p, p, i32, i32, i32, i32, i32, i32, i32, i32, i32,
+                                   i32, f32, i32, p, p, p, sz, p]),
+    "adt_tree_attn_weights_workspace_size": (sz, [i32] * 7),
+    "adt_tree_attn_weights": (i32, [p, p, p, i64, i64, p, p, p, p, i32, i32, i32, i32, i32, i32, f32, i32, p, p, p, i64,
+                                    i64, f32, p, p, sz, p]),
     "adt_kv_evict": (i32, [p, p, p, i64, i64, i64, i64, p, i32, i32, i32, i32, i32, i32, i32, p, p, p, i64, i64, i64, i64,
                            p, p, i32, p]),
     "adt_weights_compact": (i32, [p, i32, i32, i64, i64, p, i32, p, i32, p, i32, p]),

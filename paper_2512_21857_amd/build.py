@@ -31,6 +31,7 @@ SOURCES = [
     "kernels/probe.hip",
     "kernels/rope.hip",
     "kernels/blocks.hip",
+    "kernels/cache_attn.hip",
     "kernels/evict.hip",
     "api_cache.hip",
 ]

@@ -1159,7 +1159,7 @@ static adt_status device_errors() {
   if (!ADT_DEVICE_CHECKS) return ADT_OK;
   const uint32_t bits = dev_errors_take_rows() | dev_errors_take_select() | dev_errors_take_attn() |
                         dev_errors_take_gemm() | dev_errors_take_rope() | dev_errors_take_blocks() |
-                        dev_errors_take_evict();
+                        dev_errors_take_cache_attn() | dev_errors_take_evict();
   ADT_CHECK_ARG(!(bits & 0x80000000u), ADT_E_HIP, "device check: the error words could not be read");
   ADT_CHECK_ARG(bits == 0, ADT_E_DEVICE_INVARIANT, "device invariant violated:%s%s%s",
                 (bits & DEVINV_PARENT) ? " a parent not before its child" : "",

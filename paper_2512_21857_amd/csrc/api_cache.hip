@@ -104,6 +104,115 @@ extern "C" adt_status adt_block_keys(const void* k_cache, int64_t stride_b, int6
                            stride_mh, dtype, (hipStream_t)stream);
 }
 
+// What both attentions ask of their common arguments.
+static adt_status check_cache_attn(const char* who, const CacheAttn& a, int32_t B, int32_t H, int32_t dtype) {
+  ADT_CHECK_ARG(a.q && a.k && a.v && a.kv_len && a.n_q && a.n_tail && a.mask && a.out, ADT_E_ARG, "%s: null pointer",
+                who);
+  ADT_CHECK_ARG(known_dtype(dtype), ADT_E_ARG, "%s: bad dtype %d", who, dtype);
+  ADT_CHECK_ARG(B >= 1 && B <= MAX_GRID_YZ && H >= 1 && a.Hkv >= 1 && a.kv_cap >= 1, ADT_E_ARG,
+                "%s: B=%d H=%d Hkv=%d kv_cap=%d", who, B, H, a.Hkv, a.kv_cap);
+  ADT_CHECK_ARG(a.Dh == 64 || a.Dh == 128, ADT_E_SHAPE, "%s: head_dim %d not in {64, 128}", who, a.Dh);
+  ADT_CHECK_ARG(H % a.Hkv == 0 && a.Hkv <= MAX_GRID_YZ && (int64_t)B * a.Hkv <= MAX_GRID_YZ, ADT_E_SHAPE,
+                "%s: %d query heads over %d key-value heads of %d sequences", who, H, a.Hkv, B);
+  ADT_CHECK_ARG(a.nq_max >= 1 && a.nq_max <= ADT_MAX_NODES, ADT_E_CAPACITY, "%s: nq_max %d", who, a.nq_max);
+  ADT_CHECK_ARG((int64_t)a.nq_max * (H / a.Hkv) <= 8192, ADT_E_CAPACITY, "%s: %d rows of %d heads per key-value head",
+                who, a.nq_max, H / a.Hkv);
+  ADT_CHECK_ARG(a.sh >= (int64_t)a.kv_cap * a.Dh && (B == 1 || a.sb >= (int64_t)a.Hkv * a.sh), ADT_E_SHAPE,
+                "%s: cache strides too small", who);
+  const int64_t es = elem_bytes(dtype);
+  ADT_CHECK_ARG(aligned16(a.q) && aligned16(a.k) && aligned16(a.v) && aligned16(a.out) && stride16(a.sb, es) &&
+                    stride16(a.sh, es),
+                ADT_E_SHAPE, "%s: addresses and strides must be multiples of 16 bytes", who);
+  ADT_CHECK_ARG(std::isfinite(a.scale) && a.scale > 0.f, ADT_E_ARG, "%s: scale", who);
+  return ADT_OK;
+}
+
+// Sizes an attention's workspace depends on; false if the call would be refused anyway.
+static bool sized(CacheAttn& a, int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max, int32_t kv_cap,
+                  int32_t dtype) {
+  if (B < 1 || H < 1 || Hkv < 1 || H % Hkv || (Dh != 64 && Dh != 128) || nq_max < 1 || nq_max > ADT_MAX_NODES ||
+      kv_cap < 1 || !known_dtype(dtype))
+    return false;
+  a.Hkv = Hkv;
+  a.G = H / Hkv;
+  a.Dh = Dh;
+  a.nq_max = nq_max;
+  a.kv_cap = kv_cap;
+  return true;
+}
+constexpr int32_t MAX_BLOCKS = 16384;
+static bool known_block(int32_t block) { return block == 32 || block == 64 || block == 128; }
+
+extern "C" size_t adt_sparse_tree_attn_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max,
+                                                      int32_t kv_cap, int32_t block, int32_t n_sel, int32_t dtype) {
+  CacheAttn a{};
+  if (!sized(a, B, H, Hkv, Dh, nq_max, kv_cap, dtype) || !known_block(block) || n_sel < 1) return 0;
+  a.block = block;
+  a.n_blk = (int)(((int64_t)kv_cap + block - 1) / block);
+  a.n_sel = n_sel;
+  return sparse_attn_ws_bytes(a, B, dtype);
+}
+
+extern "C" adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, const void* v_cache, int64_t stride_b,
+                                           int64_t stride_h, const float* means, int64_t stride_mb, int64_t stride_mh,
+                                           const int32_t* kv_len, const int32_t* n_q, const int32_t* n_tail,
+                                           const uint64_t* anc_mask, int32_t B, int32_t H, int32_t Hkv, int32_t Dh,
+                                           int32_t nq_max, int32_t kv_cap, int32_t block, int32_t n_sel,
+                                           int32_t n_first, int32_t n_last, float scale, int32_t dtype, void* out,
+                                           int32_t* sel, void* workspace, size_t workspace_bytes, void* stream) {
+  CacheAttn a{q, k_cache, v_cache, stride_b, stride_h, kv_len, n_q, n_tail, anc_mask, Hkv, Hkv > 0 ? H / Hkv : 0, Dh,
+              nq_max, kv_cap, scale, out};
+  const adt_status e = check_cache_attn("sparse_tree_attn", a, B, H, dtype);
+  if (e) return e;
+  ADT_CHECK_ARG(means, ADT_E_ARG, "sparse_tree_attn: null pointer");
+  ADT_CHECK_ARG(known_block(block), ADT_E_SHAPE, "sparse_tree_attn: block %d not in {32, 64, 128}", block);
+  ADT_CHECK_ARG(n_sel >= 1 && n_first >= 0 && n_last >= 0 && (int64_t)n_first + n_last <= n_sel, ADT_E_ARG,
+                "sparse_tree_attn: %d first and %d last of %d blocks", n_first, n_last, n_sel);
+  const int64_t n_blk = ((int64_t)kv_cap + block - 1) / block;
+  ADT_CHECK_ARG(n_blk <= MAX_BLOCKS, ADT_E_CAPACITY, "sparse_tree_attn: %lld blocks", (long long)n_blk);
+  ADT_CHECK_ARG(stride_mh >= n_blk * Dh && (B == 1 || stride_mb >= (int64_t)Hkv * stride_mh), ADT_E_SHAPE,
+                "sparse_tree_attn: strides of the means too small for %lld blocks", (long long)n_blk);
+  ADT_CHECK_ARG(aligned16(means) && stride16(stride_mb, 4) && stride16(stride_mh, 4) && aligned16(workspace),
+                ADT_E_SHAPE, "sparse_tree_attn: addresses and strides must be multiples of 16 bytes");
+  a.block = block;
+  a.n_blk = (int)n_blk;
+  a.n_sel = n_sel;
+  const size_t need = sparse_attn_ws_bytes(a, B, dtype);
+  ADT_CHECK_ARG(workspace && workspace_bytes >= need, ADT_E_CAPACITY, "sparse_tree_attn: workspace %zu < %zu bytes",
+                workspace_bytes, need);
+  return launch_sparse_attn(a, B, means, stride_mb, stride_mh, n_first, n_last, sel, dtype, workspace,
+                            (hipStream_t)stream);
+}
+
+extern "C" size_t adt_tree_attn_weights_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max,
+                                                       int32_t kv_cap, int32_t dtype) {
+  CacheAttn a{};
+  return sized(a, B, H, Hkv, Dh, nq_max, kv_cap, dtype) ? weights_attn_ws_bytes(a, B, dtype) : 0;
+}
+
+extern "C" adt_status adt_tree_attn_weights(const void* q, const void* k_cache, const void* v_cache, int64_t stride_b,
+                                            int64_t stride_h, const int32_t* kv_len, const int32_t* n_q,
+                                            const int32_t* n_tail, const uint64_t* anc_mask, int32_t B, int32_t H,
+                                            int32_t Hkv, int32_t Dh, int32_t nq_max, int32_t kv_cap, float scale,
+                                            int32_t dtype, void* out, const float* weights_in, float* weights_out,
+                                            int64_t stride_wb, int64_t stride_wh, float decay, const float* row_weight,
+                                            void* workspace, size_t workspace_bytes, void* stream) {
+  const CacheAttn a{q, k_cache, v_cache, stride_b, stride_h, kv_len, n_q, n_tail, anc_mask, Hkv, Hkv > 0 ? H / Hkv : 0,
+                    Dh, nq_max, kv_cap, scale, out};
+  const adt_status e = check_cache_attn("tree_attn_weights", a, B, H, dtype);
+  if (e) return e;
+  ADT_CHECK_ARG(weights_out, ADT_E_ARG, "tree_attn_weights: null pointer");
+  ADT_CHECK_ARG(std::isfinite(decay), ADT_E_ARG, "tree_attn_weights: decay");
+  ADT_CHECK_ARG(stride_wh >= kv_cap && (B == 1 || stride_wb >= (int64_t)Hkv * stride_wh), ADT_E_SHAPE,
+                "tree_attn_weights: strides of the weights too small");
+  ADT_CHECK_ARG(aligned16(workspace), ADT_E_SHAPE, "tree_attn_weights: workspace not 16-byte aligned");
+  const size_t need = weights_attn_ws_bytes(a, B, dtype);
+  ADT_CHECK_ARG(workspace && workspace_bytes >= need, ADT_E_CAPACITY, "tree_attn_weights: workspace %zu < %zu bytes",
+                workspace_bytes, need);
+  return launch_weights_attn(a, B, weights_in, weights_out, stride_wb, stride_wh, decay, row_weight, dtype, workspace,
+                             (hipStream_t)stream);
+}
+
 extern "C" adt_status adt_kv_evict(const void* k_cache, const void* v_cache, const float* weights, int64_t stride_b,
                                    int64_t stride_slice, int64_t stride_wb, int64_t stride_ws, const int32_t* kv_len,
                                    int32_t B, int32_t slices, int32_t Dh, int32_t kv_cap, int32_t budget,

@@ -1,0 +1,702 @@
+// Tree attention over a long cache for grouped heads: over the blocks of the prefix that each query
+// row chose, or over all of it with the weight that every slot received.
+//
+// The query rows of one key-value head, nq * G of them (row = node * G + head of the group), go in
+// tiles of 16 through one pass over the keys with the running maximum and sum of a softmax:
+//   S^T[key][row] = K[key][:] . Q[row][:]        (A = K rows, B = Q^T)
+//   O^T[dim][row] += V^T[dim][key] . P^T[key][row]
+// A workgroup holds RT tiles (16 RT rows) in registers; its waves and the other workgroups of the
+// same rows (splits) deal the keys out in steps among themselves, each step read by one wave only,
+// so K and V come straight from memory into registers and every slot is read once per 16 RT rows.
+// What the waves of a workgroup found is merged in LDS, what the splits found by a launch of its own,
+// always in one order.  Steps never straddle the end of the prefix: the tree's own slots, which the
+// rows see through their ancestor masks, have steps of their own.
+//
+// bf16 runs on the 16x16x32 MFMA, 32 keys a step, V transposed through LDS, probabilities rounded
+// to bf16 for the second product (2^-9 a term, below the rounding of the output itself); fp32 on
+// the 16x16x4 MFMA, 16 keys a step, without LDS.  Scores, softmax sums and outputs are fp32.
+//
+// A masked score is dropped by selection, so whatever a slot's key holds does not matter to rows
+// that do not see it.  Its value does meet their zero weight in the second product, and 0 * inf is
+// NaN; a wave whose results come out not finite therefore goes through its steps once more with
+// such values taken out of the product and added for the rows that see them only.
+#include <algorithm>
+#include <type_traits>
+
+#include "../launch.h"
+
+namespace adt {
+
+ADT_DEVICE_ERROR_WORD(cache_attn)
+
+constexpr int CA_WAVES = 4;
+constexpr int CA_THREADS = CA_WAVES * WAVE;
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// LDS written by a wave's lanes before, read by others of its lanes after.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
+
+// What the two types differ in.  Lane (l, g) = (lane % 16, lane / 16) holds the scores of row l and
+// the KT keys key(sub, r) = 16 sub + 4 g + r of a step, and the outputs dim(t, r) of row l.
+template <typename T, int DH>
+struct Tile;
+
+template <int DH>
+struct Tile<uint16_t, DH> {
+  static constexpr int KT = 32, SUBS = 2, KS = DH / 32, OT = DH / 16, VG = DH / 64;
+  static constexpr int VP = DH + 16;     // LDS row of V, padded so that a transpose load's rows fall on distinct banks
+  static constexpr int LDS_BYTES = KT * VP * 2;
+  struct Query {
+    bf16x8 f[KS];
+  };
+  struct Step {
+    bf16x8 k[SUBS][KS];
+    u16x8 v[VG][4];
+  };
+  static __device__ __forceinline__ int dim(int t, int g, int r) { return t * 16 + 4 * g + r; }
+  static __device__ __forceinline__ void zero(Query& x) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) x.f[j] = bf16x8{};
+  }
+  static __device__ __forceinline__ void load(Query& x, const uint16_t* row, int g) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) x.f[j] = *reinterpret_cast<const bf16x8*>(row + j * 32 + g * 8);
+  }
+  // the step's keys key0 .. key0 + 31; those past `last` repeat it
+  static __device__ __forceinline__ void load_k(Step& s, const uint16_t* k, int key0, int last, int l, int g) {
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub) {
+      const uint16_t* row = k + (int64_t)min(key0 + sub * 16 + l, last) * DH + g * 8;
+#pragma unroll
+      for (int j = 0; j < KS; ++j) s.k[sub][j] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(row + j * 32));
+    }
+  }
+  static __device__ __forceinline__ void load_v(Step& s, const uint16_t* v, int key0, int last, int l, int g) {
+    const int lane = g * 16 + l;
+#pragma unroll
+    for (int j = 0; j < VG; ++j) {
+      const int gi = lane + j * WAVE, c = gi % (DH / 8) * 8, r4 = gi / (DH / 8) * 4;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        s.v[j][u] = __builtin_nontemporal_load(reinterpret_cast<const u16x8*>(v + (int64_t)min(key0 + r4 + u, last) * DH + c));
+    }
+  }
+  // V into the wave's LDS rows
+  static __device__ __forceinline__ void stage(const Step& s, void* lds, int l, int g) {
+    uint16_t(*rows)[VP] = reinterpret_cast<uint16_t(*)[VP]>(lds);
+    const int lane = g * 16 + l;
+#pragma unroll
+    for (int j = 0; j < VG; ++j) {
+      const int gi = lane + j * WAVE, c = gi % (DH / 8) * 8, r4 = gi / (DH / 8) * 4;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) *reinterpret_cast<u16x8*>(&rows[r4 + u][c]) = s.v[j][u];
+    }
+    wave_lds_fence();
+  }
+  static __device__ __forceinline__ void scores(f32x4 (&st)[SUBS], const Step& s, const Query& x) {
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub) {
+      st[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < KS; ++j) st[sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s.k[sub][j], x.f[j], st[sub], 0, 0, 0);
+    }
+  }
+  // S[row][key] of 16 rows and the keys 16 sub + l
+  static __device__ __forceinline__ void col_scores(f32x4& st, const Step& s, int sub, const Query& x) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.f[j], s.k[sub][j], st, 0, 0, 0);
+  }
+  // O^T += V^T P^T; lane (l, g) of the transpose load that addresses row k0 + l / 4, dims
+  // d0 + 4 (l % 4)..+3 gets V[k0 + s][d0 + l], s = 0..3
+  template <bool SAFE>
+  static __device__ __forceinline__ void add(f32x4 (&o)[OT], const f32x4 (&p)[SUBS], const Step&, void* lds, int l, int g) {
+    uint16_t(*rows)[VP] = reinterpret_cast<uint16_t(*)[VP]>(lds);
+    bf16x8 b;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) b[r] = (__bf16)(p[r / 4][r % 4]);
+    const int col = 4 * (l & 3), row = l >> 2;
+#pragma unroll
+    for (int t = 0; t < OT; ++t) {
+      v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)&rows[4 * g + row][t * 16 + col]);
+      v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)&rows[16 + 4 * g + row][t * 16 + col]);
+      if (SAFE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((lo[e] & 0x7f80) == 0x7f80) lo[e] = 0;
+          if ((hi[e] & 0x7f80) == 0x7f80) hi[e] = 0;
+        }
+      }
+      const bf16x8 a = __builtin_bit_cast(bf16x8, v8i16{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, o[t], 0, 0, 0);
+    }
+  }
+};
+
+template <int DH>
+struct Tile<float, DH> {
+  static constexpr int KT = 16, SUBS = 1, OT = DH / 16;
+  static constexpr int LDS_BYTES = 0;
+  struct Query {
+    f32x4 f[DH / 16];
+  };
+  struct Step {
+    f32x4 k[DH / 16];
+    f32x4 v[4][DH / 64];     // v[r][c]: key 4 g + r, dims 64 c + 4 l .. + 3
+  };
+  // output tile 4 c + e takes the dims 64 c + 4 i + e of its rows i
+  static __device__ __forceinline__ int dim(int t, int g, int r) { return t / 4 * 64 + 16 * g + 4 * r + t % 4; }
+  static __device__ __forceinline__ void zero(Query& x) {
+#pragma unroll
+    for (int j = 0; j < DH / 16; ++j) x.f[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  static __device__ __forceinline__ void load(Query& x, const float* row, int g) {
+#pragma unroll
+    for (int j = 0; j < DH / 16; ++j) x.f[j] = *reinterpret_cast<const f32x4*>(row + j * 16 + g * 4);
+  }
+  static __device__ __forceinline__ void load_k(Step& s, const float* k, int key0, int last, int l, int g) {
+    const float* row = k + (int64_t)min(key0 + l, last) * DH + g * 4;
+#pragma unroll
+    for (int j = 0; j < DH / 16; ++j) s.k[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row + j * 16));
+  }
+  static __device__ __forceinline__ void load_v(Step& s, const float* v, int key0, int last, int l, int g) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float* row = v + (int64_t)min(key0 + 4 * g + r, last) * DH + 4 * l;
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c) s.v[r][c] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row + c * 64));
+    }
+  }
+  static __device__ __forceinline__ void stage(const Step&, void*, int, int) {}
+  static __device__ __forceinline__ void scores(f32x4 (&st)[SUBS], const Step& s, const Query& x) {
+    st[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < DH / 16; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(s.k[j][e], x.f[j][e], st[0], 0, 0, 0);
+  }
+  static __device__ __forceinline__ void col_scores(f32x4& st, const Step& s, int, const Query& x) {
+#pragma unroll
+    for (int j = 0; j < DH / 16; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_16x16x4f32(x.f[j][e], s.k[j][e], st, 0, 0, 0);
+  }
+  template <bool SAFE>
+  static __device__ __forceinline__ void add(f32x4 (&o)[OT], const f32x4 (&p)[SUBS], const Step& s, void*, int, int) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < OT; ++t) {
+        float a = s.v[r][t / 4][t % 4];
+        if (SAFE && not_finite(a)) a = 0.f;
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, p[0][r], o[t], 0, 0, 0);
+      }
+  }
+};
+
+// (registers: outputs 16 RT DH / 64 a lane, and a step's K and V: one wave per SIMD at RT = 4)
+template <typename T, int DH, int RT, bool SPARSE>
+__global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel(CacheAttn a, int splits,
+                                                                                float* __restrict__ part_o,
+                                                                                float* __restrict__ part_ml) {
+  typedef Tile<T, DH> X;
+  constexpr int KT = X::KT, SUBS = X::SUBS, OT = X::OT;
+  constexpr int PP = KT + 1;                                       // row of the probabilities in LDS
+  constexpr int MP = DH + 4;                                       // row of a merged tile
+  constexpr int STEP_BYTES = CA_WAVES * (X::LDS_BYTES + 16 * PP * 4);
+  constexpr int MERGE_BYTES = CA_WAVES * 16 * (MP + 2) * 4;
+  __shared__ __attribute__((aligned(16))) unsigned char smem[STEP_BYTES > MERGE_BYTES ? STEP_BYTES : MERGE_BYTES];
+  extern __shared__ uint16_t chosen[];                             // SPARSE: the blocks that any row chose
+  const int h = blockIdx.x % a.Hkv, rg = blockIdx.x / a.Hkv, b = blockIdx.y, sp = blockIdx.z;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+  const int l = lane & 15, g = lane >> 4;
+  const int rows = a.nq_max * a.G, live_rows = max(0, min(a.n_q[b], a.nq_max)) * a.G;
+  const int r0 = rg * 16 * RT;
+  if (r0 >= live_rows) return;
+  const int L = max(0, min(a.kv_len[b], a.kv_cap));
+  const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
+  if (threadIdx.x == 0 && (int64_t)a.kv_len[b] + a.n_tail[b] > a.kv_cap) dev_fail(DEVINV_KV_RANGE);
+  const uint64_t* marks = SPARSE ? a.marks + ((int64_t)b * a.Hkv + h) * a.n_blk * ADT_MASK_WORDS : nullptr;
+  const int per_blk = SPARSE ? a.block / KT : 0;
+  int prefix_steps = (L + KT - 1) / KT;
+  if (SPARSE) {
+    // the marked blocks, in order
+    int* wave_n = reinterpret_cast<int*>(smem);
+    const int live = (L + a.block - 1) / a.block;
+    int n = 0;
+    for (int base = 0; base < live; base += CA_THREADS) {
+      const int j = base + threadIdx.x;
+      const bool on = j < live && (marks[2 * j] | marks[2 * j + 1]) != 0;
+      const uint64_t bal = __ballot(on);
+      if (lane == 0) wave_n[wave] = __popcll(bal);
+      __syncthreads();
+      int at = n + __popcll(bal & ((1ull << lane) - 1));
+#pragma unroll
+      for (int w = 0; w < CA_WAVES; ++w) {
+        const int c = wave_n[w];
+        if (w < wave) at += c;
+        n += c;
+      }
+      if (on) chosen[at] = (uint16_t)j;
+      __syncthreads();
+    }
+    prefix_steps = n * per_blk;
+  }
+  const int steps = prefix_steps + (total - L + KT - 1) / KT;
+  const T* kb = (const T*)a.k + b * a.sb + h * a.sh;
+  const T* vb = (const T*)a.v + b * a.sb + h * a.sh;
+
+  typename X::Query q[RT];
+  uint64_t aw0[RT], aw1[RT];
+  int node[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    X::zero(q[t]);
+    aw0[t] = aw1[t] = 0;
+    node[t] = -1;
+    const int row = r0 + t * 16 + l;
+    if (row < live_rows) {
+      const int i = row / a.G, u = row - i * a.G;
+      node[t] = i;
+      X::load(q[t], (const T*)a.q + (((int64_t)b * a.nq_max + i) * a.Hkv + h) * a.G * DH + (int64_t)u * DH, g);
+      const uint64_t* mp = a.mask + ((int64_t)b * a.nq_max + i) * ADT_MASK_WORDS;
+      aw0[t] = mp[0];
+      aw1[t] = mp[1];
+    }
+  }
+  const float scale_log2 = a.scale * LOG2E;
+  void* lds = smem + wave * X::LDS_BYTES;
+  float* pl = reinterpret_cast<float*>(smem + CA_WAVES * X::LDS_BYTES) + wave * 16 * PP;
+
+  f32x4 o[RT][OT];
+  float m_run[RT], l_run[RT];      // running maximum (log2 domain), this lane's share of the sum
+  typename X::Step step;
+  // key0, the last key, and the rows that chose the step's block
+  int key0 = 0, last = 0;
+  uint64_t w0 = 0, w1 = 0;
+  auto request = [&](int s, int& key0, int& last, uint64_t& w0, uint64_t& w1) {
+    if (s < prefix_steps) {
+      key0 = s * KT;
+      last = L - 1;
+      if (SPARSE) {
+        const int j = __builtin_amdgcn_readfirstlane((int)chosen[s / per_blk]);
+        key0 = j * a.block + s % per_blk * KT;
+        last = min(L, (j + 1) * a.block) - 1;
+        w0 = marks[2 * j];
+        w1 = marks[2 * j + 1];
+      }
+    } else {
+      key0 = L + (s - prefix_steps) * KT;
+      last = total - 1;
+    }
+    X::load_k(step, kb, key0, last, l, g);
+    X::load_v(step, vb, key0, last, l, g);
+  };
+  auto pass = [&](auto safe_tag) {
+    constexpr bool SAFE = decltype(safe_tag)::value;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      m_run[t] = -INFINITY;
+      l_run[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < OT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int stride = splits * CA_WAVES;
+    int s = sp * CA_WAVES + wave;
+    if (s < steps) request(s, key0, last, w0, w1);
+    for (; s < steps; s += stride) {
+      const int k0 = key0, k_last = last;
+      const uint64_t c0 = w0, c1 = w1;
+      const bool tail = s >= prefix_steps;
+      X::stage(step, lds, l, g);
+      f32x4 st[RT][SUBS];
+      bool sees[RT];
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const uint64_t w = node[t] < 64 ? c0 : c1;
+        sees[t] = node[t] >= 0 && (tail || !SPARSE || (w >> (node[t] & 63) & 1));
+        if (!SPARSE || __any(sees[t])) X::scores(st[t], step, q[t]);
+      }
+      if constexpr (X::LDS_BYTES > 0) {
+        if (s + stride < steps) request(s + stride, key0, last, w0, w1);
+      }
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        if (SPARSE && !__any(sees[t])) continue;
+        float mx = -INFINITY;
+        if (!tail && !SPARSE && k0 + KT - 1 <= k_last) {
+#pragma unroll
+          for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[t][sub][r]);
+        } else {
+#pragma unroll
+          for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int key = k0 + sub * 16 + 4 * g + r, j = key - L;
+              const uint64_t w = j < 64 ? aw0[t] : aw1[t];
+              const bool vis = sees[t] & (key <= k_last) & (!tail | (bool)(w >> (j & 63) & 1));
+              const float v = vis ? st[t][sub][r] : -INFINITY;
+              st[t][sub][r] = v;
+              mx = fmaxf(mx, v);
+              if (SAFE) pl[l * PP + sub * 16 + 4 * g + r] = vis ? 0.f : -1.f;
+            }
+        }
+        mx = xor16_max(mx);
+        mx = xor32_max(mx);
+        const float m_new = fmaxf(m_run[t], mx * scale_log2);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;     // nothing seen yet: weights 0, not NaN
+        const float alpha = m_new == m_run[t] ? 1.f : exp2_hw(m_run[t] - m_use);
+        m_run[t] = m_new;
+        float rs = 0.f;
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = exp2_hw(fmaf(st[t][sub][r], scale_log2, -m_use));
+            st[t][sub][r] = p;
+            rs += p;
+            if (SAFE) {
+              float* x = &pl[l * PP + sub * 16 + 4 * g + r];
+              if (!tail && !SPARSE && k0 + KT - 1 <= k_last) *x = p;
+              else if (*x == 0.f) *x = p;
+            }
+          }
+        l_run[t] = l_run[t] * alpha + rs;
+        if (!__all(alpha == 1.f)) {
+#pragma unroll
+          for (int d = 0; d < OT; ++d) o[t][d] *= alpha;
+        }
+        X::template add<SAFE>(o[t], st[t], step, lds, l, g);
+        if (SAFE) {
+          // values that are not finite, for the rows that see them (probability >= 0 or NaN in pl)
+          wave_lds_fence();
+          for (int key = 0; key < KT; ++key) {
+            const float p = pl[l * PP + key];
+            const T* row = vb + (int64_t)min(k0 + key, k_last) * DH;
+#pragma unroll
+            for (int d = 0; d < OT; ++d)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float v = Elem<T>::load(row, X::dim(d, g, r));
+                if (not_finite(v) && !(p < 0.f)) o[t][d][r] += p * v;
+              }
+          }
+          wave_lds_fence();
+        }
+      }
+      if (X::LDS_BYTES > 0) wave_lds_fence();
+      if constexpr (X::LDS_BYTES == 0) {
+        if (s + stride < steps) request(s + stride, key0, last, w0, w1);
+      }
+    }
+  };
+  pass(std::false_type{});
+  float odd = 0.f;
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int d = 0; d < OT; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) odd += o[t][d][r] * 0.f;
+  if (__any(odd != odd)) pass(std::true_type{});
+
+  // merge of the waves, tile by tile, in wave order
+  float* mo = reinterpret_cast<float*>(smem);                      // [wave][16][MP]
+  float* mml = mo + CA_WAVES * 16 * MP;                            // [wave][16][2]
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    l_run[t] = xor16_add(l_run[t]);
+    l_run[t] = xor32_add(l_run[t]);
+    __syncthreads();
+    float* row = mo + (wave * 16 + l) * MP;
+#pragma unroll
+    for (int d = 0; d < OT; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) row[X::dim(d, g, r)] = o[t][d][r];
+    if (g == 0) {
+      mml[(wave * 16 + l) * 2] = m_run[t];
+      mml[(wave * 16 + l) * 2 + 1] = l_run[t];
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < 16 * (DH / 4); idx += CA_THREADS) {
+      const int i = idx / (DH / 4), d = idx % (DH / 4) * 4, rr = r0 + t * 16 + i;
+      if (rr >= live_rows) continue;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < CA_WAVES; ++w) M = fmaxf(M, mml[(w * 16 + i) * 2]);
+      float ls = 0.f;
+      f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < CA_WAVES; ++w) {
+        const float mw = mml[(w * 16 + i) * 2], lw = mml[(w * 16 + i) * 2 + 1];
+        const float wt = mw == -INFINITY && lw == 0.f ? 0.f : exp2_hw(mw - (M == -INFINITY ? 0.f : M));
+        if (wt == 0.f && lw == lw) continue;
+        ls += wt * lw;
+        acc += wt * *reinterpret_cast<const f32x4*>(&mo[(w * 16 + i) * MP + d]);
+      }
+      const int64_t pair = (int64_t)b * a.Hkv + h, at = (pair * splits + sp) * rows + rr;
+      if (splits == 1) {
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * DH + (int64_t)(rr % a.G) * DH + d;
+        store4((T*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      } else {
+        *reinterpret_cast<f32x4*>(part_o + at * DH + d) = acc;
+      }
+      if (part_ml && d == 0) {
+        part_ml[at * 2] = M;
+        part_ml[at * 2 + 1] = ls;
+      }
+    }
+  }
+}
+
+// Log-sum-exp merge of the splits, in split order, four dims of one row per thread; row_ml (if
+// given) gets the rows' maximum and sum.
+__global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, int splits, int is_bf16,
+                                                                 const float* __restrict__ part_o,
+                                                                 const float* __restrict__ part_ml,
+                                                                 float* __restrict__ row_ml) {
+  const int h = blockIdx.y, b = blockIdx.z, per = a.Dh / 4;
+  const int idx = blockIdx.x * CA_THREADS + threadIdx.x, rr = idx / per, d = idx % per * 4;
+  if (rr >= max(0, min(a.n_q[b], a.nq_max)) * a.G) return;
+  const int rows = a.nq_max * a.G;
+  const int64_t pair = (int64_t)b * a.Hkv + h, base = pair * splits * rows + rr;
+  float M = -INFINITY;
+  for (int s = 0; s < splits; ++s) M = fmaxf(M, part_ml[(base + (int64_t)s * rows) * 2]);
+  float ls = 0.f;
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) {
+    const int64_t at = base + (int64_t)s * rows;
+    const float mw = part_ml[at * 2], lw = part_ml[at * 2 + 1];
+    const f32x4 x = *reinterpret_cast<const f32x4*>(part_o + at * a.Dh + d);
+    const float wt = mw == -INFINITY && lw == 0.f ? 0.f : exp2_hw(mw - (M == -INFINITY ? 0.f : M));
+    if (wt == 0.f && lw == lw) continue;
+    ls += wt * lw;
+    acc += wt * x;
+  }
+  const float inv = ls == 0.f ? 0.f : 1.f / ls;
+  const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * a.Dh + (int64_t)(rr % a.G) * a.Dh + d;
+  if (is_bf16) store4((uint16_t*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  else store4((float*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  if (row_ml && d == 0) {
+    row_ml[(pair * rows + rr) * 2] = M;
+    row_ml[(pair * rows + rr) * 2 + 1] = ls;
+  }
+}
+
+// The weight every slot received: S[row][key] once more, now with the rows' final maximum and sum,
+// p = 2^(s - m) / l, added over the rows.  A wave takes 16 SUBS keys, keeps them in registers and
+// goes through the query rows tile by tile (A = Q rows, B = K^T: lane (l, g) gets rows 4 g + r of
+// key l, so a column adds up within its lanes).
+template <typename T> struct ColSubs { static constexpr int n = 4; };
+template <> struct ColSubs<float> { static constexpr int n = 2; };
+
+template <typename T, int DH>
+__global__ __launch_bounds__(CA_THREADS) void slot_weights_kernel(CacheAttn a, const float* __restrict__ row_ml,
+                                                                  const float* __restrict__ w_in,
+                                                                  float* __restrict__ w_out, int64_t stride_wb,
+                                                                  int64_t stride_wh, float decay,
+                                                                  const float* __restrict__ row_weight) {
+  typedef Tile<T, DH> X;
+  constexpr int SUBS = ColSubs<T>::n, PER = X::SUBS;    // 16-key columns per wave, and per loaded step
+  constexpr int KEYS = CA_WAVES * SUBS * 16;
+  extern __shared__ float2 rows_mc[];                   // per row: maximum, row weight / sum
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int L = max(0, min(a.kv_len[b], a.kv_cap));
+  const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
+  if ((int)blockIdx.x * KEYS >= total) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+  const int l = lane & 15, g = lane >> 4;
+  const int live_rows = max(0, min(a.n_q[b], a.nq_max)) * a.G;
+  const int64_t pair = (int64_t)b * a.Hkv + h;
+  const int tiles = (live_rows + 15) / 16;
+  for (int r = threadIdx.x; r < tiles * 16; r += CA_THREADS) {
+    float2 mc = make_float2(INFINITY, 0.f);             // a row that saw nothing, or is none: weight 0
+    if (r < live_rows) {
+      const float* ml = row_ml + (pair * a.nq_max * a.G + r) * 2;
+      const float rw = row_weight ? row_weight[(int64_t)b * a.nq_max + r / a.G] : 1.f;
+      if (ml[1] != 0.f) mc = make_float2(ml[0] == -INFINITY ? 0.f : ml[0], rw / ml[1]);
+    }
+    rows_mc[r] = mc;
+  }
+  __syncthreads();
+  const int key0 = blockIdx.x * KEYS + wave * SUBS * 16;
+  if (key0 >= total) return;
+  const T* kb = (const T*)a.k + b * a.sb + h * a.sh;
+  typename X::Step step[SUBS / PER];
+#pragma unroll
+  for (int i = 0; i < SUBS / PER; ++i) X::load_k(step[i], kb, key0 + i * X::KT, total - 1, l, g);
+  const bool tail = key0 + SUBS * 16 > L;
+  const float scale_log2 = a.scale * LOG2E;
+  float col[SUBS];
+#pragma unroll
+  for (int s = 0; s < SUBS; ++s) col[s] = 0.f;
+  for (int t = 0; t < tiles; ++t) {
+    const int row = min(t * 16 + l, live_rows - 1), i = row / a.G, u = row - i * a.G;
+    typename X::Query q;
+    X::load(q, (const T*)a.q + (((int64_t)b * a.nq_max + i) * a.Hkv + h) * a.G * DH + (int64_t)u * DH, g);
+    float2 mc[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) mc[r] = rows_mc[t * 16 + 4 * g + r];
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      f32x4 st{0.f, 0.f, 0.f, 0.f};
+      X::col_scores(st, step[s / PER], s % PER, q);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        bool vis = t * 16 + 4 * g + r < live_rows;
+        if (tail) {
+          const int key = key0 + s * 16 + l, j = key - L;
+          if (vis && j >= 0) {
+            const int node = (t * 16 + 4 * g + r) / a.G;
+            const uint64_t* mp = a.mask + ((int64_t)b * a.nq_max + node) * ADT_MASK_WORDS;
+            vis = j < ADT_MAX_NODES && (mp[j >> 6] >> (j & 63) & 1);
+          }
+        }
+        const float p = exp2_hw(fmaf(st[r], scale_log2, -mc[r].x)) * mc[r].y;
+        col[s] += vis ? p : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < SUBS; ++s) {
+    col[s] = xor16_add(col[s]);
+    col[s] = xor32_add(col[s]);
+  }
+#pragma unroll
+  for (int s = 0; s < SUBS; ++s) {
+    const int key = key0 + s * 16 + l;
+    if (g == s && key < total) {
+      const int64_t at = b * stride_wb + h * stride_wh + key;
+      w_out[at] = key < L && w_in ? decay * w_in[at] + col[s] : col[s];
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- host
+static size_t align_up16(size_t x) { return (x + 15) / 16 * 16; }
+
+static int row_tiles(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+
+// Key splits: workgroups for about two rounds of the CUs (one where a workgroup fills its CU), but
+// at least two steps for every wave at the most keys the launch may meet.
+static int cache_splits(const CacheAttn& a, int B, int dtype) {
+  const int rows = a.nq_max * a.G, rt = row_tiles(rows), kt = dtype == ADT_BF16 ? 32 : 16;
+  const int64_t pairs = (int64_t)B * a.Hkv * ((rows + 16 * rt - 1) / (16 * rt));
+  int64_t keys = a.kv_cap;
+  if (a.block) keys = std::min<int64_t>(keys, (int64_t)a.n_sel * a.nq_max * a.block + ADT_MAX_NODES);
+  const int64_t most = (keys + 2 * CA_WAVES * kt - 1) / (2 * CA_WAVES * kt);
+  const int64_t want = ((rt == 4 ? 256 : 512) + pairs - 1) / pairs;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 64));
+}
+
+static size_t part_floats(const CacheAttn& a, int B, int splits) {
+  return (size_t)B * a.Hkv * splits * a.nq_max * a.G * (a.Dh + 2);
+}
+
+template <typename T, int DH, int RT, bool SPARSE>
+static void attn_rt(const CacheAttn& a, int B, int splits, float* part_o, float* part_ml, hipStream_t st) {
+  const int groups = (a.nq_max * a.G + 16 * RT - 1) / (16 * RT);
+  const size_t list = SPARSE ? align_up16((size_t)a.n_blk * 2) : 0;
+  cache_attn_kernel<T, DH, RT, SPARSE><<<dim3(a.Hkv * groups, B, splits), CA_THREADS, list, st>>>(a, splits, part_o, part_ml);
+}
+template <typename T, int DH>
+static void attn_dh(const CacheAttn& a, int B, int splits, float* part_o, float* part_ml, hipStream_t st) {
+  const int rt = row_tiles(a.nq_max * a.G);
+#define ADT_CA(RTV)                                                             \
+  if (a.block) attn_rt<T, DH, RTV, true>(a, B, splits, part_o, part_ml, st);    \
+  else attn_rt<T, DH, RTV, false>(a, B, splits, part_o, part_ml, st)
+  if (rt == 1) { ADT_CA(1); }
+  else if (rt == 2) { ADT_CA(2); }
+  else { ADT_CA(4); }
+#undef ADT_CA
+}
+
+// part: partials of `splits` splits (part_floats), row_ml: [B][Hkv][rows][2] or null
+static adt_status attn_passes(const CacheAttn& a, int B, int splits, float* part, float* row_ml, int dtype,
+                              hipStream_t st) {
+  float* part_o = splits > 1 ? part : nullptr;
+  float* part_ml = splits > 1 ? part + (size_t)B * a.Hkv * splits * a.nq_max * a.G * a.Dh : row_ml;
+  if (dtype == ADT_BF16) {
+    if (a.Dh == 128) attn_dh<uint16_t, 128>(a, B, splits, part_o, part_ml, st);
+    else attn_dh<uint16_t, 64>(a, B, splits, part_o, part_ml, st);
+  } else {
+    if (a.Dh == 128) attn_dh<float, 128>(a, B, splits, part_o, part_ml, st);
+    else attn_dh<float, 64>(a, B, splits, part_o, part_ml, st);
+  }
+  ADT_LAUNCH_CHECK();
+  if (splits > 1) {
+    const int threads = a.nq_max * a.G * (a.Dh / 4);
+    cache_merge_kernel<<<dim3((threads + CA_THREADS - 1) / CA_THREADS, a.Hkv, B), CA_THREADS, 0, st>>>(
+        a, splits, dtype == ADT_BF16, part_o, part_ml, row_ml);
+    ADT_LAUNCH_CHECK();
+  }
+  return ADT_OK;
+}
+
+// Workspace of attention over chosen blocks: scores, marks, partials.
+static size_t sparse_layout(const CacheAttn& a, int B, int dtype, size_t* marks, size_t* part) {
+  size_t off = align_up16(block_select_ws_bytes(B, a.Hkv, a.nq_max, a.n_blk));
+  *marks = off;
+  off += (size_t)B * a.Hkv * a.n_blk * ADT_MASK_WORDS * 8;
+  *part = off;
+  const int S = cache_splits(a, B, dtype);
+  return off + (S > 1 ? part_floats(a, B, S) * sizeof(float) : 0);
+}
+
+size_t sparse_attn_ws_bytes(const CacheAttn& a, int B, int dtype) {
+  size_t marks, part;
+  return sparse_layout(a, B, dtype, &marks, &part);
+}
+
+adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb, int64_t mh, int n_first, int n_last,
+                              int32_t* sel, int dtype, void* ws, hipStream_t st) {
+  size_t marks, part;
+  sparse_layout(a, B, dtype, &marks, &part);
+  uint64_t* mk = (uint64_t*)((char*)ws + marks);
+  adt_status e = launch_block_select(a.q, means, mb, mh, a.kv_len, a.n_q, B, a.Hkv, a.G, a.Dh, a.nq_max, a.kv_cap,
+                                     a.block, a.n_sel, n_first, n_last, dtype, (double*)ws, mk, sel, st);
+  if (e) return e;
+  a.marks = mk;
+  return attn_passes(a, B, cache_splits(a, B, dtype), (float*)((char*)ws + part), nullptr, dtype, st);
+}
+
+static size_t row_ml_bytes(const CacheAttn& a, int B) {
+  return align_up16((size_t)B * a.Hkv * a.nq_max * a.G * 2 * sizeof(float));
+}
+
+size_t weights_attn_ws_bytes(const CacheAttn& a, int B, int dtype) {
+  const int S = cache_splits(a, B, dtype);
+  return row_ml_bytes(a, B) + (S > 1 ? part_floats(a, B, S) * sizeof(float) : 0);
+}
+
+adt_status launch_weights_attn(const CacheAttn& a, int B, const float* w_in, float* w_out, int64_t stride_wb,
+                               int64_t stride_wh, float decay, const float* row_weight, int dtype, void* ws,
+                               hipStream_t st) {
+  float* row_ml = (float*)ws;
+  adt_status e = attn_passes(a, B, cache_splits(a, B, dtype), (float*)((char*)ws + row_ml_bytes(a, B)), row_ml, dtype, st);
+  if (e) return e;
+  const size_t lds = (size_t)(a.nq_max * a.G + 15) / 16 * 16 * sizeof(float2);
+#define ADT_SW(TV, DHV)                                                                                             \
+  slot_weights_kernel<TV, DHV><<<dim3((a.kv_cap + CA_WAVES * ColSubs<TV>::n * 16 - 1) / (CA_WAVES * ColSubs<TV>::n * 16), \
+                                      a.Hkv, B),                                                                    \
+                                 CA_THREADS, lds, st>>>(a, row_ml, w_in, w_out, stride_wb, stride_wh, decay, row_weight)
+  if (dtype == ADT_BF16) {
+    if (a.Dh == 128) ADT_SW(uint16_t, 128);
+    else ADT_SW(uint16_t, 64);
+  } else {
+    if (a.Dh == 128) ADT_SW(float, 128);
+    else ADT_SW(float, 64);
+  }
+#undef ADT_SW
+  ADT_LAUNCH_CHECK();
+  return ADT_OK;
+}
+
+}  // namespace adt

@@ -7,6 +7,7 @@
 // moves the rows.  Selecting is bound by its passes over the weights (they stay in the L2), moving
 // by memory: the kept rows are read once and written once.
 #include "../launch.h"
+#include "../rank.h"
 
 namespace adt {
 
@@ -25,10 +26,8 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const float* 
                                                                    int64_t stride_ws, const int32_t* __restrict__ kv_len,
                                                                    int kv_cap, int slices, int budget, int n_first,
                                                                    int n_last, int32_t* __restrict__ kept) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t wave_n[2][SEL_THREADS / WAVE];
-  __shared__ uint32_t pick[3];      // digit, keys above it, whether the digit's keys are just those needed
-  const int s = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = tid / WAVE, lane = tid % WAVE;
+  __shared__ RankScratch<SEL_THREADS> sh;
+  const int s = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int L = max(0, min(kv_len[b], kv_cap));
   if (kv_len[b] > kv_cap && tid == 0) dev_fail(DEVINV_KV_RANGE);
   int32_t* out = kept + ((int64_t)b * slices + s) * budget;
@@ -38,80 +37,10 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const float* 
   }
   const float* row = w + b * stride_wb + s * stride_ws;
   const int lo = n_first, hi = L - n_last;              // budget < L, so the middle is not empty
-  int need = budget - n_first - n_last;
-  // the key of the last slot that stays, digit by digit from the top: keys whose higher digits
-  // equal `prefix` are counted by their next digit
-  uint32_t prefix = 0, mask = 0;
-  bool all_equal = false;                               // every key with this prefix stays
-  for (int shift = 24; shift >= 0 && need > 0 && !all_equal; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int i = lo + tid; i < hi; i += SEL_THREADS) {
-      const uint32_t k = weight_key(row[i]);
-      if ((k & mask) == prefix) atomicAdd(&hist[k >> shift & 255], 1u);
-    }
-    __syncthreads();
-    if (wave == 0) {
-      // lane l holds the digits 255 - 4 l .. 252 - 4 l, so a prefix sum over lanes counts from the top
-      uint32_t c[4], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum += c[j] = hist[255 - 4 * lane - j];
-      uint32_t incl = sum;
-#pragma unroll
-      for (int o = 1; o < WAVE; o <<= 1) {
-        const uint32_t up = __shfl_up(incl, o, WAVE);
-        if (lane >= o) incl += up;
-      }
-      uint32_t above = incl - sum;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (above < (uint32_t)need && above + c[j] >= (uint32_t)need) {
-          pick[0] = 255 - 4 * lane - j;
-          pick[1] = above;
-          pick[2] = above + c[j] == (uint32_t)need;
-        }
-        above += c[j];
-      }
-    }
-    __syncthreads();
-    prefix |= pick[0] << shift;
-    mask |= 255u << shift;
-    need -= pick[1];
-    all_equal = pick[2];
-    __syncthreads();
-  }
-  // in slot order: a key above the prefix stays, and of those with the prefix the first `need`
-  uint32_t kept_n = 0, equal_n = 0;
-  for (int base = 0; base < L; base += SEL_THREADS) {
-    const int i = base + tid;
-    bool stays = i < lo || (i >= hi && i < L), equal = false;
-    if (i >= lo && i < hi && budget > n_first + n_last) {
-      const uint32_t k = weight_key(row[i]);
-      stays = (k & mask) > prefix;
-      equal = (k & mask) == prefix;
-    }
-    const uint64_t below = (1ull << lane) - 1;
-    const uint64_t eq = __ballot(equal);
-    if (lane == 0) wave_n[0][wave] = __popcll(eq);
-    __syncthreads();
-    uint32_t rank = equal_n + __popcll(eq & below), all_eq = 0;
-    for (int v = 0; v < SEL_THREADS / WAVE; ++v) {
-      if (v < wave) rank += wave_n[0][v];
-      all_eq += wave_n[0][v];
-    }
-    equal_n += all_eq;
-    stays = stays || (equal && rank < (uint32_t)need);
-    const uint64_t st = __ballot(stays);
-    if (lane == 0) wave_n[1][wave] = __popcll(st);
-    __syncthreads();
-    uint32_t at = kept_n + __popcll(st & below), all_st = 0;
-    for (int v = 0; v < SEL_THREADS / WAVE; ++v) {
-      if (v < wave) at += wave_n[1][v];
-      all_st += wave_n[1][v];
-    }
-    kept_n += all_st;
-    if (stays) out[at] = i;
-  }
+  const int need = budget - n_first - n_last;
+  auto key = [&](int i) { return weight_key(row[i]); };
+  const RankCut<uint32_t> cut = rank_cut<uint32_t, SEL_THREADS>(key, lo, hi, need, sh);
+  rank_emit(key, L, lo, hi, need == 0, cut, sh, [&](int at, int i) { out[at] = i; });
 }
 
 // Rows of the kept slots of one slice to its first slots: a workgroup takes a stripe of STRIPE

@@ -305,6 +305,35 @@ adt_status launch_block_keys(const void* k, int64_t sb, int64_t sh, const int32_
                              int Hkv, int Dh, int block, int kv_cap, float* means, int64_t mb, int64_t mh, int dtype,
                              hipStream_t st);
 
+size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk);   // scores
+// Marks the blocks each row takes (marks [B][Hkv][n_blk][ADT_MASK_WORDS], bit i: row i) and lists
+// them in sel (may be null).
+adt_status launch_block_select(const void* q, const float* means, int64_t mb, int64_t mh, const int32_t* kv_len,
+                               const int32_t* n_q, int B, int Hkv, int G, int Dh, int nq_max, int kv_cap, int block,
+                               int n_sel, int n_first, int n_last, int dtype, double* score, uint64_t* marks,
+                               int32_t* sel, hipStream_t st);
+
+// cache_attn.hip
+// Attention of G query heads per key-value head; block = 0: over the whole prefix.
+struct CacheAttn {
+  const void *q, *k, *v;
+  int64_t sb, sh;
+  const int32_t *kv_len, *n_q, *n_tail;
+  const uint64_t* mask;
+  int Hkv, G, Dh, nq_max, kv_cap;
+  float scale;
+  void* out;
+  int block = 0, n_blk = 0, n_sel = 0;
+  const uint64_t* marks = nullptr;
+};
+size_t sparse_attn_ws_bytes(const CacheAttn& a, int B, int dtype);
+adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb, int64_t mh, int n_first, int n_last,
+                              int32_t* sel, int dtype, void* ws, hipStream_t st);
+size_t weights_attn_ws_bytes(const CacheAttn& a, int B, int dtype);
+adt_status launch_weights_attn(const CacheAttn& a, int B, const float* w_in, float* w_out, int64_t stride_wb,
+                               int64_t stride_wh, float decay, const float* row_weight, int dtype, void* ws,
+                               hipStream_t st);
+
 // evict.hip
 struct EvictMove {
   const void *k, *v;

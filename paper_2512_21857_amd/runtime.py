@@ -234,6 +234,89 @@ def _weight_strides(what: str, w: torch.Tensor, like: torch.Tensor):
     return (w.stride(0) if B > 1 else heads * sh), sh
 
 
+def _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap, out):
+    """Checks what both attentions over a cache share; (dtype, sizes, strides, out)."""
+    dt = _dt(q)
+    B, n, H, Dh = q.shape
+    _want("q", q, q, q.dtype, (B, n, H, Dh))
+    _want("k_cache", k_cache, q, q.dtype)
+    if k_cache.dim() != 4 or k_cache.shape[0] != B or k_cache.shape[3] != Dh or k_cache.shape[2] < kv_cap:
+        raise ValueError(f"caches {(B, 'heads', kv_cap, Dh)} expected, not {tuple(k_cache.shape)}")
+    sb, sh = _cache_strides(k_cache, v_cache)
+    for name, t in (("kv_len", kv_len), ("n_q", n_q), ("n_tail", n_tail)):
+        _want(name, t, q, torch.int32, (B,))
+    _want("mask", mask, q, torch.int64, (B, n, abi.MASK_WORDS))
+    out = torch.empty_like(q) if out is None else out
+    _want("out", out, q, q.dtype, (B, n, H, Dh))
+    return dt, B, n, H, k_cache.shape[1], Dh, sb, sh, out
+
+
+def sparse_tree_attn_workspace(B: int, H: int, Hkv: int, Dh: int, nq_max: int, kv_cap: int, block: int, n_sel: int,
+                               dtype: torch.dtype = torch.bfloat16, device="cuda") -> torch.Tensor:
+    dt = abi.BF16 if dtype == torch.bfloat16 else abi.F32
+    n = lib().adt_sparse_tree_attn_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, block, n_sel, dt)
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def sparse_tree_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, means: torch.Tensor,
+                     kv_len: torch.Tensor, n_q: torch.Tensor, n_tail: torch.Tensor, mask: torch.Tensor, kv_cap: int,
+                     block: int, n_sel: int, n_first: int = 1, n_last: int = 1, scale: Optional[float] = None,
+                     out: Optional[torch.Tensor] = None, sel: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Tree attention of q [B][n][H][Dh] over caches [B][Hkv][S][Dh] in which every row sees n_sel
+    blocks of the prefix: the first n_first, the last n_last and the best by means (block_keys of
+    the cache).  sel: int32 [B][n][Hkv][n_sel], gets the chosen blocks."""
+    dt, B, n, H, Hkv, Dh, sb, sh, out = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap, out)
+    _want("means", means, q, torch.float32)
+    if means.dim() != 4 or means.shape[:2] != (B, Hkv) or means.shape[3] != Dh or means.shape[2] * block < kv_cap:
+        raise ValueError(f"means of {kv_cap} slots in blocks of {block} expected, not {tuple(means.shape)}")
+    mb, mh = _cache_strides(means)
+    _want("sel", sel, q, torch.int32, (B, n, Hkv, n_sel))
+    if workspace is None:
+        workspace = sparse_tree_attn_workspace(B, H, Hkv, Dh, n, kv_cap, block, n_sel, q.dtype, q.device)
+    _want("workspace", workspace, q, torch.uint8)
+    scale = 1.0 / float(np.sqrt(Dh)) if scale is None else scale
+    _on_device(lib().adt_sparse_tree_attn, q.device, _p(q), _p(k_cache), _p(v_cache), sb, sh, _p(means), mb, mh,
+               _p(kv_len), _p(n_q), _p(n_tail), _p(mask), B, H, Hkv, Dh, n, kv_cap, block, n_sel, n_first, n_last, scale,
+               dt, _p(out), _p(sel), _p(workspace), workspace.numel())
+    return out
+
+
+def tree_attn_weights_workspace(B: int, H: int, Hkv: int, Dh: int, nq_max: int, kv_cap: int,
+                                dtype: torch.dtype = torch.bfloat16, device="cuda") -> torch.Tensor:
+    dt = abi.BF16 if dtype == torch.bfloat16 else abi.F32
+    n = lib().adt_tree_attn_weights_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, dt)
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def tree_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len: torch.Tensor,
+                      n_q: torch.Tensor, n_tail: torch.Tensor, mask: torch.Tensor, kv_cap: int,
+                      weights: Optional[torch.Tensor] = None, decay: float = 1.0,
+                      row_weight: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                      out: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None):
+    """Tree attention of q [B][n][H][Dh] over caches [B][Hkv][S][Dh]; also weights_out fp32
+    [B][Hkv][S] = decay * weights + the softmax weight each slot received (row i counting
+    row_weight[b][i]).  weights_out defaults to weights, in place, or to new zeros.  Returns
+    (out, weights_out)."""
+    dt, B, n, H, Hkv, Dh, sb, sh, out = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap, out)
+    if weights_out is None:
+        weights_out = weights if weights is not None else torch.zeros(k_cache.shape[:3], dtype=torch.float32,
+                                                                      device=q.device)
+    wb, wh = _weight_strides("weights_out", weights_out, k_cache)
+    if weights is not None and _weight_strides("weights", weights, k_cache) != (wb, wh):
+        raise ValueError("weights and weights_out must have the same strides")
+    _want("row_weight", row_weight, q, torch.float32, (B, n))
+    if workspace is None:
+        workspace = tree_attn_weights_workspace(B, H, Hkv, Dh, n, kv_cap, q.dtype, q.device)
+    _want("workspace", workspace, q, torch.uint8)
+    scale = 1.0 / float(np.sqrt(Dh)) if scale is None else scale
+    _on_device(lib().adt_tree_attn_weights, q.device, _p(q), _p(k_cache), _p(v_cache), sb, sh, _p(kv_len), _p(n_q),
+               _p(n_tail), _p(mask), B, H, Hkv, Dh, n, kv_cap, scale, dt, _p(out), _p(weights), _p(weights_out), wb, wh,
+               decay, _p(row_weight), _p(workspace), workspace.numel())
+    return out, weights_out
+
+
 def kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor, kv_len: torch.Tensor, budget: int,
              n_first: int = 0, n_last: int = 0, k_out: Optional[torch.Tensor] = None,
              v_out: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,

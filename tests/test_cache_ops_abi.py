@@ -86,3 +86,104 @@ def test_rope_freqs_refusals(L, kw, code):
     kw = {"rot": 64, "scaling": 0, **kw}
     assert freqs(L, kw.pop("rot"), kw.pop("scaling"), **kw)[0] == getattr(abi, code)
     assert L.adt_rope_freqs(None, None, None) == abi.E_ARG
+
+
+KEYS = dict(k=FAKE, sb=2 * 64 * 100, sh=64 * 100, start=None, kv_len=FAKE, B=2, Hkv=2, Dh=64, block=32, cap=100, means=FAKE,
+            mb=2 * 64 * 4, mh=64 * 4, dtype=1, stream=None)
+
+
+@pytest.mark.parametrize("changed,code", [
+    (dict(k=None), "E_ARG"), (dict(kv_len=None), "E_ARG"), (dict(means=None), "E_ARG"), (dict(dtype=-1), "E_ARG"),
+    (dict(B=0), "E_ARG"), (dict(Hkv=70000), "E_ARG"), (dict(Dh=96), "E_SHAPE"), (dict(block=48), "E_SHAPE"),
+    (dict(block=0), "E_SHAPE"), (dict(block=16), "E_SHAPE"), (dict(sh=64 * 99), "E_SHAPE"), (dict(mh=64 * 3), "E_SHAPE"),
+    (dict(sb=64), "E_SHAPE"), (dict(mb=64 * 4), "E_SHAPE"), (dict(k=FAKE + 8), "E_SHAPE"), (dict(means=FAKE + 4), "E_SHAPE"),
+    (dict(sh=64 * 100 + 4, sb=4 * 64 * 100), "E_SHAPE"),
+])
+def test_block_keys_refusals(L, changed, code):
+    from paper_2512_21857_amd import abi
+    assert call(L.adt_block_keys, KEYS, **changed) == getattr(abi, code), changed
+    assert "block_keys" in abi.last_error()
+
+
+ATTN = dict(q=FAKE, k=FAKE, v=FAKE, sb=2 * 64 * 100, sh=64 * 100)
+SIZES = dict(kv_len=FAKE, n_q=FAKE, n_tail=FAKE, mask=FAKE, B=2, H=4, Hkv=2, Dh=64, nq_max=8, cap=100)
+SPARSE = {**ATTN, **dict(means=FAKE, mb=2 * 64 * 4, mh=64 * 4), **SIZES,
+          **dict(block=32, n_sel=3, n_first=1, n_last=1, scale=0.125, dtype=1, out=FAKE, sel=None, ws=FAKE, ws_bytes=1 << 30,
+                 stream=None)}
+RATED = {**ATTN, **SIZES, **dict(scale=0.125, dtype=1, out=FAKE, w_in=None, w_out=FAKE, wb=200, wh=100, decay=1.0, rw=None,
+                                 ws=FAKE, ws_bytes=1 << 30, stream=None)}
+COMMON = [
+    (dict(q=None), "E_ARG"), (dict(mask=None), "E_ARG"), (dict(n_tail=None), "E_ARG"), (dict(out=None), "E_ARG"),
+    (dict(dtype=3), "E_ARG"), (dict(B=0), "E_ARG"), (dict(H=0), "E_ARG"), (dict(Hkv=0), "E_ARG"), (dict(H=5), "E_SHAPE"),
+    (dict(Dh=96), "E_SHAPE"), (dict(nq_max=129), "E_CAPACITY"), (dict(nq_max=0), "E_CAPACITY"),
+    (dict(nq_max=128, H=256, Hkv=2), "E_CAPACITY"), (dict(sh=64 * 99), "E_SHAPE"), (dict(sb=64 * 100), "E_SHAPE"),
+    (dict(k=FAKE + 2), "E_SHAPE"), (dict(out=FAKE + 8), "E_SHAPE"), (dict(sh=64 * 100 + 4, sb=4 * 64 * 100), "E_SHAPE"),
+    (dict(scale=0.0), "E_ARG"), (dict(scale=math.inf), "E_ARG"), (dict(ws=None), "E_CAPACITY"), (dict(ws=FAKE + 4), "E_SHAPE"),
+    (dict(ws_bytes=64), "E_CAPACITY"),
+]
+
+
+@pytest.mark.parametrize("changed,code", COMMON + [
+    (dict(means=None), "E_ARG"), (dict(block=16), "E_SHAPE"), (dict(n_sel=0), "E_ARG"), (dict(n_first=2, n_last=2), "E_ARG"),
+    (dict(n_first=-1), "E_ARG"), (dict(mh=64 * 3), "E_SHAPE"), (dict(means=FAKE + 4), "E_SHAPE"),
+    (dict(B=1, cap=16385 * 32, sh=64 * 16385 * 32, mh=64 * 16385), "E_CAPACITY"),
+])
+def test_sparse_tree_attn_refusals(L, changed, code):
+    from paper_2512_21857_amd import abi
+    assert call(L.adt_sparse_tree_attn, SPARSE, **changed) == getattr(abi, code), changed
+    assert "sparse_tree_attn" in abi.last_error()
+
+
+@pytest.mark.parametrize("changed,code", COMMON + [
+    (dict(w_out=None), "E_ARG"), (dict(decay=math.nan), "E_ARG"), (dict(wh=99), "E_SHAPE"), (dict(wb=100), "E_SHAPE"),
+])
+def test_tree_attn_weights_refusals(L, changed, code):
+    from paper_2512_21857_amd import abi
+    assert call(L.adt_tree_attn_weights, RATED, **changed) == getattr(abi, code), changed
+    assert "tree_attn_weights" in abi.last_error()
+
+
+def test_attention_workspaces(L):
+    """Sizes for what the calls take, 0 for what they refuse."""
+    sparse = lambda *a: L.adt_sparse_tree_attn_workspace_size(*a)       # noqa: E731
+    rated = lambda *a: L.adt_tree_attn_weights_workspace_size(*a)       # noqa: E731
+    assert sparse(1, 32, 8, 128, 61, 4096, 64, 16, 1) > 0 and rated(1, 32, 8, 128, 61, 4096, 1) > 0
+    for bad in ((0, 32, 8, 128, 61, 4096), (1, 33, 8, 128, 61, 4096), (1, 32, 8, 96, 61, 4096), (1, 32, 8, 128, 129, 4096),
+                (1, 32, 8, 128, 61, 0)):
+        assert sparse(*bad, 64, 16, 1) == 0 and rated(*bad, 1) == 0
+    assert sparse(1, 32, 8, 128, 61, 4096, 48, 16, 1) == 0 and sparse(1, 32, 8, 128, 61, 4096, 64, 0, 1) == 0
+    assert rated(1, 32, 8, 128, 61, 4096, 2) == 0
+
+
+EVICT = dict(k=FAKE, v=FAKE, w=FAKE, sb=2 * 64 * 100, ss=64 * 100, wb=200, ws=100, kv_len=FAKE, B=2, slices=2, Dh=64, cap=100,
+             budget=40, n_first=4, n_last=8, ko=2 * FAKE, vo=2 * FAKE, wo=2 * FAKE, osb=2 * 64 * 40, oss=64 * 40, owb=80, ows=40,
+             kept=FAKE, new_len=FAKE, dtype=1, stream=None)
+
+
+@pytest.mark.parametrize("changed,code", [
+    (dict(k=None), "E_ARG"), (dict(w=None), "E_ARG"), (dict(wo=None), "E_ARG"), (dict(kept=None), "E_ARG"),
+    (dict(new_len=None), "E_ARG"), (dict(dtype=2), "E_ARG"), (dict(slices=0), "E_ARG"), (dict(budget=0), "E_ARG"),
+    (dict(n_first=-1), "E_ARG"), (dict(n_first=20, n_last=21), "E_ARG"), (dict(Dh=65), "E_SHAPE"),
+    (dict(Dh=8200, sb=1 << 30, ss=1 << 22, osb=1 << 30, oss=1 << 22), "E_SHAPE"), (dict(ko=FAKE), "E_ARG"),
+    (dict(ko=FAKE, vo=FAKE, wo=FAKE), "E_SHAPE"), (dict(ss=64 * 99), "E_SHAPE"), (dict(ws=99), "E_SHAPE"),
+    (dict(oss=64 * 39), "E_SHAPE"), (dict(ows=39), "E_SHAPE"), (dict(osb=64 * 40), "E_SHAPE"), (dict(wb=100), "E_SHAPE"),
+    (dict(k=FAKE + 8), "E_SHAPE"), (dict(ss=64 * 100 + 4, sb=4 * 64 * 100), "E_SHAPE"),
+])
+def test_kv_evict_refusals(L, changed, code):
+    from paper_2512_21857_amd import abi
+    assert call(L.adt_kv_evict, EVICT, **changed) == getattr(abi, code), changed
+    assert "kv_evict" in abi.last_error()
+
+
+WCOMPACT = dict(w=FAKE, B=2, slices=2, wb=200, ws=100, kv_len=FAKE, cap=100, path=FAKE, path_stride=5, n_acc=FAKE, a_max=4,
+                stream=None)
+
+
+@pytest.mark.parametrize("changed,code", [
+    (dict(w=None), "E_ARG"), (dict(path=None), "E_ARG"), (dict(B=0), "E_ARG"), (dict(a_max=128, path_stride=200), "E_CAPACITY"),
+    (dict(a_max=5), "E_CAPACITY"), (dict(ws=99), "E_SHAPE"), (dict(wb=100), "E_SHAPE"),
+])
+def test_weights_compact_refusals(L, changed, code):
+    from paper_2512_21857_amd import abi
+    assert call(L.adt_weights_compact, WCOMPACT, **changed) == getattr(abi, code), changed
+    assert call(L.adt_weights_compact, WCOMPACT, a_max=0) == abi.OK

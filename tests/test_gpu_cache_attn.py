@@ -1,0 +1,372 @@
+"""Attention over a long cache on the GPU (chosen blocks, rated slots) against plain 64-bit
+implementations.
+
+Tolerances, per element, from the roundings on the way: a score is a sum of Dh products in fp32,
+off by at most ds = Dh 2^-24 scale sum |q_d k_d|, so a probability by 2 ds + 2^-20 of itself
+(numerator and sum; the exponential's and the factors' ulps in the 2^-20); in bf16 it then enters
+the second product rounded, 2^-8 of itself at most; that product and the merges add up to 2^-24 per
+term; the output's own rounding is 2^-8 (bf16) or 2^-24 of it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def rt():
+    from paper_2512_21857_amd import runtime
+    assert torch.cuda.is_available()
+    return runtime
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, dtype, *shape):
+    return torch.empty(*shape, device="cuda").normal_(generator=g).to(DT[dtype])
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+
+
+def tree_paths(n, rng):
+    """[n][n] truth values: node j on the path from the root to node i of a random tree."""
+    p = np.zeros((n, n), dtype=bool)
+    for i in range(n):
+        if i:
+            p[i] = p[rng.integers(max(0, i - 12), i)]
+        p[i, i] = True
+    return p
+
+
+def packed(paths, n):
+    w = np.zeros((n, 2), dtype=np.uint64)
+    for i, j in zip(*np.nonzero(paths)):
+        w[i, j // 64] |= np.uint64(1) << np.uint64(j % 64)
+    return w.view(np.int64)
+
+
+class Case:
+    """Inputs of one call; caches may be one layer of a larger allocation."""
+
+    def __init__(self, dtype, H, Hkv, Dh, n, L, rows=None, cap=None, seed=1, layers=0, q_scale=1.0):
+        g, rng = gen(seed), np.random.default_rng(seed)
+        self.dtype, self.H, self.Hkv, self.Dh, self.n, self.L, self.B = dtype, H, Hkv, Dh, n, L, len(L)
+        self.rows = rows or [max(1, n - b * (n // 3)) for b in range(self.B)]
+        self.tails = [min(n, r + (1 if b % 2 else 0)) for b, r in enumerate(self.rows)]
+        self.cap = cap or max(l + t for l, t in zip(L, self.tails)) + 5
+        shape = (self.B, layers, Hkv, self.cap, Dh) if layers else (self.B, Hkv, self.cap, Dh)
+        self.kbig, self.vbig = normal(g, dtype, *shape), normal(g, dtype, *shape)
+        self.k, self.v = (self.kbig[:, 1], self.vbig[:, 1]) if layers else (self.kbig, self.vbig)
+        self.q = (q_scale * torch.empty(self.B, n, H, Dh, device="cuda").normal_(generator=g)).to(DT[dtype])
+        self.paths = [tree_paths(n, rng) for _ in range(self.B)]
+        for b in range(self.B):
+            # what lies behind the tail is never read
+            self.k[b, :, L[b] + self.tails[b]:] = math.nan
+            self.v[b, :, L[b] + self.tails[b]:] = math.nan
+        self.mask = torch.from_numpy(np.stack([packed(p, n) for p in self.paths])).cuda()
+        self.scale = 1 / math.sqrt(Dh)
+
+    def dev(self):
+        return i32(self.L), i32(self.rows), i32(self.tails), self.mask
+
+    def tail_see(self, b):
+        """[rows][tails]: what the rows see of the tree's slots, as the mask's bits say."""
+        m = self.mask[b].cpu().numpy().view(np.uint64)
+        t = [[bool(int(m[i, j // 64]) >> (j % 64) & 1) for j in range(self.tails[b])] for i in range(self.rows[b])]
+        return torch.tensor(t, dtype=torch.bool, device="cuda").view(self.rows[b], self.tails[b])
+
+
+def attend(c, b, h, see):
+    """Outputs [rows][G][Dh], weights [rows][G][slots] and their tolerances, in 64 bits."""
+    m, L, T, G = c.rows[b], c.L[b], c.L[b] + c.tails[b], c.H // c.Hkv
+    q = c.q[b, :m, h * G: (h + 1) * G].double().reshape(m * G, c.Dh)
+    k, v = c.k[b, h, :T].double(), c.v[b, h, :T].double()
+    s = see.repeat_interleave(G, 0)
+    k0, v0 = torch.nan_to_num(k, 0, 0, 0), torch.nan_to_num(v, 0, 0, 0)
+    x = (q @ k.t().contiguous() * c.scale).masked_fill(~s, -math.inf)
+    ds = torch.where(s, q.abs() @ k0.abs().t().contiguous(), torch.zeros_like(x)).amax(1, keepdim=True)
+    ds = ds * (c.scale * c.Dh * 2.0 ** -24)
+    top = x.amax(1, keepdim=True)
+    e = torch.exp(x - torch.where(top == -math.inf, torch.zeros_like(top), top))
+    total = e.sum(1, keepdim=True)
+    p = torch.where(~s | (total == 0), torch.zeros_like(e), e / total)     # an unseen slot has no weight
+    # a value that is not finite counts only where it is seen
+    pv = p @ v0
+    odd = ~torch.isfinite(v)
+    if odd.any():
+        for j in odd.any(1).nonzero().flatten().tolist():
+            pv = torch.where(s[:, j: j + 1] & odd[j][None], pv + p[:, j: j + 1] * v[j][None], pv)
+    terms = T + 8
+    rel = 2 * ds + 2.0 ** -20 + terms * 2.0 ** -24 + (2.0 ** -8 if c.dtype == "bf16" else 0.0)
+    tol = rel * (torch.nan_to_num(p) @ v0.abs()) + STEP[c.dtype] * pv.abs() + 1e-30
+    wtol = torch.nan_to_num(p) * (2 * ds + 2.0 ** -20 + terms * 2.0 ** -24)
+    return pv.view(m, G, c.Dh), tol.view(m, G, c.Dh), p.view(m, G, T), wtol.view(m, G, T)
+
+
+def close(got, want, tol, what):
+    got = got.double()
+    same = (got == want) | (torch.isnan(got) & torch.isnan(want))
+    bad = ~(same | ((got - want).abs() <= tol))
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()}, off by {(got - want).abs()[bad].max().item():.3e}"
+
+
+def choose(c, b, h, means, block, n_sel, first, last):
+    """[rows][blocks] truth values: the blocks each row takes."""
+    m, G, L = c.rows[b], c.H // c.Hkv, c.L[b]
+    n = -(-L // block)
+    q = c.q[b, :m, h * G: (h + 1) * G].double().sum(1)
+    score = (q @ means[b, h, :n].double().t().contiguous()).cpu().numpy()
+    out = np.zeros((m, n), dtype=bool)
+    for i in range(m):
+        if n <= n_sel:
+            out[i] = True
+            continue
+        mid = sorted(range(first, n - last), key=lambda j: (score[i, j] != score[i, j], -score[i, j], j))
+        out[i, :first] = True
+        out[i, n - last:] = True
+        out[i, mid[: n_sel - first - last]] = True
+    return out
+
+
+def check_sparse(rt, c, block, n_sel, first=1, last=1, means=None, kv_cap=None, out=None):
+    kv_len, n_q, n_tail, mask = c.dev()
+    means = rt.block_keys(c.k, kv_len, block) if means is None else means
+    out = torch.full_like(c.q, 3.0)
+    sel = torch.full((c.B, c.n, c.Hkv, n_sel), -7, dtype=torch.int32, device="cuda")
+    got = rt.sparse_tree_attn(c.q, c.k, c.v, means, kv_len, n_q, n_tail, mask, kv_cap or c.cap, block, n_sel, first, last,
+                              out=out, sel=sel)
+    assert got is out
+    G = c.H // c.Hkv
+    for b in range(c.B):
+        m = c.rows[b]
+        n = -(-c.L[b] // block)
+        assert torch.all(out[b, m:] == 3.0) and torch.all(sel[b, m:] == -7)
+        for h in range(c.Hkv):
+            took = choose(c, b, h, means, block, n_sel, first, last)
+            for i in range(m):
+                want = np.nonzero(took[i])[0].tolist()
+                assert sel[b, i, h].tolist() == want + [-1] * (n_sel - len(want)), (b, i, h)
+            blk = torch.from_numpy(took).cuda().repeat_interleave(block, 1)[:, : c.L[b]]
+            want, tol, _, _ = attend(c, b, h, torch.cat([blk, c.tail_see(b)], 1))
+            close(out[b, :m, h * G: (h + 1) * G], want, tol, f"sparse b={b} h={h} L={c.L[b]} rows={m}")
+    return out
+
+
+SPARSE = [
+    # H, Hkv, Dh, n, L, block, n_sel, first, last
+    (8, 8, 128, 1, [1000], 64, 5, 1, 1),
+    (32, 8, 128, 1, [3001, 40, 0], 64, 7, 1, 2),
+    (8, 2, 64, 5, [513, 512, 1, 31], 32, 3, 1, 1),          # 20 rows: two tiles
+    (4, 4, 64, 17, [300, 777], 32, 4, 0, 1),
+    (4, 1, 128, 13, [2000, 129], 128, 4, 2, 2),             # only the ends
+    (6, 2, 128, 61, [1500, 1499], 32, 12, 1, 1),            # 183 rows: three groups of 64
+    (5, 5, 64, 128, [2345], 64, 9, 0, 0),
+    (16, 1, 64, 128, [700], 32, 6, 1, 1),                   # 2048 rows of one key-value head
+    (2, 2, 64, 3, [5000], 32, 150, 3, 5),                   # nearly all
+    (2, 2, 128, 2, [100], 32, 40, 0, 0),                    # fewer blocks than asked for
+    (3, 3, 64, 7, [64, 65, 63], 64, 1, 0, 1),               # one block
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv,Dh,n,L,block,n_sel,first,last", SPARSE)
+def test_sparse_tree_attn(rt, dtype, H, Hkv, Dh, n, L, block, n_sel, first, last):
+    print(f"sparse {dtype} H={H}/{Hkv} Dh={Dh} n={n} L={L} block={block} sel={n_sel}", flush=True)
+    check_sparse(rt, Case(dtype, H, Hkv, Dh, n, L, seed=n + len(L)), block, n_sel, first, last)
+
+
+def test_sparse_more_blocks_than_lds_keys(rt):
+    """More than 4096 blocks: the selection reads its keys anew; and many splits."""
+    check_sparse(rt, Case("bf16", 2, 1, 64, 2, [140000], seed=4), 32, 33, 1, 1)
+
+
+def test_sparse_layer_of_a_larger_cache(rt):
+    check_sparse(rt, Case("bf16", 4, 2, 64, 9, [400, 333], layers=3), 32, 4)
+
+
+def test_sparse_ties_take_the_lower_block(rt):
+    c = Case("bf16", 4, 2, 64, 3, [640], seed=5)
+    means = torch.zeros(1, 2, -(-c.cap // 32), 64, device="cuda")     # every score the same
+    check_sparse(rt, c, 32, 6, 1, 1, means=means)
+    means[:, :, 7] = math.nan                                          # NaN is below every number
+    means[:, :, 3:5] = 1e30
+    check_sparse(rt, c, 32, 6, 1, 1, means=means)
+    means[:] = math.nan
+    check_sparse(rt, c, 32, 6, 0, 0, means=means)
+
+
+def test_sparse_near_scores_take_the_better_block(rt):
+    """Means of two blocks apart by one fp32 step in one dim: double tells them apart for every row."""
+    c = Case("f32", 2, 2, 64, 40, [640], seed=6)
+    means = torch.empty(1, 2, -(-c.cap // 32), 64, device="cuda").normal_(generator=gen(60))
+    means[:, :, 2:18] = means[:, :, 2:3]
+    for j in range(2, 18):
+        means[:, :, j, 0] = torch.tensor(1.0 + (j * 7 % 16) * 2.0 ** -23, device="cuda")
+    check_sparse(rt, c, 32, 8, 1, 1, means=means)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sparse_values_that_are_not_finite(rt, dtype):
+    """Infinities and NaN in keys and values reach only the rows that see their slots."""
+    c = Case(dtype, 4, 2, 64, 20, [640, 0], rows=[20, 20], seed=7)
+    means = rt.block_keys(c.k, i32(c.L), 32)
+    c.v[0, :, 100] = math.nan
+    c.v[0, :, 333, 5] = math.inf
+    c.v[0, 1, 500, 9] = -math.inf
+    c.v[0, :, 640 + 7] = math.inf               # a tree node's
+    c.k[0, 0, 200] = math.nan
+    c.v[1, :, 3] = math.nan
+    c.k[1, 1, 9] = math.inf
+    out = check_sparse(rt, c, 32, 5, 0, 1, means=means)
+    assert torch.isfinite(out[0].float()).any() and not torch.isfinite(out[0].float()).all()
+
+
+def test_sparse_rows_that_see_nothing(rt):
+    c = Case("bf16", 4, 2, 128, 6, [0, 40], rows=[6, 6], seed=8)
+    c.mask[0, 2:4] = 0
+    c.mask[1, 0] = 0
+    out = check_sparse(rt, c, 32, 1, 0, 1)
+    assert not out[0, 2:4].any()
+
+
+def test_sparse_no_rows_and_clamped_counts(rt):
+    c = Case("bf16", 4, 2, 64, 6, [100, 90, 80], rows=[0, 6, 3], seed=9)
+    check_sparse(rt, c, 32, 2)
+
+
+# ---------------------------------------------------------------------------- rated slots
+def check_weights(rt, c, decay=1.0, rated=False, w_in="given", place=False, seed=3):
+    kv_len, n_q, n_tail, mask = c.dev()
+    g = gen(seed)
+    w = torch.rand(c.B, c.Hkv, c.cap, generator=g, device="cuda")
+    for b in range(c.B):
+        w[b, :, c.L[b]:] = math.nan                         # earlier weight of new slots is not read
+    rating = torch.rand(c.B, c.n, generator=g, device="cuda") if rated else None
+    w0 = w.clone()
+    wo = w if place else torch.full_like(w, -5.0)
+    out = torch.full_like(c.q, 3.0)
+    got, gw = rt.tree_attn_weights(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, c.cap, weights=None if w_in is None else w,
+                                   decay=decay, row_weight=rating, out=out, weights_out=wo)
+    assert got is out and gw is wo
+    G = c.H // c.Hkv
+    for b in range(c.B):
+        m, L, T = c.rows[b], c.L[b], c.L[b] + c.tails[b]
+        assert torch.all(out[b, m:] == 3.0)
+        assert torch.all((wo[b, :, T:] == -5.0) | torch.isnan(wo[b, :, T:]))
+        see = torch.cat([torch.ones(m, L, dtype=torch.bool, device="cuda"), c.tail_see(b)], 1)
+        r = rating[b, :m].double() if rated else torch.ones(m, dtype=torch.float64, device="cuda")
+        for h in range(c.Hkv):
+            want, tol, p, ptol = attend(c, b, h, see)
+            close(out[b, :m, h * G: (h + 1) * G], want, tol, f"rated b={b} h={h} L={L} rows={m}")
+            add = (r[:, None, None] * p).sum((0, 1))
+            atol = (r[:, None, None] * ptol).sum((0, 1)) + (m * G + 2) * 2.0 ** -24 * add
+            if w_in is not None:
+                add[:L] += decay * w0[b, h, :L].double()
+                atol[:L] += 2.0 ** -23 * add[:L].abs()
+            close(wo[b, h, :T], add, atol + 1e-30, f"weights b={b} h={h} L={L} rows={m}")
+    return out, wo
+
+
+RATED = [
+    (8, 8, 128, 1, [1000]),
+    (32, 8, 128, 1, [3001, 40, 0]),
+    (8, 2, 64, 5, [513, 512, 1, 31]),
+    (4, 4, 64, 17, [300, 777]),
+    (4, 1, 128, 13, [2000, 129]),
+    (6, 2, 128, 61, [1500, 1499]),
+    (5, 5, 64, 128, [2345]),
+    (16, 1, 64, 128, [700]),
+    (40, 40, 64, 33, [256, 255, 257, 64, 0]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv,Dh,n,L", RATED)
+def test_tree_attn_weights(rt, dtype, H, Hkv, Dh, n, L):
+    print(f"rated {dtype} H={H}/{Hkv} Dh={Dh} n={n} L={L}", flush=True)
+    check_weights(rt, Case(dtype, H, Hkv, Dh, n, L, seed=n + len(L)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tree_attn_weights_forms(rt, dtype):
+    c = Case(dtype, 8, 4, 64, 11, [200, 77], seed=12)
+    check_weights(rt, c, decay=0.75, rated=True, place=True)
+    check_weights(rt, c, w_in=None)
+    check_weights(rt, c, decay=0.0, rated=True)
+    check_weights(rt, Case(dtype, 4, 2, 64, 9, [400, 333], layers=3), decay=0.5)
+
+
+def test_tree_attn_weights_peaked_and_low_scores(rt):
+    """One slot takes nearly everything; and scores all far below zero (down to -1e4) still sum to one."""
+    c = Case("bf16", 4, 2, 64, 7, [500], seed=13, q_scale=20.0)
+    check_weights(rt, c)
+    c = Case("f32", 2, 2, 64, 3, [90], seed=14)
+    c.q[:] = -c.q.abs() * 1000
+    c.k[:, :, :93] = c.k[:, :, :93].abs()
+    out, w = check_weights(rt, c, w_in=None)
+    assert abs(w[0, :, :93].double().sum().item() - 2 * 3) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tree_attn_weights_values_that_are_not_finite(rt, dtype):
+    c = Case(dtype, 4, 2, 64, 20, [150, 0], rows=[20, 20], seed=15)
+    c.v[0, 0, 150 + 7] = math.inf
+    c.v[0, 1, 150 + 3, 4] = math.nan
+    c.k[0, 1, 150 + 9] = math.nan
+    c.v[1, :, 5] = -math.inf
+    c.k[1, 0, 2] = math.inf
+    out, w = check_weights(rt, c)
+    assert torch.isfinite(out[0].float()).any() and not torch.isfinite(out[0].float()).all()
+    assert torch.isfinite(w[0, 0, :150]).all()
+
+
+def test_tree_attn_weights_rows_that_see_nothing(rt):
+    c = Case("bf16", 4, 2, 128, 6, [0, 40, 30], rows=[6, 6, 0], seed=16)
+    c.mask[0, 2:4] = 0
+    c.mask[1, 0] = 0
+    out, w = check_weights(rt, c)
+    assert not out[0, 2:4].any()
+
+
+def test_attention_over_more_than_two_billion_elements(rt):
+    """The last head of a cache whose elements pass 32 bits, by both attentions."""
+    free = torch.cuda.mem_get_info()[0]
+    if free < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    c = Case.__new__(Case)
+    g = gen(17)
+    c.dtype, c.H, c.Hkv, c.Dh, c.n, c.B, c.scale = "bf16", 18, 9, 128, 2, 1, 128 ** -0.5
+    c.cap, c.L, c.rows, c.tails = 1_900_032, [1_900_000], [2], [2]
+    c.k, c.v = (torch.empty(1, 9, c.cap, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert c.k.numel() > 2 ** 31
+    for h in range(9):
+        c.k[:, h].normal_(generator=g)
+        c.v[:, h].normal_(generator=g)
+    c.q = normal(g, "bf16", 1, 2, 18, 128)
+    c.mask = torch.tensor([[[1, 0], [3, 0]]], dtype=torch.int64, device="cuda")
+    kv_len, n_q, n_tail, mask = c.dev()
+    out, w = rt.tree_attn_weights(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, c.cap)
+    see = torch.cat([torch.ones(2, c.L[0], dtype=torch.bool, device="cuda"), c.tail_see(0)], 1)
+    want, tol, p, ptol = attend(c, 0, 8, see)
+    close(out[0, :, 16:18], want, tol, "rated")
+    add = p.sum((0, 1))
+    close(w[0, 8, : add.numel()], add, ptol.sum((0, 1)) + 6 * 2.0 ** -24 * add, "weights")
+    means = rt.block_keys(c.k, kv_len, 128)
+    out = rt.sparse_tree_attn(c.q, c.k, c.v, means, kv_len, n_q, n_tail, mask, c.cap, 128, 20)
+    took = choose(c, 0, 8, means, 128, 20, 1, 1)
+    blk = torch.from_numpy(took).cuda().repeat_interleave(128, 1)[:, : c.L[0]]
+    want, tol, _, _ = attend(c, 0, 8, torch.cat([blk, c.tail_see(0)], 1))
+    close(out[0, :, 16:18], want, tol, "sparse")
