@@ -112,42 +112,55 @@ def kv_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len: torch.Tenso
                                _p(path), path.shape[1], _p(n_acc), a_max, dt, _stream()))
 
 
-def _on_device(fn, dev: torch.device, *args) -> None:
-    """fn(*args, stream) with `dev` current, on its current stream."""
-    if torch.cuda.current_device() == dev.index:
-        check(fn(*args, _stream()))
+# The wrappers below are called once or more per layer of a decoding loop, where their own time
+# counts: they pass addresses as plain integers and check a tensor in one expression.
+def _on_device(fn, dev: int, *args) -> None:
+    """fn(*args, stream) with device `dev` current, on its current stream."""
+    if torch._C._cuda_getDevice() == dev:
+        code = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
     else:
         with torch.cuda.device(dev):
-            check(fn(*args, _stream()))
+            code = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if code:
+        check(code)
 
 
-def _want(what: str, t: Optional[torch.Tensor], like: torch.Tensor, dtype: torch.dtype, shape=None) -> None:
-    """An optional tensor beside `like`: same device, this dtype, contiguous and of this shape."""
-    if t is None:
-        return
-    if t.device != like.device or t.dtype != dtype:
-        raise ValueError(f"{what}: {dtype} on {like.device} expected, not {t.dtype} on {t.device}")
-    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
-        raise ValueError(f"{what}: contiguous {tuple(shape)} expected, not {tuple(t.shape)} with strides {t.stride()}")
+def _ptr(what: str, t: torch.Tensor, dev: int, dtype: torch.dtype, shape: tuple) -> int:
+    """Address of a contiguous tensor of this device, type and shape."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    raise ValueError(f"{what}: contiguous {dtype} {tuple(shape)} on device {dev} expected, not {t.dtype} "
+                     f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _dt(t: torch.Tensor) -> int:
-    dt = {torch.float32: abi.F32, torch.bfloat16: abi.BF16}.get(t.dtype)
-    if dt is None or not t.is_cuda:
+def _opt(what: str, t: Optional[torch.Tensor], dev: int, dtype: torch.dtype, shape: tuple) -> Optional[int]:
+    return None if t is None else _ptr(what, t, dev, dtype, shape)
+
+
+ABI_DT = {torch.float32: abi.F32, torch.bfloat16: abi.BF16}
+
+
+def _dt(t: torch.Tensor):
+    """(device index, ABI type) of a float32 or bfloat16 device tensor."""
+    dt, dev = ABI_DT.get(t.dtype), t.get_device()
+    if dt is None or dev < 0:
         raise ValueError(f"float32 or bfloat16 device tensors expected, not {t.dtype} on {t.device}")
-    return dt
+    return dev, dt
 
 
-def _cache_strides(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor] = None):
-    """(stride_b, stride_h) of caches [B][heads][slots][Dh] whose slots are contiguous rows; a layer
-    of a larger cache will do."""
-    B, heads, slots, Dh = k_cache.shape
-    if k_cache.stride(3) != 1 or k_cache.stride(2) != Dh:
-        raise ValueError(f"cache rows must be contiguous, not strides {k_cache.stride()}")
-    if v_cache is not None and (v_cache.shape != k_cache.shape or v_cache.dtype != k_cache.dtype or
-                                v_cache.device != k_cache.device or v_cache.stride() != k_cache.stride()):
-        raise ValueError("key and value caches must have one shape, layout, type and device")
-    return (k_cache.stride(0) if B > 1 else heads * k_cache.stride(1)), (k_cache.stride(1) if heads > 1 else slots * Dh)
+def _caches(k_cache: torch.Tensor, v_cache: torch.Tensor, dev: int, dtype: torch.dtype):
+    """(shape, stride_b, stride_h) of caches [B][heads][slots][Dh] whose slots are contiguous rows; a
+    layer of a larger cache will do."""
+    shape, strides = k_cache.shape, k_cache.stride()
+    if (len(shape) != 4 or strides[3] != 1 or strides[2] != shape[3] or k_cache.dtype is not dtype
+            or k_cache.get_device() != dev or v_cache.shape != shape or v_cache.stride() != strides
+            or v_cache.dtype is not dtype or v_cache.get_device() != dev):
+        raise ValueError(f"two caches [B][heads][slots][Dh] of {dtype} on device {dev} with contiguous rows and one layout "
+                         f"expected, not {tuple(shape)} {k_cache.dtype} with strides {strides} on {k_cache.device} and "
+                         f"{tuple(v_cache.shape)} {v_cache.dtype} with strides {v_cache.stride()} on {v_cache.device}")
+    # the stride of a dimension of one is whatever the view left there
+    sh = strides[1] if shape[1] > 1 else shape[2] * shape[3]
+    return shape, (strides[0] if shape[0] > 1 else shape[1] * sh), sh
 
 
 ROPE_LAYOUTS = {"half": abi.ROPE_HALF, "interleaved": abi.ROPE_INTERLEAVED}
@@ -165,13 +178,17 @@ def rope_freqs(rot_dim: int, theta: float = 10000.0, scaling: str = "plain", fac
     return torch.tensor(list(freq), dtype=torch.float64, device=device), gain.value
 
 
-def _row_stride(what: str, t: torch.Tensor) -> int:
-    """Elements between the rows of t [B][n][heads][Dh], all [B][n] rows evenly apart."""
-    B, n, heads, Dh = t.shape
-    ld = t.stride(1) if n > 1 else (t.stride(0) if B > 1 else heads * Dh)
-    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != Dh) or (B > 1 and t.stride(0) != n * ld):
-        raise ValueError(f"{what}: rows of contiguous heads, evenly apart, expected, not strides {t.stride()}")
-    return ld
+def _rows(what: str, t: torch.Tensor, dev: int, dtype: torch.dtype, B: int, n: int, Dh: int):
+    """(heads, elements between rows) of rows [B][n][heads][Dh], contiguous in themselves and evenly
+    apart: a part of a projection's output will do."""
+    shape, st = t.shape, t.stride()
+    if (len(shape) == 4 and shape[0] == B and shape[1] == n and shape[3] == Dh and t.dtype is dtype
+            and t.get_device() == dev and st[3] == 1 and (shape[2] == 1 or st[2] == Dh)):
+        ld = st[1] if n > 1 else (st[0] if B > 1 else shape[2] * Dh)
+        if B == 1 or st[0] == n * ld:
+            return shape[2], ld
+    raise ValueError(f"{what}: {dtype} rows [{B}][{n}][heads][{Dh}] of contiguous heads, evenly apart, on device {dev} "
+                     f"expected, not {t.dtype} {tuple(shape)} with strides {st} on {t.device}")
 
 
 def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, kv_len: torch.Tensor,
@@ -181,26 +198,22 @@ def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Te
     pos int32 [B][n] over the first 2 * len(freq) dims; keys and values of rows i < n_rows[b] to
     slots kv_len[b] + i of the caches [B][Hkv][S][Dh].  Returns the rotated queries (`out`, which
     may be q where its rows are contiguous)."""
-    dt = _dt(q)
-    B, n, H, Dh = q.shape
-    Hkv = k.shape[2]
-    for name, t in (("k", k), ("v", v)):
-        _want(name, t, q, q.dtype)
-        if t.shape != (B, n, Hkv, Dh):
-            raise ValueError(f"{name}: {(B, n, Hkv, Dh)} expected, not {tuple(t.shape)}")
-    _want("k_cache", k_cache, q, q.dtype)
-    if k_cache.dim() != 4 or k_cache.shape[:2] != (B, Hkv) or k_cache.shape[3] != Dh:
-        raise ValueError(f"caches {(B, Hkv, 'slots', Dh)} expected, not {tuple(k_cache.shape)}")
-    sb, sh = _cache_strides(k_cache, v_cache)
-    _want("pos", pos, q, torch.int32, (B, n))
-    _want("kv_len", kv_len, q, torch.int32, (B,))
-    _want("n_rows", n_rows, q, torch.int32, (B,))
-    _want("freq", freq, q, torch.float64, (freq.numel(),))
-    out = torch.empty(B, n, H, Dh, dtype=q.dtype, device=q.device) if out is None else out
-    _want("out", out, q, q.dtype, (B, n, H, Dh))
-    _on_device(lib().adt_rope_append, q.device, _p(q), _p(k), _p(v), _row_stride("q", q), _row_stride("k", k),
-               _row_stride("v", v), _p(pos), _p(kv_len), _p(n_rows), _p(freq), gain, 2 * freq.numel(),
-               ROPE_LAYOUTS[layout], B, n, H, Hkv, Dh, _p(out), _p(k_cache), _p(v_cache), sb, sh, k_cache.shape[2], dt)
+    dev, dt = _dt(q)
+    dtype = q.dtype
+    B, n, _, Dh = q.shape
+    H, ldq = _rows("q", q, dev, dtype, B, n, Dh)
+    Hkv, ldk = _rows("k", k, dev, dtype, B, n, Dh)
+    Hv, ldv = _rows("v", v, dev, dtype, B, n, Dh)
+    cs, sb, sh = _caches(k_cache, v_cache, dev, dtype)
+    if Hv != Hkv or cs[0] != B or cs[1] != Hkv or cs[3] != Dh:
+        raise ValueError(f"{Hkv} key heads, {Hv} value heads and caches {tuple(cs)} do not go together")
+    if out is None:
+        out = torch.empty(B, n, H, Dh, dtype=dtype, device=q.device)
+    _on_device(lib().adt_rope_append, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), ldq, ldk, ldv,
+               _ptr("pos", pos, dev, torch.int32, (B, n)), _ptr("kv_len", kv_len, dev, torch.int32, (B,)),
+               _ptr("n_rows", n_rows, dev, torch.int32, (B,)), _ptr("freq", freq, dev, torch.float64, freq.shape), gain,
+               2 * freq.numel(), ROPE_LAYOUTS[layout], B, n, H, Hkv, Dh, _ptr("out", out, dev, dtype, (B, n, H, Dh)),
+               k_cache.data_ptr(), v_cache.data_ptr(), sb, sh, cs[2], dt)
     return out
 
 
@@ -209,52 +222,37 @@ def block_keys(k_cache: torch.Tensor, kv_len: torch.Tensor, block: int, start: O
     """Mean keys fp32 [B][Hkv][blocks][Dh] of the blocks of `block` slots of k_cache [B][Hkv][S][Dh]:
     those from start[b] / block (default 0) to the last one of the prefix; others stay (a new
     tensor starts at zero)."""
-    dt = _dt(k_cache)
-    B, Hkv, S, Dh = k_cache.shape
-    sb, sh = _cache_strides(k_cache)
+    dev, dt = _dt(k_cache)
+    (B, Hkv, S, Dh), sb, sh = _caches(k_cache, k_cache, dev, k_cache.dtype)
     n_blk = -(-S // block) if block > 0 else 0
     if out is None:
         out = torch.zeros(B, Hkv, n_blk, Dh, dtype=torch.float32, device=k_cache.device)
-    _want("out", out, k_cache, torch.float32, (B, Hkv, n_blk, Dh))
-    _want("kv_len", kv_len, k_cache, torch.int32, (B,))
-    _want("start", start, k_cache, torch.int32, (B,))
-    _on_device(lib().adt_block_keys, k_cache.device, _p(k_cache), sb, sh, _p(start), _p(kv_len), B, Hkv, Dh, block, S,
-               _p(out), Hkv * n_blk * Dh, n_blk * Dh, dt)
+    _on_device(lib().adt_block_keys, dev, k_cache.data_ptr(), sb, sh, _opt("start", start, dev, torch.int32, (B,)),
+               _ptr("kv_len", kv_len, dev, torch.int32, (B,)), B, Hkv, Dh, block, S,
+               _ptr("out", out, dev, torch.float32, (B, Hkv, n_blk, Dh)), Hkv * n_blk * Dh, n_blk * Dh, dt)
     return out
 
 
-def _weight_strides(what: str, w: torch.Tensor, like: torch.Tensor):
-    """(stride_b, stride_h) of weights fp32 [B][heads][>= slots]."""
-    _want(what, w, like, torch.float32)
-    if w.dim() != 3 or w.shape[:2] != like.shape[:2] or w.shape[2] < like.shape[2] or w.stride(2) != 1:
-        raise ValueError(f"{what}: {(like.shape[0], like.shape[1], like.shape[2])} with contiguous slots expected, not "
-                         f"{tuple(w.shape)} with strides {w.stride()}")
-    B, heads, slots = w.shape
-    sh = w.stride(1) if heads > 1 else slots
-    return (w.stride(0) if B > 1 else heads * sh), sh
-
-
 def _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap, out):
-    """Checks what both attentions over a cache share; (dtype, sizes, strides, out)."""
-    dt = _dt(q)
+    """What both attentions over a cache share: (device, type, sizes, strides, output) checked, and the
+    addresses of the lengths and masks."""
+    dev, dt = _dt(q)
+    dtype = q.dtype
     B, n, H, Dh = q.shape
-    _want("q", q, q, q.dtype, (B, n, H, Dh))
-    _want("k_cache", k_cache, q, q.dtype)
-    if k_cache.dim() != 4 or k_cache.shape[0] != B or k_cache.shape[3] != Dh or k_cache.shape[2] < kv_cap:
-        raise ValueError(f"caches {(B, 'heads', kv_cap, Dh)} expected, not {tuple(k_cache.shape)}")
-    sb, sh = _cache_strides(k_cache, v_cache)
-    for name, t in (("kv_len", kv_len), ("n_q", n_q), ("n_tail", n_tail)):
-        _want(name, t, q, torch.int32, (B,))
-    _want("mask", mask, q, torch.int64, (B, n, abi.MASK_WORDS))
-    out = torch.empty_like(q) if out is None else out
-    _want("out", out, q, q.dtype, (B, n, H, Dh))
-    return dt, B, n, H, k_cache.shape[1], Dh, sb, sh, out
+    cs, sb, sh = _caches(k_cache, v_cache, dev, dtype)
+    if cs[0] != B or cs[3] != Dh or cs[2] < kv_cap or not q.is_contiguous():
+        raise ValueError(f"contiguous queries {tuple(q.shape)}, caches {tuple(cs)} and {kv_cap} slots do not go together")
+    if out is None:
+        out = torch.empty_like(q)
+    return (dev, dt, B, n, H, cs[1], Dh, sb, sh, out, _ptr("out", out, dev, dtype, (B, n, H, Dh)),
+            (_ptr("kv_len", kv_len, dev, torch.int32, (B,)), _ptr("n_q", n_q, dev, torch.int32, (B,)),
+             _ptr("n_tail", n_tail, dev, torch.int32, (B,)),
+             _ptr("mask", mask, dev, torch.int64, (B, n, abi.MASK_WORDS))))
 
 
 def sparse_tree_attn_workspace(B: int, H: int, Hkv: int, Dh: int, nq_max: int, kv_cap: int, block: int, n_sel: int,
                                dtype: torch.dtype = torch.bfloat16, device="cuda") -> torch.Tensor:
-    dt = abi.BF16 if dtype == torch.bfloat16 else abi.F32
-    n = lib().adt_sparse_tree_attn_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, block, n_sel, dt)
+    n = lib().adt_sparse_tree_attn_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, block, n_sel, ABI_DT[dtype])
     return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
 
 
@@ -266,27 +264,35 @@ def sparse_tree_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     """Tree attention of q [B][n][H][Dh] over caches [B][Hkv][S][Dh] in which every row sees n_sel
     blocks of the prefix: the first n_first, the last n_last and the best by means (block_keys of
     the cache).  sel: int32 [B][n][Hkv][n_sel], gets the chosen blocks."""
-    dt, B, n, H, Hkv, Dh, sb, sh, out = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap, out)
-    _want("means", means, q, torch.float32)
-    if means.dim() != 4 or means.shape[:2] != (B, Hkv) or means.shape[3] != Dh or means.shape[2] * block < kv_cap:
-        raise ValueError(f"means of {kv_cap} slots in blocks of {block} expected, not {tuple(means.shape)}")
-    mb, mh = _cache_strides(means)
-    _want("sel", sel, q, torch.int32, (B, n, Hkv, n_sel))
+    dev, dt, B, n, H, Hkv, Dh, sb, sh, out, out_p, lens = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap,
+                                                                     out)
+    ms, mb, mh = _caches(means, means, dev, torch.float32)
+    if ms[0] != B or ms[1] != Hkv or ms[3] != Dh or ms[2] * block < kv_cap:
+        raise ValueError(f"means of {kv_cap} slots in blocks of {block} expected, not {tuple(ms)}")
     if workspace is None:
         workspace = sparse_tree_attn_workspace(B, H, Hkv, Dh, n, kv_cap, block, n_sel, q.dtype, q.device)
-    _want("workspace", workspace, q, torch.uint8)
-    scale = 1.0 / float(np.sqrt(Dh)) if scale is None else scale
-    _on_device(lib().adt_sparse_tree_attn, q.device, _p(q), _p(k_cache), _p(v_cache), sb, sh, _p(means), mb, mh,
-               _p(kv_len), _p(n_q), _p(n_tail), _p(mask), B, H, Hkv, Dh, n, kv_cap, block, n_sel, n_first, n_last, scale,
-               dt, _p(out), _p(sel), _p(workspace), workspace.numel())
+    _on_device(lib().adt_sparse_tree_attn, dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sb, sh,
+               means.data_ptr(), mb, mh, *lens, B, H, Hkv, Dh, n, kv_cap, block, n_sel, n_first, n_last,
+               Dh ** -0.5 if scale is None else scale, dt, out_p, _opt("sel", sel, dev, torch.int32, (B, n, Hkv, n_sel)),
+               _ptr("workspace", workspace, dev, torch.uint8, workspace.shape), workspace.numel())
     return out
 
 
 def tree_attn_weights_workspace(B: int, H: int, Hkv: int, Dh: int, nq_max: int, kv_cap: int,
                                 dtype: torch.dtype = torch.bfloat16, device="cuda") -> torch.Tensor:
-    dt = abi.BF16 if dtype == torch.bfloat16 else abi.F32
-    n = lib().adt_tree_attn_weights_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, dt)
+    n = lib().adt_tree_attn_weights_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, ABI_DT[dtype])
     return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+
+
+def _weights(what: str, w: torch.Tensor, dev: int, B: int, heads: int, slots: int):
+    """(stride_b, stride_h) of weights fp32 [B][heads][>= slots] with contiguous slots."""
+    shape, st = w.shape, w.stride()
+    if (len(shape) != 3 or shape[0] != B or shape[1] != heads or shape[2] < slots or st[2] != 1
+            or w.dtype is not torch.float32 or w.get_device() != dev):
+        raise ValueError(f"{what}: float32 [{B}][{heads}][{slots}] with contiguous slots on device {dev} expected, not "
+                         f"{w.dtype} {tuple(shape)} with strides {st} on {w.device}")
+    sh = st[1] if heads > 1 else shape[2]
+    return (st[0] if B > 1 else heads * sh), sh
 
 
 def tree_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len: torch.Tensor,
@@ -296,24 +302,24 @@ def tree_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Ten
                       out: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
                       workspace: Optional[torch.Tensor] = None):
     """Tree attention of q [B][n][H][Dh] over caches [B][Hkv][S][Dh]; also weights_out fp32
-    [B][Hkv][S] = decay * weights + the softmax weight each slot received (row i counting
+    [B][Hkv][>= kv_cap] = decay * weights + the softmax weight each slot received (row i counting
     row_weight[b][i]).  weights_out defaults to weights, in place, or to new zeros.  Returns
     (out, weights_out)."""
-    dt, B, n, H, Hkv, Dh, sb, sh, out = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap, out)
+    dev, dt, B, n, H, Hkv, Dh, sb, sh, out, out_p, lens = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap,
+                                                                     out)
     if weights_out is None:
-        weights_out = weights if weights is not None else torch.zeros(k_cache.shape[:3], dtype=torch.float32,
+        weights_out = weights if weights is not None else torch.zeros(B, Hkv, k_cache.shape[2], dtype=torch.float32,
                                                                       device=q.device)
-    wb, wh = _weight_strides("weights_out", weights_out, k_cache)
-    if weights is not None and _weight_strides("weights", weights, k_cache) != (wb, wh):
+    wb, wh = _weights("weights_out", weights_out, dev, B, Hkv, kv_cap)
+    if weights is not None and _weights("weights", weights, dev, B, Hkv, kv_cap) != (wb, wh):
         raise ValueError("weights and weights_out must have the same strides")
-    _want("row_weight", row_weight, q, torch.float32, (B, n))
     if workspace is None:
         workspace = tree_attn_weights_workspace(B, H, Hkv, Dh, n, kv_cap, q.dtype, q.device)
-    _want("workspace", workspace, q, torch.uint8)
-    scale = 1.0 / float(np.sqrt(Dh)) if scale is None else scale
-    _on_device(lib().adt_tree_attn_weights, q.device, _p(q), _p(k_cache), _p(v_cache), sb, sh, _p(kv_len), _p(n_q),
-               _p(n_tail), _p(mask), B, H, Hkv, Dh, n, kv_cap, scale, dt, _p(out), _p(weights), _p(weights_out), wb, wh,
-               decay, _p(row_weight), _p(workspace), workspace.numel())
+    _on_device(lib().adt_tree_attn_weights, dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sb, sh, *lens, B, H,
+               Hkv, Dh, n, kv_cap, Dh ** -0.5 if scale is None else scale, dt, out_p,
+               None if weights is None else weights.data_ptr(), weights_out.data_ptr(), wb, wh, decay,
+               _opt("row_weight", row_weight, dev, torch.float32, (B, n)),
+               _ptr("workspace", workspace, dev, torch.uint8, workspace.shape), workspace.numel())
     return out, weights_out
 
 
@@ -322,44 +328,43 @@ def kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor
              v_out: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
              kept: Optional[torch.Tensor] = None, new_len: Optional[torch.Tensor] = None):
     """Keeps `budget` slots of every slice of the caches [B][slices][S][Dh]: the first n_first, the
-    last n_last and those of the largest weights fp32 [B][slices][S], in order.  In place, or into
+    last n_last and those of the largest weights fp32 [B][slices][>= S], in order.  In place, or into
     k_out, v_out and weights_out [B][slices][>= budget].  Returns (kept int32 [B][slices][budget],
     new_len int32 [B]; new_len may be kv_len)."""
-    dt = _dt(k_cache)
-    B, slices, S, Dh = k_cache.shape
-    sb, ss = _cache_strides(k_cache, v_cache)
-    wb, ws = _weight_strides("weights", weights, k_cache)
-    if (k_out is None) != (v_out is None) or (k_out is None) != (weights_out is None):
+    dev, dt = _dt(k_cache)
+    dtype = k_cache.dtype
+    (B, slices, S, Dh), sb, ss = _caches(k_cache, v_cache, dev, dtype)
+    wb, ws = _weights("weights", weights, dev, B, slices, S)
+    if k_out is None and v_out is None and weights_out is None:
+        k_out, v_out, weights_out, osb, oss, owb, ows = k_cache, v_cache, weights, sb, ss, wb, ws
+    elif k_out is None or v_out is None or weights_out is None:
         raise ValueError("k_out, v_out and weights_out are given together or not at all")
-    if k_out is None:
-        k_out, v_out, weights_out = k_cache, v_cache, weights
-    _want("k_out", k_out, k_cache, k_cache.dtype)
-    if k_out.dim() != 4 or k_out.shape[:2] != (B, slices) or k_out.shape[3] != Dh or k_out.shape[2] < min(S, budget):
-        raise ValueError(f"k_out: {(B, slices, min(S, budget), Dh)} expected, not {tuple(k_out.shape)}")
-    osb, oss = _cache_strides(k_out, v_out)
-    owb, ows = _weight_strides("weights_out", weights_out, k_out)
-    kept = torch.full((B, slices, budget), -1, dtype=torch.int32, device=k_cache.device) if kept is None else kept
-    new_len = torch.empty(B, dtype=torch.int32, device=k_cache.device) if new_len is None else new_len
-    _want("kept", kept, k_cache, torch.int32, (B, slices, budget))
-    _want("kv_len", kv_len, k_cache, torch.int32, (B,))
-    _want("new_len", new_len, k_cache, torch.int32, (B,))
-    _on_device(lib().adt_kv_evict, k_cache.device, _p(k_cache), _p(v_cache), _p(weights), sb, ss, wb, ws, _p(kv_len), B,
-               slices, Dh, S, budget, n_first, n_last, _p(k_out), _p(v_out), _p(weights_out), osb, oss, owb, ows,
-               _p(kept), _p(new_len), dt)
+    else:
+        os, osb, oss = _caches(k_out, v_out, dev, dtype)
+        if os[0] != B or os[1] != slices or os[2] < min(S, budget) or os[3] != Dh:
+            raise ValueError(f"k_out: {(B, slices, min(S, budget), Dh)} expected, not {tuple(os)}")
+        owb, ows = _weights("weights_out", weights_out, dev, B, slices, min(S, budget))
+    if kept is None:
+        kept = torch.full((B, slices, max(budget, 0)), -1, dtype=torch.int32, device=k_cache.device)
+    if new_len is None:
+        new_len = torch.empty(B, dtype=torch.int32, device=k_cache.device)
+    _on_device(lib().adt_kv_evict, dev, k_cache.data_ptr(), v_cache.data_ptr(), weights.data_ptr(), sb, ss, wb, ws,
+               _ptr("kv_len", kv_len, dev, torch.int32, (B,)), B, slices, Dh, S, budget, n_first, n_last, k_out.data_ptr(),
+               v_out.data_ptr(), weights_out.data_ptr(), osb, oss, owb, ows,
+               _ptr("kept", kept, dev, torch.int32, (B, slices, budget)), _ptr("new_len", new_len, dev, torch.int32, (B,)),
+               dt)
     return kept, new_len
 
 
 def weights_compact(weights: torch.Tensor, kv_len: torch.Tensor, path: torch.Tensor, n_acc: torch.Tensor,
                     a_max: int) -> None:
     """Moves the weights fp32 [B][slices][S] of an accepted path as kv_compact moves its rows."""
+    dev = _dt(weights)[0]
     B, slices, S = weights.shape
-    wb, ws = _weight_strides("weights", weights, weights)
-    _want("kv_len", kv_len, weights, torch.int32, (B,))
-    _want("n_acc", n_acc, weights, torch.int32, (B,))
-    _want("path", path, weights, torch.int32, (B, path.shape[-1]))
-    _require_cuda(weights)
-    _on_device(lib().adt_weights_compact, weights.device, _p(weights), B, slices, wb, ws, _p(kv_len), S, _p(path),
-               path.shape[1], _p(n_acc), a_max)
+    wb, ws = _weights("weights", weights, dev, B, slices, S)
+    _on_device(lib().adt_weights_compact, dev, weights.data_ptr(), B, slices, wb, ws,
+               _ptr("kv_len", kv_len, dev, torch.int32, (B,)), S, _ptr("path", path, dev, torch.int32, (B, path.shape[-1])),
+               path.shape[-1], _ptr("n_acc", n_acc, dev, torch.int32, (B,)), a_max)
 
 
 def accept_cfg(mode: str = "greedy", temperature: float = 1.0, top_k: int = 0, delta: float = 0.0,
