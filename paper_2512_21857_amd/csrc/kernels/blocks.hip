@@ -128,7 +128,8 @@ __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(const double* 
                                                                   unsigned long long* __restrict__ marks,
                                                                   int32_t* __restrict__ sel) {
   extern __shared__ uint64_t keys[];
-  __shared__ RankScratch<BS_THREADS> sh;
+  typedef RankShape<BS_THREADS, BS_LDS_KEYS / BS_THREADS, 8, 1, LDS> BlockRank;
+  __shared__ typename BlockRank::Scratch sh;
   const int i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   if (i >= min(n_q[b], nq_max)) return;
   const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block;
@@ -151,9 +152,14 @@ __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(const double* 
     __syncthreads();
   }
   const int lo = n_first, hi = live - n_last, need = n_sel - n_first - n_last;
-  auto key = [&](int j) { return LDS ? keys[j] : score_key(row[j]); };
-  const RankCut<uint64_t> cut = rank_cut<uint64_t, BS_THREADS>(key, lo, hi, need, sh);
-  rank_emit(key, live, lo, hi, need == 0, cut, sh, take);
+  // the ends, then the blocks between them that the scores select
+  for (int m = tid; m < lo; m += BS_THREADS) take(m, m);
+  for (int m = tid; m < n_last; m += BS_THREADS) take(n_sel - n_last + m, hi + m);
+  if (need == 0) return;
+  auto value = [&](int j) { return LDS ? keys[lo + j] : score_key(row[lo + j]); };
+  auto ranked = rank_row<uint64_t, BlockRank>(value, [](uint64_t k) { return k; }, hi - lo, sh);
+  ranked.cut(need);
+  ranked.emit([&](int at, int j) { take(lo + at, lo + j); });
 }
 
 size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk) {

@@ -1,115 +1,187 @@
 // Selection by rank within one workgroup: the `need` largest of a row of unsigned keys, found by
-// radix (eight bits a pass, from the top, ending early once a digit's keys are just those still
-// needed), and written out in index order.  Ties go to the lower index.
+// radix from the top digit down (ending early once a digit's keys are just those still needed), and
+// their indices written out in order.  Ties go to the lower index.
 #pragma once
 
 #include "common.h"
 
 namespace adt {
 
-template <int THREADS>
-struct RankScratch {
-  uint32_t hist[256];
-  uint32_t wave_n[2][THREADS / WAVE];
-  uint32_t pick[3];     // digit, keys above it, whether the digit's keys are just those needed
+// THREADS threads, V keys each per round, digits of BITS bits counted in COPIES histograms side by
+// side (neighbouring lanes count in different ones: keys that agree in a digit, as many do in the
+// first, queue for one counter).  ONE: rows have at most THREADS * V keys.
+template <int THREADS_, int V_, int BITS_, int COPIES_, bool ONE_>
+struct RankShape {
+  static constexpr bool ONE = ONE_;
+  static constexpr int THREADS = THREADS_, V = V_, BITS = BITS_, COPIES = COPIES_;
+  static constexpr int BINS = 1 << BITS, WAVES = THREADS / WAVE, ROUND = THREADS * V;
+  static_assert(BINS % THREADS == 0, "bins per thread");
+  struct Scratch {
+    uint32_t hist[COPIES * (BINS + 1)];       // (a digit's copies lie in different banks)
+    uint32_t wave_n[2][WAVES];
+    uint32_t pick[3];                         // digit, keys above it, whether the digit's keys are just those needed
+  };
 };
 
-// Keys with (key & mask) > prefix are selected, and of those with (key & mask) == prefix the
-// first `need`.
-template <typename K>
-struct RankCut {
+// One row of n keys.  The workgroup goes through it in rounds of THREADS * V: wave w of a round holds
+// the 64 V keys from 64 V w on, V a lane, 64 apart.  A row of ONE round is read once and stays in
+// registers; a longer one is read anew in every pass.  value(i) gives what is read, key(value) its
+// key.  Both methods are called by every thread of the workgroup.
+template <typename K, class S, class VF, class KF>
+struct RankRow {
+  static constexpr int V = S::V;
+  VF value;
+  KF key;
+  int n, rounds;
+  typename S::Scratch& sh;
+  K k[V];
+  // keys with (key & mask) > prefix are selected, and of those with (key & mask) == prefix the first `need`
+  // (settled: all of those)
   K prefix = 0, mask = 0;
-  int need = 0;
-};
+  uint32_t need = 0;
+  bool settled = false;
 
-// The cut that selects `need` (0 <= need <= hi - lo) of key(lo) .. key(hi - 1).  Called by every
-// thread of the workgroup; ends with a barrier.
-template <typename K, int THREADS, class F>
-__device__ __forceinline__ RankCut<K> rank_cut(F key, int lo, int hi, int need, RankScratch<THREADS>& sh) {
-  static_assert(THREADS >= 256, "a thread per digit");
-  RankCut<K> cut;
-  cut.need = need;
-  const int tid = threadIdx.x, lane = tid % WAVE;
-  bool all_equal = need == 0;                           // every key with this prefix is selected
-  for (int shift = 8 * (int)sizeof(K) - 8; shift >= 0 && !all_equal; shift -= 8) {
-    if (tid < 256) sh.hist[tid] = 0;
-    __syncthreads();
-    for (int i = lo + tid; i < hi; i += THREADS) {
-      const K k = key(i);
-      if ((k & cut.mask) == cut.prefix) atomicAdd(&sh.hist[(int)(k >> shift) & 255], 1u);
-    }
-    __syncthreads();
-    if (tid < WAVE) {
-      // lane l holds the digits 255 - 4 l .. 252 - 4 l, so a prefix sum over lanes counts from the top
-      uint32_t c[4], sum = 0;
+  __device__ __forceinline__ RankRow(VF value, KF key, int n, typename S::Scratch& sh)
+      : value(value), key(key), n(n), rounds(S::ONE ? 1 : (n + S::ROUND - 1) / S::ROUND), sh(sh) {}
+
+  // index of this lane's key j of a round: first(round) + 64 j
+  __device__ __forceinline__ int first(int round) const {
+    return round * S::ROUND + (int)threadIdx.x / WAVE * WAVE * V + (int)threadIdx.x % WAVE;
+  }
+  // All values are requested before the first is used.  Places past the end get key 0: no key is
+  // less, and of equal keys those before them go first, so none of them is ever selected (and the
+  // loops over keys need no test for the end, whose V masks would fill the scalar registers).
+  __device__ __forceinline__ void load(int round) {
+    decltype(value(0)) x[V];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum += c[j] = sh.hist[255 - 4 * lane - j];
+    for (int j = 0; j < V; ++j) x[j] = value(min(first(round) + j * WAVE, n - 1));
+#pragma unroll
+    for (int j = 0; j < V; ++j) k[j] = first(round) + j * WAVE < n ? key(x[j]) : 0;
+  }
+
+  // Finds the cut that selects `count` (0 < count <= n) keys.
+  __device__ __forceinline__ void cut(int count) {
+    need = count;
+    const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
+    uint32_t* mine = sh.hist + tid % S::COPIES * (S::BINS + 1);
+    if (S::ONE) load(0);
+    for (int top = 8 * (int)sizeof(K); top > 0 && !settled; top -= S::BITS) {
+      const int shift = top > S::BITS ? top - S::BITS : 0, digit = (1 << (top - shift)) - 1;
+      for (int i = tid; i < S::COPIES * (S::BINS + 1); i += S::THREADS) sh.hist[i] = 0;
+      __syncthreads();
+      for (int r = 0; r < rounds; ++r) {
+        if (!S::ONE) load(r);
+        int left = (n - first(r) + WAVE - 1) / WAVE;     // (they are not counted: one counter would take them all)
+        asm volatile("" : "+v"(left));
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          if (j < left && (k[j] & mask) == prefix) atomicAdd(&mine[(int)(k[j] >> shift) & digit], 1u);
+          __builtin_amdgcn_sched_barrier(0);         // (or the compares of all V pile up in scalar registers)
+        }
+      }
+      __syncthreads();
+      // thread t holds the digits B t .. B t + B - 1 from the top; sums of all digits above, then its own
+      constexpr int B = S::BINS / S::THREADS;
+      uint32_t c[B], sum = 0;
+#pragma unroll
+      for (int j = 0; j < B; ++j) {
+        c[j] = 0;
+#pragma unroll
+        for (int u = 0; u < S::COPIES; ++u) c[j] += sh.hist[u * (S::BINS + 1) + S::BINS - 1 - (tid * B + j)];
+        sum += c[j];
+      }
       uint32_t incl = sum;
 #pragma unroll
       for (int o = 1; o < WAVE; o <<= 1) {
         const uint32_t up = __shfl_up(incl, o, WAVE);
         if (lane >= o) incl += up;
       }
+      if (lane == WAVE - 1) sh.wave_n[0][wave] = incl;
+      __syncthreads();
       uint32_t above = incl - sum;
+      for (int w = 0; w < wave; ++w) above += sh.wave_n[0][w];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (above < (uint32_t)cut.need && above + c[j] >= (uint32_t)cut.need) {
-          sh.pick[0] = 255 - 4 * lane - j;
+      for (int j = 0; j < B; ++j) {
+        if (above < need && above + c[j] >= need) {
+          sh.pick[0] = S::BINS - 1 - (tid * B + j);
           sh.pick[1] = above;
-          sh.pick[2] = above + c[j] == (uint32_t)cut.need;
+          sh.pick[2] = above + c[j] == need;
         }
         above += c[j];
       }
+      __syncthreads();
+      prefix |= (K)sh.pick[0] << shift;
+      mask |= (K)digit << shift;
+      need -= sh.pick[1];
+      settled = sh.pick[2] && prefix != 0;          // (places past the end have key 0 as well: by the tie rule)
     }
-    __syncthreads();
-    cut.prefix |= (K)sh.pick[0] << shift;
-    cut.mask |= (K)255 << shift;
-    cut.need -= sh.pick[1];
-    all_equal = sh.pick[2];
-    __syncthreads();
   }
-  return cut;
-}
 
-// Calls out(rank, i), in rank order, for every i of [0, n) that is outside [lo, hi) or selected by
-// the cut (none of [lo, hi) if `none`).  Called by every thread of the workgroup.
-template <typename K, int THREADS, class F, class O>
-__device__ __forceinline__ void rank_emit(F key, int n, int lo, int hi, bool none, const RankCut<K>& cut,
-                                          RankScratch<THREADS>& sh, O out) {
-  const int tid = threadIdx.x, wave = tid / WAVE, lane = tid % WAVE;
-  const uint64_t below = (1ull << lane) - 1;
-  uint32_t done = 0, equal_n = 0;
-  for (int base = 0; base < n; base += THREADS) {
-    const int i = base + tid;
-    bool stays = i < lo || (i >= hi && i < n), equal = false;
-    if (i >= lo && i < hi && !none) {
-      const K k = key(i);
-      stays = (k & cut.mask) > cut.prefix;
-      equal = (k & cut.mask) == cut.prefix;
-    }
-    const uint64_t eq = __ballot(equal);
-    if (lane == 0) sh.wave_n[0][wave] = __popcll(eq);
-    __syncthreads();
-    uint32_t rank = equal_n + __popcll(eq & below);
-#pragma unroll
-    for (int v = 0; v < THREADS / WAVE; ++v) {
-      const uint32_t c = sh.wave_n[0][v];
-      if (v < wave) rank += c;
-      equal_n += c;
-    }
-    stays = stays || (equal && rank < (uint32_t)cut.need);
-    const uint64_t st = __ballot(stays);
-    if (lane == 0) sh.wave_n[1][wave] = __popcll(st);
-    __syncthreads();
-    uint32_t at = done + __popcll(st & below);
-#pragma unroll
-    for (int v = 0; v < THREADS / WAVE; ++v) {
-      const uint32_t c = sh.wave_n[1][v];
-      if (v < wave) at += c;
-      done += c;
-    }
-    if (stays) out((int)at, i);
+  // Calls out(rank, i), in rank order, for every key i that the cut selects.  A wave counts its
+  // selected keys, and once all waves have, writes from where those before it end.
+  template <class O>
+  __device__ __forceinline__ void emit(O out) {
+    if (settled) emit_as<true>(out);
+    else emit_as<false>(out);
   }
+  template <bool SETTLED, class O>
+  __device__ __forceinline__ void emit_as(O out) {
+    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const uint64_t below = (1ull << lane) - 1;
+    uint32_t done = 0, equal_done = 0;
+    for (int r = 0; r < rounds; ++r) {
+      if (!S::ONE) load(r);
+      uint32_t n_in = 0, n_equal = 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const K m = k[j] & mask;
+        n_in += __popcll(__ballot(SETTLED ? m >= prefix : m > prefix));
+        if (!SETTLED) n_equal += __popcll(__ballot(m == prefix));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __syncthreads();
+      if (lane == 0) {
+        sh.wave_n[0][wave] = n_in;
+        sh.wave_n[1][wave] = n_equal;
+      }
+      __syncthreads();
+      // of the equal keys before this wave's, the first `need` are selected
+      uint32_t in0 = 0, equal0 = 0, in_all = 0, equal_all = 0;
+#pragma unroll
+      for (int w = 0; w < S::WAVES; ++w) {
+        if (w == wave) {
+          in0 = in_all;
+          equal0 = equal_all;
+        }
+        in_all += sh.wave_n[0][w];
+        equal_all += sh.wave_n[1][w];
+      }
+      uint32_t eq = equal_done + equal0, at = done + in0 + min(eq, need) - min(equal_done, need);
+      const int i0 = first(r);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const K m = k[j] & mask;
+        bool in = SETTLED ? m >= prefix : m > prefix;
+        if (!SETTLED) {
+          const bool equal = m == prefix;
+          const uint64_t eqs = __ballot(equal);
+          in = in || (equal && eq + __popcll(eqs & below) < need);
+          eq += __popcll(eqs);
+        }
+        const uint64_t ins = __ballot(in);
+        if (in) out((int)(at + __popcll(ins & below)), i0 + j * WAVE);
+        at += __popcll(ins);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      done += in_all + min(equal_done + equal_all, need) - min(equal_done, need);
+      equal_done += equal_all;
+    }
+  }
+};
+
+template <typename K, class S, class VF, class KF>
+__device__ __forceinline__ RankRow<K, S, VF, KF> rank_row(VF value, KF key, int n, typename S::Scratch& sh) {
+  return RankRow<K, S, VF, KF>(value, key, n, sh);
 }
 
 }  // namespace adt
