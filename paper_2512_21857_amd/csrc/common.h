@@ -152,6 +152,12 @@ __device__ inline uint64_t quantised_exp_weight(float d) {
   return (uint64_t)rint(ldexp(p, (int)k + 32));
 }
 
+// LDS written by a wave's lanes before, read by others of its lanes after.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, WAVE);

@@ -1,5 +1,7 @@
 // Blocks of cache slots and what a query thinks of them: the mean key of every block of the
 // prefix, kept beside the cache, and for every query row the blocks it will attend to.
+#include <algorithm>
+
 #include "../launch.h"
 #include "../rank.h"
 
@@ -65,7 +67,7 @@ __global__ __launch_bounds__(BK_WAVES * WAVE) void block_keys_kernel(const T* __
 // the order of a sum (in float, one choice in some ten thousand would).  Also clears the blocks'
 // row marks for the selection that follows.
 typedef double f64x4 __attribute__((ext_vector_type(4)));
-constexpr int SC_WAVES = 4;
+constexpr int SC_WAVES = 4, SC_TILES = 2;      // waves, and 16-block tiles per wave
 template <typename T, int DH>
 __global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* __restrict__ q,
                                                                       const float* __restrict__ means, int64_t mb,
@@ -74,37 +76,56 @@ __global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* _
                                                                       int nq_max, int kv_cap, int block, int n_blk,
                                                                       double* __restrict__ score,
                                                                       uint64_t* __restrict__ marks) {
+  constexpr int QP = DH + 2;      // a row of query sums in LDS, padded: 16 rows at one dim on distinct banks
+  __shared__ __attribute__((aligned(16))) double qs[16 * QP];
   const int h = blockIdx.z % Hkv, b = blockIdx.z / Hkv;
   const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block;
-  const int j0 = (blockIdx.x * SC_WAVES + threadIdx.x / WAVE) * 16, i0 = blockIdx.y * 16;
-  if (j0 >= live) return;
-  const int lane = threadIdx.x % WAVE, lq = lane & 15, g = lane >> 4;
-  if (i0 == 0 && lane < 32) {
-    const int j = j0 + lane / 2;
-    if (j < n_blk) marks[((int64_t)blockIdx.z * n_blk + j) * ADT_MASK_WORDS + (lane & 1)] = 0;
+  const int first = blockIdx.x * SC_WAVES * SC_TILES * 16, i0 = blockIdx.y * 16;
+  if (first >= live) return;
+  if (i0 == 0 && (int)threadIdx.x < SC_WAVES * SC_TILES * 16 && first + (int)threadIdx.x < n_blk) {
+    uint64_t* mk = marks + ((int64_t)blockIdx.z * n_blk + first + threadIdx.x) * ADT_MASK_WORDS;
+    mk[0] = 0;
+    mk[1] = 0;
   }
   const int nq = min(n_q[b], nq_max);
   if (i0 >= nq) return;
-  const bool row = i0 + lq < nq;
-  const T* qp = q + (((int64_t)b * nq_max + min(i0 + lq, nq - 1)) * Hkv + h) * G * DH + 4 * g;
-  const float* mp = means + b * mb + h * mh + (int64_t)min(j0 + lq, live - 1) * DH + 4 * g;
-  f64x4 acc{0.0, 0.0, 0.0, 0.0};
-#pragma unroll
-  for (int d = 0; d < DH; d += 16) {
-    const f32x4 m = *reinterpret_cast<const f32x4*>(mp + d);
+  // the rows' sums over the heads, once for the workgroup: four dims per thread and turn
+  for (int x = threadIdx.x; x < 16 * (DH / 4); x += SC_WAVES * WAVE) {
+    const int i = x / (DH / 4), d = x % (DH / 4) * 4;
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int u = 0; u < G; ++u)
+    if (i0 + i < nq) {
+      const T* qp = q + (((int64_t)b * nq_max + i0 + i) * Hkv + h) * G * DH + d;
+      for (int u = 0; u < G; ++u) {
+        T t[4];
+        __builtin_memcpy(t, __builtin_assume_aligned(qp + (int64_t)u * DH, 4 * sizeof(T)), 4 * sizeof(T));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] += (double)Elem<T>::load(qp + (int64_t)u * DH + d, e);
+        for (int e = 0; e < 4; ++e) s[e] += (double)Elem<T>::load(t, e);
+      }
+    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)m[e], row ? s[e] : 0.0, acc, 0, 0, 0);
+    for (int e = 0; e < 4; ++e) qs[i * QP + d + e] = s[e];
   }
-  if (!row) return;
-  double* out = score + ((int64_t)blockIdx.z * nq_max + i0 + lq) * n_blk + j0;
+  __syncthreads();
+  const int lane = threadIdx.x % WAVE, lq = lane & 15, g = lane >> 4;
 #pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (j0 + 4 * r + g < live) out[4 * r + g] = acc[r];
+  for (int t = 0; t < SC_TILES; ++t) {
+    const int j0 = first + (threadIdx.x / WAVE * SC_TILES + t) * 16;
+    if (j0 >= live) break;
+    const float* mp = means + b * mb + h * mh + (int64_t)min(j0 + lq, live - 1) * DH + 4 * g;
+    f32x4 m[DH / 16];
+#pragma unroll
+    for (int d = 0; d < DH / 16; ++d) m[d] = *reinterpret_cast<const f32x4*>(mp + 16 * d);
+    f64x4 acc{0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int e = 0; e < DH / 4; ++e)
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)m[e / 4][e % 4], qs[lq * QP + e / 4 * 16 + 4 * g + e % 4], acc, 0,
+                                                 0, 0);
+    if (i0 + lq >= nq) continue;
+    double* out = score + ((int64_t)blockIdx.z * nq_max + i0 + lq) * n_blk + j0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (j0 + 4 * r + g < live) out[4 * r + g] = acc[r];
+  }
 }
 
 // Scores in an unsigned order: larger score, larger key; -0 equals +0; NaN below all.
@@ -114,55 +135,187 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-// The n_sel blocks of one query row and key-value head per workgroup: the first and last, and the
-// best of those between by radix selection; written in order, and the row marked in each of them.
-// The keys are held in LDS, or, where there are more than BS_LDS_KEYS, read anew in every pass.
-constexpr int BS_THREADS = 256;
-constexpr int BS_LDS_KEYS = 4096;
-template <bool LDS>
-__global__ __launch_bounds__(BS_THREADS) void block_select_kernel(const double* __restrict__ score,
-                                                                  const int32_t* __restrict__ kv_len,
-                                                                  const int32_t* __restrict__ n_q, int Hkv, int nq_max,
-                                                                  int kv_cap, int block, int n_blk, int n_sel,
-                                                                  int n_first, int n_last,
-                                                                  unsigned long long* __restrict__ marks,
-                                                                  int32_t* __restrict__ sel) {
-  extern __shared__ uint64_t keys[];
-  typedef RankShape<BS_THREADS, BS_LDS_KEYS / BS_THREADS, 8, 1, LDS> BlockRank;
-  __shared__ typename BlockRank::Scratch sh;
-  const int i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  if (i >= min(n_q[b], nq_max)) return;
-  const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block;
-  const int64_t pair = (int64_t)b * Hkv + h;
-  unsigned long long* mk = marks + pair * n_blk * ADT_MASK_WORDS + i / 64;
-  const unsigned long long bit = 1ull << (i & 63);
-  int32_t* out = sel ? sel + (((int64_t)b * nq_max + i) * Hkv + h) * n_sel : nullptr;
-  auto take = [&](int at, int j) {
-    atomicOr(mk + (int64_t)j * ADT_MASK_WORDS, bit);
+// The n_sel blocks of one query row and key-value head: the first and last, and the best of those
+// between by radix selection; written in order, and the row marked in each of them.
+struct BlockPick {
+  int live, n_sel, n_first, n_last;
+  int32_t* out;                       // the row's list, or null
+  unsigned long long* marks;          // the row's word of the first block's mark
+  unsigned long long bit;
+  __device__ __forceinline__ void take(int at, int j) const {
+    atomicOr(marks + (int64_t)j * ADT_MASK_WORDS, bit);
     if (out) out[at] = j;
-  };
-  if (live <= n_sel) {
-    for (int j = tid; j < live; j += BS_THREADS) take(j, j);
-    for (int j = live + tid; out && j < n_sel; j += BS_THREADS) out[j] = -1;
-    return;
   }
-  const double* row = score + (pair * nq_max + i) * n_blk;
-  if (LDS) {
-    for (int j = tid; j < live; j += BS_THREADS) keys[j] = score_key(row[j]);
-    __syncthreads();
+  // what the scores do not decide, by `n` threads of which this is number t; whether they decide the rest
+  __device__ __forceinline__ bool ends(int t, int n) const {
+    if (live <= n_sel) {
+      for (int j = t; j < live; j += n) take(j, j);
+      for (int j = live + t; out && j < n_sel; j += n) out[j] = -1;
+      return false;
+    }
+    for (int m = t; m < n_first; m += n) take(m, m);
+    for (int m = t; m < n_last; m += n) take(n_sel - n_last + m, live - n_last + m);
+    return n_sel > n_first + n_last;
   }
-  const int lo = n_first, hi = live - n_last, need = n_sel - n_first - n_last;
-  // the ends, then the blocks between them that the scores select
-  for (int m = tid; m < lo; m += BS_THREADS) take(m, m);
-  for (int m = tid; m < n_last; m += BS_THREADS) take(n_sel - n_last + m, hi + m);
-  if (need == 0) return;
-  auto value = [&](int j) { return LDS ? keys[lo + j] : score_key(row[lo + j]); };
-  auto ranked = rank_row<uint64_t, BlockRank>(value, [](uint64_t k) { return k; }, hi - lo, sh);
-  ranked.cut(need);
-  ranked.emit([&](int at, int j) { take(lo + at, lo + j); });
+};
+struct BlockRows {
+  const double* score;                // [B][Hkv][nq_max][n_blk]
+  const int32_t *kv_len, *n_q;
+  int Hkv, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last;
+  unsigned long long* marks;
+  int32_t* sel;
+  __device__ __forceinline__ BlockPick pick(int i, int h, int b) const {
+    const int L = max(0, min(kv_len[b], kv_cap));
+    return BlockPick{(L + block - 1) / block, n_sel, n_first, n_last,
+                     sel ? sel + (((int64_t)b * nq_max + i) * Hkv + h) * n_sel : nullptr,
+                     marks + ((int64_t)b * Hkv + h) * n_blk * ADT_MASK_WORDS + i / 64, 1ull << (i & 63)};
+  }
+  __device__ __forceinline__ const double* row(int i, int h, int b) const {
+    return score + (((int64_t)b * Hkv + h) * nq_max + i) * n_blk;
+  }
+};
+
+// A wave per row, keys in LDS (n_blk a wave).
+constexpr int BS_THREADS = 256, BS_WAVES = BS_THREADS / WAVE;
+constexpr int BS_WAVE_KEYS = 1024;
+__global__ __launch_bounds__(BS_THREADS) void block_select_wave_kernel(BlockRows a) {
+  extern __shared__ uint64_t keys[];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[BS_WAVES][256];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+  const int i = blockIdx.x * BS_WAVES + wave, h = blockIdx.y, b = blockIdx.z;
+  if (i >= min(a.n_q[b], a.nq_max)) return;
+  const BlockPick p = a.pick(i, h, b);
+  if (!p.ends(lane, WAVE)) return;
+  const double* row = a.row(i, h, b) + p.n_first;
+  uint64_t* k = keys + wave * a.n_blk;
+  const int n = p.live - p.n_first - p.n_last;
+  for (int j = lane; j < n; j += WAVE) k[j] = score_key(row[j]);
+  wave_lds_fence();
+  wave_select(k, n, p.n_sel - p.n_first - p.n_last, hist[wave], [&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
+}
+
+// A workgroup per row, for rows of more blocks; the keys are read anew in every pass.
+__global__ __launch_bounds__(BS_THREADS) void block_select_kernel(BlockRows a) {
+  typedef RankShape<BS_THREADS, 8, 8, 1, false> Rank;
+  __shared__ typename Rank::Scratch sh;
+  const int i = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  if (i >= min(a.n_q[b], a.nq_max)) return;
+  const BlockPick p = a.pick(i, h, b);
+  if (!p.ends(threadIdx.x, BS_THREADS)) return;
+  const double* row = a.row(i, h, b) + p.n_first;
+  auto ranked = rank_row<uint64_t, Rank>([&](int j) { return row[j]; }, [](double s) { return score_key(s); },
+                                         p.live - p.n_first - p.n_last, sh);
+  ranked.cut(p.n_sel - p.n_first - p.n_last);
+  ranked.emit([&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
+}
+
+// Score and selection in one launch for up to BC_ROWS query rows: a workgroup per key-value head,
+// whose 16-lane groups take a block each (a lane DH / 16 dims, the row's sum over the lanes by
+// rotations within the group), leave the keys in LDS, and whose first waves then select for one row
+// each, eight bits a pass.  For more rows the scores want every CU: their matrix products keep a CU
+// busy for 7 us at 512 blocks and 16 rows, whatever the number of rows below that, where these
+// products take their number's share.
+constexpr int BC_THREADS = 1024;
+constexpr int BC_ROWS = 4;
+constexpr int BC_LDS_BYTES = 144 * 1024;
+static size_t choose_lds_bytes(int nq_max, int n_blk) {
+  return (size_t)n_blk * (nq_max * sizeof(uint64_t) + sizeof(uint32_t));
+}
+static bool choose_at_once(int nq_max, int n_blk) {
+  return nq_max <= BC_ROWS && choose_lds_bytes(nq_max, n_blk) <= BC_LDS_BYTES;
+}
+
+// x + x of the lane C places on, round the 16 lanes of a row
+template <int C>
+__device__ __forceinline__ double add_rotated(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, 0x120 + C, 0xf, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), 0x120 + C, 0xf, 0xf, false);
+  return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+template <typename T, int DH, int R>
+__global__ __launch_bounds__(BC_THREADS) void block_choose_kernel(
+    const T* __restrict__ q, const float* __restrict__ means, int64_t mb, int64_t mh, const int32_t* __restrict__ kv_len,
+    const int32_t* __restrict__ n_q, int Hkv, int G, int nq_max, int kv_cap, int block, int n_blk, int n_sel, int n_first,
+    int n_last, uint64_t* __restrict__ marks, int32_t* __restrict__ sel) {
+  constexpr int PER = DH / 16, GROUPS = BC_THREADS / 16, UN = 4;
+  extern __shared__ uint64_t keys[];                      // [nq_max][n_blk], then the row bits of each block
+  __shared__ double qs[R][DH];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[R][256];
+  uint32_t* bits = reinterpret_cast<uint32_t*>(keys + (size_t)nq_max * n_blk);
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block, nq = min(n_q[b], nq_max);
+  for (int j = tid; j < live; j += BC_THREADS) bits[j] = 0;
+  for (int x = tid; x < R * DH; x += BC_THREADS) {
+    const int i = x / DH, d = x % DH;
+    double s = 0.0;
+    if (i < nq) {
+      const T* qp = q + (((int64_t)b * nq_max + i) * Hkv + h) * G * DH + d;
+      for (int u = 0; u < G; ++u) s += (double)Elem<T>::load(qp, (int64_t)u * DH);
+    }
+    qs[i][d] = s;
+  }
+  __syncthreads();
+  if (live > n_sel) {
+    const int c = tid % 16 * PER;
+    double x[R][PER];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[i][e] = qs[i][c + e];
+    const float* mp = means + b * mb + h * mh + c;
+    for (int j0 = tid / 16; j0 < live; j0 += GROUPS * UN) {
+      f32x4 m[UN][PER / 4];
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+#pragma unroll
+        for (int e = 0; e < PER / 4; ++e)
+          m[u][e] = *reinterpret_cast<const f32x4*>(mp + (int64_t)min(j0 + u * GROUPS, live - 1) * DH + 4 * e);
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          double s = 0.0;
+#pragma unroll
+          for (int e = 0; e < PER; ++e) s = fma((double)m[u][e / 4][e % 4], x[i][e], s);
+          s = add_rotated<8>(s);
+          s = add_rotated<4>(s);
+          s = add_rotated<2>(s);
+          s = add_rotated<1>(s);
+          if (tid % 16 == i && i < nq && j0 + u * GROUPS < live) keys[(size_t)i * n_blk + j0 + u * GROUPS] = score_key(s);
+        }
+    }
+  }
+  __syncthreads();
+  const int i = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
+  if (i < nq) {
+    int32_t* out = sel ? sel + (((int64_t)b * nq_max + i) * Hkv + h) * n_sel : nullptr;
+    auto take = [&](int at, int j) {
+      atomicOr(&bits[j], 1u << i);
+      if (out) out[at] = j;
+    };
+    if (live <= n_sel) {
+      for (int j = lane; j < live; j += WAVE) take(j, j);
+      for (int j = live + lane; out && j < n_sel; j += WAVE) out[j] = -1;
+    } else {
+      const int lo = n_first, hi = live - n_last, need = n_sel - n_first - n_last;
+      for (int m = lane; m < lo; m += WAVE) take(m, m);
+      for (int m = lane; m < n_last; m += WAVE) take(n_sel - n_last + m, hi + m);
+      if (need > 0)
+        wave_select(keys + (size_t)i * n_blk + lo, hi - lo, need, hist[i], [&](int at, int j) { take(lo + at, lo + j); });
+    }
+  }
+  __syncthreads();
+  uint64_t* mk = marks + ((int64_t)b * Hkv + h) * n_blk * ADT_MASK_WORDS;
+  for (int j = tid; j < live; j += BC_THREADS) {
+    mk[(int64_t)j * ADT_MASK_WORDS] = bits[j];
+    mk[(int64_t)j * ADT_MASK_WORDS + 1] = 0;
+  }
 }
 
 size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk) {
+  if (choose_at_once(nq_max, n_blk)) return 0;
   return (size_t)B * Hkv * nq_max * n_blk * sizeof(double);
 }
 
@@ -171,7 +324,27 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
                                int n_sel, int n_first, int n_last, int dtype, double* score, uint64_t* marks,
                                int32_t* sel, hipStream_t st) {
   const int n_blk = (kv_cap + block - 1) / block;
-  const dim3 grid((n_blk + 16 * SC_WAVES - 1) / (16 * SC_WAVES), (nq_max + 15) / 16, B * Hkv);
+  if (choose_at_once(nq_max, n_blk)) {
+#define ADT_BC(TV, DHV, RV)                                                                                             \
+  block_choose_kernel<TV, DHV, RV><<<dim3(Hkv, B), BC_THREADS, choose_lds_bytes(nq_max, n_blk), st>>>(                  \
+      (const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last, marks, sel)
+#define ADT_BCR(TV, DHV)                       \
+  if (nq_max == 1) ADT_BC(TV, DHV, 1);         \
+  else ADT_BC(TV, DHV, BC_ROWS)
+    if (dtype == ADT_BF16) {
+      if (Dh == 128) { ADT_BCR(uint16_t, 128); }
+      else { ADT_BCR(uint16_t, 64); }
+    } else {
+      if (Dh == 128) { ADT_BCR(float, 128); }
+      else { ADT_BCR(float, 64); }
+    }
+#undef ADT_BCR
+#undef ADT_BC
+    ADT_LAUNCH_CHECK();
+    return ADT_OK;
+  }
+  const int per = 16 * SC_WAVES * SC_TILES;
+  const dim3 grid((n_blk + per - 1) / per, (nq_max + 15) / 16, B * Hkv);
 #define ADT_SC(TV, DHV)                                                                                            \
   block_score_kernel<TV, DHV><<<grid, SC_WAVES * WAVE, 0, st>>>((const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G,  \
                                                                 nq_max, kv_cap, block, n_blk, score, marks)
@@ -184,13 +357,13 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
   }
 #undef ADT_SC
   ADT_LAUNCH_CHECK();
-  const dim3 rows(nq_max, Hkv, B);
-#define ADT_BS(LDSV, BYTES)                                                                                            \
-  block_select_kernel<LDSV><<<rows, BS_THREADS, BYTES, st>>>(score, kv_len, n_q, Hkv, nq_max, kv_cap, block, n_blk,    \
-                                                             n_sel, n_first, n_last, (unsigned long long*)marks, sel)
-  if (n_blk <= BS_LDS_KEYS) ADT_BS(true, n_blk * sizeof(uint64_t));
-  else ADT_BS(false, 0);
-#undef ADT_BS
+  const BlockRows rows{score, kv_len, n_q, Hkv, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last,
+                       (unsigned long long*)marks, sel};
+  if (n_blk <= BS_WAVE_KEYS)
+    block_select_wave_kernel<<<dim3((nq_max + BS_WAVES - 1) / BS_WAVES, Hkv, B), BS_THREADS,
+                               BS_WAVES * n_blk * sizeof(uint64_t), st>>>(rows);
+  else
+    block_select_kernel<<<dim3(nq_max, Hkv, B), BS_THREADS, 0, st>>>(rows);
   ADT_LAUNCH_CHECK();
   return ADT_OK;
 }

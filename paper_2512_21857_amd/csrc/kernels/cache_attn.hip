@@ -12,7 +12,7 @@
 // always in one order.  Steps never straddle the end of the prefix: the tree's own slots, which the
 // rows see through their ancestor masks, have steps of their own.
 //
-// bf16 runs on the 16x16x32 MFMA, 32 keys a step, V transposed through LDS, probabilities rounded
+// (bf16 with more than 16 rows: cache_attn_shared_kernel.)  bf16 runs on the 16x16x32 MFMA, 32 keys a step, V transposed through LDS, probabilities rounded
 // to bf16 for the second product (2^-9 a term, below the rounding of the output itself); fp32 on
 // the 16x16x4 MFMA, 16 keys a step, without LDS.  Scores, softmax sums and outputs are fp32.
 //
@@ -33,12 +33,6 @@ constexpr int CA_WAVES = 4;
 constexpr int CA_THREADS = CA_WAVES * WAVE;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-// LDS written by a wave's lanes before, read by others of its lanes after.
-__device__ __forceinline__ void wave_lds_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 __device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
 
 // What the two types differ in.  Lane (l, g) = (lane % 16, lane / 16) holds the scores of row l and
@@ -48,7 +42,7 @@ struct Tile;
 
 template <int DH>
 struct Tile<uint16_t, DH> {
-  static constexpr int KT = 32, SUBS = 2, KS = DH / 32, OT = DH / 16, VG = DH / 64;
+  static constexpr int DIM = DH, KT = 32, SUBS = 2, KS = DH / 32, OT = DH / 16, VG = DH / 64;
   static constexpr int VP = DH + 16;     // LDS row of V, padded so that a transpose load's rows fall on distinct banks
   static constexpr int LDS_BYTES = KT * VP * 2;
   struct Query {
@@ -139,7 +133,7 @@ struct Tile<uint16_t, DH> {
 
 template <int DH>
 struct Tile<float, DH> {
-  static constexpr int KT = 16, SUBS = 1, OT = DH / 16;
+  static constexpr int DIM = DH, KT = 16, SUBS = 1, OT = DH / 16;
   static constexpr int LDS_BYTES = 0;
   struct Query {
     f32x4 f[DH / 16];
@@ -198,6 +192,56 @@ struct Tile<float, DH> {
   }
 };
 
+// The blocks j < live that any row marked, in order, into `chosen`; their number.  Called by the NW waves
+// of a workgroup; scratch: NW ints of LDS.  Ends with a barrier where live > 0.
+template <int NW>
+__device__ __forceinline__ int list_marked(const uint64_t* marks, int live, uint16_t* chosen, int* scratch) {
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+  int n = 0;
+  for (int base = 0; base < live; base += NW * WAVE) {
+    const int j = base + threadIdx.x;
+    const bool on = j < live && (marks[2 * j] | marks[2 * j + 1]) != 0;
+    const uint64_t bal = __ballot(on);
+    if (lane == 0) scratch[wave] = __popcll(bal);
+    __syncthreads();
+    int at = n + __popcll(bal & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const int c = scratch[w];
+      if (w < wave) at += c;
+      n += c;
+    }
+    if (on) chosen[at] = (uint16_t)j;
+    __syncthreads();
+  }
+  return n;
+}
+
+// What a step's values that are not finite add to the rows that see them: o[t][r] (dim(t, r) of row
+// l) += p v over the keys of the step whose value v at that dim is one.  p: this lane's probabilities
+// of row l, for keys 16 sub + 4 g + r; seen(key): whether row l sees key k0 + key.
+template <class X, typename T, class F>
+__device__ __forceinline__ void add_not_finite(f32x4 (&o)[X::OT], const f32x4 (&p)[X::SUBS], const T* v, int k0, int last,
+                                               int l, int g, F seen) {
+  for (int key = 0; key < X::KT; ++key) {
+    float mine = 0.f;
+#pragma unroll
+    for (int sub = 0; sub < X::SUBS; ++sub)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mine = key / 16 == sub && key % 4 == r ? p[sub][r] : mine;
+    const float pk = __shfl(mine, l + 16 * (key % 16 / 4), WAVE);
+    const bool vis = seen(key);
+    const T* row = v + (int64_t)min(k0 + key, last) * X::DIM;
+#pragma unroll
+    for (int t = 0; t < X::OT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = Elem<T>::load(row, X::dim(t, g, r));
+        if (vis && not_finite(x)) o[t][r] += pk * x;
+      }
+  }
+}
+
 // (registers: outputs 16 RT DH / 64 a lane, and a step's K and V: one wave per SIMD at RT = 4)
 template <typename T, int DH, int RT, bool SPARSE>
 __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel(CacheAttn a, int splits,
@@ -205,9 +249,8 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
                                                                                 float* __restrict__ part_ml) {
   typedef Tile<T, DH> X;
   constexpr int KT = X::KT, SUBS = X::SUBS, OT = X::OT;
-  constexpr int PP = KT + 1;                                       // row of the probabilities in LDS
   constexpr int MP = DH + 4;                                       // row of a merged tile
-  constexpr int STEP_BYTES = CA_WAVES * (X::LDS_BYTES + 16 * PP * 4);
+  constexpr int STEP_BYTES = CA_WAVES * X::LDS_BYTES;
   constexpr int MERGE_BYTES = CA_WAVES * 16 * (MP + 2) * 4;
   __shared__ __attribute__((aligned(16))) unsigned char smem[STEP_BYTES > MERGE_BYTES ? STEP_BYTES : MERGE_BYTES];
   extern __shared__ uint16_t chosen[];                             // SPARSE: the blocks that any row chose
@@ -224,27 +267,7 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
   const int per_blk = SPARSE ? a.block / KT : 0;
   int prefix_steps = (L + KT - 1) / KT;
   if (SPARSE) {
-    // the marked blocks, in order
-    int* wave_n = reinterpret_cast<int*>(smem);
-    const int live = (L + a.block - 1) / a.block;
-    int n = 0;
-    for (int base = 0; base < live; base += CA_THREADS) {
-      const int j = base + threadIdx.x;
-      const bool on = j < live && (marks[2 * j] | marks[2 * j + 1]) != 0;
-      const uint64_t bal = __ballot(on);
-      if (lane == 0) wave_n[wave] = __popcll(bal);
-      __syncthreads();
-      int at = n + __popcll(bal & ((1ull << lane) - 1));
-#pragma unroll
-      for (int w = 0; w < CA_WAVES; ++w) {
-        const int c = wave_n[w];
-        if (w < wave) at += c;
-        n += c;
-      }
-      if (on) chosen[at] = (uint16_t)j;
-      __syncthreads();
-    }
-    prefix_steps = n * per_blk;
+    prefix_steps = list_marked<CA_WAVES>(marks, (L + a.block - 1) / a.block, chosen, reinterpret_cast<int*>(smem)) * per_blk;
   }
   const int steps = prefix_steps + (total - L + KT - 1) / KT;
   const T* kb = (const T*)a.k + b * a.sb + h * a.sh;
@@ -270,7 +293,6 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
   }
   const float scale_log2 = a.scale * LOG2E;
   void* lds = smem + wave * X::LDS_BYTES;
-  float* pl = reinterpret_cast<float*>(smem + CA_WAVES * X::LDS_BYTES) + wave * 16 * PP;
 
   f32x4 o[RT][OT];
   float m_run[RT], l_run[RT];      // running maximum (log2 domain), this lane's share of the sum
@@ -344,7 +366,6 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
               const float v = vis ? st[t][sub][r] : -INFINITY;
               st[t][sub][r] = v;
               mx = fmaxf(mx, v);
-              if (SAFE) pl[l * PP + sub * 16 + 4 * g + r] = vis ? 0.f : -1.f;
             }
         }
         mx = xor16_max(mx);
@@ -361,11 +382,6 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
             const float p = exp2_hw(fmaf(st[t][sub][r], scale_log2, -m_use));
             st[t][sub][r] = p;
             rs += p;
-            if (SAFE) {
-              float* x = &pl[l * PP + sub * 16 + 4 * g + r];
-              if (!tail && !SPARSE && k0 + KT - 1 <= k_last) *x = p;
-              else if (*x == 0.f) *x = p;
-            }
           }
         l_run[t] = l_run[t] * alpha + rs;
         if (!__all(alpha == 1.f)) {
@@ -373,22 +389,11 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
           for (int d = 0; d < OT; ++d) o[t][d] *= alpha;
         }
         X::template add<SAFE>(o[t], st[t], step, lds, l, g);
-        if (SAFE) {
-          // values that are not finite, for the rows that see them (probability >= 0 or NaN in pl)
-          wave_lds_fence();
-          for (int key = 0; key < KT; ++key) {
-            const float p = pl[l * PP + key];
-            const T* row = vb + (int64_t)min(k0 + key, k_last) * DH;
-#pragma unroll
-            for (int d = 0; d < OT; ++d)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float v = Elem<T>::load(row, X::dim(d, g, r));
-                if (not_finite(v) && !(p < 0.f)) o[t][d][r] += p * v;
-              }
-          }
-          wave_lds_fence();
-        }
+        if (SAFE)
+          add_not_finite<X>(o[t], st[t], vb, k0, k_last, l, g, [&](int key) {
+            const int j = k0 + key - L;
+            return sees[t] & (k0 + key <= k_last) & (!tail | (bool)((j < 64 ? aw0[t] : aw1[t]) >> (j & 63) & 1));
+          });
       }
       if (X::LDS_BYTES > 0) wave_lds_fence();
       if constexpr (X::LDS_BYTES == 0) {
@@ -456,8 +461,296 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
   }
 }
 
-// Log-sum-exp merge of the splits, in split order, four dims of one row per thread; row_ml (if
-// given) gets the rows' maximum and sum.
+// Many rows (more than 16) in bf16: the waves of a workgroup share the keys instead.  A stage of two
+// 32-key steps comes into LDS once, fetched by all threads into registers one to three stages ahead;
+// wave w computes row tile w % TILES, for step w / TILES of the stage (KH = 2) or both (KH = 1), so a
+// wave holds one tile's outputs and the CU two or four waves per SIMD.  Rows of K and V lie in 16-byte
+// chunks swizzled by row, so that the operand reads (16 rows of one chunk column; 8 rows of two in the
+// transpose load) touch distinct banks.
+template <int DH>
+__device__ __forceinline__ int swz_k(int row) { return DH == 128 ? (row & 15) : ((row >> 1) & 7); }
+template <int DH>
+__device__ __forceinline__ int swz_v(int row) { return DH == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
+
+template <int DH, int NW, int KH, int P, bool SPARSE>
+__global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shared_kernel(CacheAttn a, int splits,
+                                                                                   float* __restrict__ part_o,
+                                                                                   float* __restrict__ part_ml) {
+  typedef Tile<uint16_t, DH> X;
+  constexpr int TILES = NW / KH, KT = X::KT, SK = 2 * KT;          // keys per stage
+  constexpr int CH = DH / 8, OT = DH / 16, KS = DH / 32;
+  constexpr int BYTES = SK * DH * 2;                               // a stage of K or of V
+  constexpr int LOADS = BYTES / (NW * WAVE * 16);                  // 16-byte loads per thread, stage and operand
+  constexpr int OWN = 2 / KH;                                      // steps of a stage per wave
+  static_assert((KH - 1) * TILES * (OT * 4 + 2) * WAVE * 4 <= 4 * BYTES, "merge area");
+  __shared__ __attribute__((aligned(16))) unsigned char smem[4 * BYTES];   // [buffer][K, V]
+  extern __shared__ uint16_t chosen[];                             // SPARSE: the blocks that any row chose
+  const int h = blockIdx.x % a.Hkv, rg = blockIdx.x / a.Hkv, b = blockIdx.y, sp = blockIdx.z;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
+  const int l = lane & 15, g = lane >> 4;
+  const int tile = wave % TILES, kpart = wave / TILES;
+  const int rows = a.nq_max * a.G, live_rows = max(0, min(a.n_q[b], a.nq_max)) * a.G;
+  const int r0 = rg * 16 * TILES;
+  if (r0 >= live_rows) return;
+  const int L = max(0, min(a.kv_len[b], a.kv_cap));
+  const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
+  if (tid == 0 && (int64_t)a.kv_len[b] + a.n_tail[b] > a.kv_cap) dev_fail(DEVINV_KV_RANGE);
+  const uint64_t* marks = SPARSE ? a.marks + ((int64_t)b * a.Hkv + h) * a.n_blk * ADT_MASK_WORDS : nullptr;
+  const int per_blk = SPARSE ? a.block / KT : 1;
+  const int prefix_steps = SPARSE ? list_marked<NW>(marks, (L + a.block - 1) / a.block, chosen, (int*)smem) * per_blk
+                                  : (L + KT - 1) / KT;
+  const int steps = prefix_steps + (total - L + KT - 1) / KT;
+  const int stages = max(0, ((steps + 1) / 2 - sp + splits - 1) / splits);   // of this split: sp, sp + splits, ...
+  const uint16_t* kb = (const uint16_t*)a.k + b * a.sb + h * a.sh;
+  const uint16_t* vb = (const uint16_t*)a.v + b * a.sb + h * a.sh;
+
+  typename X::Query q;
+  X::zero(q);
+  uint64_t aw0 = 0, aw1 = 0;
+  int node = -1;
+  const int row = r0 + tile * 16 + l;
+  if (row < live_rows) {
+    node = row / a.G;
+    X::load(q, (const uint16_t*)a.q + (((int64_t)b * a.nq_max + node) * a.Hkv + h) * a.G * DH + (int64_t)(row - node * a.G) * DH, g);
+    const uint64_t* mp = a.mask + ((int64_t)b * a.nq_max + node) * ADT_MASK_WORDS;
+    aw0 = mp[0];
+    aw1 = mp[1];
+  }
+  const bool tile_live = r0 + tile * 16 < live_rows;
+  const float scale_log2 = a.scale * LOG2E;
+
+  // first key and last of step s (a step past the end has none: last < key0)
+  auto bounds = [&](int s, int& key0, int& last) {
+    if (s >= steps) {
+      key0 = 0;
+      last = -1;
+    } else if (s >= prefix_steps) {
+      key0 = L + (s - prefix_steps) * KT;
+      last = total - 1;
+    } else if (SPARSE) {
+      const int j = __builtin_amdgcn_readfirstlane((int)chosen[s / per_blk]);
+      key0 = j * a.block + s % per_blk * KT;
+      last = min(L, (j + 1) * a.block) - 1;
+    } else {
+      key0 = s * KT;
+      last = L - 1;
+    }
+  };
+  // Slot x (16 bytes) of a stage holds row x / CH, chunk (x % CH) ^ swizzle(row); thread t fills slots
+  // r * NW * 64 + t.  Rows past a step's last key repeat it.  Requests are never skipped (a stage past
+  // the range reads the head's first row), so the count of loads in flight is the same on every path.
+  u16x8 kr[P][LOADS], vr[P][LOADS];
+  uint64_t mk[P][OWN][2] = {};
+  auto fetch = [&](int u, int i) {
+    const int s0 = 2 * (sp + splits * i);
+    int key0[2], last[2];
+    bounds(i < stages ? s0 : steps, key0[0], last[0]);
+    bounds(i < stages ? s0 + 1 : steps, key0[1], last[1]);
+#pragma unroll
+    for (int r = 0; r < LOADS; ++r) {
+      const int slot = r * NW * WAVE + tid, x = slot / CH, phys = slot % CH;
+      const int half = x / KT;
+      const int key = max(0, min((half ? key0[1] : key0[0]) + x % KT, half ? last[1] : last[0]));
+      kr[u][r] = __builtin_nontemporal_load(
+          reinterpret_cast<const u16x8*>(kb + (int64_t)key * DH + (phys ^ swz_k<DH>(x)) * 8));
+      vr[u][r] = __builtin_nontemporal_load(
+          reinterpret_cast<const u16x8*>(vb + (int64_t)key * DH + (phys ^ swz_v<DH>(x)) * 8));
+    }
+    if (SPARSE) {
+#pragma unroll
+      for (int w = 0; w < OWN; ++w) {
+        const int s = min(s0 + (KH == 2 ? kpart : w), max(prefix_steps - 1, 0));
+        const int j = i < stages && prefix_steps > 0 ? (int)chosen[s / per_blk] : 0;
+        mk[u][w][0] = prefix_steps > 0 ? marks[2 * j] : 0;
+        mk[u][w][1] = prefix_steps > 0 ? marks[2 * j + 1] : 0;
+      }
+    }
+  };
+  auto store = [&](int u, int buf) {
+    unsigned char* at = smem + buf * 2 * BYTES;
+#pragma unroll
+    for (int r = 0; r < LOADS; ++r) {
+      const int slot = r * NW * WAVE + tid;
+      *reinterpret_cast<u16x8*>(at + slot * 16) = kr[u][r];
+      *reinterpret_cast<u16x8*>(at + BYTES + slot * 16) = vr[u][r];
+    }
+  };
+
+  f32x4 o[OT];
+  float m_run, l_run;             // running maximum (log2 domain), this lane's share of the sum
+  // this wave's steps of stage i, whose blocks the rows of `m` chose
+  auto compute = [&](auto safe_tag, int i, const uint64_t (&m)[OWN][2]) {
+    constexpr bool SAFE = decltype(safe_tag)::value;
+    const unsigned char* ks = smem + (i & 1) * 2 * BYTES;
+    const unsigned char* vs = ks + BYTES;
+#pragma unroll
+    for (int w = 0; w < OWN; ++w) {
+      const int half = KH == 2 ? kpart : w, s = 2 * (sp + splits * i) + half;
+      if (s >= steps) continue;
+      int k0, k_last;
+      bounds(s, k0, k_last);
+      const bool tail = s >= prefix_steps;
+      const bool sees = node >= 0 && (tail || !SPARSE || ((node < 64 ? m[w][0] : m[w][1]) >> (node & 63) & 1));
+      if (SPARSE && !__any(sees)) continue;
+      f32x4 st[2];
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        st[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int x = half * KT + sub * 16 + l;
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          const bf16x8 f = *reinterpret_cast<const bf16x8*>(ks + x * DH * 2 + ((j * 4 + g) ^ swz_k<DH>(x)) * 16);
+          st[sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q.f[j], st[sub], 0, 0, 0);
+        }
+      }
+      auto seen = [&](int key) {
+        const int j = k0 + key - L;
+        return sees & (k0 + key <= k_last) & (!tail | (bool)((j < 64 ? aw0 : aw1) >> (j & 63) & 1));
+      };
+      float mx = -INFINITY;
+      if (!tail && !SPARSE && k0 + KT - 1 <= k_last) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, st[e / 4][e % 4]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float v = seen(e / 4 * 16 + 4 * g + e % 4) ? st[e / 4][e % 4] : -INFINITY;
+          st[e / 4][e % 4] = v;
+          mx = fmaxf(mx, v);
+        }
+      }
+      mx = xor16_max(mx);
+      mx = xor32_max(mx);
+      const float m_new = fmaxf(m_run, mx * scale_log2);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;     // nothing seen yet: weights 0, not NaN
+      const float alpha = m_new == m_run ? 1.f : exp2_hw(m_run - m_use);
+      m_run = m_new;
+      float rs = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = exp2_hw(fmaf(st[e / 4][e % 4], scale_log2, -m_use));
+        st[e / 4][e % 4] = p;
+        rs += p;
+      }
+      l_run = l_run * alpha + rs;
+      if (!__all(alpha == 1.f)) {
+#pragma unroll
+        for (int d = 0; d < OT; ++d) o[d] *= alpha;
+      }
+      bf16x8 pb;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) pb[e] = (__bf16)st[e / 4][e % 4];
+      const int lo_x = half * KT + 4 * g + (l >> 2), hi_x = lo_x + 16;
+#pragma unroll
+      for (int d = 0; d < OT; ++d) {
+        const int c = 2 * d + ((l & 3) >> 1), part = l & 1;
+        v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_v4i16*)(vs + lo_x * DH * 2 + ((c ^ swz_v<DH>(lo_x)) * 16) + part * 8));
+        v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_v4i16*)(vs + hi_x * DH * 2 + ((c ^ swz_v<DH>(hi_x)) * 16) + part * 8));
+        if (SAFE) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((lo[e] & 0x7f80) == 0x7f80) lo[e] = 0;
+            if ((hi[e] & 0x7f80) == 0x7f80) hi[e] = 0;
+          }
+        }
+        const bf16x8 f = __builtin_bit_cast(bf16x8, v8i16{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pb, o[d], 0, 0, 0);
+      }
+      if (SAFE) add_not_finite<X>(o, st, vb, k0, k_last, l, g, seen);
+    }
+  };
+  auto pass = [&](auto safe_tag) {
+    m_run = -INFINITY;
+    l_run = 0.f;
+#pragma unroll
+    for (int d = 0; d < OT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // (the stages are requested in order: the scheduler may not interleave them, or the first one
+    // stored could be the last to arrive)
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+      fetch(u, u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    for (int base = 0; base < stages; base += P) {
+#pragma unroll
+      for (int u = 0; u < P; ++u) {
+        const int i = base + u;
+        uint64_t m[OWN][2];
+#pragma unroll
+        for (int w = 0; w < OWN; ++w) {
+          m[w][0] = mk[u][w][0];
+          m[w][1] = mk[u][w][1];
+        }
+        // the buffer written here was last read two stages ago, before the previous barrier
+        store(u, i & 1);
+        __syncthreads();
+        fetch(u, i + P);
+        if (tile_live && i < stages) compute(safe_tag, i, m);
+      }
+    }
+  };
+  __syncthreads();                // (the marked blocks are listed)
+  pass(std::false_type{});
+  float odd = 0.f;
+#pragma unroll
+  for (int d = 0; d < OT; ++d)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) odd += o[d][r] * 0.f;
+  if (__syncthreads_or(odd != odd)) pass(std::true_type{});
+
+  l_run = xor16_add(l_run);
+  l_run = xor32_add(l_run);
+  if constexpr (KH > 1) {
+    // the second part of a tile passes its state through LDS to the first
+    float* mo = reinterpret_cast<float*>(smem) + (size_t)tile * (OT * 4 + 2) * WAVE;
+    __syncthreads();
+    if (kpart == 1) {
+#pragma unroll
+      for (int d = 0; d < OT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mo[(d * 4 + r) * WAVE + lane] = o[d][r];
+      mo[OT * 4 * WAVE + lane] = m_run;
+      mo[(OT * 4 + 1) * WAVE + lane] = l_run;
+    }
+    __syncthreads();
+    if (kpart == 0) {
+      const float m1 = mo[OT * 4 * WAVE + lane], l1 = mo[(OT * 4 + 1) * WAVE + lane];
+      const float M = fmaxf(m_run, m1), Mu = M == -INFINITY ? 0.f : M;
+      const float w0 = m_run == -INFINITY && l_run == 0.f ? 0.f : exp2_hw(m_run - Mu);
+      const float w1 = m1 == -INFINITY && l1 == 0.f ? 0.f : exp2_hw(m1 - Mu);
+#pragma unroll
+      for (int d = 0; d < OT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = mo[(d * 4 + r) * WAVE + lane];
+          o[d][r] = (w0 == 0.f ? 0.f : o[d][r] * w0) + (w1 == 0.f ? 0.f : x * w1);
+        }
+      l_run = (w0 == 0.f && l_run == l_run ? 0.f : l_run * w0) + (w1 == 0.f && l1 == l1 ? 0.f : l1 * w1);
+      m_run = M;
+    }
+  }
+  if (kpart == 0 && node >= 0) {
+    const int64_t at = (((int64_t)b * a.Hkv + h) * splits + sp) * rows + row;
+    if (splits == 1) {
+      const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+      uint16_t* to = (uint16_t*)a.out + (((int64_t)b * a.nq_max + node) * a.Hkv + h) * a.G * DH + (int64_t)(row - node * a.G) * DH;
+#pragma unroll
+      for (int d = 0; d < OT; ++d) store4(to + d * 16 + 4 * g, o[d][0] * inv, o[d][1] * inv, o[d][2] * inv, o[d][3] * inv);
+    } else {
+#pragma unroll
+      for (int d = 0; d < OT; ++d) *reinterpret_cast<f32x4*>(part_o + at * DH + d * 16 + 4 * g) = o[d];
+    }
+    if (part_ml && g == 0) {
+      part_ml[at * 2] = m_run;
+      part_ml[at * 2 + 1] = l_run;
+    }
+  }
+}
+
+// Log-sum-exp merge of the splits, in split order, four dims of one row per thread, eight splits
+// requested at a time; row_ml (if given) gets the rows' maximum and sum.
 __global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, int splits, int is_bf16,
                                                                  const float* __restrict__ part_o,
                                                                  const float* __restrict__ part_ml,
@@ -467,18 +760,32 @@ __global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, in
   if (rr >= max(0, min(a.n_q[b], a.nq_max)) * a.G) return;
   const int rows = a.nq_max * a.G;
   const int64_t pair = (int64_t)b * a.Hkv + h, base = pair * splits * rows + rr;
-  float M = -INFINITY;
-  for (int s = 0; s < splits; ++s) M = fmaxf(M, part_ml[(base + (int64_t)s * rows) * 2]);
-  float ls = 0.f;
+  float M = -INFINITY, ls = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const int64_t at = base + (int64_t)s * rows;
-    const float mw = part_ml[at * 2], lw = part_ml[at * 2 + 1];
-    const f32x4 x = *reinterpret_cast<const f32x4*>(part_o + at * a.Dh + d);
-    const float wt = mw == -INFINITY && lw == 0.f ? 0.f : exp2_hw(mw - (M == -INFINITY ? 0.f : M));
-    if (wt == 0.f && lw == lw) continue;
-    ls += wt * lw;
-    acc += wt * x;
+  for (int s0 = 0; s0 < splits; s0 += 8) {
+    float2 ml[8];
+    f32x4 x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t at = base + (int64_t)min(s0 + j, splits - 1) * rows;
+      ml[j] = *reinterpret_cast<const float2*>(part_ml + at * 2);
+      x[j] = *reinterpret_cast<const f32x4*>(part_o + at * a.Dh + d);
+    }
+    float Mn = M;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) Mn = fmaxf(Mn, ml[j].x);
+    const float Mu = Mn == -INFINITY ? 0.f : Mn, down = M == -INFINITY ? 1.f : exp2_hw(M - Mu);
+    M = Mn;
+    ls *= down;
+    acc *= down;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (s0 + j >= splits) continue;
+      const float wt = ml[j].x == -INFINITY && ml[j].y == 0.f ? 0.f : exp2_hw(ml[j].x - Mu);
+      if (wt == 0.f && ml[j].y == ml[j].y) continue;
+      ls += wt * ml[j].y;
+      acc += wt * x[j];
+    }
   }
   const float inv = ls == 0.f ? 0.f : 1.f / ls;
   const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * a.Dh + (int64_t)(rr % a.G) * a.Dh + d;
@@ -582,59 +889,87 @@ __global__ __launch_bounds__(CA_THREADS) void slot_weights_kernel(CacheAttn a, c
 // ----------------------------------------------------------------------------- host
 static size_t align_up16(size_t x) { return (x + 15) / 16 * 16; }
 
-static int row_tiles(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
-
-// Key splits: workgroups for about two rounds of the CUs (one where a workgroup fills its CU), but
-// at least two steps for every wave at the most keys the launch may meet.
-static int cache_splits(const CacheAttn& a, int B, int dtype) {
-  const int rows = a.nq_max * a.G, rt = row_tiles(rows), kt = dtype == ADT_BF16 ? 32 : 16;
-  const int64_t pairs = (int64_t)B * a.Hkv * ((rows + 16 * rt - 1) / (16 * rt));
+// How a launch covers its rows and keys.
+struct CachePlan {
+  bool shared;      // the waves of a workgroup share the keys (bf16, more than 16 rows)
+  int tiles;        // row tiles per workgroup
+  int groups;       // workgroups side by side for the rows of one key-value head
+  int splits;
+};
+// Key splits: enough workgroups for the CUs (two each where they fit: waves with keys of their own and
+// few rows), but at least two steps for every wave, or three stages for a workgroup that shares them, at
+// the most keys the launch may meet.
+static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
+  const int rows = a.nq_max * a.G;
+  CachePlan p;
+  p.shared = dtype == ADT_BF16 && rows > 16;
+  p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 || !p.shared ? 4 : 8;
+  p.groups = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
   int64_t keys = a.kv_cap;
   if (a.block) keys = std::min<int64_t>(keys, (int64_t)a.n_sel * a.nq_max * a.block + ADT_MAX_NODES);
-  const int64_t most = (keys + 2 * CA_WAVES * kt - 1) / (2 * CA_WAVES * kt);
-  const int64_t want = ((rt == 4 ? 256 : 512) + pairs - 1) / pairs;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 64));
+  const int least = p.shared ? 3 * 64 : 2 * CA_WAVES * (dtype == ADT_BF16 ? 32 : 16);
+  const int64_t pairs = (int64_t)B * a.Hkv * p.groups;
+  const int64_t want = ((p.shared || p.tiles == 4 ? 256 : 512) + pairs - 1) / pairs;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, (keys + least - 1) / least), 64));
+  return p;
 }
 
 static size_t part_floats(const CacheAttn& a, int B, int splits) {
   return (size_t)B * a.Hkv * splits * a.nq_max * a.G * (a.Dh + 2);
 }
 
-template <typename T, int DH, int RT, bool SPARSE>
-static void attn_rt(const CacheAttn& a, int B, int splits, float* part_o, float* part_ml, hipStream_t st) {
-  const int groups = (a.nq_max * a.G + 16 * RT - 1) / (16 * RT);
+template <typename T, int DH, bool SPARSE>
+static void attn_launch(const CacheAttn& a, int B, const CachePlan& p, float* part_o, float* part_ml, hipStream_t st) {
   const size_t list = SPARSE ? align_up16((size_t)a.n_blk * 2) : 0;
-  cache_attn_kernel<T, DH, RT, SPARSE><<<dim3(a.Hkv * groups, B, splits), CA_THREADS, list, st>>>(a, splits, part_o, part_ml);
-}
-template <typename T, int DH>
-static void attn_dh(const CacheAttn& a, int B, int splits, float* part_o, float* part_ml, hipStream_t st) {
-  const int rt = row_tiles(a.nq_max * a.G);
-#define ADT_CA(RTV)                                                             \
-  if (a.block) attn_rt<T, DH, RTV, true>(a, B, splits, part_o, part_ml, st);    \
-  else attn_rt<T, DH, RTV, false>(a, B, splits, part_o, part_ml, st)
-  if (rt == 1) { ADT_CA(1); }
-  else if (rt == 2) { ADT_CA(2); }
-  else { ADT_CA(4); }
+  const dim3 grid(a.Hkv * p.groups, B, p.splits);
+#define ADT_CA(RT) cache_attn_kernel<T, DH, RT, SPARSE><<<grid, CA_THREADS, list, st>>>(a, p.splits, part_o, part_ml)
+#define ADT_CS(NW, KH, P) \
+  cache_attn_shared_kernel<DH, NW, KH, P, SPARSE><<<grid, NW * WAVE, list, st>>>(a, p.splits, part_o, part_ml)
+  // stages in flight: three where a workgroup has its CU to itself (keys split), one where two share it
+  if constexpr (sizeof(T) == 2) {
+    if (p.shared) {
+      if (p.splits > 1) {
+        if (p.tiles == 2) ADT_CS(4, 2, 3);
+        else if (p.tiles == 4) ADT_CS(8, 2, 3);
+        else ADT_CS(8, 1, 3);
+      } else {
+        if (p.tiles == 2) ADT_CS(4, 2, 1);
+        else if (p.tiles == 4) ADT_CS(8, 2, 1);
+        else ADT_CS(8, 1, 1);
+      }
+    } else {
+      ADT_CA(1);
+    }
+  } else {
+    if (p.tiles == 1) ADT_CA(1);
+    else if (p.tiles == 2) ADT_CA(2);
+    else ADT_CA(4);
+  }
+#undef ADT_CS
 #undef ADT_CA
 }
 
-// part: partials of `splits` splits (part_floats), row_ml: [B][Hkv][rows][2] or null
-static adt_status attn_passes(const CacheAttn& a, int B, int splits, float* part, float* row_ml, int dtype,
+// part: partials of the plan's splits (part_floats), row_ml: [B][Hkv][rows][2] or null
+static adt_status attn_passes(const CacheAttn& a, int B, const CachePlan& p, float* part, float* row_ml, int dtype,
                               hipStream_t st) {
-  float* part_o = splits > 1 ? part : nullptr;
-  float* part_ml = splits > 1 ? part + (size_t)B * a.Hkv * splits * a.nq_max * a.G * a.Dh : row_ml;
+  float* part_o = p.splits > 1 ? part : nullptr;
+  float* part_ml = p.splits > 1 ? part + (size_t)B * a.Hkv * p.splits * a.nq_max * a.G * a.Dh : row_ml;
+#define ADT_AL(TV, DHV)                                                        \
+  if (a.block) attn_launch<TV, DHV, true>(a, B, p, part_o, part_ml, st);       \
+  else attn_launch<TV, DHV, false>(a, B, p, part_o, part_ml, st)
   if (dtype == ADT_BF16) {
-    if (a.Dh == 128) attn_dh<uint16_t, 128>(a, B, splits, part_o, part_ml, st);
-    else attn_dh<uint16_t, 64>(a, B, splits, part_o, part_ml, st);
+    if (a.Dh == 128) { ADT_AL(uint16_t, 128); }
+    else { ADT_AL(uint16_t, 64); }
   } else {
-    if (a.Dh == 128) attn_dh<float, 128>(a, B, splits, part_o, part_ml, st);
-    else attn_dh<float, 64>(a, B, splits, part_o, part_ml, st);
+    if (a.Dh == 128) { ADT_AL(float, 128); }
+    else { ADT_AL(float, 64); }
   }
+#undef ADT_AL
   ADT_LAUNCH_CHECK();
-  if (splits > 1) {
+  if (p.splits > 1) {
     const int threads = a.nq_max * a.G * (a.Dh / 4);
     cache_merge_kernel<<<dim3((threads + CA_THREADS - 1) / CA_THREADS, a.Hkv, B), CA_THREADS, 0, st>>>(
-        a, splits, dtype == ADT_BF16, part_o, part_ml, row_ml);
+        a, p.splits, dtype == ADT_BF16, part_o, part_ml, row_ml);
     ADT_LAUNCH_CHECK();
   }
   return ADT_OK;
@@ -646,7 +981,7 @@ static size_t sparse_layout(const CacheAttn& a, int B, int dtype, size_t* marks,
   *marks = off;
   off += (size_t)B * a.Hkv * a.n_blk * ADT_MASK_WORDS * 8;
   *part = off;
-  const int S = cache_splits(a, B, dtype);
+  const int S = cache_plan(a, B, dtype).splits;
   return off + (S > 1 ? part_floats(a, B, S) * sizeof(float) : 0);
 }
 
@@ -664,7 +999,7 @@ adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb
                                      a.block, a.n_sel, n_first, n_last, dtype, (double*)ws, mk, sel, st);
   if (e) return e;
   a.marks = mk;
-  return attn_passes(a, B, cache_splits(a, B, dtype), (float*)((char*)ws + part), nullptr, dtype, st);
+  return attn_passes(a, B, cache_plan(a, B, dtype), (float*)((char*)ws + part), nullptr, dtype, st);
 }
 
 static size_t row_ml_bytes(const CacheAttn& a, int B) {
@@ -672,7 +1007,7 @@ static size_t row_ml_bytes(const CacheAttn& a, int B) {
 }
 
 size_t weights_attn_ws_bytes(const CacheAttn& a, int B, int dtype) {
-  const int S = cache_splits(a, B, dtype);
+  const int S = cache_plan(a, B, dtype).splits;
   return row_ml_bytes(a, B) + (S > 1 ? part_floats(a, B, S) * sizeof(float) : 0);
 }
 
@@ -680,7 +1015,7 @@ adt_status launch_weights_attn(const CacheAttn& a, int B, const float* w_in, flo
                                int64_t stride_wh, float decay, const float* row_weight, int dtype, void* ws,
                                hipStream_t st) {
   float* row_ml = (float*)ws;
-  adt_status e = attn_passes(a, B, cache_splits(a, B, dtype), (float*)((char*)ws + row_ml_bytes(a, B)), row_ml, dtype, st);
+  adt_status e = attn_passes(a, B, cache_plan(a, B, dtype), (float*)((char*)ws + row_ml_bytes(a, B)), row_ml, dtype, st);
   if (e) return e;
   const size_t lds = (size_t)(a.nq_max * a.G + 15) / 16 * 16 * sizeof(float2);
 #define ADT_SW(TV, DHV)                                                                                             \

@@ -184,4 +184,60 @@ __device__ __forceinline__ RankRow<K, S, VF, KF> rank_row(VF value, KF key, int 
   return RankRow<K, S, VF, KF>(value, key, n, sh);
 }
 
+// The same for one wave and keys in LDS: calls out(rank, i), in order, for the `need` (0 < need <= n)
+// largest of key[0] .. key[n - 1].  hist: 256 counters of LDS of the wave's own.
+template <class O>
+__device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need_, uint32_t* hist, O out) {
+  const int lane = threadIdx.x % WAVE;
+  uint64_t prefix = 0, mask = 0;
+  uint32_t need = need_;
+  bool settled = false;
+  for (int shift = 56; shift >= 0 && !settled; shift -= 8) {
+    reinterpret_cast<uint4*>(hist)[lane] = make_uint4(0, 0, 0, 0);
+    wave_lds_fence();
+    for (int i = lane; i < n; i += WAVE) {
+      const uint64_t k = key[i];
+      if ((k & mask) == prefix) atomicAdd(&hist[(int)(k >> shift) & 255], 1u);
+    }
+    wave_lds_fence();
+    // lane l holds the digits 255 - 4 l down to 252 - 4 l
+    const uint4 c = reinterpret_cast<const uint4*>(hist)[WAVE - 1 - lane];
+    const uint32_t sum = c.x + c.y + c.z + c.w;
+    uint32_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < WAVE; o <<= 1) {
+      const uint32_t up = __shfl_up(incl, o, WAVE);
+      if (lane >= o) incl += up;
+    }
+    const uint32_t above = incl - sum;
+    const int at = __ffsll((unsigned long long)__ballot(above < need && incl >= need)) - 1;
+    // within that lane's four digits, from the top
+    const uint32_t rest = need - __shfl(above, at, WAVE);
+    const uint32_t w = __shfl(c.w, at, WAVE), z = __shfl(c.z, at, WAVE), y = __shfl(c.y, at, WAVE),
+                   x = __shfl(c.x, at, WAVE);
+    uint32_t digit = 255 - 4 * at, over = 0, count = w;
+    if (rest > w) { digit -= 1; over = w; count = z; }
+    if (rest > w + z) { digit -= 1; over = w + z; count = y; }
+    if (rest > w + z + y) { digit -= 1; over = w + z + y; count = x; }
+    need = rest - over;
+    settled = count == need;
+    prefix |= (uint64_t)digit << shift;
+    mask |= 255ull << shift;
+    wave_lds_fence();
+  }
+  const uint64_t below = (1ull << lane) - 1;
+  uint32_t done = 0, eq = 0;
+  for (int base = 0; base < n; base += WAVE) {
+    const int i = base + lane;
+    const uint64_t m = i < n ? key[i] & mask : 0;
+    const bool equal = i < n && m == prefix;
+    const uint64_t eqs = __ballot(equal);
+    const bool in = i < n && (m > prefix || (equal && eq + __popcll(eqs & below) < need));
+    eq += __popcll(eqs);
+    const uint64_t ins = __ballot(in);
+    if (in) out((int)(done + __popcll(ins & below)), i);
+    done += __popcll(ins);
+  }
+}
+
 }  // namespace adt
