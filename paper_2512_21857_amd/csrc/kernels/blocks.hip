@@ -65,7 +65,7 @@ __global__ __launch_bounds__(BK_WAVES * WAVE) void block_keys_kernel(const T* __
 // lane (l, g) gets blocks 4 r + g of row l.  In double, where the sum of 128 products is off by
 // 2^-50 or so of its terms: a choice between two blocks then depends on the inputs alone, not on
 // the order of a sum (in float, one choice in some ten thousand would).  Also clears the blocks'
-// row marks for the selection that follows.
+// row marks and the pair's count of arrivals for the selection that follows.
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 constexpr int SC_WAVES = 4, SC_TILES = 2;      // waves, and 16-block tiles per wave
 template <typename T, int DH>
@@ -75,12 +75,14 @@ __global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* _
                                                                       const int32_t* __restrict__ n_q, int Hkv, int G,
                                                                       int nq_max, int kv_cap, int block, int n_blk,
                                                                       double* __restrict__ score,
-                                                                      uint64_t* __restrict__ marks) {
+                                                                      uint64_t* __restrict__ marks,
+                                                                      uint32_t* __restrict__ arrived) {
   constexpr int QP = DH + 2;      // a row of query sums in LDS, padded: 16 rows at one dim on distinct banks
   __shared__ __attribute__((aligned(16))) double qs[16 * QP];
   const int h = blockIdx.z % Hkv, b = blockIdx.z / Hkv;
   const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block;
   const int first = blockIdx.x * SC_WAVES * SC_TILES * 16, i0 = blockIdx.y * 16;
+  if (first == 0 && i0 == 0 && threadIdx.x == 0) arrived[blockIdx.z] = 0;
   if (first >= live) return;
   if (i0 == 0 && (int)threadIdx.x < SC_WAVES * SC_TILES * 16 && first + (int)threadIdx.x < n_blk) {
     uint64_t* mk = marks + ((int64_t)blockIdx.z * n_blk + first + threadIdx.x) * ADT_MASK_WORDS;
@@ -128,6 +130,40 @@ __global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* _
   }
 }
 
+// The blocks j < live with a mark (w0(j), w1(j)), in order, into the pair's list.  Called by every
+// thread of the workgroup; scratch: an int of LDS per wave.
+template <int THREADS, class F>
+__device__ __forceinline__ void list_marked(const BlockLists& lists, int64_t pair, int n_blk, int live, int* scratch,
+                                            F mark) {
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+  uint16_t* blocks = lists.blocks + pair * n_blk;
+  uint64_t* marks = lists.marks + pair * n_blk * ADT_MASK_WORDS;
+  int n = 0;
+  for (int base = 0; base < live; base += THREADS) {
+    const int j = base + threadIdx.x;
+    uint64_t w0 = 0, w1 = 0;
+    if (j < live) mark(j, w0, w1);
+    const bool on = (w0 | w1) != 0;
+    const uint64_t bal = __ballot(on);
+    if (lane == 0) scratch[wave] = __popcll(bal);
+    __syncthreads();
+    int at = n + __popcll(bal & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < THREADS / WAVE; ++w) {
+      const int c = scratch[w];
+      if (w < wave) at += c;
+      n += c;
+    }
+    if (on) {
+      blocks[at] = (uint16_t)j;
+      marks[2 * at] = w0;
+      marks[2 * at + 1] = w1;
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) lists.count[pair] = n;
+}
+
 // Scores in an unsigned order: larger score, larger key; -0 equals +0; NaN below all.
 __device__ __forceinline__ uint64_t score_key(double s) {
   if (s != s) return 0;
@@ -162,8 +198,30 @@ struct BlockRows {
   const double* score;                // [B][Hkv][nq_max][n_blk]
   const int32_t *kv_len, *n_q;
   int Hkv, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last;
-  unsigned long long* marks;
+  unsigned long long* marks;          // [B][Hkv][n_blk][ADT_MASK_WORDS], zero before
+  uint32_t* arrived;                  // [B][Hkv], zero before
+  BlockLists lists;
   int32_t* sel;
+  // The last workgroup of a pair to get here lists the marked blocks: marks are set by atomics, complete
+  // at the agent's coherence point (waited for) before the arrival counts, and read past the local caches.
+  template <int THREADS>
+  __device__ __forceinline__ void finish(int h, int b, int* scratch) const {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    const int64_t pair = (int64_t)b * Hkv + h;
+    if (threadIdx.x == 0)
+      scratch[0] = __hip_atomic_fetch_add(arrived + pair, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == gridDim.x;
+    __syncthreads();
+    const int last = scratch[0];
+    __syncthreads();
+    if (!last) return;
+    const int L = max(0, min(kv_len[b], kv_cap));
+    const unsigned long long* mk = marks + pair * n_blk * ADT_MASK_WORDS;
+    list_marked<THREADS>(lists, pair, n_blk, (L + block - 1) / block, scratch, [&](int j, uint64_t& w0, uint64_t& w1) {
+      w0 = __hip_atomic_load(mk + 2 * (int64_t)j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      w1 = __hip_atomic_load(mk + 2 * (int64_t)j + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
+  }
   __device__ __forceinline__ BlockPick pick(int i, int h, int b) const {
     const int L = max(0, min(kv_len[b], kv_cap));
     return BlockPick{(L + block - 1) / block, n_sel, n_first, n_last,
@@ -183,15 +241,19 @@ __global__ __launch_bounds__(BS_THREADS) void block_select_wave_kernel(BlockRows
   __shared__ __attribute__((aligned(16))) uint32_t hist[BS_WAVES][256];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
   const int i = blockIdx.x * BS_WAVES + wave, h = blockIdx.y, b = blockIdx.z;
-  if (i >= min(a.n_q[b], a.nq_max)) return;
-  const BlockPick p = a.pick(i, h, b);
-  if (!p.ends(lane, WAVE)) return;
-  const double* row = a.row(i, h, b) + p.n_first;
-  uint64_t* k = keys + wave * a.n_blk;
-  const int n = p.live - p.n_first - p.n_last;
-  for (int j = lane; j < n; j += WAVE) k[j] = score_key(row[j]);
-  wave_lds_fence();
-  wave_select(k, n, p.n_sel - p.n_first - p.n_last, hist[wave], [&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
+  if (i < min(a.n_q[b], a.nq_max)) {
+    const BlockPick p = a.pick(i, h, b);
+    if (p.ends(lane, WAVE)) {
+      const double* row = a.row(i, h, b) + p.n_first;
+      uint64_t* k = keys + wave * a.n_blk;
+      const int n = p.live - p.n_first - p.n_last;
+      for (int j = lane; j < n; j += WAVE) k[j] = score_key(row[j]);
+      wave_lds_fence();
+      wave_select(k, n, p.n_sel - p.n_first - p.n_last, hist[wave],
+                  [&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
+    }
+  }
+  a.finish<BS_THREADS>(h, b, (int*)hist);
 }
 
 // A workgroup per row, for rows of more blocks; the keys are read anew in every pass.
@@ -199,14 +261,17 @@ __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(BlockRows a) {
   typedef RankShape<BS_THREADS, 8, 8, 1, false> Rank;
   __shared__ typename Rank::Scratch sh;
   const int i = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  if (i >= min(a.n_q[b], a.nq_max)) return;
-  const BlockPick p = a.pick(i, h, b);
-  if (!p.ends(threadIdx.x, BS_THREADS)) return;
-  const double* row = a.row(i, h, b) + p.n_first;
-  auto ranked = rank_row<uint64_t, Rank>([&](int j) { return row[j]; }, [](double s) { return score_key(s); },
-                                         p.live - p.n_first - p.n_last, sh);
-  ranked.cut(p.n_sel - p.n_first - p.n_last);
-  ranked.emit([&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
+  if (i < min(a.n_q[b], a.nq_max)) {
+    const BlockPick p = a.pick(i, h, b);
+    if (p.ends(threadIdx.x, BS_THREADS)) {
+      const double* row = a.row(i, h, b) + p.n_first;
+      auto ranked = rank_row<uint64_t, Rank>([&](int j) { return row[j]; }, [](double s) { return score_key(s); },
+                                             p.live - p.n_first - p.n_last, sh);
+      ranked.cut(p.n_sel - p.n_first - p.n_last);
+      ranked.emit([&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
+    }
+  }
+  a.finish<BS_THREADS>(h, b, (int*)&sh);
 }
 
 // Score and selection in one launch for up to BC_ROWS query rows: a workgroup per key-value head,
@@ -238,7 +303,7 @@ template <typename T, int DH, int R>
 __global__ __launch_bounds__(BC_THREADS) void block_choose_kernel(
     const T* __restrict__ q, const float* __restrict__ means, int64_t mb, int64_t mh, const int32_t* __restrict__ kv_len,
     const int32_t* __restrict__ n_q, int Hkv, int G, int nq_max, int kv_cap, int block, int n_blk, int n_sel, int n_first,
-    int n_last, uint64_t* __restrict__ marks, int32_t* __restrict__ sel) {
+    int n_last, BlockLists lists, int32_t* __restrict__ sel) {
   constexpr int PER = DH / 16, GROUPS = BC_THREADS / 16, UN = 4;
   extern __shared__ uint64_t keys[];                      // [nq_max][n_blk], then the row bits of each block
   __shared__ double qs[R][DH];
@@ -307,27 +372,25 @@ __global__ __launch_bounds__(BC_THREADS) void block_choose_kernel(
     }
   }
   __syncthreads();
-  uint64_t* mk = marks + ((int64_t)b * Hkv + h) * n_blk * ADT_MASK_WORDS;
-  for (int j = tid; j < live; j += BC_THREADS) {
-    mk[(int64_t)j * ADT_MASK_WORDS] = bits[j];
-    mk[(int64_t)j * ADT_MASK_WORDS + 1] = 0;
-  }
+  list_marked<BC_THREADS>(lists, (int64_t)b * Hkv + h, n_blk, live, (int*)hist, [&](int j, uint64_t& w0, uint64_t&) { w0 = bits[j]; });
 }
 
+// Scratch: scores, marks, arrivals.
 size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk) {
   if (choose_at_once(nq_max, n_blk)) return 0;
-  return (size_t)B * Hkv * nq_max * n_blk * sizeof(double);
+  const size_t pairs = (size_t)B * Hkv;
+  return pairs * n_blk * ((size_t)nq_max * sizeof(double) + ADT_MASK_WORDS * sizeof(uint64_t)) + pairs * sizeof(uint32_t);
 }
 
 adt_status launch_block_select(const void* q, const float* means, int64_t mb, int64_t mh, const int32_t* kv_len,
                                const int32_t* n_q, int B, int Hkv, int G, int Dh, int nq_max, int kv_cap, int block,
-                               int n_sel, int n_first, int n_last, int dtype, double* score, uint64_t* marks,
+                               int n_sel, int n_first, int n_last, int dtype, void* ws, const BlockLists& lists,
                                int32_t* sel, hipStream_t st) {
   const int n_blk = (kv_cap + block - 1) / block;
   if (choose_at_once(nq_max, n_blk)) {
 #define ADT_BC(TV, DHV, RV)                                                                                             \
   block_choose_kernel<TV, DHV, RV><<<dim3(Hkv, B), BC_THREADS, choose_lds_bytes(nq_max, n_blk), st>>>(                  \
-      (const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last, marks, sel)
+      (const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last, lists, sel)
 #define ADT_BCR(TV, DHV)                       \
   if (nq_max == 1) ADT_BC(TV, DHV, 1);         \
   else ADT_BC(TV, DHV, BC_ROWS)
@@ -343,11 +406,16 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
     ADT_LAUNCH_CHECK();
     return ADT_OK;
   }
+  const size_t pairs = (size_t)B * Hkv;
+  double* score = (double*)ws;
+  uint64_t* marks = (uint64_t*)(score + pairs * nq_max * n_blk);
+  uint32_t* arrived = (uint32_t*)(marks + pairs * n_blk * ADT_MASK_WORDS);
   const int per = 16 * SC_WAVES * SC_TILES;
   const dim3 grid((n_blk + per - 1) / per, (nq_max + 15) / 16, B * Hkv);
 #define ADT_SC(TV, DHV)                                                                                            \
   block_score_kernel<TV, DHV><<<grid, SC_WAVES * WAVE, 0, st>>>((const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G,  \
-                                                                nq_max, kv_cap, block, n_blk, score, marks)
+                                                                nq_max, kv_cap, block, n_blk, score, marks,      \
+                                                                arrived)
   if (dtype == ADT_BF16) {
     if (Dh == 128) ADT_SC(uint16_t, 128);
     else ADT_SC(uint16_t, 64);
@@ -358,7 +426,7 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
 #undef ADT_SC
   ADT_LAUNCH_CHECK();
   const BlockRows rows{score, kv_len, n_q, Hkv, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last,
-                       (unsigned long long*)marks, sel};
+                       (unsigned long long*)marks, arrived, lists, sel};
   if (n_blk <= BS_WAVE_KEYS)
     block_select_wave_kernel<<<dim3((nq_max + BS_WAVES - 1) / BS_WAVES, Hkv, B), BS_THREADS,
                                BS_WAVES * n_blk * sizeof(uint64_t), st>>>(rows);

@@ -192,29 +192,20 @@ struct Tile<float, DH> {
   }
 };
 
-// The blocks j < live that any row marked, in order, into `chosen`; their number.  Called by the NW waves
-// of a workgroup; scratch: NW ints of LDS.  Ends with a barrier where live > 0.
-template <int NW>
-__device__ __forceinline__ int list_marked(const uint64_t* marks, int live, uint16_t* chosen, int* scratch) {
-  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
-  int n = 0;
-  for (int base = 0; base < live; base += NW * WAVE) {
-    const int j = base + threadIdx.x;
-    const bool on = j < live && (marks[2 * j] | marks[2 * j + 1]) != 0;
-    const uint64_t bal = __ballot(on);
-    if (lane == 0) scratch[wave] = __popcll(bal);
-    __syncthreads();
-    int at = n + __popcll(bal & ((1ull << lane) - 1));
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const int c = scratch[w];
-      if (w < wave) at += c;
-      n += c;
-    }
-    if (on) chosen[at] = (uint16_t)j;
-    __syncthreads();
-  }
-  return n;
+// How the keys of one (sequence, key-value head, row group) are dealt out: `units` of them (steps, or
+// stages of two) to `n` of the launch's splits, at least `per` each, so that a split is worth its
+// start whatever the launch's bounds were, and short sequences and long ones take workgroups of much
+// the same work.  Split 0 leaves n for the merge.
+struct Deal {
+  int splits, per;          // of the launch; units per split
+  int32_t* live;            // [B][Hkv][groups] n, or null (one split)
+  __device__ __forceinline__ int splits_of(int units) const { return max(1, min(splits, (units + per - 1) / per)); }
+};
+
+// The chosen blocks of a pair into LDS; ends with a barrier.
+__device__ __forceinline__ void copy_list(const uint16_t* blocks, int count, uint16_t* chosen) {
+  for (int j = threadIdx.x; j < count; j += blockDim.x) chosen[j] = blocks[j];
+  __syncthreads();
 }
 
 // What a step's values that are not finite add to the rows that see them: o[t][r] (dim(t, r) of row
@@ -244,7 +235,7 @@ __device__ __forceinline__ void add_not_finite(f32x4 (&o)[X::OT], const f32x4 (&
 
 // (registers: outputs 16 RT DH / 64 a lane, and a step's K and V: one wave per SIMD at RT = 4)
 template <typename T, int DH, int RT, bool SPARSE>
-__global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel(CacheAttn a, int splits,
+__global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel(CacheAttn a, Deal deal,
                                                                                 float* __restrict__ part_o,
                                                                                 float* __restrict__ part_ml) {
   typedef Tile<T, DH> X;
@@ -263,13 +254,15 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
   const int L = max(0, min(a.kv_len[b], a.kv_cap));
   const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
   if (threadIdx.x == 0 && (int64_t)a.kv_len[b] + a.n_tail[b] > a.kv_cap) dev_fail(DEVINV_KV_RANGE);
-  const uint64_t* marks = SPARSE ? a.marks + ((int64_t)b * a.Hkv + h) * a.n_blk * ADT_MASK_WORDS : nullptr;
-  const int per_blk = SPARSE ? a.block / KT : 0;
-  int prefix_steps = (L + KT - 1) / KT;
-  if (SPARSE) {
-    prefix_steps = list_marked<CA_WAVES>(marks, (L + a.block - 1) / a.block, chosen, reinterpret_cast<int*>(smem)) * per_blk;
-  }
+  const int64_t pair = (int64_t)b * a.Hkv + h;
+  const int per_blk = SPARSE ? a.block / KT : 1;
+  const int prefix_steps = SPARSE ? a.lists.count[pair] * per_blk : (L + KT - 1) / KT;
   const int steps = prefix_steps + (total - L + KT - 1) / KT;
+  const int splits = deal.splits, n_live = deal.splits_of(steps);
+  if (sp >= n_live) return;
+  if (deal.live && sp == 0 && threadIdx.x == 0) deal.live[(int64_t)b * gridDim.x + blockIdx.x] = n_live;
+  const uint64_t* marks = a.lists.marks + pair * a.n_blk * ADT_MASK_WORDS;
+  if (SPARSE) copy_list(a.lists.blocks + pair * a.n_blk, a.lists.count[pair], chosen);
   const T* kb = (const T*)a.k + b * a.sb + h * a.sh;
   const T* vb = (const T*)a.v + b * a.sb + h * a.sh;
 
@@ -305,11 +298,11 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
       key0 = s * KT;
       last = L - 1;
       if (SPARSE) {
-        const int j = __builtin_amdgcn_readfirstlane((int)chosen[s / per_blk]);
+        const int at = s / per_blk, j = __builtin_amdgcn_readfirstlane((int)chosen[at]);
         key0 = j * a.block + s % per_blk * KT;
         last = min(L, (j + 1) * a.block) - 1;
-        w0 = marks[2 * j];
-        w1 = marks[2 * j + 1];
+        w0 = marks[2 * at];
+        w1 = marks[2 * at + 1];
       }
     } else {
       key0 = L + (s - prefix_steps) * KT;
@@ -327,7 +320,7 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
 #pragma unroll
       for (int d = 0; d < OT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int stride = splits * CA_WAVES;
+    const int stride = n_live * CA_WAVES;
     int s = sp * CA_WAVES + wave;
     if (s < steps) request(s, key0, last, w0, w1);
     for (; s < steps; s += stride) {
@@ -445,8 +438,8 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
         ls += wt * lw;
         acc += wt * *reinterpret_cast<const f32x4*>(&mo[(w * 16 + i) * MP + d]);
       }
-      const int64_t pair = (int64_t)b * a.Hkv + h, at = (pair * splits + sp) * rows + rr;
-      if (splits == 1) {
+      const int64_t at = (pair * splits + sp) * rows + rr;
+      if (n_live == 1) {
         const float inv = ls == 0.f ? 0.f : 1.f / ls;
         const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * DH + (int64_t)(rr % a.G) * DH + d;
         store4((T*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
@@ -473,7 +466,7 @@ template <int DH>
 __device__ __forceinline__ int swz_v(int row) { return DH == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
 
 template <int DH, int NW, int KH, int P, bool SPARSE>
-__global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shared_kernel(CacheAttn a, int splits,
+__global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shared_kernel(CacheAttn a, Deal deal,
                                                                                    float* __restrict__ part_o,
                                                                                    float* __restrict__ part_ml) {
   typedef Tile<uint16_t, DH> X;
@@ -495,12 +488,16 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
   const int L = max(0, min(a.kv_len[b], a.kv_cap));
   const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
   if (tid == 0 && (int64_t)a.kv_len[b] + a.n_tail[b] > a.kv_cap) dev_fail(DEVINV_KV_RANGE);
-  const uint64_t* marks = SPARSE ? a.marks + ((int64_t)b * a.Hkv + h) * a.n_blk * ADT_MASK_WORDS : nullptr;
+  const int64_t pair = (int64_t)b * a.Hkv + h;
   const int per_blk = SPARSE ? a.block / KT : 1;
-  const int prefix_steps = SPARSE ? list_marked<NW>(marks, (L + a.block - 1) / a.block, chosen, (int*)smem) * per_blk
-                                  : (L + KT - 1) / KT;
+  const int prefix_steps = SPARSE ? a.lists.count[pair] * per_blk : (L + KT - 1) / KT;
   const int steps = prefix_steps + (total - L + KT - 1) / KT;
-  const int stages = max(0, ((steps + 1) / 2 - sp + splits - 1) / splits);   // of this split: sp, sp + splits, ...
+  const int splits = deal.splits, n_live = deal.splits_of((steps + 1) / 2);
+  if (sp >= n_live) return;
+  if (deal.live && sp == 0 && tid == 0) deal.live[(int64_t)b * gridDim.x + blockIdx.x] = n_live;
+  const int stages = max(0, ((steps + 1) / 2 - sp + n_live - 1) / n_live);   // of this split: sp, sp + n_live, ...
+  const uint32_t* marks = reinterpret_cast<const uint32_t*>(a.lists.marks + pair * a.n_blk * ADT_MASK_WORDS);
+  if (SPARSE) copy_list(a.lists.blocks + pair * a.n_blk, a.lists.count[pair], chosen);
   const uint16_t* kb = (const uint16_t*)a.k + b * a.sb + h * a.sh;
   const uint16_t* vb = (const uint16_t*)a.v + b * a.sb + h * a.sh;
 
@@ -540,9 +537,9 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
   // r * NW * 64 + t.  Rows past a step's last key repeat it.  Requests are never skipped (a stage past
   // the range reads the head's first row), so the count of loads in flight is the same on every path.
   u16x8 kr[P][LOADS], vr[P][LOADS];
-  uint64_t mk[P][OWN][2] = {};
+  uint32_t mk[P][OWN] = {};       // of the blocks' marks, the word with this lane's row
   auto fetch = [&](int u, int i) {
-    const int s0 = 2 * (sp + splits * i);
+    const int s0 = 2 * (sp + n_live * i);
     int key0[2], last[2];
     bounds(i < stages ? s0 : steps, key0[0], last[0]);
     bounds(i < stages ? s0 + 1 : steps, key0[1], last[1]);
@@ -560,9 +557,8 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
 #pragma unroll
       for (int w = 0; w < OWN; ++w) {
         const int s = min(s0 + (KH == 2 ? kpart : w), max(prefix_steps - 1, 0));
-        const int j = i < stages && prefix_steps > 0 ? (int)chosen[s / per_blk] : 0;
-        mk[u][w][0] = prefix_steps > 0 ? marks[2 * j] : 0;
-        mk[u][w][1] = prefix_steps > 0 ? marks[2 * j + 1] : 0;
+        const int at = i < stages ? s / per_blk : 0;
+        mk[u][w] = prefix_steps > 0 ? marks[4 * at + (max(node, 0) >> 5)] : 0;
       }
     }
   };
@@ -579,18 +575,18 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
   f32x4 o[OT];
   float m_run, l_run;             // running maximum (log2 domain), this lane's share of the sum
   // this wave's steps of stage i, whose blocks the rows of `m` chose
-  auto compute = [&](auto safe_tag, int i, const uint64_t (&m)[OWN][2]) {
+  auto compute = [&](auto safe_tag, int i, const uint32_t (&m)[OWN]) {
     constexpr bool SAFE = decltype(safe_tag)::value;
     const unsigned char* ks = smem + (i & 1) * 2 * BYTES;
     const unsigned char* vs = ks + BYTES;
 #pragma unroll
     for (int w = 0; w < OWN; ++w) {
-      const int half = KH == 2 ? kpart : w, s = 2 * (sp + splits * i) + half;
+      const int half = KH == 2 ? kpart : w, s = 2 * (sp + n_live * i) + half;
       if (s >= steps) continue;
       int k0, k_last;
       bounds(s, k0, k_last);
       const bool tail = s >= prefix_steps;
-      const bool sees = node >= 0 && (tail || !SPARSE || ((node < 64 ? m[w][0] : m[w][1]) >> (node & 63) & 1));
+      const bool sees = node >= 0 && (tail || !SPARSE || (m[w] >> (node & 31) & 1));
       if (SPARSE && !__any(sees)) continue;
       f32x4 st[2];
 #pragma unroll
@@ -677,12 +673,9 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
 #pragma unroll
       for (int u = 0; u < P; ++u) {
         const int i = base + u;
-        uint64_t m[OWN][2];
+        uint32_t m[OWN];
 #pragma unroll
-        for (int w = 0; w < OWN; ++w) {
-          m[w][0] = mk[u][w][0];
-          m[w][1] = mk[u][w][1];
-        }
+        for (int w = 0; w < OWN; ++w) m[w] = mk[u][w];
         // the buffer written here was last read two stages ago, before the previous barrier
         store(u, i & 1);
         __syncthreads();
@@ -691,7 +684,6 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
       }
     }
   };
-  __syncthreads();                // (the marked blocks are listed)
   pass(std::false_type{});
   float odd = 0.f;
 #pragma unroll
@@ -732,8 +724,8 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
     }
   }
   if (kpart == 0 && node >= 0) {
-    const int64_t at = (((int64_t)b * a.Hkv + h) * splits + sp) * rows + row;
-    if (splits == 1) {
+    const int64_t at = (pair * splits + sp) * rows + row;
+    if (n_live == 1) {
       const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
       uint16_t* to = (uint16_t*)a.out + (((int64_t)b * a.nq_max + node) * a.Hkv + h) * a.G * DH + (int64_t)(row - node * a.G) * DH;
 #pragma unroll
@@ -751,7 +743,7 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
 
 // Log-sum-exp merge of the splits, in split order, four dims of one row per thread, eight splits
 // requested at a time; row_ml (if given) gets the rows' maximum and sum.
-__global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, int splits, int is_bf16,
+__global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, Deal deal, int group_rows, int is_bf16,
                                                                  const float* __restrict__ part_o,
                                                                  const float* __restrict__ part_ml,
                                                                  float* __restrict__ row_ml) {
@@ -759,7 +751,16 @@ __global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, in
   const int idx = blockIdx.x * CA_THREADS + threadIdx.x, rr = idx / per, d = idx % per * 4;
   if (rr >= max(0, min(a.n_q[b], a.nq_max)) * a.G) return;
   const int rows = a.nq_max * a.G;
-  const int64_t pair = (int64_t)b * a.Hkv + h, base = pair * splits * rows + rr;
+  const int64_t pair = (int64_t)b * a.Hkv + h, base = pair * deal.splits * rows + rr;
+  const int groups = (rows + group_rows - 1) / group_rows;
+  const int splits = deal.live[((int64_t)b * groups + rr / group_rows) * a.Hkv + h];
+  if (splits == 1) {               // the output is written; its maximum and sum are the only ones
+    if (row_ml && d == 0) {
+      row_ml[(pair * rows + rr) * 2] = part_ml[base * 2];
+      row_ml[(pair * rows + rr) * 2 + 1] = part_ml[base * 2 + 1];
+    }
+    return;
+  }
   float M = -INFINITY, ls = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < splits; s0 += 8) {
@@ -894,41 +895,55 @@ struct CachePlan {
   bool shared;      // the waves of a workgroup share the keys (bf16, more than 16 rows)
   int tiles;        // row tiles per workgroup
   int groups;       // workgroups side by side for the rows of one key-value head
-  int splits;
+  int splits, per;  // most splits of the keys; steps (stages where shared) per split
+  int deep;         // stages in flight
 };
-// Key splits: enough workgroups for the CUs (two each where they fit: waves with keys of their own and
-// few rows), but at least two steps for every wave, or three stages for a workgroup that shares them, at
-// the most keys the launch may meet.
+// Splits: as many as give the workgroups that the CUs hold at once (`slots`) equal shares of the keys
+// the launch expects, the slots of the cache or n_sel blocks; sequences that have more take more.  At
+// least three stages, or two steps for each wave, pay for a split's start and its partial results.  A
+// workgroup that shares its keys keeps one stage in flight where two of them fit a CU, and three where
+// there is so little work (under eight stages a CU) that one to a CU is all there is.
 static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
   const int rows = a.nq_max * a.G;
   CachePlan p;
   p.shared = dtype == ADT_BF16 && rows > 16;
   p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 || !p.shared ? 4 : 8;
   p.groups = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
-  int64_t keys = a.kv_cap;
-  if (a.block) keys = std::min<int64_t>(keys, (int64_t)a.n_sel * a.nq_max * a.block + ADT_MAX_NODES);
-  const int least = p.shared ? 3 * 64 : 2 * CA_WAVES * (dtype == ADT_BF16 ? 32 : 16);
+  const int unit = p.shared ? 64 : dtype == ADT_BF16 ? 32 : 16, least = p.shared ? 3 : 2 * CA_WAVES;
+  int64_t most = a.kv_cap, expect = most;      // keys
+  if (a.block) {
+    most = std::min<int64_t>(most, (int64_t)a.n_sel * a.nq_max * a.block + ADT_MAX_NODES);
+    expect = std::min<int64_t>(expect, (int64_t)a.n_sel * a.block + a.nq_max);
+  }
+  most = (most + unit - 1) / unit + 1;
+  expect = (expect + unit - 1) / unit;
   const int64_t pairs = (int64_t)B * a.Hkv * p.groups;
-  const int64_t want = ((p.shared || p.tiles == 4 ? 256 : 512) + pairs - 1) / pairs;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, (keys + least - 1) / least), 64));
+  p.deep = p.shared && pairs * expect < 8 * 256 ? 3 : 1;
+  const int slots = p.shared ? (p.deep > 1 ? 256 : 512) : p.tiles == 1 ? 768 : p.tiles == 2 ? 512 : 256;
+  p.per = (int)std::max<int64_t>(least, (pairs * expect + slots - 1) / slots);
+  int64_t splits = (most + p.per - 1) / p.per;
+  splits = std::min<int64_t>(splits, std::max<int64_t>(1, (p.deep > 1 ? slots : 4 * slots) / pairs));
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, 64));
   return p;
 }
 
-static size_t part_floats(const CacheAttn& a, int B, int splits) {
-  return (size_t)B * a.Hkv * splits * a.nq_max * a.G * (a.Dh + 2);
+// Partial results of a plan with splits, in floats: outputs, maxima and sums, numbers of splits.
+static size_t part_floats(const CacheAttn& a, int B, const CachePlan& p) {
+  if (p.splits == 1) return 0;
+  return (size_t)B * a.Hkv * ((size_t)p.splits * a.nq_max * a.G * (a.Dh + 2) + p.groups);
 }
 
 template <typename T, int DH, bool SPARSE>
-static void attn_launch(const CacheAttn& a, int B, const CachePlan& p, float* part_o, float* part_ml, hipStream_t st) {
+static void attn_launch(const CacheAttn& a, int B, const CachePlan& p, const Deal& deal, float* part_o, float* part_ml,
+                        hipStream_t st) {
   const size_t list = SPARSE ? align_up16((size_t)a.n_blk * 2) : 0;
   const dim3 grid(a.Hkv * p.groups, B, p.splits);
-#define ADT_CA(RT) cache_attn_kernel<T, DH, RT, SPARSE><<<grid, CA_THREADS, list, st>>>(a, p.splits, part_o, part_ml)
+#define ADT_CA(RT) cache_attn_kernel<T, DH, RT, SPARSE><<<grid, CA_THREADS, list, st>>>(a, deal, part_o, part_ml)
 #define ADT_CS(NW, KH, P) \
-  cache_attn_shared_kernel<DH, NW, KH, P, SPARSE><<<grid, NW * WAVE, list, st>>>(a, p.splits, part_o, part_ml)
-  // stages in flight: three where a workgroup has its CU to itself (keys split), one where two share it
+  cache_attn_shared_kernel<DH, NW, KH, P, SPARSE><<<grid, NW * WAVE, list, st>>>(a, deal, part_o, part_ml)
   if constexpr (sizeof(T) == 2) {
     if (p.shared) {
-      if (p.splits > 1) {
+      if (p.deep > 1) {
         if (p.tiles == 2) ADT_CS(4, 2, 3);
         else if (p.tiles == 4) ADT_CS(8, 2, 3);
         else ADT_CS(8, 1, 3);
@@ -952,11 +967,13 @@ static void attn_launch(const CacheAttn& a, int B, const CachePlan& p, float* pa
 // part: partials of the plan's splits (part_floats), row_ml: [B][Hkv][rows][2] or null
 static adt_status attn_passes(const CacheAttn& a, int B, const CachePlan& p, float* part, float* row_ml, int dtype,
                               hipStream_t st) {
+  const size_t rows = (size_t)B * a.Hkv * p.splits * a.nq_max * a.G;
   float* part_o = p.splits > 1 ? part : nullptr;
-  float* part_ml = p.splits > 1 ? part + (size_t)B * a.Hkv * p.splits * a.nq_max * a.G * a.Dh : row_ml;
+  float* part_ml = p.splits > 1 ? part + rows * a.Dh : row_ml;
+  const Deal deal{p.splits, p.per, p.splits > 1 ? (int32_t*)(part_ml + rows * 2) : nullptr};
 #define ADT_AL(TV, DHV)                                                        \
-  if (a.block) attn_launch<TV, DHV, true>(a, B, p, part_o, part_ml, st);       \
-  else attn_launch<TV, DHV, false>(a, B, p, part_o, part_ml, st)
+  if (a.block) attn_launch<TV, DHV, true>(a, B, p, deal, part_o, part_ml, st);       \
+  else attn_launch<TV, DHV, false>(a, B, p, deal, part_o, part_ml, st)
   if (dtype == ADT_BF16) {
     if (a.Dh == 128) { ADT_AL(uint16_t, 128); }
     else { ADT_AL(uint16_t, 64); }
@@ -969,37 +986,41 @@ static adt_status attn_passes(const CacheAttn& a, int B, const CachePlan& p, flo
   if (p.splits > 1) {
     const int threads = a.nq_max * a.G * (a.Dh / 4);
     cache_merge_kernel<<<dim3((threads + CA_THREADS - 1) / CA_THREADS, a.Hkv, B), CA_THREADS, 0, st>>>(
-        a, p.splits, dtype == ADT_BF16, part_o, part_ml, row_ml);
+        a, deal, 16 * p.tiles, dtype == ADT_BF16, part_o, part_ml, row_ml);
     ADT_LAUNCH_CHECK();
   }
   return ADT_OK;
 }
 
-// Workspace of attention over chosen blocks: scores, marks, partials.
-static size_t sparse_layout(const CacheAttn& a, int B, int dtype, size_t* marks, size_t* part) {
-  size_t off = align_up16(block_select_ws_bytes(B, a.Hkv, a.nq_max, a.n_blk));
-  *marks = off;
-  off += (size_t)B * a.Hkv * a.n_blk * ADT_MASK_WORDS * 8;
-  *part = off;
-  const int S = cache_plan(a, B, dtype).splits;
-  return off + (S > 1 ? part_floats(a, B, S) * sizeof(float) : 0);
+// Workspace of attention over chosen blocks: the selection's scratch, the lists, partial results.
+struct SparseWs {
+  size_t marks, blocks, count, part, bytes;
+};
+static SparseWs sparse_ws(const CacheAttn& a, int B, const CachePlan& p) {
+  const size_t pairs = (size_t)B * a.Hkv;
+  SparseWs w;
+  w.marks = align_up16(block_select_ws_bytes(B, a.Hkv, a.nq_max, a.n_blk));
+  w.blocks = w.marks + pairs * a.n_blk * ADT_MASK_WORDS * sizeof(uint64_t);
+  w.count = align_up16(w.blocks + pairs * a.n_blk * sizeof(uint16_t));
+  w.part = align_up16(w.count + pairs * sizeof(int32_t));
+  w.bytes = w.part + part_floats(a, B, p) * sizeof(float);
+  return w;
 }
 
 size_t sparse_attn_ws_bytes(const CacheAttn& a, int B, int dtype) {
-  size_t marks, part;
-  return sparse_layout(a, B, dtype, &marks, &part);
+  return sparse_ws(a, B, cache_plan(a, B, dtype)).bytes;
 }
 
 adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb, int64_t mh, int n_first, int n_last,
                               int32_t* sel, int dtype, void* ws, hipStream_t st) {
-  size_t marks, part;
-  sparse_layout(a, B, dtype, &marks, &part);
-  uint64_t* mk = (uint64_t*)((char*)ws + marks);
+  const CachePlan p = cache_plan(a, B, dtype);
+  const SparseWs w = sparse_ws(a, B, p);
+  char* base = (char*)ws;
+  a.lists = BlockLists{(int32_t*)(base + w.count), (uint16_t*)(base + w.blocks), (uint64_t*)(base + w.marks)};
   adt_status e = launch_block_select(a.q, means, mb, mh, a.kv_len, a.n_q, B, a.Hkv, a.G, a.Dh, a.nq_max, a.kv_cap,
-                                     a.block, a.n_sel, n_first, n_last, dtype, (double*)ws, mk, sel, st);
+                                     a.block, a.n_sel, n_first, n_last, dtype, ws, a.lists, sel, st);
   if (e) return e;
-  a.marks = mk;
-  return attn_passes(a, B, cache_plan(a, B, dtype), (float*)((char*)ws + part), nullptr, dtype, st);
+  return attn_passes(a, B, p, (float*)(base + w.part), nullptr, dtype, st);
 }
 
 static size_t row_ml_bytes(const CacheAttn& a, int B) {
@@ -1007,8 +1028,7 @@ static size_t row_ml_bytes(const CacheAttn& a, int B) {
 }
 
 size_t weights_attn_ws_bytes(const CacheAttn& a, int B, int dtype) {
-  const int S = cache_plan(a, B, dtype).splits;
-  return row_ml_bytes(a, B) + (S > 1 ? part_floats(a, B, S) * sizeof(float) : 0);
+  return row_ml_bytes(a, B) + part_floats(a, B, cache_plan(a, B, dtype)) * sizeof(float);
 }
 
 adt_status launch_weights_attn(const CacheAttn& a, int B, const float* w_in, float* w_out, int64_t stride_wb,

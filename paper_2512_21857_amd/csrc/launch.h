@@ -305,12 +305,18 @@ adt_status launch_block_keys(const void* k, int64_t sb, int64_t sh, const int32_
                              int Hkv, int Dh, int block, int kv_cap, float* means, int64_t mb, int64_t mh, int dtype,
                              hipStream_t st);
 
-size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk);   // scores
-// Marks the blocks each row takes (marks [B][Hkv][n_blk][ADT_MASK_WORDS], bit i: row i) and lists
-// them in sel (may be null).
+// The blocks that the rows of each (sequence, key-value head) chose, any of them: their number, the
+// blocks in order, and for each of them the rows that chose it (bit i: row i).
+struct BlockLists {
+  int32_t* count;        // [B][Hkv]
+  uint16_t* blocks;      // [B][Hkv][n_blk]
+  uint64_t* marks;       // [B][Hkv][n_blk][ADT_MASK_WORDS]
+};
+size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk);   // scratch (16-byte aligned)
+// Fills the lists (and sel, which may be null).
 adt_status launch_block_select(const void* q, const float* means, int64_t mb, int64_t mh, const int32_t* kv_len,
                                const int32_t* n_q, int B, int Hkv, int G, int Dh, int nq_max, int kv_cap, int block,
-                               int n_sel, int n_first, int n_last, int dtype, double* score, uint64_t* marks,
+                               int n_sel, int n_first, int n_last, int dtype, void* ws, const BlockLists& lists,
                                int32_t* sel, hipStream_t st);
 
 // cache_attn.hip
@@ -324,7 +330,7 @@ struct CacheAttn {
   float scale;
   void* out;
   int block = 0, n_blk = 0, n_sel = 0;
-  const uint64_t* marks = nullptr;
+  BlockLists lists{};
 };
 size_t sparse_attn_ws_bytes(const CacheAttn& a, int B, int dtype);
 adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb, int64_t mh, int n_first, int n_last,
