@@ -237,7 +237,8 @@ __device__ __forceinline__ void add_not_finite(f32x4 (&o)[X::OT], const f32x4 (&
 template <typename T, int DH, int RT, bool SPARSE>
 __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel(CacheAttn a, Deal deal,
                                                                                 float* __restrict__ part_o,
-                                                                                float* __restrict__ part_ml) {
+                                                                                float* __restrict__ part_ml,
+                                                                                float* __restrict__ kept) {
   typedef Tile<T, DH> X;
   constexpr int KT = X::KT, SUBS = X::SUBS, OT = X::OT;
   constexpr int MP = DH + 4;                                       // row of a merged tile
@@ -360,6 +361,15 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
               st[t][sub][r] = v;
               mx = fmaxf(mx, v);
             }
+        }
+        if (RT == 1 && !SPARSE && kept && node[0] >= 0) {
+          // the masked scores, for the weights of the slots
+          float* to = kept + (pair * rows + l) * a.kv_cap + k0 + 4 * g;
+#pragma unroll
+          for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (k0 + sub * 16 + 4 * g + r <= k_last) to[sub * 16 + r] = st[0][sub][r];
         }
         mx = xor16_max(mx);
         mx = xor32_max(mx);
@@ -741,34 +751,44 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
   }
 }
 
-// Log-sum-exp merge of the splits, in split order, four dims of one row per thread, eight splits
-// requested at a time; row_ml (if given) gets the rows' maximum and sum.
-__global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, Deal deal, int group_rows, int is_bf16,
-                                                                 const float* __restrict__ part_o,
-                                                                 const float* __restrict__ part_ml,
-                                                                 float* __restrict__ row_ml) {
-  const int h = blockIdx.y, b = blockIdx.z, per = a.Dh / 4;
-  const int idx = blockIdx.x * CA_THREADS + threadIdx.x, rr = idx / per, d = idx % per * 4;
-  if (rr >= max(0, min(a.n_q[b], a.nq_max)) * a.G) return;
-  const int rows = a.nq_max * a.G;
+// Log-sum-exp merge of the splits: DH / 4 threads take four dims each of one row, and `count` groups of
+// them deal out the row's splits, up to eight requested at a time; the groups' sums meet in LDS, in
+// their order.  A workgroup takes as many rows as fit it, from row r0 on.  row_ml (if given) gets the
+// rows' maxima and sums.
+struct MergeScratch {
+  f32x4 acc[CA_THREADS];
+  float2 ml[CA_THREADS];
+};
+__device__ __forceinline__ void merge_rows(const CacheAttn& a, const Deal& deal, int group_rows, bool bf16, int r0,
+                                           int count, int h, int b, const float* part_o, const float* part_ml,
+                                           float* row_ml, MergeScratch& sh) {
+  const int per = a.Dh / 4, unit = threadIdx.x / per, grp = unit % count, d = threadIdx.x % per * 4;
+  const int live = max(0, min(a.n_q[b], a.nq_max)) * a.G;
+  if (r0 >= live) return;
+  const int rr = r0 + unit / count;
+  const int rows = a.nq_max * a.G, groups = (rows + group_rows - 1) / group_rows;
   const int64_t pair = (int64_t)b * a.Hkv + h, base = pair * deal.splits * rows + rr;
-  const int groups = (rows + group_rows - 1) / group_rows;
-  const int splits = deal.live[((int64_t)b * groups + rr / group_rows) * a.Hkv + h];
-  if (splits == 1) {               // the output is written; its maximum and sum are the only ones
-    if (row_ml && d == 0) {
-      row_ml[(pair * rows + rr) * 2] = part_ml[base * 2];
-      row_ml[(pair * rows + rr) * 2 + 1] = part_ml[base * 2 + 1];
-    }
-    return;
+  const int splits = rr < live ? deal.live[((int64_t)b * groups + rr / group_rows) * a.Hkv + h] : 0;
+  // (one split has written the output; its maximum and sum are the only ones)
+  if (splits == 1 && row_ml && grp == 0 && d == 0) {
+    row_ml[(pair * rows + rr) * 2] = part_ml[base * 2];
+    row_ml[(pair * rows + rr) * 2 + 1] = part_ml[base * 2 + 1];
   }
   float M = -INFINITY, ls = 0.f;
   f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < splits; s0 += 8) {
+  // (w, l, x) into the running (M, ls, acc); a part that saw nothing (-inf, 0) adds nothing
+  auto add = [&](float m, float l, const f32x4& x, float Mu) {
+    const float wt = m == -INFINITY && l == 0.f ? 0.f : exp2_hw(m - Mu);
+    if (wt == 0.f && l == l) return;
+    ls += wt * l;
+    acc += wt * x;
+  };
+  for (int s0 = splits > 1 ? grp : splits; s0 < splits; s0 += 8 * count) {
     float2 ml[8];
     f32x4 x[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int64_t at = base + (int64_t)min(s0 + j, splits - 1) * rows;
+      const int64_t at = base + (int64_t)min(s0 + j * count, splits - 1) * rows;
       ml[j] = *reinterpret_cast<const float2*>(part_ml + at * 2);
       x[j] = *reinterpret_cast<const f32x4*>(part_o + at * a.Dh + d);
     }
@@ -780,17 +800,28 @@ __global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, De
     ls *= down;
     acc *= down;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (s0 + j >= splits) continue;
-      const float wt = ml[j].x == -INFINITY && ml[j].y == 0.f ? 0.f : exp2_hw(ml[j].x - Mu);
-      if (wt == 0.f && ml[j].y == ml[j].y) continue;
-      ls += wt * ml[j].y;
-      acc += wt * x[j];
+    for (int j = 0; j < 8; ++j)
+      if (s0 + j * count < splits) add(ml[j].x, ml[j].y, x[j], Mu);
+  }
+  if (count > 1) {
+    sh.acc[threadIdx.x] = acc;
+    sh.ml[threadIdx.x] = make_float2(M, ls);
+    __syncthreads();
+    if (grp > 0) return;
+    const int n = min(count, splits);
+    for (int g = 1; g < n; ++g) M = fmaxf(M, sh.ml[threadIdx.x + g * per].x);
+    const float Mu = M == -INFINITY ? 0.f : M;
+    ls = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < n; ++g) {
+      const float2 ml = sh.ml[threadIdx.x + g * per];
+      add(ml.x, ml.y, sh.acc[threadIdx.x + g * per], Mu);
     }
   }
+  if (splits <= 1) return;
   const float inv = ls == 0.f ? 0.f : 1.f / ls;
   const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * a.Dh + (int64_t)(rr % a.G) * a.Dh + d;
-  if (is_bf16) store4((uint16_t*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  if (bf16) store4((uint16_t*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
   else store4((float*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
   if (row_ml && d == 0) {
     row_ml[(pair * rows + rr) * 2] = M;
@@ -798,93 +829,209 @@ __global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, De
   }
 }
 
-// The weight every slot received: S[row][key] once more, now with the rows' final maximum and sum,
-// p = 2^(s - m) / l, added over the rows.  A wave takes 16 SUBS keys, keeps them in registers and
-// goes through the query rows tile by tile (A = Q rows, B = K^T: lane (l, g) gets rows 4 g + r of
-// key l, so a column adds up within its lanes).
-template <typename T> struct ColSubs { static constexpr int n = 4; };
-template <> struct ColSubs<float> { static constexpr int n = 2; };
+__global__ __launch_bounds__(CA_THREADS) void cache_merge_kernel(CacheAttn a, Deal deal, int group_rows, int count,
+                                                                 int is_bf16,
+                                                                 const float* __restrict__ part_o,
+                                                                 const float* __restrict__ part_ml,
+                                                                 float* __restrict__ row_ml) {
+  __shared__ MergeScratch sh;
+  merge_rows(a, deal, group_rows, is_bf16, blockIdx.x * (CA_THREADS / (a.Dh / 4) / count), count, blockIdx.y, blockIdx.z,
+             part_o, part_ml, row_ml, sh);
+}
 
+// Where the weights of the slots go.
+struct SlotWeights {
+  const float* in;
+  float* out;
+  int64_t stride_b, stride_h;
+  float decay;
+  const float* row_weight;
+  __device__ __forceinline__ float rating(int b, int nq_max, int node) const {
+    return row_weight ? row_weight[(int64_t)b * nq_max + node] : 1.f;
+  }
+  __device__ __forceinline__ void store(int b, int h, int key, int L, float sum) const {
+    const int64_t at = b * stride_b + h * stride_h + key;
+    out[at] = key < L && in ? decay * in[at] + sum : sum;
+  }
+};
+
+// A row's maximum and its weight over its sum, what a slot's weight takes of it; a row that saw
+// nothing adds 2^(-inf - inf) * 0.
+__device__ __forceinline__ float2 row_factor(float m, float sum, float rating) {
+  if (sum == 0.f) return make_float2(INFINITY, 0.f);
+  return make_float2(m == -INFINITY ? 0.f : m, rating / sum);
+}
+
+// The weight every slot received: S[row][key] once more, now with the rows' final maximum and sum,
+// p = 2^(s - m) / l, added over the rows.  A wave takes CHUNK keys at a time, keeps them in registers,
+// the next ones requested meanwhile, and goes through the query rows tile by tile (A = Q rows, B =
+// K^T: lane (l, g) gets rows 4 g + r of key l, so a column adds up within its lanes).  The queries of
+// up to QROWS rows lie in LDS; more are read from the L2 again for every chunk.
+constexpr int SW_CHUNK = 32;        // keys per wave and turn
 template <typename T, int DH>
-__global__ __launch_bounds__(CA_THREADS) void slot_weights_kernel(CacheAttn a, const float* __restrict__ row_ml,
-                                                                  const float* __restrict__ w_in,
-                                                                  float* __restrict__ w_out, int64_t stride_wb,
-                                                                  int64_t stride_wh, float decay,
-                                                                  const float* __restrict__ row_weight) {
+struct SlotTile {
+  static constexpr int PITCH = DH + 16 / (int)sizeof(T);                              // a query row in LDS
+  static constexpr int QROWS = 128 * 256 / (DH * (int)sizeof(T)) < 128 ? 64 : 128;
+};
+
+template <typename T, int DH, bool QLDS>
+__global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weights_kernel(
+    CacheAttn a, const float* __restrict__ row_ml, int turns, SlotWeights sw) {
   typedef Tile<T, DH> X;
-  constexpr int SUBS = ColSubs<T>::n, PER = X::SUBS;    // 16-key columns per wave, and per loaded step
-  constexpr int KEYS = CA_WAVES * SUBS * 16;
-  extern __shared__ float2 rows_mc[];                   // per row: maximum, row weight / sum
-  const int h = blockIdx.y, b = blockIdx.z;
+  constexpr int STEPS = SW_CHUNK / X::KT, SUBS = SW_CHUNK / 16, PITCH = SlotTile<T, DH>::PITCH, V = 16 / sizeof(T);
+  extern __shared__ __attribute__((aligned(16))) unsigned char rows_lds[];   // factors, then the queries
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int L = max(0, min(a.kv_len[b], a.kv_cap));
   const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
-  if ((int)blockIdx.x * KEYS >= total) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+  const int first = blockIdx.x * turns * CA_WAVES * SW_CHUNK;
+  if (first >= total) return;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
   const int l = lane & 15, g = lane >> 4;
-  const int live_rows = max(0, min(a.n_q[b], a.nq_max)) * a.G;
+  const int live_rows = max(0, min(a.n_q[b], a.nq_max)) * a.G, tiles = (live_rows + 15) / 16;
   const int64_t pair = (int64_t)b * a.Hkv + h;
-  const int tiles = (live_rows + 15) / 16;
-  for (int r = threadIdx.x; r < tiles * 16; r += CA_THREADS) {
-    float2 mc = make_float2(INFINITY, 0.f);             // a row that saw nothing, or is none: weight 0
+  const T* kb = (const T*)a.k + b * a.sb + h * a.sh;
+  typename X::Step step[2][STEPS];
+  auto request = [&](int u, int k0) {
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) X::load_k(step[u][i], kb, min(k0, total - 1) + i * X::KT, total - 1, l, g);
+  };
+  request(0, first + wave * SW_CHUNK);
+  float2* factor = reinterpret_cast<float2*>(rows_lds);
+  T* qs = reinterpret_cast<T*>(factor + tiles * 16);
+  auto q_row = [&](int r) {
+    const int i = r / a.G;
+    return (const T*)a.q + (((int64_t)b * a.nq_max + i) * a.Hkv + h) * a.G * DH + (int64_t)(r - i * a.G) * DH;
+  };
+  for (int r = tid; r < tiles * 16; r += CA_THREADS) {
+    float2 f = make_float2(INFINITY, 0.f);
     if (r < live_rows) {
       const float* ml = row_ml + (pair * a.nq_max * a.G + r) * 2;
-      const float rw = row_weight ? row_weight[(int64_t)b * a.nq_max + r / a.G] : 1.f;
-      if (ml[1] != 0.f) mc = make_float2(ml[0] == -INFINITY ? 0.f : ml[0], rw / ml[1]);
+      f = row_factor(ml[0], ml[1], sw.rating(b, a.nq_max, r / a.G));
     }
-    rows_mc[r] = mc;
+    factor[r] = f;
+  }
+  if (QLDS) {
+    for (int x = tid; x < tiles * 16 * (DH / V); x += CA_THREADS) {
+      const int r = x / (DH / V), c = x % (DH / V) * V;
+      *reinterpret_cast<u16x8*>(qs + r * PITCH + c) = *reinterpret_cast<const u16x8*>(q_row(min(r, live_rows - 1)) + c);
+    }
   }
   __syncthreads();
-  const int key0 = blockIdx.x * KEYS + wave * SUBS * 16;
-  if (key0 >= total) return;
-  const T* kb = (const T*)a.k + b * a.sb + h * a.sh;
-  typename X::Step step[SUBS / PER];
-#pragma unroll
-  for (int i = 0; i < SUBS / PER; ++i) X::load_k(step[i], kb, key0 + i * X::KT, total - 1, l, g);
-  const bool tail = key0 + SUBS * 16 > L;
   const float scale_log2 = a.scale * LOG2E;
-  float col[SUBS];
+  auto turn = [&](int u, int key0) {
+    const bool tail = key0 + SW_CHUNK > L;
+    float col[SUBS];
 #pragma unroll
-  for (int s = 0; s < SUBS; ++s) col[s] = 0.f;
-  for (int t = 0; t < tiles; ++t) {
-    const int row = min(t * 16 + l, live_rows - 1), i = row / a.G, u = row - i * a.G;
-    typename X::Query q;
-    X::load(q, (const T*)a.q + (((int64_t)b * a.nq_max + i) * a.Hkv + h) * a.G * DH + (int64_t)u * DH, g);
-    float2 mc[4];
+    for (int s = 0; s < SUBS; ++s) col[s] = 0.f;
+    for (int t = 0; t < tiles; ++t) {
+      typename X::Query q;
+      X::load(q, QLDS ? qs + (t * 16 + l) * PITCH : q_row(min(t * 16 + l, live_rows - 1)), g);
+      float2 f[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) mc[r] = rows_mc[t * 16 + 4 * g + r];
+      for (int r = 0; r < 4; ++r) f[r] = factor[t * 16 + 4 * g + r];
 #pragma unroll
-    for (int s = 0; s < SUBS; ++s) {
-      f32x4 st{0.f, 0.f, 0.f, 0.f};
-      X::col_scores(st, step[s / PER], s % PER, q);
+      for (int s = 0; s < SUBS; ++s) {
+        f32x4 st{0.f, 0.f, 0.f, 0.f};
+        X::col_scores(st, step[u][s / X::SUBS], s % X::SUBS, q);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        bool vis = t * 16 + 4 * g + r < live_rows;
-        if (tail) {
-          const int key = key0 + s * 16 + l, j = key - L;
-          if (vis && j >= 0) {
-            const int node = (t * 16 + 4 * g + r) / a.G;
-            const uint64_t* mp = a.mask + ((int64_t)b * a.nq_max + node) * ADT_MASK_WORDS;
+        for (int r = 0; r < 4; ++r) {
+          const int row = t * 16 + 4 * g + r, key = key0 + s * 16 + l, j = key - L;
+          bool vis = row < live_rows;
+          if (tail && vis && j >= 0) {
+            const uint64_t* mp = a.mask + ((int64_t)b * a.nq_max + row / a.G) * ADT_MASK_WORDS;
             vis = j < ADT_MAX_NODES && (mp[j >> 6] >> (j & 63) & 1);
           }
+          const float p = exp2_hw(fmaf(st[r], scale_log2, -f[r].x)) * f[r].y;
+          col[s] += vis ? p : 0.f;
         }
-        const float p = exp2_hw(fmaf(st[r], scale_log2, -mc[r].x)) * mc[r].y;
-        col[s] += vis ? p : 0.f;
+      }
+    }
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
+      col[s] = xor16_add(col[s]);
+      col[s] = xor32_add(col[s]);
+      const int key = key0 + s * 16 + l;
+      if (g == s && key < total) sw.store(b, h, key, L, col[s]);
+    }
+  };
+  const int stride = CA_WAVES * SW_CHUNK;
+  int key0 = first + wave * SW_CHUNK;
+  for (int c = 0; c < turns && key0 < total; c += 2, key0 += 2 * stride) {
+    request(1, key0 + stride);
+    turn(0, key0);
+    if (c + 1 >= turns || key0 + stride >= total) break;
+    request(0, key0 + 2 * stride);
+    turn(1, key0 + stride);
+  }
+}
+
+// The same where the attention kept its masked scores (kept [B][Hkv][rows][kv_cap] fp32: few rows), and
+// the merge of its splits in the same launch: the first `merges` workgroups of a pair merge a row each,
+// the others take ST_KEYS keys, for which they merge the rows' maxima and sums themselves.
+constexpr int ST_KEYS = 4 * CA_THREADS, ST_ROWS = 16;
+__global__ __launch_bounds__(CA_THREADS) void slot_weights_kept_kernel(CacheAttn a, Deal deal, int is_bf16, int merges,
+                                                                       const float* __restrict__ kept,
+                                                                       const float* __restrict__ part_o,
+                                                                       const float* __restrict__ part_ml,
+                                                                       SlotWeights sw) {
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
+  __shared__ MergeScratch sh;
+  if ((int)blockIdx.x < merges) {
+    merge_rows(a, deal, ST_ROWS, is_bf16, blockIdx.x, CA_THREADS / (a.Dh / 4), h, b, part_o, part_ml, nullptr, sh);
+    return;
+  }
+  const int L = max(0, min(a.kv_len[b], a.kv_cap));
+  const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
+  const int key0 = (blockIdx.x - merges) * ST_KEYS + tid;
+  if (key0 - tid >= total) return;
+  __shared__ float2 factor[ST_ROWS];
+  const int rows = a.nq_max * a.G, live_rows = max(0, min(a.n_q[b], a.nq_max)) * a.G;
+  const int64_t pair = (int64_t)b * a.Hkv + h;
+  {
+    // row r's splits by the 16 lanes 16 r .. 16 r + 15
+    const int r = tid / 16;
+    float m = -INFINITY, ls = 0.f;
+    if (r < live_rows) {
+      const int splits = deal.live ? deal.live[(int64_t)b * a.Hkv + h] : 1;
+      const float* ml = part_ml + (pair * deal.splits * rows + r) * 2;
+      for (int s = tid % 16; s < splits; s += 16) m = fmaxf(m, ml[(int64_t)s * rows * 2]);
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, WAVE));
+      for (int s = tid % 16; s < splits; s += 16) {
+        const float ms = ml[(int64_t)s * rows * 2], l = ml[(int64_t)s * rows * 2 + 1];
+        if (ms != -INFINITY || l != 0.f) ls += l * exp2_hw(ms - (m == -INFINITY ? 0.f : m));
+      }
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) ls += __shfl_xor(ls, o, WAVE);
+    }
+    if (tid % 16 == 0) factor[r] = r < live_rows ? row_factor(m, ls, sw.rating(b, a.nq_max, r / a.G)) : make_float2(INFINITY, 0.f);
+  }
+  __syncthreads();
+  const float scale_log2 = a.scale * LOG2E;
+  const float* s0 = kept + pair * rows * a.kv_cap;
+  float sum[ST_KEYS / CA_THREADS] = {};
+  for (int r = 0; r < live_rows; r += 4) {
+    float x[4][ST_KEYS / CA_THREADS];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < ST_KEYS / CA_THREADS; ++j)
+        x[u][j] = s0[(int64_t)min(r + u, live_rows - 1) * a.kv_cap + min(key0 + j * CA_THREADS, total - 1)];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (r + u >= live_rows) continue;
+      const float2 f = factor[r + u];
+#pragma unroll
+      for (int j = 0; j < ST_KEYS / CA_THREADS; ++j) {
+        // (a masked score is -inf and stays 0 whatever the row's factor: not NaN for a row that is)
+        const float p = exp2_hw(fmaf(x[u][j], scale_log2, -f.x)) * f.y;
+        sum[j] += x[u][j] == -INFINITY ? 0.f : p;
       }
     }
   }
 #pragma unroll
-  for (int s = 0; s < SUBS; ++s) {
-    col[s] = xor16_add(col[s]);
-    col[s] = xor32_add(col[s]);
-  }
-#pragma unroll
-  for (int s = 0; s < SUBS; ++s) {
-    const int key = key0 + s * 16 + l;
-    if (g == s && key < total) {
-      const int64_t at = b * stride_wb + h * stride_wh + key;
-      w_out[at] = key < L && w_in ? decay * w_in[at] + col[s] : col[s];
-    }
-  }
+  for (int j = 0; j < ST_KEYS / CA_THREADS; ++j)
+    if (key0 + j * CA_THREADS < total) sw.store(b, h, key0 + j * CA_THREADS, L, sum[j]);
 }
 
 // ----------------------------------------------------------------------------- host
@@ -921,7 +1068,8 @@ static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
   p.deep = p.shared && pairs * expect < 8 * 256 ? 3 : 1;
   const int slots = p.shared ? (p.deep > 1 ? 256 : 512) : p.tiles == 1 ? 768 : p.tiles == 2 ? 512 : 256;
   p.per = (int)std::max<int64_t>(least, (pairs * expect + slots - 1) / slots);
-  int64_t splits = (most + p.per - 1) / p.per;
+  // (a few units more than one share are no reason for partial results and their merge)
+  int64_t splits = most <= p.per + p.per / 4 ? 1 : (most + p.per - 1) / p.per;
   splits = std::min<int64_t>(splits, std::max<int64_t>(1, (p.deep > 1 ? slots : 4 * slots) / pairs));
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, 64));
   return p;
@@ -935,10 +1083,10 @@ static size_t part_floats(const CacheAttn& a, int B, const CachePlan& p) {
 
 template <typename T, int DH, bool SPARSE>
 static void attn_launch(const CacheAttn& a, int B, const CachePlan& p, const Deal& deal, float* part_o, float* part_ml,
-                        hipStream_t st) {
+                        float* kept, hipStream_t st) {
   const size_t list = SPARSE ? align_up16((size_t)a.n_blk * 2) : 0;
   const dim3 grid(a.Hkv * p.groups, B, p.splits);
-#define ADT_CA(RT) cache_attn_kernel<T, DH, RT, SPARSE><<<grid, CA_THREADS, list, st>>>(a, deal, part_o, part_ml)
+#define ADT_CA(RT) cache_attn_kernel<T, DH, RT, SPARSE><<<grid, CA_THREADS, list, st>>>(a, deal, part_o, part_ml, kept)
 #define ADT_CS(NW, KH, P) \
   cache_attn_shared_kernel<DH, NW, KH, P, SPARSE><<<grid, NW * WAVE, list, st>>>(a, deal, part_o, part_ml)
   if constexpr (sizeof(T) == 2) {
@@ -964,16 +1112,24 @@ static void attn_launch(const CacheAttn& a, int B, const CachePlan& p, const Dea
 #undef ADT_CA
 }
 
-// part: partials of the plan's splits (part_floats), row_ml: [B][Hkv][rows][2] or null
-static adt_status attn_passes(const CacheAttn& a, int B, const CachePlan& p, float* part, float* row_ml, int dtype,
-                              hipStream_t st) {
+// The attention's partial results in `part` (part_floats); one split leaves its rows' maxima and sums in
+// row_ml ([B][Hkv][rows][2], may be null).
+struct Partials {
+  float *o, *ml;
+  Deal deal;
+};
+static Partials partials(const CacheAttn& a, int B, const CachePlan& p, float* part, float* row_ml) {
+  if (p.splits == 1) return Partials{nullptr, row_ml, Deal{1, p.per, nullptr}};
   const size_t rows = (size_t)B * a.Hkv * p.splits * a.nq_max * a.G;
-  float* part_o = p.splits > 1 ? part : nullptr;
-  float* part_ml = p.splits > 1 ? part + rows * a.Dh : row_ml;
-  const Deal deal{p.splits, p.per, p.splits > 1 ? (int32_t*)(part_ml + rows * 2) : nullptr};
-#define ADT_AL(TV, DHV)                                                        \
-  if (a.block) attn_launch<TV, DHV, true>(a, B, p, deal, part_o, part_ml, st);       \
-  else attn_launch<TV, DHV, false>(a, B, p, deal, part_o, part_ml, st)
+  float* ml = part + rows * a.Dh;
+  return Partials{part, ml, Deal{p.splits, p.per, (int32_t*)(ml + rows * 2)}};
+}
+
+static adt_status attn_launches(const CacheAttn& a, int B, const CachePlan& p, const Partials& w, float* kept, int dtype,
+                                hipStream_t st) {
+#define ADT_AL(TV, DHV)                                                                  \
+  if (a.block) attn_launch<TV, DHV, true>(a, B, p, w.deal, w.o, w.ml, kept, st);         \
+  else attn_launch<TV, DHV, false>(a, B, p, w.deal, w.o, w.ml, kept, st)
   if (dtype == ADT_BF16) {
     if (a.Dh == 128) { ADT_AL(uint16_t, 128); }
     else { ADT_AL(uint16_t, 64); }
@@ -983,12 +1139,18 @@ static adt_status attn_passes(const CacheAttn& a, int B, const CachePlan& p, flo
   }
 #undef ADT_AL
   ADT_LAUNCH_CHECK();
-  if (p.splits > 1) {
-    const int threads = a.nq_max * a.G * (a.Dh / 4);
-    cache_merge_kernel<<<dim3((threads + CA_THREADS - 1) / CA_THREADS, a.Hkv, B), CA_THREADS, 0, st>>>(
-        a, deal, 16 * p.tiles, dtype == ADT_BF16, part_o, part_ml, row_ml);
-    ADT_LAUNCH_CHECK();
-  }
+  return ADT_OK;
+}
+
+static adt_status merge_launch(const CacheAttn& a, int B, const CachePlan& p, const Partials& w, float* row_ml, int dtype,
+                               hipStream_t st) {
+  if (p.splits == 1) return ADT_OK;
+  // a thread for every four outputs, or for few outputs and many splits several
+  const int rows = a.nq_max * a.G, fit = CA_THREADS / (a.Dh / 4);
+  const int count = p.splits > 8 && (int64_t)B * a.Hkv * rows * (a.Dh / 4) < 65536 ? fit : 1;
+  cache_merge_kernel<<<dim3((rows * count + fit - 1) / fit, a.Hkv, B), CA_THREADS, 0, st>>>(
+      a, w.deal, 16 * p.tiles, count, dtype == ADT_BF16, w.o, w.ml, row_ml);
+  ADT_LAUNCH_CHECK();
   return ADT_OK;
 }
 
@@ -1020,34 +1182,70 @@ adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb
   adt_status e = launch_block_select(a.q, means, mb, mh, a.kv_len, a.n_q, B, a.Hkv, a.G, a.Dh, a.nq_max, a.kv_cap,
                                      a.block, a.n_sel, n_first, n_last, dtype, ws, a.lists, sel, st);
   if (e) return e;
-  return attn_passes(a, B, p, (float*)(base + w.part), nullptr, dtype, st);
+  const Partials parts = partials(a, B, p, (float*)(base + w.part), nullptr);
+  e = attn_launches(a, B, p, parts, nullptr, dtype, st);
+  return e ? e : merge_launch(a, B, p, parts, nullptr, dtype, st);
 }
 
-static size_t row_ml_bytes(const CacheAttn& a, int B) {
-  return align_up16((size_t)B * a.Hkv * a.nq_max * a.G * 2 * sizeof(float));
+// Workspace of attention that rates its slots: the rows' maxima and sums, the scores where they are
+// kept, partial results.  Scores are kept, instead of computed again from the keys, where they take
+// at most an eighth of the keys' bytes (written and read, a quarter of reading the keys again: one row
+// of four heads over 65333 slots of 8 key-value heads, 32.7 us -> 8 for the slots' weights and the merge).
+struct WeightsWs {
+  bool keep;
+  size_t kept, part, bytes;
+};
+static WeightsWs weights_ws(const CacheAttn& a, int B, const CachePlan& p, int dtype) {
+  const int rows = a.nq_max * a.G, es = dtype == ADT_BF16 ? 2 : 4;
+  const size_t pairs = (size_t)B * a.Hkv;
+  WeightsWs w;
+  w.keep = rows <= ST_ROWS && rows * 4 * 8 <= a.Dh * es;
+  w.kept = align_up16(pairs * rows * 2 * sizeof(float));
+  w.part = w.kept + (w.keep ? align_up16(pairs * rows * a.kv_cap * sizeof(float)) : 0);
+  w.bytes = w.part + part_floats(a, B, p) * sizeof(float);
+  return w;
 }
 
 size_t weights_attn_ws_bytes(const CacheAttn& a, int B, int dtype) {
-  return row_ml_bytes(a, B) + part_floats(a, B, cache_plan(a, B, dtype)) * sizeof(float);
+  return weights_ws(a, B, cache_plan(a, B, dtype), dtype).bytes;
 }
 
 adt_status launch_weights_attn(const CacheAttn& a, int B, const float* w_in, float* w_out, int64_t stride_wb,
                                int64_t stride_wh, float decay, const float* row_weight, int dtype, void* ws,
                                hipStream_t st) {
-  float* row_ml = (float*)ws;
-  adt_status e = attn_passes(a, B, cache_plan(a, B, dtype), (float*)((char*)ws + row_ml_bytes(a, B)), row_ml, dtype, st);
+  const CachePlan p = cache_plan(a, B, dtype);
+  const WeightsWs w = weights_ws(a, B, p, dtype);
+  const SlotWeights sw{w_in, w_out, stride_wb, stride_wh, decay, row_weight};
+  float *row_ml = (float*)ws, *kept = w.keep ? (float*)((char*)ws + w.kept) : nullptr;
+  const Partials parts = partials(a, B, p, (float*)((char*)ws + w.part), row_ml);
+  adt_status e = attn_launches(a, B, p, parts, kept, dtype, st);
   if (e) return e;
-  const size_t lds = (size_t)(a.nq_max * a.G + 15) / 16 * 16 * sizeof(float2);
-#define ADT_SW(TV, DHV)                                                                                             \
-  slot_weights_kernel<TV, DHV><<<dim3((a.kv_cap + CA_WAVES * ColSubs<TV>::n * 16 - 1) / (CA_WAVES * ColSubs<TV>::n * 16), \
-                                      a.Hkv, B),                                                                    \
-                                 CA_THREADS, lds, st>>>(a, row_ml, w_in, w_out, stride_wb, stride_wh, decay, row_weight)
+  const int rows = a.nq_max * a.G;
+  if (w.keep) {
+    const int merges = p.splits > 1 ? rows : 0;
+    slot_weights_kept_kernel<<<dim3(merges + (a.kv_cap + ST_KEYS - 1) / ST_KEYS, a.Hkv, B), CA_THREADS, 0, st>>>(
+        a, parts.deal, dtype == ADT_BF16, merges, kept, parts.o, parts.ml, sw);
+    ADT_LAUNCH_CHECK();
+    return ADT_OK;
+  }
+  e = merge_launch(a, B, p, parts, row_ml, dtype, st);
+  if (e) return e;
+  // turns: four where that leaves two workgroups a CU or more, fewer for fewer keys
+  const int64_t units = ((int64_t)a.kv_cap + CA_WAVES * SW_CHUNK - 1) / (CA_WAVES * SW_CHUNK);
+  const int turns = (int)std::max<int64_t>(1, std::min<int64_t>(4, units * B * a.Hkv / 512));
+  const dim3 grid((units + turns - 1) / turns, a.Hkv, B);
+  const int padded = (rows + 15) / 16 * 16;
+#define ADT_SW(TV, DHV)                                                                                                 \
+  if (rows <= SlotTile<TV, DHV>::QROWS)                                                                                 \
+    slot_weights_kernel<TV, DHV, true>                                                                                  \
+        <<<grid, CA_THREADS, padded * (sizeof(float2) + SlotTile<TV, DHV>::PITCH * sizeof(TV)), st>>>(a, row_ml, turns, sw);   \
+  else slot_weights_kernel<TV, DHV, false><<<grid, CA_THREADS, padded * sizeof(float2), st>>>(a, row_ml, turns, sw)
   if (dtype == ADT_BF16) {
-    if (a.Dh == 128) ADT_SW(uint16_t, 128);
-    else ADT_SW(uint16_t, 64);
+    if (a.Dh == 128) { ADT_SW(uint16_t, 128); }
+    else { ADT_SW(uint16_t, 64); }
   } else {
-    if (a.Dh == 128) ADT_SW(float, 128);
-    else ADT_SW(float, 64);
+    if (a.Dh == 128) { ADT_SW(float, 128); }
+    else { ADT_SW(float, 64); }
   }
 #undef ADT_SW
   ADT_LAUNCH_CHECK();
