@@ -849,9 +849,12 @@ struct SlotWeights {
   __device__ __forceinline__ float rating(int b, int nq_max, int node) const {
     return row_weight ? row_weight[(int64_t)b * nq_max + node] : 1.f;
   }
-  __device__ __forceinline__ void store(int b, int h, int key, int L, float sum) const {
-    const int64_t at = b * stride_b + h * stride_h + key;
-    out[at] = key < L && in ? decay * in[at] + sum : sum;
+  // the earlier weight of a slot (0: none), and its new one
+  __device__ __forceinline__ float before(int b, int h, int key, int L) const {
+    return key < L && in ? in[b * stride_b + h * stride_h + key] : 0.f;
+  }
+  __device__ __forceinline__ void store(int b, int h, int key, int L, float was, float sum) const {
+    out[b * stride_b + h * stride_h + key] = key < L && in ? decay * was + sum : sum;
   }
 };
 
@@ -918,50 +921,72 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
   }
   __syncthreads();
   const float scale_log2 = a.scale * LOG2E;
-  auto turn = [&](int u, int key0) {
+  // (a turn's earlier weights are requested before the next turn's keys: loads return in order, and
+  // asked for last they would have every turn wait for the keys of the next)
+  auto turn = [&](int u, int key0, const float (&was)[SUBS]) {
     const bool tail = key0 + SW_CHUNK > L;
     float col[SUBS];
 #pragma unroll
     for (int s = 0; s < SUBS; ++s) col[s] = 0.f;
-    for (int t = 0; t < tiles; ++t) {
+    // masked: some row of the tile is none, or some key is the tree's
+    auto tile = [&](auto masked_tag, int t) {
+      constexpr bool MASKED = decltype(masked_tag)::value;
       typename X::Query q;
       X::load(q, QLDS ? qs + (t * 16 + l) * PITCH : q_row(min(t * 16 + l, live_rows - 1)), g);
       float2 f[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) f[r] = factor[t * 16 + 4 * g + r];
+      f32x4 st[SUBS];
 #pragma unroll
       for (int s = 0; s < SUBS; ++s) {
-        f32x4 st{0.f, 0.f, 0.f, 0.f};
-        X::col_scores(st, step[u][s / X::SUBS], s % X::SUBS, q);
+        st[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+        X::col_scores(st[s], step[u][s / X::SUBS], s % X::SUBS, q);
+      }
+#pragma unroll
+      for (int s = 0; s < SUBS; ++s)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int row = t * 16 + 4 * g + r, key = key0 + s * 16 + l, j = key - L;
-          bool vis = row < live_rows;
-          if (tail && vis && j >= 0) {
-            const uint64_t* mp = a.mask + ((int64_t)b * a.nq_max + row / a.G) * ADT_MASK_WORDS;
-            vis = j < ADT_MAX_NODES && (mp[j >> 6] >> (j & 63) & 1);
+          const float p = exp2_hw(fmaf(st[s][r], scale_log2, -f[r].x)) * f[r].y;
+          if (MASKED) {
+            const int row = t * 16 + 4 * g + r, j = key0 + s * 16 + l - L;
+            bool vis = row < live_rows;
+            if (vis && j >= 0) {
+              const uint64_t* mp = a.mask + ((int64_t)b * a.nq_max + row / a.G) * ADT_MASK_WORDS;
+              vis = j < ADT_MAX_NODES && (mp[j >> 6] >> (j & 63) & 1);
+            }
+            col[s] += vis ? p : 0.f;
+          } else {
+            col[s] += p;
           }
-          const float p = exp2_hw(fmaf(st[r], scale_log2, -f[r].x)) * f[r].y;
-          col[s] += vis ? p : 0.f;
         }
-      }
+    };
+    for (int t = 0; t < tiles; ++t) {
+      if (tail || t * 16 + 16 > live_rows) tile(std::true_type{}, t);
+      else tile(std::false_type{}, t);
     }
 #pragma unroll
     for (int s = 0; s < SUBS; ++s) {
       col[s] = xor16_add(col[s]);
       col[s] = xor32_add(col[s]);
       const int key = key0 + s * 16 + l;
-      if (g == s && key < total) sw.store(b, h, key, L, col[s]);
+      if (g == s && key < total) sw.store(b, h, key, L, was[s], col[s]);
     }
+  };
+  auto earlier = [&](float (&was)[SUBS], int key0) {
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) was[s] = sw.before(b, h, key0 + s * 16 + l, L);
   };
   const int stride = CA_WAVES * SW_CHUNK;
   int key0 = first + wave * SW_CHUNK;
   for (int c = 0; c < turns && key0 < total; c += 2, key0 += 2 * stride) {
+    float was[SUBS];
+    earlier(was, key0);
     request(1, key0 + stride);
-    turn(0, key0);
+    turn(0, key0, was);
     if (c + 1 >= turns || key0 + stride >= total) break;
+    earlier(was, key0 + stride);
     request(0, key0 + 2 * stride);
-    turn(1, key0 + stride);
+    turn(1, key0 + stride, was);
   }
 }
 
@@ -1009,7 +1034,9 @@ __global__ __launch_bounds__(CA_THREADS) void slot_weights_kept_kernel(CacheAttn
   __syncthreads();
   const float scale_log2 = a.scale * LOG2E;
   const float* s0 = kept + pair * rows * a.kv_cap;
-  float sum[ST_KEYS / CA_THREADS] = {};
+  float sum[ST_KEYS / CA_THREADS] = {}, was[ST_KEYS / CA_THREADS];
+#pragma unroll
+  for (int j = 0; j < ST_KEYS / CA_THREADS; ++j) was[j] = sw.before(b, h, key0 + j * CA_THREADS, L);
   for (int r = 0; r < live_rows; r += 4) {
     float x[4][ST_KEYS / CA_THREADS];
 #pragma unroll
@@ -1031,7 +1058,7 @@ __global__ __launch_bounds__(CA_THREADS) void slot_weights_kept_kernel(CacheAttn
   }
 #pragma unroll
   for (int j = 0; j < ST_KEYS / CA_THREADS; ++j)
-    if (key0 + j * CA_THREADS < total) sw.store(b, h, key0 + j * CA_THREADS, L, sum[j]);
+    if (key0 + j * CA_THREADS < total) sw.store(b, h, key0 + j * CA_THREADS, L, was[j], sum[j]);
 }
 
 // ----------------------------------------------------------------------------- host
