@@ -35,6 +35,12 @@ constexpr int CA_THREADS = CA_WAVES * WAVE;
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
 
+template <bool NT, class V>
+__device__ __forceinline__ V load16(const V* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+
 // What the two types differ in.  Lane (l, g) = (lane % 16, lane / 16) holds the scores of row l and
 // the KT keys key(sub, r) = 16 sub + 4 g + r of a step, and the outputs dim(t, r) of row l.
 template <typename T, int DH>
@@ -62,12 +68,13 @@ struct Tile<uint16_t, DH> {
     for (int j = 0; j < KS; ++j) x.f[j] = *reinterpret_cast<const bf16x8*>(row + j * 32 + g * 8);
   }
   // the step's keys key0 .. key0 + 31; those past `last` repeat it
+  template <bool NT = true>
   static __device__ __forceinline__ void load_k(Step& s, const uint16_t* k, int key0, int last, int l, int g) {
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub) {
       const uint16_t* row = k + (int64_t)min(key0 + sub * 16 + l, last) * DH + g * 8;
 #pragma unroll
-      for (int j = 0; j < KS; ++j) s.k[sub][j] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(row + j * 32));
+      for (int j = 0; j < KS; ++j) s.k[sub][j] = load16<NT>(reinterpret_cast<const bf16x8*>(row + j * 32));
     }
   }
   static __device__ __forceinline__ void load_v(Step& s, const uint16_t* v, int key0, int last, int l, int g) {
@@ -152,10 +159,11 @@ struct Tile<float, DH> {
 #pragma unroll
     for (int j = 0; j < DH / 16; ++j) x.f[j] = *reinterpret_cast<const f32x4*>(row + j * 16 + g * 4);
   }
+  template <bool NT = true>
   static __device__ __forceinline__ void load_k(Step& s, const float* k, int key0, int last, int l, int g) {
     const float* row = k + (int64_t)min(key0 + l, last) * DH + g * 4;
 #pragma unroll
-    for (int j = 0; j < DH / 16; ++j) s.k[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(row + j * 16));
+    for (int j = 0; j < DH / 16; ++j) s.k[j] = load16<NT>(reinterpret_cast<const f32x4*>(row + j * 16));
   }
   static __device__ __forceinline__ void load_v(Step& s, const float* v, int key0, int last, int l, int g) {
 #pragma unroll
@@ -558,7 +566,7 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
       const int slot = r * NW * WAVE + tid, x = slot / CH, phys = slot % CH;
       const int half = x / KT;
       const int key = max(0, min((half ? key0[1] : key0[0]) + x % KT, half ? last[1] : last[0]));
-      kr[u][r] = __builtin_nontemporal_load(
+      kr[u][r] = load16<false>(      // (kept in the caches: the slots' weights take the keys once more)
           reinterpret_cast<const u16x8*>(kb + (int64_t)key * DH + (phys ^ swz_k<DH>(x)) * 8));
       vr[u][r] = __builtin_nontemporal_load(
           reinterpret_cast<const u16x8*>(vb + (int64_t)key * DH + (phys ^ swz_v<DH>(x)) * 8));
@@ -896,7 +904,7 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
   typename X::Step step[2][STEPS];
   auto request = [&](int u, int k0) {
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i) X::load_k(step[u][i], kb, min(k0, total - 1) + i * X::KT, total - 1, l, g);
+    for (int i = 0; i < STEPS; ++i) X::template load_k<false>(step[u][i], kb, min(k0, total - 1) + i * X::KT, total - 1, l, g);
   };
   request(0, first + wave * SW_CHUNK);
   float2* factor = reinterpret_cast<float2*>(rows_lds);
@@ -981,11 +989,11 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
   for (int c = 0; c < turns && key0 < total; c += 2, key0 += 2 * stride) {
     float was[SUBS];
     earlier(was, key0);
-    request(1, key0 + stride);
+    if (c + 1 < turns) request(1, key0 + stride);
     turn(0, key0, was);
     if (c + 1 >= turns || key0 + stride >= total) break;
     earlier(was, key0 + stride);
-    request(0, key0 + 2 * stride);
+    if (c + 2 < turns) request(0, key0 + 2 * stride);
     turn(1, key0 + stride, was);
   }
 }
