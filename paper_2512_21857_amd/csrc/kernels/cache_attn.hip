@@ -271,7 +271,6 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
   if (sp >= n_live) return;
   if (deal.live && sp == 0 && threadIdx.x == 0) deal.live[(int64_t)b * gridDim.x + blockIdx.x] = n_live;
   const uint64_t* marks = a.lists.marks + pair * a.n_blk * ADT_MASK_WORDS;
-  if (SPARSE) copy_list(a.lists.blocks + pair * a.n_blk, a.lists.count[pair], chosen);
   const T* kb = (const T*)a.k + b * a.sb + h * a.sh;
   const T* vb = (const T*)a.v + b * a.sb + h * a.sh;
 
@@ -293,6 +292,7 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
       aw1[t] = mp[1];
     }
   }
+  if (SPARSE) copy_list(a.lists.blocks + pair * a.n_blk, a.lists.count[pair], chosen);
   const float scale_log2 = a.scale * LOG2E;
   void* lds = smem + wave * X::LDS_BYTES;
 
@@ -515,7 +515,6 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
   if (deal.live && sp == 0 && tid == 0) deal.live[(int64_t)b * gridDim.x + blockIdx.x] = n_live;
   const int stages = max(0, ((steps + 1) / 2 - sp + n_live - 1) / n_live);   // of this split: sp, sp + n_live, ...
   const uint32_t* marks = reinterpret_cast<const uint32_t*>(a.lists.marks + pair * a.n_blk * ADT_MASK_WORDS);
-  if (SPARSE) copy_list(a.lists.blocks + pair * a.n_blk, a.lists.count[pair], chosen);
   const uint16_t* kb = (const uint16_t*)a.k + b * a.sb + h * a.sh;
   const uint16_t* vb = (const uint16_t*)a.v + b * a.sb + h * a.sh;
 
@@ -531,6 +530,7 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
     aw0 = mp[0];
     aw1 = mp[1];
   }
+  if (SPARSE) copy_list(a.lists.blocks + pair * a.n_blk, a.lists.count[pair], chosen);
   const bool tile_live = r0 + tile * 16 < live_rows;
   const float scale_log2 = a.scale * LOG2E;
 
