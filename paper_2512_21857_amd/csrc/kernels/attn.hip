@@ -50,16 +50,6 @@ __device__ __forceinline__ bool key_visible(int key, int k_end, int L, uint64_t 
 // are zero for every purpose here).
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Two floats written through to, or read from, the point where the device's XCDs see the same memory.
-__device__ __forceinline__ void agent_store2(float* p, float a, float b) {
-  const uint64_t v = (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a);
-  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 agent_load2(const float* p) {
-  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-
 // The work-balanced sequence order (defined with the shared-block kernel below).
 __device__ int balanced_seq(int y, int B, const int32_t* kv_len, const int32_t* n_q, const int32_t* n_tail,
                             int nq_max, int kv_cap, int* scratch);

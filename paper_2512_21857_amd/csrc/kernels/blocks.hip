@@ -97,11 +97,17 @@ __global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* _
     double s[4] = {0.0, 0.0, 0.0, 0.0};
     if (i0 + i < nq) {
       const T* qp = q + (((int64_t)b * nq_max + i0 + i) * Hkv + h) * G * DH + d;
-      for (int u = 0; u < G; ++u) {
-        T t[4];
-        __builtin_memcpy(t, __builtin_assume_aligned(qp + (int64_t)u * DH, 4 * sizeof(T)), 4 * sizeof(T));
+      for (int u0 = 0; u0 < G; u0 += 4) {       // four heads requested at a time
+        T t[4][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] += (double)Elem<T>::load(t, e);
+        for (int u = 0; u < 4; ++u)
+          __builtin_memcpy(t[u], __builtin_assume_aligned(qp + (int64_t)min(u0 + u, G - 1) * DH, 4 * sizeof(T)),
+                           4 * sizeof(T));
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (u0 + u < G)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += (double)Elem<T>::load(t[u], e);
       }
     }
 #pragma unroll
@@ -161,7 +167,10 @@ __device__ __forceinline__ void list_marked(const BlockLists& lists, int64_t pai
     }
     __syncthreads();
   }
-  if (threadIdx.x == 0) lists.count[pair] = n;
+  if (threadIdx.x == 0) {
+    lists.count[pair] = n;
+    lists.arrived[pair] = 0;
+  }
 }
 
 // Scores in an unsigned order: larger score, larger key; -0 equals +0; NaN below all.
@@ -311,32 +320,43 @@ __global__ __launch_bounds__(BC_THREADS) void block_choose_kernel(
   uint32_t* bits = reinterpret_cast<uint32_t*>(keys + (size_t)nq_max * n_blk);
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block, nq = min(n_q[b], nq_max);
+  // the first blocks' means, requested ahead of the queries' sums
+  const int c = tid % 16 * PER;
+  const float* mp = means + b * mb + h * mh + c;
+  f32x4 m[UN][PER / 4];
+  auto request = [&](int j0) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+#pragma unroll
+      for (int e = 0; e < PER / 4; ++e)
+        m[u][e] = *reinterpret_cast<const f32x4*>(mp + (int64_t)min(j0 + u * GROUPS, live - 1) * DH + 4 * e);
+  };
+  if (live > n_sel) request(tid / 16);
   for (int j = tid; j < live; j += BC_THREADS) bits[j] = 0;
   for (int x = tid; x < R * DH; x += BC_THREADS) {
     const int i = x / DH, d = x % DH;
     double s = 0.0;
     if (i < nq) {
       const T* qp = q + (((int64_t)b * nq_max + i) * Hkv + h) * G * DH + d;
-      for (int u = 0; u < G; ++u) s += (double)Elem<T>::load(qp, (int64_t)u * DH);
+      for (int u0 = 0; u0 < G; u0 += 4) {         // four heads requested at a time
+        float t[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) t[u] = Elem<T>::load(qp, (int64_t)min(u0 + u, G - 1) * DH);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s += u0 + u < G ? (double)t[u] : 0.0;
+      }
     }
     qs[i][d] = s;
   }
   __syncthreads();
   if (live > n_sel) {
-    const int c = tid % 16 * PER;
     double x[R][PER];
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int e = 0; e < PER; ++e) x[i][e] = qs[i][c + e];
-    const float* mp = means + b * mb + h * mh + c;
     for (int j0 = tid / 16; j0 < live; j0 += GROUPS * UN) {
-      f32x4 m[UN][PER / 4];
-#pragma unroll
-      for (int u = 0; u < UN; ++u)
-#pragma unroll
-        for (int e = 0; e < PER / 4; ++e)
-          m[u][e] = *reinterpret_cast<const f32x4*>(mp + (int64_t)min(j0 + u * GROUPS, live - 1) * DH + 4 * e);
+      if (j0 >= GROUPS * UN) request(j0);
 #pragma unroll
       for (int u = 0; u < UN; ++u)
 #pragma unroll

@@ -8,8 +8,8 @@
 // A workgroup holds RT tiles (16 RT rows) in registers; its waves and the other workgroups of the
 // same rows (splits) deal the keys out in steps among themselves, each step read by one wave only,
 // so K and V come straight from memory into registers and every slot is read once per 16 RT rows.
-// What the waves of a workgroup found is merged in LDS, what the splits found by a launch of its own,
-// always in one order.  Steps never straddle the end of the prefix: the tree's own slots, which the
+// What the waves of a workgroup found is merged in LDS, what the splits found by a launch of its own (few
+// rows over chosen blocks: by the last split), always in one order.  Steps never straddle the end of the prefix: the tree's own slots, which the
 // rows see through their ancestor masks, have steps of their own.
 //
 // (bf16 with more than 16 rows: cache_attn_shared_kernel.)  bf16 runs on the 16x16x32 MFMA, 32 keys a step, V transposed through LDS, probabilities rounded
@@ -216,6 +216,31 @@ __device__ __forceinline__ void copy_list(const uint16_t* blocks, int count, uin
   __syncthreads();
 }
 
+// Log-sum-exp merge of parts (m, l, o), eight at a time and in order.
+struct RunningMerge {
+  float m = -INFINITY, l = 0.f;
+  f32x4 o{0.f, 0.f, 0.f, 0.f};
+  // one part at the running maximum `top` (0 where that is -inf); one that saw nothing, (-inf, 0), adds nothing
+  __device__ __forceinline__ void add_one(float pm, float pl, const f32x4& po, float top) {
+    const float wt = pm == -INFINITY && pl == 0.f ? 0.f : exp2_hw(pm - top);
+    if (wt == 0.f && pl == pl) return;
+    l += wt * pl;
+    o += wt * po;
+  }
+  __device__ __forceinline__ void add(const float2 (&ml)[8], const f32x4 (&x)[8], int n, int stride = 1) {
+    float mn = m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mn = fmaxf(mn, ml[j].x);
+    const float top = mn == -INFINITY ? 0.f : mn, down = m == -INFINITY ? 1.f : exp2_hw(m - top);
+    m = mn;
+    l *= down;
+    o *= down;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j * stride < n) add_one(ml[j].x, ml[j].y, x[j], top);
+  }
+};
+
 // What a step's values that are not finite add to the rows that see them: o[t][r] (dim(t, r) of row
 // l) += p v over the keys of the step whose value v at that dim is one.  p: this lane's probabilities
 // of row l, for keys 16 sub + 4 g + r; seen(key): whether row l sees key k0 + key.
@@ -249,6 +274,7 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
                                                                                 float* __restrict__ kept) {
   typedef Tile<T, DH> X;
   constexpr int KT = X::KT, SUBS = X::SUBS, OT = X::OT;
+  constexpr bool MERGE = SPARSE && RT == 1;
   constexpr int MP = DH + 4;                                       // row of a merged tile
   constexpr int STEP_BYTES = CA_WAVES * X::LDS_BYTES;
   constexpr int MERGE_BYTES = CA_WAVES * 16 * (MP + 2) * 4;
@@ -461,13 +487,53 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
         const float inv = ls == 0.f ? 0.f : 1.f / ls;
         const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * DH + (int64_t)(rr % a.G) * DH + d;
         store4((T*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      } else if (MERGE) {
+        agent_store2(part_o + at * DH + d, acc[0], acc[1]);
+        agent_store2(part_o + at * DH + d + 2, acc[2], acc[3]);
       } else {
         *reinterpret_cast<f32x4*>(part_o + at * DH + d) = acc;
       }
       if (part_ml && d == 0) {
-        part_ml[at * 2] = M;
-        part_ml[at * 2 + 1] = ls;
+        if (MERGE) {
+          agent_store2(part_ml + at * 2, M, ls);
+        } else {
+          part_ml[at * 2] = M;
+          part_ml[at * 2 + 1] = ls;
+        }
       }
+    }
+  }
+  // Few rows over chosen blocks: the last split of the pair to get here merges them all, in split order,
+  // four dims of one row a thread.  The partials of a split are complete at the agent's coherence point
+  // (write-through stores, waited for) before its arrival counts, and are read past the local caches.
+  if constexpr (MERGE) {
+    if (n_live == 1) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    uint32_t* last = reinterpret_cast<uint32_t*>(smem);
+    if (threadIdx.x == 0)
+      *last = __hip_atomic_fetch_add(a.lists.arrived + pair, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+    __syncthreads();
+    if (*last != (uint32_t)n_live) return;
+    for (int idx = threadIdx.x; idx < live_rows * (DH / 4); idx += CA_THREADS) {
+      const int rr = idx / (DH / 4), d = idx % (DH / 4) * 4;
+      const int64_t base = pair * splits * rows + rr;
+      RunningMerge acc;
+      for (int s0 = 0; s0 < n_live; s0 += 8) {       // eight splits requested at a time
+        float2 ml[8];
+        f32x4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int64_t at = base + (int64_t)min(s0 + j, n_live - 1) * rows;
+          ml[j] = agent_load2(part_ml + at * 2);
+          const float2 lo = agent_load2(part_o + at * DH + d), hi = agent_load2(part_o + at * DH + d + 2);
+          x[j] = f32x4{lo.x, lo.y, hi.x, hi.y};
+        }
+        acc.add(ml, x, n_live - s0);
+      }
+      const float inv = acc.l == 0.f ? 0.f : 1.f / acc.l;
+      const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * DH + (int64_t)(rr % a.G) * DH + d;
+      store4((T*)a.out + at_o, acc.o[0] * inv, acc.o[1] * inv, acc.o[2] * inv, acc.o[3] * inv);
     }
   }
 }
@@ -782,15 +848,7 @@ __device__ __forceinline__ void merge_rows(const CacheAttn& a, const Deal& deal,
     row_ml[(pair * rows + rr) * 2] = part_ml[base * 2];
     row_ml[(pair * rows + rr) * 2 + 1] = part_ml[base * 2 + 1];
   }
-  float M = -INFINITY, ls = 0.f;
-  f32x4 acc{0.f, 0.f, 0.f, 0.f};
-  // (w, l, x) into the running (M, ls, acc); a part that saw nothing (-inf, 0) adds nothing
-  auto add = [&](float m, float l, const f32x4& x, float Mu) {
-    const float wt = m == -INFINITY && l == 0.f ? 0.f : exp2_hw(m - Mu);
-    if (wt == 0.f && l == l) return;
-    ls += wt * l;
-    acc += wt * x;
-  };
+  RunningMerge acc;
   for (int s0 = splits > 1 ? grp : splits; s0 < splits; s0 += 8 * count) {
     float2 ml[8];
     f32x4 x[8];
@@ -800,40 +858,31 @@ __device__ __forceinline__ void merge_rows(const CacheAttn& a, const Deal& deal,
       ml[j] = *reinterpret_cast<const float2*>(part_ml + at * 2);
       x[j] = *reinterpret_cast<const f32x4*>(part_o + at * a.Dh + d);
     }
-    float Mn = M;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) Mn = fmaxf(Mn, ml[j].x);
-    const float Mu = Mn == -INFINITY ? 0.f : Mn, down = M == -INFINITY ? 1.f : exp2_hw(M - Mu);
-    M = Mn;
-    ls *= down;
-    acc *= down;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (s0 + j * count < splits) add(ml[j].x, ml[j].y, x[j], Mu);
+    acc.add(ml, x, splits - s0, count);
   }
   if (count > 1) {
-    sh.acc[threadIdx.x] = acc;
-    sh.ml[threadIdx.x] = make_float2(M, ls);
+    sh.acc[threadIdx.x] = acc.o;
+    sh.ml[threadIdx.x] = make_float2(acc.m, acc.l);
     __syncthreads();
     if (grp > 0) return;
     const int n = min(count, splits);
-    for (int g = 1; g < n; ++g) M = fmaxf(M, sh.ml[threadIdx.x + g * per].x);
-    const float Mu = M == -INFINITY ? 0.f : M;
-    ls = 0.f;
-    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = 1; g < n; ++g) acc.m = fmaxf(acc.m, sh.ml[threadIdx.x + g * per].x);
+    const float top = acc.m == -INFINITY ? 0.f : acc.m;
+    acc.l = 0.f;
+    acc.o = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int g = 0; g < n; ++g) {
       const float2 ml = sh.ml[threadIdx.x + g * per];
-      add(ml.x, ml.y, sh.acc[threadIdx.x + g * per], Mu);
+      acc.add_one(ml.x, ml.y, sh.acc[threadIdx.x + g * per], top);
     }
   }
   if (splits <= 1) return;
-  const float inv = ls == 0.f ? 0.f : 1.f / ls;
+  const float inv = acc.l == 0.f ? 0.f : 1.f / acc.l;
   const int64_t at_o = (((int64_t)b * a.nq_max + rr / a.G) * a.Hkv + h) * a.G * a.Dh + (int64_t)(rr % a.G) * a.Dh + d;
-  if (bf16) store4((uint16_t*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-  else store4((float*)a.out + at_o, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+  if (bf16) store4((uint16_t*)a.out + at_o, acc.o[0] * inv, acc.o[1] * inv, acc.o[2] * inv, acc.o[3] * inv);
+  else store4((float*)a.out + at_o, acc.o[0] * inv, acc.o[1] * inv, acc.o[2] * inv, acc.o[3] * inv);
   if (row_ml && d == 0) {
-    row_ml[(pair * rows + rr) * 2] = M;
-    row_ml[(pair * rows + rr) * 2 + 1] = ls;
+    row_ml[(pair * rows + rr) * 2] = acc.m;
+    row_ml[(pair * rows + rr) * 2 + 1] = acc.l;
   }
 }
 
@@ -1191,7 +1240,7 @@ static adt_status merge_launch(const CacheAttn& a, int B, const CachePlan& p, co
 
 // Workspace of attention over chosen blocks: the selection's scratch, the lists, partial results.
 struct SparseWs {
-  size_t marks, blocks, count, part, bytes;
+  size_t marks, blocks, count, arrived, part, bytes;
 };
 static SparseWs sparse_ws(const CacheAttn& a, int B, const CachePlan& p) {
   const size_t pairs = (size_t)B * a.Hkv;
@@ -1199,7 +1248,8 @@ static SparseWs sparse_ws(const CacheAttn& a, int B, const CachePlan& p) {
   w.marks = align_up16(block_select_ws_bytes(B, a.Hkv, a.nq_max, a.n_blk));
   w.blocks = w.marks + pairs * a.n_blk * ADT_MASK_WORDS * sizeof(uint64_t);
   w.count = align_up16(w.blocks + pairs * a.n_blk * sizeof(uint16_t));
-  w.part = align_up16(w.count + pairs * sizeof(int32_t));
+  w.arrived = w.count + pairs * sizeof(int32_t);
+  w.part = align_up16(w.arrived + pairs * sizeof(uint32_t));
   w.bytes = w.part + part_floats(a, B, p) * sizeof(float);
   return w;
 }
@@ -1213,13 +1263,14 @@ adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb
   const CachePlan p = cache_plan(a, B, dtype);
   const SparseWs w = sparse_ws(a, B, p);
   char* base = (char*)ws;
-  a.lists = BlockLists{(int32_t*)(base + w.count), (uint16_t*)(base + w.blocks), (uint64_t*)(base + w.marks)};
+  a.lists = BlockLists{(int32_t*)(base + w.count), (uint16_t*)(base + w.blocks), (uint64_t*)(base + w.marks),
+                       (uint32_t*)(base + w.arrived)};
   adt_status e = launch_block_select(a.q, means, mb, mh, a.kv_len, a.n_q, B, a.Hkv, a.G, a.Dh, a.nq_max, a.kv_cap,
                                      a.block, a.n_sel, n_first, n_last, dtype, ws, a.lists, sel, st);
   if (e) return e;
   const Partials parts = partials(a, B, p, (float*)(base + w.part), nullptr);
   e = attn_launches(a, B, p, parts, nullptr, dtype, st);
-  return e ? e : merge_launch(a, B, p, parts, nullptr, dtype, st);
+  return e || p.tiles == 1 ? e : merge_launch(a, B, p, parts, nullptr, dtype, st);
 }
 
 // Workspace of attention that rates its slots: the rows' maxima and sums, the scores where they are

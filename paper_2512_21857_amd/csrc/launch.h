@@ -311,6 +311,7 @@ struct BlockLists {
   int32_t* count;        // [B][Hkv]
   uint16_t* blocks;      // [B][Hkv][n_blk]
   uint64_t* marks;       // [B][Hkv][n_blk][ADT_MASK_WORDS]
+  uint32_t* arrived;     // [B][Hkv] zeroed along with the lists, for the splits that read them
 };
 size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk);   // scratch (16-byte aligned)
 // Fills the lists (and sel, which may be null).

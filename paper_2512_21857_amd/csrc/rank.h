@@ -90,12 +90,7 @@ struct RankRow {
         for (int u = 0; u < S::COPIES; ++u) c[j] += sh.hist[u * (S::BINS + 1) + S::BINS - 1 - (tid * B + j)];
         sum += c[j];
       }
-      uint32_t incl = sum;
-#pragma unroll
-      for (int o = 1; o < WAVE; o <<= 1) {
-        const uint32_t up = __shfl_up(incl, o, WAVE);
-        if (lane >= o) incl += up;
-      }
+      const uint32_t incl = wave_prefix_sum(sum);
       if (lane == WAVE - 1) sh.wave_n[0][wave] = incl;
       __syncthreads();
       uint32_t above = incl - sum;
@@ -203,18 +198,12 @@ __device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need
     // lane l holds the digits 255 - 4 l down to 252 - 4 l
     const uint4 c = reinterpret_cast<const uint4*>(hist)[WAVE - 1 - lane];
     const uint32_t sum = c.x + c.y + c.z + c.w;
-    uint32_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < WAVE; o <<= 1) {
-      const uint32_t up = __shfl_up(incl, o, WAVE);
-      if (lane >= o) incl += up;
-    }
+    const uint32_t incl = wave_prefix_sum(sum);
     const uint32_t above = incl - sum;
     const int at = __ffsll((unsigned long long)__ballot(above < need && incl >= need)) - 1;
     // within that lane's four digits, from the top
-    const uint32_t rest = need - __shfl(above, at, WAVE);
-    const uint32_t w = __shfl(c.w, at, WAVE), z = __shfl(c.z, at, WAVE), y = __shfl(c.y, at, WAVE),
-                   x = __shfl(c.x, at, WAVE);
+    auto of_lane = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, at); };
+    const uint32_t rest = need - of_lane(above), w = of_lane(c.w), z = of_lane(c.z), y = of_lane(c.y), x = of_lane(c.x);
     uint32_t digit = 255 - 4 * at, over = 0, count = w;
     if (rest > w) { digit -= 1; over = w; count = z; }
     if (rest > w + z) { digit -= 1; over = w + z; count = y; }

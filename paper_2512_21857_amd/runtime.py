@@ -114,13 +114,18 @@ def kv_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len: torch.Tenso
 
 # The wrappers below are called once or more per layer of a decoding loop, where their own time
 # counts: they pass addresses as plain integers and check a tensor in one expression.
-def _on_device(fn, dev: int, *args) -> None:
+_I32, _I64, _F32, _F64, _U8 = torch.int32, torch.int64, torch.float32, torch.float64, torch.uint8
+_current_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _on_device(dev: int, fn, args: tuple) -> None:
     """fn(*args, stream) with device `dev` current, on its current stream."""
-    if torch._C._cuda_getDevice() == dev:
-        code = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if _current_device() == dev:
+        code = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            code = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+            code = fn(*args, _raw_stream(dev))
     if code:
         check(code)
 
@@ -155,8 +160,8 @@ def _caches(k_cache: torch.Tensor, v_cache: torch.Tensor, dev: int, dtype: torch
     if (len(shape) != 4 or strides[3] != 1 or strides[2] != shape[3] or k_cache.dtype is not dtype
             or k_cache.get_device() != dev or v_cache.shape != shape or v_cache.stride() != strides
             or v_cache.dtype is not dtype or v_cache.get_device() != dev):
-        raise ValueError(f"two caches [B][heads][slots][Dh] of {dtype} on device {dev} with contiguous rows and one layout "
-                         f"expected, not {tuple(shape)} {k_cache.dtype} with strides {strides} on {k_cache.device} and "
+        raise ValueError(f"two caches [B][heads][slots][Dh] of {dtype} on device {dev} with contiguous rows and one "
+                         f"layout expected, not {tuple(shape)} {k_cache.dtype} with strides {strides} on {k_cache.device} and "
                          f"{tuple(v_cache.shape)} {v_cache.dtype} with strides {v_cache.stride()} on {v_cache.device}")
     # the stride of a dimension of one is whatever the view left there
     sh = strides[1] if shape[1] > 1 else shape[2] * shape[3]
@@ -175,7 +180,7 @@ def rope_freqs(rot_dim: int, theta: float = 10000.0, scaling: str = "plain", fac
     freq = (C.c_double * max(rot_dim // 2, 1))()
     gain = C.c_float()
     check(lib().adt_rope_freqs(C.byref(cfg), freq, C.byref(gain)))
-    return torch.tensor(list(freq), dtype=torch.float64, device=device), gain.value
+    return torch.tensor(list(freq), dtype=_F64, device=device), gain.value
 
 
 def _rows(what: str, t: torch.Tensor, dev: int, dtype: torch.dtype, B: int, n: int, Dh: int):
@@ -203,17 +208,20 @@ def rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Te
     B, n, _, Dh = q.shape
     H, ldq = _rows("q", q, dev, dtype, B, n, Dh)
     Hkv, ldk = _rows("k", k, dev, dtype, B, n, Dh)
-    Hv, ldv = _rows("v", v, dev, dtype, B, n, Dh)
+    if v.shape == k.shape and v.stride() == k.stride() and v.dtype is dtype and v.get_device() == dev:
+        Hv, ldv = Hkv, ldk
+    else:
+        Hv, ldv = _rows("v", v, dev, dtype, B, n, Dh)
     cs, sb, sh = _caches(k_cache, v_cache, dev, dtype)
     if Hv != Hkv or cs[0] != B or cs[1] != Hkv or cs[3] != Dh:
         raise ValueError(f"{Hkv} key heads, {Hv} value heads and caches {tuple(cs)} do not go together")
     if out is None:
         out = torch.empty(B, n, H, Dh, dtype=dtype, device=q.device)
-    _on_device(lib().adt_rope_append, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), ldq, ldk, ldv,
-               _ptr("pos", pos, dev, torch.int32, (B, n)), _ptr("kv_len", kv_len, dev, torch.int32, (B,)),
-               _ptr("n_rows", n_rows, dev, torch.int32, (B,)), _ptr("freq", freq, dev, torch.float64, freq.shape), gain,
+    _on_device(dev, lib().adt_rope_append, (q.data_ptr(), k.data_ptr(), v.data_ptr(), ldq, ldk, ldv,
+               _ptr("pos", pos, dev, _I32, (B, n)), _ptr("kv_len", kv_len, dev, _I32, (B,)),
+               _ptr("n_rows", n_rows, dev, _I32, (B,)), _ptr("freq", freq, dev, _F64, freq.shape), gain,
                2 * freq.numel(), ROPE_LAYOUTS[layout], B, n, H, Hkv, Dh, _ptr("out", out, dev, dtype, (B, n, H, Dh)),
-               k_cache.data_ptr(), v_cache.data_ptr(), sb, sh, cs[2], dt)
+               k_cache.data_ptr(), v_cache.data_ptr(), sb, sh, cs[2], dt))
     return out
 
 
@@ -226,10 +234,10 @@ def block_keys(k_cache: torch.Tensor, kv_len: torch.Tensor, block: int, start: O
     (B, Hkv, S, Dh), sb, sh = _caches(k_cache, k_cache, dev, k_cache.dtype)
     n_blk = -(-S // block) if block > 0 else 0
     if out is None:
-        out = torch.zeros(B, Hkv, n_blk, Dh, dtype=torch.float32, device=k_cache.device)
-    _on_device(lib().adt_block_keys, dev, k_cache.data_ptr(), sb, sh, _opt("start", start, dev, torch.int32, (B,)),
-               _ptr("kv_len", kv_len, dev, torch.int32, (B,)), B, Hkv, Dh, block, S,
-               _ptr("out", out, dev, torch.float32, (B, Hkv, n_blk, Dh)), Hkv * n_blk * Dh, n_blk * Dh, dt)
+        out = torch.zeros(B, Hkv, n_blk, Dh, dtype=_F32, device=k_cache.device)
+    _on_device(dev, lib().adt_block_keys, (k_cache.data_ptr(), sb, sh, _opt("start", start, dev, _I32, (B,)),
+               _ptr("kv_len", kv_len, dev, _I32, (B,)), B, Hkv, Dh, block, S,
+               _ptr("out", out, dev, _F32, (B, Hkv, n_blk, Dh)), Hkv * n_blk * Dh, n_blk * Dh, dt))
     return out
 
 
@@ -241,19 +249,20 @@ def _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap, out):
     B, n, H, Dh = q.shape
     cs, sb, sh = _caches(k_cache, v_cache, dev, dtype)
     if cs[0] != B or cs[3] != Dh or cs[2] < kv_cap or not q.is_contiguous():
-        raise ValueError(f"contiguous queries {tuple(q.shape)}, caches {tuple(cs)} and {kv_cap} slots do not go together")
+        raise ValueError(f"contiguous queries {tuple(q.shape)}, caches {tuple(cs)} and {kv_cap} slots do not go "
+                         "together")
     if out is None:
         out = torch.empty_like(q)
     return (dev, dt, B, n, H, cs[1], Dh, sb, sh, out, _ptr("out", out, dev, dtype, (B, n, H, Dh)),
-            (_ptr("kv_len", kv_len, dev, torch.int32, (B,)), _ptr("n_q", n_q, dev, torch.int32, (B,)),
-             _ptr("n_tail", n_tail, dev, torch.int32, (B,)),
-             _ptr("mask", mask, dev, torch.int64, (B, n, abi.MASK_WORDS))))
+            (_ptr("kv_len", kv_len, dev, _I32, (B,)), _ptr("n_q", n_q, dev, _I32, (B,)),
+             _ptr("n_tail", n_tail, dev, _I32, (B,)),
+             _ptr("mask", mask, dev, _I64, (B, n, abi.MASK_WORDS))))
 
 
 def sparse_tree_attn_workspace(B: int, H: int, Hkv: int, Dh: int, nq_max: int, kv_cap: int, block: int, n_sel: int,
                                dtype: torch.dtype = torch.bfloat16, device="cuda") -> torch.Tensor:
     n = lib().adt_sparse_tree_attn_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, block, n_sel, ABI_DT[dtype])
-    return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+    return torch.empty(max(n, 16), dtype=_U8, device=device)
 
 
 def sparse_tree_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, means: torch.Tensor,
@@ -264,31 +273,31 @@ def sparse_tree_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     """Tree attention of q [B][n][H][Dh] over caches [B][Hkv][S][Dh] in which every row sees n_sel
     blocks of the prefix: the first n_first, the last n_last and the best by means (block_keys of
     the cache).  sel: int32 [B][n][Hkv][n_sel], gets the chosen blocks."""
-    dev, dt, B, n, H, Hkv, Dh, sb, sh, out, out_p, lens = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap,
-                                                                     out)
-    ms, mb, mh = _caches(means, means, dev, torch.float32)
+    dev, dt, B, n, H, Hkv, Dh, sb, sh, out, out_p, lens = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask,
+                                                                     kv_cap, out)
+    ms, mb, mh = _caches(means, means, dev, _F32)
     if ms[0] != B or ms[1] != Hkv or ms[3] != Dh or ms[2] * block < kv_cap:
         raise ValueError(f"means of {kv_cap} slots in blocks of {block} expected, not {tuple(ms)}")
     if workspace is None:
         workspace = sparse_tree_attn_workspace(B, H, Hkv, Dh, n, kv_cap, block, n_sel, q.dtype, q.device)
-    _on_device(lib().adt_sparse_tree_attn, dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sb, sh,
+    _on_device(dev, lib().adt_sparse_tree_attn, (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sb, sh,
                means.data_ptr(), mb, mh, *lens, B, H, Hkv, Dh, n, kv_cap, block, n_sel, n_first, n_last,
-               Dh ** -0.5 if scale is None else scale, dt, out_p, _opt("sel", sel, dev, torch.int32, (B, n, Hkv, n_sel)),
-               _ptr("workspace", workspace, dev, torch.uint8, workspace.shape), workspace.numel())
+               Dh ** -0.5 if scale is None else scale, dt, out_p, _opt("sel", sel, dev, _I32, (B, n, Hkv, n_sel)),
+               _ptr("workspace", workspace, dev, _U8, workspace.shape), workspace.numel()))
     return out
 
 
 def tree_attn_weights_workspace(B: int, H: int, Hkv: int, Dh: int, nq_max: int, kv_cap: int,
                                 dtype: torch.dtype = torch.bfloat16, device="cuda") -> torch.Tensor:
     n = lib().adt_tree_attn_weights_workspace_size(B, H, Hkv, Dh, nq_max, kv_cap, ABI_DT[dtype])
-    return torch.empty(max(n, 16), dtype=torch.uint8, device=device)
+    return torch.empty(max(n, 16), dtype=_U8, device=device)
 
 
 def _weights(what: str, w: torch.Tensor, dev: int, B: int, heads: int, slots: int):
     """(stride_b, stride_h) of weights fp32 [B][heads][>= slots] with contiguous slots."""
     shape, st = w.shape, w.stride()
     if (len(shape) != 3 or shape[0] != B or shape[1] != heads or shape[2] < slots or st[2] != 1
-            or w.dtype is not torch.float32 or w.get_device() != dev):
+            or w.dtype is not _F32 or w.get_device() != dev):
         raise ValueError(f"{what}: float32 [{B}][{heads}][{slots}] with contiguous slots on device {dev} expected, not "
                          f"{w.dtype} {tuple(shape)} with strides {st} on {w.device}")
     sh = st[1] if heads > 1 else shape[2]
@@ -305,21 +314,21 @@ def tree_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Ten
     [B][Hkv][>= kv_cap] = decay * weights + the softmax weight each slot received (row i counting
     row_weight[b][i]).  weights_out defaults to weights, in place, or to new zeros.  Returns
     (out, weights_out)."""
-    dev, dt, B, n, H, Hkv, Dh, sb, sh, out, out_p, lens = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask, kv_cap,
-                                                                     out)
+    dev, dt, B, n, H, Hkv, Dh, sb, sh, out, out_p, lens = _attn_args(q, k_cache, v_cache, kv_len, n_q, n_tail, mask,
+                                                                     kv_cap, out)
     if weights_out is None:
-        weights_out = weights if weights is not None else torch.zeros(B, Hkv, k_cache.shape[2], dtype=torch.float32,
+        weights_out = weights if weights is not None else torch.zeros(B, Hkv, k_cache.shape[2], dtype=_F32,
                                                                       device=q.device)
     wb, wh = _weights("weights_out", weights_out, dev, B, Hkv, kv_cap)
     if weights is not None and _weights("weights", weights, dev, B, Hkv, kv_cap) != (wb, wh):
         raise ValueError("weights and weights_out must have the same strides")
     if workspace is None:
         workspace = tree_attn_weights_workspace(B, H, Hkv, Dh, n, kv_cap, q.dtype, q.device)
-    _on_device(lib().adt_tree_attn_weights, dev, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sb, sh, *lens, B, H,
-               Hkv, Dh, n, kv_cap, Dh ** -0.5 if scale is None else scale, dt, out_p,
+    _on_device(dev, lib().adt_tree_attn_weights, (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), sb, sh, *lens,
+               B, H, Hkv, Dh, n, kv_cap, Dh ** -0.5 if scale is None else scale, dt, out_p,
                None if weights is None else weights.data_ptr(), weights_out.data_ptr(), wb, wh, decay,
-               _opt("row_weight", row_weight, dev, torch.float32, (B, n)),
-               _ptr("workspace", workspace, dev, torch.uint8, workspace.shape), workspace.numel())
+               _opt("row_weight", row_weight, dev, _F32, (B, n)),
+               _ptr("workspace", workspace, dev, _U8, workspace.shape), workspace.numel()))
     return out, weights_out
 
 
@@ -345,14 +354,13 @@ def kv_evict(k_cache: torch.Tensor, v_cache: torch.Tensor, weights: torch.Tensor
             raise ValueError(f"k_out: {(B, slices, min(S, budget), Dh)} expected, not {tuple(os)}")
         owb, ows = _weights("weights_out", weights_out, dev, B, slices, min(S, budget))
     if kept is None:
-        kept = torch.full((B, slices, max(budget, 0)), -1, dtype=torch.int32, device=k_cache.device)
+        kept = torch.full((B, slices, max(budget, 0)), -1, dtype=_I32, device=k_cache.device)
     if new_len is None:
-        new_len = torch.empty(B, dtype=torch.int32, device=k_cache.device)
-    _on_device(lib().adt_kv_evict, dev, k_cache.data_ptr(), v_cache.data_ptr(), weights.data_ptr(), sb, ss, wb, ws,
-               _ptr("kv_len", kv_len, dev, torch.int32, (B,)), B, slices, Dh, S, budget, n_first, n_last, k_out.data_ptr(),
+        new_len = torch.empty(B, dtype=_I32, device=k_cache.device)
+    _on_device(dev, lib().adt_kv_evict, (k_cache.data_ptr(), v_cache.data_ptr(), weights.data_ptr(), sb, ss, wb, ws,
+               _ptr("kv_len", kv_len, dev, _I32, (B,)), B, slices, Dh, S, budget, n_first, n_last, k_out.data_ptr(),
                v_out.data_ptr(), weights_out.data_ptr(), osb, oss, owb, ows,
-               _ptr("kept", kept, dev, torch.int32, (B, slices, budget)), _ptr("new_len", new_len, dev, torch.int32, (B,)),
-               dt)
+               _ptr("kept", kept, dev, _I32, (B, slices, budget)), _ptr("new_len", new_len, dev, _I32, (B,)), dt))
     return kept, new_len
 
 
@@ -362,9 +370,9 @@ def weights_compact(weights: torch.Tensor, kv_len: torch.Tensor, path: torch.Ten
     dev = _dt(weights)[0]
     B, slices, S = weights.shape
     wb, ws = _weights("weights", weights, dev, B, slices, S)
-    _on_device(lib().adt_weights_compact, dev, weights.data_ptr(), B, slices, wb, ws,
-               _ptr("kv_len", kv_len, dev, torch.int32, (B,)), S, _ptr("path", path, dev, torch.int32, (B, path.shape[-1])),
-               path.shape[-1], _ptr("n_acc", n_acc, dev, torch.int32, (B,)), a_max)
+    _on_device(dev, lib().adt_weights_compact, (weights.data_ptr(), B, slices, wb, ws,
+               _ptr("kv_len", kv_len, dev, _I32, (B,)), S, _ptr("path", path, dev, _I32, (B, path.shape[-1])),
+               path.shape[-1], _ptr("n_acc", n_acc, dev, _I32, (B,)), a_max))
 
 
 def accept_cfg(mode: str = "greedy", temperature: float = 1.0, top_k: int = 0, delta: float = 0.0,
