@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/adt.h"
 
 namespace adt {
@@ -166,6 +168,18 @@ __device__ __forceinline__ void agent_store2(float* p, float a, float b) {
 __device__ __forceinline__ float2 agent_load2(const float* p) {
   const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// Maximum over the wave: rotations within the rows of 16 lanes, then lane swaps (VALU only).
+__device__ __forceinline__ float wave_max_dpp(float v) {
+  auto turned = [](float x, auto ctrl) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  v = fmaxf(v, turned(v, std::integral_constant<int, 0x128>{}));      // row_ror 8, 4, 2, 1
+  v = fmaxf(v, turned(v, std::integral_constant<int, 0x124>{}));
+  v = fmaxf(v, turned(v, std::integral_constant<int, 0x122>{}));
+  v = fmaxf(v, turned(v, std::integral_constant<int, 0x121>{}));
+  return xor32_max(xor16_max(v));
 }
 
 // Sum over the lanes up to and including this one, by shifts within the rows of 16 lanes and then by

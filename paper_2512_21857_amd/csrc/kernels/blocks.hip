@@ -60,43 +60,25 @@ __global__ __launch_bounds__(BK_WAVES * WAVE) void block_keys_kernel(const T* __
   }
 }
 
-// Scores of 16 blocks for 16 query rows per wave on the fp64 MFMA: A = mean keys (lane (l, g): block
-// l, dims 16 j + 4 g + e), B = the rows' queries summed over the heads that share the keys, so
-// lane (l, g) gets blocks 4 r + g of row l.  In double, where the sum of 128 products is off by
-// 2^-50 or so of its terms: a choice between two blocks then depends on the inputs alone, not on
-// the order of a sum (in float, one choice in some ten thousand would).  Also clears the blocks'
-// row marks and the pair's count of arrivals for the selection that follows.
+// Scores are products of the rows' queries, summed over the heads that share the keys, with the mean
+// keys.  In double, where the sum of 128 products is off by 2^-50 or so of its terms: a choice between
+// two blocks then depends on the inputs alone, not on the order of a sum (in float, one choice in
+// some ten thousand would).
+//
+// On the fp64 MFMA, 16 blocks and 16 query rows per wave: A = mean keys (lane (l, g): block l, dims
+// 16 d + 4 g + e), B = the rows' sums, so lane (l, g) gets blocks 4 r + g of row l.
 typedef double f64x4 __attribute__((ext_vector_type(4)));
-constexpr int SC_WAVES = 4, SC_TILES = 2;      // waves, and 16-block tiles per wave
-template <typename T, int DH>
-__global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* __restrict__ q,
-                                                                      const float* __restrict__ means, int64_t mb,
-                                                                      int64_t mh, const int32_t* __restrict__ kv_len,
-                                                                      const int32_t* __restrict__ n_q, int Hkv, int G,
-                                                                      int nq_max, int kv_cap, int block, int n_blk,
-                                                                      double* __restrict__ score,
-                                                                      uint64_t* __restrict__ marks,
-                                                                      uint32_t* __restrict__ arrived) {
-  constexpr int QP = DH + 2;      // a row of query sums in LDS, padded: 16 rows at one dim on distinct banks
-  __shared__ __attribute__((aligned(16))) double qs[16 * QP];
-  const int h = blockIdx.z % Hkv, b = blockIdx.z / Hkv;
-  const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block;
-  const int first = blockIdx.x * SC_WAVES * SC_TILES * 16, i0 = blockIdx.y * 16;
-  if (first == 0 && i0 == 0 && threadIdx.x == 0) arrived[blockIdx.z] = 0;
-  if (first >= live) return;
-  if (i0 == 0 && (int)threadIdx.x < SC_WAVES * SC_TILES * 16 && first + (int)threadIdx.x < n_blk) {
-    uint64_t* mk = marks + ((int64_t)blockIdx.z * n_blk + first + threadIdx.x) * ADT_MASK_WORDS;
-    mk[0] = 0;
-    mk[1] = 0;
-  }
-  const int nq = min(n_q[b], nq_max);
-  if (i0 >= nq) return;
-  // the rows' sums over the heads, once for the workgroup: four dims per thread and turn
-  for (int x = threadIdx.x; x < 16 * (DH / 4); x += SC_WAVES * WAVE) {
+template <int DH>
+constexpr int SUM_PITCH = DH + 2;           // a row of sums in LDS, padded: 16 rows at one dim on distinct banks
+// rows i0 .. i0 + rows - 1 (zero from nq on), four dims per thread and turn; no barrier
+template <typename T, int DH, int THREADS>
+__device__ __forceinline__ void sum_queries(double* sums, const T* q, int i0, int rows, int nq, int h, int64_t row0,
+                                            int Hkv, int G) {
+  for (int x = threadIdx.x; x < rows * (DH / 4); x += THREADS) {
     const int i = x / (DH / 4), d = x % (DH / 4) * 4;
     double s[4] = {0.0, 0.0, 0.0, 0.0};
     if (i0 + i < nq) {
-      const T* qp = q + (((int64_t)b * nq_max + i0 + i) * Hkv + h) * G * DH + d;
+      const T* qp = q + ((row0 + i0 + i) * Hkv + h) * G * DH + d;
       for (int u0 = 0; u0 < G; u0 += 4) {       // four heads requested at a time
         T t[4][4];
 #pragma unroll
@@ -111,25 +93,58 @@ __global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* _
       }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) qs[i * QP + d + e] = s[e];
+    for (int e = 0; e < 4; ++e) sums[i * SUM_PITCH<DH> + d + e] = s[e];
   }
+}
+// sums: of 16 rows; mean: lane (l, g)'s block's mean key + 4 g
+template <int DH>
+__device__ __forceinline__ f64x4 tile_scores(const double* sums, const float* mean, int l, int g) {
+  f32x4 m[DH / 16];
+#pragma unroll
+  for (int d = 0; d < DH / 16; ++d) m[d] = *reinterpret_cast<const f32x4*>(mean + 16 * d);
+  f64x4 acc{0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+  for (int e = 0; e < DH / 4; ++e)
+    acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)m[e / 4][e % 4],
+                                               sums[l * SUM_PITCH<DH> + e / 4 * 16 + 4 * g + e % 4], acc, 0, 0, 0);
+  return acc;
+}
+
+// Scores to memory, for more blocks than one workgroup's LDS holds the keys of; also clears the blocks'
+// row marks and the pair's count of arrivals for the selection that follows.
+constexpr int SC_WAVES = 4, SC_TILES = 2;      // waves, and 16-block tiles per wave
+template <typename T, int DH>
+__global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* __restrict__ q,
+                                                                      const float* __restrict__ means, int64_t mb,
+                                                                      int64_t mh, const int32_t* __restrict__ kv_len,
+                                                                      const int32_t* __restrict__ n_q, int Hkv, int G,
+                                                                      int nq_max, int kv_cap, int block, int n_blk,
+                                                                      double* __restrict__ score,
+                                                                      uint64_t* __restrict__ marks,
+                                                                      uint32_t* __restrict__ arrived) {
+  __shared__ __attribute__((aligned(16))) double sums[16 * SUM_PITCH<DH>];
+  const int h = blockIdx.z % Hkv, b = blockIdx.z / Hkv;
+  const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block;
+  const int first = blockIdx.x * SC_WAVES * SC_TILES * 16, i0 = blockIdx.y * 16;
+  if (first == 0 && i0 == 0 && threadIdx.x == 0) arrived[blockIdx.z] = 0;
+  if (first >= live) return;
+  if (i0 == 0 && (int)threadIdx.x < SC_WAVES * SC_TILES * 16 && first + (int)threadIdx.x < n_blk) {
+    uint64_t* mk = marks + ((int64_t)blockIdx.z * n_blk + first + threadIdx.x) * ADT_MASK_WORDS;
+    mk[0] = 0;
+    mk[1] = 0;
+  }
+  const int nq = min(n_q[b], nq_max);
+  if (i0 >= nq) return;
+  sum_queries<T, DH, SC_WAVES * WAVE>(sums, q, i0, 16, nq, h, (int64_t)b * nq_max, Hkv, G);
   __syncthreads();
-  const int lane = threadIdx.x % WAVE, lq = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x % WAVE, l = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int t = 0; t < SC_TILES; ++t) {
     const int j0 = first + (threadIdx.x / WAVE * SC_TILES + t) * 16;
     if (j0 >= live) break;
-    const float* mp = means + b * mb + h * mh + (int64_t)min(j0 + lq, live - 1) * DH + 4 * g;
-    f32x4 m[DH / 16];
-#pragma unroll
-    for (int d = 0; d < DH / 16; ++d) m[d] = *reinterpret_cast<const f32x4*>(mp + 16 * d);
-    f64x4 acc{0.0, 0.0, 0.0, 0.0};
-#pragma unroll
-    for (int e = 0; e < DH / 4; ++e)
-      acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)m[e / 4][e % 4], qs[lq * QP + e / 4 * 16 + 4 * g + e % 4], acc, 0,
-                                                 0, 0);
-    if (i0 + lq >= nq) continue;
-    double* out = score + ((int64_t)blockIdx.z * nq_max + i0 + lq) * n_blk + j0;
+    const f64x4 acc = tile_scores<DH>(sums, means + b * mb + h * mh + (int64_t)min(j0 + l, live - 1) * DH + 4 * g, l, g);
+    if (i0 + l >= nq) continue;
+    double* out = score + ((int64_t)blockIdx.z * nq_max + i0 + l) * n_blk + j0;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (j0 + 4 * r + g < live) out[4 * r + g] = acc[r];
@@ -173,11 +188,15 @@ __device__ __forceinline__ void list_marked(const BlockLists& lists, int64_t pai
   }
 }
 
-// Scores in an unsigned order: larger score, larger key; -0 equals +0; NaN below all.
+// Scores in an unsigned order: larger score, larger key; -0 equals +0; NaN below all.  key_score: back again.
 __device__ __forceinline__ uint64_t score_key(double s) {
   if (s != s) return 0;
   const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
   return u >> 63 ? ~u : u | 1ull << 63;
+}
+
+__device__ __forceinline__ float key_score(uint64_t k) {
+  return (float)__builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k);
 }
 
 // The n_sel blocks of one query row and key-value head: the first and last, and the best of those
@@ -242,30 +261,8 @@ struct BlockRows {
   }
 };
 
-// A wave per row, keys in LDS (n_blk a wave).
-constexpr int BS_THREADS = 256, BS_WAVES = BS_THREADS / WAVE;
-constexpr int BS_WAVE_KEYS = 1024;
-__global__ __launch_bounds__(BS_THREADS) void block_select_wave_kernel(BlockRows a) {
-  extern __shared__ uint64_t keys[];
-  __shared__ __attribute__((aligned(16))) uint32_t hist[BS_WAVES][256];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
-  const int i = blockIdx.x * BS_WAVES + wave, h = blockIdx.y, b = blockIdx.z;
-  if (i < min(a.n_q[b], a.nq_max)) {
-    const BlockPick p = a.pick(i, h, b);
-    if (p.ends(lane, WAVE)) {
-      const double* row = a.row(i, h, b) + p.n_first;
-      uint64_t* k = keys + wave * a.n_blk;
-      const int n = p.live - p.n_first - p.n_last;
-      for (int j = lane; j < n; j += WAVE) k[j] = score_key(row[j]);
-      wave_lds_fence();
-      wave_select(k, n, p.n_sel - p.n_first - p.n_last, hist[wave],
-                  [&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
-    }
-  }
-  a.finish<BS_THREADS>(h, b, (int*)hist);
-}
-
-// A workgroup per row, for rows of more blocks; the keys are read anew in every pass.
+constexpr int BS_THREADS = 256;
+// A workgroup per row, on the scores in memory; the keys are read anew in every pass.
 __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(BlockRows a) {
   typedef RankShape<BS_THREADS, 8, 8, 1, false> Rank;
   __shared__ typename Rank::Scratch sh;
@@ -283,20 +280,32 @@ __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(BlockRows a) {
   a.finish<BS_THREADS>(h, b, (int*)&sh);
 }
 
-// Score and selection in one launch for up to BC_ROWS query rows: a workgroup per key-value head,
-// whose 16-lane groups take a block each (a lane DH / 16 dims, the row's sum over the lanes by
-// rotations within the group), leave the keys in LDS, and whose first waves then select for one row
-// each, eight bits a pass.  For more rows the scores want every CU: their matrix products keep a CU
-// busy for 7 us at 512 blocks and 16 rows, whatever the number of rows below that, where these
-// products take their number's share.
+// Score and selection in one launch, a workgroup of 16 waves per key-value head, for as many blocks as
+// its LDS holds the keys of.  The waves find the scores together, leave their keys in LDS and then
+// select for a row each; the rows' marks meet in LDS, so the pair's list is written without another
+// workgroup's.  For up to BC_ROWS query rows by products of their own: 16-lane groups take a block each
+// (a lane DH / 16 dims, the row's sum over the lanes by rotations within the group), where the matrix
+// product would cost the same as for 16 rows.  For more rows by the matrix product, 16, 32 or 64 rows at
+// a time, as the LDS allows.
 constexpr int BC_THREADS = 1024;
 constexpr int BC_ROWS = 4;
 constexpr int BC_LDS_BYTES = 144 * 1024;
+// rows taken at a time by the matrix product (0: not even 16); their keys, sums and the blocks' marks
+// (the histograms, 16 KB, lie beside them)
+static size_t choose_tiles_lds(int batch, int Dh, int n_blk) {
+  return (size_t)batch * ((size_t)n_blk * sizeof(uint64_t) + (Dh + 2) * sizeof(double)) +
+         (size_t)n_blk * ADT_MASK_WORDS * sizeof(uint64_t);
+}
+static int choose_batch(int nq_max, int Dh, int n_blk) {
+  for (int batch = 64; batch >= 16; batch /= 2)
+    if ((batch == 16 || nq_max > batch / 2) && choose_tiles_lds(batch, Dh, n_blk) <= BC_LDS_BYTES - 16 * 1024) return batch;
+  return 0;
+}
 static size_t choose_lds_bytes(int nq_max, int n_blk) {
   return (size_t)n_blk * (nq_max * sizeof(uint64_t) + sizeof(uint32_t));
 }
-static bool choose_at_once(int nq_max, int n_blk) {
-  return nq_max <= BC_ROWS && choose_lds_bytes(nq_max, n_blk) <= BC_LDS_BYTES;
+static bool choose_at_once(int nq_max, int Dh, int n_blk) {
+  return nq_max <= BC_ROWS ? choose_lds_bytes(nq_max, n_blk) <= BC_LDS_BYTES : choose_batch(nq_max, Dh, n_blk) > 0;
 }
 
 // x + x of the lane C places on, round the 16 lanes of a row
@@ -388,16 +397,74 @@ __global__ __launch_bounds__(BC_THREADS) void block_choose_kernel(
       for (int m = lane; m < lo; m += WAVE) take(m, m);
       for (int m = lane; m < n_last; m += WAVE) take(n_sel - n_last + m, hi + m);
       if (need > 0)
-        wave_select(keys + (size_t)i * n_blk + lo, hi - lo, need, hist[i], [&](int at, int j) { take(lo + at, lo + j); });
+        wave_select(keys + (size_t)i * n_blk + lo, hi - lo, need, hist[i], key_score,
+                    [&](int at, int j) { take(lo + at, lo + j); });
     }
   }
   __syncthreads();
   list_marked<BC_THREADS>(lists, (int64_t)b * Hkv + h, n_blk, live, (int*)hist, [&](int j, uint64_t& w0, uint64_t&) { w0 = bits[j]; });
 }
 
+template <typename T, int DH>
+__global__ __launch_bounds__(BC_THREADS) void block_choose_tiles_kernel(
+    const T* __restrict__ q, const float* __restrict__ means, int64_t mb, int64_t mh, const int32_t* __restrict__ kv_len,
+    const int32_t* __restrict__ n_q, int Hkv, int G, int nq_max, int kv_cap, int block, int n_blk, int n_sel, int n_first,
+    int n_last, int batch, BlockLists lists, int32_t* __restrict__ sel) {
+  constexpr int WAVES = BC_THREADS / WAVE;
+  extern __shared__ uint64_t keys[];                      // [batch][n_blk]; the sums; the rows that marked each block
+  __shared__ __attribute__((aligned(16))) uint32_t hist[WAVES][256];
+  double* sums = reinterpret_cast<double*>(keys + (size_t)batch * n_blk);
+  uint32_t* bits = reinterpret_cast<uint32_t*>(sums + batch * SUM_PITCH<DH>);      // [n_blk][4]
+  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE, l = lane & 15, g = lane >> 4;
+  const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block, nq = min(n_q[b], nq_max);
+  const int tiles = (live + 15) / 16;
+  for (int j = tid; j < 4 * live; j += BC_THREADS) bits[j] = 0;
+  for (int i0 = 0; i0 < nq; i0 += batch) {
+    const int rows = min(batch, (nq - i0 + 15) / 16 * 16);
+    if (live > n_sel) {
+      sum_queries<T, DH, BC_THREADS>(sums, q, i0, rows, nq, h, (int64_t)b * nq_max, Hkv, G);
+      __syncthreads();
+      for (int t = wave; t < tiles * (rows / 16); t += WAVES) {
+        const int j0 = t % tiles * 16, r0 = t / tiles * 16;
+        const f64x4 acc = tile_scores<DH>(sums + r0 * SUM_PITCH<DH>,
+                                          means + b * mb + h * mh + (int64_t)min(j0 + l, live - 1) * DH + 4 * g, l, g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (j0 + 4 * r + g < live) keys[(size_t)(r0 + l) * n_blk + j0 + 4 * r + g] = score_key(acc[r]);
+      }
+    }
+    __syncthreads();
+    for (int r = wave; r < rows && i0 + r < nq; r += WAVES) {
+      const int i = i0 + r;
+      int32_t* out = sel ? sel + (((int64_t)b * nq_max + i) * Hkv + h) * n_sel : nullptr;
+      auto take = [&](int at, int j) {
+        atomicOr(&bits[4 * j + (i >> 5)], 1u << (i & 31));
+        if (out) out[at] = j;
+      };
+      if (live <= n_sel) {
+        for (int j = lane; j < live; j += WAVE) take(j, j);
+        for (int j = live + lane; out && j < n_sel; j += WAVE) out[j] = -1;
+      } else {
+        const int lo = n_first, hi = live - n_last, need = n_sel - n_first - n_last;
+        for (int m = lane; m < lo; m += WAVE) take(m, m);
+        for (int m = lane; m < n_last; m += WAVE) take(n_sel - n_last + m, hi + m);
+        if (need > 0)
+          wave_select(keys + (size_t)r * n_blk + lo, hi - lo, need, hist[wave], key_score,
+                      [&](int at, int j) { take(lo + at, lo + j); });
+      }
+    }
+    __syncthreads();
+  }
+  list_marked<BC_THREADS>(lists, (int64_t)b * Hkv + h, n_blk, live, (int*)hist, [&](int j, uint64_t& w0, uint64_t& w1) {
+    w0 = (uint64_t)bits[4 * j + 1] << 32 | bits[4 * j];
+    w1 = (uint64_t)bits[4 * j + 3] << 32 | bits[4 * j + 2];
+  });
+}
+
 // Scratch: scores, marks, arrivals.
-size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk) {
-  if (choose_at_once(nq_max, n_blk)) return 0;
+size_t block_select_ws_bytes(int B, int Hkv, int Dh, int nq_max, int n_blk) {
+  if (choose_at_once(nq_max, Dh, n_blk)) return 0;
   const size_t pairs = (size_t)B * Hkv;
   return pairs * n_blk * ((size_t)nq_max * sizeof(double) + ADT_MASK_WORDS * sizeof(uint64_t)) + pairs * sizeof(uint32_t);
 }
@@ -407,13 +474,19 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
                                int n_sel, int n_first, int n_last, int dtype, void* ws, const BlockLists& lists,
                                int32_t* sel, hipStream_t st) {
   const int n_blk = (kv_cap + block - 1) / block;
-  if (choose_at_once(nq_max, n_blk)) {
+  if (choose_at_once(nq_max, Dh, n_blk)) {
+    const int batch = choose_batch(nq_max, Dh, n_blk);
 #define ADT_BC(TV, DHV, RV)                                                                                             \
   block_choose_kernel<TV, DHV, RV><<<dim3(Hkv, B), BC_THREADS, choose_lds_bytes(nq_max, n_blk), st>>>(                  \
       (const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last, lists, sel)
-#define ADT_BCR(TV, DHV)                       \
-  if (nq_max == 1) ADT_BC(TV, DHV, 1);         \
-  else ADT_BC(TV, DHV, BC_ROWS)
+#define ADT_BT(TV, DHV)                                                                                                 \
+  block_choose_tiles_kernel<TV, DHV><<<dim3(Hkv, B), BC_THREADS, choose_tiles_lds(batch, DHV, n_blk), st>>>(            \
+      (const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last, batch,    \
+      lists, sel)
+#define ADT_BCR(TV, DHV)                                \
+  if (nq_max == 1) ADT_BC(TV, DHV, 1);                  \
+  else if (nq_max <= BC_ROWS) ADT_BC(TV, DHV, BC_ROWS); \
+  else ADT_BT(TV, DHV)
     if (dtype == ADT_BF16) {
       if (Dh == 128) { ADT_BCR(uint16_t, 128); }
       else { ADT_BCR(uint16_t, 64); }
@@ -422,6 +495,7 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
       else { ADT_BCR(float, 64); }
     }
 #undef ADT_BCR
+#undef ADT_BT
 #undef ADT_BC
     ADT_LAUNCH_CHECK();
     return ADT_OK;
@@ -447,11 +521,7 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
   ADT_LAUNCH_CHECK();
   const BlockRows rows{score, kv_len, n_q, Hkv, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last,
                        (unsigned long long*)marks, arrived, lists, sel};
-  if (n_blk <= BS_WAVE_KEYS)
-    block_select_wave_kernel<<<dim3((nq_max + BS_WAVES - 1) / BS_WAVES, Hkv, B), BS_THREADS,
-                               BS_WAVES * n_blk * sizeof(uint64_t), st>>>(rows);
-  else
-    block_select_kernel<<<dim3(nq_max, Hkv, B), BS_THREADS, 0, st>>>(rows);
+  block_select_kernel<<<dim3(nq_max, Hkv, B), BS_THREADS, 0, st>>>(rows);
   ADT_LAUNCH_CHECK();
   return ADT_OK;
 }

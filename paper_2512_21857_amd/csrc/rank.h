@@ -179,13 +179,31 @@ __device__ __forceinline__ RankRow<K, S, VF, KF> rank_row(VF value, KF key, int 
   return RankRow<K, S, VF, KF>(value, key, n, sh);
 }
 
-// The same for one wave and keys in LDS: calls out(rank, i), in order, for the `need` (0 < need <= n)
-// largest of key[0] .. key[n - 1].  hist: 256 counters of LDS of the wave's own.
+// Which of 256 counters in LDS (a wave's own), counted from the top, the `need`-th key falls in; need
+// becomes its rank there, count the counter's value.
+__device__ __forceinline__ uint32_t digit_of_rank(const uint32_t* hist, uint32_t& need, uint32_t& count) {
+  // lane l holds the digits 255 - 4 l down to 252 - 4 l
+  const uint4 c = reinterpret_cast<const uint4*>(hist)[WAVE - 1 - threadIdx.x % WAVE];
+  const uint32_t sum = c.x + c.y + c.z + c.w, incl = wave_prefix_sum(sum), above = incl - sum;
+  const int at = __ffsll((unsigned long long)__ballot(above < need && incl >= need)) - 1;
+  // within that lane's four digits, from the top
+  auto of_lane = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, at); };
+  const uint32_t rest = need - of_lane(above), w = of_lane(c.w), z = of_lane(c.z), y = of_lane(c.y), x = of_lane(c.x);
+  uint32_t digit = 255 - 4 * at, over = 0;
+  count = w;
+  if (rest > w) { digit -= 1; over = w; count = z; }
+  if (rest > w + z) { digit -= 1; over = w + z; count = y; }
+  if (rest > w + z + y) { digit -= 1; over = w + z + y; count = x; }
+  need = rest - over;
+  return digit;
+}
+
+// The same for one wave and keys in LDS, by eight-bit digits: calls out(rank, i), in order, for the
+// `need` (0 < need <= n) largest of key[0] .. key[n - 1].  hist: 256 counters of LDS of the wave's own.
 template <class O>
-__device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need_, uint32_t* hist, O out) {
+__device__ __forceinline__ void wave_radix_select(const uint64_t* key, int n, uint32_t need, uint32_t* hist, O out) {
   const int lane = threadIdx.x % WAVE;
   uint64_t prefix = 0, mask = 0;
-  uint32_t need = need_;
   bool settled = false;
   for (int shift = 56; shift >= 0 && !settled; shift -= 8) {
     reinterpret_cast<uint4*>(hist)[lane] = make_uint4(0, 0, 0, 0);
@@ -195,20 +213,8 @@ __device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need
       if ((k & mask) == prefix) atomicAdd(&hist[(int)(k >> shift) & 255], 1u);
     }
     wave_lds_fence();
-    // lane l holds the digits 255 - 4 l down to 252 - 4 l
-    const uint4 c = reinterpret_cast<const uint4*>(hist)[WAVE - 1 - lane];
-    const uint32_t sum = c.x + c.y + c.z + c.w;
-    const uint32_t incl = wave_prefix_sum(sum);
-    const uint32_t above = incl - sum;
-    const int at = __ffsll((unsigned long long)__ballot(above < need && incl >= need)) - 1;
-    // within that lane's four digits, from the top
-    auto of_lane = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, at); };
-    const uint32_t rest = need - of_lane(above), w = of_lane(c.w), z = of_lane(c.z), y = of_lane(c.y), x = of_lane(c.x);
-    uint32_t digit = 255 - 4 * at, over = 0, count = w;
-    if (rest > w) { digit -= 1; over = w; count = z; }
-    if (rest > w + z) { digit -= 1; over = w + z; count = y; }
-    if (rest > w + z + y) { digit -= 1; over = w + z + y; count = x; }
-    need = rest - over;
+    uint32_t count;
+    const uint32_t digit = digit_of_rank(hist, need, count);
     settled = count == need;
     prefix |= (uint64_t)digit << shift;
     mask |= 255ull << shift;
@@ -223,6 +229,70 @@ __device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need
     const uint64_t eqs = __ballot(equal);
     const bool in = i < n && (m > prefix || (equal && eq + __popcll(eqs & below) < need));
     eq += __popcll(eqs);
+    const uint64_t ins = __ballot(in);
+    if (in) out((int)(done + __popcll(ins & below)), i);
+    done += __popcll(ins);
+  }
+}
+
+// The same for keys of doubles (value(key): the double as a float, rounded; the order of keys is the
+// doubles').  One pass counts the keys in 256 even steps between the least and the greatest value: a
+// monotone rule, whatever it rounds, so the keys of the steps above the `need`-th key's are selected,
+// those below are not, and of the few in its step each lane ranks one.  (Digits from the top would
+// first tell signs and exponents, which nearly all keys share.)  Where the values' range is none, or
+// the step holds more keys than the wave has lanes, by digits after all.
+template <class VF, class O>
+__device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need_, uint32_t* hist, VF value, O out) {
+  const int lane = threadIdx.x % WAVE;
+  uint32_t need = need_;
+  float lo = INFINITY, hi = -INFINITY;
+  for (int i = lane; i < n; i += WAVE) {
+    const float f = value(key[i]);
+    lo = fminf(lo, f);
+    hi = fmaxf(hi, f);
+  }
+  lo = -wave_max_dpp(-lo);
+  hi = wave_max_dpp(hi);
+  const float range = hi - lo, per = 256.f / range;
+  if (!(range > 0.f) || !(range < INFINITY)) return wave_radix_select(key, n, need, hist, out);
+  // (a value that is no number gives step 0; its key is below all others there too)
+  auto step_of = [&](uint64_t k) { return (int)fminf(fmaxf((value(k) - lo) * per, 0.f), 255.f); };
+  reinterpret_cast<uint4*>(hist)[lane] = make_uint4(0, 0, 0, 0);
+  wave_lds_fence();
+  for (int i = lane; i < n; i += WAVE) atomicAdd(&hist[step_of(key[i])], 1u);
+  wave_lds_fence();
+  uint32_t count;
+  const int step = digit_of_rank(hist, need, count);
+  if (count > WAVE && count != need) return wave_radix_select(key, n, need_, hist, out);
+  wave_lds_fence();
+  const uint64_t below = (1ull << lane) - 1;
+  uint64_t chosen = ~0ull;                         // of the step's keys, in order
+  if (count != need) {
+    uint64_t* mine = reinterpret_cast<uint64_t*>(hist);
+    uint32_t at = 0;
+    for (int base = 0; base < n; base += WAVE) {
+      const int i = base + lane;
+      const uint64_t k = key[min(i, n - 1)];
+      const bool in = i < n && step_of(k) == step;
+      const uint64_t ins = __ballot(in);
+      if (in) mine[at + __popcll(ins & below)] = k;
+      at += __popcll(ins);
+    }
+    wave_lds_fence();
+    const uint64_t k = mine[min(lane, (int)count - 1)];
+    uint32_t rank = 0;
+    for (int j = 0; j < (int)count; ++j) {
+      const uint64_t o = mine[j];
+      rank += (o > k) | ((o == k) & (j < lane));
+    }
+    chosen = __ballot(lane < (int)count && rank < need);
+  }
+  uint32_t done = 0, at = 0;
+  for (int base = 0; base < n; base += WAVE) {
+    const int i = base + lane, s = i < n ? step_of(key[i]) : -1;
+    const uint64_t eqs = __ballot(s == step);
+    const bool in = s > step || (s == step && (count == need || (chosen >> (at + __popcll(eqs & below)) & 1)));
+    at += __popcll(eqs);
     const uint64_t ins = __ballot(in);
     if (in) out((int)(done + __popcll(ins & below)), i);
     done += __popcll(ins);
