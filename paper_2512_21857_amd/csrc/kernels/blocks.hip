@@ -110,8 +110,8 @@ __device__ __forceinline__ f64x4 tile_scores(const double* sums, const float* me
   return acc;
 }
 
-// Scores to memory, for more blocks than one workgroup's LDS holds the keys of; also clears the blocks'
-// row marks and the pair's count of arrivals for the selection that follows.
+// Scores to memory; also clears the blocks' row marks and the pair's count of arrivals for the selection
+// that follows.
 constexpr int SC_WAVES = 4, SC_TILES = 2;      // waves, and 16-block tiles per wave
 template <typename T, int DH>
 __global__ __launch_bounds__(SC_WAVES * WAVE) void block_score_kernel(const T* __restrict__ q,
@@ -261,8 +261,30 @@ struct BlockRows {
   }
 };
 
-constexpr int BS_THREADS = 256;
-// A workgroup per row, on the scores in memory; the keys are read anew in every pass.
+// A wave per row, keys in LDS (n_blk a wave).
+constexpr int BS_THREADS = 256, BS_WAVES = BS_THREADS / WAVE;
+constexpr int BS_WAVE_KEYS = 1024;
+__global__ __launch_bounds__(BS_THREADS) void block_select_wave_kernel(BlockRows a) {
+  extern __shared__ uint64_t keys[];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[BS_WAVES][256];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE;
+  const int i = blockIdx.x * BS_WAVES + wave, h = blockIdx.y, b = blockIdx.z;
+  if (i < min(a.n_q[b], a.nq_max)) {
+    const BlockPick p = a.pick(i, h, b);
+    if (p.ends(lane, WAVE)) {
+      const double* row = a.row(i, h, b) + p.n_first;
+      uint64_t* k = keys + wave * a.n_blk;
+      const int n = p.live - p.n_first - p.n_last;
+      for (int j = lane; j < n; j += WAVE) k[j] = score_key(row[j]);
+      wave_lds_fence();
+      wave_select(k, n, p.n_sel - p.n_first - p.n_last, hist[wave], key_score,
+                  [&](int at, int j) { p.take(p.n_first + at, p.n_first + j); });
+    }
+  }
+  a.finish<BS_THREADS>(h, b, (int*)hist);
+}
+
+// A workgroup per row, for rows of more blocks; the keys are read anew in every pass.
 __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(BlockRows a) {
   typedef RankShape<BS_THREADS, 8, 8, 1, false> Rank;
   __shared__ typename Rank::Scratch sh;
@@ -280,32 +302,20 @@ __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(BlockRows a) {
   a.finish<BS_THREADS>(h, b, (int*)&sh);
 }
 
-// Score and selection in one launch, a workgroup of 16 waves per key-value head, for as many blocks as
-// its LDS holds the keys of.  The waves find the scores together, leave their keys in LDS and then
-// select for a row each; the rows' marks meet in LDS, so the pair's list is written without another
-// workgroup's.  For up to BC_ROWS query rows by products of their own: 16-lane groups take a block each
-// (a lane DH / 16 dims, the row's sum over the lanes by rotations within the group), where the matrix
-// product would cost the same as for 16 rows.  For more rows by the matrix product, 16, 32 or 64 rows at
-// a time, as the LDS allows.
+// Score and selection in one launch for up to BC_ROWS query rows: a workgroup of 16 waves per key-value
+// head, whose 16-lane groups take a block each (a lane DH / 16 dims, the row's sum over the lanes by
+// rotations within the group), leave the keys in LDS, and whose first waves then select for a row each;
+// the rows' marks meet in LDS, so the pair's list is written without another workgroup's.  More rows
+// want every CU: one workgroup a head, by matrix products, took 21.7 us for 16 rows of 128 heads over
+// 320 blocks and 20.4 for 61 rows of 32 heads over 73, against 23.2 and 16.5 in two launches.
 constexpr int BC_THREADS = 1024;
 constexpr int BC_ROWS = 4;
 constexpr int BC_LDS_BYTES = 144 * 1024;
-// rows taken at a time by the matrix product (0: not even 16); their keys, sums and the blocks' marks
-// (the histograms, 16 KB, lie beside them)
-static size_t choose_tiles_lds(int batch, int Dh, int n_blk) {
-  return (size_t)batch * ((size_t)n_blk * sizeof(uint64_t) + (Dh + 2) * sizeof(double)) +
-         (size_t)n_blk * ADT_MASK_WORDS * sizeof(uint64_t);
-}
-static int choose_batch(int nq_max, int Dh, int n_blk) {
-  for (int batch = 64; batch >= 16; batch /= 2)
-    if ((batch == 16 || nq_max > batch / 2) && choose_tiles_lds(batch, Dh, n_blk) <= BC_LDS_BYTES - 16 * 1024) return batch;
-  return 0;
-}
 static size_t choose_lds_bytes(int nq_max, int n_blk) {
   return (size_t)n_blk * (nq_max * sizeof(uint64_t) + sizeof(uint32_t));
 }
-static bool choose_at_once(int nq_max, int Dh, int n_blk) {
-  return nq_max <= BC_ROWS ? choose_lds_bytes(nq_max, n_blk) <= BC_LDS_BYTES : choose_batch(nq_max, Dh, n_blk) > 0;
+static bool choose_at_once(int nq_max, int n_blk) {
+  return nq_max <= BC_ROWS && choose_lds_bytes(nq_max, n_blk) <= BC_LDS_BYTES;
 }
 
 // x + x of the lane C places on, round the 16 lanes of a row
@@ -405,66 +415,9 @@ __global__ __launch_bounds__(BC_THREADS) void block_choose_kernel(
   list_marked<BC_THREADS>(lists, (int64_t)b * Hkv + h, n_blk, live, (int*)hist, [&](int j, uint64_t& w0, uint64_t&) { w0 = bits[j]; });
 }
 
-template <typename T, int DH>
-__global__ __launch_bounds__(BC_THREADS) void block_choose_tiles_kernel(
-    const T* __restrict__ q, const float* __restrict__ means, int64_t mb, int64_t mh, const int32_t* __restrict__ kv_len,
-    const int32_t* __restrict__ n_q, int Hkv, int G, int nq_max, int kv_cap, int block, int n_blk, int n_sel, int n_first,
-    int n_last, int batch, BlockLists lists, int32_t* __restrict__ sel) {
-  constexpr int WAVES = BC_THREADS / WAVE;
-  extern __shared__ uint64_t keys[];                      // [batch][n_blk]; the sums; the rows that marked each block
-  __shared__ __attribute__((aligned(16))) uint32_t hist[WAVES][256];
-  double* sums = reinterpret_cast<double*>(keys + (size_t)batch * n_blk);
-  uint32_t* bits = reinterpret_cast<uint32_t*>(sums + batch * SUM_PITCH<DH>);      // [n_blk][4]
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
-  const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE, l = lane & 15, g = lane >> 4;
-  const int L = max(0, min(kv_len[b], kv_cap)), live = (L + block - 1) / block, nq = min(n_q[b], nq_max);
-  const int tiles = (live + 15) / 16;
-  for (int j = tid; j < 4 * live; j += BC_THREADS) bits[j] = 0;
-  for (int i0 = 0; i0 < nq; i0 += batch) {
-    const int rows = min(batch, (nq - i0 + 15) / 16 * 16);
-    if (live > n_sel) {
-      sum_queries<T, DH, BC_THREADS>(sums, q, i0, rows, nq, h, (int64_t)b * nq_max, Hkv, G);
-      __syncthreads();
-      for (int t = wave; t < tiles * (rows / 16); t += WAVES) {
-        const int j0 = t % tiles * 16, r0 = t / tiles * 16;
-        const f64x4 acc = tile_scores<DH>(sums + r0 * SUM_PITCH<DH>,
-                                          means + b * mb + h * mh + (int64_t)min(j0 + l, live - 1) * DH + 4 * g, l, g);
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (j0 + 4 * r + g < live) keys[(size_t)(r0 + l) * n_blk + j0 + 4 * r + g] = score_key(acc[r]);
-      }
-    }
-    __syncthreads();
-    for (int r = wave; r < rows && i0 + r < nq; r += WAVES) {
-      const int i = i0 + r;
-      int32_t* out = sel ? sel + (((int64_t)b * nq_max + i) * Hkv + h) * n_sel : nullptr;
-      auto take = [&](int at, int j) {
-        atomicOr(&bits[4 * j + (i >> 5)], 1u << (i & 31));
-        if (out) out[at] = j;
-      };
-      if (live <= n_sel) {
-        for (int j = lane; j < live; j += WAVE) take(j, j);
-        for (int j = live + lane; out && j < n_sel; j += WAVE) out[j] = -1;
-      } else {
-        const int lo = n_first, hi = live - n_last, need = n_sel - n_first - n_last;
-        for (int m = lane; m < lo; m += WAVE) take(m, m);
-        for (int m = lane; m < n_last; m += WAVE) take(n_sel - n_last + m, hi + m);
-        if (need > 0)
-          wave_select(keys + (size_t)r * n_blk + lo, hi - lo, need, hist[wave], key_score,
-                      [&](int at, int j) { take(lo + at, lo + j); });
-      }
-    }
-    __syncthreads();
-  }
-  list_marked<BC_THREADS>(lists, (int64_t)b * Hkv + h, n_blk, live, (int*)hist, [&](int j, uint64_t& w0, uint64_t& w1) {
-    w0 = (uint64_t)bits[4 * j + 1] << 32 | bits[4 * j];
-    w1 = (uint64_t)bits[4 * j + 3] << 32 | bits[4 * j + 2];
-  });
-}
-
 // Scratch: scores, marks, arrivals.
-size_t block_select_ws_bytes(int B, int Hkv, int Dh, int nq_max, int n_blk) {
-  if (choose_at_once(nq_max, Dh, n_blk)) return 0;
+size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk) {
+  if (choose_at_once(nq_max, n_blk)) return 0;
   const size_t pairs = (size_t)B * Hkv;
   return pairs * n_blk * ((size_t)nq_max * sizeof(double) + ADT_MASK_WORDS * sizeof(uint64_t)) + pairs * sizeof(uint32_t);
 }
@@ -474,19 +427,13 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
                                int n_sel, int n_first, int n_last, int dtype, void* ws, const BlockLists& lists,
                                int32_t* sel, hipStream_t st) {
   const int n_blk = (kv_cap + block - 1) / block;
-  if (choose_at_once(nq_max, Dh, n_blk)) {
-    const int batch = choose_batch(nq_max, Dh, n_blk);
+  if (choose_at_once(nq_max, n_blk)) {
 #define ADT_BC(TV, DHV, RV)                                                                                             \
   block_choose_kernel<TV, DHV, RV><<<dim3(Hkv, B), BC_THREADS, choose_lds_bytes(nq_max, n_blk), st>>>(                  \
       (const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last, lists, sel)
-#define ADT_BT(TV, DHV)                                                                                                 \
-  block_choose_tiles_kernel<TV, DHV><<<dim3(Hkv, B), BC_THREADS, choose_tiles_lds(batch, DHV, n_blk), st>>>(            \
-      (const TV*)q, means, mb, mh, kv_len, n_q, Hkv, G, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last, batch,    \
-      lists, sel)
-#define ADT_BCR(TV, DHV)                                \
-  if (nq_max == 1) ADT_BC(TV, DHV, 1);                  \
-  else if (nq_max <= BC_ROWS) ADT_BC(TV, DHV, BC_ROWS); \
-  else ADT_BT(TV, DHV)
+#define ADT_BCR(TV, DHV)                       \
+  if (nq_max == 1) ADT_BC(TV, DHV, 1);         \
+  else ADT_BC(TV, DHV, BC_ROWS)
     if (dtype == ADT_BF16) {
       if (Dh == 128) { ADT_BCR(uint16_t, 128); }
       else { ADT_BCR(uint16_t, 64); }
@@ -495,7 +442,6 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
       else { ADT_BCR(float, 64); }
     }
 #undef ADT_BCR
-#undef ADT_BT
 #undef ADT_BC
     ADT_LAUNCH_CHECK();
     return ADT_OK;
@@ -521,7 +467,11 @@ adt_status launch_block_select(const void* q, const float* means, int64_t mb, in
   ADT_LAUNCH_CHECK();
   const BlockRows rows{score, kv_len, n_q, Hkv, nq_max, kv_cap, block, n_blk, n_sel, n_first, n_last,
                        (unsigned long long*)marks, arrived, lists, sel};
-  block_select_kernel<<<dim3(nq_max, Hkv, B), BS_THREADS, 0, st>>>(rows);
+  if (n_blk <= BS_WAVE_KEYS)
+    block_select_wave_kernel<<<dim3((nq_max + BS_WAVES - 1) / BS_WAVES, Hkv, B), BS_THREADS,
+                               BS_WAVES * n_blk * sizeof(uint64_t), st>>>(rows);
+  else
+    block_select_kernel<<<dim3(nq_max, Hkv, B), BS_THREADS, 0, st>>>(rows);
   ADT_LAUNCH_CHECK();
   return ADT_OK;
 }

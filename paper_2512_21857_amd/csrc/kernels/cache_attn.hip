@@ -1245,7 +1245,7 @@ struct SparseWs {
 static SparseWs sparse_ws(const CacheAttn& a, int B, const CachePlan& p) {
   const size_t pairs = (size_t)B * a.Hkv;
   SparseWs w;
-  w.marks = align_up16(block_select_ws_bytes(B, a.Hkv, a.Dh, a.nq_max, a.n_blk));
+  w.marks = align_up16(block_select_ws_bytes(B, a.Hkv, a.nq_max, a.n_blk));
   w.blocks = w.marks + pairs * a.n_blk * ADT_MASK_WORDS * sizeof(uint64_t);
   w.count = align_up16(w.blocks + pairs * a.n_blk * sizeof(uint16_t));
   w.arrived = w.count + pairs * sizeof(int32_t);

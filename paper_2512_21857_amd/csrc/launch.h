@@ -313,7 +313,7 @@ struct BlockLists {
   uint64_t* marks;       // [B][Hkv][n_blk][ADT_MASK_WORDS]
   uint32_t* arrived;     // [B][Hkv] zeroed along with the lists, for the splits that read them
 };
-size_t block_select_ws_bytes(int B, int Hkv, int Dh, int nq_max, int n_blk);   // scratch (16-byte aligned)
+size_t block_select_ws_bytes(int B, int Hkv, int nq_max, int n_blk);   // scratch (16-byte aligned)
 // Fills the lists (and sel, which may be null).
 adt_status launch_block_select(const void* q, const float* means, int64_t mb, int64_t mh, const int32_t* kv_len,
                                const int32_t* n_q, int B, int Hkv, int G, int Dh, int nq_max, int kv_cap, int block,

@@ -239,64 +239,79 @@ __device__ __forceinline__ void wave_radix_select(const uint64_t* key, int n, ui
 // doubles').  One pass counts the keys in 256 even steps between the least and the greatest value: a
 // monotone rule, whatever it rounds, so the keys of the steps above the `need`-th key's are selected,
 // those below are not, and of the few in its step each lane ranks one.  (Digits from the top would
-// first tell signs and exponents, which nearly all keys share.)  Where the values' range is none, or
-// the step holds more keys than the wave has lanes, by digits after all.
-template <class VF, class O>
-__device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need_, uint32_t* hist, VF value, O out) {
+// first tell signs and exponents, which nearly all keys share.)  The keys are read once, 64 V of them at
+// the most; where there are more, the values' range is none, or the step holds more keys than the wave
+// has lanes, it goes by digits after all.
+template <int V, class VF, class O>
+__device__ __forceinline__ void wave_select_in(const uint64_t* key, int n, uint32_t need_, uint32_t* hist, VF value, O out) {
   const int lane = threadIdx.x % WAVE;
+  const uint64_t below = (1ull << lane) - 1;
   uint32_t need = need_;
-  float lo = INFINITY, hi = -INFINITY;
-  for (int i = lane; i < n; i += WAVE) {
-    const float f = value(key[i]);
-    lo = fminf(lo, f);
-    hi = fmaxf(hi, f);
+  uint64_t k[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) k[j] = key[min(j * WAVE + lane, n - 1)];
+  float f[V], lo = INFINITY, hi = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    f[j] = value(k[j]);
+    lo = fminf(lo, f[j]);                        // (places past the end repeat the last key)
+    hi = fmaxf(hi, f[j]);
   }
   lo = -wave_max_dpp(-lo);
   hi = wave_max_dpp(hi);
   const float range = hi - lo, per = 256.f / range;
   if (!(range > 0.f) || !(range < INFINITY)) return wave_radix_select(key, n, need, hist, out);
-  // (a value that is no number gives step 0; its key is below all others there too)
-  auto step_of = [&](uint64_t k) { return (int)fminf(fmaxf((value(k) - lo) * per, 0.f), 255.f); };
   reinterpret_cast<uint4*>(hist)[lane] = make_uint4(0, 0, 0, 0);
   wave_lds_fence();
-  for (int i = lane; i < n; i += WAVE) atomicAdd(&hist[step_of(key[i])], 1u);
+  int step[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    // (a value that is no number gives step 0; its key is below all others there too)
+    const bool in = j * WAVE + lane < n;
+    step[j] = in ? (int)fminf(fmaxf((f[j] - lo) * per, 0.f), 255.f) : -1;
+    if (in) atomicAdd(&hist[step[j]], 1u);
+  }
   wave_lds_fence();
   uint32_t count;
-  const int step = digit_of_rank(hist, need, count);
+  const int last = digit_of_rank(hist, need, count);     // the step that decides
   if (count > WAVE && count != need) return wave_radix_select(key, n, need_, hist, out);
   wave_lds_fence();
-  const uint64_t below = (1ull << lane) - 1;
-  uint64_t chosen = ~0ull;                         // of the step's keys, in order
+  uint64_t chosen = ~0ull;                               // of that step's keys, in order
   if (count != need) {
     uint64_t* mine = reinterpret_cast<uint64_t*>(hist);
     uint32_t at = 0;
-    for (int base = 0; base < n; base += WAVE) {
-      const int i = base + lane;
-      const uint64_t k = key[min(i, n - 1)];
-      const bool in = i < n && step_of(k) == step;
-      const uint64_t ins = __ballot(in);
-      if (in) mine[at + __popcll(ins & below)] = k;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const uint64_t ins = __ballot(step[j] == last);
+      if (step[j] == last) mine[at + __popcll(ins & below)] = k[j];
       at += __popcll(ins);
     }
     wave_lds_fence();
-    const uint64_t k = mine[min(lane, (int)count - 1)];
+    const uint64_t own = mine[min(lane, (int)count - 1)];
     uint32_t rank = 0;
     for (int j = 0; j < (int)count; ++j) {
       const uint64_t o = mine[j];
-      rank += (o > k) | ((o == k) & (j < lane));
+      rank += (o > own) | ((o == own) & (j < lane));
     }
     chosen = __ballot(lane < (int)count && rank < need);
   }
   uint32_t done = 0, at = 0;
-  for (int base = 0; base < n; base += WAVE) {
-    const int i = base + lane, s = i < n ? step_of(key[i]) : -1;
-    const uint64_t eqs = __ballot(s == step);
-    const bool in = s > step || (s == step && (count == need || (chosen >> (at + __popcll(eqs & below)) & 1)));
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const uint64_t eqs = __ballot(step[j] == last);
+    const bool in = step[j] > last || (step[j] == last && (count == need || (chosen >> (at + __popcll(eqs & below)) & 1)));
     at += __popcll(eqs);
     const uint64_t ins = __ballot(in);
-    if (in) out((int)(done + __popcll(ins & below)), i);
+    if (in) out((int)(done + __popcll(ins & below)), j * WAVE + lane);
     done += __popcll(ins);
   }
+}
+template <class VF, class O>
+__device__ __forceinline__ void wave_select(const uint64_t* key, int n, int need, uint32_t* hist, VF value, O out) {
+  if (n <= 2 * WAVE) wave_select_in<2>(key, n, need, hist, value, out);
+  else if (n <= 8 * WAVE) wave_select_in<8>(key, n, need, hist, value, out);
+  else if (n <= 16 * WAVE) wave_select_in<16>(key, n, need, hist, value, out);
+  else wave_radix_select(key, n, need, hist, out);
 }
 
 }  // namespace adt
