@@ -208,6 +208,7 @@ struct Deal {
   int splits, per;          // of the launch; units per split
   int32_t* live;            // [B][Hkv][groups] n, or null (one split)
   __device__ __forceinline__ int splits_of(int units) const { return max(1, min(splits, (units + per - 1) / per)); }
+  __device__ __forceinline__ int live_splits(int64_t i) const { return max(0, min(live[i], splits)); }
 };
 
 // The chosen blocks of a pair into LDS; ends with a barrier.
@@ -378,11 +379,14 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
       for (int t = 0; t < RT; ++t) {
         if (SPARSE && !__any(sees[t])) continue;
         float mx = -INFINITY;
-        if (!tail && !SPARSE && k0 + KT - 1 <= k_last) {
+        if (!tail && k0 + KT - 1 <= k_last) {
 #pragma unroll
           for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[t][sub][r]);
+            for (int r = 0; r < 4; ++r) {
+              if (SPARSE) st[t][sub][r] = sees[t] ? st[t][sub][r] : -INFINITY;
+              mx = fmaxf(mx, st[t][sub][r]);
+            }
         } else {
 #pragma unroll
           for (int sub = 0; sub < SUBS; ++sub)
@@ -600,38 +604,45 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
   const bool tile_live = r0 + tile * 16 < live_rows;
   const float scale_log2 = a.scale * LOG2E;
 
-  // first key and last of step s (a step past the end has none: last < key0)
-  auto bounds = [&](int s, int& key0, int& last) {
-    if (s >= steps) {
-      key0 = 0;
-      last = -1;
-    } else if (s >= prefix_steps) {
-      key0 = L + (s - prefix_steps) * KT;
-      last = total - 1;
-    } else if (SPARSE) {
-      const int j = __builtin_amdgcn_readfirstlane((int)chosen[s / per_blk]);
-      key0 = j * a.block + s % per_blk * KT;
-      last = min(L, (j + 1) * a.block) - 1;
-    } else {
-      key0 = s * KT;
-      last = L - 1;
+  // Stage i's two steps: their blocks in the list (read a stage ahead of their use, as stages are
+  // fetched in order), first keys and last ones (a step past the end has none: last < key0).
+  int block_of[2] = {0, 0};
+  auto look_up = [&](int i) {
+    if (!SPARSE) return;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const int s = 2 * (sp + n_live * i) + w;
+      block_of[w] = s < prefix_steps ? (int)chosen[s / per_blk] : 0;
     }
+  };
+  struct Span {
+    int key0, last;
+  };
+  auto span = [&](int s, int j) {
+    if (s >= steps) return Span{0, -1};
+    if (s >= prefix_steps) return Span{L + (s - prefix_steps) * KT, total - 1};
+    if (SPARSE) {
+      const int blk = __builtin_amdgcn_readfirstlane(j);
+      return Span{blk * a.block + s % per_blk * KT, min(L, (blk + 1) * a.block) - 1};
+    }
+    return Span{s * KT, L - 1};
   };
   // Slot x (16 bytes) of a stage holds row x / CH, chunk (x % CH) ^ swizzle(row); thread t fills slots
   // r * NW * 64 + t.  Rows past a step's last key repeat it.  Requests are never skipped (a stage past
   // the range reads the head's first row), so the count of loads in flight is the same on every path.
   u16x8 kr[P][LOADS], vr[P][LOADS];
+  Span sp0[P], sp1[P];
   uint32_t mk[P][OWN] = {};       // of the blocks' marks, the word with this lane's row
   auto fetch = [&](int u, int i) {
     const int s0 = 2 * (sp + n_live * i);
-    int key0[2], last[2];
-    bounds(i < stages ? s0 : steps, key0[0], last[0]);
-    bounds(i < stages ? s0 + 1 : steps, key0[1], last[1]);
+    sp0[u] = span(i < stages ? s0 : steps, block_of[0]);
+    sp1[u] = span(i < stages ? s0 + 1 : steps, block_of[1]);
+    look_up(i + 1);
 #pragma unroll
     for (int r = 0; r < LOADS; ++r) {
       const int slot = r * NW * WAVE + tid, x = slot / CH, phys = slot % CH;
       const int half = x / KT;
-      const int key = max(0, min((half ? key0[1] : key0[0]) + x % KT, half ? last[1] : last[0]));
+      const int key = max(0, min((half ? sp1[u].key0 : sp0[u].key0) + x % KT, half ? sp1[u].last : sp0[u].last));
       kr[u][r] = load16<false>(      // (kept in the caches: the slots' weights take the keys once more)
           reinterpret_cast<const u16x8*>(kb + (int64_t)key * DH + (phys ^ swz_k<DH>(x)) * 8));
       vr[u][r] = __builtin_nontemporal_load(
@@ -659,7 +670,7 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
   f32x4 o[OT];
   float m_run, l_run;             // running maximum (log2 domain), this lane's share of the sum
   // this wave's steps of stage i, whose blocks the rows of `m` chose
-  auto compute = [&](auto safe_tag, int i, const uint32_t (&m)[OWN]) {
+  auto compute = [&](auto safe_tag, int i, const Span& span0, const Span& span1, const uint32_t (&m)[OWN]) {
     constexpr bool SAFE = decltype(safe_tag)::value;
     const unsigned char* ks = smem + (i & 1) * 2 * BYTES;
     const unsigned char* vs = ks + BYTES;
@@ -667,8 +678,7 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
     for (int w = 0; w < OWN; ++w) {
       const int half = KH == 2 ? kpart : w, s = 2 * (sp + n_live * i) + half;
       if (s >= steps) continue;
-      int k0, k_last;
-      bounds(s, k0, k_last);
+      const int k0 = half ? span1.key0 : span0.key0, k_last = half ? span1.last : span0.last;
       const bool tail = s >= prefix_steps;
       const bool sees = node >= 0 && (tail || !SPARSE || (m[w] >> (node & 31) & 1));
       if (SPARSE && !__any(sees)) continue;
@@ -688,9 +698,12 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
         return sees & (k0 + key <= k_last) & (!tail | (bool)((j < 64 ? aw0 : aw1) >> (j & 63) & 1));
       };
       float mx = -INFINITY;
-      if (!tail && !SPARSE && k0 + KT - 1 <= k_last) {
+      if (!tail && k0 + KT - 1 <= k_last) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, st[e / 4][e % 4]);
+        for (int e = 0; e < 8; ++e) {
+          if (SPARSE) st[e / 4][e % 4] = sees ? st[e / 4][e % 4] : -INFINITY;
+          mx = fmaxf(mx, st[e / 4][e % 4]);
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -746,6 +759,7 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
     l_run = 0.f;
 #pragma unroll
     for (int d = 0; d < OT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    look_up(0);
     // (the stages are requested in order: the scheduler may not interleave them, or the first one
     // stored could be the last to arrive)
 #pragma unroll
@@ -758,13 +772,14 @@ __global__ __launch_bounds__(NW * WAVE, P > 1 ? 2 : NW / 2) void cache_attn_shar
       for (int u = 0; u < P; ++u) {
         const int i = base + u;
         uint32_t m[OWN];
+        const Span span0 = sp0[u], span1 = sp1[u];
 #pragma unroll
         for (int w = 0; w < OWN; ++w) m[w] = mk[u][w];
         // the buffer written here was last read two stages ago, before the previous barrier
         store(u, i & 1);
         __syncthreads();
         fetch(u, i + P);
-        if (tile_live && i < stages) compute(safe_tag, i, m);
+        if (tile_live && i < stages) compute(safe_tag, i, span0, span1, m);
       }
     }
   };
@@ -842,7 +857,7 @@ __device__ __forceinline__ void merge_rows(const CacheAttn& a, const Deal& deal,
   const int rr = r0 + unit / count;
   const int rows = a.nq_max * a.G, groups = (rows + group_rows - 1) / group_rows;
   const int64_t pair = (int64_t)b * a.Hkv + h, base = pair * deal.splits * rows + rr;
-  const int splits = rr < live ? deal.live[((int64_t)b * groups + rr / group_rows) * a.Hkv + h] : 0;
+  const int splits = rr < live ? deal.live_splits(((int64_t)b * groups + rr / group_rows) * a.Hkv + h) : 0;
   // (one split has written the output; its maximum and sum are the only ones)
   if (splits == 1 && row_ml && grp == 0 && d == 0) {
     row_ml[(pair * rows + rr) * 2] = part_ml[base * 2];
@@ -1074,7 +1089,7 @@ __global__ __launch_bounds__(CA_THREADS) void slot_weights_kept_kernel(CacheAttn
     const int r = tid / 16;
     float m = -INFINITY, ls = 0.f;
     if (r < live_rows) {
-      const int splits = deal.live ? deal.live[(int64_t)b * a.Hkv + h] : 1;
+      const int splits = deal.live ? deal.live_splits((int64_t)b * a.Hkv + h) : 1;
       const float* ml = part_ml + (pair * deal.splits * rows + r) * 2;
       for (int s = tid % 16; s < splits; s += 16) m = fmaxf(m, ml[(int64_t)s * rows * 2]);
 #pragma unroll
