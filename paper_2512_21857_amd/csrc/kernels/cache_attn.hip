@@ -1145,7 +1145,9 @@ struct CachePlan {
   int deep;         // stages in flight
 };
 // Splits: as many as give the workgroups that the CUs hold at once (`slots`) equal shares of the keys
-// the launch expects, the slots of the cache or n_sel blocks; sequences that have more take more.  At
+// the launch expects: the slots of the cache, or n_sel blocks and for the rows of a tree, which share
+// most of their choice, half as many again (sixteen sequences of 16 rows taking 48 blocks each, 110 in
+// all: 13 stages a split 108 us, 18 98, 24 107).  Sequences that have more take more splits.  At
 // least three stages, or two steps for each wave, pay for a split's start and its partial results.  A
 // workgroup that shares its keys keeps one stage in flight where two of them fit a CU, and three where
 // there is so little work (under eight stages a CU) that one to a CU is all there is.
@@ -1159,7 +1161,7 @@ static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
   int64_t most = a.kv_cap, expect = most;      // keys
   if (a.block) {
     most = std::min<int64_t>(most, (int64_t)a.n_sel * a.nq_max * a.block + ADT_MAX_NODES);
-    expect = std::min<int64_t>(expect, (int64_t)a.n_sel * a.block + a.nq_max);
+    expect = std::min<int64_t>(expect, (int64_t)a.n_sel * a.block * (a.nq_max > 1 ? 3 : 2) / 2 + a.nq_max);
   }
   most = (most + unit - 1) / unit + 1;
   expect = (expect + unit - 1) / unit;
