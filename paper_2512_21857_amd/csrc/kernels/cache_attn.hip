@@ -8,13 +8,15 @@
 // A workgroup holds RT tiles (16 RT rows) in registers; its waves and the other workgroups of the
 // same rows (splits) deal the keys out in steps among themselves, each step read by one wave only,
 // so K and V come straight from memory into registers and every slot is read once per 16 RT rows.
-// What the waves of a workgroup found is merged in LDS, what the splits found by a launch of its own (few
-// rows over chosen blocks: by the last split), always in one order.  Steps never straddle the end of the prefix: the tree's own slots, which the
-// rows see through their ancestor masks, have steps of their own.
+// What the waves of a workgroup found is merged in LDS, what the splits found by a launch of its own
+// (few rows over chosen blocks: by the last split), always in one order.  Steps never straddle the end
+// of the prefix: the tree's own slots, which the rows see through their ancestor masks, have steps of
+// their own.
 //
-// (bf16 with more than 16 rows: cache_attn_shared_kernel.)  bf16 runs on the 16x16x32 MFMA, 32 keys a step, V transposed through LDS, probabilities rounded
-// to bf16 for the second product (2^-9 a term, below the rounding of the output itself); fp32 on
-// the 16x16x4 MFMA, 16 keys a step, without LDS.  Scores, softmax sums and outputs are fp32.
+// bf16 runs on the 16x16x32 MFMA, 32 keys a step, V transposed through LDS, probabilities rounded to
+// bf16 for the second product (2^-9 a term, below the rounding of the output itself); with more than
+// 16 rows in cache_attn_shared_kernel, whose waves share the keys.  fp32 runs on the 16x16x4 MFMA, 16
+// keys a step, without LDS.  Scores, softmax sums and outputs are fp32.
 //
 // A masked score is dropped by selection, so whatever a slot's key holds does not matter to rows
 // that do not see it.  Its value does meet their zero weight in the second product, and 0 * inf is
@@ -1142,6 +1144,7 @@ struct CachePlan {
   int tiles;        // row tiles per workgroup
   int groups;       // workgroups side by side for the rows of one key-value head
   int splits, per;  // most splits of the keys; steps (stages where shared) per split
+  int likely;       // splits of the keys that the launch expects
   int deep;         // stages in flight
 };
 // Splits: as many as give the workgroups that the CUs hold at once (`slots`) equal shares of the keys
@@ -1173,6 +1176,7 @@ static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
   int64_t splits = most <= p.per + p.per / 4 ? 1 : (most + p.per - 1) / p.per;
   splits = std::min<int64_t>(splits, std::max<int64_t>(1, (p.deep > 1 ? slots : 4 * slots) / pairs));
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, 64));
+  p.likely = (int)std::min<int64_t>(p.splits, (expect + p.per - 1) / p.per);
   return p;
 }
 
@@ -1246,9 +1250,10 @@ static adt_status attn_launches(const CacheAttn& a, int B, const CachePlan& p, c
 static adt_status merge_launch(const CacheAttn& a, int B, const CachePlan& p, const Partials& w, float* row_ml, int dtype,
                                hipStream_t st) {
   if (p.splits == 1) return ADT_OK;
-  // a thread for every four outputs, or for few outputs and many splits several
+  // a thread for every four outputs, or for few outputs and many splits several (61 rows of 8 heads in
+  // 14 splits, 64 at most: 8.8 us with eight threads, 4.4 with one)
   const int rows = a.nq_max * a.G, fit = CA_THREADS / (a.Dh / 4);
-  const int count = p.splits > 8 && (int64_t)B * a.Hkv * rows * (a.Dh / 4) < 65536 ? fit : 1;
+  const int count = p.likely > 16 && (int64_t)B * a.Hkv * rows * (a.Dh / 4) < 65536 ? fit : 1;
   cache_merge_kernel<<<dim3((rows * count + fit - 1) / fit, a.Hkv, B), CA_THREADS, 0, st>>>(
       a, w.deal, 16 * p.tiles, count, dtype == ADT_BF16, w.o, w.ml, row_ml);
   ADT_LAUNCH_CHECK();

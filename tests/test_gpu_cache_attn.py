@@ -370,3 +370,240 @@ def test_attention_over_more_than_two_billion_elements(rt):
     blk = torch.from_numpy(took).cuda().repeat_interleave(128, 1)[:, : c.L[0]]
     want, tol, _, _ = attend(c, 0, 8, torch.cat([blk, c.tail_see(0)], 1))
     close(out[0, :, 16:18], want, tol, "sparse")
+
+
+# ---------------------------------------------------------------------------- how the calls are made
+def _calls(rt, seed=21):
+    """A call of every operator on inputs of its own: (function that runs it, its outputs)."""
+    c = Case("bf16", 8, 4, 64, 9, [700, 333], seed=seed)
+    kv_len, n_q, n_tail, mask = c.dev()
+    g = gen(seed + 1)
+    kc, vc = normal(g, "bf16", 2, 4, 900, 64), normal(g, "bf16", 2, 4, 900, 64)
+    w = torch.rand(2, 4, c.cap, generator=g, device="cuda")
+    means = torch.zeros(2, 4, -(-c.cap // 32), 64, device="cuda")
+    freq, gain = rt.rope_freqs(64)
+    pos = torch.randint(0, 9999, (2, 9), generator=g, device="cuda", dtype=torch.int32)
+    kv, vv = normal(g, "bf16", 2, 9, 4, 64), normal(g, "bf16", 2, 9, 4, 64)
+    o = dict(rot=torch.zeros_like(c.q), rated=torch.zeros_like(c.q), sparse=torch.zeros_like(c.q), kc=kc, vc=vc, means=means,
+             sel=torch.zeros(2, 9, 4, 5, dtype=torch.int32, device="cuda"), w=torch.zeros_like(w),
+             ko=torch.zeros(2, 4, 300, 64, dtype=torch.bfloat16, device="cuda"),
+             vo=torch.zeros(2, 4, 300, 64, dtype=torch.bfloat16, device="cuda"), wo=torch.zeros(2, 4, 300, device="cuda"),
+             kept=torch.zeros(2, 4, 300, dtype=torch.int32, device="cuda"), n=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    ws_s = rt.sparse_tree_attn_workspace(2, 8, 4, 64, 9, c.cap, 32, 5)
+    ws_w = rt.tree_attn_weights_workspace(2, 8, 4, 64, 9, c.cap)
+
+    def run():
+        rt.rope_append(c.q, kv, vv, pos, kv_len, n_q, freq, kc, vc, gain=gain, out=o["rot"])
+        rt.block_keys(c.k, kv_len, 32, out=means)
+        rt.sparse_tree_attn(c.q, c.k, c.v, means, kv_len, n_q, n_tail, mask, c.cap, 32, 5, out=o["sparse"], sel=o["sel"],
+                            workspace=ws_s)
+        rt.tree_attn_weights(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, c.cap, weights=w, out=o["rated"], weights_out=o["w"],
+                             workspace=ws_w)
+        rt.kv_evict(c.k, c.v, w, kv_len, 300, 2, 20, k_out=o["ko"], v_out=o["vo"], weights_out=o["wo"], kept=o["kept"],
+                    new_len=o["n"])
+
+    return run, o, c
+
+
+def test_calls_are_captured_and_replayed(rt):
+    """A graph of all operators, replayed with other inputs and eager work between the replays, gives
+    what the eager calls give, bit for bit."""
+    run, o, c = _calls(rt)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for r in range(4):
+        c.q.copy_(normal(gen(100 + r), "bf16", *c.q.shape))
+        run()
+        torch.cuda.synchronize()
+        want = {k: v.clone() for k, v in o.items()}
+        for v in o.values():
+            v.zero_()
+        o["kc"].copy_(want["kc"])
+        o["vc"].copy_(want["vc"])
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in o.items():
+            assert torch.equal(v.nan_to_num(), want[k].nan_to_num()), (r, k)
+
+
+def test_calls_on_another_stream_and_side_by_side(rt):
+    """Two streams at work with workspaces of their own; the results are those of the default stream."""
+    runs = [_calls(rt, seed) for seed in (31, 32)]
+    wants = []
+    for run, o, _ in runs:
+        run()
+        torch.cuda.synchronize()
+        wants.append({k: v.clone() for k, v in o.items()})
+    streams = [torch.cuda.Stream() for _ in runs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        for (run, _, _), s in zip(runs, streams):
+            with torch.cuda.stream(s):
+                run()
+    torch.cuda.synchronize()
+    for (_, o, _), want in zip(runs, wants):
+        for k, v in o.items():
+            assert torch.equal(v.nan_to_num(), want[k].nan_to_num()), k
+
+
+def test_repeated_calls_give_the_same_bits(rt):
+    """No sum depends on the order in which workgroups arrive."""
+    for H, Hkv, n, L in ((32, 8, 1, [9000]), (16, 8, 16, [5000, 700]), (8, 8, 61, [2340])):
+        c = Case("bf16", H, Hkv, 128, n, L, seed=40 + n)
+        kv_len, n_q, n_tail, mask = c.dev()
+        means = rt.block_keys(c.k, kv_len, 64)
+        first = None
+        for _ in range(5):
+            out = rt.sparse_tree_attn(c.q, c.k, c.v, means, kv_len, n_q, n_tail, mask, c.cap, 64, 20, out=torch.zeros_like(c.q))
+            o2, w = rt.tree_attn_weights(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, c.cap, out=torch.zeros_like(c.q))
+            got = [bits(out), bits(o2), bits(w)]
+            first = first or got
+            assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+def test_dense_choice_equals_tree_attention(rt):
+    """With all blocks taken, and one query head per key-value head, both attentions compute what
+    tree_attn does: within the roundings of two bf16 results of the same sums."""
+    c = Case("bf16", 6, 6, 128, 33, [500, 129], seed=50)
+    c.k.nan_to_num_(0)
+    c.v.nan_to_num_(0)
+    kv_len, n_q, n_tail, mask = c.dev()
+    want = rt.tree_attn(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, c.cap, out=torch.zeros_like(c.q)).double()
+    means = rt.block_keys(c.k, kv_len, 64)
+    a = rt.sparse_tree_attn(c.q, c.k, c.v, means, kv_len, n_q, n_tail, mask, c.cap, 64, 100, out=torch.zeros_like(c.q))
+    b, _ = rt.tree_attn_weights(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, c.cap, out=torch.zeros_like(c.q))
+    # each is within (2^-8 (rounded probabilities) + 2^-10) max|v| + 2^-8 |out| of the exact value
+    vmax = c.v.abs().amax().item()
+    for got in (a, b):
+        assert torch.all((got.double() - want).abs() <= 2 * ((2.0 ** -8 + 2.0 ** -10) * vmax + 2.0 ** -8 * want.abs()))
+
+
+def test_refusals_of_the_wrappers(rt):
+    """Tensors of other types, shapes, layouts or devices are refused before anything runs."""
+    run, o, c = _calls(rt)
+    kv_len, n_q, n_tail, mask = c.dev()
+    means = rt.block_keys(c.k, kv_len, 32)
+    good = dict(q=c.q, k=c.k, v=c.v, means=means, kv_len=kv_len, n_q=n_q, n_tail=n_tail, mask=mask)
+
+    def sparse(**changed):
+        a = {**good, **changed}
+        return rt.sparse_tree_attn(*a.values(), c.cap, 32, 5)
+
+    sparse()
+    for bad in (dict(q=c.q.half()), dict(q=c.q.cpu()), dict(q=c.q.transpose(1, 2)), dict(k=c.k.float()), dict(v=c.v[..., ::2]),
+                dict(v=c.v[:, :, :-1]), dict(means=means[:, :, :-1]), dict(means=means.double()), dict(kv_len=kv_len.long()),
+                dict(kv_len=kv_len.cpu()), dict(n_q=n_q[:1]), dict(mask=mask[:, :-1]), dict(mask=mask.int())):
+        with pytest.raises(ValueError):
+            sparse(**bad)
+    with pytest.raises(ValueError):
+        rt.sparse_tree_attn(*good.values(), c.cap + 1, 32, 5)
+    with pytest.raises(ValueError):
+        rt.sparse_tree_attn(*good.values(), c.cap, 32, 5, sel=torch.zeros(2, 9, 4, 4, dtype=torch.int32, device="cuda"))
+    from paper_2512_21857_amd import abi
+    with pytest.raises(abi.AdtError):
+        rt.sparse_tree_attn(*good.values(), c.cap, 32, 5, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    w = torch.rand(2, 4, c.cap, device="cuda")
+    for bad in (dict(weights=w.double()), dict(weights=w[:, :, :-1]), dict(weights=w, weights_out=w[:, :, ::1].transpose(0, 1)),
+                dict(row_weight=torch.ones(2, 8, device="cuda")), dict(out=c.q[:, :5])):
+        with pytest.raises(ValueError):
+            rt.tree_attn_weights(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, c.cap, **bad)
+    for bad in (dict(k_out=c.k), dict(kept=torch.zeros(2, 4, 9, dtype=torch.int32, device="cuda")),
+                dict(k_out=o["ko"][:, :, :5], v_out=o["vo"][:, :, :5], weights_out=o["wo"])):
+        with pytest.raises(ValueError):
+            rt.kv_evict(c.k, c.v, w, kv_len, 300, **bad)
+
+
+# ---------------------------------------------------------------------------- together
+def test_bounded_cache_decoding(rt):
+    """Decoding over a bounded cache, operator by operator against 64 bits: in every cycle a tree's rows are
+    rotated at their own positions and appended, attend to all slots and rate them, attend to chosen
+    blocks, an accepted path is compacted, with its weights, and the cache is cut to its budget, so that
+    slots and positions part."""
+    from paper_2512_21857_amd import abi
+    B, H, Hkv, Dh, n, cap, budget, block = 2, 4, 2, 64, 7, 256, 96, 32
+    g, rng = gen(60), np.random.default_rng(60)
+    kc, vc = (torch.zeros(B, Hkv, cap, Dh, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    w = torch.zeros(B, Hkv, cap, device="cuda")
+    freq, gain = rt.rope_freqs(Dh, scaling="ramp", factor=4.0, orig_len=512)
+    kv_len, seen = i32([0, 0]), [0, 0]
+    c = Case.__new__(Case)
+    c.dtype, c.H, c.Hkv, c.Dh, c.n, c.B, c.cap, c.scale = "bf16", H, Hkv, Dh, n, B, cap, Dh ** -0.5
+    c.k, c.v = kc, vc
+    cut = 0
+    for cycle in range(40):
+        parent = np.full((B, n), -1, dtype=np.int32)
+        for b in range(B):
+            for i in range(1, n):
+                parent[b, i] = rng.integers(max(0, i - 3), i)
+        c.rows = [n, n - cycle % 3]
+        c.tails = c.rows
+        c.L = kv_len.tolist()
+        n_rows = i32(c.rows)
+        c.mask, depth = rt.tree_masks(torch.from_numpy(parent).cuda(), n_rows)
+        pos = i32(seen)[:, None] + depth
+        qkv = normal(g, "bf16", B, n, (H + 2 * Hkv) * Dh)
+        q, k, v = (t.unflatten(-1, (-1, Dh)) for t in qkv.split([H * Dh, Hkv * Dh, Hkv * Dh], -1))
+        c.q = rt.rope_append(q, k, v, pos, kv_len, n_rows, freq, kc, vc, gain=gain)
+        t = (pos.double()[..., None] * freq)[:, :, None]
+        half = Dh // 2
+        a, b2 = k.double()[..., :half], k.double()[..., half:]
+        rot = gain * torch.cat([a * t.cos() - b2 * t.sin(), a * t.sin() + b2 * t.cos()], -1)
+        for b in range(B):
+            got = kc[b, :, c.L[b]: c.L[b] + c.rows[b]].transpose(0, 1).double()
+            assert torch.all((got - rot[b, : c.rows[b]]).abs() <= 2.0 ** -8 * rot[b, : c.rows[b]].abs() + 1e-4)
+        w0 = w.clone()
+        out, _ = rt.tree_attn_weights(c.q, kc, vc, kv_len, n_rows, n_rows, c.mask, cap, weights=w, decay=0.9)
+        means = rt.block_keys(kc, kv_len, block)
+        near = rt.sparse_tree_attn(c.q, kc, vc, means, kv_len, n_rows, n_rows, c.mask, cap, block, 3)
+        for b in range(B):
+            m, L, G = c.rows[b], c.L[b], H // Hkv
+            see = torch.cat([torch.ones(m, L, dtype=torch.bool, device="cuda"), c.tail_see(b)], 1)
+            for h in range(Hkv):
+                want, tol, p, ptol = attend(c, b, h, see)
+                close(out[b, :m, h * G: (h + 1) * G], want, tol, f"cycle {cycle} rated")
+                add = p.sum((0, 1))
+                add[:L] += 0.9 * w0[b, h, :L].double()
+                close(w[b, h, : L + m], add, ptol.sum((0, 1)) + 2.0 ** -19 * (add + 1), f"cycle {cycle} weights")
+                if L:
+                    took = choose(c, b, h, means, block, 3, 1, 1)
+                    blk = torch.from_numpy(took).cuda().repeat_interleave(block, 1)[:, :L]
+                    want, tol, _, _ = attend(c, b, h, torch.cat([blk, c.tail_see(b)], 1))
+                    close(near[b, :m, h * G: (h + 1) * G], want, tol, f"cycle {cycle} sparse")
+        # the path to a random node is accepted
+        path, n_acc = np.zeros((B, n), dtype=np.int32), []
+        for b in range(B):
+            nodes, i = [], int(rng.integers(0, c.rows[b]))
+            while i > 0:
+                nodes.append(i)
+                i = parent[b, i]
+            path[b, 1: len(nodes) + 1] = nodes[::-1]
+            n_acc.append(len(nodes))
+        kb, wb = kc.clone(), w.clone()
+        rt.kv_compact(kc, vc, kv_len, torch.from_numpy(path).cuda(), i32(n_acc), n - 1)
+        rt.weights_compact(w, kv_len, torch.from_numpy(path).cuda(), i32(n_acc), n - 1)
+        for b in range(B):
+            src = [c.L[b] + path[b, m] for m in range(n_acc[b] + 1)]
+            assert torch.equal(bits(kc[b, :, c.L[b]: c.L[b] + n_acc[b] + 1]), bits(kb[b, :, src]))
+            assert torch.equal(w[b, :, c.L[b]: c.L[b] + n_acc[b] + 1], wb[b, :, src])
+            seen[b] += n_acc[b] + 1
+        kv_len = kv_len + 1 + i32(n_acc)
+        before, kb, wb = kv_len.tolist(), kc.clone(), w.clone()
+        kept, _ = rt.kv_evict(kc, vc, w, kv_len, budget, 4, 16, new_len=kv_len)
+        for b in range(B):
+            m = min(before[b], budget)
+            assert kv_len.tolist()[b] == m
+            cut += before[b] > budget
+            for h in range(Hkv):
+                keep = kept[b, h, :m].tolist()
+                assert keep == sorted(keep) and len(set(keep)) == m
+                if before[b] > budget:
+                    assert keep[:4] == [0, 1, 2, 3] and keep[-16:] == list(range(before[b] - 16, before[b]))
+                    lost = [s for s in range(before[b]) if s not in set(keep)]
+                    assert max(wb[b, h, lost].tolist()) <= min(wb[b, h, keep[4:-16]].tolist())
+                assert torch.equal(bits(kc[b, h, :m]), bits(kb[b, h, keep])) and torch.equal(w[b, h, :m], wb[b, h, keep])
+    assert cut > 10 and min(seen) > budget      # the walk reached what it is for
+    assert abi.lib().adt_device_check(None) == abi.OK
