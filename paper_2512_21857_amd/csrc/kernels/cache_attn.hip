@@ -943,7 +943,8 @@ __device__ __forceinline__ float2 row_factor(float m, float sum, float rating) {
 // p = 2^(s - m) / l, added over the rows.  A wave takes CHUNK keys at a time, keeps them in registers,
 // the next ones requested meanwhile, and goes through the query rows tile by tile (A = Q rows, B =
 // K^T: lane (l, g) gets rows 4 g + r of key l, so a column adds up within its lanes).  The queries of
-// up to QROWS rows lie in LDS; more are read from the L2 again for every chunk.
+// up to QROWS rows lie in LDS; more are read from the L2 again for every chunk.  Few keys under many
+// rows: the waves of a workgroup take the same 32 keys and deal the row tiles out.
 constexpr int SW_CHUNK = 32;        // keys per wave and turn
 template <typename T, int DH>
 struct SlotTile {
@@ -951,7 +952,9 @@ struct SlotTile {
   static constexpr int QROWS = 128 * 256 / (DH * (int)sizeof(T)) < 128 ? 64 : 128;
 };
 
-template <typename T, int DH, bool QLDS>
+enum class Rows { LDS, L2, DEALT };
+
+template <typename T, int DH, Rows HOW>
 __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weights_kernel(
     CacheAttn a, const float* __restrict__ row_ml, int turns, SlotWeights sw) {
   typedef Tile<T, DH> X;
@@ -960,7 +963,8 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const int L = max(0, min(a.kv_len[b], a.kv_cap));
   const int total = min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)a.kv_cap);
-  const int first = blockIdx.x * turns * CA_WAVES * SW_CHUNK;
+  constexpr bool QLDS = HOW == Rows::LDS, DEALT = HOW == Rows::DEALT;
+  const int first = blockIdx.x * (DEALT ? SW_CHUNK : turns * CA_WAVES * SW_CHUNK);
   if (first >= total) return;
   const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
   const int l = lane & 15, g = lane >> 4;
@@ -972,7 +976,7 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) X::template load_k<false>(step[u][i], kb, min(k0, total - 1) + i * X::KT, total - 1, l, g);
   };
-  request(0, first + wave * SW_CHUNK);
+  request(0, DEALT ? first : first + wave * SW_CHUNK);
   float2* factor = reinterpret_cast<float2*>(rows_lds);
   T* qs = reinterpret_cast<T*>(factor + tiles * 16);
   auto q_row = [&](int r) {
@@ -997,9 +1001,8 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
   const float scale_log2 = a.scale * LOG2E;
   // (a turn's earlier weights are requested before the next turn's keys: loads return in order, and
   // asked for last they would have every turn wait for the keys of the next)
-  auto turn = [&](int u, int key0, const float (&was)[SUBS]) {
+  auto sum = [&](float (&col)[SUBS], int u, int key0, int tile0, int tile_step) {
     const bool tail = key0 + SW_CHUNK > L;
-    float col[SUBS];
 #pragma unroll
     for (int s = 0; s < SUBS; ++s) col[s] = 0.f;
     // masked: some row of the tile is none, or some key is the tree's
@@ -1034,7 +1037,7 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
           }
         }
     };
-    for (int t = 0; t < tiles; ++t) {
+    for (int t = tile0; t < tiles; t += tile_step) {
       if (tail || t * 16 + 16 > live_rows) tile(std::true_type{}, t);
       else tile(std::false_type{}, t);
     }
@@ -1042,6 +1045,13 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
     for (int s = 0; s < SUBS; ++s) {
       col[s] = xor16_add(col[s]);
       col[s] = xor32_add(col[s]);
+    }
+  };
+  auto turn = [&](int u, int key0, const float (&was)[SUBS]) {
+    float col[SUBS];
+    sum(col, u, key0, 0, 1);
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s) {
       const int key = key0 + s * 16 + l;
       if (g == s && key < total) sw.store(b, h, key, L, was[s], col[s]);
     }
@@ -1050,17 +1060,33 @@ __global__ __launch_bounds__(CA_THREADS, sizeof(T) == 2 ? 4 : 2) void slot_weigh
 #pragma unroll
     for (int s = 0; s < SUBS; ++s) was[s] = sw.before(b, h, key0 + s * 16 + l, L);
   };
-  const int stride = CA_WAVES * SW_CHUNK;
-  int key0 = first + wave * SW_CHUNK;
-  for (int c = 0; c < turns && key0 < total; c += 2, key0 += 2 * stride) {
-    float was[SUBS];
-    earlier(was, key0);
-    if (c + 1 < turns) request(1, key0 + stride);
-    turn(0, key0, was);
-    if (c + 1 >= turns || key0 + stride >= total) break;
-    earlier(was, key0 + stride);
-    if (c + 2 < turns) request(0, key0 + 2 * stride);
-    turn(1, key0 + stride, was);
+  if constexpr (DEALT) {
+    __shared__ float part[CA_WAVES][SW_CHUNK];
+    float col[SUBS];
+    sum(col, 0, first, wave, CA_WAVES);
+#pragma unroll
+    for (int s = 0; s < SUBS; ++s)
+      if (g == s) part[wave][s * 16 + l] = col[s];
+    __syncthreads();
+    const int key = first + tid;
+    if (tid >= SW_CHUNK || key >= total) return;
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < CA_WAVES; ++w) all += part[w][tid];
+    sw.store(b, h, key, L, sw.before(b, h, key, L), all);
+  } else {
+    const int stride = CA_WAVES * SW_CHUNK;
+    int key0 = first + wave * SW_CHUNK;
+    for (int c = 0; c < turns && key0 < total; c += 2, key0 += 2 * stride) {
+      float was[SUBS];
+      earlier(was, key0);
+      if (c + 1 < turns) request(1, key0 + stride);
+      turn(0, key0, was);
+      if (c + 1 >= turns || key0 + stride >= total) break;
+      earlier(was, key0 + stride);
+      if (c + 2 < turns) request(0, key0 + 2 * stride);
+      turn(1, key0 + stride, was);
+    }
   }
 }
 
@@ -1338,16 +1364,19 @@ adt_status launch_weights_attn(const CacheAttn& a, int B, const float* w_in, flo
   }
   e = merge_launch(a, B, p, parts, row_ml, dtype, st);
   if (e) return e;
-  // turns: four where that leaves two workgroups a CU or more, fewer for fewer keys
+  // turns: four where that leaves two workgroups a CU or more, fewer for fewer keys; where there is not
+  // one a CU, the waves deal out the rows instead (488 rows of 4 heads over 700 slots 53 -> 17 us)
   const int64_t units = ((int64_t)a.kv_cap + CA_WAVES * SW_CHUNK - 1) / (CA_WAVES * SW_CHUNK);
-  const int turns = (int)std::max<int64_t>(1, std::min<int64_t>(4, units * B * a.Hkv / 512));
-  const dim3 grid((units + turns - 1) / turns, a.Hkv, B);
-  const int padded = (rows + 15) / 16 * 16;
+  const bool dealt = rows >= 16 * CA_WAVES && units * B * a.Hkv < 256;
+  const int turns = dealt ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(4, units * B * a.Hkv / 512));
+  const dim3 grid(dealt ? (a.kv_cap + SW_CHUNK - 1) / SW_CHUNK : (units + turns - 1) / turns, a.Hkv, B);
+  const size_t padded = (rows + 15) / 16 * 16, factors = padded * sizeof(float2);
 #define ADT_SW(TV, DHV)                                                                                                 \
-  if (rows <= SlotTile<TV, DHV>::QROWS)                                                                                 \
-    slot_weights_kernel<TV, DHV, true>                                                                                  \
-        <<<grid, CA_THREADS, padded * (sizeof(float2) + SlotTile<TV, DHV>::PITCH * sizeof(TV)), st>>>(a, row_ml, turns, sw);   \
-  else slot_weights_kernel<TV, DHV, false><<<grid, CA_THREADS, padded * sizeof(float2), st>>>(a, row_ml, turns, sw)
+  if (dealt) slot_weights_kernel<TV, DHV, Rows::DEALT><<<grid, CA_THREADS, factors, st>>>(a, row_ml, turns, sw);        \
+  else if (rows <= SlotTile<TV, DHV>::QROWS)                                                                            \
+    slot_weights_kernel<TV, DHV, Rows::LDS>                                                                             \
+        <<<grid, CA_THREADS, factors + padded * SlotTile<TV, DHV>::PITCH * sizeof(TV), st>>>(a, row_ml, turns, sw);     \
+  else slot_weights_kernel<TV, DHV, Rows::L2><<<grid, CA_THREADS, factors, st>>>(a, row_ml, turns, sw)
   if (dtype == ADT_BF16) {
     if (a.Dh == 128) { ADT_SW(uint16_t, 128); }
     else { ADT_SW(uint16_t, 64); }
