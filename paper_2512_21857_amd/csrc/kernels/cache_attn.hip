@@ -14,9 +14,9 @@
 // their own.
 //
 // bf16 runs on the 16x16x32 MFMA, 32 keys a step, V transposed through LDS, probabilities rounded to
-// bf16 for the second product (2^-9 a term, below the rounding of the output itself); with more than
-// 16 rows in cache_attn_shared_kernel, whose waves share the keys.  fp32 runs on the 16x16x4 MFMA, 16
-// keys a step, without LDS.  Scores, softmax sums and outputs are fp32.
+// bf16 for the second product (off by 2^-8 of a term at most, as the output by its own rounding);
+// with more than 16 rows in cache_attn_shared_kernel, whose waves share the keys.  fp32 runs on the
+// 16x16x4 MFMA, 16 keys a step, without LDS.  Scores, softmax sums and outputs are fp32.
 //
 // A masked score is dropped by selection, so whatever a slot's key holds does not matter to rows
 // that do not see it.  Its value does meet their zero weight in the second product, and 0 * inf is

@@ -372,6 +372,73 @@ def test_attention_over_more_than_two_billion_elements(rt):
     close(out[0, :, 16:18], want, tol, "sparse")
 
 
+# ---------------------------------------------------------------------------- much work at once
+BATCHED = [
+    # H, Hkv, Dh, n, L: 17..32, 33..64, 65..128 and more rows of a key-value head, for enough sequences to fill the CUs
+    (32, 32, 128, 20, [1500, 64, 1339]),
+    (32, 16, 64, 17, [3000, 100, 1500, 2049]),
+    (64, 16, 64, 20, [3000, 2500, 1]),
+    (64, 8, 64, 20, [3000, 2999, 0, 2048]),
+    (16, 4, 128, 33, [4500, 4000, 4200, 128, 4499, 4300]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv,Dh,n,L", BATCHED)
+def test_tree_attn_weights_batched(rt, dtype, H, Hkv, Dh, n, L):
+    print(f"rated {dtype} H={H}/{Hkv} Dh={Dh} n={n} L={L}", flush=True)
+    check_weights(rt, Case(dtype, H, Hkv, Dh, n, L, seed=70 + n), decay=0.5)
+
+
+@pytest.mark.parametrize("H,Hkv,Dh,n,L,block,n_sel", [
+    (32, 32, 128, 20, [2500, 1300, 700], 64, 16),
+    (32, 16, 64, 17, [4000, 100, 1500, 3900], 64, 30),
+    (64, 16, 64, 20, [4000, 3000, 900], 128, 20),
+    (64, 8, 64, 20, [5000, 4097, 0, 2048], 32, 70),
+    (16, 4, 128, 5, [40000], 32, 40),                       # more than 1024 blocks, five rows
+])
+def test_sparse_tree_attn_batched(rt, H, Hkv, Dh, n, L, block, n_sel):
+    print(f"sparse H={H}/{Hkv} Dh={Dh} n={n} L={L} block={block} sel={n_sel}", flush=True)
+    check_sparse(rt, Case("bf16", H, Hkv, Dh, n, L, seed=80 + n), block, n_sel)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_short_prefixes_of_a_large_cache(rt, dtype):
+    """The launch is sized for the capacity; hardly anything of it is used."""
+    for n, H in ((1, 8), (3, 8), (20, 8), (70, 4)):
+        c = Case(dtype, H, 4, 64, n, [33, 0, 129], cap=20000, seed=90 + n)
+        check_weights(rt, c)
+        check_sparse(rt, c, 32, 3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_slots_past_the_capacity_are_not_seen(rt, dtype):
+    """kv_cap below what the lengths say: the kernels stay within it (debug builds record it)."""
+    for n, H in ((1, 8), (9, 4), (40, 8)):
+        c = Case(dtype, H, 4, 64, n, [700, 300], rows=[n, n], seed=95 + n)
+        cap = 690                                           # inside the first prefix, past all of the second
+        k, v = c.k.clone(), c.v.clone()
+        c.k[:, :, cap:] = math.nan
+        c.v[:, :, cap:] = math.nan
+        kv_len, n_q, n_tail, mask = c.dev()
+        out = rt.sparse_tree_attn(c.q, c.k, c.v, rt.block_keys(k, kv_len, 32), kv_len, n_q, n_tail, mask, cap, 32, 22)
+        rated, w = rt.tree_attn_weights(c.q, c.k, c.v, kv_len, n_q, n_tail, mask, cap,
+                                        weights_out=torch.full((2, 4, c.cap), -5.0, device="cuda"))
+        assert torch.all(w[0, :, cap:] == -5.0)
+        assert torch.isfinite(out.float()).all()
+        c.L, c.tails, c.k, c.v = [cap, 300], [0, n], k, v
+        for b in range(2):
+            for h in range(4):
+                see = torch.cat([torch.ones(n, c.L[b], dtype=torch.bool, device="cuda"), c.tail_see(b)], 1)
+                want, tol, p, ptol = attend(c, b, h, see)
+                G = H // 4
+                close(rated[b, :, h * G: (h + 1) * G], want, tol, f"rated b={b} h={h}")
+                add = p.sum((0, 1))
+                close(w[b, h, : add.numel()], add, ptol.sum((0, 1)) + (n * G + 2) * 2.0 ** -24 * add + 1e-30, "weights")
+                # (22 blocks of 32 hold the second prefix, and the first up to the capacity)
+                close(out[b, :, h * G: (h + 1) * G], want, tol, f"sparse b={b} h={h}")
+
+
 # ---------------------------------------------------------------------------- how the calls are made
 def _calls(rt, seed=21):
     """A call of every operator on inputs of its own: (function that runs it, its outputs)."""

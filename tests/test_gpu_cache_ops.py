@@ -296,3 +296,33 @@ def test_weights_compact(rt):
     assert torch.equal(w, want)
     rt.weights_compact(w, i32([299, 299]), i32([[0, 1], [0, 5]]), i32([1, 1]), 1)      # past the capacity: left alone
     assert torch.equal(w, want)
+
+
+# ---------------------------------------------------------------------------- the debug build
+def test_lengths_past_the_capacity_are_recorded(rt, monkeypatch):
+    """Device data that the host cannot check: the debug build records it, both builds stay in bounds."""
+    from paper_2512_21857_amd import abi
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    B, H, Dh, n, cap = 1, 2, 64, 3, 64
+    k, v = (torch.ones(B, H, cap, Dh, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.ones(B, n, H, Dh, dtype=torch.bfloat16, device="cuda")
+    mask = torch.full((B, n, 2), 7, dtype=torch.int64, device="cuda")
+    rows, w = i32(n), torch.ones(B, H, cap, device="cuda")
+    freq, _ = rt.rope_freqs(Dh)
+    means = torch.zeros(B, H, 2, Dh, device="cuda")
+
+    def calls(L):
+        yield lambda: rt.rope_append(q, q, q, i32(0, 1, 2)[None], i32(L), rows, freq, k, v)
+        yield lambda: rt.block_keys(k, i32(L + 3), 32, out=means)
+        yield lambda: rt.sparse_tree_attn(q, k, v, means, i32(L), rows, rows, mask, cap, 32, 1, 0, 1)
+        yield lambda: rt.tree_attn_weights(q, k, v, i32(L), rows, rows, mask, cap)
+        yield lambda: rt.kv_evict(k, v, w, i32(L + 3), 32)
+        yield lambda: rt.weights_compact(w, i32(L), i32(0, 2)[None], i32(1), 1)
+
+    for L, debug, recorded in ((61, True, False), (62, True, True), (62, False, False)):
+        monkeypatch.setattr(rt, "lib", abi.lib_debug if debug else abi.lib)
+        lib = rt.lib()
+        stream = torch.cuda.current_stream().cuda_stream
+        for i, call in enumerate(calls(L)):
+            call()
+            assert lib.adt_device_check(stream) == (abi.E_DEVICE_INVARIANT if recorded else abi.OK), (L, debug, i)
