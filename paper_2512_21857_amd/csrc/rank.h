@@ -134,6 +134,8 @@ struct RankRow {
         if (!SETTLED) n_equal += __popcll(__ballot(m == prefix));
         __builtin_amdgcn_sched_barrier(0);
       }
+      // (what lane 0 stores is counted above, key by key: sunk into its branch, V masks would wait for it)
+      asm volatile("" : "+v"(n_in), "+v"(n_equal));
       __syncthreads();
       if (lane == 0) {
         sh.wave_n[0][wave] = n_in;
@@ -152,13 +154,15 @@ struct RankRow {
         equal_all += sh.wave_n[1][w];
       }
       uint32_t eq = equal_done + equal0, at = done + in0 + min(eq, need) - min(equal_done, need);
-      const int i0 = first(r);
+      int i0 = first(r);
+      K low = prefix;
+      asm volatile("" : "+v"(i0), "+v"(low));      // (or V indices and V compares from above are kept for here)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const K m = k[j] & mask;
-        bool in = SETTLED ? m >= prefix : m > prefix;
+        bool in = SETTLED ? m >= low : m > low;
         if (!SETTLED) {
-          const bool equal = m == prefix;
+          const bool equal = m == low;
           const uint64_t eqs = __ballot(equal);
           in = in || (equal && eq + __popcll(eqs & below) < need);
           eq += __popcll(eqs);
