@@ -18,6 +18,10 @@
 // with more than 16 rows in cache_attn_shared_kernel, whose waves share the keys.  fp32 runs on the
 // 16x16x4 MFMA, 16 keys a step, without LDS.  Scores, softmax sums and outputs are fp32.
 //
+// Bound by the read of K and V, in bf16 also at 64 rows a head: one row of 32 heads over 65333 slots of 8
+// key-value heads (268 MB) 52-58 us, sixteen trees of up to 61 rows of 32 heads (398 MB) 78 us, 5.1 TB/s;
+// the chosen blocks of sixteen 16-row trees (462 MB) 98-102 us.
+//
 // A masked score is dropped by selection, so whatever a slot's key holds does not matter to rows
 // that do not see it.  Its value does meet their zero weight in the second product, and 0 * inf is
 // NaN; a wave whose results come out not finite therefore goes through its steps once more with
@@ -944,7 +948,8 @@ __device__ __forceinline__ float2 row_factor(float m, float sum, float rating) {
 // the next ones requested meanwhile, and goes through the query rows tile by tile (A = Q rows, B =
 // K^T: lane (l, g) gets rows 4 g + r of key l, so a column adds up within its lanes).  The queries of
 // up to QROWS rows lie in LDS; more are read from the L2 again for every chunk.  Few keys under many
-// rows: the waves of a workgroup take the same 32 keys and deal the row tiles out.
+// rows: the waves of a workgroup take the same 32 keys and deal the row tiles out.  Bound by the second
+// read of K: sixteen trees of up to 61 rows of 32 heads 48 us, 4.1 TB/s.
 constexpr int SW_CHUNK = 32;        // keys per wave and turn
 template <typename T, int DH>
 struct SlotTile {
@@ -1324,7 +1329,7 @@ adt_status launch_sparse_attn(CacheAttn a, int B, const float* means, int64_t mb
 // Workspace of attention that rates its slots: the rows' maxima and sums, the scores where they are
 // kept, partial results.  Scores are kept, instead of computed again from the keys, where they take
 // at most an eighth of the keys' bytes (written and read, a quarter of reading the keys again: one row
-// of four heads over 65333 slots of 8 key-value heads, 32.7 us -> 8 for the slots' weights and the merge).
+// of four heads over 65333 slots of 8 key-value heads, 32.7 us -> 6.7 for the slots' weights and the merge).
 struct WeightsWs {
   bool keep;
   size_t kept, part, bytes;

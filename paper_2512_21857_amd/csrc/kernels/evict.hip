@@ -3,9 +3,10 @@
 // together; and the weights of an accepted path, moved as the path's keys and values are.
 //
 // Two launches.  evict_select_kernel, a workgroup per slice, finds the smallest weight that stays
-// by radix selection on the weights' bits and writes the kept slots in order; evict_move_kernel
-// moves the rows.  Selecting is bound by its passes over the weights (they stay in the L2), moving
-// by memory: the kept rows are read once and written once.
+// by radix selection on the weights' bits and writes the kept slots in order; evict_copy_kernel, or
+// in place evict_place_kernel, moves the rows.  Selecting is bound by one CU's passes over its slice's
+// weights (65321 of them 28 us, 2400 of each of 1024 slices 11), moving by memory: the kept rows are
+// read once and written once (1024 of 1024 slices, 1.07 GB in all, 202 us, 5.3 TB/s).
 #include <algorithm>
 
 #include "../launch.h"

@@ -5,7 +5,8 @@
 //
 // Bound by memory: every value is read once and written once, three flops each.  A workgroup
 // takes one row (all its heads), or a part of one row's heads where there are few rows, and first
-// makes the row's rot / 2 sines and cosines, in LDS; the heads then share them.
+// makes the row's rot / 2 sines and cosines, in LDS; the heads then share them.  4096 rows of 32 + 8 + 8
+// heads of 128: 18.5 us, 5.4 TB/s; one row 3 us.
 #include <algorithm>
 
 #include "../launch.h"
