@@ -402,6 +402,25 @@ def test_sparse_tree_attn_batched(rt, H, Hkv, Dh, n, L, block, n_sel):
     check_sparse(rt, Case("bf16", H, Hkv, Dh, n, L, seed=80 + n), block, n_sel)
 
 
+@pytest.mark.parametrize("Dh,n,L,block", [
+    (64, 1, 524285, 32),                # the most blocks a call may have: 16384
+    (64, 20, 524260, 32),
+    (128, 4, 131060, 32),               # the most that four rows choose from in one launch: 4096
+    (128, 1, 393100, 32),               # and one row: 12288
+])
+def test_sparse_at_the_limits_of_blocks(rt, Dh, n, L, block):
+    print(f"sparse Dh={Dh} n={n} L={L}", flush=True)
+    n_blk = -(-L // block)
+    check_sparse(rt, Case("bf16", 2, 1, Dh, n, [L], cap=n_blk * block, seed=n + 40), block, 11)
+
+
+@pytest.mark.parametrize("dtype,L", [("bf16", [300]), ("f32", [77]), ("bf16", [17000, 40])])
+def test_tree_attn_weights_most_rows(rt, dtype, L):
+    """8192 rows of one key-value head."""
+    print(f"rated {dtype} 8192 rows L={L}", flush=True)
+    check_weights(rt, Case(dtype, 64, 1, 64, 128, L, rows=[128] * len(L), seed=66), rated=True)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_short_prefixes_of_a_large_cache(rt, dtype):
     """The launch is sized for the capacity; hardly anything of it is used."""
