@@ -1182,16 +1182,20 @@ struct CachePlan {
 // the launch expects: the slots of the cache, or n_sel blocks and for the rows of a tree, which share
 // most of their choice, half as many again (sixteen sequences of 16 rows taking 48 blocks each, 110 in
 // all: 13 stages a split 108 us, 18 98, 24 107).  Sequences that have more take more splits.  At
-// least three stages, or two steps for each wave, pay for a split's start and its partial results.  A
-// workgroup that shares its keys keeps one stage in flight where two of them fit a CU, and three where
-// there is so little work (under eight stages a CU) that one to a CU is all there is.
+// least three stages, or two steps for each wave, pay for a split's start and its partial results; in
+// fp32, whose products take longer and whose next step waits for them, one step does (17 rows over 300
+// slots 8.7 -> 6.8 us, over 16 of 141 blocks 45 -> 39 in all; bf16, one row over 32 of 511 blocks, 10.3
+// with two and 10.5 with one).  A workgroup that shares its keys keeps one stage in flight where two of
+// them fit a CU, and three where there is so little work (under eight stages a CU) that one to a CU is
+// all there is.
 static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
   const int rows = a.nq_max * a.G;
   CachePlan p;
   p.shared = dtype == ADT_BF16 && rows > 16;
   p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 || !p.shared ? 4 : 8;
   p.groups = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
-  const int unit = p.shared ? 64 : dtype == ADT_BF16 ? 32 : 16, least = p.shared ? 3 : 2 * CA_WAVES;
+  const int unit = p.shared ? 64 : dtype == ADT_BF16 ? 32 : 16;
+  const int least = p.shared ? 3 : dtype == ADT_BF16 ? 2 * CA_WAVES : CA_WAVES;
   int64_t most = a.kv_cap, expect = most;      // keys
   if (a.block) {
     most = std::min<int64_t>(most, (int64_t)a.n_sel * a.nq_max * a.block + ADT_MAX_NODES);
