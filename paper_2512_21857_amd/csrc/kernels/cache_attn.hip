@@ -1176,7 +1176,7 @@ struct CachePlan {
   int groups;       // workgroups side by side for the rows of one key-value head
   int splits, per;  // most splits of the keys; steps (stages where shared) per split
   int likely;       // splits of the keys that the launch expects
-  int deep;         // stages in flight
+  int deep;         // stages in flight (shared)
 };
 // Splits: as many as give the workgroups that the CUs hold at once (`slots`) equal shares of the keys
 // the launch expects: the slots of the cache, or n_sel blocks and for the rows of a tree, which share
@@ -1185,9 +1185,10 @@ struct CachePlan {
 // least three stages, or two steps for each wave, pay for a split's start and its partial results; in
 // fp32, whose products take longer and whose next step waits for them, one step does (17 rows over 300
 // slots 8.7 -> 6.8 us, over 16 of 141 blocks 45 -> 39 in all; bf16, one row over 32 of 511 blocks, 10.3
-// with two and 10.5 with one).  A workgroup that shares its keys keeps one stage in flight where two of
-// them fit a CU, and three where there is so little work (under eight stages a CU) that one to a CU is
-// all there is.
+// with two and 10.5 with one).  Where there is little work for workgroups that share their keys (under
+// eight stages a CU), one to a CU is all they get, and those of 128 rows, whose waves take both steps of
+// a stage, keep three stages in flight in place of one (244 rows of 8 heads over 16 of 141 blocks 55 us,
+// 62 with one; 61 rows of 32 heads over 24 of 74 blocks 37.4 with one, 38.7 with three, in all).
 static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
   const int rows = a.nq_max * a.G;
   CachePlan p;
@@ -1204,12 +1205,13 @@ static CachePlan cache_plan(const CacheAttn& a, int B, int dtype) {
   most = (most + unit - 1) / unit + 1;
   expect = (expect + unit - 1) / unit;
   const int64_t pairs = (int64_t)B * a.Hkv * p.groups;
-  p.deep = p.shared && pairs * expect < 8 * 256 ? 3 : 1;
+  const bool little = p.shared && pairs * expect < 8 * 256;
+  p.deep = little && p.tiles == 8 ? 3 : 1;
   const int slots = p.shared ? (p.deep > 1 ? 256 : 512) : p.tiles == 1 ? 768 : p.tiles == 2 ? 512 : 256;
   p.per = (int)std::max<int64_t>(least, (pairs * expect + slots - 1) / slots);
   // (a few units more than one share are no reason for partial results and their merge)
   int64_t splits = most <= p.per + p.per / 4 ? 1 : (most + p.per - 1) / p.per;
-  splits = std::min<int64_t>(splits, std::max<int64_t>(1, (p.deep > 1 ? slots : 4 * slots) / pairs));
+  splits = std::min<int64_t>(splits, std::max<int64_t>(1, (little ? 256 : 4 * slots) / pairs));
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, 64));
   p.likely = (int)std::min<int64_t>(p.splits, (expect + p.per - 1) / p.per);
   return p;
@@ -1231,15 +1233,10 @@ static void attn_launch(const CacheAttn& a, int B, const CachePlan& p, const Dea
   cache_attn_shared_kernel<DH, NW, KH, P, SPARSE><<<grid, NW * WAVE, list, st>>>(a, deal, part_o, part_ml)
   if constexpr (sizeof(T) == 2) {
     if (p.shared) {
-      if (p.deep > 1) {
-        if (p.tiles == 2) ADT_CS(4, 2, 3);
-        else if (p.tiles == 4) ADT_CS(8, 2, 3);
-        else ADT_CS(8, 1, 3);
-      } else {
-        if (p.tiles == 2) ADT_CS(4, 2, 1);
-        else if (p.tiles == 4) ADT_CS(8, 2, 1);
-        else ADT_CS(8, 1, 1);
-      }
+      if (p.tiles == 2) ADT_CS(4, 2, 1);
+      else if (p.tiles == 4) ADT_CS(8, 2, 1);
+      else if (p.deep > 1) ADT_CS(8, 1, 3);
+      else ADT_CS(8, 1, 1);
     } else {
       ADT_CA(1);
     }
