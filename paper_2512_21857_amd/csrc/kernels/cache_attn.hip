@@ -549,7 +549,7 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
 }
 
 // Many rows (more than 16) in bf16: the waves of a workgroup share the keys instead.  A stage of two
-// 32-key steps comes into LDS once, fetched by all threads into registers one to three stages ahead;
+// 32-key steps comes into LDS once, fetched by all threads into registers P stages (one or three) ahead;
 // wave w computes row tile w % TILES, for step w / TILES of the stage (KH = 2) or both (KH = 1), so a
 // wave holds one tile's outputs and the CU two or four waves per SIMD.  Rows of K and V lie in 16-byte
 // chunks swizzled by row, so that the operand reads (16 rows of one chunk column; 8 rows of two in the
