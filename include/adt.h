@@ -227,7 +227,8 @@ adt_status adt_block_keys(const void* k_cache, int64_t stride_b, int64_t stride_
  * means (adt_block_keys, with the strides given) has to be up to date for the whole prefix.
  * sel: NULL, or [B][nq_max][Hkv][n_sel] int32 out: the chosen blocks of rows i < n_q[b] in rising
  *   order, -1 after the last.  A row that sees no slot gives zeros.
- * Other arguments as in adt_tree_attn.  workspace: adt_sparse_tree_attn_workspace_size() bytes,
+ * Other arguments as in adt_tree_attn; out may be q itself (ADT_E_ARG where they overlap otherwise).
+ * workspace: adt_sparse_tree_attn_workspace_size() bytes,
  * 16-byte aligned.  ADT_E_SHAPE: Dh, block, H not a multiple of Hkv, misaligned addresses or
  * strides (16 bytes); ADT_E_CAPACITY: nq_max, workspace, more than 16384 blocks in kv_cap;
  * ADT_E_ARG: n_first + n_last > n_sel, n_sel < 1. */
@@ -252,7 +253,8 @@ adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, const void* 
  * weights_in:  element (b, h, s) at b * stride_wb + h * stride_wh + s; NULL: none
  * weights_out: the same strides; may be weights_in
  * row_weight:  [B][nq_max] fp32 (a draft's path confidences, 0 for rows not to count); NULL: ones
- * A row that sees no slot gives zeros and adds nothing.
+ * A row that sees no slot gives zeros and adds nothing.  out must not overlap q, which is read again
+ * for the weights (ADT_E_ARG).
  * workspace: adt_tree_attn_weights_workspace_size() bytes, 16-byte aligned.  H a multiple of Hkv,
  * nq_max * H / Hkv <= 8192 (ADT_E_SHAPE, ADT_E_CAPACITY); q, caches and out 16-byte aligned,
  * strides multiples of 16 bytes. */

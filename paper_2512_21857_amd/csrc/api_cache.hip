@@ -140,6 +140,11 @@ static bool sized(CacheAttn& a, int32_t B, int32_t H, int32_t Hkv, int32_t Dh, i
   a.kv_cap = kv_cap;
   return true;
 }
+// Whether the output rows share memory with the queries (both [B][nq_max][H][Dh], contiguous).
+static bool out_overlaps_q(const CacheAttn& a, int32_t B, int32_t dtype) {
+  const uintptr_t q = (uintptr_t)a.q, out = (uintptr_t)a.out;
+  return (q < out ? out - q : q - out) < (size_t)B * a.nq_max * a.Hkv * a.G * a.Dh * elem_bytes(dtype);
+}
 constexpr int32_t MAX_BLOCKS = 16384;
 static bool known_block(int32_t block) { return block == 32 || block == 64 || block == 128; }
 
@@ -180,6 +185,8 @@ extern "C" adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, c
   const size_t need = sparse_attn_ws_bytes(a, B, dtype);
   ADT_CHECK_ARG(workspace && workspace_bytes >= need, ADT_E_CAPACITY, "sparse_tree_attn: workspace %zu < %zu bytes",
                 workspace_bytes, need);
+  // (a workgroup has read its rows' queries before it writes them, so the queries themselves will do)
+  ADT_CHECK_ARG(out == q || !out_overlaps_q(a, B, dtype), ADT_E_ARG, "sparse_tree_attn: out overlaps q");
   return launch_sparse_attn(a, B, means, stride_mb, stride_mh, n_first, n_last, sel, dtype, workspace,
                             (hipStream_t)stream);
 }
@@ -209,6 +216,8 @@ extern "C" adt_status adt_tree_attn_weights(const void* q, const void* k_cache, 
   const size_t need = weights_attn_ws_bytes(a, B, dtype);
   ADT_CHECK_ARG(workspace && workspace_bytes >= need, ADT_E_CAPACITY, "tree_attn_weights: workspace %zu < %zu bytes",
                 workspace_bytes, need);
+  // (the slots' weights take the queries again after the output was written)
+  ADT_CHECK_ARG(!out_overlaps_q(a, B, dtype), ADT_E_ARG, "tree_attn_weights: out overlaps q");
   return launch_weights_attn(a, B, weights_in, weights_out, stride_wb, stride_wh, decay, row_weight, dtype, workspace,
                              (hipStream_t)stream);
 }

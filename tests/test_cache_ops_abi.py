@@ -143,6 +143,20 @@ def test_tree_attn_weights_refusals(L, changed, code):
     assert "tree_attn_weights" in abi.last_error()
 
 
+def test_outputs_over_the_queries(L):
+    """Rated attention reads its queries again after the output is written, so the two may not share
+    memory; over chosen blocks the output may be the queries, but not lie across them."""
+    from paper_2512_21857_amd import abi
+    q = 1 << 20
+    size = SIZES["B"] * SIZES["nq_max"] * SIZES["H"] * SIZES["Dh"] * 2
+    for out in (q, q + 16, q - 16, q + size - 16, q - size + 16):
+        assert call(L.adt_tree_attn_weights, RATED, q=q, out=out) == abi.E_ARG, out - q
+        assert "overlaps" in abi.last_error()
+        if out != q:
+            assert call(L.adt_sparse_tree_attn, SPARSE, q=q, out=out) == abi.E_ARG, out - q
+            assert "overlaps" in abi.last_error()
+
+
 def test_attention_workspaces(L):
     """Sizes for what the calls take, 0 for what they refuse."""
     sparse = lambda *a: L.adt_sparse_tree_attn_workspace_size(*a)       # noqa: E731

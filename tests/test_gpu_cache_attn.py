@@ -568,6 +568,24 @@ def test_dense_choice_equals_tree_attention(rt):
         assert torch.all((got.double() - want).abs() <= 2 * ((2.0 ** -8 + 2.0 ** -10) * vmax + 2.0 ** -8 * want.abs()))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,Hkv,n,L", [
+    (8, 2, 1, [900, 0, 40]),            # few rows, splits merged by the last
+    (4, 4, 20, [700, 64]),
+    (8, 2, 61, [1500, 33]),             # 244 rows: several groups
+    (4, 4, 61, [100]),                  # one split writes the output
+])
+def test_sparse_output_over_its_queries(rt, dtype, H, Hkv, n, L):
+    print(f"sparse in place {dtype} H={H}/{Hkv} n={n} L={L}", flush=True)
+    c = Case(dtype, H, Hkv, 64, n, L, seed=110 + n)
+    kv_len, n_q, n_tail, mask = c.dev()
+    means = rt.block_keys(c.k, kv_len, 32)
+    want = rt.sparse_tree_attn(c.q, c.k, c.v, means, kv_len, n_q, n_tail, mask, c.cap, 32, 5, out=c.q.clone())
+    out = c.q.clone()
+    rt.sparse_tree_attn(out, c.k, c.v, means, kv_len, n_q, n_tail, mask, c.cap, 32, 5, out=out)
+    assert torch.equal(bits(out), bits(want))
+
+
 def test_refusals_of_the_wrappers(rt):
     """Tensors of other types, shapes, layouts or devices are refused before anything runs."""
     run, o, c = _calls(rt)
