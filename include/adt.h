@@ -228,10 +228,10 @@ adt_status adt_block_keys(const void* k_cache, int64_t stride_b, int64_t stride_
  * sel: NULL, or [B][nq_max][Hkv][n_sel] int32 out: the chosen blocks of rows i < n_q[b] in rising
  *   order, -1 after the last.  A row that sees no slot gives zeros.
  * Other arguments as in adt_tree_attn; out may be q itself (ADT_E_ARG where they overlap otherwise).
- * workspace: adt_sparse_tree_attn_workspace_size() bytes,
- * 16-byte aligned.  ADT_E_SHAPE: Dh, block, H not a multiple of Hkv, misaligned addresses or
- * strides (16 bytes); ADT_E_CAPACITY: nq_max, workspace, more than 16384 blocks in kv_cap;
- * ADT_E_ARG: n_first + n_last > n_sel, n_sel < 1. */
+ * workspace: adt_sparse_tree_attn_workspace_size() bytes (0 for sizes that the call refuses),
+ * 16-byte aligned.  ADT_E_SHAPE: Dh, block, H not a multiple of Hkv, B * Hkv > 65535, misaligned
+ * addresses or strides (16 bytes); ADT_E_CAPACITY: nq_max, nq_max * H / Hkv > 8192, workspace,
+ * more than 16384 blocks in kv_cap; ADT_E_ARG: n_first + n_last > n_sel, n_sel < 1. */
 size_t adt_sparse_tree_attn_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max,
                                            int32_t kv_cap, int32_t block, int32_t n_sel, int32_t dtype);
 adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, const void* v_cache, int64_t stride_b,
@@ -255,9 +255,9 @@ adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, const void* 
  * row_weight:  [B][nq_max] fp32 (a draft's path confidences, 0 for rows not to count); NULL: ones
  * A row that sees no slot gives zeros and adds nothing.  out must not overlap q, which is read again
  * for the weights (ADT_E_ARG).
- * workspace: adt_tree_attn_weights_workspace_size() bytes, 16-byte aligned.  H a multiple of Hkv,
- * nq_max * H / Hkv <= 8192 (ADT_E_SHAPE, ADT_E_CAPACITY); q, caches and out 16-byte aligned,
- * strides multiples of 16 bytes. */
+ * workspace: adt_tree_attn_weights_workspace_size() bytes (0 for sizes that the call refuses), 16-byte
+ * aligned.  H a multiple of Hkv, B * Hkv <= 65535 (ADT_E_SHAPE), nq_max * H / Hkv <= 8192
+ * (ADT_E_CAPACITY); q, caches and out 16-byte aligned, strides multiples of 16 bytes. */
 size_t adt_tree_attn_weights_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max,
                                             int32_t kv_cap, int32_t dtype);
 adt_status adt_tree_attn_weights(const void* q, const void* k_cache, const void* v_cache, int64_t stride_b,

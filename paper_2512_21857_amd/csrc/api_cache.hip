@@ -13,6 +13,7 @@ static bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 // a stride of `elems` elements of `bytes` each that keeps 16-byte alignment
 static bool stride16(int64_t elems, int64_t bytes) { return elems >= 0 && elems * bytes % 16 == 0; }
 constexpr int32_t MAX_GRID_YZ = 65535;
+constexpr int32_t MAX_ROWS = 8192;      // query rows of one key-value head
 
 extern "C" adt_status adt_rope_freqs(const adt_rope_cfg* cfg, double* freq, float* gain) {
   ADT_CHECK_ARG(cfg && freq && gain, ADT_E_ARG, "rope_freqs: null pointer");
@@ -115,7 +116,7 @@ static adt_status check_cache_attn(const char* who, const CacheAttn& a, int32_t 
   ADT_CHECK_ARG(H % a.Hkv == 0 && a.Hkv <= MAX_GRID_YZ && (int64_t)B * a.Hkv <= MAX_GRID_YZ, ADT_E_SHAPE,
                 "%s: %d query heads over %d key-value heads of %d sequences", who, H, a.Hkv, B);
   ADT_CHECK_ARG(a.nq_max >= 1 && a.nq_max <= ADT_MAX_NODES, ADT_E_CAPACITY, "%s: nq_max %d", who, a.nq_max);
-  ADT_CHECK_ARG((int64_t)a.nq_max * (H / a.Hkv) <= 8192, ADT_E_CAPACITY, "%s: %d rows of %d heads per key-value head",
+  ADT_CHECK_ARG((int64_t)a.nq_max * (H / a.Hkv) <= MAX_ROWS, ADT_E_CAPACITY, "%s: %d rows of %d heads per key-value head",
                 who, a.nq_max, H / a.Hkv);
   ADT_CHECK_ARG(a.sh >= (int64_t)a.kv_cap * a.Dh && (B == 1 || a.sb >= (int64_t)a.Hkv * a.sh), ADT_E_SHAPE,
                 "%s: cache strides too small", who);
@@ -133,6 +134,8 @@ static bool sized(CacheAttn& a, int32_t B, int32_t H, int32_t Hkv, int32_t Dh, i
   if (B < 1 || H < 1 || Hkv < 1 || H % Hkv || (Dh != 64 && Dh != 128) || nq_max < 1 || nq_max > ADT_MAX_NODES ||
       kv_cap < 1 || !known_dtype(dtype))
     return false;
+  // (past these the products of the sizes would leave 32 bits)
+  if ((int64_t)B * Hkv > MAX_GRID_YZ || (int64_t)nq_max * (H / Hkv) > MAX_ROWS) return false;
   a.Hkv = Hkv;
   a.G = H / Hkv;
   a.Dh = Dh;
@@ -155,6 +158,7 @@ extern "C" size_t adt_sparse_tree_attn_workspace_size(int32_t B, int32_t H, int3
   a.block = block;
   a.n_blk = (int)(((int64_t)kv_cap + block - 1) / block);
   a.n_sel = n_sel;
+  if (a.n_blk > MAX_BLOCKS) return 0;
   return sparse_attn_ws_bytes(a, B, dtype);
 }
 

@@ -169,6 +169,29 @@ def test_attention_workspaces(L):
     assert rated(1, 32, 8, 128, 61, 4096, 2) == 0
 
 
+@pytest.mark.parametrize("B,H,Hkv,nq_max", [
+    (1, 1 << 30, 1, 128),               # rows of a key-value head: a multiple of 2^32
+    (1, 1 << 25, 1, 64),                # 2^31
+    (1, 8200, 1, 1), (1, 16384, 128, 65),
+    (1 << 30, 1 << 30, 1 << 30, 16), (70000, 1, 1, 1), (1024, 128, 128, 61),
+])
+def test_attention_workspaces_of_refused_sizes(L, B, H, Hkv, nq_max):
+    """More rows or pairs than a call may have: 0 as for the other refusals, whatever the sizes multiply to."""
+    from paper_2512_21857_amd import abi
+    assert L.adt_tree_attn_weights_workspace_size(B, H, Hkv, 64, nq_max, 4096, abi.BF16) == 0
+    assert L.adt_sparse_tree_attn_workspace_size(B, H, Hkv, 64, nq_max, 4096, 64, 16, abi.BF16) == 0
+
+
+def test_attention_workspaces_at_the_limits(L):
+    from paper_2512_21857_amd import abi
+    for dtype in (abi.BF16, abi.F32):
+        for B, H, Hkv, nq in ((1, 8192, 1, 1), (1, 64, 1, 128), (65535, 1, 1, 128), (1, 65535, 65535, 1)):
+            assert L.adt_tree_attn_weights_workspace_size(B, H, Hkv, 64, nq, 100, dtype) > 0
+            assert L.adt_sparse_tree_attn_workspace_size(B, H, Hkv, 64, nq, 100, 32, 3, dtype) > 0
+    assert L.adt_sparse_tree_attn_workspace_size(1, 8, 8, 64, 1, 32 * 16384, 32, 8, abi.BF16) > 0
+    assert L.adt_sparse_tree_attn_workspace_size(1, 8, 8, 64, 1, 32 * 16384 + 1, 32, 8, abi.BF16) == 0
+
+
 EVICT = dict(k=FAKE, v=FAKE, w=FAKE, sb=2 * 64 * 100, ss=64 * 100, wb=200, ws=100, kv_len=FAKE, B=2, slices=2, Dh=64, cap=100,
              budget=40, n_first=4, n_last=8, ko=2 * FAKE, vo=2 * FAKE, wo=2 * FAKE, osb=2 * 64 * 40, oss=64 * 40, owb=80, ows=40,
              kept=FAKE, new_len=FAKE, dtype=1, stream=None)
