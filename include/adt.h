@@ -210,7 +210,8 @@ adt_status adt_rope_append(const void* q, const void* k, const void* v, int64_t 
  * one of the prefix; other rows of means stay as they are.  After an append or a compaction that
  * left the first n slots as they were, start = n suffices.  kv_len: [B] device, at most kv_cap
  * (debug builds record more); start: [B] device.  k_cache as in adt_tree_attn, with Hkv heads;
- * k_cache and means 16-byte aligned, strides multiples of 16 bytes; Dh 64 or 128. */
+ * k_cache and means 16-byte aligned, strides multiples of 16 bytes; Dh 64 or 128; kv_cap at most
+ * 2^31 - 2^24 (ADT_E_CAPACITY). */
 adt_status adt_block_keys(const void* k_cache, int64_t stride_b, int64_t stride_h, const int32_t* start,
                           const int32_t* kv_len, int32_t B, int32_t Hkv, int32_t Dh, int32_t block, int32_t kv_cap,
                           float* means, int64_t stride_mb, int64_t stride_mh, int32_t dtype, void* stream);
@@ -257,7 +258,7 @@ adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, const void* 
  * for the weights (ADT_E_ARG).
  * workspace: adt_tree_attn_weights_workspace_size() bytes (0 for sizes that the call refuses), 16-byte
  * aligned.  H a multiple of Hkv, B * Hkv <= 65535 (ADT_E_SHAPE), nq_max * H / Hkv <= 8192
- * (ADT_E_CAPACITY); q, caches and out 16-byte aligned, strides multiples of 16 bytes. */
+ * and kv_cap <= 2^31 - 2^24 (ADT_E_CAPACITY); q, caches and out 16-byte aligned, strides multiples of 16 bytes. */
 size_t adt_tree_attn_weights_workspace_size(int32_t B, int32_t H, int32_t Hkv, int32_t Dh, int32_t nq_max,
                                             int32_t kv_cap, int32_t dtype);
 adt_status adt_tree_attn_weights(const void* q, const void* k_cache, const void* v_cache, int64_t stride_b,
@@ -288,7 +289,8 @@ adt_status adt_weights_compact(float* weights, int32_t B, int32_t slices, int64_
  * kv_len: device, at most kv_cap (debug builds record more; the excess is not seen).  A slice is a
  * (layer, head) as in adt_kv_compact.  Rows keep the rotation of the positions they had.
  * budget >= 1, n_first + n_last <= budget (ADT_E_ARG); rows of Dh elements whole 16-byte pieces,
- * at most 16 KB; caches 16-byte aligned, their strides multiples of 16 bytes (ADT_E_SHAPE). */
+ * at most 16 KB; caches 16-byte aligned, their strides multiples of 16 bytes (ADT_E_SHAPE); kv_cap
+ * at most 2^31 - 2^24 (ADT_E_CAPACITY). */
 adt_status adt_kv_evict(const void* k_cache, const void* v_cache, const float* weights, int64_t stride_b,
                         int64_t stride_slice, int64_t stride_wb, int64_t stride_ws, const int32_t* kv_len, int32_t B,
                         int32_t slices, int32_t Dh, int32_t kv_cap, int32_t budget, int32_t n_first, int32_t n_last,

@@ -14,6 +14,9 @@ static bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 static bool stride16(int64_t elems, int64_t bytes) { return elems >= 0 && elems * bytes % 16 == 0; }
 constexpr int32_t MAX_GRID_YZ = 65535;
 constexpr int32_t MAX_ROWS = 8192;      // query rows of one key-value head
+// Slots of a cache that kernels loop over: an index past the last one by a round of a workgroup, or of
+// a launch, still fits 32 bits.
+constexpr int32_t MAX_SLOTS = 0x7f000000;
 
 extern "C" adt_status adt_rope_freqs(const adt_rope_cfg* cfg, double* freq, float* gain) {
   ADT_CHECK_ARG(cfg && freq && gain, ADT_E_ARG, "rope_freqs: null pointer");
@@ -92,6 +95,7 @@ extern "C" adt_status adt_block_keys(const void* k_cache, int64_t stride_b, int6
   ADT_CHECK_ARG(Dh == 64 || Dh == 128, ADT_E_SHAPE, "block_keys: head_dim %d not in {64, 128}", Dh);
   ADT_CHECK_ARG(block == 32 || block == 64 || block == 128, ADT_E_SHAPE, "block_keys: block %d not in {32, 64, 128}",
                 block);
+  ADT_CHECK_ARG(kv_cap <= MAX_SLOTS, ADT_E_CAPACITY, "block_keys: kv_cap %d", kv_cap);
   ADT_CHECK_ARG(stride_h >= (int64_t)kv_cap * Dh && (B == 1 || stride_b >= (int64_t)Hkv * stride_h), ADT_E_SHAPE,
                 "block_keys: cache strides too small");
   const int64_t n_blk = ((int64_t)kv_cap + block - 1) / block;
@@ -118,6 +122,7 @@ static adt_status check_cache_attn(const char* who, const CacheAttn& a, int32_t 
   ADT_CHECK_ARG(a.nq_max >= 1 && a.nq_max <= ADT_MAX_NODES, ADT_E_CAPACITY, "%s: nq_max %d", who, a.nq_max);
   ADT_CHECK_ARG((int64_t)a.nq_max * (H / a.Hkv) <= MAX_ROWS, ADT_E_CAPACITY, "%s: %d rows of %d heads per key-value head",
                 who, a.nq_max, H / a.Hkv);
+  ADT_CHECK_ARG(a.kv_cap <= MAX_SLOTS, ADT_E_CAPACITY, "%s: kv_cap %d", who, a.kv_cap);
   ADT_CHECK_ARG(a.sh >= (int64_t)a.kv_cap * a.Dh && (B == 1 || a.sb >= (int64_t)a.Hkv * a.sh), ADT_E_SHAPE,
                 "%s: cache strides too small", who);
   const int64_t es = elem_bytes(dtype);
@@ -135,7 +140,7 @@ static bool sized(CacheAttn& a, int32_t B, int32_t H, int32_t Hkv, int32_t Dh, i
       kv_cap < 1 || !known_dtype(dtype))
     return false;
   // (past these the products of the sizes would leave 32 bits)
-  if ((int64_t)B * Hkv > MAX_GRID_YZ || (int64_t)nq_max * (H / Hkv) > MAX_ROWS) return false;
+  if ((int64_t)B * Hkv > MAX_GRID_YZ || (int64_t)nq_max * (H / Hkv) > MAX_ROWS || kv_cap > MAX_SLOTS) return false;
   a.Hkv = Hkv;
   a.G = H / Hkv;
   a.Dh = Dh;
@@ -240,6 +245,7 @@ extern "C" adt_status adt_kv_evict(const void* k_cache, const void* v_cache, con
                 "kv_evict: B=%d slices=%d Dh=%d kv_cap=%d", B, slices, Dh, kv_cap);
   ADT_CHECK_ARG(budget >= 1 && n_first >= 0 && n_last >= 0 && (int64_t)n_first + n_last <= budget, ADT_E_ARG,
                 "kv_evict: %d first and %d last of %d slots", n_first, n_last, budget);
+  ADT_CHECK_ARG(kv_cap <= MAX_SLOTS, ADT_E_CAPACITY, "kv_evict: kv_cap %d", kv_cap);
   const int64_t es = elem_bytes(dtype), row = Dh * es;
   ADT_CHECK_ARG(row % 16 == 0 && row <= 16384, ADT_E_SHAPE, "kv_evict: rows of %lld bytes", (long long)row);
   // in place: every part is its source, with the source's strides; else none of them is

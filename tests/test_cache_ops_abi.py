@@ -224,3 +224,19 @@ def test_weights_compact_refusals(L, changed, code):
     from paper_2512_21857_amd import abi
     assert call(L.adt_weights_compact, WCOMPACT, **changed) == getattr(abi, code), changed
     assert call(L.adt_weights_compact, WCOMPACT, a_max=0) == abi.OK
+
+
+@pytest.mark.parametrize("cap", [(1 << 31) - 1, (1 << 31) - (1 << 24) + 1])
+def test_capacities_near_the_end_of_32_bits(L, cap):
+    """Slots are indexed in 32 bits, up to a round past the last one: capacities that leave no room for it
+    are refused, not read at negative slots."""
+    from paper_2512_21857_amd import abi
+    far = 1 << 45
+    assert call(L.adt_kv_evict, EVICT, B=1, cap=cap, sb=far, ss=far, wb=far, ws=far) == abi.E_CAPACITY
+    assert "kv_cap" in abi.last_error()
+    assert call(L.adt_block_keys, KEYS, B=1, cap=cap, sb=far, sh=far, mb=far, mh=far) == abi.E_CAPACITY
+    assert "kv_cap" in abi.last_error()
+    assert call(L.adt_tree_attn_weights, RATED, B=1, cap=cap, sb=far, sh=far, wb=far, wh=far, ws_bytes=far) == abi.E_CAPACITY
+    assert "kv_cap" in abi.last_error()
+    assert L.adt_tree_attn_weights_workspace_size(1, 4, 2, 64, 8, cap, abi.BF16) == 0
+    assert L.adt_tree_attn_weights_workspace_size(1, 4, 2, 64, 8, (1 << 31) - (1 << 24), abi.BF16) > 0
