@@ -115,8 +115,9 @@ def kv_compact(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len: torch.Tenso
 # The wrappers below are called once or more per layer of a decoding loop, where their own time
 # counts: they pass addresses as plain integers and check a tensor in one expression.
 _I32, _I64, _F32, _F64, _U8 = torch.int32, torch.int64, torch.float32, torch.float64, torch.uint8
-_current_device = torch._C._cuda_getDevice
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# (torch's own names for the two, and its public, slower calls on a build without them)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _on_device(dev: int, fn, args: tuple) -> None:

@@ -2,6 +2,8 @@
 launched, and the host-only rotary frequencies against their formulas."""
 import ctypes as C
 import math
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -240,3 +242,22 @@ def test_capacities_near_the_end_of_32_bits(L, cap):
     assert "kv_cap" in abi.last_error()
     assert L.adt_tree_attn_weights_workspace_size(1, 4, 2, 64, 8, cap, abi.BF16) == 0
     assert L.adt_tree_attn_weights_workspace_size(1, 4, 2, 64, 8, (1 << 31) - (1 << 24), abi.BF16) > 0
+
+
+def test_runtime_needs_no_private_names_of_torch():
+    """The wrappers import, and ask the public calls, where torch has no raw device and stream queries."""
+    code = """
+import torch
+for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+from types import SimpleNamespace
+torch.cuda.current_device = lambda: 3
+torch.cuda.current_stream = lambda dev=None: SimpleNamespace(cuda_stream=100 + dev)
+from paper_2512_21857_amd import runtime
+seen = []
+runtime._on_device(3, lambda *a: seen.append(a) or 0, (1, 2))
+assert seen == [(1, 2, 103)], seen
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
