@@ -44,7 +44,7 @@ template <typename T, int VEC, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_append_kernel(RopeRows a, const double* __restrict__ freq,
                                                                    float gain) {
   __shared__ float2 cs[ROPE_MAX_PAIRS];
-  const int i = blockIdx.x, b = blockIdx.z;
+  const int i = a.row0 + blockIdx.x, b = blockIdx.z;
   if (i >= min(a.n_rows[b], a.n_max)) return;
   const int64_t row = (int64_t)b * a.n_max + i;
   const int rot = a.rot, half = rot / 2, DH = a.Dh;
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_append_kernel(RopeRows a, c
 }
 
 template <typename T>
-static adt_status rope_append(const RopeRows& a, int B, const double* freq, float gain, bool inter, hipStream_t st) {
+static adt_status rope_append(RopeRows a, int B, const double* freq, float gain, bool inter, hipStream_t st) {
   constexpr int V = 16 / sizeof(T);
   const int64_t lds[] = {a.ldq, a.ldk, a.ldv, a.stride_b, a.stride_h};
   const void* ptrs[] = {a.q, a.k, a.v, a.q_out, a.kc, a.vc};
@@ -120,21 +120,26 @@ static adt_status rope_append(const RopeRows& a, int B, const double* freq, floa
   int parts = (units + ROPE_THREADS - 1) / ROPE_THREADS;
   const int64_t rows = (int64_t)B * a.n_max;
   parts = (int)std::min<int64_t>(parts, std::max<int64_t>(1, 1024 / rows));
-  const dim3 grid(a.n_max, parts, B);
+  // (a launch has fewer than 2^32 threads in a dimension, or it wraps: more rows take several)
+  constexpr int MOST = 1 << 23;
 #define ADT_ROPE(VECV, INTERV) rope_append_kernel<T, VECV, INTERV><<<grid, ROPE_THREADS, 0, st>>>(a, freq, gain)
-  if (wide) {
-    if (inter) ADT_ROPE(V, true);
-    else ADT_ROPE(V, false);
-  } else {
-    if (inter) ADT_ROPE(1, true);
-    else ADT_ROPE(1, false);
+  for (int64_t r0 = 0; r0 < a.n_max; r0 += MOST) {
+    a.row0 = (int)r0;
+    const dim3 grid((unsigned)std::min<int64_t>(MOST, a.n_max - r0), parts, B);
+    if (wide) {
+      if (inter) ADT_ROPE(V, true);
+      else ADT_ROPE(V, false);
+    } else {
+      if (inter) ADT_ROPE(1, true);
+      else ADT_ROPE(1, false);
+    }
+    ADT_LAUNCH_CHECK();
   }
 #undef ADT_ROPE
-  ADT_LAUNCH_CHECK();
   return ADT_OK;
 }
 
-adt_status launch_rope_append(const RopeRows& a, int B, const double* freq, float gain, bool inter, int dtype,
+adt_status launch_rope_append(RopeRows a, int B, const double* freq, float gain, bool inter, int dtype,
                               hipStream_t st) {
   return dtype == ADT_BF16 ? rope_append<uint16_t>(a, B, freq, gain, inter, st)
                            : rope_append<float>(a, B, freq, gain, inter, st);

@@ -287,7 +287,7 @@ adt_status launch_codebook_knn(const float* cb, int n, int dim, int k, int32_t* 
 
 // rope.hip
 // Rows [B][n_max] of q, k, v (ld elements from row to row), rotated over the first rot dims and
-// appended; fields as the arguments of adt_rope_append.
+// appended; fields as the arguments of adt_rope_append.  row0: the first row of a launch.
 struct RopeRows {
   const void *q, *k, *v;
   int64_t ldq, ldk, ldv;
@@ -296,8 +296,9 @@ struct RopeRows {
   void *q_out, *kc, *vc;
   int64_t stride_b, stride_h;
   int kv_cap;
+  int row0 = 0;
 };
-adt_status launch_rope_append(const RopeRows& a, int B, const double* freq, float gain, bool inter, int dtype,
+adt_status launch_rope_append(RopeRows a, int B, const double* freq, float gain, bool inter, int dtype,
                               hipStream_t st);
 
 // blocks.hip

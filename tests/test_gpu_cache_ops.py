@@ -138,6 +138,23 @@ def test_rope_append_stops_at_the_capacity(rt):
     assert not vc[0, :, :8].any() and not vc[1].any() and not kc[1].any()
 
 
+def test_rope_append_more_rows_than_a_launch(rt):
+    """A launch has fewer than 2^32 threads a dimension: 2^24 rows and more take turns."""
+    g = gen(12)
+    n = (1 << 24) + 1003
+    q, k, v = (normal(g, "bf16", 1, n, 1, 2) for _ in range(3))
+    kc, vc = (torch.zeros(1, 1, n + 9, 2, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    pos = torch.randint(0, 5000, (1, n), generator=g, device="cuda", dtype=torch.int32)
+    freq, gain = rt.rope_freqs(2)
+    out = rt.rope_append(q, k, v, pos, i32([5]), i32([n - 2]), freq, kc, vc, out=torch.full_like(q, 3.0))
+    for got, x in ((out[0, : n - 2], q), (kc[0, 0, 5: n + 3, None], k)):
+        want = rope_reference(x, pos, freq, gain, "half")[0, : n - 2]
+        # (the pair's bound of the cases above: 2^-20 times its length, below 2 max|x|)
+        assert torch.all((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -19 * x.abs().max())
+    assert torch.equal(bits(vc[0, 0, 5: n + 3]), bits(v[0, : n - 2, 0])) and not vc[0, 0, n + 3:].any()
+    assert torch.all(out[0, n - 2:] == 3.0) and not kc[0, 0, n + 3:].any() and not kc[0, 0, :5].any()
+
+
 def test_rope_inverse_positions_undo(rt):
     """Rotating by -pos what was rotated by pos gives the rows back, to four roundings of fp32."""
     g = gen(4)
