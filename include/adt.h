@@ -193,7 +193,7 @@ adt_status adt_rope_freqs(const adt_rope_cfg* cfg /*[host]*/, double* freq /*[ho
  * b * stride_b + h * stride_h + slot * Dh; other rows and slots stay as they are, and so does a
  * slot that would lie at or past kv_cap (debug builds record it).  freq: device [rot_dim / 2]
  * doubles (angles are reduced in double, so far positions keep theirs).  n_max may be any
- * number of rows.  Dh even, at most 256; rot_dim even, in [2, Dh]. */
+ * number of rows, B at most 65535.  Dh even, at most 256; rot_dim even, in [2, Dh]. */
 adt_status adt_rope_append(const void* q, const void* k, const void* v, int64_t ldq, int64_t ldk, int64_t ldv,
                            const int32_t* pos, const int32_t* kv_len, const int32_t* n_rows, const double* freq,
                            float gain, int32_t rot_dim, int32_t layout, int32_t B, int32_t n_max, int32_t H,
@@ -270,7 +270,7 @@ adt_status adt_tree_attn_weights(const void* q, const void* k_cache, const void*
                                  void* stream);
 /* The weights of an accepted path, as adt_kv_compact moves its keys and values: in every slice,
  * slot kv_len[b] + m <- slot kv_len[b] + path[b][m] for m = 1..n_acc[b].  Arguments as there
- * (slots at or past kv_cap are left alone). */
+ * (slots at or past kv_cap are left alone); fewer than 2^25 slices (ADT_E_SHAPE). */
 adt_status adt_weights_compact(float* weights, int32_t B, int32_t slices, int64_t stride_wb, int64_t stride_ws,
                                const int32_t* kv_len, int32_t kv_cap, const int32_t* path, int32_t path_stride,
                                const int32_t* n_acc, int32_t a_max, void* stream);
@@ -289,8 +289,8 @@ adt_status adt_weights_compact(float* weights, int32_t B, int32_t slices, int64_
  * kv_len: device, at most kv_cap (debug builds record more; the excess is not seen).  A slice is a
  * (layer, head) as in adt_kv_compact.  Rows keep the rotation of the positions they had.
  * budget >= 1, n_first + n_last <= budget (ADT_E_ARG); rows of Dh elements whole 16-byte pieces,
- * at most 16 KB; caches 16-byte aligned, their strides multiples of 16 bytes (ADT_E_SHAPE); kv_cap
- * at most 2^31 - 2^24 (ADT_E_CAPACITY). */
+ * at most 16 KB; caches 16-byte aligned, their strides multiples of 16 bytes, fewer than 2^24
+ * slices, in place 2^23 (ADT_E_SHAPE); kv_cap at most 2^31 - 2^24 (ADT_E_CAPACITY). */
 adt_status adt_kv_evict(const void* k_cache, const void* v_cache, const float* weights, int64_t stride_b,
                         int64_t stride_slice, int64_t stride_wb, int64_t stride_ws, const int32_t* kv_len, int32_t B,
                         int32_t slices, int32_t Dh, int32_t kv_cap, int32_t budget, int32_t n_first, int32_t n_last,

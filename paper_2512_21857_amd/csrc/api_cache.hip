@@ -250,6 +250,9 @@ extern "C" adt_status adt_kv_evict(const void* k_cache, const void* v_cache, con
   ADT_CHECK_ARG(row % 16 == 0 && row <= 16384, ADT_E_SHAPE, "kv_evict: rows of %lld bytes", (long long)row);
   // in place: every part is its source, with the source's strides; else none of them is
   const bool place = k_out == k_cache;
+  // (a launch of 2^32 threads or more in a dimension would wrap: 512 a slice in place, 256 into another
+  // cache; the selection's 1024 only where 2^22 slices would be 2^38 bytes of keys)
+  ADT_CHECK_ARG(slices < (place ? 1 << 23 : 1 << 24), ADT_E_SHAPE, "kv_evict: %d slices", slices);
   ADT_CHECK_ARG((v_out == v_cache) == place && (weights_out == weights) == place, ADT_E_ARG,
                 "kv_evict: caches and weights in place or none of them");
   ADT_CHECK_ARG(!place || (out_stride_b == stride_b && out_stride_slice == stride_slice && out_stride_wb == stride_wb &&
@@ -282,6 +285,7 @@ extern "C" adt_status adt_weights_compact(float* weights, int32_t B, int32_t sli
                 "weights_compact: a_max %d path_stride %d", a_max, path_stride);
   ADT_CHECK_ARG(stride_ws >= kv_cap && (B == 1 || stride_wb >= slices * stride_ws), ADT_E_SHAPE,
                 "weights_compact: strides too small");
+  ADT_CHECK_ARG(slices < 1 << 25, ADT_E_SHAPE, "weights_compact: %d slices", slices);   // (as above, 128 a slice)
   if (a_max == 0) return ADT_OK;
   return launch_weights_compact(weights, B, slices, stride_wb, stride_ws, kv_len, kv_cap, path, path_stride, n_acc,
                                 a_max, (hipStream_t)stream);

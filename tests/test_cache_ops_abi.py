@@ -261,3 +261,17 @@ assert seen == [(1, 2, 103)], seen
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr
+
+
+def test_more_slices_than_a_launch(L):
+    """Slices whose launches would wrap at 2^32 threads are refused, not left out in silence."""
+    from paper_2512_21857_amd import abi
+    far = 1 << 45
+    wide = dict(B=1, sb=far, wb=far, osb=far, owb=far)
+    place = dict(ko=FAKE, vo=FAKE, wo=FAKE, oss=EVICT["ss"], ows=EVICT["ws"])
+    assert call(L.adt_kv_evict, EVICT, slices=1 << 24, **wide) == abi.E_SHAPE
+    assert "slices" in abi.last_error()
+    assert call(L.adt_kv_evict, EVICT, slices=1 << 23, **wide, **place) == abi.E_SHAPE
+    assert "slices" in abi.last_error()
+    assert call(L.adt_weights_compact, WCOMPACT, B=1, slices=1 << 25, wb=far) == abi.E_SHAPE
+    assert "slices" in abi.last_error()
