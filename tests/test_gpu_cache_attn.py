@@ -193,6 +193,24 @@ def test_sparse_more_blocks_than_lds_keys(rt):
     check_sparse(rt, Case("bf16", 2, 1, 64, 2, [140000], seed=4), 32, 33, 1, 1)
 
 
+@pytest.mark.parametrize("kind", ["normal", "equal", "ties", "nan"])
+def test_sparse_selection_in_rounds(rt, kind):
+    """More than four rows over more than 1024 blocks: a workgroup selects for a row and reads its scores
+    anew, here in three rounds of 2048, with ties and NaN across their ends."""
+    print(f"sparse rounds {kind}", flush=True)
+    c = Case("bf16", 2, 1, 64, 6, [140000], seed=4)
+    means = torch.empty(1, 1, -(-c.cap // 32), 64, device="cuda").normal_(generator=gen(61))
+    if kind == "equal":
+        means[:] = means[:, :, :1]
+    elif kind == "ties":
+        means[:] = means[:, :, :7].repeat(1, 1, means.shape[2] // 7 + 1, 1)[:, :, : means.shape[2]]
+    elif kind == "nan":
+        means[:, :, 9:4370] = math.nan
+        means[:, :, 2040:2056] = 1.0
+    for n_sel, first, last in ((33, 1, 1), (1, 0, 0), (2500, 0, 2)):
+        check_sparse(rt, c, 32, n_sel, first, last, means=means)
+
+
 def test_sparse_layer_of_a_larger_cache(rt):
     check_sparse(rt, Case("bf16", 4, 2, 64, 9, [400, 333], layers=3), 32, 4)
 
@@ -370,6 +388,43 @@ def test_attention_over_more_than_two_billion_elements(rt):
     blk = torch.from_numpy(took).cuda().repeat_interleave(128, 1)[:, : c.L[0]]
     want, tol, _, _ = attend(c, 0, 8, torch.cat([blk, c.tail_see(0)], 1))
     close(out[0, :, 16:18], want, tol, "sparse")
+
+
+def test_values_of_far_slots_and_heads(rt):
+    """Values past 32 bits of elements, told apart by head and slot so that a wrong address shows: head h's
+    are 2^h, four times that in the slots that take the attention, which lie at both ends, in the middle
+    and around the element 2^31."""
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    g = gen(18)
+    Hkv, Dh, L, block, n_sel = 9, 128, 1_900_000, 128, 20
+    cap = L + 32
+    k, v = (torch.empty(1, Hkv, cap, Dh, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert k.numel() > 2 ** 31
+    q = normal(g, "bf16", 1, 1, Hkv, Dh)
+    over = (2 ** 31 - (Hkv - 1) * cap * Dh) // Dh           # the last head's slot that holds the element 2^31
+    peaks = [0, L // 2, over - 1, over, over + 1, L - 1]
+    for h in range(Hkv):
+        k[:, h].normal_(generator=g)
+        v[:, h] = 2.0 ** h
+        # a score of 200, where the others' standard deviation is |q| / sqrt(Dh), about one
+        k[0, h, peaks] = (q[0, 0, h].float() * (200 * Dh ** 0.5 / q[0, 0, h].float().square().sum())).bfloat16()
+        v[0, h, peaks] = 4 * 2.0 ** h
+    mask = torch.ones(1, 1, 2, dtype=torch.int64, device="cuda")
+    one = i32([1])
+    means = rt.block_keys(k, i32([L]), block)
+    # the peaks' weights are equal, the others' share is nothing (1.9e6 exp(10 - 200)): the output is 4 2^h to
+    # the roundings of probabilities (2^-8) and output (2^-8); a mean score is 200 sqrt(Dh) / 128, above 17,
+    # in a peak's block and about one elsewhere, so all their blocks are chosen
+    want = 4 * 2.0 ** torch.arange(Hkv, device="cuda", dtype=torch.float64)
+    out, w = rt.tree_attn_weights(q, k, v, i32([L]), one, one, mask, cap)
+    assert torch.all((out[0, 0].double() - want[:, None]).abs() <= 2.0 ** -6 * want[:, None])
+    assert torch.all((w[0, :, peaks].double().sum(1) - 1).abs() <= 2.0 ** -10)
+    sel = torch.zeros(1, 1, Hkv, n_sel, dtype=torch.int32, device="cuda")
+    near = rt.sparse_tree_attn(q, k, v, means, i32([L]), one, one, mask, cap, block, n_sel, sel=sel)
+    assert torch.all((near[0, 0].double() - want[:, None]).abs() <= 2.0 ** -6 * want[:, None])
+    for h in range(Hkv):
+        assert {p // block for p in peaks} <= set(sel[0, 0, h].tolist())
 
 
 # ---------------------------------------------------------------------------- much work at once

@@ -281,6 +281,90 @@ def test_kv_evict_weight_orders(rt, kind):
         evict_case(rt, "bf16", 2, 3, 2000, 64, [2000, 1777], budget, 3, 20, weights=weights)
 
 
+@pytest.mark.parametrize("place", [True, False])
+def test_kv_evict_more_than_65535_pieces(rt, place):
+    """A budget of more than 65535 pieces of 128 rows, a workgroup each."""
+    print(f"evict 8.4 M slots place={place}", flush=True)
+    g = gen(13)
+    S, first, last = 65535 * 128 + 5000, 7, 11
+    budget = S - 1500
+    kc, vc = (torch.randint(-30000, 30000, (1, 1, S, 8), generator=g, device="cuda").to(torch.int16).view(torch.bfloat16)
+              for _ in range(2))
+    w = torch.rand(1, 1, S, generator=g, device="cuda")
+    k0, v0, w0 = kc.clone(), vc.clone(), w.clone()
+    outs = {} if place else dict(k_out=torch.zeros_like(kc), v_out=torch.zeros_like(kc), weights_out=torch.zeros_like(w))
+    kept, n = rt.kv_evict(kc, vc, w, i32([S]), budget, first, last, **outs)
+    ko, vo, wo = (kc, vc, w) if place else outs.values()
+    assert n.tolist() == [budget]
+    # (a stable sort keeps the lower slot first among equal weights)
+    order = torch.sort(w0[0, 0, first: S - last], descending=True, stable=True).indices[: budget - first - last] + first
+    keep = torch.zeros(S, dtype=torch.bool, device="cuda")
+    keep[order] = True
+    keep[:first] = True
+    keep[S - last:] = True
+    want = keep.nonzero().flatten()
+    assert torch.equal(kept[0, 0].long(), want)
+    for now, was in ((ko, k0), (vo, v0), (wo, w0)):
+        assert torch.equal(bits(now[0, 0, :budget]), bits(was[0, 0, want]))
+        assert torch.equal(bits(now[0, 0, budget:]), bits(was[0, 0, budget:]) if place else torch.zeros_like(bits(now[0, 0, budget:])))
+
+
+def ordered_weights(kind, g, *shape):
+    w = torch.rand(*shape, generator=g, device="cuda")
+    if kind == "ties":
+        return torch.floor(w * 5)
+    if kind == "all_equal":
+        return torch.full_like(w, 0.25)
+    if kind == "zeros_signed":
+        return torch.where(w < 0.5, torch.full_like(w, -0.0), torch.where(w < 0.9, torch.zeros_like(w), w))
+    if kind == "nonfinite":
+        x = torch.where(w < 0.6, torch.full_like(w, math.nan), w)
+        x = torch.where(w > 0.95, torch.full_like(w, math.inf), x)
+        return torch.where((w > 0.6) & (w < 0.7), torch.full_like(w, -math.inf), x)
+    if kind == "nan":
+        return torch.full_like(w, math.nan)
+    if kind == "negative":
+        return w - 0.5
+    if kind == "last_bits":
+        return 1.0 + torch.floor(w * 300) * 2.0 ** -23
+    return torch.exp(60 * (w - 0.5))                        # many exponents
+
+
+# capacities at both ends of every form of the selection, and lengths that fill its rounds or just do not
+@pytest.mark.parametrize("S,L", [(4096, [4096, 4095]), (4097, [4097, 4000]), (9000, [8999, 100]), (16384, [16384, 16383]),
+                                 (16385, [16385, 2000]), (40000, [39999, 17]), (65536, [65536, 65535]),
+                                 (65537, [65537, 65536]), (70000, [69999, 33000])])
+@pytest.mark.parametrize("kind", ["ties", "all_equal", "zeros_signed", "nonfinite", "nan", "negative", "last_bits", "exponents"])
+def test_kv_evict_weight_orders_at_every_capacity(rt, S, L, kind):
+    """The selection has a form for each range of capacities; every one meets ties, zeros, infinities and
+    NaN, with budgets of one slot, of some, of nearly all (into the NaN where there are any)."""
+    print(f"evict orders S={S} L={L} {kind}", flush=True)
+    g = gen(S + len(kind))
+    B, slices = 2, 2
+    kc, vc = (torch.randint(-30000, 30000, (B, slices, S, 8), generator=g, device="cuda").to(torch.int16).view(torch.bfloat16)
+              for _ in range(2))
+    w = ordered_weights(kind, g, B, slices, S)
+    wn = w.cpu().numpy()
+    for budget, first, last in ((1, 0, 0), (S // 3, 5, 64), (S - 1, 0, 0), (S - S // 8, 0, 7), (S // 2, 1, 0)):
+        ko, vo = (torch.zeros(B, slices, budget, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        kept, n = rt.kv_evict(kc, vc, w, i32(L), budget, first, last, k_out=ko, v_out=vo,
+                              weights_out=torch.zeros(B, slices, budget, device="cuda"))
+        assert n.tolist() == [min(l, budget) for l in L]
+        for b in range(B):
+            m = min(L[b], budget)
+            for s in range(slices):
+                want = np.arange(m)
+                if L[b] > budget:
+                    mid = wn[b, s, first: L[b] - last]
+                    # by NaN last, then the larger weight (-0 and 0 alike), then the lower slot
+                    order = np.lexsort((np.arange(mid.size), np.where(np.isnan(mid), 0, -mid), np.isnan(mid)))
+                    keep = np.concatenate([np.arange(first), np.arange(L[b] - last, L[b]), order[: budget - first - last] + first])
+                    want = np.sort(keep)
+                assert np.array_equal(kept[b, s, :m].cpu().numpy(), want), (budget, b, s)
+                at = torch.from_numpy(want).cuda()
+                assert torch.equal(bits(ko[b, s, :m]), bits(kc[b, s, at])) and torch.equal(bits(vo[b, s, :m]), bits(vc[b, s, at]))
+
+
 def test_kv_evict_length_in_place_and_layers(rt):
     """new_len is kv_len itself; the slices are those of one layer of a larger cache."""
     g = gen(10)
