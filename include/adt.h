@@ -253,7 +253,9 @@ adt_status adt_sparse_tree_attn(const void* q, const void* k_cache, const void* 
  * and slots behind stay as they are.  All in fp32, in a fixed order.
  * weights_in:  element (b, h, s) at b * stride_wb + h * stride_wh + s; NULL: none
  * weights_out: the same strides; may be weights_in
- * row_weight:  [B][nq_max] fp32 (a draft's path confidences, 0 for rows not to count); NULL: ones
+ * row_weight:  [B][nq_max] fp32 (a draft's path confidences, 0 for rows not to count); NULL: ones.
+ *   It is given before the rows are accepted or rejected: what a rejected row added to the prefix's
+ *   slots stays there
  * A row that sees no slot gives zeros and adds nothing.  out must not overlap q, which is read again
  * for the weights (ADT_E_ARG).
  * workspace: adt_tree_attn_weights_workspace_size() bytes (0 for sizes that the call refuses), 16-byte

@@ -307,9 +307,13 @@ __global__ __launch_bounds__(BS_THREADS) void block_select_kernel(BlockRows a) {
 // Score and selection in one launch for up to BC_ROWS query rows: a workgroup of 16 waves per key-value
 // head, whose 16-lane groups take a block each (a lane DH / 16 dims, the row's sum over the lanes by
 // rotations within the group), leave the keys in LDS, and whose first waves then select for a row each;
-// the rows' marks meet in LDS, so the pair's list is written without another workgroup's.  More rows
-// want every CU: one workgroup a head, by matrix products, took 21.7 us for 16 rows of 128 heads over
-// 320 blocks and 20.4 for 61 rows of 32 heads over 73, against 23.2 and 16.5 in two launches.
+// the rows' marks meet in LDS, so the pair's list is written without another workgroup's.  It saves a
+// launch where one row leaves it little to do, and breaks even at two to four: whole calls of one row over
+// 511 blocks of 8 key-value heads 19.3 us against 24.9 in two launches, of 128 heads 41 against 50, over 74
+// of 32 heads 16.9 against 21.4, over 141 of 512 heads 110 against 111; of four rows 33.4 against 33.0, 86
+// against 89, 20.9 against 22.1, 188 against 187, and over 74 of 512 heads 78 against 75.  More rows take two launches at any number of heads.
+// One launch by matrix products, a form of its own, was no gain for them all round: 21.7 us for 16 rows
+// of 128 heads over 320 blocks against 23.2 in two, but 20.4 for 61 rows of 32 heads over 73 against 16.5.
 constexpr int BC_THREADS = 1024;
 constexpr int BC_ROWS = 4;
 constexpr int BC_LDS_BYTES = 144 * 1024;

@@ -20,7 +20,11 @@
 //
 // Bound by the read of K and V, in bf16 also at 64 rows a head: one row of 32 heads over 65333 slots of 8
 // key-value heads (268 MB) 52-58 us, sixteen trees of up to 61 rows of 32 heads (398 MB) 78 us, 5.1 TB/s;
-// the chosen blocks of sixteen 16-row trees (462 MB) 98-102 us.
+// the chosen blocks of sixteen 16-row trees (462 MB) 98-102 us.  fp32 keeps up with up to 16 rows a head (one
+// row of 32 heads over 65333 slots, 535 MB, 111 us).  More rows are bound by latency: a step's loads start when
+// the products of the one before are done, at one wave per SIMD with four tiles, and each 64 rows read the keys
+// anew: 61 rows of 32 heads over 2340 slots 43 us (bf16 15), sixteen such trees 331 (78), 16-row trees over chosen
+// blocks 457 (99).
 //
 // A masked score is dropped by selection, so whatever a slot's key holds does not matter to rows
 // that do not see it.  Its value does meet their zero weight in the second product, and 0 * inf is
@@ -273,7 +277,8 @@ __device__ __forceinline__ void add_not_finite(f32x4 (&o)[X::OT], const f32x4 (&
   }
 }
 
-// (registers: outputs 16 RT DH / 64 a lane, and a step's K and V: one wave per SIMD at RT = 4)
+// (registers: outputs 16 RT DH / 64 a lane, and a step's K and V: one wave per SIMD at RT = 4, where head size
+// 128 over chosen blocks still spills 40 of them)
 template <typename T, int DH, int RT, bool SPARSE>
 __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel(CacheAttn a, Deal deal,
                                                                                 float* __restrict__ part_o,
@@ -551,7 +556,8 @@ __global__ __launch_bounds__(CA_THREADS, RT == 4 ? 1 : 2) void cache_attn_kernel
 // Many rows (more than 16) in bf16: the waves of a workgroup share the keys instead.  A stage of two
 // 32-key steps comes into LDS once, fetched by all threads into registers P stages (one or three) ahead;
 // wave w computes row tile w % TILES, for step w / TILES of the stage (KH = 2) or both (KH = 1), so a
-// wave holds one tile's outputs and the CU two or four waves per SIMD.  Rows of K and V lie in 16-byte
+// wave holds one tile's outputs and the CU two or four waves per SIMD (the four at head size 128 have 128
+// registers a lane: 6 are spilled over chosen blocks, with 65 and more rows 47, over all slots 7).  Rows of K and V lie in 16-byte
 // chunks swizzled by row, so that the operand reads (16 rows of one chunk column; 8 rows of two in the
 // transpose load) touch distinct banks.
 template <int DH>
@@ -1179,9 +1185,13 @@ struct CachePlan {
   int deep;         // stages in flight (shared)
 };
 // Splits: as many as give the workgroups that the CUs hold at once (`slots`) equal shares of the keys
-// the launch expects: the slots of the cache, or n_sel blocks and for the rows of a tree, which share
-// most of their choice, half as many again (sixteen sequences of 16 rows taking 48 blocks each, 110 in
-// all: 13 stages a split 108 us, 18 98, 24 107).  Sequences that have more take more splits.  At
+// the launch expects: the slots of the cache, or n_sel blocks, and for the rows of a tree half as many
+// again.  That half is a number that measured well, no estimate of the union of the rows' blocks, which
+// is larger and not known here (sixteen sequences of 16 rows taking 48 blocks each, 110 in all: 13 stages
+// a split 108 us, 18 98, 24 107; once, twice, two and a half times n_sel instead, whole calls over 31 blocks
+// of 64 slots of 8 key-value heads: sixteen sequences of 5 rows 82, 84, 68 us against 76, of 16 rows 126,
+// 111, 114 against 120, four of 16 rows 52, 51, 59 against 52, of 61 rows 178, 153, 144 against 159; one
+// sequence within 2.2 us).  Sequences that have more take more splits.  At
 // least three stages, or two steps for each wave, pay for a split's start and its partial results; in
 // fp32, whose products take longer and whose next step waits for them, one step does (17 rows over 300
 // slots 8.7 -> 6.8 us, over 16 of 141 blocks 45 -> 39 in all; bf16, one row over 32 of 511 blocks, 10.3

@@ -5,8 +5,11 @@
 // Two launches.  evict_select_kernel, a workgroup per slice, finds the smallest weight that stays
 // by radix selection on the weights' bits and writes the kept slots in order; evict_copy_kernel, or
 // in place evict_place_kernel, moves the rows.  Selecting is bound by one CU's passes over its slice's
-// weights (65321 of them 28 us, 2400 of each of 1024 slices 11), moving by memory: the kept rows are
-// read once and written once (1024 of 1024 slices, 1.07 GB in all, 202 us, 5.3 TB/s).
+// weights (65321 of them 28 us, 2400 of each of 1024 slices 11; more than 65536 are read anew in every pass,
+// 131000 of them 84), moving by memory: the kept rows are read once and written once (1024 of 1024 slices,
+// 1.07 GB in all, 202 us, 5.3 TB/s; in place 211).  In place few slices are bound by latency, a workgroup
+// for each 128 bytes of a slice's rows going through its rounds one by one: 8192 rows of 8 slices 54 us,
+// 13 into another cache.
 #include <algorithm>
 
 #include "../launch.h"
