@@ -269,6 +269,8 @@ extern "C" adt_status adt_kv_evict(const void* k_cache, const void* v_cache, con
                     stride16(stride_b, es) && stride16(stride_slice, es) && stride16(out_stride_b, es) &&
                     stride16(out_stride_slice, es),
                 ADT_E_SHAPE, "kv_evict: addresses and strides must be multiples of 16 bytes");
+  // (one cache for both, into another one for both, is moved twice to the same result; in place it is not)
+  ADT_CHECK_ARG(k_out != v_out || (!place && k_cache == v_cache), ADT_E_ARG, "kv_evict: one destination for keys and values");
   const EvictMove a{k_cache, v_cache, weights, stride_b * es, stride_slice * es, stride_wb, stride_ws, kv_len, kv_cap,
                     slices, budget, (int)row, k_out, v_out, weights_out, out_stride_b * es, out_stride_slice * es,
                     out_stride_wb, out_stride_ws, kept, new_len};

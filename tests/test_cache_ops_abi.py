@@ -275,3 +275,13 @@ def test_more_slices_than_a_launch(L):
     assert "slices" in abi.last_error()
     assert call(L.adt_weights_compact, WCOMPACT, B=1, slices=1 << 25, wb=far) == abi.E_SHAPE
     assert "slices" in abi.last_error()
+
+
+def test_one_destination_for_keys_and_values(L):
+    """Keys and values moved within one cache, each from where the other wrote, would lose rows."""
+    from paper_2512_21857_amd import abi
+    place = dict(wo=FAKE, osb=EVICT["sb"], oss=EVICT["ss"], owb=EVICT["wb"], ows=EVICT["ws"])
+    assert call(L.adt_kv_evict, EVICT, ko=FAKE, vo=FAKE, **place) == abi.E_ARG                  # one cache, in place
+    assert "destination" in abi.last_error()
+    assert call(L.adt_kv_evict, EVICT, v=3 * FAKE, ko=2 * FAKE, vo=2 * FAKE) == abi.E_ARG       # two into one
+    assert "destination" in abi.last_error()
