@@ -286,7 +286,7 @@ adt_status adt_weights_compact(float* weights, int32_t B, int32_t slices, int64_
  *   weights element (b, s, slot) at b * stride_wb + s * stride_ws + slot, fp32
  *   k_out, v_out, weights_out: the destination, with strides of its own; the source itself (each
  *     with the source's strides) for an eviction in place, else memory apart from it; keys and values
- *     need destinations of their own (ADT_E_ARG)
+ *     need destinations of their own (ADT_E_ARG), unless one cache for both goes to another
  *   kept:    [B][slices][budget] out, the kept slots in order (entries past the new length stay)
  *   new_len: [B] out, min(kv_len[b], budget); may be kv_len itself
  * kv_len: device, at most kv_cap (debug builds record more; the excess is not seen).  A slice is a

@@ -154,18 +154,27 @@ def _dt(t: torch.Tensor):
     return dev, dt
 
 
+def _steps(shape, strides):
+    """(stride_b, stride_h) of [B][heads][slots]...: the stride of a dimension of one is whatever the view
+    left there."""
+    sh = strides[1] if shape[1] > 1 else shape[2] * (shape[3] if len(shape) > 3 else 1)
+    return (strides[0] if shape[0] > 1 else shape[1] * sh), sh
+
+
 def _caches(k_cache: torch.Tensor, v_cache: torch.Tensor, dev: int, dtype: torch.dtype):
     """(shape, stride_b, stride_h) of caches [B][heads][slots][Dh] whose slots are contiguous rows; a
     layer of a larger cache will do."""
     shape, strides = k_cache.shape, k_cache.stride()
-    if (len(shape) != 4 or strides[3] != 1 or strides[2] != shape[3] or k_cache.dtype is not dtype
-            or k_cache.get_device() != dev or v_cache.shape != shape or v_cache.stride() != strides
-            or v_cache.dtype is not dtype or v_cache.get_device() != dev):
+    if (len(shape) != 4 or strides[3] != 1 or (strides[2] != shape[3] and shape[2] > 1) or k_cache.dtype is not dtype
+            or k_cache.get_device() != dev or v_cache.shape != shape or v_cache.dtype is not dtype
+            or v_cache.get_device() != dev
+            or (v_cache.stride() != strides
+                and (v_cache.stride(3) != 1 or (v_cache.stride(2) != shape[3] and shape[2] > 1)
+                     or _steps(shape, v_cache.stride()) != _steps(shape, strides)))):
         raise ValueError(f"two caches [B][heads][slots][Dh] of {dtype} on device {dev} with contiguous rows and one "
                          f"layout expected, not {tuple(shape)} {k_cache.dtype} with strides {strides} on {k_cache.device} and "
                          f"{tuple(v_cache.shape)} {v_cache.dtype} with strides {v_cache.stride()} on {v_cache.device}")
-    # the stride of a dimension of one is whatever the view left there
-    sh = strides[1] if shape[1] > 1 else shape[2] * shape[3]
+    sh = strides[1] if shape[1] > 1 else shape[2] * shape[3]      # (as in _steps, without its call)
     return shape, (strides[0] if shape[0] > 1 else shape[1] * sh), sh
 
 
@@ -297,12 +306,11 @@ def tree_attn_weights_workspace(B: int, H: int, Hkv: int, Dh: int, nq_max: int, 
 def _weights(what: str, w: torch.Tensor, dev: int, B: int, heads: int, slots: int):
     """(stride_b, stride_h) of weights fp32 [B][heads][>= slots] with contiguous slots."""
     shape, st = w.shape, w.stride()
-    if (len(shape) != 3 or shape[0] != B or shape[1] != heads or shape[2] < slots or st[2] != 1
+    if (len(shape) != 3 or shape[0] != B or shape[1] != heads or shape[2] < slots or (st[2] != 1 and shape[2] > 1)
             or w.dtype is not _F32 or w.get_device() != dev):
         raise ValueError(f"{what}: float32 [{B}][{heads}][{slots}] with contiguous slots on device {dev} expected, not "
                          f"{w.dtype} {tuple(shape)} with strides {st} on {w.device}")
-    sh = st[1] if heads > 1 else shape[2]
-    return (st[0] if B > 1 else heads * sh), sh
+    return _steps(shape, st)
 
 
 def tree_attn_weights(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv_len: torch.Tensor,

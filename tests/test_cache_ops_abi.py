@@ -285,3 +285,28 @@ def test_one_destination_for_keys_and_values(L):
     assert "destination" in abi.last_error()
     assert call(L.adt_kv_evict, EVICT, v=3 * FAKE, ko=2 * FAKE, vo=2 * FAKE) == abi.E_ARG       # two into one
     assert "destination" in abi.last_error()
+
+
+def test_strides_of_dimensions_of_one():
+    """A dimension of one has whatever stride its view left there: caches that differ in nothing else go
+    together, and those that differ in a stride that counts do not."""
+    import torch
+    from paper_2512_21857_amd import runtime as rt
+    f = torch.float32
+    layer = torch.zeros(1, 3, 2, 10, 64)[:, 1]                  # one sequence's layer of a larger cache
+    own = torch.zeros(1, 2, 10, 64)
+    assert layer.stride() != own.stride()
+    for k, v in ((layer, own), (own, layer)):
+        assert rt._caches(k, v, -1, f) == ((1, 2, 10, 64), 2 * 10 * 64, 10 * 64)
+    one = torch.zeros(2, 3, 64).as_strided((2, 3, 1, 64), (192, 64, 7, 1))      # one slot
+    assert rt._caches(one, torch.zeros(2, 3, 1, 64), -1, f) == ((2, 3, 1, 64), 192, 64)
+    head = torch.zeros(2, 5, 10, 64)[:, 2:3]                    # one head of several: the sequences lie apart
+    assert rt._caches(head, head, -1, f) == ((2, 1, 10, 64), 5 * 640, 640)
+    assert rt._weights("w", torch.zeros(2, 3).as_strided((2, 3, 1), (3, 1, 9)), -1, 2, 3, 1) == (3, 1)
+    for k, v in ((head, torch.zeros(2, 1, 10, 64)), (own, torch.zeros(1, 2, 10, 65)[..., :64]),
+                 (own, torch.zeros(1, 2, 64, 10).transpose(2, 3)), (own, torch.zeros(1, 2, 20, 64)[:, :, ::2]),
+                 (torch.zeros(1, 2, 10, 65)[..., :64],) * 2, (own, own.double())):
+        with pytest.raises(ValueError):
+            rt._caches(k, v, -1, f)
+    with pytest.raises(ValueError):
+        rt._weights("w", torch.zeros(2, 3, 8)[:, :, ::2], -1, 2, 3, 4)
