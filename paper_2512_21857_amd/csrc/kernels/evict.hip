@@ -58,37 +58,39 @@ constexpr int MOVE_THREADS = 256;
 constexpr int MOVE_ROWS = 128;
 constexpr int MOVE_UN = 8;
 __global__ __launch_bounds__(MOVE_THREADS) void evict_copy_kernel(EvictMove a) {
-  const int s = blockIdx.x, m0 = blockIdx.y * MOVE_ROWS, b = blockIdx.z;
+  const int s = blockIdx.x, b = blockIdx.z;
   // (min(kv_len, budget) is the same before and after new_len, which may be kv_len, is written)
   const int n = max(0, min(min(a.kv_len[b], a.kv_cap), a.budget));
-  if (s == 0 && m0 == 0 && threadIdx.x == 0) a.new_len[b] = n;
-  const int rows = min(MOVE_ROWS, n - m0);
-  if (rows <= 0) return;
+  if (s == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.new_len[b] = n;
   __shared__ int32_t from[MOVE_ROWS];
-  const int32_t* kept = a.kept + ((int64_t)b * a.slices + s) * a.budget + m0;
-  if ((int)threadIdx.x < rows) {
-    const int i = kept[threadIdx.x];
-    from[threadIdx.x] = i;
-    a.w_out[b * a.ostride_wb + s * a.ostride_ws + m0 + threadIdx.x] = a.w[b * a.stride_wb + s * a.stride_ws + i];
-  }
-  __syncthreads();
-  const int per = a.row_bytes / 16, pieces = rows * per;
+  for (int m0 = blockIdx.y * MOVE_ROWS; m0 < n; m0 += gridDim.y * MOVE_ROWS) {
+    const int rows = min(MOVE_ROWS, n - m0);
+    if (m0 >= (int)gridDim.y * MOVE_ROWS) __syncthreads();      // (the piece before has been moved)
+    const int32_t* kept = a.kept + ((int64_t)b * a.slices + s) * a.budget + m0;
+    if ((int)threadIdx.x < rows) {
+      const int i = kept[threadIdx.x];
+      from[threadIdx.x] = i;
+      a.w_out[b * a.ostride_wb + s * a.ostride_ws + m0 + threadIdx.x] = a.w[b * a.stride_wb + s * a.stride_ws + i];
+    }
+    __syncthreads();
+    const int per = a.row_bytes / 16, pieces = rows * per;
 #pragma unroll
-  for (int part = 0; part < 2; ++part) {
-    const char* src = (const char*)(part ? a.v : a.k) + b * a.stride_b + s * a.stride_s;
-    char* dst = (char*)(part ? a.v_out : a.k_out) + b * a.ostride_b + s * a.ostride_s + (int64_t)m0 * a.row_bytes;
-    for (int p0 = threadIdx.x; p0 < pieces; p0 += MOVE_THREADS * MOVE_UN) {
-      u16x8 x[MOVE_UN];
+    for (int part = 0; part < 2; ++part) {
+      const char* src = (const char*)(part ? a.v : a.k) + b * a.stride_b + s * a.stride_s;
+      char* dst = (char*)(part ? a.v_out : a.k_out) + b * a.ostride_b + s * a.ostride_s + (int64_t)m0 * a.row_bytes;
+      for (int p0 = threadIdx.x; p0 < pieces; p0 += MOVE_THREADS * MOVE_UN) {
+        u16x8 x[MOVE_UN];
 #pragma unroll
-      for (int j = 0; j < MOVE_UN; ++j) {
-        const int p = min(p0 + j * MOVE_THREADS, pieces - 1), m = p / per;
-        x[j] = __builtin_nontemporal_load(
-            reinterpret_cast<const u16x8*>(src + (int64_t)from[m] * a.row_bytes + (p - m * per) * 16));
-      }
+        for (int j = 0; j < MOVE_UN; ++j) {
+          const int p = min(p0 + j * MOVE_THREADS, pieces - 1), m = p / per;
+          x[j] = __builtin_nontemporal_load(
+              reinterpret_cast<const u16x8*>(src + (int64_t)from[m] * a.row_bytes + (p - m * per) * 16));
+        }
 #pragma unroll
-      for (int j = 0; j < MOVE_UN; ++j) {
-        const int p = p0 + j * MOVE_THREADS;
-        if (p < pieces) __builtin_nontemporal_store(x[j], reinterpret_cast<u16x8*>(dst + (int64_t)p * 16));
+        for (int j = 0; j < MOVE_UN; ++j) {
+          const int p = p0 + j * MOVE_THREADS;
+          if (p < pieces) __builtin_nontemporal_store(x[j], reinterpret_cast<u16x8*>(dst + (int64_t)p * 16));
+        }
       }
     }
   }
@@ -156,7 +158,9 @@ adt_status launch_kv_evict(const EvictMove& a, int B, int n_first, int n_last, h
   ADT_LAUNCH_CHECK();
   if (a.k_out != a.k) {
     const int most = std::min(a.kv_cap, a.budget);
-    evict_copy_kernel<<<dim3(a.slices, (most + MOVE_ROWS - 1) / MOVE_ROWS, B), MOVE_THREADS, 0, st>>>(a);
+    // (65535: the most workgroups that a launch may have in its second dimension)
+    const int pieces = std::min((most + MOVE_ROWS - 1) / MOVE_ROWS, 65535);
+    evict_copy_kernel<<<dim3(a.slices, pieces, B), MOVE_THREADS, 0, st>>>(a);
   } else if (a.row_bytes % 128 == 0) {
     evict_place_kernel<128><<<dim3(a.slices, 2 * (a.row_bytes / 128) + 1, B), PLACE_THREADS, 0, st>>>(a);
   } else {
