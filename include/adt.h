@@ -301,6 +301,92 @@ adt_status adt_kv_evict(const void* k_cache, const void* v_cache, const float* w
                         int64_t out_stride_wb, int64_t out_stride_ws, int32_t* kept, int32_t* new_len, int32_t dtype,
                         void* stream);
 
+/* ------------------------------------------------------------------ caches in eight bits
+ * A cache whose rows (one slot of one head, Dh values) are held in eight bits with one scale each:
+ *   scale = fl32(max |x| / top), top = 127 (ADT_I8) or 448 (ADT_E4M3, OCP e4m3 without infinities);
+ *   code  = the type's value nearest to fl32(x / scale), ties to even;  value = code * scale.
+ * A row of zeros has scale 0 and codes 0; a row with a value that is not finite has scale NaN and
+ * codes 0, so what attends to it comes out NaN and nothing else does.
+ * adt_kv_cache names a cache of any type; it is read during the call only.  k, v: element (b, h,
+ * slot, :) at b * stride_b + h * stride_h + slot * Dh; k_scale, v_scale: fp32, (b, h, slot) at
+ * b * scale_b + h * scale_h + slot, NULL for ADT_F32 and ADT_BF16.  stride_h >= cap * Dh and
+ * scale_h >= cap; with more than one sequence stride_b >= heads * stride_h and scale_b >= heads *
+ * scale_h (ADT_E_SHAPE).  B at most 65535, heads at most 32767, Dh even and at most 256
+ * (ADT_E_SHAPE); cap at most 2^31 - 2^24 (ADT_E_CAPACITY).  ADT_E_ARG: null pointers, an unknown
+ * type, scales missing or not meant, a size below 1; where a call writes, k and v the same. */
+#define ADT_E4M3 2
+#define ADT_I8 3
+typedef struct {
+  void *k, *v;
+  int64_t stride_b, stride_h;   /* elements */
+  float *k_scale, *v_scale;
+  int64_t scale_b, scale_h;     /* floats */
+  int32_t B, heads, cap, Dh;
+  int32_t type;                 /* ADT_F32, ADT_BF16, ADT_E4M3 or ADT_I8 */
+} adt_kv_cache;
+
+/* adt_rope_append for models that normalise queries and keys head by head, into a cache of any
+ * type, in one pass: each head's row x of q (k) becomes
+ *   y = x * g / sqrt(mean x^2 + eps),  then rotated as by adt_rope_append,
+ * g = q_norm (k_norm): fp32 [Dh], or [H][Dh] ([heads][Dh]) where norm_per_head is 1; NULL: that side
+ * is not normalised.  Values go to the cache as they are.  Keys are made in double up to their
+ * rounding into the cache, so that codes are those of the formula; queries in fp32.
+ * q, k, v, ld*, pos, kv_len, n_rows, freq, gain, rot_dim, layout, n_max, q_out as in
+ * adt_rope_append, with B, heads and Dh those of the cache; slots at or past cache->cap are left out
+ * (debug builds record it).  cache->type: dtype, or an eight-bit type.  q_out must not overlap q (but
+ * may be q itself where its rows are contiguous), k or v (ADT_E_ARG). */
+adt_status adt_norm_rope_append(const void* q, const void* k, const void* v, int64_t ldq, int64_t ldk, int64_t ldv,
+                                const float* q_norm, const float* k_norm, int32_t norm_per_head, float eps,
+                                const int32_t* pos, const int32_t* kv_len, const int32_t* n_rows, const double* freq,
+                                float gain, int32_t rot_dim, int32_t layout, int32_t n_max, int32_t H, int32_t dtype,
+                                void* q_out, const adt_kv_cache* cache /*[host]*/, void* stream);
+
+/* Slots from a cache of eight bits to a plain one (read back: value = code * scale, rounded once) or
+ * from a plain cache to one of eight bits: of every head, slot src_start[b] + i to slot dst_start[b] +
+ * i, i < length[b]; n_max bounds length (host).  Starts NULL: 0.  Other slots stay as they are; slots
+ * outside either cache are left out (debug builds record it).  Exactly one of the two is eight-bit
+ * (ADT_E_UNSUPPORTED); equal B, heads and Dh (ADT_E_SHAPE); the two must not overlap (ADT_E_ARG). */
+adt_status adt_cache_convert(const adt_kv_cache* src /*[host]*/, const adt_kv_cache* dst /*[host]*/,
+                             const int32_t* length, int32_t n_max, const int32_t* src_start, const int32_t* dst_start,
+                             void* stream);
+
+/* adt_kv_compact of a cache of any type, codes and scales: in every slice, slot kv_len[b] + m <- slot
+ * kv_len[b] + path[b][m] for m = 1..n_acc[b].  Arguments as there (a slice is a head of the cache);
+ * slots outside the cache are left alone.  Rows are whole 16-byte pieces, addresses and strides
+ * multiples of 16 bytes (ADT_E_SHAPE). */
+adt_status adt_cache_compact(const adt_kv_cache* cache /*[host]*/, const int32_t* kv_len, const int32_t* path,
+                             int32_t path_stride, const int32_t* n_acc, int32_t a_max, void* stream);
+
+/* Tree attention over a cache of any type, and behind a prefix that sequences share: H query heads
+ * over cache->heads key-value heads (head h reads key-value head h / (H / heads)).
+ *   out = softmax(scale * q . K) V over the slots [0, prefix_len[j]) of the shared prefix, the slots
+ *     [0, kv_len[b]) of the sequence's own cache, and its tail slots kv_len[b] + t, t < n_tail[b],
+ *     whose bit t is set in anc_mask[b][i].
+ * prefix: NULL (none), or a cache of the same type, heads and Dh whose prefix->B groups divide
+ *   cache->B: sequence b belongs to group j = b / (cache->B / prefix->B), consecutive sequences
+ *   sharing one prefix, whose keys and values are read and computed once for all rows of the group.
+ *   prefix_len: [prefix->B] device, at most prefix_cap; at most 4096 sequences a group
+ *   (ADT_E_CAPACITY).  The prefix and the own caches may lie in one allocation.
+ * kv_cap <= cache->cap and prefix_cap <= prefix->cap: host bounds of kv_len[b] + n_tail[b] and of
+ *   prefix_len, by which the launch is sized (debug builds record more; the excess is not seen).
+ * q, out: [B][nq_max][H][Dh] in dtype; other arguments as in adt_tree_attn.  Rows i < n_q[b] are
+ *   computed, others stay as they are; a row that sees no slot gives zeros.  out may be q itself
+ *   (ADT_E_ARG where they overlap otherwise).
+ * dtype ADT_BF16: cache type ADT_BF16, ADT_E4M3 or ADT_I8; ADT_F32: ADT_F32 (else ADT_E_UNSUPPORTED).
+ *   bf16 multiplies codes as they are (bf16 holds them exactly) and applies the scales to scores and
+ *   probabilities in fp32; softmax sums and outputs are fp32.
+ * workspace: adt_cache_tree_attn_workspace_size() bytes (groups = 0: no prefix; 0 where none is
+ *   needed, and for sizes that the call refuses), 16-byte aligned.  Dh 64 or 128, H a multiple of heads, B * heads <= 65535,
+ *   addresses and cache strides multiples of 16 bytes (ADT_E_SHAPE); nq_max <= ADT_MAX_NODES,
+ *   nq_max * H / heads <= 8192, workspace (ADT_E_CAPACITY). */
+size_t adt_cache_tree_attn_workspace_size(int32_t B, int32_t H, int32_t heads, int32_t Dh, int32_t nq_max,
+                                          int32_t kv_cap, int32_t groups, int32_t prefix_cap, int32_t type);
+adt_status adt_cache_tree_attn(const void* q, const adt_kv_cache* cache /*[host]*/, const int32_t* kv_len,
+                               const int32_t* n_q, const int32_t* n_tail, const uint64_t* anc_mask, int32_t H,
+                               int32_t nq_max, int32_t kv_cap, const adt_kv_cache* prefix /*[host]*/,
+                               const int32_t* prefix_len, int32_t prefix_cap, float scale, int32_t dtype, void* out,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------ c1-c3: acceptance
  * Walk from the root of one verified tree (Sec. 3.1 Eq. 1; Sec. 5.1).
  *  GREEDY: t_u = argmax of logits row u over its allowed ids (lowest id on ties); move to

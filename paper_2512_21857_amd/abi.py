@@ -15,7 +15,7 @@ DEBUG_LIB_PATH = os.path.join(PKG, "libadt_debug.so")   # device invariant check
 
 OK = 0
 E_ARG, E_SHAPE, E_CAPACITY, E_HIP, E_UNSUPPORTED, E_DEVICE_INVARIANT, E_STATE = -1, -2, -3, -4, -5, -6, -7
-F32, BF16 = 0, 1
+F32, BF16, E4M3, I8 = 0, 1, 2, 3
 MAX_NODES = 128
 MASK_WORDS = 2
 ACCEPT_GREEDY, ACCEPT_EXACT, ACCEPT_RELAXED, ACCEPT_MSS = 0, 1, 2, 3
@@ -92,6 +92,11 @@ class RopeCfg(C.Structure):
                 ("slow", f64)]
 
 
+class KvCache(C.Structure):
+    _fields_ = [("k", p), ("v", p), ("stride_b", i64), ("stride_h", i64), ("k_scale", p), ("v_scale", p),
+                ("scale_b", i64), ("scale_h", i64), ("B", i32), ("heads", i32), ("cap", i32), ("Dh", i32), ("type", i32)]
+
+
 _SIGS = {
     "adt_version": (i32, []),
     "adt_device_checks_enabled": (i32, []),
@@ -115,6 +120,12 @@ _SIGS = {
     "adt_kv_evict": (i32, [p, p, p, i64, i64, i64, i64, p, i32, i32, i32, i32, i32, i32, i32, p, p, p, i64, i64, i64, i64,
                            p, p, i32, p]),
     "adt_weights_compact": (i32, [p, i32, i32, i64, i64, p, i32, p, i32, p, i32, p]),
+    "adt_norm_rope_append": (i32, [p, p, p, i64, i64, i64, p, p, i32, f32, p, p, p, p, f32, i32, i32, i32, i32, i32, p, p,
+                                   p]),
+    "adt_cache_convert": (i32, [p, p, p, i32, p, p, p]),
+    "adt_cache_compact": (i32, [p, p, p, i32, p, i32, p]),
+    "adt_cache_tree_attn_workspace_size": (sz, [i32] * 9),
+    "adt_cache_tree_attn": (i32, [p, p, p, p, p, p, i32, i32, i32, p, p, i32, f32, i32, p, p, sz, p]),
     "adt_accept_workspace_size": (sz, [i32]),
     "adt_verify_accept": (i32, [p, i64, i32, p, p, p, p, i32, C.POINTER(AcceptCfg), u64, p, p, p, p, sz, p]),
     "adt_codebook_knn_workspace_size": (sz, [i32]),

@@ -34,6 +34,9 @@ SOURCES = [
     "kernels/cache_attn.hip",
     "kernels/evict.hip",
     "api_cache.hip",
+    "kernels/kv_rows.hip",
+    "kernels/kv_attn.hip",
+    "api_kv.hip",
 ]
 
 # Packed fp32 VALU instructions are disabled for the device code.

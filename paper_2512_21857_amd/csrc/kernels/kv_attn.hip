@@ -1,0 +1,747 @@
+// Tree attention over caches of any type, and behind a prefix that groups of sequences share.
+//
+// A row's context has up to two parts: the prefix of its group and the cache of its sequence.  Softmax
+// over both is the merge of softmax over each: a part gives the row's maximum m, sum l and
+// unnormalised output o, and
+//   out = sum of 2^(m_i - M) o_i / sum of 2^(m_i - M) l_i,  M the largest m_i.
+// So a group's prefix is one attention of all the group's rows, wherever their trees are, over keys
+// that are read once for 128 of them; a sequence's own slots are another, with the tree's mask.  Both
+// are jobs of one launch: (part, group or sequence, key-value head, block of rows, range of keys).
+// Their results meet in a second launch, always in one order; where a row's keys are all in one job,
+// that job writes the output.
+//
+// Eight-bit keys are codes kc with a scale each, so  q . k = scale (q . kc),  p v = (p scale) vc:  bf16
+// holds every code exactly, the products take codes as they are, and the scales meet scores and
+// probabilities in fp32.
+#include <algorithm>
+
+#include "../eight_bit.h"
+#include "../launch.h"
+
+namespace adt {
+
+ADT_DEVICE_ERROR_WORD(kv_attn)
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int KA_WAVES = 4;
+constexpr int KA_THREADS = KA_WAVES * WAVE;
+constexpr int KA_UNIT = 64;       // keys that a workgroup takes at a time, and that splits are counted in
+
+// How a launch covers rows and keys.  A workgroup holds `tiles` tiles of 32 rows (fp32: one).
+struct KvSide {
+  int tiles, blocks;              // tiles of a workgroup; workgroups side by side for one head's rows
+  int splits, per;                // of the keys; units of a split at least
+};
+struct KvPlan {
+  KvSide own, pre;
+  int64_t pre_jobs, jobs;         // the first pre_jobs take prefixes
+  int parts;                      // partial results a row may have: own splits, then the prefix's
+};
+
+// A job's keys: slots [0, L) and the tail [L, total) of a part, in steps of KT keys that do not straddle
+// L, and how many splits share them.
+struct Reach {
+  int L, total, prefix_steps, steps, units, live;
+};
+template <int KT>
+__device__ __forceinline__ Reach reach_of(int len, int n_tail, int cap, const KvSide& side, int least) {
+  Reach r;
+  r.L = max(0, min(len, cap));
+  r.total = (int)min((int64_t)r.L + max(0, min(n_tail, ADT_MAX_NODES)), (int64_t)cap);
+  r.prefix_steps = (r.L + KT - 1) / KT;
+  r.steps = r.prefix_steps + (r.total - r.L + KT - 1) / KT;
+  r.units = (r.steps + KA_UNIT / KT - 1) / (KA_UNIT / KT);
+  r.live = max(least, min(side.splits, (r.units + side.per - 1) / side.per));
+  return r;
+}
+template <int KT>
+__device__ __forceinline__ Reach own_reach(const KvAttn& a, const KvPlan& p, int b) {
+  return reach_of<KT>(a.own.len[b], a.n_tail[b], a.own.cap, p.own, 1);
+}
+template <int KT>
+__device__ __forceinline__ Reach pre_reach(const KvAttn& a, const KvPlan& p, int b) {
+  if (!a.groups) return Reach{};
+  return reach_of<KT>(a.pre.len[b / a.group], 0, a.pre.cap, p.pre, 0);
+}
+__device__ __forceinline__ int rows_of(const KvAttn& a, int b) { return max(0, min(a.n_q[b], a.nq_max)) * a.G; }
+
+// What a workgroup does: rows [r0, ...) of the job's `live` rows, split sp of `reach`.
+struct Job {
+  bool pre;
+  int b, h, r0, live, sp;         // b: sequence, or first sequence of the group
+  Reach reach;
+  const KvPart* part;
+  int64_t cache;                  // sequence or group
+};
+// first: LDS [group + 1], filled with the rows before each sequence of a group (prefix jobs only).
+// false: nothing to do.  Ends with a barrier where it is a prefix job.
+template <int KT>
+__device__ __forceinline__ bool take_job(const KvAttn& a, const KvPlan& p, int rows_each, int* first, Job& j) {
+  int64_t id = blockIdx.x;
+  j.pre = id < p.pre_jobs;
+  if (!j.pre) id -= p.pre_jobs;
+  const KvSide& side = j.pre ? p.pre : p.own;
+  j.h = id % a.Hkv;
+  id /= a.Hkv;
+  const int block = id % side.blocks;
+  id /= side.blocks;
+  j.sp = id % side.splits;
+  const int at = id / side.splits;
+  j.cache = at;
+  j.part = j.pre ? &a.pre : &a.own;
+  j.r0 = block * rows_each;
+  if (!j.pre) {
+    j.b = at;
+    j.live = rows_of(a, at);
+    if (j.r0 >= j.live) return false;
+    j.reach = own_reach<KT>(a, p, at);
+    if (threadIdx.x == 0 && (int64_t)a.own.len[at] + a.n_tail[at] > a.own.cap) dev_fail(DEVINV_KV_RANGE);
+    return j.sp < j.reach.live;
+  }
+  j.b = at * a.group;
+  j.reach = pre_reach<KT>(a, p, j.b);
+  if (threadIdx.x == 0 && a.pre.len[at] > a.pre.cap) dev_fail(DEVINV_KV_RANGE);
+  if (j.sp >= j.reach.live) return false;
+  if (threadIdx.x < WAVE) {
+    uint32_t before = 0;
+    if (threadIdx.x == 0) first[0] = 0;
+    for (int s = 0; s < a.group; s += WAVE) {
+      const int i = s + threadIdx.x;
+      const uint32_t upto = before + wave_prefix_sum(i < a.group ? (uint32_t)rows_of(a, j.b + i) : 0u);
+      if (i < a.group) first[i + 1] = (int)upto;
+      before = __shfl(upto, WAVE - 1, WAVE);
+    }
+  }
+  __syncthreads();
+  j.live = first[a.group];
+  return j.r0 < j.live;
+}
+// A job's row: sequence, node and head of the group; its query and its place among the sequence's rows.
+struct RowAt {
+  int b, node, u;
+  __device__ __forceinline__ int64_t q(const KvAttn& a, int h) const {
+    return ((((int64_t)b * a.nq_max + node) * a.Hkv + h) * a.G + u) * a.Dh;
+  }
+  // its partial result of split `sp`, in rows
+  __device__ __forceinline__ int64_t part(const KvAttn& a, const KvPlan& p, int h, int sp) const {
+    return (((int64_t)b * a.Hkv + h) * p.parts + sp) * ((int64_t)a.nq_max * a.G) + node * a.G + u;
+  }
+};
+__device__ __forceinline__ RowAt row_at(const KvAttn& a, const Job& j, int row, const int* first) {
+  int s = 0;
+  if (j.pre) {
+    int hi = a.group;
+    while (hi - s > 1) {
+      const int mid = (s + hi) / 2;
+      if (first[mid] <= row) s = mid;
+      else hi = mid;
+    }
+    row -= first[s];
+  }
+  return RowAt{j.b + s, row / a.G, row % a.G};
+}
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
+
+// A row's running maximum (log2 domain) and this lane's share of its sum.  step: the new maximum's
+// bound for this step's scores; returns the factor of what was summed before.
+struct Softmax {
+  float m = -INFINITY, l = 0.f;
+  __device__ __forceinline__ float raise(float mx, float& m_use) {
+    const float m_new = fmaxf(m, mx);
+    m_use = m_new == -INFINITY ? 0.f : m_new;       // nothing seen yet: weights 0, not NaN
+    const float alpha = m_new == m ? 1.f : exp2_hw(m - m_use);
+    m = m_new;
+    return alpha;
+  }
+};
+// What a part (m, l) weighs beside a maximum M of all parts; one that saw nothing weighs 0.
+__device__ __forceinline__ float part_weight(float m, float l, float M) {
+  return m == -INFINITY && l == 0.f ? 0.f : exp2_hw(m - (M == -INFINITY ? 0.f : M));
+}
+
+// ---------------------------------------------------------------------------- bf16 rows
+// A unit of 64 keys, K and V, comes into LDS once for the workgroup (eight bits turned into bf16 on the
+// way), the next one on its way into registers meanwhile.  A wave takes one tile of 32 rows through both
+// 32-key steps of a unit, or, where the job has two tiles only, through one of them:
+//   S^T[key][row] = K Q^T  (32 x 32 x 16 MFMA; lane (r, s) = (lane % 32, lane / 32) holds row r's scores of
+//                           keys 8 c + 4 s + e, c and e < 4),
+//   O^T[dim][row] += V^T P^T  (V by transpose loads, its keys in the order in which the lanes hold P).
+// A row's scores lie in two lanes, so its maximum takes one exchange; 32 rows a wave halve the LDS reads
+// that 16 would need, which are as long as the products.  Rows of K and V lie in 16-byte chunks swizzled
+// by row, so that the operand reads touch distinct banks.
+template <int DH>
+__device__ __forceinline__ int swz_k(int row) { return DH == 128 ? (row & 15) : ((row >> 1) & 7); }
+template <int DH>
+__device__ __forceinline__ int swz_v(int row) { return DH == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
+
+template <typename C, int DH>
+__global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan p, float* __restrict__ part_o,
+                                                               float* __restrict__ part_ml) {
+  constexpr int KT = 32, KS = DH / 16, OT = DH / 32;
+  constexpr int EPL = 16 / (int)sizeof(C), CPL = DH / EPL;         // elements of a load, loads of a row
+  constexpr int LOADS = KA_UNIT * CPL / KA_THREADS;
+  constexpr int BYTES = KA_UNIT * DH * 2;                          // a unit of K or of V in LDS
+  constexpr bool CODES = EIGHT<C>;
+  static_assert(2 * (OT * 16 + 2) * WAVE * 4 <= 4 * BYTES, "merge area");
+  __shared__ __attribute__((aligned(16))) unsigned char smem[4 * BYTES];    // [buffer][K, V]
+  __shared__ float scales[2][2][CODES ? KA_UNIT : 1];              // [buffer][K, V][key]
+  extern __shared__ int first[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
+  const int r = lane & 31, s = lane >> 5;
+  Job j;
+  const int tiles = (int64_t)blockIdx.x < p.pre_jobs ? p.pre.tiles : p.own.tiles;
+  if (!take_job<KT>(a, p, 32 * tiles, first, j)) return;
+  const int tile = wave % tiles, kpart = wave / tiles, KH = KA_WAVES / tiles;
+  const int L = j.reach.L, total = j.reach.total, steps = j.reach.steps, n_live = j.reach.live;
+  const int units = max(0, (j.reach.units - j.sp + n_live - 1) / n_live);   // of this split: sp, sp + n_live, ...
+  const KvPart& part = *j.part;
+  const C* kb = (const C*)part.k + j.cache * part.sb + j.h * part.sh;
+  const C* vb = (const C*)part.v + j.cache * part.sb + j.h * part.sh;
+  const float* ksb = CODES ? part.ks + j.cache * part.ssb + j.h * part.ssh : nullptr;
+  const float* vsb = CODES ? part.vs + j.cache * part.ssb + j.h * part.ssh : nullptr;
+  const float scale_log2 = a.scale * LOG2E;
+
+  bf16x8 q[KS];
+  uint64_t aw0 = 0, aw1 = 0;
+  const int row = j.r0 + tile * 32 + r;
+  const bool mine = row < j.live, tile_live = j.r0 + tile * 32 < j.live;
+  RowAt at{j.b, 0, 0};
+  if (mine) at = row_at(a, j, row, first);
+#pragma unroll
+  for (int i = 0; i < KS; ++i) q[i] = bf16x8{};
+  if (mine) {
+    const uint16_t* src = (const uint16_t*)a.q + at.q(a, j.h) + s * 8;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) q[i] = *reinterpret_cast<const bf16x8*>(src + i * 16);
+    if (!j.pre) {
+      const uint64_t* mp = a.mask + ((int64_t)at.b * a.nq_max + at.node) * ADT_MASK_WORDS;
+      aw0 = mp[0];
+      aw1 = mp[1];
+    }
+  }
+
+  // The two steps of a unit: first key and last (a step past the end has none: last < key0).
+  struct Span {
+    int key0, last;
+  };
+  auto span = [&](int st) {
+    if (st >= steps) return Span{0, -1};
+    if (st >= j.reach.prefix_steps) return Span{L + (st - j.reach.prefix_steps) * KT, total - 1};
+    return Span{st * KT, L - 1};
+  };
+  // Load x of a unit takes row x / CPL, elements (x % CPL) * EPL..; thread t takes loads i * 256 + t.  Rows
+  // past a step's last key read that one, or the head's first row, and are stored as zeros.
+  u16x8 kr[LOADS], vr[LOADS];
+  float sc = 0.f;
+  Span now[2], next[2];
+  auto fetch = [&](int i) {
+    const int st = i < units ? 2 * (j.sp + n_live * i) : steps;
+    next[0] = span(st);
+    next[1] = span(st + 1);
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
+      const Span& w = rx < KT ? next[0] : next[1];
+      const int key = max(0, min(w.key0 + rx % KT, w.last));
+      kr[u] = *reinterpret_cast<const u16x8*>(kb + (int64_t)key * DH + c * EPL);
+      vr[u] = *reinterpret_cast<const u16x8*>(vb + (int64_t)key * DH + c * EPL);
+    }
+    if (CODES && tid < 2 * KA_UNIT) {
+      const int rx = tid % KA_UNIT;
+      const Span& w = rx < KT ? next[0] : next[1];
+      const int key = w.key0 + rx % KT;
+      sc = 0.f;
+      if (key <= w.last) sc = tid < KA_UNIT ? ksb[key] * scale_log2 : vsb[key];
+    }
+  };
+  auto put = [&](unsigned char* at, int rx, int c, int swz, u16x8 v) {
+    if constexpr (CODES) {
+      const uint4 w = __builtin_bit_cast(uint4, v);
+      const u16x4 d0 = decode4_bf16<C>(w.x), d1 = decode4_bf16<C>(w.y), d2 = decode4_bf16<C>(w.z), d3 = decode4_bf16<C>(w.w);
+      unsigned char* row = at + rx * DH * 2;
+      *reinterpret_cast<u16x8*>(row + ((2 * c) ^ swz) * 16) = u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+      *reinterpret_cast<u16x8*>(row + ((2 * c + 1) ^ swz) * 16) = u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]};
+    } else {
+      *reinterpret_cast<u16x8*>(at + rx * DH * 2 + (c ^ swz) * 16) = v;
+    }
+  };
+  auto store = [&](int buf) {
+    unsigned char* to = smem + buf * 2 * BYTES;
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
+      const Span& w = rx < KT ? next[0] : next[1];
+      put(to, rx, c, swz_k<DH>(rx), kr[u]);
+      put(to + BYTES, rx, c, swz_v<DH>(rx), w.key0 + rx % KT <= w.last ? vr[u] : u16x8{});
+    }
+    if (CODES && tid < 2 * KA_UNIT) scales[buf][tid / KA_UNIT][tid % KA_UNIT] = sc;
+  };
+
+  f32x16 o[OT];
+  Softmax sm;
+#pragma unroll
+  for (int d = 0; d < OT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+
+  // step w of the unit in buffer `buf`
+  auto compute = [&](int buf, int st, int w) {
+    const unsigned char* ks = smem + buf * 2 * BYTES;
+    const unsigned char* vs = ks + BYTES;
+    const int k0 = now[w].key0, k_last = now[w].last;
+    const bool tail = st >= j.reach.prefix_steps;
+    f32x16 x;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = 0.f;
+    const int kx = w * KT + r;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const bf16x8 f = *reinterpret_cast<const bf16x8*>(ks + kx * DH * 2 + ((2 * i + s) ^ swz_k<DH>(kx)) * 16);
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[i], x, 0, 0, 0);
+    }
+    auto key_of = [&](int e) { return 8 * (e / 4) + 4 * s + e % 4; };
+    auto sees = [&](int key) {        // key of the step
+      const int t = k0 + key - L;
+      return (k0 + key <= k_last) & (!tail | (bool)((t < 64 ? aw0 : aw1) >> (t & 63) & 1));
+    };
+    if constexpr (CODES) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const f32x4 f = *reinterpret_cast<const f32x4*>(&scales[buf][0][w * KT + 8 * c + 4 * s]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * c + e] *= f[e];
+      }
+    }
+    const bool whole = !tail && k0 + KT - 1 <= k_last;
+    if (!whole) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = sees(key_of(e)) ? x[e] : -INFINITY;
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
+    mx = xor32_max(mx);
+    float m_use;
+    const float alpha = sm.raise(CODES ? mx : mx * scale_log2, m_use);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      x[e] = exp2_hw(CODES ? x[e] - m_use : fmaf(x[e], scale_log2, -m_use));
+      sum += x[e];
+    }
+    sm.l = sm.l * alpha + sum;
+    if (!__all(alpha == 1.f)) {
+#pragma unroll
+      for (int d = 0; d < OT; ++d) o[d] *= alpha;
+    }
+    if constexpr (CODES) {
+      // (a slot the row does not see may have any scale)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const f32x4 f = *reinterpret_cast<const f32x4*>(&scales[buf][1][w * KT + 8 * c + 4 * s]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * c + e] = !tail || sees(8 * c + 4 * s + e) ? x[4 * c + e] * f[e] : 0.f;
+      }
+    }
+    bf16x8 pb[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) pb[e / 8][e % 8] = (__bf16)x[e];
+    // lane i of a 16-lane group that addresses row k0 + i / 4, dims d0 + 4 (i % 4)..+3 gets V[k0 + 0..3][d0 + i]
+    const int i16 = lane & 15, hi16 = (lane >> 4) & 1;
+    bool odd = false;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int lo = w * KT + 16 * c + 4 * s + (i16 >> 2), hi = lo + 8;
+#pragma unroll
+      for (int d = 0; d < OT; ++d) {
+        const int ch = 4 * d + 2 * hi16 + ((i16 & 3) >> 1), half = (i16 & 1) * 8;
+        v4i16 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + lo * DH * 2 + (ch ^ swz_v<DH>(lo)) * 16 + half));
+        v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + hi * DH * 2 + (ch ^ swz_v<DH>(hi)) * 16 + half));
+        if (tail) {
+          // a value that is not finite may only meet the rows that see it: it is taken out here
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if ((x0[e] & 0x7f80) == 0x7f80) x0[e] = 0, odd = true;
+            if ((x1[e] & 0x7f80) == 0x7f80) x1[e] = 0, odd = true;
+          }
+        }
+        const bf16x8 f = __builtin_bit_cast(bf16x8, v8i16{x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]});
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[c], o[d], 0, 0, 0);
+      }
+    }
+    if (tail && __any(odd)) {
+      // and added here
+      for (int key = 0; key < KT; ++key) {
+        float have = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) have = e == key / 8 * 4 + key % 4 ? x[e] : have;
+        const float pk = __shfl(have, r + 32 * (key / 4 & 1), WAVE);
+        const bool vis = sees(key);
+        const int vx = w * KT + key;
+#pragma unroll
+        for (int d = 0; d < OT; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int dim = 32 * d + 8 * (e / 4) + 4 * s + e % 4;
+            const float v = bf2f(*reinterpret_cast<const uint16_t*>(vs + vx * DH * 2 + ((dim / 8) ^ swz_v<DH>(vx)) * 16 + dim % 8 * 2));
+            if (vis && not_finite(v)) o[d][e] += pk * v;
+          }
+      }
+    }
+  };
+
+  fetch(0);
+  for (int i = 0; i < units; ++i) {
+    // the buffer written here was last read two units ago, before the previous barrier
+    store(i & 1);
+    now[0] = next[0];
+    now[1] = next[1];
+    __syncthreads();
+    fetch(i + 1);
+    if (!tile_live) continue;
+    const int st = 2 * (j.sp + n_live * i);
+    for (int w = kpart; w < 2; w += KH)
+      if (st + w < steps) compute(i & 1, st + w, w);
+  }
+
+  sm.l = xor32_add(sm.l);
+  if (KH > 1) {
+    // the second wave of a tile passes its state through LDS to the first
+    float* mo = reinterpret_cast<float*>(smem) + (size_t)tile * (OT * 16 + 2) * WAVE;
+    __syncthreads();
+    if (kpart == 1) {
+#pragma unroll
+      for (int d = 0; d < OT; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mo[(d * 16 + e) * WAVE + lane] = o[d][e];
+      mo[OT * 16 * WAVE + lane] = sm.m;
+      mo[(OT * 16 + 1) * WAVE + lane] = sm.l;
+    }
+    __syncthreads();
+    if (kpart == 1) return;
+    const float m1 = mo[OT * 16 * WAVE + lane], l1 = mo[(OT * 16 + 1) * WAVE + lane], M = fmaxf(sm.m, m1);
+    const float w0 = part_weight(sm.m, sm.l, M), w1 = part_weight(m1, l1, M);
+    // (a part of weight 0 adds nothing, whatever it holds; unless its sum is NaN)
+#pragma unroll
+    for (int d = 0; d < OT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float y = mo[(d * 16 + e) * WAVE + lane];
+        o[d][e] = (w0 == 0.f ? 0.f : o[d][e] * w0) + (w1 == 0.f ? 0.f : y * w1);
+      }
+    sm.l = (w0 == 0.f && sm.l == sm.l ? 0.f : sm.l * w0) + (w1 == 0.f && l1 == l1 ? 0.f : l1 * w1);
+    sm.m = M;
+  }
+  if (!mine) return;
+  if (!j.pre && n_live == 1 && pre_reach<KT>(a, p, at.b).live == 0) {
+    const float inv = sm.l == 0.f ? 0.f : 1.f / sm.l;
+    uint16_t* to = (uint16_t*)a.out + at.q(a, j.h);
+#pragma unroll
+    for (int d = 0; d < OT; ++d)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        store4(to + 32 * d + 8 * c + 4 * s, o[d][4 * c] * inv, o[d][4 * c + 1] * inv, o[d][4 * c + 2] * inv, o[d][4 * c + 3] * inv);
+    return;
+  }
+  const int64_t to = at.part(a, p, j.h, j.pre ? p.own.splits + j.sp : j.sp);
+#pragma unroll
+  for (int d = 0; d < OT; ++d)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<f32x4*>(part_o + to * DH + 32 * d + 8 * c + 4 * s) =
+          f32x4{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
+  if (s == 0) *reinterpret_cast<float2*>(part_ml + to * 2) = make_float2(sm.m, sm.l);
+}
+
+// ---------------------------------------------------------------------------- fp32 rows
+// 32 rows a workgroup, in two tiles of 16; the waves take 16 keys of a unit each, straight from memory,
+// on the 16x16x4 MFMA (lane (l, g) = (lane % 16, lane / 16) holds row l's scores of keys 4 g + e), and
+// merge in LDS.
+template <int DH>
+__global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, KvPlan p, float* __restrict__ part_o,
+                                                                   float* __restrict__ part_ml) {
+  constexpr int KT = 16, RT = 2, OT = DH / 16, MP = DH + 4;
+  __shared__ __attribute__((aligned(16))) float mo[KA_WAVES * 16 * MP];     // [wave][16][MP]
+  __shared__ float mml[KA_WAVES * 16 * 2];
+  extern __shared__ int first[];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
+  const int l = lane & 15, g = lane >> 4;
+  Job j;
+  if (!take_job<KT>(a, p, 16 * RT, first, j)) return;
+  const int L = j.reach.L, total = j.reach.total, steps = j.reach.steps, n_live = j.reach.live;
+  const KvPart& part = *j.part;
+  const float* kb = (const float*)part.k + j.cache * part.sb + j.h * part.sh;
+  const float* vb = (const float*)part.v + j.cache * part.sb + j.h * part.sh;
+  const float scale_log2 = a.scale * LOG2E;
+
+  f32x4 q[RT][DH / 16];
+  uint64_t aw0[RT], aw1[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    aw0[t] = aw1[t] = 0;
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) q[t][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = j.r0 + t * 16 + l;
+    if (row >= j.live) continue;
+    const RowAt at = row_at(a, j, row, first);
+    const float* src = (const float*)a.q + at.q(a, j.h) + g * 4;
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) q[t][i] = *reinterpret_cast<const f32x4*>(src + i * 16);
+    if (!j.pre) {
+      const uint64_t* mp = a.mask + ((int64_t)at.b * a.nq_max + at.node) * ADT_MASK_WORDS;
+      aw0[t] = mp[0];
+      aw1[t] = mp[1];
+    }
+  }
+  f32x4 o[RT][OT];
+  Softmax sm[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int d = 0; d < OT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (int unit = j.sp; unit < j.reach.units; unit += n_live) {
+    const int st = unit * (KA_UNIT / KT) + wave;
+    if (st >= steps) break;
+    const bool tail = st >= j.reach.prefix_steps;
+    const int k0 = tail ? L + (st - j.reach.prefix_steps) * KT : st * KT, k_last = (tail ? total : L) - 1;
+    f32x4 k[DH / 16], v[4][DH / 64];
+    {
+      const float* src = kb + (int64_t)min(k0 + l, k_last) * DH + g * 4;
+#pragma unroll
+      for (int i = 0; i < DH / 16; ++i) k[i] = *reinterpret_cast<const f32x4*>(src + i * 16);
+    }
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int key = k0 + 4 * g + e;
+      const float* src = vb + (int64_t)min(key, k_last) * DH + 4 * l;
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c) {
+        v[e][c] = *reinterpret_cast<const f32x4*>(src + c * 64);
+        if (key > k_last) v[e][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (tail) {
+          // a value that is not finite may only meet the rows that see it: it is taken out here, added below
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (not_finite(v[e][c][i])) v[e][c][i] = 0.f, odd = true;
+        }
+      }
+    }
+    odd = __any(odd);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      f32x4 x{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < DH / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q[t][i][e], x, 0, 0, 0);
+      auto sees = [&](int key) {
+        const int n = k0 + key - L;
+        return (k0 + key <= k_last) & (!tail | (bool)((n < 64 ? aw0[t] : aw1[t]) >> (n & 63) & 1));
+      };
+      float mx = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = sees(4 * g + e) ? x[e] : -INFINITY;
+        mx = fmaxf(mx, x[e]);
+      }
+      mx = xor32_max(xor16_max(mx));
+      float m_use;
+      const float alpha = sm[t].raise(mx * scale_log2, m_use);
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = exp2_hw(fmaf(x[e], scale_log2, -m_use));
+        sum += x[e];
+      }
+      sm[t].l = sm[t].l * alpha + sum;
+      if (!__all(alpha == 1.f)) {
+#pragma unroll
+        for (int d = 0; d < OT; ++d) o[t][d] *= alpha;
+      }
+      // output tile 4 c + i takes the dims 64 c + 4 m + i of its rows m
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int d = 0; d < OT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][d / 4][d % 4], x[e], o[t][d], 0, 0, 0);
+      if (odd) {
+        for (int key = 0; key < KT; ++key) {
+          float have = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) have = key % 4 == e ? x[e] : have;
+          const float pk = __shfl(have, l + 16 * (key / 4), WAVE);
+          const bool vis = sees(key);
+          const float* src = vb + (int64_t)min(k0 + key, k_last) * DH;
+#pragma unroll
+          for (int d = 0; d < OT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float f = src[d / 4 * 64 + 16 * g + 4 * e + d % 4];
+              if (vis && not_finite(f)) o[t][d][e] += pk * f;
+            }
+        }
+      }
+    }
+  }
+
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    sm[t].l = xor32_add(xor16_add(sm[t].l));
+    __syncthreads();
+    float* mine = mo + (wave * 16 + l) * MP;
+#pragma unroll
+    for (int d = 0; d < OT; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine[d / 4 * 64 + 16 * g + 4 * e + d % 4] = o[t][d][e];
+    if (g == 0) {
+      mml[(wave * 16 + l) * 2] = sm[t].m;
+      mml[(wave * 16 + l) * 2 + 1] = sm[t].l;
+    }
+    __syncthreads();
+    for (int x = tid; x < 16 * (DH / 4); x += KA_THREADS) {
+      const int i = x / (DH / 4), d = x % (DH / 4) * 4, row = j.r0 + t * 16 + i;
+      if (row >= j.live) continue;
+      float M = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < KA_WAVES; ++w) M = fmaxf(M, mml[(w * 16 + i) * 2]);
+      float ls = 0.f;
+      f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < KA_WAVES; ++w) {
+        const float mw = mml[(w * 16 + i) * 2], lw = mml[(w * 16 + i) * 2 + 1], wt = part_weight(mw, lw, M);
+        if (wt == 0.f && lw == lw) continue;
+        ls += wt * lw;
+        acc += wt * *reinterpret_cast<const f32x4*>(&mo[(w * 16 + i) * MP + d]);
+      }
+      const RowAt at = row_at(a, j, row, first);
+      if (!j.pre && n_live == 1 && pre_reach<KT>(a, p, at.b).live == 0) {
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        store4((float*)a.out + at.q(a, j.h) + d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+      } else {
+        const int64_t to = at.part(a, p, j.h, j.pre ? p.own.splits + j.sp : j.sp);
+        *reinterpret_cast<f32x4*>(part_o + to * DH + d) = acc;
+        if (d == 0) *reinterpret_cast<float2*>(part_ml + to * 2) = make_float2(M, ls);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------- merge
+// A row's parts, own splits then the prefix's, in that order: a thread takes four dims of one row.
+template <typename T, int KT>
+__global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p, const float* __restrict__ part_o,
+                                                              const float* __restrict__ part_ml) {
+  const int per = a.Dh / 4, b = blockIdx.z, h = blockIdx.y;
+  const int row = blockIdx.x * (KA_THREADS / per) + threadIdx.x / per, d = threadIdx.x % per * 4;
+  if (row >= rows_of(a, b)) return;
+  const int n_own = own_reach<KT>(a, p, b).live, n = n_own + pre_reach<KT>(a, p, b).live;
+  if (n == 1) return;
+  const RowAt at{b, row / a.G, row % a.G};
+  const int64_t base = at.part(a, p, h, 0), rows = (int64_t)a.nq_max * a.G;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < n; s0 += 8) {       // eight parts requested at a time
+    float2 ml[8];
+    f32x4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int s = min(s0 + i, n - 1);
+      const int64_t from = base + (s < n_own ? s : p.own.splits + s - n_own) * rows;
+      ml[i] = *reinterpret_cast<const float2*>(part_ml + from * 2);
+      x[i] = *reinterpret_cast<const f32x4*>(part_o + from * a.Dh + d);
+    }
+    float M = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) M = fmaxf(M, ml[i].x);
+    const float down = m == -INFINITY ? 1.f : exp2_hw(m - M);
+    m = M;
+    l *= down;
+    o *= down;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (s0 + i >= n) continue;
+      const float wt = part_weight(ml[i].x, ml[i].y, M);
+      if (wt == 0.f && ml[i].y == ml[i].y) continue;
+      l += wt * ml[i].y;
+      o += wt * x[i];
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  store4((T*)a.out + at.q(a, h) + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+}
+
+// ---------------------------------------------------------------------------- host
+// Splits: as many as give the workgroups that the CUs hold at once equal shares of the keys of both
+// parts, by the bounds the launch is given; at least three units of 64 keys pay for a split's start and
+// its partial results.
+static KvPlan kv_plan(const KvAttn& a) {
+  KvPlan p{};
+  const bool f32 = a.type == ADT_F32;
+  auto side = [&](KvSide& s, int64_t rows) {
+    s.tiles = f32 ? 1 : rows <= 64 ? 2 : 4;
+    s.blocks = (int)((rows + 32 * s.tiles - 1) / (32 * s.tiles));
+  };
+  const int64_t rows = (int64_t)a.nq_max * a.G;
+  side(p.own, rows);
+  const int64_t own_pairs = (int64_t)a.B * a.Hkv * p.own.blocks, own_units = ((int64_t)a.own.cap + KA_UNIT - 1) / KA_UNIT + 1;
+  int64_t pre_pairs = 0, pre_units = 0;
+  if (a.groups) {
+    side(p.pre, rows * a.group);
+    pre_pairs = (int64_t)a.groups * a.Hkv * p.pre.blocks;
+    pre_units = ((int64_t)a.pre.cap + KA_UNIT - 1) / KA_UNIT;
+  }
+  constexpr int64_t SLOTS = 512, LEAST = 3;
+  const int64_t per = std::max<int64_t>(LEAST, (own_pairs * own_units + pre_pairs * pre_units + SLOTS - 1) / SLOTS);
+  auto split = [&](KvSide& s, int64_t pairs, int64_t units) {
+    s.per = (int)std::min<int64_t>(per, 1 << 30);
+    int64_t n = units <= per + per / 4 ? 1 : (units + per - 1) / per;
+    n = std::min<int64_t>(n, std::max<int64_t>(1, 2 * SLOTS / std::max<int64_t>(1, pairs)));
+    s.splits = (int)std::min<int64_t>(n, 64);
+  };
+  split(p.own, own_pairs, own_units);
+  if (a.groups) split(p.pre, pre_pairs, pre_units);
+  p.pre_jobs = pre_pairs * p.pre.splits;
+  p.jobs = p.pre_jobs + own_pairs * p.own.splits;
+  p.parts = p.own.splits + p.pre.splits;
+  return p;
+}
+static size_t part_rows(const KvAttn& a, const KvPlan& p) {
+  return p.parts == 1 ? 0 : (size_t)a.B * a.Hkv * p.parts * a.nq_max * a.G;
+}
+
+size_t kv_attn_ws_bytes(const KvAttn& a) { return part_rows(a, kv_plan(a)) * (a.Dh + 2) * sizeof(float); }
+
+adt_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t st) {
+  const KvPlan p = kv_plan(a);
+  // (a launch has fewer than 2^32 threads in a dimension)
+  ADT_CHECK_ARG(p.jobs < (int64_t)1 << 24, ADT_E_CAPACITY, "cache_tree_attn: %lld workgroups", (long long)p.jobs);
+  float *part_o = (float*)ws, *part_ml = part_o + part_rows(a, p) * a.Dh;
+  const size_t lds = a.groups ? (size_t)(a.group + 1) * sizeof(int) : 0;
+  const unsigned jobs = (unsigned)p.jobs;
+#define ADT_KA(CV)                                                                               \
+  if (a.Dh == 128) kv_attn_kernel<CV, 128><<<jobs, KA_THREADS, lds, st>>>(a, p, part_o, part_ml); \
+  else kv_attn_kernel<CV, 64><<<jobs, KA_THREADS, lds, st>>>(a, p, part_o, part_ml)
+  switch (a.type) {
+    case ADT_BF16: ADT_KA(uint16_t); break;
+    case ADT_E4M3: ADT_KA(E4M3); break;
+    case ADT_I8: ADT_KA(I8); break;
+    default:
+      if (a.Dh == 128) kv_attn_f32_kernel<128><<<jobs, KA_THREADS, lds, st>>>(a, p, part_o, part_ml);
+      else kv_attn_f32_kernel<64><<<jobs, KA_THREADS, lds, st>>>(a, p, part_o, part_ml);
+  }
+#undef ADT_KA
+  ADT_LAUNCH_CHECK();
+  if (p.parts == 1) return ADT_OK;
+  const int fit = KA_THREADS / (a.Dh / 4);
+  const dim3 grid((a.nq_max * a.G + fit - 1) / fit, a.Hkv, a.B);
+  if (a.type == ADT_F32) kv_merge_kernel<float, 16><<<grid, KA_THREADS, 0, st>>>(a, p, part_o, part_ml);
+  else kv_merge_kernel<uint16_t, 32><<<grid, KA_THREADS, 0, st>>>(a, p, part_o, part_ml);
+  ADT_LAUNCH_CHECK();
+  return ADT_OK;
+}
+
+}  // namespace adt

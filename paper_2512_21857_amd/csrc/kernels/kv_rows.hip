@@ -1,0 +1,490 @@
+// Rows on their way into, out of and within a cache of any type: norms of queries and keys with the
+// rotation and the append, conversion between plain and eight-bit caches, and the moves of an
+// accepted path.
+//
+// All are bound by memory: a value is read once and written once.  A head's row of Dh values goes to a
+// group of neighbouring lanes, a 16-byte piece each, so that its sum of squares and its largest size
+// are a few lane exchanges away and every access is whole lines.
+#include <algorithm>
+
+#include "../eight_bit.h"
+#include "../launch.h"
+
+namespace adt {
+
+ADT_DEVICE_ERROR_WORD(kv_rows)
+
+constexpr int KR_THREADS = 256;
+constexpr int KR_MAX_PAIRS = 128;     // Dh <= 256
+
+template <typename T, int N, int ALIGN>
+struct alignas(ALIGN) RowPack {
+  T v[N];
+};
+
+// (cos, sin) of pos * freq in double: the angle less whole quarter turns (pi / 2 in two parts, so far
+// positions lose nothing), then the Taylor sums to r^18 and r^17, whose next terms are below 2^-56 for
+// |r| <= pi / 4.
+__device__ __forceinline__ double2 turn64(double pos, double freq) {
+  const double angle = pos * freq;
+  const double n = rint(angle * 0x1.45f306dc9c883p-1);     // 2 / pi
+  double r = fma(-n, 0x1.921fb54442d18p+0, angle);
+  r = fma(-n, 0x1.1a62633145c07p-54, r);
+  const double z = r * r;
+  double c = -1.0 / 6402373705728000.0;
+  c = fma(c, z, 1.0 / 20922789888000.0);
+  c = fma(c, z, -1.0 / 87178291200.0);
+  c = fma(c, z, 1.0 / 479001600.0);
+  c = fma(c, z, -1.0 / 3628800.0);
+  c = fma(c, z, 1.0 / 40320.0);
+  c = fma(c, z, -1.0 / 720.0);
+  c = fma(c, z, 1.0 / 24.0);
+  c = fma(c, z, -0.5);
+  c = fma(c, z, 1.0);
+  double s = 1.0 / 355687428096000.0;
+  s = fma(s, z, -1.0 / 1307674368000.0);
+  s = fma(s, z, 1.0 / 6227020800.0);
+  s = fma(s, z, -1.0 / 39916800.0);
+  s = fma(s, z, 1.0 / 362880.0);
+  s = fma(s, z, -1.0 / 5040.0);
+  s = fma(s, z, 1.0 / 120.0);
+  s = fma(s, z, -1.0 / 6.0);
+  s = fma(s * z, r, r);
+  const int k = (int)((long long)n & 3);
+  const double2 t = k & 1 ? make_double2(-s, c) : make_double2(c, s);
+  return k & 2 ? make_double2(-t.x, -t.y) : t;
+}
+
+// Sum and maximum over groups of `lanes` (a power of two) neighbouring lanes, all of which take part.
+template <typename R>
+__device__ __forceinline__ R group_sum(R v, int lanes) {
+  for (int o = lanes / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, WAVE);
+  return v;
+}
+__device__ __forceinline__ float group_max(float v, int lanes) {
+  for (int o = lanes / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, WAVE));
+  return v;
+}
+
+// A row's values of this lane, N pieces of VEC of them, into an eight-bit cache row: the group agrees
+// on the scale first.  piece(j): the first dim of piece j; dims from Dh on are none (values 0).
+template <typename C, int VEC, int N, typename R, class F>
+__device__ __forceinline__ void store_codes(const R (&y)[N][VEC], int lanes, bool first, int Dh, C* row, float* scale,
+                                            F piece) {
+  float largest = 0.f, odd = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float f = (float)y[j][e];
+      largest = fmaxf(largest, fabsf(f));
+      odd += f * 0.f;               // NaN if any value is not finite
+    }
+  largest = group_max(odd != odd ? INFINITY : largest, lanes);
+  double inverse;
+  const float s = row_scale<C>(largest, inverse);
+  if (first) *scale = s;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int d = piece(j);
+    if (d >= Dh) continue;
+    float t[VEC];
+    // (a row that is not finite has inverse 0 and codes 0)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) t[e] = s == s ? (float)((double)y[j][e] * inverse) : 0.f;
+    if constexpr (VEC == 1) {
+      reinterpret_cast<uint8_t*>(row)[d] = (uint8_t)encode4<C>(t[0], 0.f, 0.f, 0.f);
+    } else {
+      RowPack<uint32_t, VEC / 4, VEC> p;
+#pragma unroll
+      for (int e = 0; e < VEC; e += 4) p.v[e / 4] = encode4<C>(t[e], t[e + 1], t[e + 2], t[e + 3]);
+      *reinterpret_cast<decltype(p)*>(row + d) = p;
+    }
+  }
+}
+
+// One row a workgroup, all its heads or a part of them; a group of `lanes` lanes takes a head at a
+// time.  VEC values are 16 bytes where sizes and addresses allow it (N = 1 piece a lane), else one
+// value (a wave a head, N = 4).  A pair's other half is read from memory beside it (the same lines).
+template <typename T, typename C, int VEC, bool INTER>
+__global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, int lanes) {
+  constexpr int N = VEC == 1 ? 4 : 1;
+  __shared__ double2 cs[KR_MAX_PAIRS];
+  const int i = a.row0 + blockIdx.x, b = blockIdx.z;
+  if (i >= min(a.n_rows[b], a.n_max)) return;
+  const int64_t row = (int64_t)b * a.n_max + i;
+  const int rot = a.rot, half = rot / 2, DH = a.c.Dh, H = a.H, Hkv = a.c.heads;
+  for (int p = threadIdx.x; p < half; p += KR_THREADS) {
+    const double2 t = turn64((double)a.pos[row], a.freq[p]);
+    cs[p] = make_double2(t.x * a.gain, t.y * a.gain);
+  }
+  __syncthreads();
+  const int64_t slot = (int64_t)a.kv_len[b] + i;
+  const bool store_kv = a.kv_len[b] >= 0 && slot < a.c.cap;
+  if (!store_kv && threadIdx.x == 0 && blockIdx.y == 0) dev_fail(DEVINV_KV_RANGE);
+  const int per = KR_THREADS / lanes, sub = threadIdx.x / lanes, l = threadIdx.x % lanes;
+  auto piece = [&](int j) { return (l + j * lanes) * VEC; };
+  typedef RowPack<T, VEC, VEC == 1 ? sizeof(T) : 16> P;
+  const int64_t srow = (int64_t)b * a.c.scale_b + slot;
+
+  // one head of queries (math in fp32) or keys (in double), row src, gains g
+  auto head = [&](auto zero, const T* src, const float* g, auto store) {
+    typedef decltype(zero) R;
+    R x[N][VEC], o[N][VEC], y[N][VEC];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int d = piece(j);
+      P own{}, other{};
+      if (d < DH) {
+        own = *reinterpret_cast<const P*>(src + d);
+        const int at = INTER ? (VEC == 1 ? d ^ 1 : d) : d < half ? d + half : d - half;
+        if (d < rot && (VEC == 1 || !INTER)) other = *reinterpret_cast<const P*>(src + at);
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        x[j][e] = (R)Elem<T>::load(own.v, e);
+        o[j][e] = (R)Elem<T>::load(INTER && VEC > 1 ? own.v : other.v, INTER && VEC > 1 ? (e ^ 1) : e);
+      }
+    }
+    R inv = (R)1;
+    if (g) {
+      R ss = (R)0;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) ss += x[j][e] * x[j][e];
+      inv = (R)1 / sqrt(group_sum(ss, lanes) / (R)DH + (R)a.eps);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int d = piece(j);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const int at = d + e;
+        R v = x[j][e] * inv, w = o[j][e] * inv;
+        if (at < DH && g) v *= (R)g[at];
+        if (at < rot) {
+          const bool second = INTER ? at & 1 : at >= half;
+          const int mate = INTER ? at ^ 1 : second ? at - half : at + half;
+          if (g) w *= (R)g[mate];
+          const double2 t = cs[INTER ? at / 2 : second ? mate : at];
+          v = second ? w * (R)t.y + v * (R)t.x : v * (R)t.x - w * (R)t.y;
+        }
+        y[j][e] = v;
+      }
+    }
+    store(y);
+  };
+  auto plain = [&](const auto& y, T* dst) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int d = piece(j);
+      if (d >= DH) continue;
+      P p;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) Elem<T>::store(p.v, e, (float)y[j][e]);
+      *reinterpret_cast<P*>(dst + d) = p;
+    }
+  };
+
+  for (int hd = blockIdx.y * per + sub; hd < H + 2 * Hkv; hd += gridDim.y * per) {
+    if (hd < H) {
+      head(0.f, (const T*)a.q + row * a.ldq + (int64_t)hd * DH, a.q_norm ? a.q_norm + (int64_t)hd * a.norm_step : nullptr,
+           [&](const auto& y) { plain(y, (T*)a.q_out + (row * H + hd) * (int64_t)DH); });
+      continue;
+    }
+    if (!store_kv) break;
+    const bool key = hd < H + Hkv;
+    const int h = hd - H - (key ? 0 : Hkv);
+    C* to = (C*)(key ? a.c.k : a.c.v) + b * a.c.stride_b + h * a.c.stride_h + slot * DH;
+    float* scale = (key ? a.c.k_scale : a.c.v_scale) + h * a.c.scale_h + srow;
+    auto store = [&](const auto& y) {
+      if constexpr (EIGHT<C>) store_codes<C, VEC, N>(y, lanes, l == 0, DH, to, scale, piece);
+      else plain(y, (T*)to);
+    };
+    if (key) {
+      head(0.0, (const T*)a.k + row * a.ldk + (int64_t)h * DH, a.k_norm ? a.k_norm + (int64_t)h * a.norm_step : nullptr,
+           store);
+    } else {
+      const T* src = (const T*)a.v + row * a.ldv + (int64_t)h * DH;
+      float y[N][VEC];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        P p{};
+        if (piece(j) < DH) p = *reinterpret_cast<const P*>(src + piece(j));
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) y[j][e] = Elem<T>::load(p.v, e);
+      }
+      store(y);
+    }
+  }
+}
+
+static int pow2_at_least(int x) {
+  int p = 1;
+  while (p < x) p *= 2;
+  return p;
+}
+
+template <typename T, typename C>
+static adt_status norm_rope(NormRopeRows a, bool inter, hipStream_t st) {
+  constexpr int V = 16 / sizeof(T);
+  const int64_t strides[] = {a.ldq, a.ldk, a.ldv}, cache[] = {a.c.stride_b, a.c.stride_h};
+  const int code = EIGHT<C> ? V : 16 / (int)sizeof(C);     // elements a cache row's piece is aligned to
+  bool wide = a.c.Dh % V == 0 && a.rot % (inter ? V : 2 * V) == 0 && (uintptr_t)a.q % 16 == 0 && (uintptr_t)a.k % 16 == 0 &&
+              (uintptr_t)a.v % 16 == 0 && (uintptr_t)a.q_out % 16 == 0 && (uintptr_t)a.c.k % 16 == 0 &&
+              (uintptr_t)a.c.v % 16 == 0;
+  for (int64_t s : strides) wide = wide && s % V == 0;
+  for (int64_t s : cache) wide = wide && s % code == 0;
+  const int lanes = wide ? pow2_at_least(a.c.Dh / V) : WAVE;
+  // few rows: a row's heads over several workgroups until some 1024 are there
+  const int per = KR_THREADS / lanes;
+  int parts = (a.H + 2 * a.c.heads + per - 1) / per;
+  const int64_t rows = (int64_t)a.c.B * a.n_max;
+  parts = (int)std::min<int64_t>(parts, std::max<int64_t>(1, 1024 / rows));
+  // (a launch has fewer than 2^32 threads in a dimension, or it wraps: more rows take several)
+  constexpr int MOST = 1 << 23;
+#define ADT_NR(VECV, INTERV) norm_rope_kernel<T, C, VECV, INTERV><<<grid, KR_THREADS, 0, st>>>(a, lanes)
+  for (int64_t r0 = 0; r0 < a.n_max; r0 += MOST) {
+    a.row0 = (int)r0;
+    const dim3 grid((unsigned)std::min<int64_t>(MOST, a.n_max - r0), parts, a.c.B);
+    if (wide) {
+      if (inter) ADT_NR(V, true);
+      else ADT_NR(V, false);
+    } else {
+      if (inter) ADT_NR(1, true);
+      else ADT_NR(1, false);
+    }
+    ADT_LAUNCH_CHECK();
+  }
+#undef ADT_NR
+  return ADT_OK;
+}
+
+adt_status launch_norm_rope_append(NormRopeRows a, bool inter, int dtype, hipStream_t st) {
+  if (dtype == ADT_BF16) {
+    if (a.c.type == ADT_E4M3) return norm_rope<uint16_t, E4M3>(a, inter, st);
+    if (a.c.type == ADT_I8) return norm_rope<uint16_t, I8>(a, inter, st);
+    return norm_rope<uint16_t, uint16_t>(a, inter, st);
+  }
+  if (a.c.type == ADT_E4M3) return norm_rope<float, E4M3>(a, inter, st);
+  if (a.c.type == ADT_I8) return norm_rope<float, I8>(a, inter, st);
+  return norm_rope<float, float>(a, inter, st);
+}
+
+// ---------------------------------------------------------------------------- conversion
+struct ConvertArgs {
+  adt_kv_cache src, dst;
+  const int32_t *length, *src_start, *dst_start;
+  int n_max;
+};
+// The rows of sequence b: first slots on either side, and how many; rows outside either cache go.
+struct ConvertSpan {
+  int64_t s0, d0;
+  int first, end;
+};
+__device__ __forceinline__ ConvertSpan convert_span(const ConvertArgs& a, int b, bool check) {
+  ConvertSpan c;
+  c.s0 = a.src_start ? a.src_start[b] : 0;
+  c.d0 = a.dst_start ? a.dst_start[b] : 0;
+  const int64_t n = min(a.length[b], a.n_max);
+  const int64_t first = max((int64_t)0, max(-c.s0, -c.d0));
+  const int64_t end = min(n, min((int64_t)a.src.cap - c.s0, (int64_t)a.dst.cap - c.d0));
+  if (check && n > 0 && (first > 0 || end < n)) dev_fail(DEVINV_KV_RANGE);
+  c.first = (int)min(first, (int64_t)a.n_max);
+  c.end = (int)max(end, (int64_t)0);
+  return c;
+}
+
+// Codes to values: a group of lanes a row, 16 codes a lane (or one, and up to four pieces).
+template <typename C, typename T, int VEC>
+__global__ __launch_bounds__(KR_THREADS) void cache_read_kernel(ConvertArgs a, int lanes) {
+  constexpr int N = VEC == 1 ? 4 : 1;
+  const int b = blockIdx.z, h = blockIdx.y >> 1, DH = a.src.Dh;
+  const bool key = !(blockIdx.y & 1);
+  const ConvertSpan c = convert_span(a, b, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0);
+  const C* src = (const C*)(key ? a.src.k : a.src.v) + b * a.src.stride_b + h * a.src.stride_h + c.s0 * DH;
+  T* dst = (T*)(key ? a.dst.k : a.dst.v) + b * a.dst.stride_b + h * a.dst.stride_h + c.d0 * DH;
+  const float* scale = (key ? a.src.k_scale : a.src.v_scale) + b * a.src.scale_b + h * a.src.scale_h + c.s0;
+  const int per = KR_THREADS / lanes, sub = threadIdx.x / lanes, l = threadIdx.x % lanes;
+  for (int64_t i = c.first + (int64_t)blockIdx.x * per + sub; i < c.end; i += (int64_t)gridDim.x * per) {
+    const float s = scale[i];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int d = (l + j * lanes) * VEC;
+      if (d >= DH) continue;
+      const int64_t at = i * DH + d;
+      if constexpr (VEC == 1) {
+        Elem<T>::store(dst, at, decode4<C>(reinterpret_cast<const uint8_t*>(src)[at]).x * s);
+      } else {
+        const uint4 w = *reinterpret_cast<const uint4*>(src + at);
+        const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float4 f = decode4<C>(q[u]);
+          store4(dst + at + 4 * u, f.x * s, f.y * s, f.z * s, f.w * s);
+        }
+      }
+    }
+  }
+}
+
+// Values to codes: a group of lanes a row.
+template <typename T, typename C, int VEC>
+__global__ __launch_bounds__(KR_THREADS) void cache_write_kernel(ConvertArgs a, int lanes) {
+  constexpr int N = VEC == 1 ? 4 : 1;
+  const int b = blockIdx.z, h = blockIdx.y >> 1, DH = a.src.Dh;
+  const bool key = !(blockIdx.y & 1);
+  const ConvertSpan c = convert_span(a, b, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0);
+  const T* src = (const T*)(key ? a.src.k : a.src.v) + b * a.src.stride_b + h * a.src.stride_h + c.s0 * DH;
+  C* dst = (C*)(key ? a.dst.k : a.dst.v) + b * a.dst.stride_b + h * a.dst.stride_h + c.d0 * DH;
+  float* scale = (key ? a.dst.k_scale : a.dst.v_scale) + b * a.dst.scale_b + h * a.dst.scale_h + c.d0;
+  const int per = KR_THREADS / lanes, sub = threadIdx.x / lanes, l = threadIdx.x % lanes;
+  auto piece = [&](int j) { return (l + j * lanes) * VEC; };
+  typedef RowPack<T, VEC, VEC == 1 ? sizeof(T) : 16> P;
+  for (int64_t i = c.first + (int64_t)blockIdx.x * per + sub; i < c.end; i += (int64_t)gridDim.x * per) {
+    float y[N][VEC];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      P p{};
+      if (piece(j) < DH) p = *reinterpret_cast<const P*>(src + i * DH + piece(j));
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) y[j][e] = Elem<T>::load(p.v, e);
+    }
+    store_codes<C, VEC, N>(y, lanes, l == 0, DH, dst + i * DH, scale + i, piece);
+  }
+}
+
+// Workgroups along the slots: one step each, unless that were more than a launch may have.
+constexpr int64_t KR_GRID = 1 << 20;
+
+template <typename C, typename T>
+static adt_status cache_read(const ConvertArgs& a, hipStream_t st) {
+  bool wide = a.src.Dh % 16 == 0 && (uintptr_t)a.src.k % 16 == 0 && (uintptr_t)a.src.v % 16 == 0 &&
+              (uintptr_t)a.dst.k % 16 == 0 && (uintptr_t)a.dst.v % 16 == 0;
+  const int64_t strides[] = {a.src.stride_b, a.src.stride_h, a.dst.stride_b, a.dst.stride_h};
+  for (int64_t s : strides) wide = wide && s % 16 == 0;
+  const int lanes = wide ? pow2_at_least(a.src.Dh / 16) : WAVE;
+  const int64_t steps = ((int64_t)a.n_max * lanes + KR_THREADS - 1) / KR_THREADS;
+  const dim3 grid((unsigned)std::min<int64_t>(KR_GRID, steps), 2 * a.src.heads, a.src.B);
+  if (wide) cache_read_kernel<C, T, 16><<<grid, KR_THREADS, 0, st>>>(a, lanes);
+  else cache_read_kernel<C, T, 1><<<grid, KR_THREADS, 0, st>>>(a, lanes);
+  ADT_LAUNCH_CHECK();
+  return ADT_OK;
+}
+
+template <typename T, typename C>
+static adt_status cache_write(const ConvertArgs& a, hipStream_t st) {
+  constexpr int V = 16 / sizeof(T);
+  bool wide = a.src.Dh % V == 0 && (uintptr_t)a.src.k % 16 == 0 && (uintptr_t)a.src.v % 16 == 0 &&
+              (uintptr_t)a.dst.k % V == 0 && (uintptr_t)a.dst.v % V == 0;
+  const int64_t strides[] = {a.src.stride_b, a.src.stride_h, a.dst.stride_b, a.dst.stride_h};
+  for (int64_t s : strides) wide = wide && s % V == 0;
+  const int lanes = wide ? pow2_at_least(a.src.Dh / V) : WAVE;
+  const int64_t steps = ((int64_t)a.n_max * lanes + KR_THREADS - 1) / KR_THREADS;
+  const dim3 grid((unsigned)std::min<int64_t>(KR_GRID, steps), 2 * a.src.heads, a.src.B);
+  if (wide) cache_write_kernel<T, C, V><<<grid, KR_THREADS, 0, st>>>(a, lanes);
+  else cache_write_kernel<T, C, 1><<<grid, KR_THREADS, 0, st>>>(a, lanes);
+  ADT_LAUNCH_CHECK();
+  return ADT_OK;
+}
+
+adt_status launch_cache_convert(const adt_kv_cache& src, const adt_kv_cache& dst, const int32_t* length, int n_max,
+                                const int32_t* src_start, const int32_t* dst_start, hipStream_t st) {
+  const ConvertArgs a{src, dst, length, src_start, dst_start, n_max};
+  if (src.type == ADT_E4M3)
+    return dst.type == ADT_BF16 ? cache_read<E4M3, uint16_t>(a, st) : cache_read<E4M3, float>(a, st);
+  if (src.type == ADT_I8) return dst.type == ADT_BF16 ? cache_read<I8, uint16_t>(a, st) : cache_read<I8, float>(a, st);
+  if (dst.type == ADT_E4M3)
+    return src.type == ADT_BF16 ? cache_write<uint16_t, E4M3>(a, st) : cache_write<float, E4M3>(a, st);
+  return src.type == ADT_BF16 ? cache_write<uint16_t, I8>(a, st) : cache_write<float, I8>(a, st);
+}
+
+// ---------------------------------------------------------------------------- accepted path
+// A workgroup takes whole slices: it reads every row that moves into registers, with its scales, and
+// writes after a barrier, as a destination may be another row's source.
+template <int RM>
+__global__ __launch_bounds__(KR_THREADS) void cache_compact_kernel(adt_kv_cache c, int row_bytes,
+                                                                   const int32_t* __restrict__ kv_len,
+                                                                   const int32_t* __restrict__ path, int path_stride,
+                                                                   const int32_t* __restrict__ n_acc, int a_max,
+                                                                   int slices_each) {
+  const int b = blockIdx.y, s0 = blockIdx.x * slices_each;
+  const int acc = min(n_acc[b], a_max);
+  const int64_t L = kv_len[b];
+  const int per_row = row_bytes / 16, per_slice = a_max * per_row, total = slices_each * per_slice;
+  const int64_t es = row_bytes / c.Dh;
+  u16x8 kr[RM], vr[RM];
+  float ks[RM], vs[RM];
+  // piece p: slice, rank on the path, 16 bytes of the row; false where nothing moves
+  struct Move {
+    int slice, piece;
+    int64_t from, to;
+  };
+  auto move = [&](int it, Move& m) {
+    const int p = threadIdx.x + it * KR_THREADS;
+    if (p >= total) return false;
+    m.slice = s0 + p / per_slice;
+    const int w = p % per_slice, rank = w / per_row + 1;
+    m.piece = w % per_row;
+    if (m.slice >= c.heads || rank > acc) return false;
+    const int node = path[(int64_t)b * path_stride + rank];
+    m.from = L + node;
+    m.to = L + rank;
+    if (node < rank || node >= ADT_MAX_NODES) {
+      dev_fail(DEVINV_PATH);
+      return false;
+    }
+    if (L < 0 || m.from >= c.cap) {
+      dev_fail(DEVINV_KV_RANGE);
+      return false;
+    }
+    return true;
+  };
+#pragma unroll
+  for (int it = 0; it < RM; ++it) {
+    Move m;
+    if (!move(it, m)) continue;
+    const int64_t at = (b * c.stride_b + m.slice * c.stride_h + m.from * c.Dh) * es;
+    kr[it] = reinterpret_cast<const u16x8*>((const char*)c.k + at)[m.piece];
+    vr[it] = reinterpret_cast<const u16x8*>((const char*)c.v + at)[m.piece];
+    if (c.k_scale && m.piece == 0) {
+      const int64_t sc = b * c.scale_b + m.slice * c.scale_h + m.from;
+      ks[it] = c.k_scale[sc];
+      vs[it] = c.v_scale[sc];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int it = 0; it < RM; ++it) {
+    Move m;
+    if (!move(it, m)) continue;
+    const int64_t at = (b * c.stride_b + m.slice * c.stride_h + m.to * c.Dh) * es;
+    reinterpret_cast<u16x8*>((char*)c.k + at)[m.piece] = kr[it];
+    reinterpret_cast<u16x8*>((char*)c.v + at)[m.piece] = vr[it];
+    if (c.k_scale && m.piece == 0) {
+      const int64_t sc = b * c.scale_b + m.slice * c.scale_h + m.to;
+      c.k_scale[sc] = ks[it];
+      c.v_scale[sc] = vs[it];
+    }
+  }
+}
+
+adt_status launch_cache_compact(const adt_kv_cache& c, const int32_t* kv_len, const int32_t* path, int path_stride,
+                                const int32_t* n_acc, int a_max, hipStream_t st) {
+  const int es = c.type == ADT_F32 ? 4 : c.type == ADT_BF16 ? 2 : 1, row_bytes = c.Dh * es;
+  const int pieces = a_max * (row_bytes / 16);      // of a slice: at most 127 * 64
+  const int rm = pieces <= 2 * KR_THREADS ? 2 : pieces <= 8 * KR_THREADS ? 8 : 32;
+  const int each = std::max(1, std::min(c.heads, rm * KR_THREADS / pieces));
+  const dim3 grid((c.heads + each - 1) / each, c.B);
+#define ADT_CC(RM) \
+  cache_compact_kernel<RM><<<grid, KR_THREADS, 0, st>>>(c, row_bytes, kv_len, path, path_stride, n_acc, a_max, each)
+  if (rm == 2) ADT_CC(2);
+  else if (rm == 8) ADT_CC(8);
+  else ADT_CC(32);
+#undef ADT_CC
+  ADT_LAUNCH_CHECK();
+  return ADT_OK;
+}
+
+}  // namespace adt

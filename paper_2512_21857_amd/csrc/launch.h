@@ -57,6 +57,8 @@ uint32_t dev_errors_take_rope();
 uint32_t dev_errors_take_evict();
 uint32_t dev_errors_take_blocks();
 uint32_t dev_errors_take_cache_attn();
+uint32_t dev_errors_take_kv_rows();
+uint32_t dev_errors_take_kv_attn();
 
 // attn.hip
 // Row of query qr of sequence b in q and out: b * rs_b + qr * rs_i (rows of H * Dh); its mask
@@ -359,5 +361,52 @@ adt_status launch_kv_evict(const EvictMove& a, int B, int n_first, int n_last, h
 adt_status launch_weights_compact(float* w, int B, int slices, int64_t stride_wb, int64_t stride_ws,
                                   const int32_t* kv_len, int kv_cap, const int32_t* path, int path_stride,
                                   const int32_t* n_acc, int a_max, hipStream_t st);
+
+// kv_rows.hip
+// Rows [B][n_max] normalised, rotated and appended to a cache; fields as the arguments of
+// adt_norm_rope_append.  row0: the first row of a launch.
+struct NormRopeRows {
+  const void *q, *k, *v;
+  int64_t ldq, ldk, ldv;
+  const float *q_norm, *k_norm;
+  int norm_step;                 // floats from one head's gains to the next
+  float eps;
+  const int32_t *pos, *kv_len, *n_rows;
+  const double* freq;
+  float gain;
+  int n_max, H, rot;
+  void* q_out;
+  adt_kv_cache c;
+  int row0 = 0;
+};
+adt_status launch_norm_rope_append(NormRopeRows a, bool inter, int dtype, hipStream_t st);
+adt_status launch_cache_convert(const adt_kv_cache& src, const adt_kv_cache& dst, const int32_t* length, int n_max,
+                                const int32_t* src_start, const int32_t* dst_start, hipStream_t st);
+adt_status launch_cache_compact(const adt_kv_cache& c, const int32_t* kv_len, const int32_t* path, int path_stride,
+                                const int32_t* n_acc, int a_max, hipStream_t st);
+
+// kv_attn.hip
+// Keys of one part of the rows' context: a cache (sequences own theirs, a group shares one), up to
+// `cap` slots of it.
+struct KvPart {
+  const void *k, *v;
+  const float *ks, *vs;
+  int64_t sb, sh, ssb, ssh;
+  const int32_t* len;
+  int cap;
+};
+struct KvAttn {
+  const void* q;
+  KvPart own, pre;
+  const int32_t *n_q, *n_tail;
+  const uint64_t* mask;
+  int B, Hkv, G, Dh, nq_max;
+  int groups, group;             // shared prefixes (0: none), sequences of each
+  int type;                      // of the caches
+  float scale;
+  void* out;
+};
+size_t kv_attn_ws_bytes(const KvAttn& a);
+adt_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t st);
 
 }  // namespace adt

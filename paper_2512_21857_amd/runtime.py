@@ -384,6 +384,151 @@ def weights_compact(weights: torch.Tensor, kv_len: torch.Tensor, path: torch.Ten
                path.shape[-1], _ptr("n_acc", n_acc, dev, _I32, (B,)), a_max))
 
 
+# ---------------------------------------------------------------------------- caches of any type
+KV_TYPES = {torch.float32: abi.F32, torch.bfloat16: abi.BF16, torch.float8_e4m3fn: abi.E4M3, torch.int8: abi.I8}
+
+
+class KVCache:
+    """A key-value cache of any type as the calls below take it: k and v [B][heads][slots][Dh] in float32,
+    bfloat16, or in eight bits (float8_e4m3fn or int8, with a float32 scale for every row, k_scale and
+    v_scale [B][heads][slots]).  Rows and scales of a head are contiguous; a layer of a larger cache will
+    do.  The tensors are checked here, once, and their addresses kept with them: a tensor that is given
+    other memory later (`resize_`, `set_`, `.data`) needs a new KVCache."""
+
+    __slots__ = ("k", "v", "k_scale", "v_scale", "B", "heads", "slots", "Dh", "dtype", "dev", "device", "_struct", "_ref")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        kind, dev = KV_TYPES.get(k.dtype), k.get_device()
+        if kind is None or dev < 0:
+            raise ValueError(f"a device tensor of {[str(t) for t in KV_TYPES]} expected, not {k.dtype} on {k.device}")
+        (B, heads, S, Dh), sb, sh = _caches(k, v, dev, k.dtype)
+        steps = (0, 0)
+        if (kind in (abi.E4M3, abi.I8)) != (k_scale is not None and v_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise ValueError("k_scale and v_scale go with eight-bit caches, and only with those")
+        if k_scale is not None:
+            steps = _weights("k_scale", k_scale, dev, B, heads, S)
+            if _weights("v_scale", v_scale, dev, B, heads, S) != steps:
+                raise ValueError("k_scale and v_scale must have the same strides")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.B, self.heads, self.slots, self.Dh, self.dtype, self.dev, self.device = B, heads, S, Dh, k.dtype, dev, k.device
+        at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self._struct = abi.KvCache(at(k), at(v), sb, sh, at(k_scale), at(v_scale), *steps, B, heads, S, Dh, kind)
+        self._ref = C.addressof(self._struct)
+
+    @classmethod
+    def zeros(cls, B: int, heads: int, slots: int, Dh: int, dtype: torch.dtype = torch.bfloat16, device="cuda"):
+        """A new cache of zeros."""
+        k, v = (torch.zeros(B, heads, slots, Dh, dtype=dtype, device=device) for _ in range(2))
+        if KV_TYPES.get(dtype) not in (abi.E4M3, abi.I8):
+            return cls(k, v)
+        return cls(k, v, *(torch.zeros(B, heads, slots, dtype=_F32, device=device) for _ in range(2)))
+
+
+def _norm(what: str, w: Optional[torch.Tensor], dev: int, heads: int, Dh: int):
+    """(address, whether it holds a gain for every head) of norm gains float32 [Dh] or [heads][Dh]."""
+    if w is None:
+        return None, None
+    each = w.dim() == 2
+    return _ptr(what, w, dev, _F32, (heads, Dh) if each else (Dh,)), each
+
+
+def norm_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, kv_len: torch.Tensor,
+                     n_rows: torch.Tensor, freq: torch.Tensor, cache: KVCache, q_norm: Optional[torch.Tensor] = None,
+                     k_norm: Optional[torch.Tensor] = None, eps: float = 1e-5, layout: str = "half", gain: float = 1.0,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """rope_append into a cache of any type, queries and keys normalised head by head before: x * norm /
+    sqrt(mean x^2 + eps), with gains float32 [Dh] for all heads or [heads][Dh] (None: that side is not
+    normalised).  Returns the rotated queries (`out`, which may be q where its rows are contiguous)."""
+    dev, dt = _dt(q)
+    dtype = q.dtype
+    B, n, _, Dh = q.shape
+    H, ldq = _rows("q", q, dev, dtype, B, n, Dh)
+    Hkv, ldk = _rows("k", k, dev, dtype, B, n, Dh)
+    Hv, ldv = _rows("v", v, dev, dtype, B, n, Dh)
+    if Hv != Hkv or cache.B != B or cache.heads != Hkv or cache.Dh != Dh or cache.dev != dev:
+        raise ValueError(f"{Hkv} key heads, {Hv} value heads of {Dh} on device {dev} and a cache of {cache.B} x {cache.heads} x "
+                         f"{cache.Dh} on device {cache.dev} do not go together")
+    qn, q_each = _norm("q_norm", q_norm, dev, H, Dh)
+    kn, k_each = _norm("k_norm", k_norm, dev, Hkv, Dh)
+    if q_each is not None and k_each is not None and q_each != k_each:
+        raise ValueError("q_norm and k_norm both hold gains for all heads, or both for every head")
+    if out is None:
+        out = torch.empty(B, n, H, Dh, dtype=dtype, device=q.device)
+    _on_device(dev, lib().adt_norm_rope_append, (q.data_ptr(), k.data_ptr(), v.data_ptr(), ldq, ldk, ldv, qn, kn,
+               1 if q_each or k_each else 0, eps, _ptr("pos", pos, dev, _I32, (B, n)),
+               _ptr("kv_len", kv_len, dev, _I32, (B,)), _ptr("n_rows", n_rows, dev, _I32, (B,)),
+               _ptr("freq", freq, dev, _F64, freq.shape), gain, 2 * freq.numel(), ROPE_LAYOUTS[layout], n, H, dt,
+               _ptr("out", out, dev, dtype, (B, n, H, Dh)), cache._ref))
+    return out
+
+
+def cache_convert(src: KVCache, dst: KVCache, length: torch.Tensor, n_max: Optional[int] = None,
+                  src_start: Optional[torch.Tensor] = None, dst_start: Optional[torch.Tensor] = None) -> KVCache:
+    """Slots of an eight-bit cache read back into a plain one, or a plain cache's slots put in eight bits: of
+    every head, src_start[b] + i to dst_start[b] + i, i < length[b] (int32 [B]; starts default to 0).
+    n_max bounds length (default: the smaller cache's slots).  Returns dst."""
+    if src.dev != dst.dev:
+        raise ValueError(f"caches on devices {src.dev} and {dst.dev}")
+    dev, B = src.dev, src.B
+    _on_device(dev, lib().adt_cache_convert, (src._ref, dst._ref, _ptr("length", length, dev, _I32, (B,)),
+               min(src.slots, dst.slots) if n_max is None else n_max, _opt("src_start", src_start, dev, _I32, (B,)),
+               _opt("dst_start", dst_start, dev, _I32, (B,))))
+    return dst
+
+
+def cache_compact(cache: KVCache, kv_len: torch.Tensor, path: torch.Tensor, n_acc: torch.Tensor, a_max: int) -> None:
+    """Moves an accepted path in place in a cache of any type, scales included, as kv_compact does; path
+    int32 [B][stride] (path[b][0] = 0)."""
+    dev, B = cache.dev, cache.B
+    _on_device(dev, lib().adt_cache_compact, (cache._ref, _ptr("kv_len", kv_len, dev, _I32, (B,)),
+               _ptr("path", path, dev, _I32, (B, path.shape[-1])), path.shape[-1], _ptr("n_acc", n_acc, dev, _I32, (B,)),
+               a_max))
+
+
+def cache_tree_attn_workspace(H: int, nq_max: int, cache: KVCache, kv_cap: Optional[int] = None,
+                              prefix: Optional[KVCache] = None, prefix_cap: Optional[int] = None) -> torch.Tensor:
+    """A workspace for cache_tree_attn calls of these sizes (bounds default to the caches' slots)."""
+    groups, pcap = (0, 0) if prefix is None else (prefix.B, prefix.slots if prefix_cap is None else prefix_cap)
+    n = lib().adt_cache_tree_attn_workspace_size(cache.B, H, cache.heads, cache.Dh, nq_max,
+                                                 cache.slots if kv_cap is None else kv_cap, groups, pcap,
+                                                 KV_TYPES[cache.dtype])
+    return torch.empty(max(n, 16), dtype=_U8, device=cache.device)
+
+
+def cache_tree_attn(q: torch.Tensor, cache: KVCache, kv_len: torch.Tensor, n_q: torch.Tensor, n_tail: torch.Tensor,
+                    mask: torch.Tensor, kv_cap: Optional[int] = None, prefix: Optional[KVCache] = None,
+                    prefix_len: Optional[torch.Tensor] = None, prefix_cap: Optional[int] = None,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Tree attention of q [B][n][H][Dh] over a cache [B][Hkv][slots][Dh] of any type; behind a prefix that
+    consecutive sequences share, if one is given: a cache [groups][Hkv][slots][Dh] of the same type,
+    prefix_len int32 [groups], each group's keys and values read once for all its rows.  kv_cap and
+    prefix_cap bound kv_len + n_tail and prefix_len (default: the caches' slots).  out may be q."""
+    dev, dt = _dt(q)
+    B, n, H, Dh = q.shape
+    if (B != cache.B or Dh != cache.Dh or dev != cache.dev or not q.is_contiguous() or (prefix is None) != (prefix_len is None)
+            or (prefix is not None and prefix.dev != dev)):
+        raise ValueError(f"contiguous queries {tuple(q.shape)} on device {dev}, a cache of {cache.B} x {cache.heads} x {cache.Dh} on "
+                         f"device {cache.dev}, and a prefix there with its lengths, or neither, expected")
+    if kv_cap is None:
+        kv_cap = cache.slots
+    if prefix is not None and prefix_cap is None:
+        prefix_cap = prefix.slots
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = cache_tree_attn_workspace(H, n, cache, kv_cap, prefix, prefix_cap)
+    _on_device(dev, lib().adt_cache_tree_attn, (q.data_ptr(), cache._ref, _ptr("kv_len", kv_len, dev, _I32, (B,)),
+               _ptr("n_q", n_q, dev, _I32, (B,)), _ptr("n_tail", n_tail, dev, _I32, (B,)),
+               _ptr("mask", mask, dev, _I64, (B, n, abi.MASK_WORDS)), H, n, kv_cap,
+               None if prefix is None else prefix._ref,
+               None if prefix is None else _ptr("prefix_len", prefix_len, dev, _I32, (prefix.B,)), prefix_cap or 0,
+               Dh ** -0.5 if scale is None else scale, dt, _ptr("out", out, dev, q.dtype, (B, n, H, Dh)),
+               _ptr("workspace", workspace, dev, _U8, workspace.shape), workspace.numel()))
+    return out
+
+
 def accept_cfg(mode: str = "greedy", temperature: float = 1.0, top_k: int = 0, delta: float = 0.0,
                knn: Optional[torch.Tensor] = None, knn_k: int = 1, seed: int = 0, children: int = 0,
                q_logits: Optional[torch.Tensor] = None, q_row: Optional[torch.Tensor] = None) -> abi.AcceptCfg:
