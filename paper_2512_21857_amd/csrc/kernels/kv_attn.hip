@@ -170,23 +170,20 @@ __device__ __forceinline__ float part_weight(float m, float l, float M) {
 //                           keys 8 c + 4 s + e, c and e < 4),
 //   O^T[dim][row] += V^T P^T  (V by transpose loads, its keys in the order in which the lanes hold P).
 // A row's scores lie in two lanes, so its maximum takes one exchange; 32 rows a wave halve the LDS reads
-// that 16 would need, which are as long as the products.  Rows of K and V lie in 16-byte chunks swizzled
-// by row, so that the operand reads touch distinct banks.
-template <int DH>
-__device__ __forceinline__ int swz_k(int row) { return DH == 128 ? (row & 15) : ((row >> 1) & 7); }
-template <int DH>
-__device__ __forceinline__ int swz_v(int row) { return DH == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3); }
-
+// that 16 would need, which are as long as the products.  LDS rows are padded so that what half a wave
+// reads at once falls on distinct banks (K: 16 rows of 16 bytes; V: 4 rows of 64), and every operand lies
+// at a constant distance from one address (swizzled rows took some 25 registers of addresses).
 template <typename C, int DH>
 __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan p, float* __restrict__ part_o,
                                                                float* __restrict__ part_ml) {
   constexpr int KT = 32, KS = DH / 16, OT = DH / 32;
   constexpr int EPL = 16 / (int)sizeof(C), CPL = DH / EPL;         // elements of a load, loads of a row
   constexpr int LOADS = KA_UNIT * CPL / KA_THREADS;
-  constexpr int BYTES = KA_UNIT * DH * 2;                          // a unit of K or of V in LDS
+  constexpr int KP = DH * 2 + 16, VP = DH * 2 + 64;                // bytes of an LDS row of K, of V
+  constexpr int BYTES = KA_UNIT * (KP + VP);                       // a unit in LDS
   constexpr bool CODES = EIGHT<C>;
-  static_assert(2 * (OT * 16 + 2) * WAVE * 4 <= 4 * BYTES, "merge area");
-  __shared__ __attribute__((aligned(16))) unsigned char smem[4 * BYTES];    // [buffer][K, V]
+  static_assert(2 * (OT * 16 + 2) * WAVE * 4 <= 2 * BYTES, "merge area");
+  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * BYTES];    // [buffer], K then V
   __shared__ float scales[2][2][CODES ? KA_UNIT : 1];              // [buffer][K, V][key]
   extern __shared__ int first[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
@@ -205,7 +202,6 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
   const float scale_log2 = a.scale * LOG2E;
 
   bf16x8 q[KS];
-  uint64_t aw0 = 0, aw1 = 0;
   const int row = j.r0 + tile * 32 + r;
   const bool mine = row < j.live, tile_live = j.r0 + tile * 32 < j.live;
   RowAt at{j.b, 0, 0};
@@ -216,14 +212,11 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
     const uint16_t* src = (const uint16_t*)a.q + at.q(a, j.h) + s * 8;
 #pragma unroll
     for (int i = 0; i < KS; ++i) q[i] = *reinterpret_cast<const bf16x8*>(src + i * 16);
-    if (!j.pre) {
-      const uint64_t* mp = a.mask + ((int64_t)at.b * a.nq_max + at.node) * ADT_MASK_WORDS;
-      aw0 = mp[0];
-      aw1 = mp[1];
-    }
   }
+  // the row's mask, 32 tail slots a word: those of a step
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) + ((int64_t)at.b * a.nq_max + at.node) * 2 * ADT_MASK_WORDS;
 
-  // The two steps of a unit: first key and last (a step past the end has none: last < key0).
+  // A step's first key and last (a step past the end has none: last < key0).
   struct Span {
     int key0, last;
   };
@@ -232,50 +225,50 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
     if (st >= j.reach.prefix_steps) return Span{L + (st - j.reach.prefix_steps) * KT, total - 1};
     return Span{st * KT, L - 1};
   };
-  // Load x of a unit takes row x / CPL, elements (x % CPL) * EPL..; thread t takes loads i * 256 + t.  Rows
+  // Load x of a unit takes row x / CPL, elements (x % CPL) * EPL..; thread t takes loads u * 256 + t.  Rows
   // past a step's last key read that one, or the head's first row, and are stored as zeros.
   u16x8 kr[LOADS], vr[LOADS];
   float sc = 0.f;
-  Span now[2], next[2];
+  Span next0{0, -1}, next1{0, -1};
   auto fetch = [&](int i) {
     const int st = i < units ? 2 * (j.sp + n_live * i) : steps;
-    next[0] = span(st);
-    next[1] = span(st + 1);
+    next0 = span(st);
+    next1 = span(st + 1);
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
       const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
-      const Span& w = rx < KT ? next[0] : next[1];
-      const int key = max(0, min(w.key0 + rx % KT, w.last));
+      const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
+      const int key = max(0, min(key0 + rx % KT, last));
       kr[u] = *reinterpret_cast<const u16x8*>(kb + (int64_t)key * DH + c * EPL);
       vr[u] = *reinterpret_cast<const u16x8*>(vb + (int64_t)key * DH + c * EPL);
     }
     if (CODES && tid < 2 * KA_UNIT) {
       const int rx = tid % KA_UNIT;
-      const Span& w = rx < KT ? next[0] : next[1];
-      const int key = w.key0 + rx % KT;
+      const int key = (rx < KT ? next0.key0 : next1.key0) + rx % KT;
       sc = 0.f;
-      if (key <= w.last) sc = tid < KA_UNIT ? ksb[key] * scale_log2 : vsb[key];
+      if (key <= (rx < KT ? next0.last : next1.last)) sc = tid < KA_UNIT ? ksb[key] * scale_log2 : vsb[key];
     }
   };
-  auto put = [&](unsigned char* at, int rx, int c, int swz, u16x8 v) {
+  auto put = [&](unsigned char* row, int c, u16x8 v) {
     if constexpr (CODES) {
       const uint4 w = __builtin_bit_cast(uint4, v);
       const u16x4 d0 = decode4_bf16<C>(w.x), d1 = decode4_bf16<C>(w.y), d2 = decode4_bf16<C>(w.z), d3 = decode4_bf16<C>(w.w);
-      unsigned char* row = at + rx * DH * 2;
-      *reinterpret_cast<u16x8*>(row + ((2 * c) ^ swz) * 16) = u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
-      *reinterpret_cast<u16x8*>(row + ((2 * c + 1) ^ swz) * 16) = u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]};
+      *reinterpret_cast<u16x8*>(row + 32 * c) = u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+      *reinterpret_cast<u16x8*>(row + 32 * c + 16) = u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]};
     } else {
-      *reinterpret_cast<u16x8*>(at + rx * DH * 2 + (c ^ swz) * 16) = v;
+      *reinterpret_cast<u16x8*>(row + 16 * c) = v;
     }
   };
   auto store = [&](int buf) {
-    unsigned char* to = smem + buf * 2 * BYTES;
+    unsigned char* to = smem + buf * BYTES;
+    const bool full = next0.key0 + KT - 1 <= next0.last && next1.key0 + KT - 1 <= next1.last;
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
       const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
-      const Span& w = rx < KT ? next[0] : next[1];
-      put(to, rx, c, swz_k<DH>(rx), kr[u]);
-      put(to + BYTES, rx, c, swz_v<DH>(rx), w.key0 + rx % KT <= w.last ? vr[u] : u16x8{});
+      const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
+      if (!full && key0 + rx % KT > last) vr[u] = u16x8{};
+      put(to + rx * KP, c, kr[u]);
+      put(to + KA_UNIT * KP + rx * VP, c, vr[u]);
     }
     if (CODES && tid < 2 * KA_UNIT) scales[buf][tid / KA_UNIT][tid % KA_UNIT] = sc;
   };
@@ -287,38 +280,36 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
 
-  // step w of the unit in buffer `buf`
-  auto compute = [&](int buf, int st, int w) {
-    const unsigned char* ks = smem + buf * 2 * BYTES;
-    const unsigned char* vs = ks + BYTES;
-    const int k0 = now[w].key0, k_last = now[w].last;
-    const bool tail = st >= j.reach.prefix_steps;
+  bool odd = false;               // a value of the tail was not finite
+  // Step w of the unit in buffer `buf`: all of its keys, or those of `seen` (bit i: key i), of whose values
+  // only a tail's may be kept from a row.
+  auto compute = [&](auto whole_tag, int buf, int w, uint32_t seen, bool tail) {
+    constexpr bool WHOLE = decltype(whole_tag)::value;
+    // this lane's part of the first 16 dims of its key, and of the first transpose load
+    const unsigned char* ks = smem + buf * BYTES + (w * KT + r) * KP + s * 16;
+    const unsigned char* vs = smem + buf * BYTES + KA_UNIT * KP + (w * KT + 4 * s + (lane & 15) / 4) * VP +
+                              (lane >> 4 & 1) * 32 + (lane & 3) * 8;
     f32x16 x;
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = 0.f;
-    const int kx = w * KT + r;
+    bf16x8 f[KS];
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      const bf16x8 f = *reinterpret_cast<const bf16x8*>(ks + kx * DH * 2 + ((2 * i + s) ^ swz_k<DH>(kx)) * 16);
-      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[i], x, 0, 0, 0);
-    }
-    auto key_of = [&](int e) { return 8 * (e / 4) + 4 * s + e % 4; };
-    auto sees = [&](int key) {        // key of the step
-      const int t = k0 + key - L;
-      return (k0 + key <= k_last) & (!tail | (bool)((t < 64 ? aw0 : aw1) >> (t & 63) & 1));
-    };
+    for (int i = 0; i < KS; ++i) f[i] = *reinterpret_cast<const bf16x8*>(ks + i * 32);
+    __builtin_amdgcn_sched_barrier(0);       // all of them requested before the first product
+#pragma unroll
+    for (int i = 0; i < KS; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], q[i], x, 0, 0, 0);
+    seen >>= 4 * s;                 // bit 8 c + e: this lane's score 4 c + e
     if constexpr (CODES) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const f32x4 f = *reinterpret_cast<const f32x4*>(&scales[buf][0][w * KT + 8 * c + 4 * s]);
+        const f32x4 by = *reinterpret_cast<const f32x4*>(&scales[buf][0][w * KT + 8 * c + 4 * s]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * c + e] *= f[e];
+        for (int e = 0; e < 4; ++e) x[4 * c + e] *= by[e];
       }
     }
-    const bool whole = !tail && k0 + KT - 1 <= k_last;
-    if (!whole) {
+    if constexpr (!WHOLE) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = sees(key_of(e)) ? x[e] : -INFINITY;
+      for (int e = 0; e < 16; ++e) x[e] = seen >> (e / 4 * 8 + e % 4) & 1 ? x[e] : -INFINITY;
     }
     float mx = x[0];
 #pragma unroll
@@ -341,70 +332,85 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
       // (a slot the row does not see may have any scale)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const f32x4 f = *reinterpret_cast<const f32x4*>(&scales[buf][1][w * KT + 8 * c + 4 * s]);
+        const f32x4 by = *reinterpret_cast<const f32x4*>(&scales[buf][1][w * KT + 8 * c + 4 * s]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * c + e] = !tail || sees(8 * c + 4 * s + e) ? x[4 * c + e] * f[e] : 0.f;
+        for (int e = 0; e < 4; ++e) x[4 * c + e] = WHOLE || (seen >> (8 * c + e) & 1) ? x[4 * c + e] * by[e] : 0.f;
       }
     }
     bf16x8 pb[2];
 #pragma unroll
     for (int e = 0; e < 16; ++e) pb[e / 8][e % 8] = (__bf16)x[e];
     // lane i of a 16-lane group that addresses row k0 + i / 4, dims d0 + 4 (i % 4)..+3 gets V[k0 + 0..3][d0 + i]
-    const int i16 = lane & 15, hi16 = (lane >> 4) & 1;
-    bool odd = false;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int lo = w * KT + 16 * c + 4 * s + (i16 >> 2), hi = lo + 8;
 #pragma unroll
       for (int d = 0; d < OT; ++d) {
-        const int ch = 4 * d + 2 * hi16 + ((i16 & 3) >> 1), half = (i16 & 1) * 8;
-        v4i16 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + lo * DH * 2 + (ch ^ swz_v<DH>(lo)) * 16 + half));
-        v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + hi * DH * 2 + (ch ^ swz_v<DH>(hi)) * 16 + half));
-        if (tail) {
-          // a value that is not finite may only meet the rows that see it: it is taken out here
+        v4i16 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + 16 * c * VP + d * 64));
+        v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + (16 * c + 8) * VP + d * 64));
+        if (!WHOLE && tail) {
+          // a value that is not finite may only meet the rows that see it: it is taken out here, and added
+          // when all keys are done
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if ((x0[e] & 0x7f80) == 0x7f80) x0[e] = 0, odd = true;
-            if ((x1[e] & 0x7f80) == 0x7f80) x1[e] = 0, odd = true;
+            const bool b0 = (x0[e] & 0x7f80) == 0x7f80, b1 = (x1[e] & 0x7f80) == 0x7f80;
+            x0[e] = b0 ? 0 : x0[e];
+            x1[e] = b1 ? 0 : x1[e];
+            odd |= b0 | b1;
           }
         }
-        const bf16x8 f = __builtin_bit_cast(bf16x8, v8i16{x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]});
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[c], o[d], 0, 0, 0);
-      }
-    }
-    if (tail && __any(odd)) {
-      // and added here
-      for (int key = 0; key < KT; ++key) {
-        float have = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) have = e == key / 8 * 4 + key % 4 ? x[e] : have;
-        const float pk = __shfl(have, r + 32 * (key / 4 & 1), WAVE);
-        const bool vis = sees(key);
-        const int vx = w * KT + key;
-#pragma unroll
-        for (int d = 0; d < OT; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int dim = 32 * d + 8 * (e / 4) + 4 * s + e % 4;
-            const float v = bf2f(*reinterpret_cast<const uint16_t*>(vs + vx * DH * 2 + ((dim / 8) ^ swz_v<DH>(vx)) * 16 + dim % 8 * 2));
-            if (vis && not_finite(v)) o[d][e] += pk * v;
-          }
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, v8i16{x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]});
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[c], o[d], 0, 0, 0);
       }
     }
   };
 
+  // units of whole prefix steps first, then the others, in code of their own: a split's units come in order
   fetch(0);
-  for (int i = 0; i < units; ++i) {
+  int i = 0;
+  for (; i < units && 2 * (j.sp + n_live * i + 1) * KT <= L; ++i) {
     // the buffer written here was last read two units ago, before the previous barrier
     store(i & 1);
-    now[0] = next[0];
-    now[1] = next[1];
+    __syncthreads();
+    fetch(i + 1);
+    if (!tile_live) continue;
+    for (int w = kpart; w < 2; w += KH) compute(std::true_type{}, i & 1, w, 0, false);
+  }
+  for (; i < units; ++i) {
+    store(i & 1);
     __syncthreads();
     fetch(i + 1);
     if (!tile_live) continue;
     const int st = 2 * (j.sp + n_live * i);
-    for (int w = kpart; w < 2; w += KH)
-      if (st + w < steps) compute(i & 1, st + w, w);
+    for (int w = kpart; w < 2 && st + w < steps; w += KH) {
+      const Span at_step = span(st + w);
+      const bool tail = st + w >= j.reach.prefix_steps;
+      const int count = at_step.last - at_step.key0 + 1;
+      uint32_t seen = count >= KT ? ~0u : (1u << count) - 1;
+      if (tail) seen &= words[(at_step.key0 - L) / KT];
+      compute(std::false_type{}, i & 1, w, seen, tail);
+    }
+  }
+  if (__any(odd)) {
+    // (whatever its weight, an infinite value makes the output infinite, and NaN makes it NaN)
+    for (int st = j.reach.prefix_steps; st < steps; ++st) {
+      if (st / 2 % n_live != j.sp || st % 2 % KH != kpart) continue;       // not this wave's step
+      const Span at_step = span(st);
+      for (int key = at_step.key0; key <= at_step.last; ++key) {
+        const bool vis = words[(key - L) / KT] >> (key - L) % KT & 1;
+#pragma unroll
+        for (int d = 0; d < OT; ++d)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const C* src = vb + (int64_t)key * DH + 32 * d + 8 * c + 4 * s;
+            f32x4 v;
+            if constexpr (CODES) v = __builtin_bit_cast(f32x4, decode4<C>(*reinterpret_cast<const uint32_t*>(src)));
+            else v = f32x4{bf2f(src[0]), bf2f(src[1]), bf2f(src[2]), bf2f(src[3])};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (vis && not_finite(v[e])) o[d][4 * c + e] += v[e];
+          }
+      }
+    }
   }
 
   sm.l = xor32_add(sm.l);
