@@ -30,7 +30,7 @@ constexpr int KA_UNIT = 64;       // keys that a workgroup takes at a time, and 
 
 // How a launch covers rows and keys.  A workgroup holds `tiles` tiles of 32 rows (fp32: one).
 struct KvSide {
-  int tiles, blocks;              // tiles of a workgroup; workgroups side by side for one head's rows
+  int tiles, blocks;              // tiles of a workgroup (1, 2 or 4); workgroups side by side for one head's rows
   int splits, per;                // of the keys; units of a split at least
 };
 struct KvPlan {
@@ -163,100 +163,283 @@ __device__ __forceinline__ float part_weight(float m, float l, float M) {
 }
 
 // ---------------------------------------------------------------------------- bf16 rows
-// A unit of 64 keys, K and V, comes into LDS once for the workgroup (eight bits turned into bf16 on the
-// way), the next one on its way into registers meanwhile.  A wave takes one tile of 32 rows through both
-// 32-key steps of a unit, or, where the job has two tiles only, through one of them:
+// A wave takes a tile of 32 rows through the keys, 32 of them a step:
 //   S^T[key][row] = K Q^T  (32 x 32 x 16 MFMA; lane (r, s) = (lane % 32, lane / 32) holds row r's scores of
 //                           keys 8 c + 4 s + e, c and e < 4),
-//   O^T[dim][row] += V^T P^T  (V by transpose loads, its keys in the order in which the lanes hold P).
-// A row's scores lie in two lanes, so its maximum takes one exchange; 32 rows a wave halve the LDS reads
-// that 16 would need, which are as long as the products.  LDS rows are padded so that what half a wave
-// reads at once falls on distinct banks (K: 16 rows of 16 bytes; V: 4 rows of 64), and every operand lies
-// at a constant distance from one address (swizzled rows took some 25 registers of addresses).
+//   O^T[dim][row] += V^T P^T  (V by transpose loads from LDS, its keys in the order in which lanes hold P).
+// A row's scores lie in two lanes, so its maximum takes one exchange, and 32 rows a wave halve the LDS
+// reads that 16 would need.
+template <int DH>
+struct RowTile {
+  static constexpr int KS = DH / 16, OT = DH / 32;
+  bf16x8 q[KS];
+  f32x16 o[OT];
+  float m = -INFINITY, l = 0.f;    // running maximum (log2 domain), this lane's share of the sum
+  bool odd = false;                // a value of the tail was not finite
+};
+// LDS rows, padded so that what half a wave reads at once falls on distinct banks (K: 16 rows of 16
+// bytes; V: 4 rows of 64), and every operand lies at a constant distance from one address (swizzled
+// rows took some 25 registers of addresses).
+template <int DH>
+constexpr int K_PITCH = DH * 2 + 16;
+template <int DH>
+constexpr int V_PITCH = DH * 2 + 64;
+
+template <int N>
+__device__ __forceinline__ float max_of(const f32x16 (&x)[N]) {
+  float m[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    m[u] = x[0][u];
+#pragma unroll
+    for (int e = u == 0 ? 4 : 4 + u; e < 16 * N; e += 4) m[u] = fmaxf(m[u], x[e / 16][e % 16]);
+  }
+  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
+// N steps at once.  k(n, f): the K operands of step n; ks, vs: LDS, the scales of this lane's keys (those of
+// the keys times the softmax's, in log2); v: LDS, this lane's first transpose load.  Where not WHOLE: the
+// keys that the row sees (bit i: key i), and whether a step is of the tail, whose values alone may be
+// kept from a row.
+template <typename C, int DH, bool WHOLE, int N, class K, class Then>
+__device__ __forceinline__ void take_steps(RowTile<DH>& t, float scale_log2, K k, Then then, const float* ks, const float* vs,
+                                           const unsigned char* v, const uint32_t (&seen)[N], const bool (&tail)[N], int s) {
+  constexpr int KS = DH / 16, OT = DH / 32, VP = V_PITCH<DH>;
+  constexpr bool CODES = EIGHT<C>;
+  f32x16 x[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    bf16x8 f[KS];
+    k(n, f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[n][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) x[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], t.q[i], x[n], 0, 0, 0);
+  }
+  then();
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if constexpr (CODES) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const f32x4 by = *reinterpret_cast<const f32x4*>(ks + 32 * n + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[n][4 * c + e] *= by[e];
+      }
+    }
+    if constexpr (!WHOLE) {
+      // bit 8 c + e, after the shift: this lane's score 4 c + e
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[n][e] = seen[n] >> 4 * s >> (e / 4 * 8 + e % 4) & 1 ? x[n][e] : -INFINITY;
+    }
+  }
+  const float mx = xor32_max(max_of(x));
+  const float m_new = fmaxf(t.m, CODES ? mx : mx * scale_log2);
+  const float m_use = m_new == -INFINITY ? 0.f : m_new;       // nothing seen yet: weights 0, not NaN
+  const float alpha = m_new == t.m ? 1.f : exp2_hw(t.m - m_use);
+  t.m = m_new;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      x[n][e] = exp2_hw(CODES ? x[n][e] - m_use : fmaf(x[n][e], scale_log2, -m_use));
+      sum[e % 4] += x[n][e];
+    }
+  t.l = t.l * alpha + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (!__all(alpha == 1.f)) {
+#pragma unroll
+    for (int d = 0; d < OT; ++d) t.o[d] *= alpha;
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if constexpr (CODES) {
+      // (a slot the row does not see may have any scale)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const f32x4 by = *reinterpret_cast<const f32x4*>(vs + 32 * n + 8 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[n][4 * c + e] = WHOLE || (seen[n] >> 4 * s >> (8 * c + e) & 1) ? x[n][4 * c + e] * by[e] : 0.f;
+      }
+    }
+    bf16x8 pb[2];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) pb[e / 8][e % 8] = (__bf16)x[n][e];
+    // lane i of a 16-lane group that addresses row k0 + i / 4, dims d0 + 4 (i % 4)..+3 gets V[k0 + 0..3][d0 + i]
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int d = 0; d < OT; ++d) {
+        v4i16 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(v + (32 * n + 16 * c) * VP + d * 64));
+        v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(v + (32 * n + 16 * c + 8) * VP + d * 64));
+        if (!WHOLE && tail[n]) {
+          // a value that is not finite may only meet the rows that see it: it is taken out here, and added
+          // when all keys are done
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool b0 = (x0[e] & 0x7f80) == 0x7f80, b1 = (x1[e] & 0x7f80) == 0x7f80;
+            x0[e] = b0 ? 0 : x0[e];
+            x1[e] = b1 ? 0 : x1[e];
+            t.odd |= b0 | b1;
+          }
+        }
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, v8i16{x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]});
+        t.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[c], t.o[d], 0, 0, 0);
+      }
+    }
+  }
+}
+// This lane's first transpose load of rows that start at `rows`.
+template <int DH>
+__device__ __forceinline__ const unsigned char* v_operand(const unsigned char* rows, int lane) {
+  return rows + (4 * (lane >> 5) + (lane & 15) / 4) * V_PITCH<DH> + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+}
+
+// 16 bytes of a row of K or V (elements e0..) into bf16 at `row` + 2 e0.
+template <typename C>
+__device__ __forceinline__ void put_bf16(unsigned char* at, u16x8 v) {
+  if constexpr (EIGHT<C>) {
+    const uint4 w = __builtin_bit_cast(uint4, v);
+    const u16x4 d0 = decode4_bf16<C>(w.x), d1 = decode4_bf16<C>(w.y), d2 = decode4_bf16<C>(w.z), d3 = decode4_bf16<C>(w.w);
+    *reinterpret_cast<u16x8*>(at) = u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
+    *reinterpret_cast<u16x8*>(at + 16) = u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]};
+  } else {
+    *reinterpret_cast<u16x8*>(at) = v;
+  }
+}
+
+// What both forms of the attention work with.
 template <typename C, int DH>
-__global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan p, float* __restrict__ part_o,
-                                                               float* __restrict__ part_ml) {
-  constexpr int KT = 32, KS = DH / 16, OT = DH / 32;
+struct KeySource {
+  const C *k, *v;
+  const float *ks, *vs;
+  int L, total, prefix_steps, steps, sp, n_live;
+  __device__ __forceinline__ KeySource(const Job& j)
+      : L(j.reach.L), total(j.reach.total), prefix_steps(j.reach.prefix_steps), steps(j.reach.steps), sp(j.sp),
+        n_live(j.reach.live) {
+    const KvPart& p = *j.part;
+    k = (const C*)p.k + j.cache * p.sb + j.h * p.sh;
+    v = (const C*)p.v + j.cache * p.sb + j.h * p.sh;
+    ks = EIGHT<C> ? p.ks + j.cache * p.ssb + j.h * p.ssh : nullptr;
+    vs = EIGHT<C> ? p.vs + j.cache * p.ssb + j.h * p.ssh : nullptr;
+  }
+  // A step's first key, and the last key of the prefix or tail that it lies in (a step past the end has none:
+  // last < key0).
+  struct Span {
+    int key0, last;
+  };
+  __device__ __forceinline__ Span span(int st) const {
+    if (st >= steps) return Span{0, -1};
+    if (st >= prefix_steps) return Span{L + (st - prefix_steps) * 32, total - 1};
+    return Span{st * 32, L - 1};
+  }
+  // the step's keys that a row of mask `words` sees
+  __device__ __forceinline__ uint32_t seen(int st, const uint32_t* words) const {
+    const Span at = span(st);
+    const int count = at.last - at.key0 + 1;
+    const uint32_t have = count >= 32 ? ~0u : (1u << max(count, 0)) - 1;
+    return st >= prefix_steps && st < steps ? have & words[st - prefix_steps] : have;
+  }
+};
+
+// Adds the values of a tail step that are not finite to the rows that see them (whatever its weight, an
+// infinite value makes the output infinite, and NaN makes it NaN).
+template <typename C, int DH>
+__device__ __forceinline__ void add_odd_values(RowTile<DH>& t, const KeySource<C, DH>& src, int st, const uint32_t* words, int s) {
+  const auto at = src.span(st);
+  for (int key = at.key0; key <= min(at.last, at.key0 + 31); ++key) {
+    const bool vis = words[st - src.prefix_steps] >> (key - at.key0) & 1;
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const C* p = src.v + (int64_t)key * DH + 32 * d + 8 * c + 4 * s;
+        f32x4 v;
+        if constexpr (EIGHT<C>) v = __builtin_bit_cast(f32x4, decode4<C>(*reinterpret_cast<const uint32_t*>(p)));
+        else v = f32x4{bf2f(p[0]), bf2f(p[1]), bf2f(p[2]), bf2f(p[3])};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (vis && not_finite(v[e])) t.o[d][4 * c + e] += v[e];
+      }
+  }
+}
+
+// Where a row's result goes: the output, if its keys were all in this job, else a partial result.
+struct RowOut {
+  bool direct;
+  int64_t at;
+};
+__device__ __forceinline__ RowOut row_out(const KvAttn& a, const KvPlan& p, const Job& j, const RowAt& at) {
+  if (!j.pre && j.reach.live == 1 && pre_reach<32>(a, p, at.b).live == 0) return {true, at.q(a, j.h)};
+  return {false, at.part(a, p, j.h, j.pre ? p.own.splits + j.sp : j.sp)};
+}
+// Outputs 32 d + 8 c + 4 s.. of a row.
+__device__ __forceinline__ void put_out(const KvAttn& a, const RowOut& to, int dim, f32x4 o, float inv, float* part_o) {
+  if (to.direct) store4((uint16_t*)a.out + to.at + dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  else *reinterpret_cast<f32x4*>(part_o + to.at * a.Dh + dim) = o;
+}
+
+// Many rows: a unit of 64 keys, K and V, comes into LDS once for the workgroup (eight bits turned into
+// bf16 on the way), the next one on its way into registers meanwhile; a wave takes its tile through both
+// steps of a unit, or, where the job has two tiles only, through one of them.
+template <typename C, int DH, int TILES>
+__device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, const Job& j, const int* first, unsigned char* smem,
+                                              float* part_o, float* part_ml) {
+  constexpr int KT = 32, KS = DH / 16, OT = DH / 32, KH = KA_WAVES / TILES, N = 2 / KH, KP = K_PITCH<DH>, VP = V_PITCH<DH>;
   constexpr int EPL = 16 / (int)sizeof(C), CPL = DH / EPL;         // elements of a load, loads of a row
   constexpr int LOADS = KA_UNIT * CPL / KA_THREADS;
-  constexpr int KP = DH * 2 + 16, VP = DH * 2 + 64;                // bytes of an LDS row of K, of V
-  constexpr int BYTES = KA_UNIT * (KP + VP);                       // a unit in LDS
+  constexpr int ROWS = KA_UNIT * (KP + VP), BYTES = ROWS + (EIGHT<C> ? 2 * KA_UNIT * 4 : 0);   // a unit: K, V, scales
   constexpr bool CODES = EIGHT<C>;
-  static_assert(2 * (OT * 16 + 2) * WAVE * 4 <= 2 * BYTES, "merge area");
-  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * BYTES];    // [buffer], K then V
-  __shared__ float scales[2][2][CODES ? KA_UNIT : 1];              // [buffer][K, V][key]
-  extern __shared__ int first[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
   const int r = lane & 31, s = lane >> 5;
-  Job j;
-  const int tiles = (int64_t)blockIdx.x < p.pre_jobs ? p.pre.tiles : p.own.tiles;
-  if (!take_job<KT>(a, p, 32 * tiles, first, j)) return;
-  const int tile = wave % tiles, kpart = wave / tiles, KH = KA_WAVES / tiles;
-  const int L = j.reach.L, total = j.reach.total, steps = j.reach.steps, n_live = j.reach.live;
+  const int tile = wave % TILES, kpart = wave / TILES;
+  const KeySource<C, DH> src(j);
+  const int n_live = src.n_live;
   const int units = max(0, (j.reach.units - j.sp + n_live - 1) / n_live);   // of this split: sp, sp + n_live, ...
-  const KvPart& part = *j.part;
-  const C* kb = (const C*)part.k + j.cache * part.sb + j.h * part.sh;
-  const C* vb = (const C*)part.v + j.cache * part.sb + j.h * part.sh;
-  const float* ksb = CODES ? part.ks + j.cache * part.ssb + j.h * part.ssh : nullptr;
-  const float* vsb = CODES ? part.vs + j.cache * part.ssb + j.h * part.ssh : nullptr;
   const float scale_log2 = a.scale * LOG2E;
 
-  bf16x8 q[KS];
+  RowTile<DH> t;
   const int row = j.r0 + tile * 32 + r;
   const bool mine = row < j.live, tile_live = j.r0 + tile * 32 < j.live;
   RowAt at{j.b, 0, 0};
   if (mine) at = row_at(a, j, row, first);
 #pragma unroll
-  for (int i = 0; i < KS; ++i) q[i] = bf16x8{};
+  for (int i = 0; i < KS; ++i) t.q[i] = bf16x8{};
   if (mine) {
-    const uint16_t* src = (const uint16_t*)a.q + at.q(a, j.h) + s * 8;
+    const uint16_t* q = (const uint16_t*)a.q + at.q(a, j.h) + s * 8;
 #pragma unroll
-    for (int i = 0; i < KS; ++i) q[i] = *reinterpret_cast<const bf16x8*>(src + i * 16);
+    for (int i = 0; i < KS; ++i) t.q[i] = *reinterpret_cast<const bf16x8*>(q + i * 16);
   }
+#pragma unroll
+  for (int d = 0; d < OT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t.o[d][e] = 0.f;
   // the row's mask, 32 tail slots a word: those of a step
   const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) + ((int64_t)at.b * a.nq_max + at.node) * 2 * ADT_MASK_WORDS;
 
-  // A step's first key and last (a step past the end has none: last < key0).
-  struct Span {
-    int key0, last;
-  };
-  auto span = [&](int st) {
-    if (st >= steps) return Span{0, -1};
-    if (st >= j.reach.prefix_steps) return Span{L + (st - j.reach.prefix_steps) * KT, total - 1};
-    return Span{st * KT, L - 1};
-  };
   // Load x of a unit takes row x / CPL, elements (x % CPL) * EPL..; thread t takes loads u * 256 + t.  Rows
   // past a step's last key read that one, or the head's first row, and are stored as zeros.
   u16x8 kr[LOADS], vr[LOADS];
   float sc = 0.f;
-  Span next0{0, -1}, next1{0, -1};
+  typename KeySource<C, DH>::Span next0{0, -1}, next1{0, -1};
   auto fetch = [&](int i) {
-    const int st = i < units ? 2 * (j.sp + n_live * i) : steps;
-    next0 = span(st);
-    next1 = span(st + 1);
+    const int st = i < units ? 2 * (j.sp + n_live * i) : src.steps;
+    next0 = src.span(st);
+    next1 = src.span(st + 1);
 #pragma unroll
     for (int u = 0; u < LOADS; ++u) {
       const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
       const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
       const int key = max(0, min(key0 + rx % KT, last));
-      kr[u] = *reinterpret_cast<const u16x8*>(kb + (int64_t)key * DH + c * EPL);
-      vr[u] = *reinterpret_cast<const u16x8*>(vb + (int64_t)key * DH + c * EPL);
+      kr[u] = *reinterpret_cast<const u16x8*>(src.k + (int64_t)key * DH + c * EPL);
+      vr[u] = *reinterpret_cast<const u16x8*>(src.v + (int64_t)key * DH + c * EPL);
     }
     if (CODES && tid < 2 * KA_UNIT) {
       const int rx = tid % KA_UNIT;
       const int key = (rx < KT ? next0.key0 : next1.key0) + rx % KT;
       sc = 0.f;
-      if (key <= (rx < KT ? next0.last : next1.last)) sc = tid < KA_UNIT ? ksb[key] * scale_log2 : vsb[key];
-    }
-  };
-  auto put = [&](unsigned char* row, int c, u16x8 v) {
-    if constexpr (CODES) {
-      const uint4 w = __builtin_bit_cast(uint4, v);
-      const u16x4 d0 = decode4_bf16<C>(w.x), d1 = decode4_bf16<C>(w.y), d2 = decode4_bf16<C>(w.z), d3 = decode4_bf16<C>(w.w);
-      *reinterpret_cast<u16x8*>(row + 32 * c) = u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
-      *reinterpret_cast<u16x8*>(row + 32 * c + 16) = u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]};
-    } else {
-      *reinterpret_cast<u16x8*>(row + 16 * c) = v;
+      if (key <= (rx < KT ? next0.last : next1.last)) sc = tid < KA_UNIT ? src.ks[key] * scale_log2 : src.vs[key];
     }
   };
   auto store = [&](int buf) {
@@ -267,199 +450,273 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
       const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
       const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
       if (!full && key0 + rx % KT > last) vr[u] = u16x8{};
-      put(to + rx * KP, c, kr[u]);
-      put(to + KA_UNIT * KP + rx * VP, c, vr[u]);
+      put_bf16<C>(to + rx * KP + c * EPL * 2, kr[u]);
+      put_bf16<C>(to + KA_UNIT * KP + rx * VP + c * EPL * 2, vr[u]);
     }
-    if (CODES && tid < 2 * KA_UNIT) scales[buf][tid / KA_UNIT][tid % KA_UNIT] = sc;
+    if (CODES && tid < 2 * KA_UNIT) reinterpret_cast<float*>(to + ROWS)[tid] = sc;
   };
-
-  f32x16 o[OT];
-  Softmax sm;
+  auto compute = [&](auto whole_tag, int buf, const uint32_t (&seen)[N], const bool (&tail)[N]) {
+    const unsigned char* base = smem + buf * BYTES;
+    const unsigned char* kl = base + (kpart * KT + r) * KP + s * 16;
+    const float* sl = reinterpret_cast<const float*>(base + ROWS) + kpart * KT + 4 * s;
+    take_steps<C, DH, decltype(whole_tag)::value, N>(
+        t, scale_log2,
+        [&](int n, bf16x8 (&f)[KS]) {
 #pragma unroll
-  for (int d = 0; d < OT; ++d)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-
-  bool odd = false;               // a value of the tail was not finite
-  // Step w of the unit in buffer `buf`: all of its keys, or those of `seen` (bit i: key i), of whose values
-  // only a tail's may be kept from a row.
-  auto compute = [&](auto whole_tag, int buf, int w, uint32_t seen, bool tail) {
-    constexpr bool WHOLE = decltype(whole_tag)::value;
-    // this lane's part of the first 16 dims of its key, and of the first transpose load
-    const unsigned char* ks = smem + buf * BYTES + (w * KT + r) * KP + s * 16;
-    const unsigned char* vs = smem + buf * BYTES + KA_UNIT * KP + (w * KT + 4 * s + (lane & 15) / 4) * VP +
-                              (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-    f32x16 x;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = 0.f;
-    bf16x8 f[KS];
-#pragma unroll
-    for (int i = 0; i < KS; ++i) f[i] = *reinterpret_cast<const bf16x8*>(ks + i * 32);
-    __builtin_amdgcn_sched_barrier(0);       // all of them requested before the first product
-#pragma unroll
-    for (int i = 0; i < KS; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], q[i], x, 0, 0, 0);
-    seen >>= 4 * s;                 // bit 8 c + e: this lane's score 4 c + e
-    if constexpr (CODES) {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const f32x4 by = *reinterpret_cast<const f32x4*>(&scales[buf][0][w * KT + 8 * c + 4 * s]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * c + e] *= by[e];
-      }
-    }
-    if constexpr (!WHOLE) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = seen >> (e / 4 * 8 + e % 4) & 1 ? x[e] : -INFINITY;
-    }
-    float mx = x[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) mx = fmaxf(mx, x[e]);
-    mx = xor32_max(mx);
-    float m_use;
-    const float alpha = sm.raise(CODES ? mx : mx * scale_log2, m_use);
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      x[e] = exp2_hw(CODES ? x[e] - m_use : fmaf(x[e], scale_log2, -m_use));
-      sum += x[e];
-    }
-    sm.l = sm.l * alpha + sum;
-    if (!__all(alpha == 1.f)) {
-#pragma unroll
-      for (int d = 0; d < OT; ++d) o[d] *= alpha;
-    }
-    if constexpr (CODES) {
-      // (a slot the row does not see may have any scale)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const f32x4 by = *reinterpret_cast<const f32x4*>(&scales[buf][1][w * KT + 8 * c + 4 * s]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * c + e] = WHOLE || (seen >> (8 * c + e) & 1) ? x[4 * c + e] * by[e] : 0.f;
-      }
-    }
-    bf16x8 pb[2];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) pb[e / 8][e % 8] = (__bf16)x[e];
-    // lane i of a 16-lane group that addresses row k0 + i / 4, dims d0 + 4 (i % 4)..+3 gets V[k0 + 0..3][d0 + i]
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-#pragma unroll
-      for (int d = 0; d < OT; ++d) {
-        v4i16 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + 16 * c * VP + d * 64));
-        v4i16 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(vs + (16 * c + 8) * VP + d * 64));
-        if (!WHOLE && tail) {
-          // a value that is not finite may only meet the rows that see it: it is taken out here, and added
-          // when all keys are done
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const bool b0 = (x0[e] & 0x7f80) == 0x7f80, b1 = (x1[e] & 0x7f80) == 0x7f80;
-            x0[e] = b0 ? 0 : x0[e];
-            x1[e] = b1 ? 0 : x1[e];
-            odd |= b0 | b1;
-          }
-        }
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, v8i16{x0[0], x0[1], x0[2], x0[3], x1[0], x1[1], x1[2], x1[3]});
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pb[c], o[d], 0, 0, 0);
-      }
-    }
+          for (int i = 0; i < KS; ++i) f[i] = *reinterpret_cast<const bf16x8*>(kl + n * KT * KP + i * 32);
+          __builtin_amdgcn_sched_barrier(0);       // all of them requested before the first product
+        },
+        [] {}, sl, sl + KA_UNIT, v_operand<DH>(base + KA_UNIT * KP + kpart * KT * VP, lane), seen, tail, s);
   };
 
   // units of whole prefix steps first, then the others, in code of their own: a split's units come in order
   fetch(0);
   int i = 0;
-  for (; i < units && 2 * (j.sp + n_live * i + 1) * KT <= L; ++i) {
+  for (; i < units && 2 * (j.sp + n_live * i + 1) * KT <= src.L; ++i) {
     // the buffer written here was last read two units ago, before the previous barrier
     store(i & 1);
     __syncthreads();
     fetch(i + 1);
-    if (!tile_live) continue;
-    for (int w = kpart; w < 2; w += KH) compute(std::true_type{}, i & 1, w, 0, false);
+    if (tile_live) compute(std::true_type{}, i & 1, {}, {});
   }
   for (; i < units; ++i) {
     store(i & 1);
     __syncthreads();
     fetch(i + 1);
     if (!tile_live) continue;
-    const int st = 2 * (j.sp + n_live * i);
-    for (int w = kpart; w < 2 && st + w < steps; w += KH) {
-      const Span at_step = span(st + w);
-      const bool tail = st + w >= j.reach.prefix_steps;
-      const int count = at_step.last - at_step.key0 + 1;
-      uint32_t seen = count >= KT ? ~0u : (1u << count) - 1;
-      if (tail) seen &= words[(at_step.key0 - L) / KT];
-      compute(std::false_type{}, i & 1, w, seen, tail);
+    const int st = 2 * (j.sp + n_live * i) + kpart;
+    uint32_t seen[N];
+    bool tail[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      seen[n] = src.seen(st + n, words);
+      tail[n] = st + n >= src.prefix_steps;
     }
+    compute(std::false_type{}, i & 1, seen, tail);
   }
-  if (__any(odd)) {
-    // (whatever its weight, an infinite value makes the output infinite, and NaN makes it NaN)
-    for (int st = j.reach.prefix_steps; st < steps; ++st) {
-      if (st / 2 % n_live != j.sp || st % 2 % KH != kpart) continue;       // not this wave's step
-      const Span at_step = span(st);
-      for (int key = at_step.key0; key <= at_step.last; ++key) {
-        const bool vis = words[(key - L) / KT] >> (key - L) % KT & 1;
-#pragma unroll
-        for (int d = 0; d < OT; ++d)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const C* src = vb + (int64_t)key * DH + 32 * d + 8 * c + 4 * s;
-            f32x4 v;
-            if constexpr (CODES) v = __builtin_bit_cast(f32x4, decode4<C>(*reinterpret_cast<const uint32_t*>(src)));
-            else v = f32x4{bf2f(src[0]), bf2f(src[1]), bf2f(src[2]), bf2f(src[3])};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (vis && not_finite(v[e])) o[d][4 * c + e] += v[e];
-          }
-      }
-    }
+  if (__any(t.odd)) {
+    for (int st = src.prefix_steps; st < src.steps; ++st)
+      if (st / 2 % n_live == j.sp && st % 2 % KH == kpart) add_odd_values(t, src, st, words, s);
   }
 
-  sm.l = xor32_add(sm.l);
-  if (KH > 1) {
+  t.l = xor32_add(t.l);
+  if constexpr (KH > 1) {
     // the second wave of a tile passes its state through LDS to the first
+    static_assert(TILES * (OT * 16 + 2) * WAVE * 4 <= 2 * ROWS, "merge area");
     float* mo = reinterpret_cast<float*>(smem) + (size_t)tile * (OT * 16 + 2) * WAVE;
     __syncthreads();
     if (kpart == 1) {
 #pragma unroll
       for (int d = 0; d < OT; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) mo[(d * 16 + e) * WAVE + lane] = o[d][e];
-      mo[OT * 16 * WAVE + lane] = sm.m;
-      mo[(OT * 16 + 1) * WAVE + lane] = sm.l;
+        for (int e = 0; e < 16; ++e) mo[(d * 16 + e) * WAVE + lane] = t.o[d][e];
+      mo[OT * 16 * WAVE + lane] = t.m;
+      mo[(OT * 16 + 1) * WAVE + lane] = t.l;
     }
     __syncthreads();
     if (kpart == 1) return;
-    const float m1 = mo[OT * 16 * WAVE + lane], l1 = mo[(OT * 16 + 1) * WAVE + lane], M = fmaxf(sm.m, m1);
-    const float w0 = part_weight(sm.m, sm.l, M), w1 = part_weight(m1, l1, M);
+    const float m1 = mo[OT * 16 * WAVE + lane], l1 = mo[(OT * 16 + 1) * WAVE + lane], M = fmaxf(t.m, m1);
+    const float w0 = part_weight(t.m, t.l, M), w1 = part_weight(m1, l1, M);
     // (a part of weight 0 adds nothing, whatever it holds; unless its sum is NaN)
 #pragma unroll
     for (int d = 0; d < OT; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float y = mo[(d * 16 + e) * WAVE + lane];
-        o[d][e] = (w0 == 0.f ? 0.f : o[d][e] * w0) + (w1 == 0.f ? 0.f : y * w1);
+        t.o[d][e] = (w0 == 0.f ? 0.f : t.o[d][e] * w0) + (w1 == 0.f ? 0.f : y * w1);
       }
-    sm.l = (w0 == 0.f && sm.l == sm.l ? 0.f : sm.l * w0) + (w1 == 0.f && l1 == l1 ? 0.f : l1 * w1);
-    sm.m = M;
+    t.l = (w0 == 0.f && t.l == t.l ? 0.f : t.l * w0) + (w1 == 0.f && l1 == l1 ? 0.f : l1 * w1);
+    t.m = M;
   }
   if (!mine) return;
-  if (!j.pre && n_live == 1 && pre_reach<KT>(a, p, at.b).live == 0) {
-    const float inv = sm.l == 0.f ? 0.f : 1.f / sm.l;
-    uint16_t* to = (uint16_t*)a.out + at.q(a, j.h);
-#pragma unroll
-    for (int d = 0; d < OT; ++d)
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        store4(to + 32 * d + 8 * c + 4 * s, o[d][4 * c] * inv, o[d][4 * c + 1] * inv, o[d][4 * c + 2] * inv, o[d][4 * c + 3] * inv);
-    return;
-  }
-  const int64_t to = at.part(a, p, j.h, j.pre ? p.own.splits + j.sp : j.sp);
+  const RowOut to = row_out(a, p, j, at);
+  const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
 #pragma unroll
   for (int d = 0; d < OT; ++d)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-      *reinterpret_cast<f32x4*>(part_o + to * DH + 32 * d + 8 * c + 4 * s) =
-          f32x4{o[d][4 * c], o[d][4 * c + 1], o[d][4 * c + 2], o[d][4 * c + 3]};
-  if (s == 0) *reinterpret_cast<float2*>(part_ml + to * 2) = make_float2(sm.m, sm.l);
+      put_out(a, to, 32 * d + 8 * c + 4 * s, f32x4{t.o[d][4 * c], t.o[d][4 * c + 1], t.o[d][4 * c + 2], t.o[d][4 * c + 3]}, inv, part_o);
+  if (!to.direct && s == 0) *reinterpret_cast<float2*>(part_ml + to.at * 2) = make_float2(t.m, t.l);
+}
+
+// Up to 32 rows: the waves take steps of their own, with no barrier between them.  K comes straight into the
+// operands' registers (eight bits: 16 codes a load, so that an operand's dims lie in pairs of 8, the
+// queries' alike), V through rows of LDS that are the wave's own; P steps are in flight.  The waves'
+// results meet in LDS, in their order.
+template <typename C, int DH>
+__device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, const Job& j, const int* first, unsigned char* smem,
+                                           float* part_o, float* part_ml) {
+  constexpr int KT = 32, KS = DH / 16, OT = DH / 32, VP = V_PITCH<DH>;
+  constexpr bool CODES = EIGHT<C>;
+  constexpr int P = CODES ? 2 : 1;
+  constexpr int EPL = 16 / (int)sizeof(C), CPL = DH / EPL;         // elements of a load, loads of a row
+  constexpr int LOADS = KT * CPL / WAVE;                           // of a step, K or V
+  constexpr int OWN = KT * VP + 2 * KT * 4;                        // a wave's LDS: V, scales
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
+  const int r = lane & 31, s = lane >> 5;
+  const KeySource<C, DH> src(j);
+  const float scale_log2 = a.scale * LOG2E;
+
+  RowTile<DH> t;
+  const int row = j.r0 + r;
+  const bool mine = row < j.live;
+  RowAt at{j.b, 0, 0};
+  if (mine) at = row_at(a, j, row, first);
+#pragma unroll
+  for (int i = 0; i < KS; ++i) t.q[i] = bf16x8{};
+  if (mine) {
+    const uint16_t* q = (const uint16_t*)a.q + at.q(a, j.h);
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      t.q[i] = *reinterpret_cast<const bf16x8*>(q + (CODES ? i / 2 * 32 + s * 16 + i % 2 * 8 : i * 16 + s * 8));
+  }
+#pragma unroll
+  for (int d = 0; d < OT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t.o[d][e] = 0.f;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) + ((int64_t)at.b * a.nq_max + at.node) * 2 * ADT_MASK_WORDS;
+  unsigned char* rows = smem + wave * OWN;
+  float* sl = reinterpret_cast<float*>(rows + KT * VP);
+
+  u16x8 kr[P][LOADS], vr[P][LOADS];
+  float sc[P];
+  const int stride = src.n_live * KA_WAVES;
+  // (a step past the end reads the head's first row, so the loads in flight are the same on every path)
+  auto fetch = [&](int u, int st) {
+    const auto at = src.span(st);
+    const C* kp = src.k + (int64_t)max(0, min(at.key0 + r, at.last)) * DH + s * EPL;
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) kr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u16x8*>(kp + x * 2 * EPL));
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int y = x * WAVE + lane, key = max(0, min(at.key0 + y / CPL, at.last));
+      vr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u16x8*>(src.v + (int64_t)key * DH + y % CPL * EPL));
+    }
+    if (CODES) {
+      const int key = max(0, min(at.key0 + r, at.last));
+      sc[u] = s ? src.vs[key] : src.ks[key];
+    }
+  };
+  auto step = [&](auto whole_tag, int u, int st) {
+    constexpr bool WHOLE = decltype(whole_tag)::value;
+    const auto span = src.span(st);
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int y = x * WAVE + lane;
+      if (!WHOLE && span.key0 + y / CPL > span.last) vr[u][x] = u16x8{};
+      put_bf16<C>(rows + y / CPL * VP + y % CPL * EPL * 2, vr[u][x]);
+    }
+    if (CODES) sl[lane] = s ? (WHOLE || span.key0 + r <= span.last ? sc[u] : 0.f) : sc[u] * scale_log2;
+    wave_lds_fence();
+    const uint32_t seen[1] = {WHOLE ? 0u : src.seen(st, words)};
+    const bool tail[1] = {!WHOLE && st >= src.prefix_steps};
+    take_steps<C, DH, WHOLE, 1>(
+        t, scale_log2,
+        [&](int, bf16x8 (&f)[KS]) {
+          if constexpr (CODES) {
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) {
+              const uint4 w = __builtin_bit_cast(uint4, kr[u][x]);
+              const u16x4 d0 = decode4_bf16<C>(w.x), d1 = decode4_bf16<C>(w.y), d2 = decode4_bf16<C>(w.z), d3 = decode4_bf16<C>(w.w);
+              f[2 * x] = __builtin_bit_cast(bf16x8, u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]});
+              f[2 * x + 1] = __builtin_bit_cast(bf16x8, u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]});
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < LOADS; ++x) f[x] = __builtin_bit_cast(bf16x8, kr[u][x]);
+          }
+        },
+        [&] { fetch(u, st + P * stride); }, sl + 4 * s, sl + KT + 4 * s, v_operand<DH>(rows, lane), seen, tail, s);
+    wave_lds_fence();
+  };
+
+  int st = j.sp * KA_WAVES + wave;
+#pragma unroll
+  for (int u = 0; u < P; ++u) {
+    fetch(u, st + u * stride);
+    __builtin_amdgcn_sched_barrier(0);     // (in order, or the first one used could be the last to arrive)
+  }
+  const int whole = src.L / KT;
+  auto loop = [&](auto whole_tag, int end) {
+    // (P steps a round: the registers of a step go by its place in the round)
+    for (;;) {
+#pragma unroll
+      for (int u = 0; u < P; ++u) {
+        if (st >= end) return u;
+        step(whole_tag, u, st);
+        st += stride;
+      }
+    }
+  };
+  int u = loop(std::true_type{}, whole);
+  if constexpr (P == 2) {
+    if (u == 1 && st < src.steps) {
+      step(std::false_type{}, 1, st);
+      st += stride;
+    }
+  }
+  loop(std::false_type{}, src.steps);
+  if (__any(t.odd)) {
+    for (int x = j.sp * KA_WAVES + wave; x < src.steps; x += stride)
+      if (x >= src.prefix_steps) add_odd_values(t, src, x, words, s);
+  }
+
+  // merge: wave w takes the outputs 32 w.. of all
+  t.l = xor32_add(t.l);
+  static_assert(KA_WAVES >= OT, "a wave for each 32 outputs");
+  float* mo = reinterpret_cast<float*>(smem);                       // [wave][OT * 16 outputs, m, l][lane]
+  constexpr int EACH = (OT * 16 + 2) * WAVE;
+  __syncthreads();
+#pragma unroll
+  for (int d = 0; d < OT; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mo[wave * EACH + (d * 16 + e) * WAVE + lane] = t.o[d][e];
+  mo[wave * EACH + OT * 16 * WAVE + lane] = t.m;
+  mo[wave * EACH + (OT * 16 + 1) * WAVE + lane] = t.l;
+  __syncthreads();
+  if (wave >= OT || !mine) return;
+  float m[KA_WAVES], l[KA_WAVES], M = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < KA_WAVES; ++w) {
+    m[w] = mo[w * EACH + OT * 16 * WAVE + lane];
+    l[w] = mo[w * EACH + (OT * 16 + 1) * WAVE + lane];
+    M = fmaxf(M, m[w]);
+  }
+  f32x16 o;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < KA_WAVES; ++w) {
+    const float wt = part_weight(m[w], l[w], M);
+    if (wt == 0.f && l[w] == l[w]) continue;
+    sum += wt * l[w];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] += wt * mo[w * EACH + (wave * 16 + e) * WAVE + lane];
+  }
+  const RowOut to = row_out(a, p, j, at);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) put_out(a, to, 32 * wave + 8 * c + 4 * s, f32x4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]}, inv, part_o);
+  if (!to.direct && wave == 0 && s == 0) *reinterpret_cast<float2*>(part_ml + to.at * 2) = make_float2(M, sum);
+}
+
+template <typename C, int DH>
+constexpr int SHARED_BYTES = 2 * (KA_UNIT * (K_PITCH<DH> + V_PITCH<DH>) + (EIGHT<C> ? 2 * KA_UNIT * 4 : 0));
+template <int DH>
+constexpr int FEW_BYTES = KA_WAVES * (DH / 2 + 2) * WAVE * 4;      // (the merge takes more than the steps)
+
+template <typename C, int DH>
+__global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan p, float* __restrict__ part_o,
+                                                               float* __restrict__ part_ml) {
+  static_assert(FEW_BYTES<DH> <= SHARED_BYTES<C, DH> && KA_WAVES * (32 * V_PITCH<DH> + 256) <= FEW_BYTES<DH>, "LDS");
+  __shared__ __attribute__((aligned(16))) unsigned char smem[SHARED_BYTES<C, DH>];
+  extern __shared__ int first[];
+  Job j;
+  const int tiles = (int64_t)blockIdx.x < p.pre_jobs ? p.pre.tiles : p.own.tiles;
+  if (!take_job<32>(a, p, 32 * tiles, first, j)) return;
+  if (tiles == 1) attend_few<C, DH>(a, p, j, first, smem, part_o, part_ml);
+  else if (tiles == 2) attend_shared<C, DH, 2>(a, p, j, first, smem, part_o, part_ml);
+  else attend_shared<C, DH, 4>(a, p, j, first, smem, part_o, part_ml);
 }
 
 // ---------------------------------------------------------------------------- fp32 rows
@@ -688,7 +945,7 @@ static KvPlan kv_plan(const KvAttn& a) {
   KvPlan p{};
   const bool f32 = a.type == ADT_F32;
   auto side = [&](KvSide& s, int64_t rows) {
-    s.tiles = f32 ? 1 : rows <= 64 ? 2 : 4;
+    s.tiles = f32 || rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
     s.blocks = (int)((rows + 32 * s.tiles - 1) / (32 * s.tiles));
   };
   const int64_t rows = (int64_t)a.nq_max * a.G;
