@@ -56,7 +56,9 @@ __device__ __forceinline__ float4 decode4(uint32_t x) {
     return make_float4(__builtin_amdgcn_cvt_f32_fp8((int)x, 0), __builtin_amdgcn_cvt_f32_fp8((int)x, 1),
                        __builtin_amdgcn_cvt_f32_fp8((int)x, 2), __builtin_amdgcn_cvt_f32_fp8((int)x, 3));
   } else {
-    return make_float4((float)(int8_t)x, (float)(int8_t)(x >> 8), (float)(int8_t)(x >> 16), (float)(int8_t)(x >> 24));
+    // (bit fields of 32 bits: the conversions take their bytes themselves; casts to int8_t go by way of 16 bits)
+    auto code = [&](uint32_t at) { return (float)(int)__builtin_amdgcn_sbfe(x, at, 8); };
+    return make_float4(code(0), code(8), code(16), code(24));
   }
 }
 // The same as bf16, which holds every code exactly.

@@ -23,6 +23,7 @@ namespace adt {
 ADT_DEVICE_ERROR_WORD(kv_attn)
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KA_WAVES = 4;
 constexpr int KA_THREADS = KA_WAVES * WAVE;
@@ -192,10 +193,15 @@ __device__ __forceinline__ float max_of(const f32x16 (&x)[N]) {
   for (int u = 0; u < 4; ++u) {
     m[u] = x[0][u];
 #pragma unroll
-    for (int e = u == 0 ? 4 : 4 + u; e < 16 * N; e += 4) m[u] = fmaxf(m[u], x[e / 16][e % 16]);
+    for (int e = 4 + u; e < 16 * N; e += 4) m[u] = fmaxf(m[u], x[e / 16][e % 16]);
   }
   return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
+
+// A row's reference of the softmax: scores count as 2^(score - m).  It is the maximum of the first scores
+// that the row saw, and is raised only where a later one is larger by more than this (in log2), so
+// that outputs are hardly ever rescaled; weights then reach 2^8, which costs nothing in floating point.
+constexpr float SLACK = 8.f;
 
 // N steps at once.  k(n, f): the K operands of step n; ks, vs: LDS, the scales of this lane's keys (those of
 // the keys times the softmax's, in log2); v: LDS, this lane's first transpose load.  Where not WHOLE: the
@@ -217,15 +223,17 @@ __device__ __forceinline__ void take_steps(RowTile<DH>& t, float scale_log2, K k
     for (int i = 0; i < KS; ++i) x[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], t.q[i], x[n], 0, 0, 0);
   }
   then();
+  // scores less the row's reference, in log2
+  const bool fresh = t.m == -INFINITY;
+  const float ref = fresh ? 0.f : t.m;
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    if constexpr (CODES) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const f32x4 by = *reinterpret_cast<const f32x4*>(ks + 32 * n + 8 * c);
+    for (int c = 0; c < 4; ++c) {
+      f32x4 by{scale_log2, scale_log2, scale_log2, scale_log2};
+      if constexpr (CODES) by = *reinterpret_cast<const f32x4*>(ks + 32 * n + 8 * c);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[n][4 * c + e] *= by[e];
-      }
+      for (int e = 0; e < 4; ++e) x[n][4 * c + e] = fmaf(x[n][4 * c + e], by[e], -ref);
     }
     if constexpr (!WHOLE) {
       // bit 8 c + e, after the shift: this lane's score 4 c + e
@@ -233,24 +241,27 @@ __device__ __forceinline__ void take_steps(RowTile<DH>& t, float scale_log2, K k
       for (int e = 0; e < 16; ++e) x[n][e] = seen[n] >> 4 * s >> (e / 4 * 8 + e % 4) & 1 ? x[n][e] : -INFINITY;
     }
   }
-  const float mx = xor32_max(max_of(x));
-  const float m_new = fmaxf(t.m, CODES ? mx : mx * scale_log2);
-  const float m_use = m_new == -INFINITY ? 0.f : m_new;       // nothing seen yet: weights 0, not NaN
-  const float alpha = m_new == t.m ? 1.f : exp2_hw(t.m - m_use);
-  t.m = m_new;
+  const float over = xor32_max(max_of(x));
+  const bool raise = over > (fresh ? -INFINITY : SLACK);
+  if (__any(raise)) {
+    // (a row's first scores have nothing to rescale)
+    const float up = raise ? over : 0.f, factor = fresh ? 1.f : exp2_hw(-up);
+    if (raise) t.m = ref + up;
+    t.l *= factor;
+#pragma unroll
+    for (int d = 0; d < OT; ++d) t.o[d] *= factor;
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n] -= up;
+  }
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      x[n][e] = exp2_hw(CODES ? x[n][e] - m_use : fmaf(x[n][e], scale_log2, -m_use));
+      x[n][e] = exp2_hw(x[n][e]);
       sum[e % 4] += x[n][e];
     }
-  t.l = t.l * alpha + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
-  if (!__all(alpha == 1.f)) {
-#pragma unroll
-    for (int d = 0; d < OT; ++d) t.o[d] *= alpha;
-  }
+  t.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     if constexpr (CODES) {
@@ -296,16 +307,17 @@ __device__ __forceinline__ const unsigned char* v_operand(const unsigned char* r
   return rows + (4 * (lane >> 5) + (lane & 15) / 4) * V_PITCH<DH> + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
 }
 
-// 16 bytes of a row of K or V (elements e0..) into bf16 at `row` + 2 e0.
+// 16 bytes of a row of K or V into bf16 at `at`.
 template <typename C>
-__device__ __forceinline__ void put_bf16(unsigned char* at, u16x8 v) {
+__device__ __forceinline__ void put_bf16(unsigned char* at, u32x4 w) {
   if constexpr (EIGHT<C>) {
-    const uint4 w = __builtin_bit_cast(uint4, v);
-    const u16x4 d0 = decode4_bf16<C>(w.x), d1 = decode4_bf16<C>(w.y), d2 = decode4_bf16<C>(w.z), d3 = decode4_bf16<C>(w.w);
-    *reinterpret_cast<u16x8*>(at) = u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]};
-    *reinterpret_cast<u16x8*>(at + 16) = u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u16x4 lo = decode4_bf16<C>(w[2 * i]), hi = decode4_bf16<C>(w[2 * i + 1]);
+      *reinterpret_cast<u16x8*>(at + 16 * i) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
   } else {
-    *reinterpret_cast<u16x8*>(at) = v;
+    *reinterpret_cast<u32x4*>(at) = w;
   }
 }
 
@@ -420,7 +432,7 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
 
   // Load x of a unit takes row x / CPL, elements (x % CPL) * EPL..; thread t takes loads u * 256 + t.  Rows
   // past a step's last key read that one, or the head's first row, and are stored as zeros.
-  u16x8 kr[LOADS], vr[LOADS];
+  u32x4 kr[LOADS], vr[LOADS];
   float sc = 0.f;
   typename KeySource<C, DH>::Span next0{0, -1}, next1{0, -1};
   auto fetch = [&](int i) {
@@ -432,8 +444,8 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
       const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
       const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
       const int key = max(0, min(key0 + rx % KT, last));
-      kr[u] = *reinterpret_cast<const u16x8*>(src.k + (int64_t)key * DH + c * EPL);
-      vr[u] = *reinterpret_cast<const u16x8*>(src.v + (int64_t)key * DH + c * EPL);
+      kr[u] = *reinterpret_cast<const u32x4*>(src.k + (int64_t)key * DH + c * EPL);
+      vr[u] = *reinterpret_cast<const u32x4*>(src.v + (int64_t)key * DH + c * EPL);
     }
     if (CODES && tid < 2 * KA_UNIT) {
       const int rx = tid % KA_UNIT;
@@ -449,7 +461,7 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
     for (int u = 0; u < LOADS; ++u) {
       const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
       const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
-      if (!full && key0 + rx % KT > last) vr[u] = u16x8{};
+      if (!full && key0 + rx % KT > last) vr[u] = u32x4{};
       put_bf16<C>(to + rx * KP + c * EPL * 2, kr[u]);
       put_bf16<C>(to + KA_UNIT * KP + rx * VP + c * EPL * 2, vr[u]);
     }
@@ -578,7 +590,7 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
   unsigned char* rows = smem + wave * OWN;
   float* sl = reinterpret_cast<float*>(rows + KT * VP);
 
-  u16x8 kr[P][LOADS], vr[P][LOADS];
+  u32x4 kr[P][LOADS], vr[P][LOADS];
   float sc[P];
   const int stride = src.n_live * KA_WAVES;
   // (a step past the end reads the head's first row, so the loads in flight are the same on every path)
@@ -586,11 +598,11 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
     const auto at = src.span(st);
     const C* kp = src.k + (int64_t)max(0, min(at.key0 + r, at.last)) * DH + s * EPL;
 #pragma unroll
-    for (int x = 0; x < LOADS; ++x) kr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u16x8*>(kp + x * 2 * EPL));
+    for (int x = 0; x < LOADS; ++x) kr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + x * 2 * EPL));
 #pragma unroll
     for (int x = 0; x < LOADS; ++x) {
       const int y = x * WAVE + lane, key = max(0, min(at.key0 + y / CPL, at.last));
-      vr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u16x8*>(src.v + (int64_t)key * DH + y % CPL * EPL));
+      vr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src.v + (int64_t)key * DH + y % CPL * EPL));
     }
     if (CODES) {
       const int key = max(0, min(at.key0 + r, at.last));
@@ -603,7 +615,7 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
 #pragma unroll
     for (int x = 0; x < LOADS; ++x) {
       const int y = x * WAVE + lane;
-      if (!WHOLE && span.key0 + y / CPL > span.last) vr[u][x] = u16x8{};
+      if (!WHOLE && span.key0 + y / CPL > span.last) vr[u][x] = u32x4{};
       put_bf16<C>(rows + y / CPL * VP + y % CPL * EPL * 2, vr[u][x]);
     }
     if (CODES) sl[lane] = s ? (WHOLE || span.key0 + r <= span.last ? sc[u] : 0.f) : sc[u] * scale_log2;
@@ -616,10 +628,11 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
           if constexpr (CODES) {
 #pragma unroll
             for (int x = 0; x < LOADS; ++x) {
-              const uint4 w = __builtin_bit_cast(uint4, kr[u][x]);
-              const u16x4 d0 = decode4_bf16<C>(w.x), d1 = decode4_bf16<C>(w.y), d2 = decode4_bf16<C>(w.z), d3 = decode4_bf16<C>(w.w);
-              f[2 * x] = __builtin_bit_cast(bf16x8, u16x8{d0[0], d0[1], d0[2], d0[3], d1[0], d1[1], d1[2], d1[3]});
-              f[2 * x + 1] = __builtin_bit_cast(bf16x8, u16x8{d2[0], d2[1], d2[2], d2[3], d3[0], d3[1], d3[2], d3[3]});
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const u16x4 lo = decode4_bf16<C>(kr[u][x][2 * i]), hi = decode4_bf16<C>(kr[u][x][2 * i + 1]);
+                f[2 * x + i] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+              }
             }
           } else {
 #pragma unroll
