@@ -79,26 +79,27 @@ struct Job {
 // false: nothing to do.  Ends with a barrier where it is a prefix job.
 template <int KT>
 __device__ __forceinline__ bool take_job(const KvAttn& a, const KvPlan& p, int rows_each, int* first, Job& j) {
-  int64_t id = blockIdx.x;
-  j.pre = id < p.pre_jobs;
-  if (!j.pre) id -= p.pre_jobs;
+  uint32_t id = blockIdx.x;
+  j.pre = id < (uint32_t)p.pre_jobs;
+  if (!j.pre) id -= (uint32_t)p.pre_jobs;
   const KvSide& side = j.pre ? p.pre : p.own;
-  j.h = id % a.Hkv;
-  id /= a.Hkv;
-  const int block = id % side.blocks;
-  id /= side.blocks;
-  j.sp = id % side.splits;
-  const int at = id / side.splits;
+  j.h = id % (uint32_t)a.Hkv;
+  id /= (uint32_t)a.Hkv;
+  const int block = id % (uint32_t)side.blocks;
+  id /= (uint32_t)side.blocks;
+  j.sp = id % (uint32_t)side.splits;
+  const int at = id / (uint32_t)side.splits;
   j.cache = at;
   j.part = j.pre ? &a.pre : &a.own;
   j.r0 = block * rows_each;
   if (!j.pre) {
+    const int n_q = a.n_q[at], len = a.own.len[at], n_tail = a.n_tail[at];     // (one wait for all three)
     j.b = at;
-    j.live = rows_of(a, at);
-    if (j.r0 >= j.live) return false;
-    j.reach = own_reach<KT>(a, p, at);
-    if (threadIdx.x == 0 && (int64_t)a.own.len[at] + a.n_tail[at] > a.own.cap) dev_fail(DEVINV_KV_RANGE);
-    return j.sp < j.reach.live;
+    j.live = max(0, min(n_q, a.nq_max)) * a.G;
+    j.reach = reach_of<KT>(len, n_tail, a.own.cap, p.own, 1);
+    if (j.r0 >= j.live || j.sp >= j.reach.live) return false;
+    if (threadIdx.x == 0 && (int64_t)len + n_tail > a.own.cap) dev_fail(DEVINV_KV_RANGE);
+    return true;
   }
   j.b = at * a.group;
   j.reach = pre_reach<KT>(a, p, j.b);
@@ -393,7 +394,7 @@ __device__ __forceinline__ void put_out(const KvAttn& a, const RowOut& to, int d
 }
 
 // Many rows: a unit of 64 keys, K and V, comes into LDS once for the workgroup (eight bits turned into
-// bf16 on the way), the next one on its way into registers meanwhile; a wave takes its tile through both
+// bf16 on the way), the next P on their way into registers meanwhile; a wave takes its tile through both
 // steps of a unit, or, where the job has two tiles only, through one of them.
 template <typename C, int DH, int TILES>
 __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, const Job& j, const int* first, unsigned char* smem,
@@ -403,6 +404,7 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
   constexpr int LOADS = KA_UNIT * CPL / KA_THREADS;
   constexpr int ROWS = KA_UNIT * (KP + VP), BYTES = ROWS + (EIGHT<C> ? 2 * KA_UNIT * 4 : 0);   // a unit: K, V, scales
   constexpr bool CODES = EIGHT<C>;
+  constexpr int P = CODES ? 2 : 1;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), lane = tid % WAVE;
   const int r = lane & 31, s = lane >> 5;
   const int tile = wave % TILES, kpart = wave / TILES;
@@ -410,6 +412,42 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
   const int n_live = src.n_live;
   const int units = max(0, (j.reach.units - j.sp + n_live - 1) / n_live);   // of this split: sp, sp + n_live, ...
   const float scale_log2 = a.scale * LOG2E;
+
+  // Load x of a unit takes row x / CPL, elements (x % CPL) * EPL..; thread t takes loads y * 256 + t.  Rows
+  // past a step's last key read that one, or the head's first row, and are stored as zeros.
+  u32x4 kr[P][LOADS], vr[P][LOADS];
+  float sc[P];
+  auto unit_step = [&](int i) { return i < units ? 2 * (j.sp + n_live * i) : src.steps; };
+  auto fetch = [&](int u, int i) {
+    const int st = unit_step(i);
+    const float* scale = wave ? src.vs : src.ks;       // (the first two waves take the scales)
+    if (st + 2 <= src.L / KT) {
+      // 64 rows in a row: constant distances from one address
+      const char* kp = (const char*)(src.k + (int64_t)st * KT * DH) + tid * 16;
+      const char* vp = (const char*)(src.v + (int64_t)st * KT * DH) + tid * 16;
+#pragma unroll
+      for (int y = 0; y < LOADS; ++y) {
+        kr[u][y] = *reinterpret_cast<const u32x4*>(kp + y * KA_THREADS * 16);
+        vr[u][y] = *reinterpret_cast<const u32x4*>(vp + y * KA_THREADS * 16);
+      }
+      if (CODES && wave < 2) sc[u] = scale[(int64_t)st * KT + lane];
+      return;
+    }
+    const auto w0 = src.span(st), w1 = src.span(st + 1);
+#pragma unroll
+    for (int y = 0; y < LOADS; ++y) {
+      const int x = y * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
+      const int key = max(0, min((rx < KT ? w0.key0 : w1.key0) + rx % KT, rx < KT ? w0.last : w1.last));
+      kr[u][y] = *reinterpret_cast<const u32x4*>(src.k + (int64_t)key * DH + c * EPL);
+      vr[u][y] = *reinterpret_cast<const u32x4*>(src.v + (int64_t)key * DH + c * EPL);
+    }
+    if (CODES && wave < 2) sc[u] = scale[max(0, min((lane < KT ? w0.key0 : w1.key0) + lane % KT, lane < KT ? w0.last : w1.last))];
+  };
+#pragma unroll
+  for (int u = 0; u < P; ++u) {
+    fetch(u, u);
+    __builtin_amdgcn_sched_barrier(0);     // (in order, or the first one used could be the last to arrive)
+  }
 
   RowTile<DH> t;
   const int row = j.r0 + tile * 32 + r;
@@ -430,42 +468,20 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
   // the row's mask, 32 tail slots a word: those of a step
   const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) + ((int64_t)at.b * a.nq_max + at.node) * 2 * ADT_MASK_WORDS;
 
-  // Load x of a unit takes row x / CPL, elements (x % CPL) * EPL..; thread t takes loads u * 256 + t.  Rows
-  // past a step's last key read that one, or the head's first row, and are stored as zeros.
-  u32x4 kr[LOADS], vr[LOADS];
-  float sc = 0.f;
-  typename KeySource<C, DH>::Span next0{0, -1}, next1{0, -1};
-  auto fetch = [&](int i) {
-    const int st = i < units ? 2 * (j.sp + n_live * i) : src.steps;
-    next0 = src.span(st);
-    next1 = src.span(st + 1);
+  auto store = [&](auto whole_tag, int u, int i) {
+    unsigned char* to = smem + (i & 1) * BYTES;
+    const auto w0 = src.span(unit_step(i)), w1 = src.span(unit_step(i) + 1);
 #pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
-      const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
-      const int key = max(0, min(key0 + rx % KT, last));
-      kr[u] = *reinterpret_cast<const u32x4*>(src.k + (int64_t)key * DH + c * EPL);
-      vr[u] = *reinterpret_cast<const u32x4*>(src.v + (int64_t)key * DH + c * EPL);
+    for (int y = 0; y < LOADS; ++y) {
+      const int x = y * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
+      if (!decltype(whole_tag)::value && (rx < KT ? w0.key0 : w1.key0) + rx % KT > (rx < KT ? w0.last : w1.last)) vr[u][y] = u32x4{};
+      put_bf16<C>(to + rx * KP + c * EPL * 2, kr[u][y]);
+      put_bf16<C>(to + KA_UNIT * KP + rx * VP + c * EPL * 2, vr[u][y]);
     }
-    if (CODES && tid < 2 * KA_UNIT) {
-      const int rx = tid % KA_UNIT;
-      const int key = (rx < KT ? next0.key0 : next1.key0) + rx % KT;
-      sc = 0.f;
-      if (key <= (rx < KT ? next0.last : next1.last)) sc = tid < KA_UNIT ? src.ks[key] * scale_log2 : src.vs[key];
+    if (CODES && wave < 2) {
+      const bool none = !decltype(whole_tag)::value && (lane < KT ? w0.key0 : w1.key0) + lane % KT > (lane < KT ? w0.last : w1.last);
+      reinterpret_cast<float*>(to + ROWS)[tid] = none ? 0.f : wave ? sc[u] : sc[u] * scale_log2;
     }
-  };
-  auto store = [&](int buf) {
-    unsigned char* to = smem + buf * BYTES;
-    const bool full = next0.key0 + KT - 1 <= next0.last && next1.key0 + KT - 1 <= next1.last;
-#pragma unroll
-    for (int u = 0; u < LOADS; ++u) {
-      const int x = u * KA_THREADS + tid, rx = x / CPL, c = x % CPL;
-      const int key0 = rx < KT ? next0.key0 : next1.key0, last = rx < KT ? next0.last : next1.last;
-      if (!full && key0 + rx % KT > last) vr[u] = u32x4{};
-      put_bf16<C>(to + rx * KP + c * EPL * 2, kr[u]);
-      put_bf16<C>(to + KA_UNIT * KP + rx * VP + c * EPL * 2, vr[u]);
-    }
-    if (CODES && tid < 2 * KA_UNIT) reinterpret_cast<float*>(to + ROWS)[tid] = sc;
   };
   auto compute = [&](auto whole_tag, int buf, const uint32_t (&seen)[N], const bool (&tail)[N]) {
     const unsigned char* base = smem + buf * BYTES;
@@ -481,31 +497,39 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
         [] {}, sl, sl + KA_UNIT, v_operand<DH>(base + KA_UNIT * KP + kpart * KT * VP, lane), seen, tail, s);
   };
 
-  // units of whole prefix steps first, then the others, in code of their own: a split's units come in order
-  fetch(0);
-  int i = 0;
-  for (; i < units && 2 * (j.sp + n_live * i + 1) * KT <= src.L; ++i) {
+  // (the registers of a unit go by its place in a round of P)
+  auto unit = [&](auto whole_tag, int u, int i) {
     // the buffer written here was last read two units ago, before the previous barrier
-    store(i & 1);
+    store(whole_tag, u, i);
     __syncthreads();
-    fetch(i + 1);
-    if (tile_live) compute(std::true_type{}, i & 1, {}, {});
-  }
-  for (; i < units; ++i) {
-    store(i & 1);
-    __syncthreads();
-    fetch(i + 1);
-    if (!tile_live) continue;
-    const int st = 2 * (j.sp + n_live * i) + kpart;
-    uint32_t seen[N];
-    bool tail[N];
+    fetch(u, i + P);
+    if (!tile_live) return;
+    uint32_t seen[N] = {};
+    bool tail[N] = {};
+    if constexpr (!decltype(whole_tag)::value) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      seen[n] = src.seen(st + n, words);
-      tail[n] = st + n >= src.prefix_steps;
+      for (int n = 0; n < N; ++n) {
+        const int st = unit_step(i) + kpart + n;
+        seen[n] = src.seen(st, words);
+        tail[n] = st >= src.prefix_steps;
+      }
     }
-    compute(std::false_type{}, i & 1, seen, tail);
-  }
+    compute(whole_tag, i & 1, seen, tail);
+  };
+  // units of whole prefix steps first, then the others, in code of their own: a split's units come in order
+  const int whole = max(0, min(units, (src.L / KA_UNIT - j.sp + n_live - 1) / n_live));
+  int i = 0;
+  auto loop = [&](auto whole_tag, int end) {
+    for (;;) {
+#pragma unroll
+      for (int u = 0; u < P; ++u) {
+        if (i >= end) return u;
+        unit(whole_tag, u, i++);
+      }
+    }
+  };
+  if (loop(std::true_type{}, whole) == 1 && i < units) unit(std::false_type{}, 1, i++);
+  loop(std::false_type{}, units);
   if (__any(t.odd)) {
     for (int st = src.prefix_steps; st < src.steps; ++st)
       if (st / 2 % n_live == j.sp && st % 2 % KH == kpart) add_odd_values(t, src, st, words, s);
@@ -569,6 +593,44 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
   const KeySource<C, DH> src(j);
   const float scale_log2 = a.scale * LOG2E;
 
+  unsigned char* rows = smem + wave * OWN;
+  float* sl = reinterpret_cast<float*>(rows + KT * VP);
+
+  u32x4 kr[P][LOADS], vr[P][LOADS];
+  float sc[P];
+  const int stride = src.n_live * KA_WAVES;
+  // (a step past the end reads the head's first row, so the loads in flight are the same on every path)
+  const float* scale = s ? src.vs : src.ks;
+  auto fetch = [&](int u, int st) {
+    if (st < src.L / KT) {
+      // 32 rows in a row: constant distances from one address
+      const char* kp = (const char*)(src.k + (int64_t)st * KT * DH) + (r * DH + s * EPL) * (int)sizeof(C);
+      const char* vp = (const char*)(src.v + (int64_t)st * KT * DH) + lane * 16;
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) kr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + x * 32));
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) vr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + x * WAVE * 16));
+      if (CODES) sc[u] = scale[(int64_t)st * KT + r];
+      return;
+    }
+    const auto at = src.span(st);
+    const C* kp = src.k + (int64_t)max(0, min(at.key0 + r, at.last)) * DH + s * EPL;
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) kr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + x * 2 * EPL));
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int y = x * WAVE + lane, key = max(0, min(at.key0 + y / CPL, at.last));
+      vr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src.v + (int64_t)key * DH + y % CPL * EPL));
+    }
+    if (CODES) sc[u] = scale[max(0, min(at.key0 + r, at.last))];
+  };
+  int st = j.sp * KA_WAVES + wave;
+#pragma unroll
+  for (int u = 0; u < P; ++u) {
+    fetch(u, st + u * stride);
+    __builtin_amdgcn_sched_barrier(0);     // (in order, or the first one used could be the last to arrive)
+  }
+
   RowTile<DH> t;
   const int row = j.r0 + r;
   const bool mine = row < j.live;
@@ -587,28 +649,6 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
 #pragma unroll
     for (int e = 0; e < 16; ++e) t.o[d][e] = 0.f;
   const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) + ((int64_t)at.b * a.nq_max + at.node) * 2 * ADT_MASK_WORDS;
-  unsigned char* rows = smem + wave * OWN;
-  float* sl = reinterpret_cast<float*>(rows + KT * VP);
-
-  u32x4 kr[P][LOADS], vr[P][LOADS];
-  float sc[P];
-  const int stride = src.n_live * KA_WAVES;
-  // (a step past the end reads the head's first row, so the loads in flight are the same on every path)
-  auto fetch = [&](int u, int st) {
-    const auto at = src.span(st);
-    const C* kp = src.k + (int64_t)max(0, min(at.key0 + r, at.last)) * DH + s * EPL;
-#pragma unroll
-    for (int x = 0; x < LOADS; ++x) kr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kp + x * 2 * EPL));
-#pragma unroll
-    for (int x = 0; x < LOADS; ++x) {
-      const int y = x * WAVE + lane, key = max(0, min(at.key0 + y / CPL, at.last));
-      vr[u][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src.v + (int64_t)key * DH + y % CPL * EPL));
-    }
-    if (CODES) {
-      const int key = max(0, min(at.key0 + r, at.last));
-      sc[u] = s ? src.vs[key] : src.ks[key];
-    }
-  };
   auto step = [&](auto whole_tag, int u, int st) {
     constexpr bool WHOLE = decltype(whole_tag)::value;
     const auto span = src.span(st);
@@ -643,12 +683,6 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
     wave_lds_fence();
   };
 
-  int st = j.sp * KA_WAVES + wave;
-#pragma unroll
-  for (int u = 0; u < P; ++u) {
-    fetch(u, st + u * stride);
-    __builtin_amdgcn_sched_barrier(0);     // (in order, or the first one used could be the last to arrive)
-  }
   const int whole = src.L / KT;
   auto loop = [&](auto whole_tag, int end) {
     // (P steps a round: the registers of a step go by its place in the round)
@@ -907,45 +941,64 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
 }
 
 // ---------------------------------------------------------------------------- merge
-// A row's parts, own splits then the prefix's, in that order: a thread takes four dims of one row.
+// A row's parts, own splits then the prefix's: DH / 4 threads take four dims each, and `count` groups of
+// them deal out the parts, up to four requested at a time; the groups' sums meet in LDS, in their order.
 template <typename T, int KT>
-__global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p, const float* __restrict__ part_o,
+__global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p, int count, const float* __restrict__ part_o,
                                                               const float* __restrict__ part_ml) {
-  const int per = a.Dh / 4, b = blockIdx.z, h = blockIdx.y;
-  const int row = blockIdx.x * (KA_THREADS / per) + threadIdx.x / per, d = threadIdx.x % per * 4;
-  if (row >= rows_of(a, b)) return;
-  const int n_own = own_reach<KT>(a, p, b).live, n = n_own + pre_reach<KT>(a, p, b).live;
-  if (n == 1) return;
+  __shared__ f32x4 so[KA_THREADS];
+  __shared__ float2 sml[KA_THREADS];
+  const int per = a.Dh / 4, b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
+  const int n_q = a.n_q[b], len = a.own.len[b], n_tail = a.n_tail[b];          // (one wait for all)
+  const int n_own = reach_of<KT>(len, n_tail, a.own.cap, p.own, 1).live, n = n_own + pre_reach<KT>(a, p, b).live;
+  const int unit = tid / per, grp = unit % count, d = tid % per * 4;
+  const int row = blockIdx.x * (KA_THREADS / per / count) + unit / count, live = max(0, min(n_q, a.nq_max)) * a.G;
+  if (n == 1 || (int)blockIdx.x * (KA_THREADS / per / count) >= live) return;
   const RowAt at{b, row / a.G, row % a.G};
   const int64_t base = at.part(a, p, h, 0), rows = (int64_t)a.nq_max * a.G;
   float m = -INFINITY, l = 0.f;
   f32x4 o{0.f, 0.f, 0.f, 0.f};
-  for (int s0 = 0; s0 < n; s0 += 8) {       // eight parts requested at a time
-    float2 ml[8];
-    f32x4 x[8];
+  auto add = [&](float pm, float pl, const f32x4& po) {       // at the maximum m
+    const float wt = part_weight(pm, pl, m);
+    if (wt == 0.f && pl == pl) return;
+    l += wt * pl;
+    o += wt * po;
+  };
+  for (int s0 = row < live ? grp : n; s0 < n; s0 += 4 * count) {
+    float2 ml[4];
+    f32x4 x[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int s = min(s0 + i, n - 1);
+    for (int i = 0; i < 4; ++i) {
+      ml[i] = make_float2(-INFINITY, 0.f);
+      const int s = s0 + i * count;
+      if (s >= n) continue;
       const int64_t from = base + (s < n_own ? s : p.own.splits + s - n_own) * rows;
       ml[i] = *reinterpret_cast<const float2*>(part_ml + from * 2);
-      x[i] = *reinterpret_cast<const f32x4*>(part_o + from * a.Dh + d);
+      x[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(part_o + from * a.Dh + d));
     }
     float M = m;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) M = fmaxf(M, ml[i].x);
+    for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i].x);
     const float down = m == -INFINITY ? 1.f : exp2_hw(m - M);
     m = M;
     l *= down;
     o *= down;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (s0 + i >= n) continue;
-      const float wt = part_weight(ml[i].x, ml[i].y, M);
-      if (wt == 0.f && ml[i].y == ml[i].y) continue;
-      l += wt * ml[i].y;
-      o += wt * x[i];
-    }
+    for (int i = 0; i < 4; ++i)
+      if (s0 + i * count < n) add(ml[i].x, ml[i].y, x[i]);
   }
+  if (count > 1) {
+    so[tid] = o;
+    sml[tid] = make_float2(m, l);
+    __syncthreads();
+    if (grp > 0) return;
+    const int groups = min(count, n);
+    for (int g = 1; g < groups; ++g) m = fmaxf(m, sml[tid + g * per].x);
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < groups; ++g) add(sml[tid + g * per].x, sml[tid + g * per].y, so[tid + g * per]);
+  }
+  if (row >= live) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   store4((T*)a.out + at.q(a, h) + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
@@ -1012,10 +1065,12 @@ adt_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t st) {
 #undef ADT_KA
   ADT_LAUNCH_CHECK();
   if (p.parts == 1) return ADT_OK;
-  const int fit = KA_THREADS / (a.Dh / 4);
-  const dim3 grid((a.nq_max * a.G + fit - 1) / fit, a.Hkv, a.B);
-  if (a.type == ADT_F32) kv_merge_kernel<float, 16><<<grid, KA_THREADS, 0, st>>>(a, p, part_o, part_ml);
-  else kv_merge_kernel<uint16_t, 32><<<grid, KA_THREADS, 0, st>>>(a, p, part_o, part_ml);
+  // a thread for every four outputs, or for few outputs of many parts several
+  const int fit = KA_THREADS / (a.Dh / 4), rows = a.nq_max * a.G;
+  const int count = p.parts > 8 && (int64_t)a.B * a.Hkv * rows * (a.Dh / 4) < 65536 ? fit : 1;
+  const dim3 grid((unsigned)(((int64_t)rows * count + fit - 1) / fit), a.Hkv, a.B);
+  if (a.type == ADT_F32) kv_merge_kernel<float, 16><<<grid, KA_THREADS, 0, st>>>(a, p, count, part_o, part_ml);
+  else kv_merge_kernel<uint16_t, 32><<<grid, KA_THREADS, 0, st>>>(a, p, count, part_o, part_ml);
   ADT_LAUNCH_CHECK();
   return ADT_OK;
 }
