@@ -69,7 +69,7 @@ __device__ __forceinline__ int rows_of(const KvAttn& a, int b) { return max(0, m
 
 // What a workgroup does: rows [r0, ...) of the job's `live` rows, split sp of `reach`.
 struct Job {
-  bool pre;
+  bool pre, direct;               // a prefix; all keys of the rows are here: the result is the output
   int b, h, r0, live, sp;         // b: sequence, or first sequence of the group
   Reach reach;
   const KvPart* part;
@@ -93,14 +93,17 @@ __device__ __forceinline__ bool take_job(const KvAttn& a, const KvPlan& p, int r
   j.part = j.pre ? &a.pre : &a.own;
   j.r0 = block * rows_each;
   if (!j.pre) {
-    const int n_q = a.n_q[at], len = a.own.len[at], n_tail = a.n_tail[at];     // (one wait for all three)
+    const int n_q = a.n_q[at], len = a.own.len[at], n_tail = a.n_tail[at];     // (one wait for all)
+    const int pre_len = a.groups ? a.pre.len[at / (uint32_t)a.group] : 0;
     j.b = at;
     j.live = max(0, min(n_q, a.nq_max)) * a.G;
     j.reach = reach_of<KT>(len, n_tail, a.own.cap, p.own, 1);
+    j.direct = j.reach.live == 1 && pre_len <= 0;
     if (j.r0 >= j.live || j.sp >= j.reach.live) return false;
     if (threadIdx.x == 0 && (int64_t)len + n_tail > a.own.cap) dev_fail(DEVINV_KV_RANGE);
     return true;
   }
+  j.direct = false;
   j.b = at * a.group;
   j.reach = pre_reach<KT>(a, p, j.b);
   if (threadIdx.x == 0 && a.pre.len[at] > a.pre.cap) dev_fail(DEVINV_KV_RANGE);
@@ -378,19 +381,15 @@ __device__ __forceinline__ void add_odd_values(RowTile<DH>& t, const KeySource<C
   }
 }
 
-// Where a row's result goes: the output, if its keys were all in this job, else a partial result.
-struct RowOut {
-  bool direct;
-  int64_t at;
-};
-__device__ __forceinline__ RowOut row_out(const KvAttn& a, const KvPlan& p, const Job& j, const RowAt& at) {
-  if (!j.pre && j.reach.live == 1 && pre_reach<32>(a, p, at.b).live == 0) return {true, at.q(a, j.h)};
-  return {false, at.part(a, p, j.h, j.pre ? p.own.splits + j.sp : j.sp)};
+// Where a row's result goes: the output, or a partial result.
+__device__ __forceinline__ int64_t row_out(const KvAttn& a, const KvPlan& p, const Job& j, const RowAt& at) {
+  return j.direct ? at.q(a, j.h) : at.part(a, p, j.h, j.pre ? p.own.splits + j.sp : j.sp);
 }
 // Outputs 32 d + 8 c + 4 s.. of a row.
-__device__ __forceinline__ void put_out(const KvAttn& a, const RowOut& to, int dim, f32x4 o, float inv, float* part_o) {
-  if (to.direct) store4((uint16_t*)a.out + to.at + dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-  else *reinterpret_cast<f32x4*>(part_o + to.at * a.Dh + dim) = o;
+template <int DH>
+__device__ __forceinline__ void put_out(const KvAttn& a, bool direct, int64_t to, int dim, f32x4 o, float inv, float* part_o) {
+  if (direct) store4((uint16_t*)a.out + to + dim, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+  else *reinterpret_cast<f32x4*>(part_o + to * DH + dim) = o;
 }
 
 // Many rows: a unit of 64 keys, K and V, comes into LDS once for the workgroup (eight bits turned into
@@ -565,14 +564,14 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
     t.m = M;
   }
   if (!mine) return;
-  const RowOut to = row_out(a, p, j, at);
+  const int64_t to = row_out(a, p, j, at);
   const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
 #pragma unroll
   for (int d = 0; d < OT; ++d)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-      put_out(a, to, 32 * d + 8 * c + 4 * s, f32x4{t.o[d][4 * c], t.o[d][4 * c + 1], t.o[d][4 * c + 2], t.o[d][4 * c + 3]}, inv, part_o);
-  if (!to.direct && s == 0) *reinterpret_cast<float2*>(part_ml + to.at * 2) = make_float2(t.m, t.l);
+      put_out<DH>(a, j.direct, to, 32 * d + 8 * c + 4 * s, f32x4{t.o[d][4 * c], t.o[d][4 * c + 1], t.o[d][4 * c + 2], t.o[d][4 * c + 3]}, inv, part_o);
+  if (!j.direct && s == 0) *reinterpret_cast<float2*>(part_ml + to * 2) = make_float2(t.m, t.l);
 }
 
 // Up to 32 rows: the waves take steps of their own, with no barrier between them.  K comes straight into the
@@ -740,11 +739,11 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[e] += wt * mo[w * EACH + (wave * 16 + e) * WAVE + lane];
   }
-  const RowOut to = row_out(a, p, j, at);
+  const int64_t to = row_out(a, p, j, at);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) put_out(a, to, 32 * wave + 8 * c + 4 * s, f32x4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]}, inv, part_o);
-  if (!to.direct && wave == 0 && s == 0) *reinterpret_cast<float2*>(part_ml + to.at * 2) = make_float2(M, sum);
+  for (int c = 0; c < 4; ++c) put_out<DH>(a, j.direct, to, 32 * wave + 8 * c + 4 * s, f32x4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]}, inv, part_o);
+  if (!j.direct && wave == 0 && s == 0) *reinterpret_cast<float2*>(part_ml + to * 2) = make_float2(M, sum);
 }
 
 template <typename C, int DH>
@@ -928,7 +927,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
         acc += wt * *reinterpret_cast<const f32x4*>(&mo[(w * 16 + i) * MP + d]);
       }
       const RowAt at = row_at(a, j, row, first);
-      if (!j.pre && n_live == 1 && pre_reach<KT>(a, p, at.b).live == 0) {
+      if (j.direct) {
         const float inv = ls == 0.f ? 0.f : 1.f / ls;
         store4((float*)a.out + at.q(a, j.h) + d, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
       } else {
