@@ -103,51 +103,117 @@ __device__ __forceinline__ void store_codes(const R (&y)[N][VEC], int lanes, boo
   }
 }
 
-// One row a workgroup, all its heads or a part of them; a group of `lanes` lanes takes a head at a
-// time.  VEC values are 16 bytes where sizes and addresses allow it (N = 1 piece a lane), else one
-// value (a wave a head, N = 4).  A pair's other half is read from memory beside it (the same lines).
+// One row a workgroup, all its heads or a part of them; a group of `lanes` lanes takes a head, and KR_HEADS
+// of them one after another, whose values are requested together and before the row's sines and cosines
+// are made (in LDS, in double): the two waits pass at once.  VEC values are 16 bytes where sizes and
+// addresses allow it (N = 1 piece a lane), else one value (a wave a head, N = 4).  A pair's other half
+// is read from memory beside it (the same lines).  A lane has the same dims of every head, so what it
+// needs of the table stays in its registers.
+constexpr int KR_HEADS = 3;
 template <typename T, typename C, int VEC, bool INTER>
 __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, int lanes) {
   constexpr int N = VEC == 1 ? 4 : 1;
+  constexpr bool MATES = !INTER || VEC == 1;      // the other half of a pair lies outside the piece
   __shared__ double2 cs[KR_MAX_PAIRS];
   const int i = a.row0 + blockIdx.x, b = blockIdx.z;
-  if (i >= min(a.n_rows[b], a.n_max)) return;
+  const int n_rows = a.n_rows[b], kv_len = a.kv_len[b];
+  if (i >= min(n_rows, a.n_max)) return;
   const int64_t row = (int64_t)b * a.n_max + i;
-  const int rot = a.rot, half = rot / 2, DH = a.c.Dh, H = a.H, Hkv = a.c.heads;
+  const int rot = a.rot, half = rot / 2, DH = a.c.Dh, H = a.H, Hkv = a.c.heads, heads = H + 2 * Hkv;
+  const int64_t slot = (int64_t)kv_len + i;
+  const bool store_kv = kv_len >= 0 && slot < a.c.cap;
+  if (!store_kv && threadIdx.x == 0 && blockIdx.y == 0) dev_fail(DEVINV_KV_RANGE);
+  const int per = KR_THREADS / lanes, sub = threadIdx.x / lanes, l = threadIdx.x % lanes;
+  const int first = blockIdx.y * per + sub, step = gridDim.y * per;
+  typedef RowPack<T, VEC, VEC == 1 ? sizeof(T) : 16> P;
+  // this lane's pieces: first dim, and that of the other half of its pairs (itself, if it is not rotated)
+  auto piece = [&](int j) { return (l + j * lanes) * VEC; };
+  auto mate = [&](int j) {
+    const int d = piece(j);
+    return d >= rot ? d : INTER ? d ^ 1 : d < half ? d + half : d - half;
+  };
+  P own[KR_HEADS][N], other[KR_HEADS][N];
+  auto request = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < KR_HEADS; ++u) {
+      const int hd = h0 + u * step;
+      if (hd >= heads) break;
+      const T* src = hd < H ? (const T*)a.q + row * a.ldq + (int64_t)hd * DH
+                     : hd < H + Hkv ? (const T*)a.k + row * a.ldk + (int64_t)(hd - H) * DH
+                                    : (const T*)a.v + row * a.ldv + (int64_t)(hd - H - Hkv) * DH;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        own[u][j] = P{};
+        if (piece(j) < DH) own[u][j] = *reinterpret_cast<const P*>(src + piece(j));
+        if constexpr (MATES) {
+          other[u][j] = P{};
+          if (piece(j) < DH && hd < H + Hkv) other[u][j] = *reinterpret_cast<const P*>(src + mate(j));
+        }
+      }
+    }
+  };
+  request(first);
   for (int p = threadIdx.x; p < half; p += KR_THREADS) {
     const double2 t = turn64((double)a.pos[row], a.freq[p]);
     cs[p] = make_double2(t.x * a.gain, t.y * a.gain);
   }
   __syncthreads();
-  const int64_t slot = (int64_t)a.kv_len[b] + i;
-  const bool store_kv = a.kv_len[b] >= 0 && slot < a.c.cap;
-  if (!store_kv && threadIdx.x == 0 && blockIdx.y == 0) dev_fail(DEVINV_KV_RANGE);
-  const int per = KR_THREADS / lanes, sub = threadIdx.x / lanes, l = threadIdx.x % lanes;
-  auto piece = [&](int j) { return (l + j * lanes) * VEC; };
-  typedef RowPack<T, VEC, VEC == 1 ? sizeof(T) : 16> P;
-  const int64_t srow = (int64_t)b * a.c.scale_b + slot;
+  // y = x c + other s, s with the sign that the half has; (1, 0) where a dim is not rotated
+  auto turn_of = [&](int j, int e) {
+    const int d = piece(j) + e;
+    if (d >= rot) return make_double2(1.0, 0.0);
+    const bool second = INTER ? d & 1 : d >= half;
+    const double2 t = cs[INTER ? d / 2 : second ? d - half : d];
+    return make_double2(t.x, second ? t.y : -t.y);
+  };
+  float2 turn[N][VEC];
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const double2 t = turn_of(j, e);
+      turn[j][e] = make_float2((float)t.x, (float)t.y);
+    }
 
-  // one head of queries (math in fp32) or keys (in double), row src, gains g
-  auto head = [&](auto zero, const T* src, const float* g, auto store) {
-    typedef decltype(zero) R;
-    R x[N][VEC], o[N][VEC], y[N][VEC];
+  // a head's gains at this lane's dims and at their mates (none: 1)
+  float gain[N][VEC], mate_gain[N][VEC];
+  auto gains = [&](const float* g) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int d = piece(j);
-      P own{}, other{};
-      if (d < DH) {
-        own = *reinterpret_cast<const P*>(src + d);
-        const int at = INTER ? (VEC == 1 ? d ^ 1 : d) : d < half ? d + half : d - half;
-        if (d < rot && (VEC == 1 || !INTER)) other = *reinterpret_cast<const P*>(src + at);
+      typedef RowPack<float, VEC, VEC == 1 ? 4 : 16> G;
+      G x, y;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x.v[e] = y.v[e] = 1.f;
+      if (g && piece(j) < DH) {
+        if constexpr (VEC == 1) {
+          x.v[0] = g[piece(j)];
+          y.v[0] = g[mate(j)];
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) x.v[e] = g[piece(j) + e];
+          if constexpr (MATES) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) y.v[e] = g[mate(j) + e];
+          }
+        }
       }
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        x[j][e] = (R)Elem<T>::load(own.v, e);
-        o[j][e] = (R)Elem<T>::load(INTER && VEC > 1 ? own.v : other.v, INTER && VEC > 1 ? (e ^ 1) : e);
+        gain[j][e] = x.v[e];
+        mate_gain[j][e] = MATES ? y.v[e] : x.v[e ^ 1];
       }
     }
+  };
+  // one head, queries in fp32 and keys in double
+  auto made = [&](auto zero, int u, bool norm, auto turned, auto store) {
+    typedef decltype(zero) R;
+    R x[N][VEC], y[N][VEC];
     R inv = (R)1;
-    if (g) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[j][e] = (R)Elem<T>::load(own[u][j].v, e);
+    if (norm) {
       R ss = (R)0;
 #pragma unroll
       for (int j = 0; j < N; ++j)
@@ -156,67 +222,61 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
       inv = (R)1 / sqrt(group_sum(ss, lanes) / (R)DH + (R)a.eps);
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int d = piece(j);
+    for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const int at = d + e;
-        R v = x[j][e] * inv, w = o[j][e] * inv;
-        if (at < DH && g) v *= (R)g[at];
-        if (at < rot) {
-          const bool second = INTER ? at & 1 : at >= half;
-          const int mate = INTER ? at ^ 1 : second ? at - half : at + half;
-          if (g) w *= (R)g[mate];
-          const double2 t = cs[INTER ? at / 2 : second ? mate : at];
-          v = second ? w * (R)t.y + v * (R)t.x : v * (R)t.x - w * (R)t.y;
-        }
-        y[j][e] = v;
+        const R w = MATES ? (R)Elem<T>::load(other[u][j].v, e) : x[j][e ^ 1];
+        const auto t = turned(j, e);
+        // (a dim that is not rotated takes nothing of another, whatever that holds)
+        const R across = piece(j) + e < rot ? w * (R)mate_gain[j][e] * (R)t.y : (R)0;
+        y[j][e] = inv * (x[j][e] * (R)gain[j][e] * (R)t.x + across);
       }
-    }
     store(y);
   };
   auto plain = [&](const auto& y, T* dst) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int d = piece(j);
-      if (d >= DH) continue;
+      if (piece(j) >= DH) continue;
       P p;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) Elem<T>::store(p.v, e, (float)y[j][e]);
-      *reinterpret_cast<P*>(dst + d) = p;
+      *reinterpret_cast<P*>(dst + piece(j)) = p;
     }
   };
-
-  for (int hd = blockIdx.y * per + sub; hd < H + 2 * Hkv; hd += gridDim.y * per) {
+  const int64_t at_scale = (int64_t)b * a.c.scale_b + slot;
+  auto take = [&](int u, int hd) {
     if (hd < H) {
-      head(0.f, (const T*)a.q + row * a.ldq + (int64_t)hd * DH, a.q_norm ? a.q_norm + (int64_t)hd * a.norm_step : nullptr,
+      if (a.norm_step || hd == first) gains(a.q_norm ? a.q_norm + (int64_t)hd * a.norm_step : nullptr);
+      made(0.f, u, a.q_norm != nullptr, [&](int j, int e) { return turn[j][e]; },
            [&](const auto& y) { plain(y, (T*)a.q_out + (row * H + hd) * (int64_t)DH); });
-      continue;
+      return;
     }
-    if (!store_kv) break;
+    if (!store_kv) return;
     const bool key = hd < H + Hkv;
     const int h = hd - H - (key ? 0 : Hkv);
     C* to = (C*)(key ? a.c.k : a.c.v) + b * a.c.stride_b + h * a.c.stride_h + slot * DH;
-    float* scale = (key ? a.c.k_scale : a.c.v_scale) + h * a.c.scale_h + srow;
+    float* scale = (key ? a.c.k_scale : a.c.v_scale) + h * a.c.scale_h + at_scale;
     auto store = [&](const auto& y) {
       if constexpr (EIGHT<C>) store_codes<C, VEC, N>(y, lanes, l == 0, DH, to, scale, piece);
       else plain(y, (T*)to);
     };
     if (key) {
-      head(0.0, (const T*)a.k + row * a.ldk + (int64_t)h * DH, a.k_norm ? a.k_norm + (int64_t)h * a.norm_step : nullptr,
-           store);
+      gains(a.k_norm ? a.k_norm + (int64_t)h * a.norm_step : nullptr);
+      made(0.0, u, a.k_norm != nullptr, turn_of, store);
     } else {
-      const T* src = (const T*)a.v + row * a.ldv + (int64_t)h * DH;
       float y[N][VEC];
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        P p{};
-        if (piece(j) < DH) p = *reinterpret_cast<const P*>(src + piece(j));
+      for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) y[j][e] = Elem<T>::load(p.v, e);
-      }
+        for (int e = 0; e < VEC; ++e) y[j][e] = Elem<T>::load(own[u][j].v, e);
       store(y);
     }
+  };
+  for (int h0 = first; h0 < heads; h0 += KR_HEADS * step) {
+    if (h0 != first) request(h0);
+#pragma unroll
+    for (int u = 0; u < KR_HEADS; ++u)
+      if (h0 + u * step < heads) take(u, h0 + u * step);
   }
 }
 
