@@ -103,26 +103,29 @@ __device__ __forceinline__ void store_codes(const R (&y)[N][VEC], int lanes, boo
   }
 }
 
-// One row a workgroup, all its heads or a part of them; a group of `lanes` lanes takes a head, and KR_HEADS
-// of them one after another, whose values are requested together and before the row's sines and cosines
-// are made (in LDS, in double): the two waits pass at once.  VEC values are 16 bytes where sizes and
-// addresses allow it (N = 1 piece a lane), else one value (a wave a head, N = 4).  A pair's other half
-// is read from memory beside it (the same lines).  A lane has the same dims of every head, so what it
-// needs of the table stays in its registers.
-constexpr int KR_HEADS = 3;
-template <typename T, typename C, int VEC, bool INTER>
+// A workgroup takes ROWS rows, all their heads or a part of them; a group of `lanes` lanes takes a head, and
+// others after it, whose values are requested HEADS heads of all rows at once, the first ones before the
+// rows' sines and cosines are made (in LDS): the two waits pass together.  Many rows go four to a
+// workgroup, which then starts a quarter as often and reads a head's gains for four; few rows one, with
+// three heads requested at once.  VEC values are 16 bytes where sizes and addresses allow it (N = 1 piece
+// a lane), else one value (a wave a head, N = 4).  A pair's other half is read from memory beside it (the
+// same lines).
+template <typename T, typename C, int VEC, bool INTER, int HEADS, int ROWS>
 __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, int lanes) {
   constexpr int N = VEC == 1 ? 4 : 1;
   constexpr bool MATES = !INTER || VEC == 1;      // the other half of a pair lies outside the piece
-  __shared__ double2 cs[KR_MAX_PAIRS];
-  const int i = a.row0 + blockIdx.x, b = blockIdx.z;
-  const int n_rows = a.n_rows[b], kv_len = a.kv_len[b];
-  if (i >= min(n_rows, a.n_max)) return;
-  const int64_t row = (int64_t)b * a.n_max + i;
+  __shared__ double2 cs[ROWS][KR_MAX_PAIRS];
+  __shared__ float2 cs32[ROWS][KR_MAX_PAIRS];
+  const int b = blockIdx.z;
+  const int n_rows = min(a.n_rows[b], a.n_max), kv_len = a.kv_len[b];
+  const int64_t i0 = a.row0 + (int64_t)blockIdx.x * ROWS;
+  if (i0 >= n_rows) return;
+  const int count = (int)min((int64_t)ROWS, n_rows - i0);
+  const int64_t row0 = (int64_t)b * a.n_max + i0, slot0 = kv_len + i0;
   const int rot = a.rot, half = rot / 2, DH = a.c.Dh, H = a.H, Hkv = a.c.heads, heads = H + 2 * Hkv;
-  const int64_t slot = (int64_t)kv_len + i;
-  const bool store_kv = kv_len >= 0 && slot < a.c.cap;
-  if (!store_kv && threadIdx.x == 0 && blockIdx.y == 0) dev_fail(DEVINV_KV_RANGE);
+  // rows whose slots lie in the cache: [0, kept) of the `count` (a negative length has none)
+  const int kept = kv_len < 0 ? 0 : (int)max((int64_t)0, min((int64_t)count, a.c.cap - slot0));
+  if (kept < count && threadIdx.x == 0 && blockIdx.y == 0) dev_fail(DEVINV_KV_RANGE);
   const int per = KR_THREADS / lanes, sub = threadIdx.x / lanes, l = threadIdx.x % lanes;
   const int first = blockIdx.y * per + sub, step = gridDim.y * per;
   typedef RowPack<T, VEC, VEC == 1 ? sizeof(T) : 16> P;
@@ -132,48 +135,52 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
     const int d = piece(j);
     return d >= rot ? d : INTER ? d ^ 1 : d < half ? d + half : d - half;
   };
-  P own[KR_HEADS][N], other[KR_HEADS][N];
+  P own[HEADS][ROWS][N], other[HEADS][ROWS][N];
   auto request = [&](int h0) {
 #pragma unroll
-    for (int u = 0; u < KR_HEADS; ++u) {
+    for (int u = 0; u < HEADS; ++u) {
       const int hd = h0 + u * step;
       if (hd >= heads) break;
-      const T* src = hd < H ? (const T*)a.q + row * a.ldq + (int64_t)hd * DH
-                     : hd < H + Hkv ? (const T*)a.k + row * a.ldk + (int64_t)(hd - H) * DH
-                                    : (const T*)a.v + row * a.ldv + (int64_t)(hd - H - Hkv) * DH;
+      const bool query = hd < H, key = !query && hd < H + Hkv;
+      const int64_t ld = query ? a.ldq : key ? a.ldk : a.ldv;
+      const T* src = (const T*)(query ? a.q : key ? a.k : a.v) + row0 * ld + (int64_t)(query ? hd : key ? hd - H : hd - H - Hkv) * DH;
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        own[u][j] = P{};
-        if (piece(j) < DH) own[u][j] = *reinterpret_cast<const P*>(src + piece(j));
-        if constexpr (MATES) {
-          other[u][j] = P{};
-          if (piece(j) < DH && hd < H + Hkv) other[u][j] = *reinterpret_cast<const P*>(src + mate(j));
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const T* at = src + min(r, count - 1) * ld;
+          own[u][r][j] = P{};
+          if (piece(j) < DH) own[u][r][j] = *reinterpret_cast<const P*>(at + piece(j));
+          if constexpr (MATES) {
+            other[u][r][j] = P{};
+            if (piece(j) < DH && (query || key)) other[u][r][j] = *reinterpret_cast<const P*>(at + mate(j));
+          }
         }
-      }
     }
   };
   request(first);
-  for (int p = threadIdx.x; p < half; p += KR_THREADS) {
-    const double2 t = turn64((double)a.pos[row], a.freq[p]);
-    cs[p] = make_double2(t.x * a.gain, t.y * a.gain);
+  for (int x = threadIdx.x; x < count * half; x += KR_THREADS) {
+    const int r = x / half, p = x % half;
+    const double2 t = turn64((double)a.pos[row0 + r], a.freq[p]);
+    cs[r][p] = make_double2(t.x * a.gain, t.y * a.gain);
+    cs32[r][p] = make_float2((float)(t.x * a.gain), (float)(t.y * a.gain));
   }
   __syncthreads();
   // y = x c + other s, s with the sign that the half has; (1, 0) where a dim is not rotated
-  auto turn_of = [&](int j, int e) {
+  auto turn_of = [&](auto zero, int r, int j, int e) {
     const int d = piece(j) + e;
-    if (d >= rot) return make_double2(1.0, 0.0);
-    const bool second = INTER ? d & 1 : d >= half;
-    const double2 t = cs[INTER ? d / 2 : second ? d - half : d];
-    return make_double2(t.x, second ? t.y : -t.y);
-  };
-  float2 turn[N][VEC];
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const double2 t = turn_of(j, e);
-      turn[j][e] = make_float2((float)t.x, (float)t.y);
+    struct {
+      decltype(zero) x, y;
+    } t{1, 0};
+    if (d < rot) {
+      const bool second = INTER ? d & 1 : d >= half;
+      const int p = INTER ? d / 2 : second ? d - half : d;
+      if constexpr (sizeof(zero) == 8) t.x = cs[r][p].x, t.y = cs[r][p].y;
+      else t.x = cs32[r][p].x, t.y = cs32[r][p].y;
+      if (!second) t.y = -t.y;
     }
+    return t;
+  };
 
   // a head's gains at this lane's dims and at their mates (none: 1)
   float gain[N][VEC], mate_gain[N][VEC];
@@ -204,15 +211,15 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
       }
     }
   };
-  // one head, queries in fp32 and keys in double
-  auto made = [&](auto zero, int u, bool norm, auto turned, auto store) {
+  // one head of a row, queries in fp32 and keys in double
+  auto made = [&](auto zero, const P (&mine)[N], const P (&mates)[N], int r, bool norm, auto store) {
     typedef decltype(zero) R;
     R x[N][VEC], y[N][VEC];
     R inv = (R)1;
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[j][e] = (R)Elem<T>::load(own[u][j].v, e);
+      for (int e = 0; e < VEC; ++e) x[j][e] = (R)Elem<T>::load(mine[j].v, e);
     if (norm) {
       R ss = (R)0;
 #pragma unroll
@@ -225,11 +232,11 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
     for (int j = 0; j < N; ++j)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const R w = MATES ? (R)Elem<T>::load(other[u][j].v, e) : x[j][e ^ 1];
-        const auto t = turned(j, e);
+        const R w = MATES ? (R)Elem<T>::load(mates[j].v, e) : x[j][e ^ 1];
+        const auto t = turn_of(zero, r, j, e);
         // (a dim that is not rotated takes nothing of another, whatever that holds)
-        const R across = piece(j) + e < rot ? w * (R)mate_gain[j][e] * (R)t.y : (R)0;
-        y[j][e] = inv * (x[j][e] * (R)gain[j][e] * (R)t.x + across);
+        const R across = piece(j) + e < rot ? w * (R)mate_gain[j][e] * t.y : (R)0;
+        y[j][e] = inv * (x[j][e] * (R)gain[j][e] * t.x + across);
       }
     store(y);
   };
@@ -243,42 +250,49 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
       *reinterpret_cast<P*>(dst + piece(j)) = p;
     }
   };
-  const int64_t at_scale = (int64_t)b * a.c.scale_b + slot;
   auto take = [&](int u, int hd) {
-    if (hd < H) {
-      if (a.norm_step || hd == first) gains(a.q_norm ? a.q_norm + (int64_t)hd * a.norm_step : nullptr);
-      made(0.f, u, a.q_norm != nullptr, [&](int j, int e) { return turn[j][e]; },
-           [&](const auto& y) { plain(y, (T*)a.q_out + (row * H + hd) * (int64_t)DH); });
-      return;
-    }
-    if (!store_kv) return;
-    const bool key = hd < H + Hkv;
-    const int h = hd - H - (key ? 0 : Hkv);
-    C* to = (C*)(key ? a.c.k : a.c.v) + b * a.c.stride_b + h * a.c.stride_h + slot * DH;
-    float* scale = (key ? a.c.k_scale : a.c.v_scale) + h * a.c.scale_h + at_scale;
-    auto store = [&](const auto& y) {
-      if constexpr (EIGHT<C>) store_codes<C, VEC, N>(y, lanes, l == 0, DH, to, scale, piece);
-      else plain(y, (T*)to);
-    };
-    if (key) {
-      gains(a.k_norm ? a.k_norm + (int64_t)h * a.norm_step : nullptr);
-      made(0.0, u, a.k_norm != nullptr, turn_of, store);
-    } else {
-      float y[N][VEC];
+    const bool query = hd < H, key = !query && hd < H + Hkv;
+    const int h = query ? hd : key ? hd - H : hd - H - Hkv;
+    const float* g = query ? a.q_norm : a.k_norm;
+    // (queries that share their gains keep them from one head to the next)
+    if ((query || key) && (!query || a.norm_step || hd == first)) gains(g ? g + (int64_t)h * a.norm_step : nullptr);
+    C* to = (C*)(key ? a.c.k : a.c.v) + b * a.c.stride_b + h * a.c.stride_h + slot0 * DH;
+    float* scale = (key ? a.c.k_scale : a.c.v_scale) + (int64_t)b * a.c.scale_b + h * a.c.scale_h + slot0;
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+    for (int r = 0; r < ROWS; ++r) {
+      if (query) {
+        if (r < count)
+          made(0.f, own[u][r], other[u][r], r, g != nullptr,
+               [&](const auto& y) { plain(y, (T*)a.q_out + ((row0 + r) * H + h) * (int64_t)DH); });
+        continue;
+      }
+      if (r >= kept) continue;
+      auto store = [&](const auto& y) {
+        if constexpr (EIGHT<C>) store_codes<C, VEC, N>(y, lanes, l == 0, DH, to + r * DH, scale + r, piece);
+        else plain(y, (T*)to + r * DH);
+      };
+      if (key) {
+        made(0.0, own[u][r], other[u][r], r, g != nullptr, store);
+      } else {
+        float y[N][VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) y[j][e] = Elem<T>::load(own[u][j].v, e);
-      store(y);
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) y[j][e] = Elem<T>::load(own[u][r][j].v, e);
+        store(y);
+      }
     }
   };
-  for (int h0 = first; h0 < heads; h0 += KR_HEADS * step) {
+  for (int h0 = first; h0 < heads; h0 += HEADS * step) {
     if (h0 != first) request(h0);
 #pragma unroll
-    for (int u = 0; u < KR_HEADS; ++u)
+    for (int u = 0; u < HEADS; ++u)
       if (h0 + u * step < heads) take(u, h0 + u * step);
   }
 }
+
+// Rows from which on they go four to a workgroup.
+constexpr int KR_MANY = 2048;
 
 static int pow2_at_least(int x) {
   int p = 1;
@@ -297,23 +311,27 @@ static adt_status norm_rope(NormRopeRows a, bool inter, hipStream_t st) {
   for (int64_t s : strides) wide = wide && s % V == 0;
   for (int64_t s : cache) wide = wide && s % code == 0;
   const int lanes = wide ? pow2_at_least(a.c.Dh / V) : WAVE;
-  // few rows: a row's heads over several workgroups until some 1024 are there
   const int per = KR_THREADS / lanes;
   int parts = (a.H + 2 * a.c.heads + per - 1) / per;
   const int64_t rows = (int64_t)a.c.B * a.n_max;
-  parts = (int)std::min<int64_t>(parts, std::max<int64_t>(1, 1024 / rows));
+  const bool many = rows >= KR_MANY && a.n_max >= 4;
+  // few rows: a row's heads over several workgroups until some 1024 are there
+  parts = many ? 1 : (int)std::min<int64_t>(parts, std::max<int64_t>(1, 1024 / rows));
   // (a launch has fewer than 2^32 threads in a dimension, or it wraps: more rows take several)
   constexpr int MOST = 1 << 23;
-#define ADT_NR(VECV, INTERV) norm_rope_kernel<T, C, VECV, INTERV><<<grid, KR_THREADS, 0, st>>>(a, lanes)
+#define ADT_NR(VECV, INTERV)                                                                        \
+  if (many) norm_rope_kernel<T, C, VECV, INTERV, 1, 4><<<grid, KR_THREADS, 0, st>>>(a, lanes);      \
+  else norm_rope_kernel<T, C, VECV, INTERV, 3, 1><<<grid, KR_THREADS, 0, st>>>(a, lanes)
   for (int64_t r0 = 0; r0 < a.n_max; r0 += MOST) {
     a.row0 = (int)r0;
-    const dim3 grid((unsigned)std::min<int64_t>(MOST, a.n_max - r0), parts, a.c.B);
+    const int64_t left = std::min<int64_t>(MOST, a.n_max - r0);
+    const dim3 grid((unsigned)(many ? (left + 3) / 4 : left), parts, a.c.B);
     if (wide) {
-      if (inter) ADT_NR(V, true);
-      else ADT_NR(V, false);
+      if (inter) { ADT_NR(V, true); }
+      else { ADT_NR(V, false); }
     } else {
-      if (inter) ADT_NR(1, true);
-      else ADT_NR(1, false);
+      if (inter) { ADT_NR(1, true); }
+      else { ADT_NR(1, false); }
     }
     ADT_LAUNCH_CHECK();
   }
