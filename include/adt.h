@@ -329,7 +329,7 @@ typedef struct {
  * type, in one pass: each head's row x of q (k) becomes
  *   y = x * g / sqrt(mean x^2 + eps),  then rotated as by adt_rope_append,
  * g = q_norm (k_norm): fp32 [Dh], or [H][Dh] ([heads][Dh]) where norm_per_head is 1; NULL: that side
- * is not normalised.  Values go to the cache as they are.  Keys are made in double up to their
+ * is not normalised.  eps >= 2^-126.  Values go to the cache as they are.  Keys are made in double up to their
  * rounding into the cache, so that codes are those of the formula; queries in fp32.
  * q, k, v, ld*, pos, kv_len, n_rows, freq, gain, rot_dim, layout, n_max, q_out as in
  * adt_rope_append, with B, heads and Dh those of the cache; slots at or past cache->cap are left out

@@ -68,7 +68,8 @@ extern "C" adt_status adt_norm_rope_append(const void* q, const void* k, const v
   ADT_CHECK_ARG(n_max >= 1 && H >= 1 && (norm_per_head == 0 || norm_per_head == 1), ADT_E_ARG,
                 "norm_rope_append: n_max=%d H=%d norm_per_head=%d", n_max, H, norm_per_head);
   ADT_CHECK_ARG(std::isfinite(gain), ADT_E_ARG, "norm_rope_append: gain");
-  ADT_CHECK_ARG((!q_norm && !k_norm) || (std::isfinite(eps) && eps > 0.f), ADT_E_ARG, "norm_rope_append: eps");
+  ADT_CHECK_ARG((!q_norm && !k_norm) || (std::isfinite(eps) && eps >= 1.17549435e-38f), ADT_E_ARG,
+                "norm_rope_append: eps");
   ADT_CHECK_ARG(rot_dim >= 2 && rot_dim <= Dh && rot_dim % 2 == 0, ADT_E_SHAPE, "norm_rope_append: rot_dim %d of %d",
                 rot_dim, Dh);
   ADT_CHECK_ARG((int64_t)H + 2 * (int64_t)heads <= (1 << 20), ADT_E_SHAPE, "norm_rope_append: %d and %d heads", H, heads);

@@ -166,23 +166,21 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
     cs32[r][p] = make_float2((float)(t.x * a.gain), (float)(t.y * a.gain));
   }
   __syncthreads();
-  // y = x c + other s, s with the sign that the half has; (1, 0) where a dim is not rotated
+  // y = x c + other s, s with the sign that the half has
   auto turn_of = [&](auto zero, int r, int j, int e) {
     const int d = piece(j) + e;
+    const bool second = INTER ? d & 1 : d >= half;
+    const int p = INTER ? d / 2 : second ? d - half : d;
     struct {
       decltype(zero) x, y;
-    } t{1, 0};
-    if (d < rot) {
-      const bool second = INTER ? d & 1 : d >= half;
-      const int p = INTER ? d / 2 : second ? d - half : d;
-      if constexpr (sizeof(zero) == 8) t.x = cs[r][p].x, t.y = cs[r][p].y;
-      else t.x = cs32[r][p].x, t.y = cs32[r][p].y;
-      if (!second) t.y = -t.y;
-    }
+    } t;
+    if constexpr (sizeof(zero) == 8) t.x = cs[r][p].x, t.y = cs[r][p].y;
+    else t.x = cs32[r][p].x, t.y = cs32[r][p].y;
+    if (!second) t.y = -t.y;
     return t;
   };
 
-  // a head's gains at this lane's dims and at their mates (none: 1)
+  // a head's gains at this lane's dims, and at their mates where those lie outside the piece (none: 1)
   float gain[N][VEC], mate_gain[N][VEC];
   auto gains = [&](const float* g) {
 #pragma unroll
@@ -207,7 +205,7 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         gain[j][e] = x.v[e];
-        mate_gain[j][e] = MATES ? y.v[e] : x.v[e ^ 1];
+        if constexpr (MATES) mate_gain[j][e] = y.v[e];
       }
     }
   };
@@ -226,18 +224,39 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
       for (int j = 0; j < N; ++j)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) ss += x[j][e] * x[j][e];
-      inv = (R)1 / sqrt(group_sum(ss, lanes) / (R)DH + (R)a.eps);
+      ss = group_sum(ss, lanes);
+      // (the hardware's reciprocal root of an fp32 number is within its last bit; squares that leave
+      // fp32 are added up again in double)
+      if (sizeof(R) == 4 && ss <= 3.402823466e38f) {
+        inv = __builtin_amdgcn_rsqf((float)ss * (1.f / (float)DH) + a.eps);
+      } else {
+        double s = (double)ss;
+        if constexpr (sizeof(R) == 4) {
+          s = 0.0;
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s += (double)x[j][e] * (double)x[j][e];
+          s = group_sum(s, lanes);
+        }
+        inv = (R)(1.0 / sqrt(s / (double)DH + (double)a.eps));
+      }
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+    for (int j = 0; j < N; ++j) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[j][e] *= (R)gain[j][e];
+      // (a piece is rotated as a whole, or not: a dim that is not takes nothing of another)
+      const bool turned = piece(j) < rot;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const R w = MATES ? (R)Elem<T>::load(mates[j].v, e) : x[j][e ^ 1];
+        y[j][e] = x[j][e] * inv;
+        if (!turned) continue;
+        const R w = MATES ? (R)Elem<T>::load(mates[j].v, e) * (R)mate_gain[j][e] : x[j][e ^ 1];
         const auto t = turn_of(zero, r, j, e);
-        // (a dim that is not rotated takes nothing of another, whatever that holds)
-        const R across = piece(j) + e < rot ? w * (R)mate_gain[j][e] * t.y : (R)0;
-        y[j][e] = inv * (x[j][e] * (R)gain[j][e] * t.x + across);
+        y[j][e] = inv * (x[j][e] * t.x + w * t.y);
       }
+    }
     store(y);
   };
   auto plain = [&](const auto& y, T* dst) {

@@ -106,6 +106,7 @@ def append_case(rt, dtype, kind, norm, layout, B, n, H, Hkv, Dh, rot, fused=True
                 rows=None, in_place=False, seed=1, edit=None):
     g = gen(seed)
     cap = cap or 40 + n
+    eps = float(np.float32(eps))            # the call takes it in fp32 (1e-5 is not one: off by 2^-26 of it)
     if fused:
         qkv = 2 * normal(g, dtype, B, n, (H + 2 * Hkv) * Dh)
         q, k, v = (t.unflatten(-1, (-1, Dh)) for t in qkv.split([H * Dh, Hkv * Dh, Hkv * Dh], -1))
@@ -219,6 +220,34 @@ def test_append_odd_rows(rt, kind, wide):
 
     append_case(rt, "f32", kind, "shared", "half", 1, 11, 2, 2, Dh, Dh, edit=edit)
     append_case(rt, "f32", kind, "none", "half", 1, 11, 2, 2, Dh, Dh, edit=edit)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_append_many_rows(rt, layout):
+    """Enough rows for four of them to a workgroup: ragged, past the cache's end, of sizes whose squares leave
+    fp32, and sequences shorter than four rows."""
+    print(f"append many {layout}", flush=True)
+
+    def edit(k, v):
+        k[0, 5] *= 2.0 ** 100
+        k[0, 6] *= 2.0 ** -100
+
+    for dtype, kind, norm in (("bf16", "int8", "heads"), ("bf16", "bf16", "shared"), ("f32", "e4m3", "shared"), ("f32", "f32", "none")):
+        append_case(rt, dtype, kind, norm, layout, 3, 703, 6, 2, 64, 48, cap=690, rows=[703, 2, 650], edit=edit)
+        append_case(rt, dtype, kind, norm, layout, 1, 2049, 4, 4, 30, 10)
+    append_case(rt, "bf16", "e4m3", "shared", layout, 1100, 2, 2, 1, 64, 64)
+
+
+def test_append_large_queries(rt):
+    """Queries whose squares leave fp32."""
+    g = gen(12)
+    q, kv = 2.0 ** 90 * normal(g, "f32", 1, 3, 4, 64), normal(g, "f32", 1, 3, 4, 64)
+    cache = new_cache(rt, g, "f32", 1, 4, 8, 64)
+    freq, _ = rt.rope_freqs(64)
+    pos, w = i32([[5, 6, 7]]), torch.ones(64, device="cuda")
+    out = rt.norm_rope_append(q, kv, kv, pos, i32([0]), i32([3]), freq, cache, q_norm=w)
+    want, length = made(q, w, float(np.float32(1e-5)), pos, freq, 1.0, "half")
+    assert torch.all((out.double() - want).abs() <= STEP["f32"] * want.abs() + 2.0 ** -20 * length)
 
 
 # ---------------------------------------------------------------------------- conversion

@@ -51,7 +51,7 @@ APPEND = dict(q=FAR, k=FAR + 0x10000, v=FAR + 0x20000, ldq=256, ldk=128, ldv=128
 @pytest.mark.parametrize("changed,code", [
     (dict(q=None), "E_ARG"), (dict(freq=None), "E_ARG"), (dict(n_rows=None), "E_ARG"), (dict(q_out=None), "E_ARG"),
     (dict(dtype=2), "E_ARG"), (dict(layout=2), "E_ARG"), (dict(n_max=0), "E_ARG"), (dict(H=0), "E_ARG"), (dict(per_head=2), "E_ARG"),
-    (dict(gain=math.inf), "E_ARG"), (dict(eps=0.0), "E_ARG"), (dict(eps=math.nan), "E_ARG"), (dict(rot=66), "E_SHAPE"),
+    (dict(gain=math.inf), "E_ARG"), (dict(eps=0.0), "E_ARG"), (dict(eps=math.nan), "E_ARG"), (dict(eps=1e-39), "E_ARG"), (dict(rot=66), "E_SHAPE"),
     (dict(rot=0), "E_SHAPE"), (dict(rot=33), "E_SHAPE"), (dict(ldq=255), "E_SHAPE"), (dict(ldk=127), "E_SHAPE"),
     (dict(ldv=127), "E_SHAPE"), (dict(q_out=FAR, ldq=512), "E_SHAPE"), (dict(q_out=FAR + 16), "E_ARG"),
     (dict(q_out=FAR + 0x10000), "E_ARG"), (dict(q_out=FAR + 0x20000 - 16), "E_ARG"), (dict(H=1 << 20, ldq=64 << 20), "E_SHAPE"),
