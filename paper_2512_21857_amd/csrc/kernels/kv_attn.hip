@@ -57,10 +57,6 @@ __device__ __forceinline__ Reach reach_of(int len, int n_tail, int cap, const Kv
   return r;
 }
 template <int KT>
-__device__ __forceinline__ Reach own_reach(const KvAttn& a, const KvPlan& p, int b) {
-  return reach_of<KT>(a.own.len[b], a.n_tail[b], a.own.cap, p.own, 1);
-}
-template <int KT>
 __device__ __forceinline__ Reach pre_reach(const KvAttn& a, const KvPlan& p, int b) {
   if (!a.groups) return Reach{};
   return reach_of<KT>(a.pre.len[b / a.group], 0, a.pre.cap, p.pre, 0);
@@ -940,72 +936,95 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
 }
 
 // ---------------------------------------------------------------------------- merge
-// A row's parts, own splits then the prefix's: DH / 4 threads take four dims each, and `count` groups of
-// them deal out the parts, up to four requested at a time; the groups' sums meet in LDS, in their order.
-template <typename T, int KT>
+// A row's parts, own splits then the prefix's, in that order: DH / 4 threads take four dims each.  Many
+// rows: ROWS of them a thread, two parts of each requested at a time.  Few rows of many parts (ROWS = 1):
+// `count` groups of threads deal out the parts, and their sums meet in LDS, in their order.
+template <typename T, int KT, int ROWS>
 __global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p, int count, const float* __restrict__ part_o,
                                                               const float* __restrict__ part_ml) {
-  __shared__ f32x4 so[KA_THREADS];
-  __shared__ float2 sml[KA_THREADS];
+  __shared__ f32x4 so[ROWS == 1 ? KA_THREADS : 1];
+  __shared__ float2 sml[ROWS == 1 ? KA_THREADS : 1];
   const int per = a.Dh / 4, b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
   const int n_q = a.n_q[b], len = a.own.len[b], n_tail = a.n_tail[b];          // (one wait for all)
   const int n_own = reach_of<KT>(len, n_tail, a.own.cap, p.own, 1).live, n = n_own + pre_reach<KT>(a, p, b).live;
-  const int unit = tid / per, grp = unit % count, d = tid % per * 4;
-  const int row = blockIdx.x * (KA_THREADS / per / count) + unit / count, live = max(0, min(n_q, a.nq_max)) * a.G;
-  if (n == 1 || (int)blockIdx.x * (KA_THREADS / per / count) >= live) return;
-  const RowAt at{b, row / a.G, row % a.G};
-  const int64_t base = at.part(a, p, h, 0), rows = (int64_t)a.nq_max * a.G;
-  float m = -INFINITY, l = 0.f;
-  f32x4 o{0.f, 0.f, 0.f, 0.f};
-  auto add = [&](float pm, float pl, const f32x4& po) {       // at the maximum m
+  const int fit = KA_THREADS / per, unit = tid / per, d = tid % per * 4;
+  const int grp = ROWS == 1 ? unit % count : 0, step = ROWS == 1 ? count : 1;
+  const int each = ROWS == 1 ? fit / count : fit * ROWS, live = max(0, min(n_q, a.nq_max)) * a.G;
+  const int row0 = blockIdx.x * each + (ROWS == 1 ? unit / count : unit);
+  if (n == 1 || (int)blockIdx.x * each >= live) return;
+  // rows row0, row0 + fit, ...; one past the last repeats it
+  constexpr int AT_ONCE = ROWS == 1 ? 4 : 2;
+  const int64_t rows = (int64_t)a.nq_max * a.G, base = ((int64_t)b * a.Hkv + h) * p.parts * rows;
+  float m[ROWS], l[ROWS];
+  f32x4 o[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+    o[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  auto add = [](float pm, float pl, const f32x4& po, float m, float& l, f32x4& o) {       // at the maximum m
     const float wt = part_weight(pm, pl, m);
     if (wt == 0.f && pl == pl) return;
     l += wt * pl;
     o += wt * po;
   };
-  for (int s0 = row < live ? grp : n; s0 < n; s0 += 4 * count) {
-    float2 ml[4];
-    f32x4 x[4];
+  for (int s0 = row0 < live ? grp : n; s0 < n; s0 += AT_ONCE * step) {
+    float2 ml[ROWS][AT_ONCE];
+    f32x4 x[ROWS][AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      ml[i] = make_float2(-INFINITY, 0.f);
-      const int s = s0 + i * count;
-      if (s >= n) continue;
-      const int64_t from = base + (s < n_own ? s : p.own.splits + s - n_own) * rows;
-      ml[i] = *reinterpret_cast<const float2*>(part_ml + from * 2);
-      x[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(part_o + from * a.Dh + d));
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        ml[r][i] = make_float2(-INFINITY, 0.f);
+        const int s = s0 + i * step;
+        if (s >= n) continue;
+        const int64_t from = base + (s < n_own ? s : p.own.splits + s - n_own) * rows + min(row0 + r * fit, live - 1);
+        ml[r][i] = *reinterpret_cast<const float2*>(part_ml + from * 2);
+        x[r][i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(part_o + from * a.Dh + d));
+      }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      float M = m[r];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) M = fmaxf(M, ml[r][i].x);
+      const float down = m[r] == -INFINITY ? 1.f : exp2_hw(m[r] - M);
+      m[r] = M;
+      l[r] *= down;
+      o[r] *= down;
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+        if (s0 + i * step < n) add(ml[r][i].x, ml[r][i].y, x[r][i], m[r], l[r], o[r]);
     }
-    float M = m;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) M = fmaxf(M, ml[i].x);
-    const float down = m == -INFINITY ? 1.f : exp2_hw(m - M);
-    m = M;
-    l *= down;
-    o *= down;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (s0 + i * count < n) add(ml[i].x, ml[i].y, x[i]);
   }
-  if (count > 1) {
-    so[tid] = o;
-    sml[tid] = make_float2(m, l);
+  if (ROWS == 1 && count > 1) {
+    so[tid] = o[0];
+    sml[tid] = make_float2(m[0], l[0]);
     __syncthreads();
     if (grp > 0) return;
     const int groups = min(count, n);
-    for (int g = 1; g < groups; ++g) m = fmaxf(m, sml[tid + g * per].x);
-    l = 0.f;
-    o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int g = 0; g < groups; ++g) add(sml[tid + g * per].x, sml[tid + g * per].y, so[tid + g * per]);
+    for (int g = 1; g < groups; ++g) m[0] = fmaxf(m[0], sml[tid + g * per].x);
+    l[0] = 0.f;
+    o[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < groups; ++g) add(sml[tid + g * per].x, sml[tid + g * per].y, so[tid + g * per], m[0], l[0], o[0]);
   }
-  if (row >= live) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  store4((T*)a.out + at.q(a, h) + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int row = row0 + r * fit;
+    if (row >= live) continue;
+    const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+    store4((T*)a.out + RowAt{b, row / a.G, row % a.G}.q(a, h) + d, o[r][0] * inv, o[r][1] * inv, o[r][2] * inv, o[r][3] * inv);
+  }
 }
 
 // ---------------------------------------------------------------------------- host
-// Splits: as many as give the workgroups that the CUs hold at once equal shares of the keys of both
-// parts, by the bounds the launch is given; at least three units of 64 keys pay for a split's start and
-// its partial results.
+// Splits: as many as give the workgroups that the CUs hold at once (two each) equal shares of the keys of
+// both parts, by the bounds the launch is given.  At least eight units of 64 keys pay for a split's start
+// and end, its partial results and their merge: one row of 32 heads over 300 slots 11.8 us with eight,
+// 11.1 + 3.9 (attention + merge) with three, 11.9 with twelve; over 700 slots 12.7 + 4.0, 12.1 + 3.9, 16.2;
+// over 8000 13.7 + 3.9, 13.8 + 4.6, 15.6 + 3.8; a 61-row tree of 32 heads over 100 slots 12.1, 13.0 + 3.8;
+// over 2300 18.3 + 4.8, 18.6 + 6.6, 19.9 + 3.9.  Shares for 1024 or 1536 workgroups in place of 512 cost more in
+// partial results than they even out (sixteen ragged 61-row trees 67 + 0, 68 + 8.7, 69 + 9.7 us).
 static KvPlan kv_plan(const KvAttn& a) {
   KvPlan p{};
   const bool f32 = a.type == ADT_F32;
@@ -1022,7 +1041,7 @@ static KvPlan kv_plan(const KvAttn& a) {
     pre_pairs = (int64_t)a.groups * a.Hkv * p.pre.blocks;
     pre_units = ((int64_t)a.pre.cap + KA_UNIT - 1) / KA_UNIT;
   }
-  constexpr int64_t SLOTS = 512, LEAST = 3;
+  constexpr int64_t SLOTS = 512, LEAST = 8;
   const int64_t per = std::max<int64_t>(LEAST, (own_pairs * own_units + pre_pairs * pre_units + SLOTS - 1) / SLOTS);
   auto split = [&](KvSide& s, int64_t pairs, int64_t units) {
     s.per = (int)std::min<int64_t>(per, 1 << 30);
@@ -1064,12 +1083,21 @@ adt_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t st) {
 #undef ADT_KA
   ADT_LAUNCH_CHECK();
   if (p.parts == 1) return ADT_OK;
-  // a thread for every four outputs, or for few outputs of many parts several
+  // a thread for every four outputs, or for few outputs of many parts several, or for many outputs one for
+  // sixteen: trees of 61 rows of 32 heads of 128 dims, two or three parts, with one row a thread and with
+  // four: 4 trees 6.9, 7.9 us, 8 trees 7.9, 7.3, 16 trees 11.6, 7.9, 32 trees 21.1, 14.3
   const int fit = KA_THREADS / (a.Dh / 4), rows = a.nq_max * a.G;
-  const int count = p.parts > 8 && (int64_t)a.B * a.Hkv * rows * (a.Dh / 4) < 65536 ? fit : 1;
-  const dim3 grid((unsigned)(((int64_t)rows * count + fit - 1) / fit), a.Hkv, a.B);
-  if (a.type == ADT_F32) kv_merge_kernel<float, 16><<<grid, KA_THREADS, 0, st>>>(a, p, count, part_o, part_ml);
-  else kv_merge_kernel<uint16_t, 32><<<grid, KA_THREADS, 0, st>>>(a, p, count, part_o, part_ml);
+  const int64_t outputs = (int64_t)a.B * a.Hkv * rows * (a.Dh / 4);
+  const int count = p.parts > 8 && outputs < 65536 ? fit : 1;
+  const bool many = outputs >= 1 << 18;
+  const int64_t each = many ? 4 * fit : fit / count;
+  const dim3 grid((unsigned)((rows + each - 1) / each), a.Hkv, a.B);
+#define ADT_KM(TV, KTV)                                                                                     \
+  if (many) kv_merge_kernel<TV, KTV, 4><<<grid, KA_THREADS, 0, st>>>(a, p, count, part_o, part_ml);         \
+  else kv_merge_kernel<TV, KTV, 1><<<grid, KA_THREADS, 0, st>>>(a, p, count, part_o, part_ml)
+  if (a.type == ADT_F32) { ADT_KM(float, 16); }
+  else { ADT_KM(uint16_t, 32); }
+#undef ADT_KM
   ADT_LAUNCH_CHECK();
   return ADT_OK;
 }

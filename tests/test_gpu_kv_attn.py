@@ -205,6 +205,16 @@ def test_many_sequences_behind_one_prefix(rt, kind):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+def test_many_rows_of_few_parts(rt, kind):
+    """More than 2^18 groups of four outputs, whose parts meet several rows to a thread; row counts that are no
+    multiple of them, one and none."""
+    B = 9
+    c = Case(rt, kind, 32, 32, 128, 61, [3 + 17 * b for b in range(B)], rows=[61, 60, 1, 0, 33, 32, 31, 17, 61], P=[130])
+    print(f"many rows {kind}", flush=True)
+    c.check(rt)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_nothing_to_see(rt, kind):
     """Rows without any slot give zeros, with and without a prefix; empty prefixes, trees and sequences."""
     print(f"nothing {kind}", flush=True)
