@@ -808,51 +808,61 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
 #pragma unroll
     for (int d = 0; d < OT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  for (int unit = j.sp; unit < j.reach.units; unit += n_live) {
-    const int st = unit * (KA_UNIT / KT) + wave;
-    if (st >= steps) break;
+  // this wave's steps: those of the split's units that are its own
+  const int stride = n_live * (KA_UNIT / KT);
+  struct Span {
+    int k0, last;
+  };
+  auto span = [&](int st) {
     const bool tail = st >= j.reach.prefix_steps;
-    const int k0 = tail ? L + (st - j.reach.prefix_steps) * KT : st * KT, k_last = (tail ? total : L) - 1;
-    f32x4 k[DH / 16], v[4][DH / 64];
-    {
-      const float* src = kb + (int64_t)min(k0 + l, k_last) * DH + g * 4;
+    return Span{tail ? L + (st - j.reach.prefix_steps) * KT : st * KT, (tail ? total : L) - 1};
+  };
+  // the next step's keys are requested when this one's scores are done, its values when this one's are used
+  f32x4 k[DH / 16], v[4][DH / 64];
+  auto fetch_k = [&](int st) {
+    if (st >= steps) return;
+    const Span s = span(st);
+    const float* src = kb + (int64_t)min(s.k0 + l, s.last) * DH + g * 4;
 #pragma unroll
-      for (int i = 0; i < DH / 16; ++i) k[i] = *reinterpret_cast<const f32x4*>(src + i * 16);
-    }
-    bool odd = false;
+    for (int i = 0; i < DH / 16; ++i) k[i] = *reinterpret_cast<const f32x4*>(src + i * 16);
+  };
+  auto fetch_v = [&](int st) {
+    if (st >= steps) return;
+    const Span s = span(st);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int key = k0 + 4 * g + e;
-      const float* src = vb + (int64_t)min(key, k_last) * DH + 4 * l;
+      const float* src = vb + (int64_t)min(s.k0 + 4 * g + e, s.last) * DH + 4 * l;
 #pragma unroll
-      for (int c = 0; c < DH / 64; ++c) {
-        v[e][c] = *reinterpret_cast<const f32x4*>(src + c * 64);
-        if (key > k_last) v[e][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (tail) {
-          // a value that is not finite may only meet the rows that see it: it is taken out here, added below
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (not_finite(v[e][c][i])) v[e][c][i] = 0.f, odd = true;
-        }
-      }
+      for (int c = 0; c < DH / 64; ++c) v[e][c] = *reinterpret_cast<const f32x4*>(src + c * 64);
     }
-    odd = __any(odd);
+  };
+  int st = j.sp * (KA_UNIT / KT) + wave;
+  fetch_k(st);
+  fetch_v(st);
+  for (; st < steps; st += stride) {
+    const bool tail = st >= j.reach.prefix_steps;
+    const int k0 = span(st).k0, k_last = span(st).last;
+    f32x4 x[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      f32x4 x{0.f, 0.f, 0.f, 0.f};
+      x[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < DH / 16; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q[t][i][e], x, 0, 0, 0);
-      auto sees = [&](int key) {
-        const int n = k0 + key - L;
-        return (k0 + key <= k_last) & (!tail | (bool)((n < 64 ? aw0[t] : aw1[t]) >> (n & 63) & 1));
-      };
+        for (int e = 0; e < 4; ++e) x[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[i][e], q[t][i][e], x[t], 0, 0, 0);
+    }
+    fetch_k(st + stride);
+    auto sees = [&](int t, int key) {
+      const int n = k0 + key - L;
+      return (k0 + key <= k_last) & (!tail | (bool)((n < 64 ? aw0[t] : aw1[t]) >> (n & 63) & 1));
+    };
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
       float mx = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[e] = sees(4 * g + e) ? x[e] : -INFINITY;
-        mx = fmaxf(mx, x[e]);
+        x[t][e] = sees(t, 4 * g + e) ? x[t][e] : -INFINITY;
+        mx = fmaxf(mx, x[t][e]);
       }
       mx = xor32_max(xor16_max(mx));
       float m_use;
@@ -860,26 +870,43 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
       float sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[e] = exp2_hw(fmaf(x[e], scale_log2, -m_use));
-        sum += x[e];
+        x[t][e] = exp2_hw(fmaf(x[t][e], scale_log2, -m_use));
+        sum += x[t][e];
       }
       sm[t].l = sm[t].l * alpha + sum;
       if (!__all(alpha == 1.f)) {
 #pragma unroll
         for (int d = 0; d < OT; ++d) o[t][d] *= alpha;
       }
+    }
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < DH / 64; ++c) {
+        if (k0 + 4 * g + e > k_last) v[e][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (tail) {
+          // a value that is not finite may only meet the rows that see it: it is taken out here, added below
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (not_finite(v[e][c][i])) v[e][c][i] = 0.f, odd = true;
+        }
+      }
+    odd = __any(odd);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
       // output tile 4 c + i takes the dims 64 c + 4 m + i of its rows m
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int d = 0; d < OT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][d / 4][d % 4], x[e], o[t][d], 0, 0, 0);
+        for (int d = 0; d < OT; ++d) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e][d / 4][d % 4], x[t][e], o[t][d], 0, 0, 0);
       if (odd) {
         for (int key = 0; key < KT; ++key) {
           float have = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) have = key % 4 == e ? x[e] : have;
+          for (int e = 0; e < 4; ++e) have = key % 4 == e ? x[t][e] : have;
           const float pk = __shfl(have, l + 16 * (key / 4), WAVE);
-          const bool vis = sees(key);
+          const bool vis = sees(t, key);
           const float* src = vb + (int64_t)min(k0 + key, k_last) * DH;
 #pragma unroll
           for (int d = 0; d < OT; ++d)
@@ -891,6 +918,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
         }
       }
     }
+    fetch_v(st + stride);
   }
 
 #pragma unroll
@@ -1024,7 +1052,10 @@ __global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p
 // 11.1 + 3.9 (attention + merge) with three, 11.9 with twelve; over 700 slots 12.7 + 4.0, 12.1 + 3.9, 16.2;
 // over 8000 13.7 + 3.9, 13.8 + 4.6, 15.6 + 3.8; a 61-row tree of 32 heads over 100 slots 12.1, 13.0 + 3.8;
 // over 2300 18.3 + 4.8, 18.6 + 6.6, 19.9 + 3.9.  Shares for 1024 or 1536 workgroups in place of 512 cost more in
-// partial results than they even out (sixteen ragged 61-row trees 67 + 0, 68 + 8.7, 69 + 9.7 us).
+// partial results than they even out (sixteen ragged 61-row trees 67 + 0, 68 + 8.7, 69 + 9.7 us).  fp32, whose
+// waves take their steps one after the other from memory, at least two: one row over 300 slots 11.7 + 4.0
+// with two, 14.4 + 3.9 with three, 19.2 with eight; over 2000 11.8 + 4.0, 14.5 + 3.9, 26.4 + 4.0; over 8000 24.8 +
+// 5.2, 25.0 + 5.0, 28.7 + 4.6; a 61-row tree over 2300 45.7 + 4.8, 45.7 + 4.7, 55.5 + 4.8.
 static KvPlan kv_plan(const KvAttn& a) {
   KvPlan p{};
   const bool f32 = a.type == ADT_F32;
@@ -1041,7 +1072,7 @@ static KvPlan kv_plan(const KvAttn& a) {
     pre_pairs = (int64_t)a.groups * a.Hkv * p.pre.blocks;
     pre_units = ((int64_t)a.pre.cap + KA_UNIT - 1) / KA_UNIT;
   }
-  constexpr int64_t SLOTS = 512, LEAST = 8;
+  const int64_t SLOTS = 512, LEAST = f32 ? 2 : 8;
   const int64_t per = std::max<int64_t>(LEAST, (own_pairs * own_units + pre_pairs * pre_units + SLOTS - 1) / SLOTS);
   auto split = [&](KvSide& s, int64_t pairs, int64_t units) {
     s.per = (int)std::min<int64_t>(per, 1 << 30);
