@@ -376,9 +376,10 @@ adt_status adt_cache_compact(const adt_kv_cache* cache /*[host]*/, const int32_t
  *   bf16 multiplies codes as they are (bf16 holds them exactly) and applies the scales to scores and
  *   probabilities in fp32; softmax sums and outputs are fp32.
  * workspace: adt_cache_tree_attn_workspace_size() bytes (groups = 0: no prefix; 0 where none is
- *   needed, and for sizes that the call refuses), 16-byte aligned.  Dh 64 or 128, H a multiple of heads, B * heads <= 65535,
- *   addresses and cache strides multiples of 16 bytes (ADT_E_SHAPE); nq_max <= ADT_MAX_NODES,
- *   nq_max * H / heads <= 8192, workspace (ADT_E_CAPACITY). */
+ *   needed, and for sizes past the limits that follow), 16-byte aligned.  Dh 64 or 128, H a multiple
+ *   of heads, B * heads <= 65535, addresses and cache strides multiples of 16 bytes (ADT_E_SHAPE);
+ *   nq_max <= ADT_MAX_NODES, nq_max * H / heads <= 8192, workspace (ADT_E_CAPACITY).  A call whose rows
+ *   and splits come to 2^24 workgroups or more is refused as well (ADT_E_CAPACITY). */
 size_t adt_cache_tree_attn_workspace_size(int32_t B, int32_t H, int32_t heads, int32_t Dh, int32_t nq_max,
                                           int32_t kv_cap, int32_t groups, int32_t prefix_cap, int32_t type);
 adt_status adt_cache_tree_attn(const void* q, const adt_kv_cache* cache /*[host]*/, const int32_t* kv_len,

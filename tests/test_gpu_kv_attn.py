@@ -205,6 +205,40 @@ def test_many_sequences_behind_one_prefix(rt, kind):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+def test_the_largest_group(rt, kind):
+    """4096 sequences behind one prefix, one more is refused."""
+    B, Dh, P = 4096, 64, 70
+    g = gen(11)
+    cache, prefix = (rt.KVCache(*filled(g, kind, n, 1, s, Dh)) for n, s in ((B, 4), (1, P)))
+    dt = DT["f32" if kind == "f32" else "bf16"]
+    q = torch.empty(B, 1, 2, Dh, device="cuda").normal_(generator=g).to(dt)
+    kv_len = torch.arange(B, dtype=torch.int32, device="cuda") % 4
+    one = torch.ones(B, dtype=torch.int32, device="cuda")
+    mask = torch.zeros(B, 1, 2, dtype=torch.int64, device="cuda")
+    mask[:, :, 0] = 1
+    print(f"largest group {kind}", flush=True)
+    out = rt.cache_tree_attn(q, cache, kv_len, one, one, mask, prefix=prefix, prefix_len=i32([P]))
+    kd, vd = (values(x, s, slice(None), 0) for x, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)))
+    pk, pv = (values(x, s, 0, 0) for x, s in ((prefix.k, prefix.k_scale), (prefix.v, prefix.v_scale)))
+    k = torch.cat([pk[None].expand(B, -1, -1), kd], 1)
+    v = torch.cat([pv[None].expand(B, -1, -1), vd], 1)
+    see = torch.cat([torch.ones(B, P, dtype=torch.bool, device="cuda"), torch.arange(4, device="cuda")[None] <= kv_len[:, None]], 1)
+    qd, scale = q[:, 0].double(), 1 / math.sqrt(Dh)
+    x = ((qd[:, :, None] * k[:, None]).sum(-1) * scale).masked_fill(~see[:, None], -math.inf)
+    w = torch.softmax(x, -1)
+    want = (w[..., None] * v[:, None]).sum(2)
+    ds = ((qd.abs()[:, :, None] * k.abs()[:, None]).sum(-1).amax(-1, keepdim=True)) * (scale * (Dh + 3) * 2.0 ** -24)
+    rel = 2 * ds + 2.0 ** -20 + (P + 12) * 2.0 ** -24 + (0.0 if kind == "f32" else 2.0 ** -8)
+    tol = rel * (w[..., None] * v.abs()[:, None]).sum(2) + STEP["f32" if kind == "f32" else "bf16"] * want.abs() + 1e-30
+    assert ((out[:, 0].double() - want).abs() <= tol).all()
+    more = rt.KVCache.zeros(B + 1, 1, 4, Dh, DT[kind])
+    n = torch.ones(B + 1, dtype=torch.int32, device="cuda")
+    with pytest.raises(RuntimeError, match="sequences a group"):
+        rt.cache_tree_attn(torch.zeros(B + 1, 1, 2, Dh, dtype=dt, device="cuda"), more, n, n, n,
+                           torch.zeros(B + 1, 1, 2, dtype=torch.int64, device="cuda"), prefix=prefix, prefix_len=i32([P]))
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_many_rows_of_few_parts(rt, kind):
     """More than 2^18 groups of four outputs, whose parts meet several rows to a thread; row counts that are no
     multiple of them, one and none."""
