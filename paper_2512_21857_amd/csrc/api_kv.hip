@@ -50,6 +50,10 @@ static Stretch extent(const adt_kv_cache& c, const void* p) {
   const uint64_t elems = (uint64_t)(c.B - 1) * c.stride_b + (uint64_t)(c.heads - 1) * c.stride_h + (uint64_t)c.cap * c.Dh;
   return {(uintptr_t)p, elems * elem_bytes(c.type)};
 }
+static Stretch scale_extent(const adt_kv_cache& c, const float* p) {
+  const uint64_t n = (uint64_t)(c.B - 1) * c.scale_b + (uint64_t)(c.heads - 1) * c.scale_h + (uint64_t)c.cap;
+  return {(uintptr_t)p, n * sizeof(float)};
+}
 
 extern "C" adt_status adt_norm_rope_append(const void* q, const void* k, const void* v, int64_t ldq, int64_t ldk,
                                            int64_t ldv, const float* q_norm, const float* k_norm,
@@ -106,6 +110,11 @@ extern "C" adt_status adt_cache_convert(const adt_kv_cache* src, const adt_kv_ca
   for (const void* s : {src->k, src->v})
     for (const void* d : {dst->k, dst->v})
       ADT_CHECK_ARG(!overlap(extent(*src, s), extent(*dst, d)), ADT_E_ARG, "cache_convert: the caches overlap");
+  // (the scales are the eight-bit side's, beside the other side's keys and values)
+  const adt_kv_cache &codes = eight_bit(src->type) ? *src : *dst, &plain = eight_bit(src->type) ? *dst : *src;
+  for (const float* s : {codes.k_scale, codes.v_scale})
+    for (const void* x : {plain.k, plain.v})
+      ADT_CHECK_ARG(!overlap(scale_extent(codes, s), extent(plain, x)), ADT_E_ARG, "cache_convert: the caches overlap");
   return launch_cache_convert(*src, *dst, length, n_max, src_start, dst_start, (hipStream_t)stream);
 }
 

@@ -102,6 +102,17 @@ def test_cache_convert_refusals(L):
         assert call(L.adt_cache_convert, ok, **changed) == code, changed
 
 
+@pytest.mark.parametrize("scales", ["k_scale", "v_scale"])
+def test_cache_convert_refuses_scales_among_values(L, scales):
+    """1600 bytes of scales, 51200 of values: neither direction may write one while reading the other."""
+    from paper_2512_21857_amd import abi
+    for at in (FAR - 1584, FAR, FAR + 51184):
+        codes = cache(**{scales: at})
+        assert call(L.adt_cache_convert, {**CONVERT, "src": codes, "dst": plain(FAR)}) == abi.E_ARG, hex(at)
+        assert call(L.adt_cache_convert, {**CONVERT, "src": plain(FAR), "dst": codes}) == abi.E_ARG, hex(at)
+    assert "overlap" in abi.last_error()
+
+
 COMPACT = dict(cache=None, kv_len=FAKE, path=FAKE, stride=9, n_acc=FAKE, a_max=8, stream=None)
 
 
