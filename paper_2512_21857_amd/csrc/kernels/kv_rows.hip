@@ -5,6 +5,11 @@
 // All are bound by memory: a value is read once and written once.  A head's row of Dh values goes to a
 // group of neighbouring lanes, a 16-byte piece each, so that its sum of squares and its largest size
 // are a few lane exchanges away and every access is whole lines.
+//
+// Measured (a 4 GiB copy reads and writes 4.68 TB/s): 4001 rows of 32 query and 8 + 8 key and value heads
+// of 128 dims into int8, half of each head rotated, 28.9 us (3.1 TB/s); 61 rows of 32 heads into e4m3 6.0 us (latency);
+// sixteen e4m3 caches of 512 to 4096 slots of 8 heads read back 48-52 us (a copy's rate); 1100 slots of 32
+// heads put in int8 11.9 us (2.3 TB/s), read back 6.9 (4.0); 12 rows of each of 1024 slices moved 4.9 us (latency).
 #include <algorithm>
 
 #include "../eight_bit.h"
@@ -105,8 +110,8 @@ __device__ __forceinline__ void store_codes(const R (&y)[N][VEC], int lanes, boo
 
 // A workgroup takes ROWS rows, all their heads or a part of them; a group of `lanes` lanes takes a head, and
 // others after it, whose values are requested HEADS heads of all rows at once, the first ones before the
-// rows' sines and cosines are made (in LDS): the two waits pass together.  Many rows go four to a
-// workgroup, which then starts a quarter as often and reads a head's gains for four; few rows one, with
+// rows' sines and cosines are made (in LDS): the two waits pass together.  Many rows go two to a
+// workgroup, which then starts half as often and reads a head's gains for two; few rows one, with
 // three heads requested at once.  VEC values are 16 bytes where sizes and addresses allow it (N = 1 piece
 // a lane), else one value (a wave a head, N = 4).  A pair's other half is read from memory beside it (the
 // same lines).
@@ -310,8 +315,12 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
   }
 }
 
-// Rows from which on they go four to a workgroup.
-constexpr int KR_MANY = 2048;
+// Rows from which on they go two to a workgroup.  One, two and four to a workgroup, 32 + 8 + 8 heads of 128
+// dims into int8, rotated in halves: 1000 rows 12.3, 15.1, 20.6 us; 1536 18.6, 17.1; 4001 36.8, 32.4, 40.6; 8000 68.6, 59.8,
+// 65.0; half of each head in neighbouring pairs: 1250 rows 13.2, 15.2; 1536 16.0, 16.2; 1750 18.7, 17.8; fp32 into
+// fp32: 1250 17.5, 19.7; 1750 24.2, 21.6; 4001 45.3, 38.4, 36.1.  (Four hold so many registers that few
+// workgroups share a CU.)
+constexpr int KR_MANY = 1536;
 
 static int pow2_at_least(int x) {
   int p = 1;
@@ -333,18 +342,18 @@ static adt_status norm_rope(NormRopeRows a, bool inter, hipStream_t st) {
   const int per = KR_THREADS / lanes;
   int parts = (a.H + 2 * a.c.heads + per - 1) / per;
   const int64_t rows = (int64_t)a.c.B * a.n_max;
-  const bool many = rows >= KR_MANY && a.n_max >= 4;
+  const bool many = rows >= KR_MANY && a.n_max >= 2;
   // few rows: a row's heads over several workgroups until some 1024 are there
   parts = many ? 1 : (int)std::min<int64_t>(parts, std::max<int64_t>(1, 1024 / rows));
   // (a launch has fewer than 2^32 threads in a dimension, or it wraps: more rows take several)
   constexpr int MOST = 1 << 23;
 #define ADT_NR(VECV, INTERV)                                                                        \
-  if (many) norm_rope_kernel<T, C, VECV, INTERV, 1, 4><<<grid, KR_THREADS, 0, st>>>(a, lanes);      \
+  if (many) norm_rope_kernel<T, C, VECV, INTERV, 1, 2><<<grid, KR_THREADS, 0, st>>>(a, lanes);      \
   else norm_rope_kernel<T, C, VECV, INTERV, 3, 1><<<grid, KR_THREADS, 0, st>>>(a, lanes)
   for (int64_t r0 = 0; r0 < a.n_max; r0 += MOST) {
     a.row0 = (int)r0;
     const int64_t left = std::min<int64_t>(MOST, a.n_max - r0);
-    const dim3 grid((unsigned)(many ? (left + 3) / 4 : left), parts, a.c.B);
+    const dim3 grid((unsigned)(many ? (left + 1) / 2 : left), parts, a.c.B);
     if (wide) {
       if (inter) { ADT_NR(V, true); }
       else { ADT_NR(V, false); }
@@ -393,7 +402,8 @@ __device__ __forceinline__ ConvertSpan convert_span(const ConvertArgs& a, int b,
   return c;
 }
 
-// Codes to values: a group of lanes a row, 16 codes a lane (or one, and up to four pieces).
+// Codes to values: a group of lanes a row, 16 codes a lane (or one, and up to four pieces).  A lane takes one
+// row at a time; four in flight were no faster.
 template <typename C, typename T, int VEC>
 __global__ __launch_bounds__(KR_THREADS) void cache_read_kernel(ConvertArgs a, int lanes) {
   constexpr int N = VEC == 1 ? 4 : 1;

@@ -224,8 +224,8 @@ def test_append_odd_rows(rt, kind, wide):
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 def test_append_many_rows(rt, layout):
-    """Enough rows for four of them to a workgroup: ragged, past the cache's end, of sizes whose squares leave
-    fp32, and sequences shorter than four rows."""
+    """Enough rows for several of them to a workgroup: ragged, past the cache's end, of sizes whose squares leave
+    fp32, and sequences of two rows."""
     print(f"append many {layout}", flush=True)
 
     def edit(k, v):
@@ -236,6 +236,14 @@ def test_append_many_rows(rt, layout):
         append_case(rt, dtype, kind, norm, layout, 3, 703, 6, 2, 64, 48, cap=690, rows=[703, 2, 650], edit=edit)
         append_case(rt, dtype, kind, norm, layout, 1, 2049, 4, 4, 30, 10)
     append_case(rt, "bf16", "e4m3", "shared", layout, 1100, 2, 2, 1, 64, 64)
+
+
+@pytest.mark.parametrize("dtype,kind", [("bf16", "int8"), ("bf16", "e4m3"), ("f32", "f32")])
+def test_append_many_single_rows(rt, dtype, kind):
+    """A decoding step of many sequences: one row each, some with none, caches that are full."""
+    print(f"append single {dtype} {kind}", flush=True)
+    append_case(rt, dtype, kind, "shared", "half", 1600, 1, 2, 1, 64, 64, rows=[int(b % 5 > 0) for b in range(1600)])
+    append_case(rt, dtype, kind, "heads", "interleaved", 1537, 3, 2, 1, 64, 32, cap=4, rows=[b % 4 for b in range(1537)])
 
 
 def test_append_large_queries(rt):
