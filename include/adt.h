@@ -330,7 +330,8 @@ typedef struct {
  *   y = x * g / sqrt(mean x^2 + eps),  then rotated as by adt_rope_append,
  * g = q_norm (k_norm): fp32 [Dh], or [H][Dh] ([heads][Dh]) where norm_per_head is 1; NULL: that side
  * is not normalised.  eps >= 2^-126.  Values go to the cache as they are.  Keys are made in double up to their
- * rounding into the cache, so that codes are those of the formula; queries in fp32.
+ * rounding into the cache, so that codes are those of the formula; queries in fp32, with their values lessened
+ * first where squares, products or sums leave it, so they are infinite where the formula's result is.
  * q, k, v, ld*, pos, kv_len, n_rows, freq, gain, rot_dim, layout, n_max, q_out as in
  * adt_rope_append, with B, heads and Dh those of the cache; slots at or past cache->cap are left out
  * (debug builds record it).  cache->type: dtype, or an eight-bit type.  q_out must not overlap q (but

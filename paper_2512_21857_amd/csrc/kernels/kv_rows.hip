@@ -214,52 +214,68 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
       }
     }
   };
-  // one head of a row, queries in fp32 and keys in double
-  auto made = [&](auto zero, const P (&mine)[N], const P (&mates)[N], int r, bool norm, auto store) {
-    typedef decltype(zero) R;
-    R x[N][VEC], y[N][VEC];
-    R inv = (R)1;
+  // Sum of squares of a row's values times `unit`.
+  auto squares = [&](auto unit, const P (&mine)[N]) {
+    decltype(unit) ss = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[j][e] = (R)Elem<T>::load(mine[j].v, e);
-    if (norm) {
-      R ss = (R)0;
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) ss += x[j][e] * x[j][e];
-      ss = group_sum(ss, lanes);
-      // (the hardware's reciprocal root of an fp32 number is within its last bit; squares that leave
-      // fp32 are added up again in double)
-      if (sizeof(R) == 4 && ss <= 3.402823466e38f) {
-        inv = __builtin_amdgcn_rsqf((float)ss * (1.f / (float)DH) + a.eps);
-      } else {
-        double s = (double)ss;
-        if constexpr (sizeof(R) == 4) {
-          s = 0.0;
-#pragma unroll
-          for (int j = 0; j < N; ++j)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) s += (double)x[j][e] * (double)x[j][e];
-          s = group_sum(s, lanes);
-        }
-        inv = (R)(1.0 / sqrt(s / (double)DH + (double)a.eps));
+      for (int e = 0; e < VEC; ++e) {
+        const auto x = (decltype(unit))Elem<T>::load(mine[j].v, e) * unit;
+        ss += x * x;
       }
-    }
+    return group_sum(ss, lanes);
+  };
+  // This lane's values of a row, times `first` and `second` before anything else and `last` after, with the gains and
+  // the turns between them.
+  auto turned = [&](const P (&mine)[N], const P (&mates)[N], int r, auto first, auto second, auto last, auto& y) {
+    typedef decltype(first) R;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
+      R x[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[j][e] *= (R)gain[j][e];
+      for (int e = 0; e < VEC; ++e) x[e] = (R)Elem<T>::load(mine[j].v, e) * first * second * (R)gain[j][e];
       // (a piece is rotated as a whole, or not: a dim that is not takes nothing of another)
-      const bool turned = piece(j) < rot;
+      const bool whole = piece(j) < rot;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        y[j][e] = x[j][e] * inv;
-        if (!turned) continue;
-        const R w = MATES ? (R)Elem<T>::load(mates[j].v, e) * (R)mate_gain[j][e] : x[j][e ^ 1];
-        const auto t = turn_of(zero, r, j, e);
-        y[j][e] = inv * (x[j][e] * t.x + w * t.y);
+        y[j][e] = x[e] * last;
+        if (!whole) continue;
+        const R w = MATES ? (R)Elem<T>::load(mates[j].v, e) * first * second * (R)mate_gain[j][e] : x[e ^ 1];
+        const auto t = turn_of(first, r, j, e);
+        y[j][e] = last * (x[e] * t.x + w * t.y);
+      }
+    }
+  };
+  // one head of a row, queries in fp32 and keys in double
+  auto made = [&](auto zero, const P (&mine)[N], const P (&mates)[N], int r, bool norm, auto store) {
+    typedef decltype(zero) R;
+    R y[N][VEC];
+    if constexpr (sizeof(R) == 8) {
+      turned(mine, mates, r, 1.0, 1.0, norm ? 1.0 / sqrt(squares(1.0, mine) / (double)DH + (double)a.eps) : 1.0, y);
+    } else {
+      // the factor of a row's values times `unit` (the hardware's reciprocal root of an fp32 number is within its
+      // last bit)
+      auto factor = [&](float ss, float unit) { return __builtin_amdgcn_rsqf(ss * (1.f / (float)DH) + a.eps * unit * unit); };
+      const float ss = norm ? squares(1.f, mine) : 0.f;
+      const bool past = !(ss <= 3.402823466e38f);
+      bool again = past;
+      if (!past) {
+        turned(mine, mates, r, 1.f, 1.f, norm ? factor(ss, 1.f) : 1.f, y);
+        float odd = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) odd += y[j][e] * 0.f;        // NaN if any is not finite
+        again = odd != odd;
+      }
+      if (again) {
+        // Squares, or products with gains and turns, left fp32: the row's factor comes before those, and values whose
+        // squares are too large, or that have no factor, are made 2^70 times smaller first.
+        const float unit = norm && !past ? 1.f : 0x1p-70f;
+        float inv = 1.f;
+        if (norm) inv = factor(past ? squares(unit, mine) : ss, unit);
+        turned(mine, mates, r, unit, inv, norm ? 1.f : 0x1p70f, y);
       }
     }
     store(y);

@@ -258,6 +258,48 @@ def test_append_large_queries(rt):
     assert torch.all((out.double() - want).abs() <= STEP["f32"] * want.abs() + 2.0 ** -20 * length)
 
 
+def expect_queries(out, want, length, dtype):
+    """Queries are the formula's to the roundings counted above; past the type's largest value they are infinite."""
+    most = torch.finfo(DT[dtype]).max
+    got = out.double()
+    past = want.abs() > 1.01 * most
+    assert torch.equal(got[past], torch.sign(want[past]) * math.inf)
+    inside = want.abs() < 0.99 * most
+    assert torch.all(((got - want).abs() <= STEP[dtype] * want.abs() + 2.0 ** -20 * length)[inside])
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Dh,rot", [(1, 64, 48), (2, 30, 10), (800, 64, 64)])
+def test_append_queries_at_the_end_of_fp32(rt, dtype, layout, B, Dh, rot):
+    """Squares, products with the gains and sums of pairs that leave fp32 where the normalised query does not,
+    and pairs whose parts do where their sum does not: as they are, and among ordinary rows."""
+    print(f"append ends {dtype} {layout} B={B} Dh={Dh}", flush=True)
+    n, H, Hkv = 4, 3, 1
+    g = gen(21)
+    q = normal(g, "f32", B, n, H, Dh)
+    sign = torch.where(q < 0, -1.0, 1.0)
+    q[:, 0] = 3.3e38                                       # every pair's halves are the type's largest
+    q[:, 1] = sign[:, 1] * 3.3e38 * torch.rand(B, H, Dh, device="cuda", generator=g)
+    q[:, 2, 0] *= 2.0 ** 100                               # one head of an ordinary row
+    q = q.to(DT[dtype])
+    kv = normal(g, dtype, B, n, Hkv, Dh)
+    pos = torch.randint(0, 5000, (B, n), generator=g, device="cuda", dtype=torch.int32)
+    freq, _ = rt.rope_freqs(rot, 10000.0)
+    eps, L, rows = float(np.float32(1e-5)), i32([0] * B), i32([n] * B)
+    shared, heads = 1.0 + 2.0 * torch.rand(Dh, device="cuda", generator=g), 1.0 + torch.rand(H, Dh, device="cuda", generator=g)
+    for w, gain in ((shared, 1.25), (heads, 0.75), (None, 1.0), (None, 2.0)):
+        cache = new_cache(rt, g, dtype, B, Hkv, n, Dh)
+        kn = None if w is None else torch.ones(Hkv, Dh, device="cuda") if w.dim() == 2 else w
+        out = rt.norm_rope_append(q, kv, kv, pos, L, rows, freq, cache, q_norm=w, k_norm=kn, eps=eps, layout=layout, gain=gain)
+        expect_queries(out, *made(q, w, eps, pos, freq, gain, layout), dtype)
+    # gains so large that a value times them leaves fp32, and the row's factor brings it back
+    w = torch.full((Dh,), 2.0 ** 70, device="cuda")
+    q = 2.0 ** 60 * normal(g, dtype, B, n, H, Dh)
+    out = rt.norm_rope_append(q, kv, kv, pos, L, rows, freq, cache, q_norm=w, eps=eps, layout=layout)
+    expect_queries(out, *made(q, w, eps, pos, freq, 1.0, layout), dtype)
+
+
 # ---------------------------------------------------------------------------- conversion
 def convert_case(rt, dtype, kind, write, B, heads, Dh, cap, L, s0=None, d0=None, n_max=None, dcap=None, layers=0, seed=3, edit=None):
     g = gen(seed)
