@@ -170,6 +170,118 @@ __device__ __forceinline__ float part_weight(float m, float l, float M) {
   return m == -INFINITY && l == 0.f ? 0.f : exp2_hw(m - (M == -INFINITY ? 0.f : M));
 }
 
+// ---------------------------------------------------------------------------- rows that left fp32
+// Weighted values may add up to more than fp32 holds where it holds their mean: values past 2^120, or past 2^128 over
+// their number.  The output is then not finite though the sum of weights is, which every row is tested for where its
+// output is written; such a row is made again: by a wave, from all its keys, with weights of 2^-34 at most, so that
+// 2^32 of them keep the sum of the largest values below 2^126.  (Far slower, and by one code for all types.)
+
+// Whether any of N times four outputs is not finite, though the sum of weights l is.
+template <int N>
+__device__ __forceinline__ bool left_fp32(const f32x4 (&o)[N], float l) {
+  f32x4 x = o[0] * 0.f;
+#pragma unroll
+  for (int n = 1; n < N; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(o[n][e], 0.f, x[e]);
+  const float sum = (x[0] + x[1]) + (x[2] + x[3]);        // 0, or NaN
+  return sum != sum && !not_finite(l);
+}
+__device__ __forceinline__ float element(int type, const void* p, int64_t i) {
+  if (type == ADT_F32) return ((const float*)p)[i];
+  if (type == ADT_BF16) return bf2f(((const uint16_t*)p)[i]);
+  const uint8_t x = ((const uint8_t*)p)[i];
+  return type == ADT_E4M3 ? decode4<E4M3>(x).x : decode4<I8>(x).x;
+}
+// Row `row` (node and head of the group) of sequence b; all lanes of the wave take part.  A kernel's first argument is
+// `a`: read anew from where it lies, and the lane counted anew, they are not kept through the loops before, whose
+// registers they would take.
+__device__ __forceinline__ void row_again(int b, int h, int row) {
+  typedef const __attribute__((address_space(4))) uint32_t Word;
+  Word* args = (Word*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(args));
+  struct {
+    uint32_t w[sizeof(KvAttn) / 4];
+  } words;
+#pragma unroll
+  for (size_t i = 0; i < sizeof(KvAttn) / 4; ++i) words.w[i] = args[i];
+  const KvAttn a = __builtin_bit_cast(KvAttn, words);
+  const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), rows_type = a.type == ADT_F32 ? ADT_F32 : ADT_BF16;
+  const int64_t at = RowAt{b, row / a.G, row % a.G}.q(a, h);
+  const uint64_t* mask = a.mask + ((int64_t)b * a.nq_max + row / a.G) * ADT_MASK_WORDS;
+  float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};            // of dims lane and lane + 64
+#pragma unroll 1
+  for (int own = a.groups ? 0 : 1; own < 2; ++own) {
+    const KvPart& p = own ? a.own : a.pre;
+    const int64_t of = own ? b : b / a.group;
+    const int L = max(0, min(p.len[of], p.cap));
+    const int total = own ? (int)min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)p.cap) : L;
+    const int64_t base = of * p.sb + h * p.sh, scales = of * p.ssb + h * p.ssh;
+#pragma unroll 1
+    for (int64_t key0 = 0; key0 < total; key0 += WAVE) {
+      const int64_t key = key0 + lane, n = key - L;
+      const bool seen = key < total && (n < 0 || (mask[n / 64] >> (n % 64) & 1));
+      float x = -INFINITY, by = 1.f;
+      if (seen) {
+        x = 0.f;
+#pragma unroll 1
+        for (int d = 0; d < a.Dh; ++d) x = fmaf(element(rows_type, a.q, at + d), element(a.type, p.k, base + key * a.Dh + d), x);
+        x *= a.scale * LOG2E;
+        if (p.ks) x *= p.ks[scales + key], by = p.vs[scales + key];
+      }
+      const float top = fmaxf(m, wave_max(x)), ref = top == -INFINITY ? 0.f : top, down = top == m ? 1.f : exp2_hw(m - ref);
+      const float w = seen ? exp2_hw(x - ref) * 0x1p-34f : 0.f;
+      m = top;
+      l = l * down + w;
+      o[0] *= down;
+      o[1] *= down;
+#pragma unroll 1
+      for (int k = 0; k < WAVE; ++k) {
+        if (!__builtin_amdgcn_readlane(seen, k)) continue;
+        const float wk = __shfl(w * by, k, WAVE);
+        const int64_t v = base + (key0 + k) * a.Dh + lane;
+        o[0] += wk * element(a.type, p.v, v);
+        if (a.Dh > WAVE) o[1] += wk * element(a.type, p.v, v + WAVE);
+      }
+    }
+  }
+  l = wave_sum(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l, most = a.type == ADT_F32 ? 3.402823466e38f : 3.389531389e38f;
+  for (int c = 0; c < a.Dh / WAVE; ++c) {
+    // (a mean of finite values is: where a rounding takes it past the type's largest, it is that)
+    float y = o[c] * inv;
+    if (fabsf(y) > most && !not_finite(o[c])) y = copysignf(most, y);
+    if (a.type == ADT_F32) Elem<float>::store((float*)a.out, at + lane + c * WAVE, y);
+    else Elem<uint16_t>::store((uint16_t*)a.out, at + lane + c * WAVE, y);
+  }
+}
+// Of a wave whose rows have `per` neighbouring lanes each: the lanes of those rows of which one says so.
+__device__ __forceinline__ uint64_t rows_lanes(bool left, int per) {
+  const uint64_t any = __ballot(left), group = (1ull << per) - 1;
+  uint64_t all = 0;
+  if (any)
+    for (int i = 0; i < WAVE; i += per) all |= any >> i & group ? group << i : 0;
+  return all;
+}
+
+// Makes the rows of sets of such lanes again; row_of(set, lane): the row.
+template <int N, class F>
+__device__ __forceinline__ void lanes_again(const uint64_t (&sets)[N], int b, int h, F row_of, int per) {
+  uint64_t any = 0;
+#pragma unroll
+  for (int y = 0; y < N; ++y) any |= sets[y];
+  if (!any) return;
+#pragma unroll 1
+  for (int y = 0; y < N; ++y) {
+    uint64_t lanes = sets[0];
+#pragma unroll
+    for (int z = 1; z < N; ++z) lanes = y == z ? sets[z] : lanes;
+#pragma unroll 1
+    for (int i = 0; i < WAVE; i += per)
+      if (lanes >> i & 1) row_again(b, h, row_of(y, i));
+  }
+}
+
 // ---------------------------------------------------------------------------- bf16 rows
 // A wave takes a tile of 32 rows through the keys, 32 of them a step:
 //   S^T[key][row] = K Q^T  (32 x 32 x 16 MFMA; lane (r, s) = (lane % 32, lane / 32) holds row r's scores of
@@ -207,7 +319,7 @@ __device__ __forceinline__ float max_of(const f32x16 (&x)[N]) {
 
 // A row's reference of the softmax: scores count as 2^(score - m).  It is the maximum of the first scores
 // that the row saw, and is raised only where a later one is larger by more than this (in log2), so
-// that outputs are hardly ever rescaled; weights then reach 2^8, which costs nothing in floating point.
+// that outputs are hardly ever rescaled; weights then reach 2^8.
 constexpr float SLACK = 8.f;
 
 // N steps at once.  k(n, f): the K operands of step n; ks, vs: LDS, the scales of this lane's keys (those of
@@ -397,9 +509,10 @@ __device__ __forceinline__ void put_out(const KvAttn& a, bool direct, int64_t to
 
 // Many rows: a unit of 64 keys, K and V, comes into LDS once for the workgroup (eight bits turned into
 // bf16 on the way), the next P on their way into registers meanwhile; a wave takes its tile through both
-// steps of a unit, or, where the job has two tiles only, through one of them.
+// steps of a unit, or, where the job has two tiles only, through one of them.  Returns which of its tile's rows (bits) a
+// wave has to make again.
 template <typename C, int DH, int TILES>
-__device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, const Job& j, const int* first, unsigned char* smem,
+__device__ __forceinline__ uint32_t attend_shared(const KvAttn& a, const KvPlan& p, const Job& j, const int* first, unsigned char* smem,
                                               float* part_o, float* part_ml) {
   constexpr int KT = 32, KS = DH / 16, OT = DH / 32, KH = KA_WAVES / TILES, N = 2 / KH, KP = K_PITCH<DH>, VP = V_PITCH<DH>;
   constexpr int EPL = 16 / (int)sizeof(C), CPL = DH / EPL;         // elements of a load, loads of a row
@@ -552,7 +665,7 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
       mo[(OT * 16 + 1) * WAVE + lane] = t.l;
     }
     __syncthreads();
-    if (kpart == 1) return;
+    if (kpart == 1) return 0;
     const float m1 = mo[OT * 16 * WAVE + lane], l1 = mo[(OT * 16 + 1) * WAVE + lane], M = fmaxf(t.m, m1);
     const float w0 = part_weight(t.m, t.l, M), w1 = part_weight(m1, l1, M);
     // (a part of weight 0 adds nothing, whatever it holds; unless its sum is NaN)
@@ -566,7 +679,17 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
     t.l = (w0 == 0.f && t.l == t.l ? 0.f : t.l * w0) + (w1 == 0.f && l1 == l1 ? 0.f : l1 * w1);
     t.m = M;
   }
-  if (!mine) return;
+  uint32_t which = 0;
+  if (j.direct) {
+    f32x4 o[4 * OT];
+#pragma unroll
+    for (int d = 0; d < OT; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[4 * d + e / 4][e % 4] = t.o[d][e];
+    const uint64_t any = __ballot(mine && left_fp32(o, t.l));
+    which = (uint32_t)(any | any >> 32);
+  }
+  if (!mine || (which >> r & 1)) return which;
   const int64_t to = row_out(a, p, j, at);
   const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
 #pragma unroll
@@ -575,15 +698,16 @@ __device__ __forceinline__ void attend_shared(const KvAttn& a, const KvPlan& p, 
     for (int c = 0; c < 4; ++c)
       put_out<DH>(a, j.direct, to, 32 * d + 8 * c + 4 * s, f32x4{t.o[d][4 * c], t.o[d][4 * c + 1], t.o[d][4 * c + 2], t.o[d][4 * c + 3]}, inv, part_o);
   if (!j.direct && s == 0) *reinterpret_cast<float2*>(part_ml + to * 2) = make_float2(t.m, t.l);
+  return which;
 }
 
 // Up to 32 rows: the waves take steps of their own, with no barrier between them.  K comes straight into the
 // operands' registers (eight bits: 16 codes a load, so that an operand's dims lie in pairs of 8, the
 // queries' alike), V through rows of LDS that are the wave's own; P steps are in flight.  The waves'
-// results meet in LDS, in their order.
+// results meet in LDS, in their order.  again: LDS, 0.  Returns which of the rows have to be made again.
 template <typename C, int DH>
-__device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, const Job& j, const int* first, unsigned char* smem,
-                                           float* part_o, float* part_ml) {
+__device__ __forceinline__ uint32_t attend_few(const KvAttn& a, const KvPlan& p, const Job& j, const int* first, unsigned char* smem,
+                                           uint32_t* again, float* part_o, float* part_ml) {
   constexpr int KT = 32, KS = DH / 16, OT = DH / 32, VP = V_PITCH<DH>;
   constexpr bool CODES = EIGHT<C>;
   constexpr int P = CODES ? 2 : 1;
@@ -723,7 +847,8 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
   mo[wave * EACH + OT * 16 * WAVE + lane] = t.m;
   mo[wave * EACH + (OT * 16 + 1) * WAVE + lane] = t.l;
   __syncthreads();
-  if (wave >= OT || !mine) return;
+  const bool writes = wave < OT && mine;
+  if (!j.direct && !writes) return 0;
   float m[KA_WAVES], l[KA_WAVES], M = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int w = 0; w < KA_WAVES; ++w) {
@@ -731,22 +856,34 @@ __device__ __forceinline__ void attend_few(const KvAttn& a, const KvPlan& p, con
     l[w] = mo[w * EACH + (OT * 16 + 1) * WAVE + lane];
     M = fmaxf(M, m[w]);
   }
-  f32x16 o;
+  f32x4 o[4];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) o[e] = 0.f;
+  for (int c = 0; c < 4; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (writes) {
 #pragma unroll
-  for (int w = 0; w < KA_WAVES; ++w) {
-    const float wt = part_weight(m[w], l[w], M);
-    if (wt == 0.f && l[w] == l[w]) continue;
-    sum += wt * l[w];
+    for (int w = 0; w < KA_WAVES; ++w) {
+      const float wt = part_weight(m[w], l[w], M);
+      if (wt == 0.f && l[w] == l[w]) continue;
+      sum += wt * l[w];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) o[e] += wt * mo[w * EACH + (wave * 16 + e) * WAVE + lane];
+      for (int e = 0; e < 16; ++e) o[e / 4][e % 4] += wt * mo[w * EACH + (wave * 16 + e) * WAVE + lane];
+    }
+  }
+  uint32_t which = 0;
+  if (j.direct) {
+    // (a row's outputs are in several waves, and out may be q: all of them leave it, or none does)
+    const uint64_t any = __ballot(writes && left_fp32(o, sum));
+    if (any && lane == 0) atomicOr(again, (uint32_t)(any | any >> 32));
+    __syncthreads();
+    which = *again;
+    if (!writes || (which >> r & 1)) return which;
   }
   const int64_t to = row_out(a, p, j, at);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) put_out<DH>(a, j.direct, to, 32 * wave + 8 * c + 4 * s, f32x4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]}, inv, part_o);
+  for (int c = 0; c < 4; ++c) put_out<DH>(a, j.direct, to, 32 * wave + 8 * c + 4 * s, o[c], inv, part_o);
   if (!j.direct && wave == 0 && s == 0) *reinterpret_cast<float2*>(part_ml + to * 2) = make_float2(M, sum);
+  return which;
 }
 
 template <typename C, int DH>
@@ -759,13 +896,22 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
                                                                float* __restrict__ part_ml) {
   static_assert(FEW_BYTES<DH> <= SHARED_BYTES<C, DH> && KA_WAVES * (32 * V_PITCH<DH> + 256) <= FEW_BYTES<DH>, "LDS");
   __shared__ __attribute__((aligned(16))) unsigned char smem[SHARED_BYTES<C, DH>];
+  __shared__ uint32_t again;
   extern __shared__ int first[];
+  if (threadIdx.x == 0) again = 0;
   Job j;
   const int tiles = (int64_t)blockIdx.x < p.pre_jobs ? p.pre.tiles : p.own.tiles;
   if (!take_job<32>(a, p, 32 * tiles, first, j)) return;
-  if (tiles == 1) attend_few<C, DH>(a, p, j, first, smem, part_o, part_ml);
-  else if (tiles == 2) attend_shared<C, DH, 2>(a, p, j, first, smem, part_o, part_ml);
-  else attend_shared<C, DH, 4>(a, p, j, first, smem, part_o, part_ml);
+  // (the shared forms' rows are those of the wave's tile)
+  uint32_t which;
+  if (tiles == 1) which = attend_few<C, DH>(a, p, j, first, smem, &again, part_o, part_ml);
+  else if (tiles == 2) which = attend_shared<C, DH, 2>(a, p, j, first, smem, part_o, part_ml);
+  else which = attend_shared<C, DH, 4>(a, p, j, first, smem, part_o, part_ml);
+  if (!which) return;
+  const int wave = threadIdx.x / WAVE, row0 = j.r0 + wave % tiles * 32;
+#pragma unroll 1
+  for (int i = tiles == 1 ? wave : 0; i < 32; i += tiles == 1 ? KA_WAVES : 1)
+    if (which >> i & 1) row_again(j.b, j.h, row0 + i);
 }
 
 // ---------------------------------------------------------------------------- fp32 rows
@@ -928,6 +1074,8 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
     fetch_v(st + stride);
   }
 
+  constexpr int SETS = DH / 64;
+  uint64_t again[RT * SETS] = {};       // lanes whose rows have to be made again
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     sm[t].l = xor32_add(xor16_add(sm[t].l));
@@ -942,9 +1090,10 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
       mml[(wave * 16 + l) * 2 + 1] = sm[t].l;
     }
     __syncthreads();
-    for (int x = tid; x < 16 * (DH / 4); x += KA_THREADS) {
+#pragma unroll
+    for (int x0 = 0; x0 < 16 * (DH / 4); x0 += KA_THREADS) {
+      const int x = x0 + tid;
       const int i = x / (DH / 4), d = x % (DH / 4) * 4, row = j.r0 + t * 16 + i;
-      if (row >= j.live) continue;
       float M = -INFINITY;
 #pragma unroll
       for (int w = 0; w < KA_WAVES; ++w) M = fmaxf(M, mml[(w * 16 + i) * 2]);
@@ -957,6 +1106,12 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
         ls += wt * lw;
         acc += wt * *reinterpret_cast<const f32x4*>(&mo[(w * 16 + i) * MP + d]);
       }
+      if (j.direct) {
+        const f32x4 outputs[1] = {acc};
+        again[t * SETS + x0 / KA_THREADS] = rows_lanes(row < j.live && left_fp32(outputs, ls), DH / 4);
+        if (again[t * SETS + x0 / KA_THREADS] >> lane & 1) continue;
+      }
+      if (row >= j.live) continue;
       const RowAt at = row_at(a, j, row, first);
       if (j.direct) {
         const float inv = ls == 0.f ? 0.f : 1.f / ls;
@@ -968,6 +1123,8 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
       }
     }
   }
+  lanes_again(again, j.b, j.h, [&](int y, int i) { return j.r0 + y / SETS * 16 + (y % SETS * KA_THREADS + wave * WAVE + i) / (DH / 4); },
+              DH / 4);
 }
 
 // ---------------------------------------------------------------------------- merge
@@ -1036,20 +1193,24 @@ __global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p
     so[tid] = o[0];
     sml[tid] = make_float2(m[0], l[0]);
     __syncthreads();
-    if (grp > 0) return;
-    const int groups = min(count, n);
+    const int groups = grp > 0 ? 0 : min(count, n);
     for (int g = 1; g < groups; ++g) m[0] = fmaxf(m[0], sml[tid + g * per].x);
     l[0] = 0.f;
     o[0] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int g = 0; g < groups; ++g) add(sml[tid + g * per].x, sml[tid + g * per].y, so[tid + g * per], m[0], l[0], o[0]);
   }
+  uint64_t again[ROWS];        // lanes whose rows have to be made again
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     const int row = row0 + r * fit;
-    if (row >= live) continue;
+    const bool writes = row < live && grp == 0;
+    const f32x4 outputs[1] = {o[r]};
+    again[r] = rows_lanes(writes && left_fp32(outputs, l[r]), per);
+    if (!writes || (again[r] >> (tid % WAVE) & 1)) continue;
     const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
     store4((T*)a.out + RowAt{b, row / a.G, row % a.G}.q(a, h) + d, o[r][0] * inv, o[r][1] * inv, o[r][2] * inv, o[r][3] * inv);
   }
+  lanes_again(again, b, h, [&](int r, int i) { return __builtin_amdgcn_readlane(row0, i) + r * fit; }, per);
 }
 
 // ---------------------------------------------------------------------------- host

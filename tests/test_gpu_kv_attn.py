@@ -7,6 +7,7 @@ of itself (numerator and sum; the exponential's and the factors' ulps in the 2^-
 enters the second product, times its value's scale, rounded: 2^-8 of itself at most; that product and
 the merges add up to 2^-24 per term; the output's own rounding is 2^-8 (bf16) or 2^-24 of it."""
 import math
+import re
 
 import numpy as np
 import pytest
@@ -367,6 +368,53 @@ def test_slots_past_32_bits(rt, kind):
         ds = (q[0, :, h].double().abs() @ k.abs().t().contiguous()).amax(1, keepdim=True) * (c.scale * (Dh + 3) * 2.0 ** -24)
         tol = (2 * ds + 2.0 ** -8 + 2.0 ** -16) * (e / total @ v.abs()) + 2.0 ** -8 * want.abs() + 1e-6
         assert torch.all((got[0, :, h].double() - want).abs() <= tol)
+
+
+def few_bits(c, which, value):
+    """Sets every value of a case's caches (which: 1, the values' tensors) to about `value`: of the dim's sign, a tenth of it less at most."""
+    g = gen(31)
+    for t in [c.t] + ([c.pt] if c.P is not None else []):
+        x, sign = t[which], torch.where(torch.rand(c.Dh, device="cuda", generator=g) < 0.5, -1.0, 1.0)
+        near = 1.0 - 0.1 * torch.rand(x.shape, device="cuda", generator=g)
+        if c.kind in TOP:
+            x.copy_((near * sign * TOP[c.kind]).to(DT[c.kind]))
+            t[which + 2].masked_fill_(torch.isfinite(t[which + 2]), value / TOP[c.kind])
+        else:
+            x.copy_(torch.where(torch.isnan(x.float()), x.float(), near * sign * value))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("H,Hkv,Dh,n,L,P", [
+    (4, 2, 64, 5, [300, 9], None),            # up to 32 rows, one split
+    (4, 2, 128, 4, [5000], None),             # several
+    (8, 2, 64, 17, [90, 7], None),            # three tiles
+    (2, 2, 128, 61, [3000], None),            # two tiles, several splits
+    (8, 2, 64, 40, [70, 0, 300, 31], [700, 0]),
+    (32, 32, 128, 61, [3, 20, 37, 54], [2500]),
+])
+def test_values_at_the_end_of_fp32(rt, kind, H, Hkv, Dh, n, L, P):
+    """Values whose weighted sums leave fp32, though no mean of them does; and values as small."""
+    print(f"large values {kind} H={H}/{Hkv} Dh={Dh} n={n} L={L} P={P}", flush=True)
+    c = Case(rt, kind, H, Hkv, Dh, n, L, P=P, seed=6, q_scale=3.0)
+    for value in (3e38, 2.0 ** 121, 1e-25):
+        few_bits(c, 1, value)
+        was = c.q.clone()
+        c.check(rt)
+        out = c.call(rt, out=c.q)
+        c.q = was
+        c.check(rt, out=out, rest=was)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_the_largest_values(rt, kind):
+    """Every value the type's largest: so is every output."""
+    print(f"largest values {kind}", flush=True)
+    most = torch.finfo(DT[kind]).max
+    for P, n in ((None, 3), ([900], 40)):
+        c = Case(rt, kind, 4, 2, 64, n, [1000, 30], P=P, q_scale=3.0)
+        for t in [c.t] + ([c.pt] if P else []):
+            t[1].copy_(torch.where(torch.isnan(t[1]), t[1], torch.full_like(t[1], most)))
+        c.check(rt)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
