@@ -375,7 +375,10 @@ adt_status adt_cache_compact(const adt_kv_cache* cache /*[host]*/, const int32_t
  *   (ADT_E_ARG where they overlap otherwise).
  * dtype ADT_BF16: cache type ADT_BF16, ADT_E4M3 or ADT_I8; ADT_F32: ADT_F32 (else ADT_E_UNSUPPORTED).
  *   bf16 multiplies codes as they are (bf16 holds them exactly) and applies the scales to scores and
- *   probabilities in fp32; softmax sums and outputs are fp32.
+ *   probabilities in fp32; softmax sums and outputs are fp32.  A row whose weighted values add up to more
+ *   than fp32 holds (values past 2^120, or past 2^128 over their number) is made again with smaller
+ *   weights, far slower, so that its mean is right; not so where a value that it sees is not finite: then
+ *   such sums are not finite either, unless out is q.
  * workspace: adt_cache_tree_attn_workspace_size() bytes (groups = 0: no prefix; 0 where none is
  *   needed, and for sizes past the limits that follow), 16-byte aligned.  Dh 64 or 128, H a multiple
  *   of heads, B * heads <= 65535, addresses and cache strides multiples of 16 bytes (ADT_E_SHAPE);

@@ -21,6 +21,7 @@
 // time on the vector instructions of the softmax and of turning codes into bf16, which overlap the
 // matrix products of another wave only in part; 17 rows over 300 slots 7.8, latency.
 #include <algorithm>
+#include <cstddef>
 
 #include "../eight_bit.h"
 #include "../launch.h"
@@ -174,7 +175,8 @@ __device__ __forceinline__ float part_weight(float m, float l, float M) {
 // Weighted values may add up to more than fp32 holds where it holds their mean: values past 2^120, or past 2^128 over
 // their number.  The output is then not finite though the sum of weights is, which every row is tested for where its
 // output is written; such a row is made again: by a wave, from all its keys, with weights of 2^-34 at most, so that
-// 2^32 of them keep the sum of the largest values below 2^126.  (Far slower, and by one code for all types.)
+// 2^32 of them keep the sum of the largest values below 2^126.  (Far slower, and by one code for all types.)  Where
+// a value that the row sees is not finite itself, its outputs stay as they are.
 
 // Whether any of N times four outputs is not finite, though the sum of weights l is.
 template <int N>
@@ -193,41 +195,127 @@ __device__ __forceinline__ float element(int type, const void* p, int64_t i) {
   const uint8_t x = ((const uint8_t*)p)[i];
   return type == ADT_E4M3 ? decode4<E4M3>(x).x : decode4<I8>(x).x;
 }
-// Row `row` (node and head of the group) of sequence b; all lanes of the wave take part.  A kernel's first argument is
-// `a`: read anew from where it lies, and the lane counted anew, they are not kept through the loops before, whose
-// registers they would take.
-__device__ __forceinline__ void row_again(int b, int h, int row) {
-  typedef const __attribute__((address_space(4))) uint32_t Word;
-  Word* args = (Word*)__builtin_amdgcn_kernarg_segment_ptr();
-  asm volatile("" : "+s"(args));
+// Whether any element in 16 bytes is not finite.
+__device__ __forceinline__ bool odd_elements(int type, u32x4 w) {
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = w[i] & 0x7fffffffu, low = w[i] & 0x7fffu, none = (w[i] & 0x7f7f7f7fu) ^ 0x7f7f7f7fu;
+    if (type == ADT_F32) odd |= x >= 0x7f800000u;
+    else if (type == ADT_BF16) odd |= x >= 0x7f800000u || low >= 0x7f80u;
+    else if (type == ADT_E4M3) odd |= ((none - 0x01010101u) & ~none & 0x80808080u) != 0;      // a byte of `none` is 0
+  }
+  return odd;
+}
+// A structure that lies in constant memory.
+typedef const __attribute__((address_space(4))) uint32_t ConstWord;
+template <typename S>
+__device__ __forceinline__ S read_words(ConstWord* from) {
   struct {
-    uint32_t w[sizeof(KvAttn) / 4];
+    uint32_t w[sizeof(S) / 4];
   } words;
 #pragma unroll
-  for (size_t i = 0; i < sizeof(KvAttn) / 4; ++i) words.w[i] = args[i];
-  const KvAttn a = __builtin_bit_cast(KvAttn, words);
-  const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), rows_type = a.type == ADT_F32 ? ADT_F32 : ADT_BF16;
+  for (size_t i = 0; i < sizeof(S) / 4; ++i) words.w[i] = from[i];
+  return __builtin_bit_cast(S, words);
+}
+// What the code of this section works with.  A kernel's first argument is `a`: read anew from where it lies, and the lane
+// counted anew, they are not kept through the loops before, whose registers they would take.
+struct Anew {
+  ConstWord* args;
+  KvAttn a;
+  int lane;
+  __device__ __forceinline__ Anew() : args((ConstWord*)__builtin_amdgcn_kernarg_segment_ptr()) {
+    asm volatile("" : "+s"(args));
+    a = read_words<KvAttn>(args);
+    lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+  }
+};
+// A part of the context of sequence b's rows: L slots that all of them see, and up to `total` a tail.
+struct Keys {
+  const void *k, *v;
+  const float *ks, *vs;
+  int L, total;
+  int64_t base, scales;
+  __device__ __forceinline__ Keys(const Anew& n, bool own, int b, int h) {
+    const KvPart p = read_words<KvPart>(n.args + (own ? offsetof(KvAttn, own) : offsetof(KvAttn, pre)) / 4);
+    const int64_t of = own ? b : b / n.a.group;
+    k = p.k, v = p.v, ks = p.ks, vs = p.vs;
+    L = max(0, min(p.len[of], p.cap));
+    total = own ? (int)min((int64_t)L + max(0, min(n.a.n_tail[b], ADT_MAX_NODES)), (int64_t)p.cap) : L;
+    base = of * p.sb + h * p.sh;
+    scales = of * p.ssb + h * p.ssh;
+  }
+};
+// Whether a lane's values of the slots [from, to) are finite, for those that sees(slot) says; the whole wave's lanes take
+// all of them, until one is not.
+template <class F>
+__device__ __forceinline__ bool odd_values(const Anew& n, const Keys& k, int from, int to, F sees) {
+  const int type = n.a.type, bytes = type == ADT_F32 ? 4 : type == ADT_BF16 ? 2 : 1, row_log2 = __builtin_ctz(n.a.Dh * bytes);
+  const char* v = (const char*)k.v + k.base * bytes;
+  const int64_t end = type == ADT_I8 ? 0 : (int64_t)to << row_log2;
+  constexpr int AT_ONCE = 4;
+  bool odd = false;
+#pragma unroll 1
+  for (int64_t at0 = (int64_t)from << row_log2; at0 < end; at0 += AT_ONCE * WAVE * 16) {
+    u32x4 w[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) w[i] = *reinterpret_cast<const u32x4*>(v + min(at0 + (i * WAVE + n.lane) * 16, end - 16));
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int64_t at = at0 + (i * WAVE + n.lane) * 16;
+      odd |= at < end && odd_elements(type, w[i]) && sees(at >> row_log2);
+    }
+    if (__any(odd)) return true;
+  }
+  if (k.vs) {
+#pragma unroll 4
+    for (int64_t key = from + n.lane; key < to; key += WAVE) odd |= not_finite(k.vs[k.scales + key]) && sees(key);
+  }
+  return __any(odd);
+}
+// Whether a value that all rows of sequence b see is not finite: its rows are then left as they are.  Where outputs are
+// written over the queries they are not there yet: false.
+__device__ __forceinline__ bool odd_for_all(int b, int h) {
+  const Anew n;
+  if (n.a.out == n.a.q) return false;
+#pragma unroll 1
+  for (int own = n.a.groups ? 0 : 1; own < 2; ++own) {
+    const Keys k(n, own, b, h);
+    if (odd_values(n, k, 0, k.L, [](int64_t) { return true; })) return true;
+  }
+  return false;
+}
+// Row `row` (node and head of the group) of sequence b; all lanes of the wave take part.  Its outputs are written before,
+// unless they are its queries.
+__device__ __forceinline__ void row_again(int b, int h, int row) {
+  const Anew n;
+  const KvAttn& a = n.a;
+  const int lane = n.lane, rows_type = a.type == ADT_F32 ? ADT_F32 : ADT_BF16;
   const int64_t at = RowAt{b, row / a.G, row % a.G}.q(a, h);
   const uint64_t* mask = a.mask + ((int64_t)b * a.nq_max + row / a.G) * ADT_MASK_WORDS;
+  auto sees = [&](const Keys& k, int64_t key) {
+    const int64_t t = key - k.L;
+    return key < k.total && (t < 0 || (mask[t / 64] >> (t % 64) & 1));
+  };
+  if (a.out != a.q) {
+    const Keys k(n, true, b, h);
+    if (odd_values(n, k, k.L, k.total, [&](int64_t key) { return sees(k, key); })) return;
+  }
   float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};            // of dims lane and lane + 64
 #pragma unroll 1
   for (int own = a.groups ? 0 : 1; own < 2; ++own) {
-    const KvPart& p = own ? a.own : a.pre;
-    const int64_t of = own ? b : b / a.group;
-    const int L = max(0, min(p.len[of], p.cap));
-    const int total = own ? (int)min((int64_t)L + max(0, min(a.n_tail[b], ADT_MAX_NODES)), (int64_t)p.cap) : L;
-    const int64_t base = of * p.sb + h * p.sh, scales = of * p.ssb + h * p.ssh;
+    const Keys p(n, own, b, h);
 #pragma unroll 1
-    for (int64_t key0 = 0; key0 < total; key0 += WAVE) {
-      const int64_t key = key0 + lane, n = key - L;
-      const bool seen = key < total && (n < 0 || (mask[n / 64] >> (n % 64) & 1));
+    for (int64_t key0 = 0; key0 < p.total; key0 += WAVE) {
+      const int64_t key = key0 + lane;
+      const bool seen = sees(p, key);
       float x = -INFINITY, by = 1.f;
       if (seen) {
         x = 0.f;
 #pragma unroll 1
-        for (int d = 0; d < a.Dh; ++d) x = fmaf(element(rows_type, a.q, at + d), element(a.type, p.k, base + key * a.Dh + d), x);
+        for (int d = 0; d < a.Dh; ++d) x = fmaf(element(rows_type, a.q, at + d), element(a.type, p.k, p.base + key * a.Dh + d), x);
         x *= a.scale * LOG2E;
-        if (p.ks) x *= p.ks[scales + key], by = p.vs[scales + key];
+        if (p.ks) x *= p.ks[p.scales + key], by = p.vs[p.scales + key];
       }
       const float top = fmaxf(m, wave_max(x)), ref = top == -INFINITY ? 0.f : top, down = top == m ? 1.f : exp2_hw(m - ref);
       const float w = seen ? exp2_hw(x - ref) * 0x1p-34f : 0.f;
@@ -239,7 +327,7 @@ __device__ __forceinline__ void row_again(int b, int h, int row) {
       for (int k = 0; k < WAVE; ++k) {
         if (!__builtin_amdgcn_readlane(seen, k)) continue;
         const float wk = __shfl(w * by, k, WAVE);
-        const int64_t v = base + (key0 + k) * a.Dh + lane;
+        const int64_t v = p.base + (key0 + k) * a.Dh + lane;
         o[0] += wk * element(a.type, p.v, v);
         if (a.Dh > WAVE) o[1] += wk * element(a.type, p.v, v + WAVE);
       }
@@ -271,6 +359,8 @@ __device__ __forceinline__ void lanes_again(const uint64_t (&sets)[N], int b, in
 #pragma unroll
   for (int y = 0; y < N; ++y) any |= sets[y];
   if (!any) return;
+  __threadfence_block();
+  if (odd_for_all(b, h)) return;
 #pragma unroll 1
   for (int y = 0; y < N; ++y) {
     uint64_t lanes = sets[0];
@@ -689,7 +779,7 @@ __device__ __forceinline__ uint32_t attend_shared(const KvAttn& a, const KvPlan&
     const uint64_t any = __ballot(mine && left_fp32(o, t.l));
     which = (uint32_t)(any | any >> 32);
   }
-  if (!mine || (which >> r & 1)) return which;
+  if (!mine || (a.out == a.q && (which >> r & 1))) return which;
   const int64_t to = row_out(a, p, j, at);
   const float inv = t.l == 0.f ? 0.f : 1.f / t.l;
 #pragma unroll
@@ -871,12 +961,12 @@ __device__ __forceinline__ uint32_t attend_few(const KvAttn& a, const KvPlan& p,
   }
   uint32_t which = 0;
   if (j.direct) {
-    // (a row's outputs are in several waves, and out may be q: all of them leave it, or none does)
+    // (a row's outputs are in several waves: where out is q all of them leave it, or none does)
     const uint64_t any = __ballot(writes && left_fp32(o, sum));
     if (any && lane == 0) atomicOr(again, (uint32_t)(any | any >> 32));
     __syncthreads();
     which = *again;
-    if (!writes || (which >> r & 1)) return which;
+    if (!writes || (a.out == a.q && (which >> r & 1))) return which;
   }
   const int64_t to = row_out(a, p, j, at);
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -908,6 +998,10 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
   else if (tiles == 2) which = attend_shared<C, DH, 2>(a, p, j, first, smem, part_o, part_ml);
   else which = attend_shared<C, DH, 4>(a, p, j, first, smem, part_o, part_ml);
   if (!which) return;
+  // (the rows are written anew after their outputs are; few rows' by another wave: the bits are the workgroup's)
+  if (tiles == 1) __syncthreads();
+  else __threadfence_block();
+  if (odd_for_all(j.b, j.h)) return;
   const int wave = threadIdx.x / WAVE, row0 = j.r0 + wave % tiles * 32;
 #pragma unroll 1
   for (int i = tiles == 1 ? wave : 0; i < 32; i += tiles == 1 ? KA_WAVES : 1)
@@ -1109,7 +1203,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
       if (j.direct) {
         const f32x4 outputs[1] = {acc};
         again[t * SETS + x0 / KA_THREADS] = rows_lanes(row < j.live && left_fp32(outputs, ls), DH / 4);
-        if (again[t * SETS + x0 / KA_THREADS] >> lane & 1) continue;
+        if (a.out == a.q && (again[t * SETS + x0 / KA_THREADS] >> lane & 1)) continue;
       }
       if (row >= j.live) continue;
       const RowAt at = row_at(a, j, row, first);
@@ -1206,7 +1300,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p
     const bool writes = row < live && grp == 0;
     const f32x4 outputs[1] = {o[r]};
     again[r] = rows_lanes(writes && left_fp32(outputs, l[r]), per);
-    if (!writes || (again[r] >> (tid % WAVE) & 1)) continue;
+    if (!writes || (a.out == a.q && (again[r] >> (tid % WAVE) & 1))) continue;
     const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
     store4((T*)a.out + RowAt{b, row / a.G, row % a.G}.q(a, h) + d, o[r][0] * inv, o[r][1] * inv, o[r][2] * inv, o[r][3] * inv);
   }

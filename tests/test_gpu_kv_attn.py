@@ -417,6 +417,35 @@ def test_the_largest_values(rt, kind):
         c.check(rt)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,L,P", [(5, [300], None), (40, [70, 33], None), (61, [3000], None), (33, [20, 90], [800])])
+def test_not_finite_among_the_largest_values(rt, kind, n, L, P):
+    """A tail slot that is not finite, where the sums of the others' values leave fp32: rows that do not see it are the
+    formula's, in those that do what it reaches is not finite; in place too."""
+    print(f"odd among large {kind} n={n} L={L} P={P}", flush=True)
+    c = Case(rt, kind, 4, 2, 64, n, L, P=P, seed=8, q_scale=2.0)
+    few_bits(c, 1, 3e38)
+    slots = [c.rows[b] // 2 for b in range(c.B)]
+    for b, slot in enumerate(slots):
+        if kind in TOP:
+            c.t[3][b, :, L[b] + slot] = math.nan
+        else:
+            c.t[1][b, :, L[b] + slot, 7] = math.nan
+    was = c.q.clone()
+    for out in (torch.full_like(c.q, 7.0), c.q):
+        c.call(rt, out=out)
+        out, c.q = out.clone(), was
+        for b, slot in enumerate(slots):
+            see = c.tail_see(b)[:, slot]
+            for h in range(2):
+                want, tol = c.reference(b, h)
+                got = out[b, : c.rows[b], 2 * h: 2 * h + 2].double()
+                assert see.any() and not torch.isfinite(want[see]).all()
+                assert torch.all(((got - want).abs() <= tol)[~see])
+                odd = ~torch.isfinite(want)
+                assert not torch.isfinite(got[odd]).any()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
 def test_streams_and_graphs(rt, kind):
     """Another stream, two captured graphs that share a workspace, replayed between eager calls, each
