@@ -166,7 +166,8 @@ struct Softmax {
     return alpha;
   }
 };
-// What a part (m, l) weighs beside a maximum M of all parts; one that saw nothing weighs 0.
+// What a part (m, l) weighs beside a maximum M of all parts; one that saw nothing weighs 0.  Parts add up whatever they
+// weigh: outputs that are not finite make the sum so even times 0, as they would among the keys of one part.
 __device__ __forceinline__ float part_weight(float m, float l, float M) {
   return m == -INFINITY && l == 0.f ? 0.f : exp2_hw(m - (M == -INFINITY ? 0.f : M));
 }
@@ -586,6 +587,11 @@ __device__ __forceinline__ void add_odd_values(RowTile<DH>& t, const KeySource<C
   }
 }
 
+// a times u and b times v, rounded each: the two parts of a row alike.
+__device__ __forceinline__ float both(float a, float u, float b, float v) {
+#pragma clang fp contract(off)
+  return a * u + b * v;
+}
 // Where a row's result goes: the output, or a partial result.
 __device__ __forceinline__ int64_t row_out(const KvAttn& a, const KvPlan& p, const Job& j, const RowAt& at) {
   return j.direct ? at.q(a, j.h) : at.part(a, p, j.h, j.pre ? p.own.splits + j.sp : j.sp);
@@ -758,15 +764,14 @@ __device__ __forceinline__ uint32_t attend_shared(const KvAttn& a, const KvPlan&
     if (kpart == 1) return 0;
     const float m1 = mo[OT * 16 * WAVE + lane], l1 = mo[(OT * 16 + 1) * WAVE + lane], M = fmaxf(t.m, m1);
     const float w0 = part_weight(t.m, t.l, M), w1 = part_weight(m1, l1, M);
-    // (a part of weight 0 adds nothing, whatever it holds; unless its sum is NaN)
 #pragma unroll
     for (int d = 0; d < OT; ++d)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float y = mo[(d * 16 + e) * WAVE + lane];
-        t.o[d][e] = (w0 == 0.f ? 0.f : t.o[d][e] * w0) + (w1 == 0.f ? 0.f : y * w1);
+        t.o[d][e] = both(t.o[d][e], w0, y, w1);
       }
-    t.l = (w0 == 0.f && t.l == t.l ? 0.f : t.l * w0) + (w1 == 0.f && l1 == l1 ? 0.f : l1 * w1);
+    t.l = both(t.l, w0, l1, w1);
     t.m = M;
   }
   uint32_t which = 0;
@@ -953,7 +958,6 @@ __device__ __forceinline__ uint32_t attend_few(const KvAttn& a, const KvPlan& p,
 #pragma unroll
     for (int w = 0; w < KA_WAVES; ++w) {
       const float wt = part_weight(m[w], l[w], M);
-      if (wt == 0.f && l[w] == l[w]) continue;
       sum += wt * l[w];
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[e / 4][e % 4] += wt * mo[w * EACH + (wave * 16 + e) * WAVE + lane];
@@ -1196,7 +1200,6 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
 #pragma unroll
       for (int w = 0; w < KA_WAVES; ++w) {
         const float mw = mml[(w * 16 + i) * 2], lw = mml[(w * 16 + i) * 2 + 1], wt = part_weight(mw, lw, M);
-        if (wt == 0.f && lw == lw) continue;
         ls += wt * lw;
         acc += wt * *reinterpret_cast<const f32x4*>(&mo[(w * 16 + i) * MP + d]);
       }
@@ -1251,9 +1254,9 @@ __global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p
   }
   auto add = [](float pm, float pl, const f32x4& po, float m, float& l, f32x4& o) {       // at the maximum m
     const float wt = part_weight(pm, pl, m);
-    if (wt == 0.f && pl == pl) return;
-    l += wt * pl;
-    o += wt * po;
+    l = fmaf(wt, pl, l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(wt, po[e], o[e]);
   };
   for (int s0 = row0 < live ? grp : n; s0 < n; s0 += AT_ONCE * step) {
     float2 ml[ROWS][AT_ONCE];

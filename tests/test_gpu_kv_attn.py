@@ -446,6 +446,46 @@ def test_not_finite_among_the_largest_values(rt, kind, n, L, P):
                 assert not torch.isfinite(got[odd]).any()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,L,P,at", [
+    (2, [200], None, 3),              # one split, waves that meet
+    (2, [6000], None, 3),             # several
+    (40, [100], None, 3),             # two tiles
+    (40, [6000], None, 70),
+    (2, [50], [200], -3),             # in the prefix
+    (70, [50], [3000], -3),
+])
+def test_not_finite_without_weight(rt, kind, n, L, P, at):
+    """A seen slot whose value (scale) is not finite makes the row's output not finite, however little the slot weighs: the
+    last slot before the tail, whose key is the queries', weighs 2^300 times as much."""
+    print(f"weightless {kind} n={n} L={L} P={P}", flush=True)
+    c = Case(rt, kind, 2, 2, 64, n, L, P=P, seed=7)
+    c.q.copy_(c.q[:, :1].expand_as(c.q).clone())
+    for h in range(2):
+        key = c.q[0, 0, h].float() * 45
+        if kind in TOP:
+            s = key.abs().max() / TOP[kind]
+            t = (key / s).clamp(-TOP[kind], TOP[kind])
+            c.t[0][0, h, L[0] - 1] = (t.round() if kind == "int8" else t).to(DT[kind])
+            c.t[2][0, h, L[0] - 1] = s
+        else:
+            c.t[0][0, h, L[0] - 1] = key.to(DT[kind])
+    t, slot = (c.t, at) if at >= 0 else (c.pt, -at)
+    if kind in TOP:
+        t[3][0, 0, slot] = math.nan
+    else:
+        t[1][0, 0, slot, 9] = math.inf
+        t[1][0, 0, slot, 33] = math.nan
+    out = c.call(rt, out=torch.full_like(c.q, 7.0))
+    for h in range(2):
+        want, tol = c.reference(0, h)
+        got = out[0, : c.rows[0], h: h + 1].double()
+        odd = ~torch.isfinite(want)
+        assert odd.any() == (h == 0) and torch.equal(~torch.isfinite(got), odd)
+        assert torch.equal(torch.isnan(got)[torch.isnan(want)], torch.isnan(want)[torch.isnan(want)])
+        assert torch.all(((got - want).abs() <= tol)[~odd])
+
+
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
 def test_streams_and_graphs(rt, kind):
     """Another stream, two captured graphs that share a workspace, replayed between eager calls, each
