@@ -380,7 +380,8 @@ adt_status adt_cache_compact(const adt_kv_cache* cache /*[host]*/, const int32_t
  *   weights, far slower, so that its mean is right; not so where a value that it sees is not finite: then
  *   such sums are not finite either, unless out is q.
  * workspace: adt_cache_tree_attn_workspace_size() bytes (groups = 0: no prefix; 0 where none is
- *   needed, and for sizes past the limits that follow), 16-byte aligned.  Dh 64 or 128, H a multiple
+ *   needed, and for sizes past the limits that follow), 16-byte aligned.  The size for some kv_cap and
+ *   prefix_cap holds for smaller ones too, and without the prefix.  Dh 64 or 128, H a multiple
  *   of heads, B * heads <= 65535, addresses and cache strides multiples of 16 bytes (ADT_E_SHAPE);
  *   nq_max <= ADT_MAX_NODES, nq_max * H / heads <= 8192, workspace (ADT_E_CAPACITY).  A call whose rows
  *   and splits come to 2^24 workgroups or more is refused as well (ADT_E_CAPACITY). */

@@ -210,7 +210,7 @@ extern "C" adt_status adt_cache_tree_attn(const void* q, const adt_kv_cache* cac
   a.mask = anc_mask;
   a.scale = scale;
   a.out = out;
-  const size_t need = kv_attn_ws_bytes(a);
+  const size_t need = kv_attn_ws_need(a);
   ADT_CHECK_ARG(need == 0 || (workspace && workspace_bytes >= need), ADT_E_CAPACITY,
                 "cache_tree_attn: workspace %zu < %zu bytes", workspace_bytes, need);
   // (a workgroup has read its rows' queries before any row is written, so the queries themselves will do)

@@ -1321,7 +1321,9 @@ __global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p
 // waves take their steps one after the other from memory, at least two: one row over 300 slots 11.7 + 4.0
 // with two, 14.4 + 3.9 with three, 19.2 with eight; over 2000 11.8 + 4.0, 14.5 + 3.9, 26.4 + 4.0; over 8000 24.8 +
 // 5.2, 25.0 + 5.0, 28.7 + 4.6; a 61-row tree over 2300 45.7 + 4.8, 45.7 + 4.7, 55.5 + 4.8.
-static KvPlan kv_plan(const KvAttn& a) {
+// most: the parts that the plans of these bounds and of any smaller ones have at most.  A share is LEAST units or more, and
+// one pair's keys of SLOTS shares a SLOTS-th of its side's or more, so a side has at most as many splits as either makes.
+static KvPlan kv_plan(const KvAttn& a, int* most = nullptr) {
   KvPlan p{};
   const bool f32 = a.type == ADT_F32;
   auto side = [&](KvSide& s, int64_t rows) {
@@ -1344,7 +1346,11 @@ static KvPlan kv_plan(const KvAttn& a) {
     int64_t n = units <= per + per / 4 ? 1 : (units + per - 1) / per;
     n = std::min<int64_t>(n, std::max<int64_t>(1, 2 * SLOTS / std::max<int64_t>(1, pairs)));
     s.splits = (int)std::min<int64_t>(n, 64);
+    int64_t top = units <= LEAST + LEAST / 4 ? 1 : (units + LEAST - 1) / LEAST;
+    top = std::min(top, std::max<int64_t>(1, (SLOTS + pairs - 1) / std::max<int64_t>(1, pairs)));
+    if (most) *most += (int)std::min<int64_t>(top, 64);
   };
+  if (most) *most = 0;
   split(p.own, own_pairs, own_units);
   if (a.groups) split(p.pre, pre_pairs, pre_units);
   p.pre_jobs = pre_pairs * p.pre.splits;
@@ -1352,17 +1358,20 @@ static KvPlan kv_plan(const KvAttn& a) {
   p.parts = p.own.splits + p.pre.splits;
   return p;
 }
-static size_t part_rows(const KvAttn& a, const KvPlan& p) {
-  return p.parts == 1 ? 0 : (size_t)a.B * a.Hkv * p.parts * a.nq_max * a.G;
-}
+static size_t part_rows(const KvAttn& a, int parts) { return parts == 1 ? 0 : (size_t)a.B * a.Hkv * parts * a.nq_max * a.G; }
 
-size_t kv_attn_ws_bytes(const KvAttn& a) { return part_rows(a, kv_plan(a)) * (a.Dh + 2) * sizeof(float); }
+size_t kv_attn_ws_bytes(const KvAttn& a) {
+  int most;
+  kv_plan(a, &most);
+  return part_rows(a, most) * (a.Dh + 2) * sizeof(float);
+}
+size_t kv_attn_ws_need(const KvAttn& a) { return part_rows(a, kv_plan(a).parts) * (a.Dh + 2) * sizeof(float); }
 
 adt_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t st) {
   const KvPlan p = kv_plan(a);
   // (a launch has fewer than 2^32 threads in a dimension)
   ADT_CHECK_ARG(p.jobs < (int64_t)1 << 24, ADT_E_CAPACITY, "cache_tree_attn: %lld workgroups", (long long)p.jobs);
-  float *part_o = (float*)ws, *part_ml = part_o + part_rows(a, p) * a.Dh;
+  float *part_o = (float*)ws, *part_ml = part_o + part_rows(a, p.parts) * a.Dh;
   const size_t lds = a.groups ? (size_t)(a.group + 1) * sizeof(int) : 0;
   const unsigned jobs = (unsigned)p.jobs;
 #define ADT_KA(CV)                                                                               \

@@ -406,7 +406,8 @@ struct KvAttn {
   float scale;
   void* out;
 };
-size_t kv_attn_ws_bytes(const KvAttn& a);
+size_t kv_attn_ws_bytes(const KvAttn& a);     // for these bounds (own.cap, pre.cap) and any smaller ones
+size_t kv_attn_ws_need(const KvAttn& a);      // what one launch uses
 adt_status launch_kv_attn(const KvAttn& a, void* ws, hipStream_t st);
 
 }  // namespace adt

@@ -488,7 +488,8 @@ def cache_compact(cache: KVCache, kv_len: torch.Tensor, path: torch.Tensor, n_ac
 
 def cache_tree_attn_workspace(H: int, nq_max: int, cache: KVCache, kv_cap: Optional[int] = None,
                               prefix: Optional[KVCache] = None, prefix_cap: Optional[int] = None) -> torch.Tensor:
-    """A workspace for cache_tree_attn calls of these sizes (bounds default to the caches' slots)."""
+    """A workspace for cache_tree_attn calls of these sizes (bounds default to the caches' slots), of smaller bounds, and
+    without the prefix."""
     groups, pcap = (0, 0) if prefix is None else (prefix.B, prefix.slots if prefix_cap is None else prefix_cap)
     n = lib().adt_cache_tree_attn_workspace_size(cache.B, H, cache.heads, cache.Dh, nq_max,
                                                  cache.slots if kv_cap is None else kv_cap, groups, pcap,

@@ -486,6 +486,22 @@ def test_not_finite_without_weight(rt, kind, n, L, P, at):
         assert torch.all(((got - want).abs() <= tol)[~odd])
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_workspace_for_smaller_bounds(rt, kind):
+    """A workspace for the largest bounds serves every smaller one, and a call without the prefix."""
+    print(f"bounds {kind}", flush=True)
+    for c in (Case(rt, kind, 32, 8, 128, 1, [40], cap=20000), Case(rt, kind, 8, 8, 64, 61, [40, 7, 0, 33], cap=2400, P=[60], pcap=2112),
+              Case(rt, kind, 32, 8, 64, 1, [3, 40, 7, 0], cap=576, P=[60], pcap=20000)):
+        ws = rt.cache_tree_attn_workspace(c.H, c.n, c.cache, prefix=c.prefix)
+        pcaps = [None] if c.P is None else [c.prefix.slots, c.prefix.slots // 3, 700, 128, 60]
+        for cap in (c.cap, c.cap * 5 // 8, c.cap // 5, 128, 101):
+            for pcap in pcaps:
+                c.check(rt, kv_cap=cap, prefix_cap=pcap, workspace=ws)
+        if c.P is not None:
+            P, c.P, c.prefix = c.P, None, None
+            c.check(rt, workspace=ws)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
 def test_streams_and_graphs(rt, kind):
     """Another stream, two captured graphs that share a workspace, replayed between eager calls, each

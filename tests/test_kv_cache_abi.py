@@ -194,6 +194,23 @@ def test_cache_tree_attn_workspace_sizes(L):
     assert 2 * 4096 * 15 * 8192 * 66 * 4 <= size(4096, 3840, 15, 64, 32, 0x7f000000, 1, 0x7f000000, 0) < 1 << 50
 
 
+@pytest.mark.parametrize("B,H,heads,Dh,nq,kv_cap,groups,prefix_cap", [
+    (1, 32, 8, 128, 1, 65536, 0, 0), (16, 32, 32, 128, 61, 2560, 1, 2112), (64, 32, 8, 128, 1, 576, 1, 32768),
+    (4, 4, 4, 64, 17, 192, 2, 256), (2, 8, 1, 64, 40, 5000, 1, 300), (3, 6, 2, 128, 8, 30000, 3, 30000), (1, 1, 1, 64, 1, 0x7f000000, 1, 0x7f000000),
+])
+def test_cache_tree_attn_workspace_holds_for_smaller_bounds(L, B, H, heads, Dh, nq, kv_cap, groups, prefix_cap):
+    """What is enough for some bounds is enough for every pair of smaller ones, and without the prefix."""
+    size = L.adt_cache_tree_attn_workspace_size
+    for kind in (0, 1, 2, 3):
+        steps = lambda top: sorted({max(1, top * i // 40) for i in range(1, 41)} | {max(1, int(top / 1.3 ** i)) for i in range(60)})  # noqa: E731
+        caps, pcaps = steps(kv_cap), steps(prefix_cap) if groups else [0]
+        sizes = [[size(B, H, heads, Dh, nq, c, groups, p, kind) for p in pcaps] for c in caps]
+        for i in range(len(caps)):
+            for j in range(len(pcaps)):
+                assert (i == 0 or sizes[i][j] >= sizes[i - 1][j]) and (j == 0 or sizes[i][j] >= sizes[i][j - 1]), (kind, caps[i], pcaps[j])
+            assert not groups or sizes[i][0] >= size(B, H, heads, Dh, nq, caps[i], 0, 0, kind)
+
+
 def test_python_cache_refusals():
     import torch
     from paper_2512_21857_amd import runtime as rt
