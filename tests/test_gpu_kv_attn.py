@@ -370,6 +370,70 @@ def test_slots_past_32_bits(rt, kind):
         assert torch.all((got[0, :, h].double() - want).abs() <= tol)
 
 
+def planned_parts(rt, c, **kw):
+    """How many partial results a row may have in a call: what it asks for when it gets too little workspace."""
+    try:
+        c.call(rt, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"), **kw)
+    except rt.abi.AdtError as e:
+        need = int(re.search(r"< (\d+) bytes", str(e)).group(1))
+        return need // (c.B * c.H * c.n * (c.Dh + 2) * 4)
+    return 1
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("H,Hkv,Dh,n,L,P,least", [
+    (2, 2, 128, 61, [3000], None, 4),             # two tiles of 32 rows, units dealt out to several workgroups
+    (2, 2, 128, 61, [2975, 40], None, 4),         # ends within a unit's first half; a sequence of one split
+    (2, 1, 64, 17, [2113], None, 3),              # two tiles that two rows short of one share
+    (8, 1, 64, 40, [5000, 33], None, 4),          # four tiles, three blocks of rows
+    (4, 1, 128, 128, [4031], None, 4),            # a tail of four steps at the end of a split
+    (4, 2, 64, 20, [70, 9, 300], [4000], 4),      # 120 rows behind a prefix of several splits, own slots of one
+    (2, 1, 128, 61, [700, 5000], [4033, 90], 6),  # several splits of either part
+])
+def test_many_rows_of_several_splits(rt, kind, H, Hkv, Dh, n, L, P, least):
+    """The keys of more than 32 rows dealt out to several workgroups, with tail slots that are not finite."""
+    print(f"splits {kind} H={H}/{Hkv} Dh={Dh} n={n} L={L} P={P}", flush=True)
+    c = Case(rt, kind, H, Hkv, Dh, n, L, P=P, seed=5)
+    assert planned_parts(rt, c) >= least
+    c.check(rt)
+    for b in range(len(L)):
+        at = c.L[b] + c.tails[b] - 1
+        if kind in TOP:
+            c.t[3][b, 0, at] = math.nan
+            c.t[2][b, 0, at - 1] = math.nan
+        else:
+            c.t[1][b, 0, at, 5] = math.inf
+            c.t[0][b, 0, at - 1, 7] = math.nan
+    c.check(rt)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("Dh", [64, 128])
+def test_many_rows_of_several_parts(rt, kind, Dh):
+    """More than 2^18 groups of four outputs that meet several rows to a thread, two parts a round: four, three and one
+    of them in the groups' rows."""
+    if kind == "f32":
+        # (whose workgroups take 32 rows: so many of 64 dims never split)
+        B, n, P = 8 * 128 // Dh, 32, [2500, 1200]
+        c = Case(rt, kind, 32, 32, Dh, n, [3 + 7 * b for b in range(B)], rows=[32 - b % 5 * 7 for b in range(B)], P=P)
+    else:
+        B, n, P = 9, 61, [2500, 1800, 0]
+        c = Case(rt, kind, 32, 32, Dh, n, [3 + 17 * b for b in range(B)], rows=[61, 60, 1, 0, 33, 32, 31, 17, 61], P=P)
+    print(f"many parts {kind} Dh={Dh}", flush=True)
+    assert B * 32 * n * Dh // 4 >= 1 << 18 and planned_parts(rt, c) >= (4 if kind != "f32" else 3 if Dh == 128 else 2)
+    c.check(rt)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("Dh", [64, 128])
+def test_few_rows_of_many_parts(rt, kind, Dh):
+    """More than eight parts of few rows, which groups of threads deal out, at either size of a head."""
+    c = Case(rt, kind, 2, 1, Dh, 4, [6000, 3000], rows=[4, 3])
+    print(f"few rows, many parts {kind} Dh={Dh}", flush=True)
+    assert planned_parts(rt, c) > 8
+    c.check(rt)
+
+
 def few_bits(c, which, value):
     """Sets every value of a case's caches (which: 1, the values' tensors) to about `value`: of the dim's sign, a tenth of it less at most."""
     g = gen(31)
