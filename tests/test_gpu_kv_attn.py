@@ -566,6 +566,62 @@ def test_a_workspace_for_smaller_bounds(rt, kind):
             c.check(rt, workspace=ws)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_the_largest_group_of_large_heads(rt, kind):
+    """4096 sequences behind one prefix, heads of 128: rows of one block from many of them, none in some."""
+    B = 4096
+    c = Case(rt, kind, 1, 1, 128, 2, [b % 3 for b in range(B)], rows=[b % 7 % 3 for b in range(B)], tails=[2] * B, P=[70])
+    print(f"largest group, 128 {kind}", flush=True)
+    out = torch.full_like(c.q, 7.0)
+    c.call(rt, out=out)
+    few, c.B = c.B, c.B
+    for b in list(range(0, 40)) + list(range(2040, 2060)) + list(range(few - 20, few)):
+        want, tol = c.reference(b, 0)
+        assert torch.all((out[b, : c.rows[b]].double() - want).abs() <= tol)
+        assert torch.all(out[b, c.rows[b]:] == 7.0)
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
+def test_offsets_past_32_bits(rt, kind):
+    """Slots of one head whose elements lie past 2^31, and sequences and groups whose elements lie past 2^32."""
+    print(f"far offsets {kind}", flush=True)
+    cap, Dh, B = 17_200_000, 128, 2                    # 2.2e9 codes a head, 4.4e9 in all
+    c = Case(rt, kind, 2, 1, Dh, 2, [40, 33], rows=[2, 2], tails=[2, 2], P=[50, 41])
+    far = cap - 60
+    big = [[torch.zeros(B, 1, cap, Dh, dtype=torch.int8, device="cuda").view(DT[kind]) for _ in range(2)] +
+           [torch.zeros(B, 1, cap, device="cuda") for _ in range(2)] for _ in range(2)]
+    for x, t, n in ((big[0], c.t, [42, 35]), (big[1], c.pt, [50, 41])):
+        for b in range(B):
+            for i in range(4):
+                y, z = (u.view(torch.int8) if u.element_size() == 1 else u for u in (x[i], t[i]))
+                y[b, :, far: far + n[b]] = z[b, :, : n[b]]
+    own, pre = (rt.KVCache(*x) for x in big)
+    q = 40.0 * c.q
+    for behind in (True, False):
+        got = rt.cache_tree_attn(q, own, i32([far + l for l in c.L]), i32(c.rows), i32(c.tails), c.mask, prefix=pre if behind else None,
+                                 prefix_len=i32([far + p for p in c.P]) if behind else None)
+        # in 64 bits: the far slots, and the others of score and value 0
+        for b in range(B):
+            T = c.L[b] + 2
+            k, v = (values(x, s, b, 0, slice(0, T)) for x, s in ((c.t[0], c.t[2]), (c.t[1], c.t[3])))
+            see = torch.cat([torch.ones(2, c.L[b], dtype=torch.bool, device="cuda"), c.tail_see(b)], 1)
+            if behind:
+                pk, pv = (values(x, s, b, 0, slice(0, c.P[b])) for x, s in ((c.pt[0], c.pt[2]), (c.pt[1], c.pt[3])))
+                k, v = torch.cat([pk, k]), torch.cat([pv, v])
+                see = torch.cat([torch.ones(2, c.P[b], dtype=torch.bool, device="cuda"), see], 1)
+            see = see.repeat_interleave(2, 0)
+            rows = q[b].double().reshape(4, Dh)
+            x = (rows @ k.t().contiguous() * c.scale).masked_fill(~see, -math.inf)
+            top = x.amax(1, keepdim=True).clamp(min=0)
+            e = torch.exp(x - top)
+            total = e.sum(1, keepdim=True) + (2 if behind else 1) * far * torch.exp(-top)
+            want = e @ v / total
+            # scores up to 40 times a usual one: 2 ds of them; the weights of the others, one by one in fp32
+            ds = (rows.abs() @ k.abs().t().contiguous()).amax(1, keepdim=True) * (c.scale * (Dh + 3) * 2.0 ** -24)
+            tol = (2 * ds + 2.0 ** -8 + 2.0 ** -16) * (e / total @ v.abs()) + 2.0 ** -8 * want.abs() + 1e-6
+            assert torch.all((got[b].double().reshape(4, Dh) - want).abs() <= tol)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "int8"])
 def test_streams_and_graphs(rt, kind):
     """Another stream, two captured graphs that share a workspace, replayed between eager calls, each
