@@ -405,6 +405,14 @@ def test_compact(rt, kind, B, slices, Dh, cap, n, a_max):
                 assert torch.equal(bits(x[b])[:, L[b] + 1: L[b] + 1 + a], bits(y[b])[:, src])
 
 
+@pytest.mark.parametrize("kind,Dh,n,a_max", [("f32", 128, 128, 127), ("f32", 128, 100, 65), ("f32", 256, 128, 127), ("f32", 256, 60, 33),
+                                             ("bf16", 256, 128, 127), ("bf16", 256, 128, 65)])
+def test_compact_long_paths(rt, kind, Dh, n, a_max):
+    """Paths of so many 16-byte pieces that a thread moves up to 32 of them."""
+    assert a_max * Dh * DT[kind].itemsize // 16 > 2048
+    test_compact(rt, kind, 3, 5, Dh, 300, n, a_max)
+
+
 def test_compact_leaves_what_is_outside(rt):
     """Slots past the cache and path entries outside the tree stay where they are."""
     g = gen(6)
