@@ -450,6 +450,39 @@ def test_caches_past_32_bits(rt):
     assert torch.equal(bits(window.k), bits((k[:, :, cap - 9:].float() * scales[0][:, :, cap - 9:, None]).bfloat16()))
 
 
+@pytest.mark.parametrize("kind", ["int8", "bf16"])
+def test_slots_of_a_head_past_32_bits(rt, kind):
+    """Slots of one head whose elements lie past 2^31: append, conversion either way and a path there."""
+    g = gen(10)
+    cap, Dh = 8_400_000, 256                             # 2.15e9 elements a head
+    caches = {k: rt.KVCache.zeros(1, 1, cap, Dh, DT[k]) for k in ("int8", "bf16")}
+    cache, other = caches[kind], caches["bf16" if kind == "int8" else "int8"]
+    L = cap - 9
+    x, y = normal(g, "bf16", 1, 8, 1, Dh), normal(g, "bf16", 1, 8, 1, Dh)
+    freq, _ = rt.rope_freqs(Dh)
+    print(f"far slots {kind}", flush=True)
+    rt.norm_rope_append(x, x, y, torch.zeros(1, 8, dtype=torch.int32, device="cuda"), i32([L]), i32([8]), freq, cache)
+    for t, c, scale in ((x, cache.k, cache.k_scale), (y, cache.v, cache.v_scale)):
+        rows = t[0].transpose(0, 1)
+        if kind == "int8":
+            want, by = codes_of(rows.double(), "int8")
+            assert torch.equal(c[0, :, L: L + 8].float(), want.float()) and torch.equal(scale[0, :, L: L + 8], by)
+        else:
+            assert torch.equal(bits(c[0, :, L: L + 8]), bits(rows))
+        assert not c[0, :, L - 3: L].any() and not c[0, :, L + 8:].any() and not c[0, :, :8].any()
+    was = cache.v[:, :, L:].clone()
+    rt.cache_compact(cache, i32([L]), i32([[0, 3, 7]]), i32([2]), 2)
+    assert torch.equal(cache.v[:, :, L + 1], was[:, :, 3]) and torch.equal(cache.v[:, :, L + 2], was[:, :, 7])
+    rt.cache_convert(cache, other, i32([9]), 9, i32([L]), i32([L]))
+    for c, d, cs, ds in ((cache.k, other.k, cache.k_scale, other.k_scale), (cache.v, other.v, cache.v_scale, other.v_scale)):
+        if kind == "int8":
+            assert torch.equal(bits(d[:, :, L:]), bits((c[:, :, L:].float() * cs[:, :, L:, None]).bfloat16()))
+        else:
+            want, by = codes_of(c[:, :, L:].double(), "int8")
+            assert torch.equal(d[:, :, L:].float(), want.float()) and torch.equal(ds[:, :, L:], by)
+        assert not d[:, :, :9].any() and not d[:, :, L - 3: L].any()
+
+
 def test_python_checks(rt):
     g = gen(9)
     c8, cb = new_cache(rt, g, "e4m3", 2, 2, 20, 64), new_cache(rt, g, "bf16", 2, 2, 20, 64)
