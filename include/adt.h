@@ -303,10 +303,14 @@ adt_status adt_kv_evict(const void* k_cache, const void* v_cache, const float* w
 
 /* ------------------------------------------------------------------ caches in eight bits
  * A cache whose rows (one slot of one head, Dh values) are held in eight bits with one scale each:
- *   scale = fl32(max |x| / top), top = 127 (ADT_I8) or 448 (ADT_E4M3, OCP e4m3 without infinities);
+ *   scale = fl32(max |x| / top), top = 127 (ADT_I8) or 448 (ADT_E4M3, OCP e4m3 without infinities),
+ *           of rows made in double (keys that are normalised or rotated) with max |x| rounded to fp32 first;
  *   code  = the type's value nearest to fl32(x / scale), ties to even;  value = code * scale.
- * A row of zeros has scale 0 and codes 0; a row with a value that is not finite has scale NaN and
- * codes 0, so what attends to it comes out NaN and nothing else does.
+ * A row of zeros has scale 0 and codes 0; a row with a value that is not finite (in fp32) has scale NaN
+ * and codes 0, so what attends to it comes out NaN and nothing else does.
+ * For plain caches without norms and prefixes adt_rope_append, adt_kv_compact and adt_tree_attn (as many
+ * key-value heads as query heads) do the same: in bf16 adt_rope_append and adt_tree_attn are the faster
+ * ones, in fp32 adt_cache_tree_attn by a factor of several; for long paths adt_kv_compact.
  * adt_kv_cache names a cache of any type; it is read during the call only.  k, v: element (b, h,
  * slot, :) at b * stride_b + h * stride_h + slot * Dh; k_scale, v_scale: fp32, (b, h, slot) at
  * b * scale_b + h * scale_h + slot, NULL for ADT_F32 and ADT_BF16.  stride_h >= cap * Dh and
@@ -329,9 +333,11 @@ typedef struct {
  * type, in one pass: each head's row x of q (k) becomes
  *   y = x * g / sqrt(mean x^2 + eps),  then rotated as by adt_rope_append,
  * g = q_norm (k_norm): fp32 [Dh], or [H][Dh] ([heads][Dh]) where norm_per_head is 1; NULL: that side
- * is not normalised.  eps >= 2^-126.  Values go to the cache as they are.  Keys are made in double up to their
- * rounding into the cache, so that codes are those of the formula; queries in fp32, with their values lessened
- * first where squares, products or sums leave it, so they are infinite where the formula's result is.
+ * is not normalised.  (No mean is taken out and no bias added: models whose norms do that are not
+ * served.)  eps >= 2^-126.  Values go to the cache as they are.  Keys are made in double up to their
+ * rounding into the cache, so that codes are those of the formula; queries in fp32, with their values
+ * lessened first where squares, products or sums leave it, so they are infinite where the formula's
+ * result is.
  * q, k, v, ld*, pos, kv_len, n_rows, freq, gain, rot_dim, layout, n_max, q_out as in
  * adt_rope_append, with B, heads and Dh those of the cache; slots at or past cache->cap are left out
  * (debug builds record it).  cache->type: dtype, or an eight-bit type.  q_out must not overlap q (but
@@ -342,7 +348,7 @@ adt_status adt_norm_rope_append(const void* q, const void* k, const void* v, int
                                 float gain, int32_t rot_dim, int32_t layout, int32_t n_max, int32_t H, int32_t dtype,
                                 void* q_out, const adt_kv_cache* cache /*[host]*/, void* stream);
 
-/* Slots from a cache of eight bits to a plain one (read back: value = code * scale, rounded once) or
+/* Slots from a cache of eight bits to a plain one (read back: code * scale in fp32, rounded to bf16 then) or
  * from a plain cache to one of eight bits: of every head, slot src_start[b] + i to slot dst_start[b] +
  * i, i < length[b]; n_max bounds length (host).  Starts NULL: 0.  Other slots stay as they are; slots
  * outside either cache are left out (debug builds record it).  Exactly one of the two is eight-bit
@@ -375,10 +381,12 @@ adt_status adt_cache_compact(const adt_kv_cache* cache /*[host]*/, const int32_t
  *   (ADT_E_ARG where they overlap otherwise).
  * dtype ADT_BF16: cache type ADT_BF16, ADT_E4M3 or ADT_I8; ADT_F32: ADT_F32 (else ADT_E_UNSUPPORTED).
  *   bf16 multiplies codes as they are (bf16 holds them exactly) and applies the scales to scores and
- *   probabilities in fp32; softmax sums and outputs are fp32.  A row whose weighted values add up to more
- *   than fp32 holds (values past 2^120, or past 2^128 over their number) is made again with smaller
- *   weights, far slower, so that its mean is right; not so where a value that it sees is not finite: then
- *   such sums are not finite either, unless out is q.
+ *   probabilities in fp32; softmax sums and outputs are fp32, probabilities (times the scales of the
+ *   values) enter their product rounded to bf16.  Where the product of a query and a key (over codes:
+ *   before its scale) passes fp32's largest value, the row is NaN.  A row whose weighted values add up to
+ *   more than fp32 holds (values past 2^120, or past 2^128 over their number) is made again with smaller
+ *   weights, far slower, so that its mean is right; not so where a value that it sees is not finite:
+ *   then such sums are not finite either, unless out is q.
  * workspace: adt_cache_tree_attn_workspace_size() bytes (groups = 0: no prefix; 0 where none is
  *   needed, and for sizes past the limits that follow), 16-byte aligned.  The size for some kv_cap and
  *   prefix_cap holds for smaller ones too, and without the prefix.  Dh 64 or 128, H a multiple

@@ -16,10 +16,11 @@
 //
 // What bounds it, measured (attention + merge; a 4 GiB copy moves 4.68 TB/s, an 8192-cubed bf16 product
 // 1242 TFLOP/s): one row of 32 heads on 8 over 65333 int8 slots 36 + 5.2 us, 3.8 TB/s of codes; sixteen ragged
-// trees of up to 61 rows of 32 heads over 512 to 2400 e4m3 slots 55-66 us, behind one prefix of 2100 bf16 slots
-// 58 + 8.5; one row of each of 64 sequences behind 32700 int8 slots 70 + 7.8: those with many rows for a key spend their
-// time on the vector instructions of the softmax and of turning codes into bf16, which overlap the
-// matrix products of another wave only in part; 17 rows over 300 slots 7.8, latency.
+// trees of up to 61 rows of 32 heads over 512 to 2400 e4m3 slots 57-68 us, behind one prefix of 2100 bf16 slots
+// 58 + 8.6; one row of each of 64 sequences behind 32700 int8 slots 71 + 7.4: in those with many rows for a key a CU
+// holds waves for 66-74 % of the launch, as workgroups are uneven, and within that time the matrix products (14-21 % of
+// the launch) and the vector instructions of the softmax and of turning codes into bf16 (26-35 %) overlap only
+// in part; 17 rows over 300 slots 7.9, latency.
 #include <algorithm>
 #include <cstddef>
 
@@ -484,6 +485,8 @@ __device__ __forceinline__ void take_steps(RowTile<DH>& t, float scale_log2, K k
           x[n][4 * c + e] = WHOLE || (seen[n] >> 4 * s >> (8 * c + e) & 1) ? x[n][4 * c + e] * by[e] : 0.f;
       }
     }
+    // (rounded to bf16 for the product, as no other operand enters it: 2^-9 of a weight at most, results 0.0024 of
+    // their size from 64 bits where the output's own rounding leaves 0.0017; the sum of weights is not rounded)
     bf16x8 pb[2];
 #pragma unroll
     for (int e = 0; e < 16; ++e) pb[e / 8][e % 8] = (__bf16)x[n][e];

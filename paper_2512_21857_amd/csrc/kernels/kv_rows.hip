@@ -7,9 +7,9 @@
 // are a few lane exchanges away and every access is whole lines.
 //
 // Measured (a 4 GiB copy reads and writes 4.68 TB/s): 4001 rows of 32 query and 8 + 8 key and value heads
-// of 128 dims into int8, half of each head rotated, 28.9 us (3.1 TB/s); 61 rows of 32 heads into e4m3 6.0 us (latency);
+// of 128 dims into int8, half of each head rotated, 26.9 us (3.3 TB/s); 61 rows of 32 heads into e4m3 5.7 us (latency);
 // sixteen e4m3 caches of 512 to 4096 slots of 8 heads read back 48-52 us (a copy's rate); 1100 slots of 32
-// heads put in int8 11.9 us (2.3 TB/s), read back 6.9 (4.0); 12 rows of each of 1024 slices moved 4.9 us (latency).
+// heads put in int8 12 us (2.3 TB/s), read back 7.0 (3.9); 12 rows of each of 1024 slices moved 4.9 us (latency).
 #include <algorithm>
 
 #include "../eight_bit.h"
@@ -332,9 +332,9 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
 }
 
 // Rows from which on they go two to a workgroup.  One, two and four to a workgroup, 32 + 8 + 8 heads of 128
-// dims into int8, rotated in halves: 1000 rows 12.3, 15.1, 20.6 us; 1536 18.6, 17.1; 4001 36.8, 32.4, 40.6; 8000 68.6, 59.8,
-// 65.0; half of each head in neighbouring pairs: 1250 rows 13.2, 15.2; 1536 16.0, 16.2; 1750 18.7, 17.8; fp32 into
-// fp32: 1250 17.5, 19.7; 1750 24.2, 21.6; 4001 45.3, 38.4, 36.1.  (Four hold so many registers that few
+// dims into int8, rotated in halves: 1000 rows 11.8, 13.3, 18.8 us; 1536 16.8, 15.1; 4001 35.4, 29.9, 38.2; 8000 64.8, 53.7,
+// 58.7; half of each head in neighbouring pairs: 1250 rows 11.5, 12.8; 1536 13.2, 13.8; 1750 16.9, 15.3; fp32 into
+// fp32: 1250 17.7, 19.3; 1750 24.9, 20.9; 4001 45.7, 38.7, 35.7.  (Four hold so many registers that few
 // workgroups share a CU.)
 constexpr int KR_MANY = 1536;
 
