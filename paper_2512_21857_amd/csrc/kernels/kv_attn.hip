@@ -177,8 +177,9 @@ __device__ __forceinline__ float part_weight(float m, float l, float M) {
 // Weighted values may add up to more than fp32 holds where it holds their mean: values past 2^120, or past 2^128 over
 // their number.  The output is then not finite though the sum of weights is, which every row is tested for where its
 // output is written; such a row is made again: by a wave, from all its keys, with weights of 2^-34 at most, so that
-// 2^32 of them keep the sum of the largest values below 2^126.  (Far slower, and by one code for all types.)  Where
-// a value that the row sees is not finite itself, its outputs stay as they are.
+// 2^32 of them keep the sum of the largest values below 2^126.  (Far slower: a 61-row tree of 32 heads over 2300 bf16
+// slots 0.9 ms in place of 22 us, one row over 65333 16 ms in place of 67 us.)  Where a value that the row sees is not
+// finite itself, its outputs stay as they are.
 
 // Whether any of N times four outputs is not finite, though the sum of weights l is.
 template <int N>
@@ -191,12 +192,26 @@ __device__ __forceinline__ bool left_fp32(const f32x4 (&o)[N], float l) {
   const float sum = (x[0] + x[1]) + (x[2] + x[3]);        // 0, or NaN
   return sum != sum && !not_finite(l);
 }
-__device__ __forceinline__ float element(int type, const void* p, int64_t i) {
-  if (type == ADT_F32) return ((const float*)p)[i];
-  if (type == ADT_BF16) return bf2f(((const uint16_t*)p)[i]);
-  const uint8_t x = ((const uint8_t*)p)[i];
-  return type == ADT_E4M3 ? decode4<E4M3>(x).x : decode4<I8>(x).x;
-}
+// The values of a lane's piece of a row: 16 bytes, or eight codes.
+template <typename C>
+constexpr int PIECE = sizeof(C) == 4 ? 4 : 8;
+template <typename C>
+struct alignas(PIECE<C> * sizeof(C)) Piece {
+  uint32_t w[PIECE<C> * sizeof(C) / 4];
+  __device__ __forceinline__ void values(float (&f)[PIECE<C>]) const {
+#pragma unroll
+    for (int i = 0; i < PIECE<C> * (int)sizeof(C) / 4; ++i) {
+      if constexpr (EIGHT<C>) {
+        const float4 x = decode4<C>(w[i]);
+        f[4 * i] = x.x, f[4 * i + 1] = x.y, f[4 * i + 2] = x.z, f[4 * i + 3] = x.w;
+      } else if constexpr (sizeof(C) == 2) {
+        f[2 * i] = __uint_as_float(w[i] << 16), f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      } else {
+        f[i] = __uint_as_float(w[i]);
+      }
+    }
+  }
+};
 // Whether any element in 16 bytes is not finite.
 __device__ __forceinline__ bool odd_elements(int type, u32x4 w) {
   bool odd = false;
@@ -287,13 +302,17 @@ __device__ __forceinline__ bool odd_for_all(int b, int h) {
   }
   return false;
 }
-// Row `row` (node and head of the group) of sequence b; all lanes of the wave take part.  Its outputs are written before,
-// unless they are its queries.
+// Row `row` (node and head of the group) of sequence b; all lanes of the wave take part: a group of lanes a key, a piece
+// of it each, AT_ONCE keys in flight; the groups, whose sums are their own, meet at the end.  Outputs are written
+// before, unless they are the queries.
+template <typename C, int AT_ONCE = 4>
 __device__ __forceinline__ void row_again(int b, int h, int row) {
+  typedef std::conditional_t<sizeof(C) == 4, float, uint16_t> T;
+  constexpr int EPL = PIECE<C>;
   const Anew n;
   const KvAttn& a = n.a;
-  const int lane = n.lane, rows_type = a.type == ADT_F32 ? ADT_F32 : ADT_BF16;
-  const int64_t at = RowAt{b, row / a.G, row % a.G}.q(a, h);
+  const int per = a.Dh / EPL, groups = WAVE / per, group = n.lane / per, dim = n.lane % per * EPL;
+  const int64_t at = RowAt{b, row / a.G, row % a.G}.q(a, h) + dim;
   const uint64_t* mask = a.mask + ((int64_t)b * a.nq_max + row / a.G) * ADT_MASK_WORDS;
   auto sees = [&](const Keys& k, int64_t key) {
     const int64_t t = key - k.L;
@@ -303,46 +322,64 @@ __device__ __forceinline__ void row_again(int b, int h, int row) {
     const Keys k(n, true, b, h);
     if (odd_values(n, k, k.L, k.total, [&](int64_t key) { return sees(k, key); })) return;
   }
-  float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};            // of dims lane and lane + 64
+  const float scale_log2 = a.scale * LOG2E;
+  float q[EPL], o[EPL], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) {
+    q[e] = Elem<T>::load((const T*)a.q, at + e);
+    o[e] = 0.f;
+  }
 #pragma unroll 1
   for (int own = a.groups ? 0 : 1; own < 2; ++own) {
     const Keys p(n, own, b, h);
 #pragma unroll 1
-    for (int64_t key0 = 0; key0 < p.total; key0 += WAVE) {
-      const int64_t key = key0 + lane;
-      const bool seen = sees(p, key);
-      float x = -INFINITY, by = 1.f;
-      if (seen) {
-        x = 0.f;
-#pragma unroll 1
-        for (int d = 0; d < a.Dh; ++d) x = fmaf(element(rows_type, a.q, at + d), element(a.type, p.k, p.base + key * a.Dh + d), x);
-        x *= a.scale * LOG2E;
-        if (p.ks) x *= p.ks[p.scales + key], by = p.vs[p.scales + key];
+    for (int64_t key0 = group; key0 - group < p.total; key0 += groups * AT_ONCE) {
+      Piece<C> kr[AT_ONCE], vr[AT_ONCE];
+      float by_k[AT_ONCE], by_v[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int64_t key = min(key0 + i * groups, (int64_t)p.total - 1), from = p.base + key * a.Dh + dim;
+        kr[i] = *reinterpret_cast<const Piece<C>*>((const C*)p.k + from);
+        vr[i] = *reinterpret_cast<const Piece<C>*>((const C*)p.v + from);
+        by_k[i] = EIGHT<C> ? p.ks[p.scales + key] * scale_log2 : scale_log2;
+        by_v[i] = EIGHT<C> ? p.vs[p.scales + key] : 1.f;
       }
-      const float top = fmaxf(m, wave_max(x)), ref = top == -INFINITY ? 0.f : top, down = top == m ? 1.f : exp2_hw(m - ref);
-      const float w = seen ? exp2_hw(x - ref) * 0x1p-34f : 0.f;
-      m = top;
-      l = l * down + w;
-      o[0] *= down;
-      o[1] *= down;
-#pragma unroll 1
-      for (int k = 0; k < WAVE; ++k) {
-        if (!__builtin_amdgcn_readlane(seen, k)) continue;
-        const float wk = __shfl(w * by, k, WAVE);
-        const int64_t v = p.base + (key0 + k) * a.Dh + lane;
-        o[0] += wk * element(a.type, p.v, v);
-        if (a.Dh > WAVE) o[1] += wk * element(a.type, p.v, v + WAVE);
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const bool seen = sees(p, key0 + i * groups);
+        float f[EPL], x = 0.f;
+        kr[i].values(f);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) x = fmaf(q[e], f[e], x);
+        for (int k = per / 2; k >= 1; k /= 2) x += __shfl_xor(x, k, WAVE);
+        x = seen ? x * by_k[i] : -INFINITY;
+        const float top = fmaxf(m, x), ref = top == -INFINITY ? 0.f : top, down = top == m ? 1.f : exp2_hw(m - ref);
+        const float w = seen ? exp2_hw(x - ref) * 0x1p-34f : 0.f, by = seen ? w * by_v[i] : 0.f;
+        m = top;
+        l = l * down + w;
+        vr[i].values(f);
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) o[e] = o[e] * down + (seen ? by * f[e] : 0.f);
       }
     }
   }
-  l = wave_sum(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l, most = a.type == ADT_F32 ? 3.402823466e38f : 3.389531389e38f;
-  for (int c = 0; c < a.Dh / WAVE; ++c) {
+  float M = m;
+  for (int k = per; k < WAVE; k *= 2) M = fmaxf(M, __shfl_xor(M, k, WAVE));
+  const float weight = part_weight(m, l, M);
+  auto sum = [&](float x) {
+    x *= weight;
+    for (int k = per; k < WAVE; k *= 2) x += __shfl_xor(x, k, WAVE);
+    return x;
+  };
+  l = sum(l);
+  const float inv = l == 0.f ? 0.f : 1.f / l, most = sizeof(T) == 4 ? 3.402823466e38f : 3.389531389e38f;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) {
     // (a mean of finite values is: where a rounding takes it past the type's largest, it is that)
-    float y = o[c] * inv;
-    if (fabsf(y) > most && !not_finite(o[c])) y = copysignf(most, y);
-    if (a.type == ADT_F32) Elem<float>::store((float*)a.out, at + lane + c * WAVE, y);
-    else Elem<uint16_t>::store((uint16_t*)a.out, at + lane + c * WAVE, y);
+    const float s = sum(o[e]);
+    float y = s * inv;
+    if (fabsf(y) > most && !not_finite(s)) y = copysignf(most, y);
+    if (group == 0) Elem<T>::store((T*)a.out, at + e, y);
   }
 }
 // Of a wave whose rows have `per` neighbouring lanes each: the lanes of those rows of which one says so.
@@ -354,9 +391,9 @@ __device__ __forceinline__ uint64_t rows_lanes(bool left, int per) {
   return all;
 }
 
-// Makes the rows of sets of such lanes again; row_of(set, lane): the row.
-template <int N, class F>
-__device__ __forceinline__ void lanes_again(const uint64_t (&sets)[N], int b, int h, F row_of, int per) {
+// Makes the rows of sets of such lanes again; row_of(set, lane): the row.  T: the rows' type.
+template <typename T, int N, class F>
+__device__ __forceinline__ void lanes_again(const uint64_t (&sets)[N], int type, int b, int h, F row_of, int per) {
   uint64_t any = 0;
 #pragma unroll
   for (int y = 0; y < N; ++y) any |= sets[y];
@@ -370,7 +407,12 @@ __device__ __forceinline__ void lanes_again(const uint64_t (&sets)[N], int b, in
     for (int z = 1; z < N; ++z) lanes = y == z ? sets[z] : lanes;
 #pragma unroll 1
     for (int i = 0; i < WAVE; i += per)
-      if (lanes >> i & 1) row_again(b, h, row_of(y, i));
+      if (lanes >> i & 1) {
+        if constexpr (sizeof(T) == 4) row_again<float, 2>(b, h, row_of(y, i));
+        else if (type == ADT_BF16) row_again<uint16_t, 2>(b, h, row_of(y, i));
+        else if (type == ADT_E4M3) row_again<E4M3, 2>(b, h, row_of(y, i));
+        else row_again<I8, 2>(b, h, row_of(y, i));
+      }
   }
 }
 
@@ -1012,7 +1054,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_kernel(KvAttn a, KvPlan
   const int wave = threadIdx.x / WAVE, row0 = j.r0 + wave % tiles * 32;
 #pragma unroll 1
   for (int i = tiles == 1 ? wave : 0; i < 32; i += tiles == 1 ? KA_WAVES : 1)
-    if (which >> i & 1) row_again(j.b, j.h, row0 + i);
+    if (which >> i & 1) row_again<C>(j.b, j.h, row0 + i);
 }
 
 // ---------------------------------------------------------------------------- fp32 rows
@@ -1223,7 +1265,7 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
       }
     }
   }
-  lanes_again(again, j.b, j.h, [&](int y, int i) { return j.r0 + y / SETS * 16 + (y % SETS * KA_THREADS + wave * WAVE + i) / (DH / 4); },
+  lanes_again<float>(again, a.type, j.b, j.h, [&](int y, int i) { return j.r0 + y / SETS * 16 + (y % SETS * KA_THREADS + wave * WAVE + i) / (DH / 4); },
               DH / 4);
 }
 
@@ -1231,8 +1273,9 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
 // A row's parts, own splits then the prefix's, in that order: DH / 4 threads take four dims each.  Many
 // rows: ROWS of them a thread, two parts of each requested at a time.  Few rows of many parts (ROWS = 1):
 // `count` groups of threads deal out the parts, and their sums meet in LDS, in their order.
+// (The bound on registers is what the merge needs: rows that are made again, two keys at once, fit it.)
 template <typename T, int KT, int ROWS>
-__global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p, int count, const float* __restrict__ part_o,
+__global__ __launch_bounds__(KA_THREADS, ROWS == 1 ? 6 : 5) void kv_merge_kernel(KvAttn a, KvPlan p, int count, const float* __restrict__ part_o,
                                                               const float* __restrict__ part_ml) {
   __shared__ f32x4 so[ROWS == 1 ? KA_THREADS : 1];
   __shared__ float2 sml[ROWS == 1 ? KA_THREADS : 1];
@@ -1310,7 +1353,7 @@ __global__ __launch_bounds__(KA_THREADS) void kv_merge_kernel(KvAttn a, KvPlan p
     const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
     store4((T*)a.out + RowAt{b, row / a.G, row % a.G}.q(a, h) + d, o[r][0] * inv, o[r][1] * inv, o[r][2] * inv, o[r][3] * inv);
   }
-  lanes_again(again, b, h, [&](int r, int i) { return __builtin_amdgcn_readlane(row0, i) + r * fit; }, per);
+  lanes_again<T>(again, a.type, b, h, [&](int r, int i) { return __builtin_amdgcn_readlane(row0, i) + r * fit; }, per);
 }
 
 // ---------------------------------------------------------------------------- host
