@@ -270,12 +270,20 @@ __global__ __launch_bounds__(KR_THREADS) void norm_rope_kernel(NormRopeRows a, i
         again = odd != odd;
       }
       if (again) {
-        // Squares, or products with gains and turns, left fp32: the row's factor comes before those, and values whose
-        // squares are too large, or that have no factor, are made 2^70 times smaller first.
-        const float unit = norm && !past ? 1.f : 0x1p-70f;
-        float inv = 1.f;
-        if (norm) inv = factor(past ? squares(unit, mine) : ss, unit);
-        turned(mine, mates, r, unit, inv, norm ? 1.f : 0x1p70f, y);
+        // Squares, or products with gains and turns, left fp32: the row's factor comes before those.  Values whose squares
+        // are too large are made 2^70 times smaller for them, and half of that goes to the factor, so that neither they nor it
+        // leave fp32 at its lower end; values that have no factor are made as much smaller until the end.
+        float first = 1.f, second = 1.f;
+        if (!norm) first = 0x1p-70f;
+        else if (past) first = 0x1p-35f, second = 0x1p-35f * factor(squares(0x1p-70f, mine), 0x1p-70f);
+        else second = factor(ss, 1.f);
+        // (a value that was finite stays: what is small beside a large one would be lost)
+        float z[N][VEC];
+        turned(mine, mates, r, first, second, norm ? 1.f : 0x1p70f, z);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) y[j][e] = past || !(fabsf(y[j][e]) <= 3.402823466e38f) ? z[j][e] : y[j][e];
       }
     }
     store(y);

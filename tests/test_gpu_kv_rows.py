@@ -259,13 +259,16 @@ def test_append_large_queries(rt):
 
 
 def expect_queries(out, want, length, dtype):
-    """Queries are the formula's to the roundings counted above; past the type's largest value they are infinite."""
+    """Queries are the formula's to the roundings counted above; past the type's largest value they are infinite.  Below the
+    smallest normal value, 2^-126, a rounding is off by half the smallest step whatever the size: 2^-134 the output's in
+    bf16; 2^-150 each of up to 16 in fp32, which gains of up to 3 and two terms of a pair carry on: 2^-143."""
+    least = (2.0 ** -134 if dtype == "bf16" else 0.0) + 2.0 ** -143
     most = torch.finfo(DT[dtype]).max
     got = out.double()
     past = want.abs() > 1.01 * most
     assert torch.equal(got[past], torch.sign(want[past]) * math.inf)
     inside = want.abs() < 0.99 * most
-    assert torch.all(((got - want).abs() <= STEP[dtype] * want.abs() + 2.0 ** -20 * length)[inside])
+    assert torch.all(((got - want).abs() <= STEP[dtype] * want.abs() + 2.0 ** -20 * length + least)[inside])
 
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
@@ -293,11 +296,42 @@ def test_append_queries_at_the_end_of_fp32(rt, dtype, layout, B, Dh, rot):
         kn = None if w is None else torch.ones(Hkv, Dh, device="cuda") if w.dim() == 2 else w
         out = rt.norm_rope_append(q, kv, kv, pos, L, rows, freq, cache, q_norm=w, k_norm=kn, eps=eps, layout=layout, gain=gain)
         expect_queries(out, *made(q, w, eps, pos, freq, gain, layout), dtype)
+    # small values of rows whose squares leave fp32
+    few = 2.0 ** 66 * normal(g, dtype, B, n, H, Dh)
+    few[..., 1::2] *= 2.0 ** -119                          # normalised some 2^-119, beside 1
+    out = rt.norm_rope_append(few, kv, kv, pos, L, rows, freq, new_cache(rt, g, dtype, B, Hkv, n, Dh), q_norm=shared, eps=eps, layout=layout)
+    expect_queries(out, *made(few, shared, eps, pos, freq, 1.0, layout), dtype)
     # gains so large that a value times them leaves fp32, and the row's factor brings it back
     w = torch.full((Dh,), 2.0 ** 70, device="cuda")
     q = 2.0 ** 60 * normal(g, dtype, B, n, H, Dh)
     out = rt.norm_rope_append(q, kv, kv, pos, L, rows, freq, cache, q_norm=w, eps=eps, layout=layout)
     expect_queries(out, *made(q, w, eps, pos, freq, 1.0, layout), dtype)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_small_queries_beside_large_ones(rt, dtype, layout):
+    """A pair whose sum leaves fp32 changes nothing of the pairs beside it, however small they are."""
+    print(f"append small beside large {dtype} {layout}", flush=True)
+    for Dh, rot in ((64, 64), (128, 48), (30, 10)):
+        g = gen(22)
+        q = 1e-30 * (1.0 + torch.rand(1, 40, 4, Dh, device="cuda", generator=g))
+        a, b = (0, rot // 2) if layout == "half" else (0, 1)
+        q[..., a], q[..., b] = 3.3e38, -3.3e38
+        q[0, ::5, :, Dh - 1] = math.inf
+        q = q.to(DT[dtype])
+        kv = normal(g, dtype, 1, 40, 1, Dh)
+        pos = torch.arange(40, dtype=torch.int32, device="cuda")[None]
+        freq, _ = rt.rope_freqs(rot)
+        cache = new_cache(rt, g, dtype, 1, 1, 40, Dh)
+        out = rt.norm_rope_append(q, kv, kv, pos, i32([0]), i32([40]), freq, cache, layout=layout, gain=1.5)
+        finite = q.double()
+        finite[torch.isinf(finite)] = 0.0
+        want, length = made(finite, None, 0.0, pos, freq, 1.5, layout)
+        keep = torch.ones(Dh, dtype=torch.bool, device="cuda")
+        keep[[a, b, Dh - 1] + ([Dh // 2 - 1] if layout == "half" and rot == Dh else [Dh - 2])] = False      # (and the infinite ones' mates)
+        expect_queries(out[..., keep], want[..., keep], length[..., keep], dtype)
+        expect_queries(out[:, 1::5], want[:, 1::5], length[:, 1::5], dtype)
 
 
 # ---------------------------------------------------------------------------- conversion
