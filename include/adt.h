@@ -384,8 +384,8 @@ adt_status adt_cache_compact(const adt_kv_cache* cache /*[host]*/, const int32_t
  *   probabilities in fp32; softmax sums and outputs are fp32, probabilities (times the scales of the
  *   values) enter their product rounded to bf16.  Where the product of a query and a key (over codes:
  *   before its scale) passes fp32's largest value, the row is NaN.  A row whose weighted values add up to
- *   more than fp32 holds (values past 2^120, or past 2^128 over their number) is made again with smaller
- *   weights, far slower, so that its mean is right; not so where a value that it sees is not finite:
+ *   more than fp32 holds (values past 2^120, or past 2^128 over their number) is made again with sums in
+ *   double, far slower, so that its mean is right; not so where a value that it sees is not finite:
  *   then such sums are not finite either, unless out is q.
  * workspace: adt_cache_tree_attn_workspace_size() bytes (groups = 0: no prefix; 0 where none is
  *   needed, and for sizes past the limits that follow), 16-byte aligned.  The size for some kv_cap and

@@ -176,10 +176,9 @@ __device__ __forceinline__ float part_weight(float m, float l, float M) {
 // ---------------------------------------------------------------------------- rows that left fp32
 // Weighted values may add up to more than fp32 holds where it holds their mean: values past 2^120, or past 2^128 over
 // their number.  The output is then not finite though the sum of weights is, which every row is tested for where its
-// output is written; such a row is made again: by a wave, from all its keys, with weights of 2^-34 at most, so that
-// 2^32 of them keep the sum of the largest values below 2^126.  (Far slower: a 61-row tree of 32 heads over 2300 bf16
-// slots 0.9 ms in place of 22 us, one row over 65333 16 ms in place of 67 us.)  Where a value that the row sees is not
-// finite itself, its outputs stay as they are.
+// output is written; such a row is made again: by a wave, from all its keys, with sums in double.  (Far slower: a 61-row
+// tree of 32 heads over 2300 bf16 slots 0.9 ms in place of 22 us, one row over 65333 17 ms in place of 67 us.)  Where a
+// value that the row sees is not finite itself, its outputs stay as they are.
 
 // Whether any of N times four outputs is not finite, though the sum of weights l is.
 template <int N>
@@ -323,11 +322,12 @@ __device__ __forceinline__ void row_again(int b, int h, int row) {
     if (odd_values(n, k, k.L, k.total, [&](int64_t key) { return sees(k, key); })) return;
   }
   const float scale_log2 = a.scale * LOG2E;
-  float q[EPL], o[EPL], m = -INFINITY, l = 0.f;
+  float q[EPL], m = -INFINITY;
+  double o[EPL], l = 0.0;
 #pragma unroll
   for (int e = 0; e < EPL; ++e) {
     q[e] = Elem<T>::load((const T*)a.q, at + e);
-    o[e] = 0.f;
+    o[e] = 0.0;
   }
 #pragma unroll 1
   for (int own = a.groups ? 0 : 1; own < 2; ++own) {
@@ -354,31 +354,32 @@ __device__ __forceinline__ void row_again(int b, int h, int row) {
         for (int k = per / 2; k >= 1; k /= 2) x += __shfl_xor(x, k, WAVE);
         x = seen ? x * by_k[i] : -INFINITY;
         const float top = fmaxf(m, x), ref = top == -INFINITY ? 0.f : top, down = top == m ? 1.f : exp2_hw(m - ref);
-        const float w = seen ? exp2_hw(x - ref) * 0x1p-34f : 0.f, by = seen ? w * by_v[i] : 0.f;
+        const double w = seen ? (double)exp2_hw(x - ref) : 0.0, by = seen ? w * (double)by_v[i] : 0.0;
         m = top;
-        l = l * down + w;
+        l = l * (double)down + w;
         vr[i].values(f);
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) o[e] = o[e] * down + (seen ? by * f[e] : 0.f);
+        for (int e = 0; e < EPL; ++e) o[e] = o[e] * (double)down + (seen ? by * (double)f[e] : 0.0);
       }
     }
   }
   float M = m;
   for (int k = per; k < WAVE; k *= 2) M = fmaxf(M, __shfl_xor(M, k, WAVE));
-  const float weight = part_weight(m, l, M);
-  auto sum = [&](float x) {
+  const double weight = (double)part_weight(m, (float)l, M);
+  auto sum = [&](double x) {
     x *= weight;
     for (int k = per; k < WAVE; k *= 2) x += __shfl_xor(x, k, WAVE);
     return x;
   };
   l = sum(l);
-  const float inv = l == 0.f ? 0.f : 1.f / l, most = sizeof(T) == 4 ? 3.402823466e38f : 3.389531389e38f;
+  const double inv = l == 0.0 ? 0.0 : 1.0 / l;
+  const float most = sizeof(T) == 4 ? 3.402823466e38f : 3.389531389e38f;
 #pragma unroll
   for (int e = 0; e < EPL; ++e) {
     // (a mean of finite values is: where a rounding takes it past the type's largest, it is that)
-    const float s = sum(o[e]);
-    float y = s * inv;
-    if (fabsf(y) > most && !not_finite(s)) y = copysignf(most, y);
+    const double s = sum(o[e]);
+    float y = (float)(s * inv);
+    if (fabsf(y) > most && fabs(s) < (double)INFINITY) y = copysignf(most, y);
     if (group == 0) Elem<T>::store((T*)a.out, at + e, y);
   }
 }
@@ -1273,9 +1274,9 @@ __global__ __launch_bounds__(KA_THREADS, 2) void kv_attn_f32_kernel(KvAttn a, Kv
 // A row's parts, own splits then the prefix's, in that order: DH / 4 threads take four dims each.  Many
 // rows: ROWS of them a thread, two parts of each requested at a time.  Few rows of many parts (ROWS = 1):
 // `count` groups of threads deal out the parts, and their sums meet in LDS, in their order.
-// (The bound on registers is what the merge needs: rows that are made again, two keys at once, fit it.)
+// (Five waves a SIMD are what the four-row form needs; rows that are made again, two keys at once, fit that.)
 template <typename T, int KT, int ROWS>
-__global__ __launch_bounds__(KA_THREADS, ROWS == 1 ? 6 : 5) void kv_merge_kernel(KvAttn a, KvPlan p, int count, const float* __restrict__ part_o,
+__global__ __launch_bounds__(KA_THREADS, 5) void kv_merge_kernel(KvAttn a, KvPlan p, int count, const float* __restrict__ part_o,
                                                               const float* __restrict__ part_ml) {
   __shared__ f32x4 so[ROWS == 1 ? KA_THREADS : 1];
   __shared__ float2 sml[ROWS == 1 ? KA_THREADS : 1];

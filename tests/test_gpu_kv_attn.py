@@ -470,6 +470,26 @@ def test_values_at_the_end_of_fp32(rt, kind, H, Hkv, Dh, n, L, P):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("n,L,P", [(3, [300], None), (40, [70], None), (4, [5000], None), (40, [70, 33], [700])])
+def test_small_values_beside_the_largest(rt, kind, n, L, P):
+    """Dims of small values beside dims whose sums leave fp32."""
+    print(f"small beside large {kind} n={n} L={L} P={P}", flush=True)
+    c = Case(rt, kind, 4, 2, 64, n, L, P=P, seed=9)
+    few_bits(c, 1, 3e38)
+    for t in [c.t] + ([c.pt] if P else []):
+        t[1][..., ::3] *= 2.0 ** -119
+        t[1][..., ::3] *= 2.0 ** -119                       # (some 2^-110)
+        assert t[1][..., ::3].any()
+    out = c.check(rt)
+    for b in range(c.B):
+        for h in range(2):
+            want, tol = c.reference(b, h)
+            got = out[b, : c.rows[b], 2 * h: 2 * h + 2].double()
+            # (without the allowance for what is far below 1)
+            assert torch.all(((got - want).abs() <= tol - 1e-30 + 2.0 ** -149)[..., ::3])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_the_largest_values(rt, kind):
     """Every value the type's largest: so is every output."""
     print(f"largest values {kind}", flush=True)
